@@ -501,6 +501,169 @@ typedef struct lrnnx_lti_step_args {
 
 int lrnnx_lti_step(const lrnnx_lti_step_args *args);
 
+/* ------------------------------------------------------------------ gated delta rule
+ * A linear RNN whose state is a matrix S [dk,dv] for every head, written by a rank-one correction a step.  With decay
+ * exp(g) (g <= 0 for a decay; -infinity forgets everything), write strength beta, and S_{-1} = s0 or 0:
+ *     S'  = exp(g_t) S_{t-1},   e_t = v_t - S'^T k_t,   S_t = S' + k_t (beta_t e_t)^T,   o_t = scale S_t^T q_t.
+ * q, k: [B,L,Hk,dk], v, o: [B,L,Hv,dv] in io_dtype, g, beta: [B,L,Hv] in gate_dtype (LRNNX_F32, or the I/O type); Hv is a
+ * multiple of Hk, value head h reads key head h / (Hv/Hk).  Tensors take element strides for batch entry, step and head; the
+ * last axis is contiguous (g and beta: any three strides).  Rows of any alignment and width are accepted; bfloat16 rows of
+ * 64 or 128 elements (dk) at 16-byte steps are read in place, others are first copied into the workspace.
+ * s0, s_last: [B,Hv,dk,dv] float, contiguous, optional.  1 <= dk <= 128, 1 <= dv <= 256; B, Hv <= 65535; any L >= 1.
+ * The keys are used as they are: a recurrence with beta |k|^2 > 2 grows, as its definition says.
+ * Packed variable-length batches: with cu_seqlens != NULL (device memory [B+1], ascending) q, k, v, g, beta, o are [L,H,...]
+ * (batch strides ignored) and sequence b is steps cu_seqlens[b] .. cu_seqlens[b+1]-1; s0 and s_last stay [B,Hv,dk,dv].
+ * Boundaries are clamped to [0,L]; steps outside every sequence are neither read as part of one nor written.  The last state
+ * of a sequence without steps is its first.
+ * saved (optional): what lrnnx_gated_delta_bwd needs from this call (states every 64 steps, corrections e, solved matrices),
+ * lrnnx_gated_delta_saved_bytes(args) bytes, opaque, 16-byte aligned, to be handed to the backward call unchanged together
+ * with the same inputs.  workspace: lrnnx_gated_delta_fwd_workspace_bytes(args) bytes, 16-byte aligned.
+ * Accumulation, states and gates are float32; products run on matrix units whose factors are bfloat16 numbers or sums of
+ * two (results rounded to bfloat16) or three (float32 results) of them.  Results are bitwise reproducible.            */
+typedef struct lrnnx_delta_fwd_args {
+    size_t struct_size;
+    int32_t B, Hk, Hv, dk, dv;
+    int32_t io_dtype, gate_dtype;
+    float scale;
+    int64_t L;
+    const int64_t *cu_seqlens;
+    const void *q;      int64_t q_stride_b, q_stride_l, q_stride_h;
+    const void *k;      int64_t k_stride_b, k_stride_l, k_stride_h;
+    const void *v;      int64_t v_stride_b, v_stride_l, v_stride_h;
+    const void *g;      int64_t g_stride_b, g_stride_l, g_stride_h;
+    const void *beta;   int64_t beta_stride_b, beta_stride_l, beta_stride_h;
+    const float *s0;                                               /* [B,Hv,dk,dv] or NULL */
+    void *o;            int64_t o_stride_b, o_stride_l, o_stride_h;
+    float *s_last;                                                 /* [B,Hv,dk,dv] out or NULL */
+    void *saved;        size_t saved_bytes;                        /* out or NULL */
+    void *workspace;    size_t workspace_bytes;
+    void *stream;
+} lrnnx_delta_fwd_args;
+
+int lrnnx_gated_delta_fwd(const lrnnx_delta_fwd_args *args);
+/* Host only; sizes, types, strides, alignment, and which pointers are given decide.  0 for invalid sizes. */
+size_t lrnnx_gated_delta_fwd_workspace_bytes(const lrnnx_delta_fwd_args *args);
+size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *args);
+
+/* Reverse-mode derivative of lrnnx_gated_delta_fwd for upstream gradients dout (of o, strided as o) and, optionally, ds_last
+ * (of s_last): dq, dk [B,L,Hk,dk] (summed over the value heads that share them), dv [B,L,Hv,dv] in io_dtype, dg, dbeta
+ * [B,L,Hv] in gate_dtype, ds0 [B,Hv,dk,dv] float (optional), all contiguous ([L,H,...] for a packed batch; rows of steps
+ * outside every sequence are not written).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
+ * Gradients of g are those of the log decay.  With bfloat16 I/O and float32 gates dg and dbeta are as accurate as
+ * products of factors in 16 bits leave them (about 1e-3 of their norm); ds0 is accurate to float32 if s0 was given.   */
+typedef struct lrnnx_delta_bwd_args {
+    size_t struct_size;
+    int32_t B, Hk, Hv, dk, dv;
+    int32_t io_dtype, gate_dtype;
+    float scale;
+    int64_t L;
+    const int64_t *cu_seqlens;
+    const void *q;      int64_t q_stride_b, q_stride_l, q_stride_h;
+    const void *k;      int64_t k_stride_b, k_stride_l, k_stride_h;
+    const void *v;      int64_t v_stride_b, v_stride_l, v_stride_h;
+    const void *g;      int64_t g_stride_b, g_stride_l, g_stride_h;
+    const void *beta;   int64_t beta_stride_b, beta_stride_l, beta_stride_h;
+    const float *s0;
+    const void *dout;   int64_t dout_stride_b, dout_stride_l, dout_stride_h;
+    const float *ds_last;                                          /* [B,Hv,dk,dv] or NULL */
+    const void *saved;  size_t saved_bytes;
+    void *dq;
+    void *dkey;
+    void *dval;
+    void *dg;
+    void *dbeta;
+    float *ds0;                                                    /* [B,Hv,dk,dv] out or NULL */
+    void *workspace;    size_t workspace_bytes;
+    void *stream;
+} lrnnx_delta_bwd_args;
+
+int lrnnx_gated_delta_bwd(const lrnnx_delta_bwd_args *args);
+size_t lrnnx_gated_delta_bwd_workspace_bytes(const lrnnx_delta_bwd_args *args);
+
+/* One step of it (generation): state [B,Hv,dk,dv] float, updated IN PLACE; q, k [B,Hk,dk], v, o [B,Hv,dv] in io_dtype and
+ * g, beta [B,Hv] in gate_dtype with strides for batch entry and head.  L calls reproduce the forward call on L steps up to
+ * rounding.                                                                                                           */
+typedef struct lrnnx_delta_step_args {
+    size_t struct_size;
+    int32_t B, Hk, Hv, dk, dv;
+    int32_t io_dtype, gate_dtype;
+    float scale;
+    const void *q;      int64_t q_stride_b, q_stride_h;
+    const void *k;      int64_t k_stride_b, k_stride_h;
+    const void *v;      int64_t v_stride_b, v_stride_h;
+    const void *g;      int64_t g_stride_b, g_stride_h;
+    const void *beta;   int64_t beta_stride_b, beta_stride_h;
+    float *state;                                                  /* [B,Hv,dk,dv] in/out, contiguous */
+    void *o;            int64_t o_stride_b, o_stride_h;
+    void *stream;
+} lrnnx_delta_step_args;
+
+int lrnnx_gated_delta_step(const lrnnx_delta_step_args *args);
+
+/* ------------------------------------------------------------------ norms around a block
+ * What lies between the inside of one block and the inside of the next, on M rows of D elements:
+ *     n = x / sqrt(mean(x^2) + eps)          over each of `groups` equal parts of the row, if post_weight is given (else n = x)
+ *     m = post_weight n act(gate)            act: silu (gate_act 0) or sigmoid (1); post_weight and gate optional
+ *     h = residual + res_scale m             residual and res_scale optional
+ *     y = pre_weight h / sqrt(mean(h^2) + eps)   over the row; optional
+ * (the norm and gate of every head's output: groups = heads, nothing after m; a block boundary: groups = 1, residual, the
+ * next block's pre_weight).  x, gate, y in io_dtype, residual and h in res_dtype (LRNNX_F32 or the I/O type; without a
+ * residual res_dtype is that of h); post_weight [D], or [D/groups] if post_shared (one weight for all groups), res_scale and
+ * pre_weight [D] float.  Rows have element strides, h and y are contiguous.  1 <= D <= 8192, D a multiple of groups.
+ * y is formed from h before h is rounded.  h == residual (the same buffer) is allowed.                                 */
+typedef struct lrnnx_norm_fwd_args {
+    size_t struct_size;
+    int64_t M;
+    int32_t D, groups, post_shared, gate_act;
+    int32_t io_dtype, res_dtype;
+    float eps;
+    int32_t reserved;
+    const void *x;          int64_t x_stride;
+    const float *post_weight;
+    const void *gate;       int64_t gate_stride;
+    const void *residual;   int64_t residual_stride;
+    const float *res_scale;
+    const float *pre_weight;
+    void *h;                                                       /* [M,D] out */
+    void *y;                                                       /* [M,D] out; required with pre_weight, else NULL */
+    void *stream;
+} lrnnx_norm_fwd_args;
+
+int lrnnx_block_norm_fwd(const lrnnx_norm_fwd_args *args);
+
+/* Its reverse-mode derivative for upstream gradients dh (res_dtype) and dy (io_dtype; only with pre_weight), either optional.
+ * Everything is formed again from the inputs of the forward call.  dx, dgate [M,D] io_dtype, dresidual [M,D] res_dtype,
+ * dpost_weight, dres_scale, dpre_weight float in the shapes of the weights: each is written if given, and may be NULL
+ * (dx may not); each needs its input.  All contiguous, 16-byte aligned or not.  The weights' gradients are summed in a fixed
+ * order (bitwise reproducible) through the workspace: lrnnx_block_norm_bwd_workspace_bytes(M, D) bytes.                */
+typedef struct lrnnx_norm_bwd_args {
+    size_t struct_size;
+    int64_t M;
+    int32_t D, groups, post_shared, gate_act;
+    int32_t io_dtype, res_dtype;
+    float eps;
+    int32_t reserved;
+    const void *x;          int64_t x_stride;
+    const float *post_weight;
+    const void *gate;       int64_t gate_stride;
+    const void *residual;   int64_t residual_stride;
+    const float *res_scale;
+    const float *pre_weight;
+    const void *dh;         int64_t dh_stride;
+    const void *dy;         int64_t dy_stride;
+    void *dx;
+    void *dgate;
+    void *dresidual;
+    float *dpost_weight;
+    float *dres_scale;
+    float *dpre_weight;
+    void *workspace;        size_t workspace_bytes;
+    void *stream;
+} lrnnx_norm_bwd_args;
+
+int lrnnx_block_norm_bwd(const lrnnx_norm_bwd_args *args);
+size_t lrnnx_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
+
 /* ------------------------------------------------------------------ queries (host only, no GPU needed) */
 typedef enum { LRNNX_WS_FWD = 0, LRNNX_WS_BWD = 1, LRNNX_WS_LTI = 2, LRNNX_WS_LTI_BWD = 3, LRNNX_WS_DIAG = 4,
                LRNNX_WS_DIAG_BWD = 5, LRNNX_WS_BWD_COMPLEX = 6,

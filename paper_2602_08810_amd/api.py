@@ -119,17 +119,59 @@ class LtiStepArgs(ctypes.Structure):
     _fields_ = [("struct_size", _sz), ("B", _i32), ("P", _i32), ("lambda_", _vp), ("x", _vp), ("v", _vp), ("stream", _vp)]
 
 
+def _strided(name, axes):
+    return [(name, _vp)] + [(f"{name}_stride_{x}", _i64) for x in axes]
+
+
+_DELTA_HEAD = [("struct_size", _sz), ("B", _i32), ("Hk", _i32), ("Hv", _i32), ("dk", _i32), ("dv", _i32),
+               ("io_dtype", _i32), ("gate_dtype", _i32), ("scale", ctypes.c_float)]
+_DELTA_INPUTS = [("L", _i64), ("cu_seqlens", _vp), *_strided("q", "blh"), *_strided("k", "blh"), *_strided("v", "blh"),
+                 *_strided("g", "blh"), *_strided("beta", "blh"), ("s0", _vp)]
+_SCRATCH = [("workspace", _vp), ("workspace_bytes", _sz), ("stream", _vp)]
+
+
+class DeltaFwdArgs(ctypes.Structure):             # lrnnx_delta_fwd_args
+    _fields_ = _DELTA_HEAD + _DELTA_INPUTS + _strided("o", "blh") + [("s_last", _vp), ("saved", _vp), ("saved_bytes", _sz)] + _SCRATCH
+
+
+class DeltaBwdArgs(ctypes.Structure):             # lrnnx_delta_bwd_args
+    _fields_ = (_DELTA_HEAD + _DELTA_INPUTS + _strided("dout", "blh") + [("ds_last", _vp), ("saved", _vp), ("saved_bytes", _sz)]
+                + [(n, _vp) for n in ("dq", "dkey", "dval", "dg", "dbeta", "ds0")] + _SCRATCH)
+
+
+class DeltaStepArgs(ctypes.Structure):            # lrnnx_delta_step_args
+    _fields_ = (_DELTA_HEAD + _strided("q", "bh") + _strided("k", "bh") + _strided("v", "bh") + _strided("g", "bh")
+                + _strided("beta", "bh") + [("state", _vp)] + _strided("o", "bh") + [("stream", _vp)])
+
+
+_NORM_HEAD = [("struct_size", _sz), ("M", _i64), ("D", _i32), ("groups", _i32), ("post_shared", _i32), ("gate_act", _i32),
+              ("io_dtype", _i32), ("res_dtype", _i32), ("eps", ctypes.c_float), ("reserved", _i32),
+              ("x", _vp), ("x_stride", _i64), ("post_weight", _vp), ("gate", _vp), ("gate_stride", _i64),
+              ("residual", _vp), ("residual_stride", _i64), ("res_scale", _vp), ("pre_weight", _vp)]
+
+
+class NormFwdArgs(ctypes.Structure):              # lrnnx_norm_fwd_args
+    _fields_ = _NORM_HEAD + [("h", _vp), ("y", _vp), ("stream", _vp)]
+
+
+class NormBwdArgs(ctypes.Structure):              # lrnnx_norm_bwd_args
+    _fields_ = (_NORM_HEAD + [("dh", _vp), ("dh_stride", _i64), ("dy", _vp), ("dy_stride", _i64)]
+                + [(n, _vp) for n in ("dx", "dgate", "dresidual", "dpost_weight", "dres_scale", "dpre_weight")] + _SCRATCH)
+
+
 def _packer(cls):
     """Packs the values of an argument struct's fields in order (0, not None, stands for NULL).  One call of 0.6 us, where 34
     attributes set one by one take 3.7: the general path of the forward call of 16 rows of 256 steps takes 15.3 us, of a generated
     token of 64 x 1536 channels 11.0 (csrc/binding.cpp: 6.6 and 5.0)."""
-    code = {_vp: "Q", _i32: "i", _i64: "q", _sz: "Q"}
+    code = {_vp: "Q", _i32: "i", _i64: "q", _sz: "Q", ctypes.c_float: "f"}
     p = struct.Struct("=" + "".join(code[t] for _, t in cls._fields_))
     assert p.size == ctypes.sizeof(cls), f"{cls.__name__}: padded"
     return p.pack
 
 
 _pack_fwd, _pack_bwd, _pack_step = _packer(FwdArgs), _packer(BwdArgs), _packer(StepArgs)
+_pack_delta_fwd, _pack_delta_bwd, _pack_delta_step = _packer(DeltaFwdArgs), _packer(DeltaBwdArgs), _packer(DeltaStepArgs)
+_pack_norm_fwd, _pack_norm_bwd = _packer(NormFwdArgs), _packer(NormBwdArgs)
 _FWD_SIZE, _BWD_SIZE, _STEP_SIZE = ctypes.sizeof(FwdArgs), ctypes.sizeof(BwdArgs), ctypes.sizeof(StepArgs)
 
 _lib = None
@@ -181,10 +223,14 @@ def lib():
         L.lrnnx_status_string.argtypes = [ctypes.c_int]
         L.lrnnx_status_string.restype = ctypes.c_char_p
         of_bytes, size_of_bytes = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_char_p), ctypes.CFUNCTYPE(_sz, ctypes.c_char_p)
-        for n in ("lrnnx_selective_scan_fwd", "lrnnx_selective_scan_bwd", "lrnnx_selective_step"):
+        for n in ("lrnnx_selective_scan_fwd", "lrnnx_selective_scan_bwd", "lrnnx_selective_step", "lrnnx_gated_delta_fwd",
+                  "lrnnx_gated_delta_bwd", "lrnnx_gated_delta_step", "lrnnx_block_norm_fwd", "lrnnx_block_norm_bwd"):
             _packed[n] = of_bytes((n, L))
-        n = "lrnnx_selective_scan_bwd_workspace_bytes"
-        _packed[n] = size_of_bytes((n, L))
+        for n in ("lrnnx_selective_scan_bwd_workspace_bytes", "lrnnx_gated_delta_fwd_workspace_bytes",
+                  "lrnnx_gated_delta_saved_bytes", "lrnnx_gated_delta_bwd_workspace_bytes"):
+            _packed[n] = size_of_bytes((n, L))
+        L.lrnnx_block_norm_bwd_workspace_bytes.argtypes = [_i64, _i64]
+        L.lrnnx_block_norm_bwd_workspace_bytes.restype = _sz
         from . import _binding
         _binding.bind(_check, L.lrnnx_ckpt_interval(), tuple(ctypes.cast(getattr(L, "lrnnx_" + n), _vp).value for n in (
             "selective_scan_fwd", "selective_scan_bwd", "selective_scan_bwd_workspace_bytes", "selective_scan_fwd_complex",
@@ -954,3 +1000,243 @@ def lrnnx_lti_step(lam, x, v):
     a.stream = _stream()
     _check(lib().lrnnx_lti_step(ctypes.byref(a)))
     return x
+
+
+# ---------------------------------------------------------------- gated delta rule
+_DELTA_FWD_SIZE, _DELTA_BWD_SIZE, _DELTA_STEP_SIZE = (ctypes.sizeof(c) for c in (DeltaFwdArgs, DeltaBwdArgs, DeltaStepArgs))
+_NORM_FWD_SIZE, _NORM_BWD_SIZE = ctypes.sizeof(NormFwdArgs), ctypes.sizeof(NormBwdArgs)
+
+
+def _rows(t, name, shape, dtype):
+    """(ptr, strides) of a tensor with a contiguous last axis; `shape` with that axis."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    *st, last = t.stride()
+    if last != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: expected a contiguous last axis")
+    return (t.data_ptr(), *st)
+
+
+def _gates(g, beta, shape, io):
+    """(gate code, (ptr, strides) of g, of beta): float32, or the I/O type."""
+    if g.dtype != beta.dtype or g.dtype not in (torch.float32, io):
+        raise TypeError(f"g, beta: expected both float32 or both {io}, got {g.dtype} and {beta.dtype}")
+    for t, name in ((g, "g"), (beta, "beta")):
+        if t.shape != shape:
+            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return BF16 if g.dtype == torch.bfloat16 else F32, (g.data_ptr(), *g.stride()), (beta.data_ptr(), *beta.stride())
+
+
+def _out_rows(t, name, shape, dtype):
+    """(ptr, strides) of an output whose rows must not overlap."""
+    r = _rows(t, name, shape, dtype)
+    need = shape[-1]
+    for stride, count in sorted(zip(r[1:], shape[:-1])):
+        if count > 1:
+            if stride < need:
+                raise ValueError(f"{name}: output rows overlap")
+            need = stride * count
+    return r
+
+
+def _delta_head(q, k, v, cu_seqlens, scale):
+    """What the calls over a sequence have in common; the packed form gets a batch axis of one."""
+    if q.dim() != (4 if cu_seqlens is None else 3) or k.dim() != q.dim() or v.dim() != q.dim():
+        raise ValueError("q, k, v: expected [B,L,H,d], or [L,H,d] with cu_seqlens")
+    S = _check_cu(cu_seqlens) if cu_seqlens is not None else None
+    if S is not None:
+        q, k, v = q.unsqueeze(0), k.unsqueeze(0), v.unsqueeze(0)
+    lead, (Hk, dk), (Hv, dv) = q.shape[:2], q.shape[2:], v.shape[2:]
+    if scale is None:
+        scale = dk ** -0.5
+    return q, k, v, lead, S if S is not None else lead[0], Hk, Hv, dk, dv, float(scale)
+
+
+def _delta_inputs(q, k, v, g, beta, s0, lead, B, Hk, Hv, dk, dv, io, packed):
+    if packed:
+        g, beta = g.unsqueeze(0), beta.unsqueeze(0)
+    gate, g, beta = _gates(g, beta, (*lead, Hv), io)
+    return gate, (*_rows(q, "q", (*lead, Hk, dk), io), *_rows(k, "k", (*lead, Hk, dk), io), *_rows(v, "v", (*lead, Hv, dv), io),
+                  *g, *beta, _f32c(s0, "s0", (B, Hv, dk, dv)))
+
+
+def _scratch(workspace, nbytes, device, name="workspace"):
+    if workspace is None:
+        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous uint8 tensor")
+    return workspace
+
+
+@_device_checked
+def lrnnx_gated_delta_fwd(q, k, v, g, beta, scale=None, s0=None, cu_seqlens=None, return_last_state=False, return_saved=False,
+                          out=None, workspace=None):
+    """o [B,L,Hv,dv] of the gated delta rule, and optionally the last state [B,Hv,dk,dv] float32 and `saved`, the opaque
+    buffer that lrnnx_gated_delta_bwd takes; see lrnnx_delta_fwd_args.
+
+    q, k [B,L,Hk,dk], v [B,L,Hv,dv] float32 or bfloat16, any strides with a contiguous last axis; g (log decay), beta
+    [B,L,Hv] float32 or the I/O type; scale: dk ** -0.5 by default.  With `cu_seqlens` (int64 [S+1] on the device) the
+    batch is packed: q, k, v, g, beta, o without the batch axis, s0 and the last state [S,Hv,dk,dv]."""
+    packed, io = cu_seqlens is not None, v.dtype
+    q, k, v, lead, B, Hk, Hv, dk, dv, scale = _delta_head(q, k, v, cu_seqlens, scale)
+    code = _io_dtype(v)
+    gate, inputs = _delta_inputs(q, k, v, g, beta, s0, lead, B, Hk, Hv, dk, dv, io, packed)
+    o = torch.empty((*lead, Hv, dv), dtype=io, device=v.device) if out is None else out.unsqueeze(0) if packed else out
+    po = _out_rows(o, "out", (*lead, Hv, dv), io)
+    s_last = torch.empty((B, Hv, dk, dv), dtype=torch.float32, device=v.device) if return_last_state else None
+    head = (_DELTA_FWD_SIZE, B, Hk, Hv, dk, dv, code, gate, scale, lead[1], cu_seqlens.data_ptr() if packed else 0, *inputs, *po,
+            0 if s_last is None else s_last.data_ptr())
+    saved, psaved, nsaved = None, 0, 0
+    if _lib is None:
+        lib()
+    if return_saved:
+        nsaved = _call("lrnnx_gated_delta_saved_bytes", _pack_delta_fwd(*head, 0, 0, 0, 0, 0))
+        saved = torch.empty(max(nsaved, 16), dtype=torch.uint8, device=v.device)
+        psaved = saved.data_ptr()
+    workspace = _scratch(workspace, 0 if workspace is not None else
+                         _call("lrnnx_gated_delta_fwd_workspace_bytes", _pack_delta_fwd(*head, psaved, nsaved, 0, 0, 0)), v.device)
+    _check(_call("lrnnx_gated_delta_fwd", _pack_delta_fwd(*head, psaved, nsaved, workspace.data_ptr(), workspace.numel(), _stream())))
+    res = (o[0] if packed else o,) + ((s_last,) if return_last_state else ()) + ((saved,) if return_saved else ())
+    return res[0] if len(res) == 1 else res
+
+
+@_device_checked
+def lrnnx_gated_delta_bwd(q, k, v, g, beta, do, saved, scale=None, s0=None, ds_last=None, want_ds0=False, cu_seqlens=None,
+                          workspace=None):
+    """Gradients of sum(do * o) (and sum(ds_last * s_last)) as a dict: dq, dk, dv in the I/O type, dg, dbeta in the gates'
+    type, ds0 float32 if wanted; see lrnnx_delta_bwd_args.  Inputs, scale, s0 and cu_seqlens as in the forward call that
+    returned `saved`."""
+    packed, io = cu_seqlens is not None, v.dtype
+    gdt, device = g.dtype, v.device
+    q, k, v, lead, B, Hk, Hv, dk, dv, scale = _delta_head(q, k, v, cu_seqlens, scale)
+    code = _io_dtype(v)
+    gate, inputs = _delta_inputs(q, k, v, g, beta, s0, lead, B, Hk, Hv, dk, dv, io, packed)
+    pdo = _rows(do.unsqueeze(0) if packed else do, "do", (*lead, Hv, dv), io)
+    if saved.dtype != torch.uint8 or not saved.is_contiguous():
+        raise TypeError("saved: expected the buffer that the forward call returned")
+    rows = lead[1:] if packed else lead
+    dq, dkey = (torch.empty((*rows, Hk, dk), dtype=io, device=device) for _ in range(2))
+    dval = torch.empty((*rows, Hv, dv), dtype=io, device=device)
+    dg, dbeta = (torch.empty((*rows, Hv), dtype=gdt, device=device) for _ in range(2))
+    ds0 = torch.empty((B, Hv, dk, dv), dtype=torch.float32, device=device) if want_ds0 else None
+    head = (_DELTA_BWD_SIZE, B, Hk, Hv, dk, dv, code, gate, scale, lead[1], cu_seqlens.data_ptr() if packed else 0, *inputs, *pdo,
+            _f32c(ds_last, "ds_last", (B, Hv, dk, dv)), saved.data_ptr(), saved.numel(), dq.data_ptr(), dkey.data_ptr(),
+            dval.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), 0 if ds0 is None else ds0.data_ptr())
+    workspace = _scratch(workspace, 0 if workspace is not None else
+                         _call("lrnnx_gated_delta_bwd_workspace_bytes", _pack_delta_bwd(*head, 0, 0, 0)), device)
+    _check(_call("lrnnx_gated_delta_bwd", _pack_delta_bwd(*head, workspace.data_ptr(), workspace.numel(), _stream())))
+    res = dict(dq=dq, dk=dkey, dv=dval, dg=dg, dbeta=dbeta)
+    if want_ds0:
+        res["ds0"] = ds0
+    return res
+
+
+@_device_checked
+def lrnnx_gated_delta_step(q, k, v, g, beta, state, scale=None, out=None):
+    """One token: updates state [B,Hv,dk,dv] float32 in place and returns o [B,Hv,dv]; q, k [B,Hk,dk], v [B,Hv,dv], g, beta
+    [B,Hv]; see lrnnx_delta_step_args."""
+    io = v.dtype
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q, k, v: expected [B,H,d]")
+    (B, Hk, dk), (_, Hv, dv) = q.shape, v.shape
+    gate, pg, pbeta = _gates(g, beta, (B, Hv), io)
+    o = torch.empty((B, Hv, dv), dtype=io, device=v.device) if out is None else out
+    _check(_call("lrnnx_gated_delta_step", _pack_delta_step(
+        _DELTA_STEP_SIZE, B, Hk, Hv, dk, dv, _io_dtype(v), gate, dk ** -0.5 if scale is None else float(scale),
+        *_rows(q, "q", (B, Hk, dk), io), *_rows(k, "k", (B, Hk, dk), io), *_rows(v, "v", (B, Hv, dv), io), *pg, *pbeta,
+        _f32c(state, "state", (B, Hv, dk, dv)), *_out_rows(o, "out", (B, Hv, dv), io), _stream())))
+    return o
+
+
+# ---------------------------------------------------------------- norms around a block
+GATE_ACT = {"silu": 0, "sigmoid": 1}
+
+
+def _matrix(t, name, shape, dtypes):
+    """(ptr, row stride) of an optional tensor [..., D] as M rows."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if t.stride(-1) != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: expected a contiguous last axis")
+    row, need = None, None
+    for stride, count in zip(reversed(t.stride()[:-1]), reversed(shape[:-1])):       # one stride for all rows
+        if count > 1:
+            if row is None:
+                row, need = stride, stride * count
+            elif stride != need:
+                raise ValueError(f"{name}: rows are not evenly spaced")
+            else:
+                need = stride * count
+    return t.data_ptr(), shape[-1] if row is None else row
+
+
+def _norm_head(x, post_weight, groups, gate, gate_act, residual, res_scale, pre_weight, eps, size, res_dtype):
+    if x.dim() < 1:
+        raise ValueError("x: expected [..., D]")
+    io, shape, D = x.dtype, x.shape, x.shape[-1]
+    code, groups = _io_dtype(x), int(groups)
+    if res_dtype not in (torch.float32, io):
+        raise TypeError(f"residual: dtype {res_dtype}, expected torch.float32 or {io}")
+    if groups < 1 or D % groups:
+        raise ValueError("D must be a multiple of groups")
+    shared = post_weight is not None and groups > 1 and post_weight.shape == (D // groups,)
+    return (size, x.numel() // max(D, 1), D, groups, int(shared), _code(gate_act, GATE_ACT), code, _io_dtype_of(res_dtype), float(eps), 0,
+            *_matrix(x, "x", shape, (io,)), _f32c(post_weight, "post_weight", (D // groups,) if shared else (D,)),
+            *_matrix(gate, "gate", shape, (io,)), *_matrix(residual, "residual", shape, (res_dtype,)),
+            _f32c(res_scale, "res_scale", (D,)), _f32c(pre_weight, "pre_weight", (D,)))
+
+
+def _io_dtype_of(dtype):
+    return BF16 if dtype == torch.bfloat16 else F32
+
+
+@_device_checked
+def lrnnx_block_norm_fwd(x, post_weight=None, groups=1, gate=None, gate_act="silu", residual=None, res_scale=None, pre_weight=None,
+                         eps=1e-6, out=None):
+    """(h, y): the norm, gate and residual sum after a block and the norm before the next; see lrnnx_norm_fwd_args.
+
+    x, gate [..., D]; post_weight [D] or [D // groups] (one for all groups), res_scale, pre_weight [D] float32; residual
+    [..., D] float32 or the I/O type, which is h's type too (x's without a residual).  y is None without pre_weight.  `out`
+    takes h (it may be the residual)."""
+    res_dtype = residual.dtype if residual is not None else out.dtype if out is not None else x.dtype
+    head = _norm_head(x, post_weight, groups, gate, gate_act, residual, res_scale, pre_weight, eps, _NORM_FWD_SIZE, res_dtype)
+    h = torch.empty(x.shape, dtype=res_dtype, device=x.device) if out is None else out
+    if h.shape != x.shape or not h.is_contiguous():
+        raise ValueError(f"out: expected a contiguous tensor of shape {tuple(x.shape)}")
+    y = None if pre_weight is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check(_call("lrnnx_block_norm_fwd", _pack_norm_fwd(*head, h.data_ptr(), 0 if y is None else y.data_ptr(), _stream())))
+    return h, y
+
+
+@_device_checked
+def lrnnx_block_norm_bwd(x, dh=None, dy=None, post_weight=None, groups=1, gate=None, gate_act="silu", residual=None, res_scale=None,
+                         pre_weight=None, eps=1e-6, workspace=None):
+    """Gradients of sum(dh * h) + sum(dy * y) as a dict: dx, and dgate, dresidual, dpost_weight, dres_scale, dpre_weight for
+    the inputs given; see lrnnx_norm_bwd_args.  Inputs as in the forward call; dh in h's type, dy in x's."""
+    if dh is None and dy is None:
+        raise ValueError("dh, dy: one of them is needed")
+    res_dtype = residual.dtype if residual is not None else dh.dtype if dh is not None else x.dtype
+    head = _norm_head(x, post_weight, groups, gate, gate_act, residual, res_scale, pre_weight, eps, _NORM_BWD_SIZE, res_dtype)
+    D = x.shape[-1]
+    grads = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device))
+    if gate is not None:
+        grads["dgate"] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if residual is not None:
+        grads["dresidual"] = torch.empty(x.shape, dtype=res_dtype, device=x.device)
+    for name, w in (("dpost_weight", post_weight), ("dres_scale", res_scale), ("dpre_weight", pre_weight)):
+        if w is not None:
+            grads[name] = torch.empty_like(w)
+    ptrs = [grads[n].data_ptr() if n in grads else 0 for n in ("dx", "dgate", "dresidual", "dpost_weight", "dres_scale", "dpre_weight")]
+    workspace = _scratch(workspace, 0 if workspace is not None else lib().lrnnx_block_norm_bwd_workspace_bytes(head[1], D), x.device)
+    _check(_call("lrnnx_block_norm_bwd", _pack_norm_bwd(
+        *head, *_matrix(dh, "dh", x.shape, (res_dtype,)), *_matrix(dy, "dy", x.shape, (x.dtype,)), *ptrs,
+        workspace.data_ptr(), workspace.numel(), _stream())))
+    return grads

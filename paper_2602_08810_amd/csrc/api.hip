@@ -279,7 +279,7 @@ extern "C" {
 
 int64_t lrnnx_ckpt_interval(void) { return kCkptInterval; }
 int64_t lrnnx_packed_ckpt_slots(int64_t L, int64_t B) { return (L < 0 || B < 0) ? 0 : L / kCkptInterval + B; }
-int lrnnx_version(void) { return 300; }   // major * 100 + minor; the major number changes with any struct layout
+int lrnnx_version(void) { return 301; }   // major * 100 + minor; the major number changes with any struct layout
 
 int lrnnx_selective_scan_bwd_chunks(int64_t B, int64_t D, int64_t N, int64_t L, int bc_groups, int path, int complex_a) {
     const int bcg = bc_groups > 1 ? bc_groups : 1;

@@ -1,0 +1,70 @@
+// Host-visible parameter block and launcher declarations of the gated delta rule.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lrnnx {
+
+constexpr int kDeltaSlot = 64;           // steps between saved states; a slot holds two chunks
+constexpr int kDeltaChunk = 32;          // steps whose corrections are solved for together
+
+// Rows of a matrix operand in bfloat16: element (plane, batch, step, head, column) at plane * plane_stride + b * sb + t * sl + h * sh + column,
+// rows 16-byte aligned and zero beyond the head's width up to the padded one.  A float32 operand is the sum of three planes.
+struct DeltaRows {
+    const uint16_t *p;
+    int64_t plane, sb, sl, sh;
+};
+
+struct DeltaParams {
+    int B, Hk, Hv, dk, dv, dvp;          // dvp: dv padded to whole matrix tiles (32)
+    int64_t L, nslots, slots_each;       // slots in all; of one sequence (batch form)
+    float scale;
+    int io, gate_io;                     // 1: bfloat16 inputs; gate_io: g and beta in the I/O type
+    const int64_t *cu;
+    DeltaRows q, k, dout;
+    const void *v, *g, *beta;
+    int64_t v_sb, v_sl, v_sh, g_sb, g_sl, g_sh, be_sb, be_sl, be_sh;
+    const float *s0;
+    void *o;
+    int64_t o_sb, o_sl, o_sh;
+    int o_vec;                           // rows of o take stores of four elements
+    float *s_last;
+    uint16_t *mat_t, *mat_a;             // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands
+    uint16_t *mat_tt, *mat_at;           // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
+    float *scal;                         // per slot, head and chunk: exp(G), exp(G_end - G), beta
+    uint16_t *states, *err;              // saved for the backward pass; null: not wanted
+    // backward
+    const float *ds_last;
+    float *ds0;
+    uint16_t *dstates, *z;
+    void *dq, *dkk, *dvv, *dg, *dbeta;
+    int wave_cols;                       // (launch) waves of 16 columns a workgroup
+    int np, np_adjoint;                  // planes of the state chain, of its adjoint
+};
+
+struct DeltaPack {                       // a strided operand copied into planes
+    const void *src;
+    int64_t sb, sl, sh;
+    uint16_t *dst;
+    int64_t plane;
+    int B, H, d, dp, planes, io;
+    int64_t L;
+};
+
+hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s);
+hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s);
+
+struct DeltaStepParams {
+    int B, Hk, Hv, dk, dv, gate_io;
+    float scale;
+    const void *q, *k, *v, *g, *beta;
+    int64_t q_sb, q_sh, k_sb, k_sh, v_sb, v_sh, g_sb, g_sh, be_sb, be_sh, o_sb, o_sh;
+    float *state;
+    void *o;
+};
+hipError_t launch_delta_step(const DeltaStepParams &p, int io, hipStream_t s);
+
+}  // namespace lrnnx

@@ -1,0 +1,304 @@
+// C ABI of the gated delta rule and of the norms around a block: argument checks, layout of workspace and saved data, launches.
+// Nothing here allocates, frees or synchronises; see include/lrnnx.h for the contract.
+#include "../../include/lrnnx.h"
+#include "delta.hpp"
+#include "block_norm.hpp"
+
+using namespace lrnnx;
+
+namespace {
+
+inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool on_elem(const void *p, size_t es) { return (reinterpret_cast<uintptr_t>(p) & (es - 1)) == 0; }
+inline size_t elem(int dtype) { return dtype == LRNNX_BF16 ? 2 : 4; }
+
+// What the forward and the backward call have in common.
+struct Shape {
+    int B, Hk, Hv, dk, dv, dkp, dvp, bf16, planes;       // planes: bfloat16 numbers that a factor read from memory is the sum of
+    int64_t L, rows, nslots, slots_each;
+};
+
+template <class A> int common_checks(const A *a) {
+    if (a->B < 1 || a->Hk < 1 || a->Hv < 1 || a->dk < 1 || a->dv < 1 || a->L < 1) return LRNNX_ERR_INVALID_ARG;
+    if (a->Hv % a->Hk) return LRNNX_ERR_INVALID_ARG;
+    if (a->io_dtype != LRNNX_F32 && a->io_dtype != LRNNX_BF16) return LRNNX_ERR_INVALID_ARG;
+    if (a->gate_dtype != LRNNX_F32 && a->gate_dtype != a->io_dtype) return LRNNX_ERR_INVALID_ARG;
+    if (a->dk > 128 || a->dv > 256 || a->B > 65535 || a->Hv > 65535) return LRNNX_ERR_UNSUPPORTED;
+    // rows, slots and their arrays stay countable; a slot and head is a workgroup of one launch
+    if (a->L > ((int64_t)1 << 40)) return LRNNX_ERR_UNSUPPORTED;
+    const int64_t slots = a->cu_seqlens ? a->L / kDeltaSlot + a->B : a->B * ((a->L + kDeltaSlot - 1) / kDeltaSlot);
+    if (slots > (int64_t)0x7fffffff / a->Hv) return LRNNX_ERR_UNSUPPORTED;
+    return LRNNX_OK;
+}
+template <class A> Shape shape_of(const A *a) {
+    Shape s;
+    s.B = a->B; s.Hk = a->Hk; s.Hv = a->Hv; s.dk = a->dk; s.dv = a->dv; s.L = a->L;
+    s.dkp = a->dk > 64 ? 128 : 64; s.dvp = (int)up(a->dv, 32);
+    s.bf16 = a->io_dtype == LRNNX_BF16; s.planes = s.bf16 ? 1 : 3;
+    s.rows = (a->cu_seqlens ? 1 : (int64_t)a->B) * a->L;
+    s.slots_each = (a->L + kDeltaSlot - 1) / kDeltaSlot;
+    s.nslots = a->cu_seqlens ? a->L / kDeltaSlot + a->B : a->B * s.slots_each;
+    return s;
+}
+inline int adjoint_planes(const Shape &s, bool s0) { return !s.bf16 || s0 ? 3 : 2; }
+
+// Strided rows of `width` elements that the matrix kernels can read as they lie.
+bool rows_in_place(const Shape &s, const void *p, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, int H) {
+    return s.bf16 && width == padded && on16(p) && (one_batch || s.B == 1 || sb % 8 == 0) && (s.L == 1 || sl % 8 == 0) && (H == 1 || sh % 8 == 0);
+}
+
+// Lays arrays out one after the other, 256-byte aligned; with a null base it only counts.
+struct Layout {
+    char *base;
+    size_t at = 0;
+    template <class T> T *take(int64_t count) {
+        const size_t here = (at + 255) / 256 * 256;
+        at = here + (size_t)count * sizeof(T);
+        return base ? reinterpret_cast<T *>(base + here) : nullptr;
+    }
+};
+inline int64_t mats(const Shape &s) { return s.nslots * s.Hv * 2; }
+inline int a_planes(const Shape &s) { return s.bf16 ? 2 : 3; }
+
+void lay_saved(const Shape &s, bool s0, Layout &l, DeltaParams &p) {
+    p.states = l.take<uint16_t>(s.nslots * s.Hv * (s.bf16 ? 1 : 3) * s.dkp * s.dvp);
+    p.err = l.take<uint16_t>((int64_t)(s.bf16 ? 2 : 3) * s.rows * s.Hv * s.dvp);
+    p.mat_tt = l.take<uint16_t>(mats(s) * 2 * adjoint_planes(s, s0) * 512);
+    p.mat_at = l.take<uint16_t>(mats(s) * 2 * a_planes(s) * 512);
+    p.scal = l.take<float>(mats(s) * 96);
+}
+
+DeltaRows lay_rows(const Shape &s, Layout &l, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, bool &copied) {
+    copied = !rows_in_place(s, src, width, padded, sb, sl, sh, one_batch, H);
+    DeltaRows r;
+    if (!copied) {
+        r.p = reinterpret_cast<const uint16_t *>(src); r.plane = 0; r.sb = sb; r.sl = sl; r.sh = sh;
+        return r;
+    }
+    r.plane = s.rows * H * padded;
+    r.p = l.take<uint16_t>(s.planes * r.plane);
+    r.sb = s.L * H * padded; r.sl = (int64_t)H * padded; r.sh = padded;
+    return r;
+}
+hipError_t copy_rows(const Shape &s, const DeltaRows &r, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, hipStream_t st) {
+    DeltaPack k{};
+    k.src = src; k.sb = sb; k.sl = sl; k.sh = sh;
+    k.dst = const_cast<uint16_t *>(r.p); k.plane = r.plane;
+    k.B = one_batch ? 1 : s.B; k.H = H; k.d = width; k.dp = padded; k.planes = s.planes; k.io = s.bf16; k.L = s.L;
+    return launch_delta_pack(k, st);
+}
+
+template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
+    p.B = s.B; p.Hk = s.Hk; p.Hv = s.Hv; p.dk = s.dk; p.dv = s.dv; p.dvp = s.dvp;
+    p.L = s.L; p.nslots = s.nslots; p.slots_each = s.slots_each; p.scale = a->scale;
+    p.io = s.bf16; p.gate_io = a->gate_dtype == LRNNX_BF16; p.cu = a->cu_seqlens;
+    p.v = a->v; p.g = a->g; p.beta = a->beta;
+    p.v_sb = a->v_stride_b; p.v_sl = a->v_stride_l; p.v_sh = a->v_stride_h;
+    p.g_sb = a->g_stride_b; p.g_sl = a->g_stride_l; p.g_sh = a->g_stride_h;
+    p.be_sb = a->beta_stride_b; p.be_sl = a->beta_stride_l; p.be_sh = a->beta_stride_h;
+    p.s0 = a->s0;
+}
+
+// Wavefronts of 16 columns a workgroup: as many as leave a workgroup for every compute unit.
+int waves_of(const Shape &s) {
+    const int64_t tiles = s.dvp / 16;
+    for (int w = 8; w > 2; w /= 2)
+        if ((int64_t)s.B * s.Hv * ((tiles + w - 1) / w) >= 256) return w;
+    return 2;
+}
+
+struct FwdPlan { DeltaParams p; bool copy_q, copy_k; size_t bytes, saved; };
+FwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *saved) {
+    FwdPlan f{};
+    set_inputs(a, s, f.p);
+    const bool one = a->cu_seqlens != nullptr;
+    f.p.np = !s.bf16 || a->s0 || a->s_last ? 3 : 2;
+    f.p.np_adjoint = adjoint_planes(s, a->s0 != nullptr);
+    f.p.wave_cols = waves_of(s);
+    Layout l{ws}, sv{saved};
+    f.p.q = lay_rows(s, l, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, f.copy_q);
+    f.p.k = lay_rows(s, l, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, f.copy_k);
+    f.p.mat_t = l.take<uint16_t>(mats(s) * 2 * f.p.np * 512);
+    f.p.mat_a = l.take<uint16_t>(mats(s) * 2 * a_planes(s) * 512);
+    if (a->saved || !ws) lay_saved(s, a->s0 != nullptr, sv, f.p);
+    if (!a->saved) f.p.scal = l.take<float>(mats(s) * 96);
+    f.bytes = l.at; f.saved = sv.at;
+    return f;
+}
+
+struct BwdPlan { DeltaParams p; bool copy_q, copy_k, copy_d; size_t bytes, saved; };
+BwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, char *saved) {
+    BwdPlan f{};
+    set_inputs(a, s, f.p);
+    const bool one = a->cu_seqlens != nullptr;
+    f.p.np = adjoint_planes(s, a->s0 != nullptr);
+    f.p.wave_cols = waves_of(s);
+    Layout l{ws}, sv{saved};
+    f.p.q = lay_rows(s, l, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, f.copy_q);
+    f.p.k = lay_rows(s, l, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, f.copy_k);
+    f.p.dout = lay_rows(s, l, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one, f.copy_d);
+    lay_saved(s, a->s0 != nullptr, sv, f.p);
+    f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * (s.bf16 ? 1 : 3) * s.dkp * s.dvp);
+    f.p.z = l.take<uint16_t>((int64_t)(s.bf16 ? 2 : 3) * s.rows * s.Hv * s.dvp);
+    f.bytes = l.at; f.saved = sv.at;
+    return f;
+}
+
+template <class A> bool inputs_given(const A *a) { return a->q && a->k && a->v && a->g && a->beta; }
+template <class A> bool inputs_on_elements(const A *a) {
+    const size_t es = elem(a->io_dtype), gs = elem(a->gate_dtype);
+    return on_elem(a->q, es) && on_elem(a->k, es) && on_elem(a->v, es) && on_elem(a->g, gs) && on_elem(a->beta, gs) && on_elem(a->s0, 4) &&
+           on_elem(a->cu_seqlens, 8);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lrnnx_gated_delta_fwd_workspace_bytes(const lrnnx_delta_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_fwd_args) || common_checks(a) != LRNNX_OK) return 0;
+    return plan_fwd(a, shape_of(a), nullptr, nullptr).bytes;
+}
+size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_fwd_args) || common_checks(a) != LRNNX_OK) return 0;
+    return plan_fwd(a, shape_of(a), nullptr, nullptr).saved;
+}
+
+int lrnnx_gated_delta_fwd(const lrnnx_delta_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_fwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = common_checks(a)) return e;
+    if (!inputs_given(a) || !a->o) return LRNNX_ERR_INVALID_ARG;
+    const size_t es = elem(a->io_dtype);
+    if (!inputs_on_elements(a) || !on_elem(a->o, es) || !on_elem(a->s_last, 4) || !on16(a->saved) || !on16(a->workspace)) return LRNNX_ERR_INVALID_ARG;
+    const Shape s = shape_of(a);
+    FwdPlan f = plan_fwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(a->saved));
+    if (!a->workspace || a->workspace_bytes < f.bytes || (a->saved && a->saved_bytes < f.saved)) return LRNNX_ERR_WORKSPACE;
+    DeltaParams &p = f.p;
+    p.o = a->o; p.o_sb = a->o_stride_b; p.o_sl = a->o_stride_l; p.o_sh = a->o_stride_h; p.s_last = a->s_last;
+    const bool one = a->cu_seqlens != nullptr;
+    p.o_vec = (reinterpret_cast<uintptr_t>(a->o) & (4 * es - 1)) == 0 && (one || s.B == 1 || a->o_stride_b % 4 == 0) &&
+              (s.L == 1 || a->o_stride_l % 4 == 0) && (s.Hv == 1 || a->o_stride_h % 4 == 0);
+    const hipStream_t st = reinterpret_cast<hipStream_t>(a->stream);
+    if (f.copy_q && copy_rows(s, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if (f.copy_k && copy_rows(s, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if (launch_delta_prep(p, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    return launch_delta_scan(p, st) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+size_t lrnnx_gated_delta_bwd_workspace_bytes(const lrnnx_delta_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_bwd_args) || common_checks(a) != LRNNX_OK) return 0;
+    return plan_bwd(a, shape_of(a), nullptr, nullptr).bytes;
+}
+
+int lrnnx_gated_delta_bwd(const lrnnx_delta_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_bwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = common_checks(a)) return e;
+    if (!inputs_given(a) || !a->dout || !a->saved || !a->dq || !a->dkey || !a->dval || !a->dg || !a->dbeta) return LRNNX_ERR_INVALID_ARG;
+    const size_t es = elem(a->io_dtype), gs = elem(a->gate_dtype);
+    if (!inputs_on_elements(a) || !on_elem(a->dout, es) || !on_elem(a->ds_last, 4) || !on16(a->saved) || !on_elem(a->dq, es) || !on_elem(a->dkey, es) ||
+        !on_elem(a->dval, es) || !on_elem(a->dg, gs) || !on_elem(a->dbeta, gs) || !on_elem(a->ds0, 4) || !on16(a->workspace))
+        return LRNNX_ERR_INVALID_ARG;
+    const Shape s = shape_of(a);
+    BwdPlan f = plan_bwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(const_cast<void *>(a->saved)));
+    if (!a->workspace || a->workspace_bytes < f.bytes || a->saved_bytes < f.saved) return LRNNX_ERR_WORKSPACE;
+    DeltaParams &p = f.p;
+    p.ds_last = a->ds_last; p.ds0 = a->ds0;
+    auto on4 = [&](const void *q) { return (reinterpret_cast<uintptr_t>(q) & (4 * es - 1)) == 0; };
+    p.o_vec = s.dv % 4 == 0 && on4(a->dval) && on4(a->dq) && on4(a->dkey);
+    p.dq = a->dq; p.dkk = a->dkey; p.dvv = a->dval; p.dg = a->dg; p.dbeta = a->dbeta;
+    const bool one = a->cu_seqlens != nullptr;
+    const hipStream_t st = reinterpret_cast<hipStream_t>(a->stream);
+    if (f.copy_q && copy_rows(s, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if (f.copy_k && copy_rows(s, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if (f.copy_d && copy_rows(s, p.dout, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one, st) != hipSuccess)
+        return LRNNX_ERR_LAUNCH;
+    if (launch_delta_adjoint(p, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    return launch_delta_grads(p, st) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+int lrnnx_gated_delta_step(const lrnnx_delta_step_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_delta_step_args)) return LRNNX_ERR_INVALID_ARG;
+    if (a->B < 1 || a->Hk < 1 || a->Hv < 1 || a->dk < 1 || a->dv < 1 || a->Hv % a->Hk) return LRNNX_ERR_INVALID_ARG;
+    if (a->io_dtype != LRNNX_F32 && a->io_dtype != LRNNX_BF16) return LRNNX_ERR_INVALID_ARG;
+    if (a->gate_dtype != LRNNX_F32 && a->gate_dtype != a->io_dtype) return LRNNX_ERR_INVALID_ARG;
+    if (a->dk > 128 || a->dv > 256 || a->B > 65535 || a->Hv > 65535) return LRNNX_ERR_UNSUPPORTED;
+    if (!a->q || !a->k || !a->v || !a->g || !a->beta || !a->state || !a->o) return LRNNX_ERR_INVALID_ARG;
+    const size_t es = elem(a->io_dtype), gs = elem(a->gate_dtype);
+    if (!on_elem(a->q, es) || !on_elem(a->k, es) || !on_elem(a->v, es) || !on_elem(a->o, es) || !on_elem(a->g, gs) || !on_elem(a->beta, gs) ||
+        !on_elem(a->state, 4))
+        return LRNNX_ERR_INVALID_ARG;
+    DeltaStepParams p{};
+    p.B = a->B; p.Hk = a->Hk; p.Hv = a->Hv; p.dk = a->dk; p.dv = a->dv; p.gate_io = a->gate_dtype == LRNNX_BF16; p.scale = a->scale;
+    p.q = a->q; p.k = a->k; p.v = a->v; p.g = a->g; p.beta = a->beta; p.state = a->state; p.o = a->o;
+    p.q_sb = a->q_stride_b; p.q_sh = a->q_stride_h; p.k_sb = a->k_stride_b; p.k_sh = a->k_stride_h; p.v_sb = a->v_stride_b; p.v_sh = a->v_stride_h;
+    p.g_sb = a->g_stride_b; p.g_sh = a->g_stride_h; p.be_sb = a->beta_stride_b; p.be_sh = a->beta_stride_h; p.o_sb = a->o_stride_b; p.o_sh = a->o_stride_h;
+    return launch_delta_step(p, a->io_dtype == LRNNX_BF16, reinterpret_cast<hipStream_t>(a->stream)) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+}  // extern "C"
+
+namespace {
+
+template <class A> int norm_checks(const A *a) {
+    if (a->M < 1 || a->D < 1 || a->groups < 1 || a->D % a->groups || a->gate_act < 0 || a->gate_act > 1) return LRNNX_ERR_INVALID_ARG;
+    if (a->io_dtype != LRNNX_F32 && a->io_dtype != LRNNX_BF16) return LRNNX_ERR_INVALID_ARG;
+    if (a->res_dtype != LRNNX_F32 && a->res_dtype != a->io_dtype) return LRNNX_ERR_INVALID_ARG;
+    if (!(a->eps >= 0.0f) || !a->x) return LRNNX_ERR_INVALID_ARG;
+    if (a->D > 8192 || a->M > ((int64_t)1 << 40)) return LRNNX_ERR_UNSUPPORTED;
+    const size_t es = elem(a->io_dtype), rs = elem(a->res_dtype);
+    if (!on_elem(a->x, es) || !on_elem(a->gate, es) || !on_elem(a->residual, rs) || !on_elem(a->post_weight, 4) || !on_elem(a->res_scale, 4) ||
+        !on_elem(a->pre_weight, 4))
+        return LRNNX_ERR_INVALID_ARG;
+    return LRNNX_OK;
+}
+template <class A> NormParams norm_params(const A *a) {
+    NormParams p{};
+    p.M = a->M; p.D = a->D; p.groups = a->groups; p.width = a->D / a->groups; p.post_shared = a->post_shared != 0 && a->groups > 1;
+    p.io = a->io_dtype == LRNNX_BF16; p.res_io = a->res_dtype == LRNNX_BF16; p.gate_act = a->gate_act; p.eps = a->eps;
+    p.x = a->x; p.gate = a->gate; p.res = a->residual;
+    p.x_s = a->x_stride; p.gate_s = a->gate_stride; p.res_s = a->residual_stride;
+    p.post = a->post_weight; p.scale = a->res_scale; p.pre = a->pre_weight;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lrnnx_block_norm_fwd(const lrnnx_norm_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_norm_fwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = norm_checks(a)) return e;
+    if (!a->h || (a->pre_weight != nullptr) != (a->y != nullptr)) return LRNNX_ERR_INVALID_ARG;
+    if (!on_elem(a->h, elem(a->res_dtype)) || !on_elem(a->y, elem(a->io_dtype))) return LRNNX_ERR_INVALID_ARG;
+    NormParams p = norm_params(a);
+    p.h = a->h; p.y = a->y;
+    return launch_norm_fwd(p, reinterpret_cast<hipStream_t>(a->stream)) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+size_t lrnnx_block_norm_bwd_workspace_bytes(int64_t M, int64_t D) {
+    if (M < 1 || D < 1 || D > 8192) return 0;
+    return (size_t)norm_bwd_blocks(M, (int)D) * 3 * (size_t)D * sizeof(float);
+}
+
+int lrnnx_block_norm_bwd(const lrnnx_norm_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_norm_bwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = norm_checks(a)) return e;
+    if (!a->dx || (!a->dh && !a->dy) || (a->dy && !a->pre_weight)) return LRNNX_ERR_INVALID_ARG;
+    if ((a->dgate && !a->gate) || (a->dresidual && !a->residual) || (a->dpost_weight && !a->post_weight) || (a->dres_scale && !a->res_scale) ||
+        (a->dpre_weight && !a->pre_weight))
+        return LRNNX_ERR_INVALID_ARG;
+    const size_t es = elem(a->io_dtype), rs = elem(a->res_dtype);
+    if (!on_elem(a->dh, rs) || !on_elem(a->dy, es) || !on_elem(a->dx, es) || !on_elem(a->dgate, es) || !on_elem(a->dresidual, rs) ||
+        !on_elem(a->dpost_weight, 4) || !on_elem(a->dres_scale, 4) || !on_elem(a->dpre_weight, 4) || !on16(a->workspace))
+        return LRNNX_ERR_INVALID_ARG;
+    if (!a->workspace || a->workspace_bytes < lrnnx_block_norm_bwd_workspace_bytes(a->M, a->D)) return LRNNX_ERR_WORKSPACE;
+    NormParams p = norm_params(a);
+    p.dh = a->dh; p.dy = a->dy; p.dh_s = a->dh_stride; p.dy_s = a->dy_stride;
+    p.dx = a->dx; p.dgate = a->dgate; p.dres = a->dresidual;
+    p.dpost = a->dpost_weight; p.dscale = a->dres_scale; p.dpre = a->dpre_weight;
+    p.sums = reinterpret_cast<float *>(a->workspace); p.blocks = norm_bwd_blocks(a->M, a->D);
+    return launch_norm_bwd(p, reinterpret_cast<hipStream_t>(a->stream)) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+}  // extern "C"

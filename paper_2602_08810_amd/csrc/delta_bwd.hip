@@ -1,0 +1,625 @@
+// Gated delta rule, backward.  With the notation of the forward pass, dS1 the gradient of the state after a chunk of 32 steps:
+//     dU  = A^T dO + diag(exp(G_C - G)) K dS1
+//     Z   = ((I + diag(beta) N)^-1)^T dU                                    the gradient of what each step writes;  dV = diag(beta) Z
+//     dS0 = exp(G_C) dS1 + (scale diag(exp G) Q)^T dO - (diag(exp G) K)^T diag(beta) Z
+// k_delta_adjoint walks the chunks backwards with that (the forward states do not enter).  Z, like E, does not depend on where chunks are cut, so
+// k_delta_grads takes slots of 64 steps, all side by side, with the states S0 and dS1 at their ends (D_ij = exp(G_i - G_j)):
+//     F = scale (dO U^T) o D  (j <= i),      H = -(diag(beta) Z U^T) o D  (j < i)
+//     dQ = scale diag(exp G) dO S0^T + F K
+//     dK = -diag(exp G) diag(beta) Z S0^T + (H + H^T) K + F^T Q + diag(exp(G_C - G)) U dS1^T
+//     dbeta_t = z_t . e_t,     dg_t = sum of dG_i over i >= t,
+//     dG_i = sum_j M_ij - sum_j M_ji + q_i . (state part of dQ_i) + k_i . (-.. Z S0^T part) - k_i . (U dS1^T part),   M = F o Q K^T + H o K K^T
+//     and at the slot's last step also the sum of k . (U dS1^T part) and exp(G_C) <S0, dS1>.
+// M is formed once and added to rows and subtracted from columns in float32, so that what cancels in the sums of dG does so exactly.
+#include "delta_common.hpp"
+
+namespace lrnnx {
+
+// ---------------------------------------------------------------- the walk backwards
+// As in the forward walk a wavefront owns 16 columns of dS, and everything it computes of them stays in its registers.
+template <int NPI, int NP, int DK, int NBUF> struct AdjLds {
+    static constexpr int NPA = NPI == 3 ? 3 : 2;
+    struct Buf {
+        uint16_t k[NPI][32][DK + 8], kt[NPI][DK][40], qt[NPI][DK][40];
+        uint16_t t[2][NP][512], a[2][NPA][512];
+        float scal[96];
+    } buf[NBUF];
+};
+
+template <int NPI, int NP, int DK, int NW> __global__ __launch_bounds__(NW * 64) void k_delta_adjoint(const DeltaParams p) {
+    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
+    constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
+    extern __shared__ __align__(16) char lds_raw[];
+    using Lds = AdjLds<NPI, NP, DK, NBUF>;
+    Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row16 = lane & 15, g4 = lane >> 4;
+    const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
+    const DeltaSeq sq = delta_seq(p, b);
+    const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;
+    const bool col_in = n0 < p.dv, mine = c0 < p.dvp;
+    const int64_t nchunk = (sq.len + 31) / 32;
+
+    f32x4 S[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * m + 4 * g4 + r;
+            S[m][r] = p.ds_last && col_in && d < p.dk ? p.ds_last[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] : 0.0f;
+        }
+
+    const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
+    const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + sq.at * p.dout.sl + h * p.dout.sh + (mine ? n0 : 0);
+
+    constexpr int QUADS = 8 * (DK / 4), MATS = (2 * NP + 2 * NPA) * 64;
+    constexpr int IQ = (QUADS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
+    uint2 kreg[IQ][NPI][4], qreg[IQ][NPI][4];
+    uint4 mreg[IM];
+    float sreg[2];
+    uint16_t dreg[NPI][2][4];
+    auto fetch = [&](int64_t ch) {
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+#pragma unroll
+        for (int x = 0; x < IQ; ++x) {
+            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
+            if (QUADS % NT && i >= QUADS) break;
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = 4 * tq + e;
+                    const int64_t row = t0 + (t < n ? t : 0);
+                    kreg[x][pl][e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + row * p.k.sl + 4 * dq);
+                    qreg[x][pl][e] = *reinterpret_cast<const uint2 *>(qp + pl * p.q.plane + row * p.q.sl + 4 * dq);
+                    if (t >= n) kreg[x][pl][e] = qreg[x][pl][e] = make_uint2(0, 0);
+                }
+        }
+        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
+#pragma unroll
+        for (int x = 0; x < IM; ++x) {
+            const int i = tid + x * NT;
+            if (MATS % NT && i >= MATS) break;
+            const uint16_t *from = i < 128 * NP ? p.mat_tt + mat * (2 * NP * 512) + i * 8 : p.mat_at + mat * (2 * NPA * 512) + (i - 128 * NP) * 8;
+            mreg[x] = *reinterpret_cast<const uint4 *>(from);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (tid + x * NT < 96) sreg[x] = p.scal[mat * 96 + tid + x * NT];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * m + 4 * g4 + r;
+#pragma unroll
+                for (int pl = 0; pl < NPI; ++pl) {
+                    dreg[pl][m][r] = dp[pl * p.dout.plane + (t0 + (t < n ? t : 0)) * p.dout.sl];
+                    if (t >= n || !mine) dreg[pl][m][r] = 0;
+                }
+            }
+    };
+    auto put = [&](typename Lds::Buf &B) {
+#pragma unroll
+        for (int x = 0; x < IQ; ++x) {
+            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
+            if (QUADS % NT && i >= QUADS) break;
+            const int col = (dq >> 3) * 32 + quad_place(dq & 7), place = quad_place(tq);
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl) {
+                uint2 c[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
+                transpose_quad(kreg[x][pl], c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
+                transpose_quad(qreg[x][pl], c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.qt[pl][4 * dq + e][place]) = c[e];
+            }
+        }
+        uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
+#pragma unroll
+        for (int x = 0; x < IM; ++x) {
+            const int i = tid + x * NT;
+            if (MATS % NT && i >= MATS) break;
+            mats[i] = mreg[x];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (tid + x * NT < 96) B.scal[tid + x * NT] = sreg[x];
+    };
+
+    if (nchunk > 0) {
+        fetch(nchunk - 1);
+        put(lds.buf[NBUF == 2 ? (nchunk - 1) & 1 : 0]);
+    }
+    __syncthreads();
+    for (int64_t ch = nchunk - 1; ch >= 0; --ch) {
+        const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
+        Frag dof[NPI];
+        f32x4 dO[2] = {};
+#pragma unroll
+        for (int pl = 0; pl < NPI; ++pl) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dO[m][r] += load_io(&dreg[pl][m][r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                dof[pl].u[e] = (uint32_t)dreg[pl][e >> 1][2 * (e & 1)] | (uint32_t)dreg[pl][e >> 1][2 * (e & 1) + 1] << 16;
+        }
+        if (ch > 0) fetch(ch - 1);
+
+        const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
+        if (((ch & 1) || ch == nchunk - 1) && mine) {
+            uint16_t *to = p.dstates + sh * NPS * DK * p.dvp + n0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    uint32_t w[NPS];
+                    split2<NPS>(S[m][r], S[m][r + 1], w);
+#pragma unroll
+                    for (int i = 0; i < NPS; ++i) {
+                        uint16_t *q = to + ((int64_t)i * DK + 16 * m + 4 * g4 + r) * p.dvp;
+                        q[0] = (uint16_t)w[i];
+                        q[p.dvp] = (uint16_t)(w[i] >> 16);
+                    }
+                }
+        }
+        // dU
+        f32x4 X[2] = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag s[NP];
+            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                Frag a[NPI];
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
+                X[m] = mm(a, s, X[m]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f32x4 en = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[m][r] *= en[r];
+            Frag a[NPA];
+#pragma unroll
+            for (int i = 0; i < NPA; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
+            X[m] = mm(a, dof, X[m]);
+        }
+        Frag uf[NP];
+        split_tiles<NP>(X[0], X[1], uf);
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        f32x4 R[2];                                         // exp(G) beta z
+        f32x4 W[2];                                         // scale exp(G) dO
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            Frag t[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) t[i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+            const f32x4 z = mm(t, uf, f32x4{}), zt = mm(uf, t, f32x4{});
+            const int tt = 16 * m + row16;
+            uint32_t lo[NPE], hi[NPE];
+            split2<NPE>(zt[0], zt[1], lo);
+            split2<NPE>(zt[2], zt[3], hi);
+            if (tt < n && mine)
+#pragma unroll
+                for (int i = 0; i < NPE; ++i)
+                    *reinterpret_cast<uint2 *>(p.z + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + tt) * p.Hv + h) * p.dvp + c0 + 4 * g4) = make_uint2(lo[i], hi[i]);
+            const f32x4 be = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]), gam = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { R[m][r] = -gam[r] * be[r] * z[r]; W[m][r] = p.scale * gam[r] * dO[m][r]; }
+        }
+        Frag rf[NP], wf[NP];
+        split_tiles<NP>(R[0], R[1], rf);
+        split_tiles<NP>(W[0], W[1], wf);
+        const float gend = B.scal[31];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            Frag a[NPI], c[NPI];
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                a[i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][8 * g4]);
+                c[i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][16 * m + row16][8 * g4]);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[m][r] *= gend;
+            S[m] = mm(a, rf, S[m]);
+            S[m] = mm(c, wf, S[m]);
+        }
+        if (NBUF == 1) __syncthreads();
+        if (ch > 0) put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0]);
+        __syncthreads();
+    }
+    if (p.ds0 && col_in)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = 16 * m + 4 * g4 + r;
+                if (d < p.dk) p.ds0[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] = S[m][r];
+            }
+}
+
+// ---------------------------------------------------------------- the gradients of a slot
+// A workgroup takes the 64 steps of a slot and a key head, value head by value head; a wavefront owns 16 of the steps, one to a lane of each group
+// of 16, and every product is arranged so that its results lie a step to a lane: gates are a number to a lane, F and H go from one product's
+// results into the next one's operand without leaving the lane, and rows of dQ and dK come out four neighbouring elements at a time.  Both
+// orientations of F and H are computed (one as products with the rows of others, one the other way round), which costs less than turning them.
+template <int NPI, int DK> struct GradLds {
+    uint16_t kt[NPI][DK][72], qt[NPI][DK][72];              // K^T, Q^T, steps placed as results of matrix instructions hold them
+    double G[64];
+    float beta[64], dG[64], ends[4], dots[4];
+};
+
+template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_delta_grads(const DeltaParams p) {
+    constexpr int KS = DK / 32, MT = DK / 16, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, NPF = NPI == 3 ? 3 : 2;
+    extern __shared__ __align__(16) char lds_raw[];
+    GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
+    const int64_t slot = blockIdx.x / (unsigned)p.Hk;
+    const int hk = (int)(blockIdx.x - slot * p.Hk), share = p.Hv / p.Hk;
+    DeltaSeq sq;
+    int64_t t0;
+    int b;
+    const int n = delta_slot(p, slot, sq, t0, b);
+    if (n == 0) return;
+    const int64_t at = sq.at + t0, row0 = sq.row + t0, rows = (int64_t)(p.cu ? 1 : p.B) * p.L;
+    const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
+    const int own = 16 * wave + row16, own_row = own < n ? own : 0;
+    const bool own_in = own < n;
+
+    // K^T and Q^T into LDS: 16 quads of steps by DK / 4 quads of columns
+    for (int i = tid; i < 16 * (DK / 4); i += 256) {
+        const int tq = i / (DK / 4), dq = i % (DK / 4), place = (tq >> 3) * 32 + quad_place(tq & 7);
+#pragma unroll
+        for (int pl = 0; pl < NPI; ++pl) {
+            uint2 kw[4], qw[4], c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = 4 * tq + e;
+                kw[e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + (t < n ? t : 0) * p.k.sl + 4 * dq);
+                qw[e] = *reinterpret_cast<const uint2 *>(qp + pl * p.q.plane + (t < n ? t : 0) * p.q.sl + 4 * dq);
+                if (t >= n) kw[e] = qw[e] = make_uint2(0, 0);
+            }
+            transpose_quad(kw, c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&lds.kt[pl][4 * dq + e][place]) = c[e];
+            transpose_quad(qw, c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&lds.qt[pl][4 * dq + e][place]) = c[e];
+        }
+    }
+    // rows of the slot as operands: step 16 m + row16, terms 32 ks + 8 g4 ..
+    auto rows_of = [&](const uint16_t *base, int64_t plane, int64_t stride, int t, int ks, auto np, Frag *f) {
+        constexpr int P = decltype(np)::value;
+        const bool in = t < n;
+        const uint16_t *q = base + (in ? t : 0) * stride + 32 * ks + 8 * g4;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            f[i].v = *reinterpret_cast<const uint4 *>(q + i * plane);
+            if (!in) f[i].v = make_uint4(0, 0, 0, 0);
+        }
+    };
+    using PI = std::integral_constant<int, NPI>;
+    using PE = std::integral_constant<int, NPE>;
+
+    f32x4 dq[MT], dk[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) dq[m] = dk[m] = f32x4{};
+
+    for (int sh = 0; sh < share; ++sh) {
+        const int h = hk * share + sh;
+        const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
+        const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
+        const int64_t eplane = rows * p.Hv * p.dvp, estride = (int64_t)p.Hv * p.dvp;
+        const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPS * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPS * DK * p.dvp;
+        const int ksv = p.dvp / 32;
+
+        __syncthreads();                                    // the last head's sums have been read; K^T and Q^T are there
+        if (wave == 0) {
+            const bool in = lane < n;
+            const int64_t t = at + (in ? lane : 0);
+            const float gr = load_gate(p.g, sq.ib * p.g_sb + t * p.g_sl + h * p.g_sh, p.io, p.gate_io);
+            const float be = load_gate(p.beta, sq.ib * p.be_sb + t * p.be_sl + h * p.be_sh, p.io, p.gate_io);
+            double G = in ? gate_log(gr) : 0.0;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const double o = __shfl_up(G, m, 64);
+                if (lane >= m) G += o;
+            }
+            lds.G[lane] = G;
+            lds.beta[lane] = in ? be : 0.0f;
+        }
+        __syncthreads();
+        const double Gown = lds.G[own];
+        const float bown = lds.beta[own], gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
+
+        // products over the columns of v: other steps' rows with this lane's step
+        f32x4 P1t[4] = {}, P1[4] = {}, P2t[4] = {}, P2[4] = {};      // dO_own . e_j; dO_i . e_own; z_own . e_j; z_i . e_own
+        float dbeta = 0.0f;
+        for (int ks = 0; ks < ksv; ++ks) {
+            Frag dO[NPI], e[NPE], z[NPE];
+            rows_of(dp, p.dout.plane, p.dout.sl, own, ks, PI(), dO);
+            rows_of(ep, eplane, estride, own, ks, PE(), e);
+            rows_of(zp, eplane, estride, own, ks, PE(), z);
+            f32x4 zs[2] = {}, es[2] = {};
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+#pragma unroll
+                for (int i = NPE - 1; i >= 0; --i) {
+                    zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
+                    es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
+                }
+            // dV = beta z
+            const int c = 32 * ks + 8 * g4;
+            IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + own_row) * p.Hv + h) * p.dv + c;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                f32x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) { dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
+                if (own_in) {
+                    if (p.o_vec && c + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
+                    else
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                if (m <= wave) {
+                    Frag er[NPE];
+                    rows_of(ep, eplane, estride, 16 * m + row16, ks, PE(), er);
+                    P1t[m] = mm(er, dO, P1t[m]);
+                    P2t[m] = mm(er, z, P2t[m]);
+                }
+                if (m >= wave) {
+                    Frag dr[NPI], zr[NPE];
+                    rows_of(dp, p.dout.plane, p.dout.sl, 16 * m + row16, ks, PI(), dr);
+                    rows_of(zp, eplane, estride, 16 * m + row16, ks, PE(), zr);
+                    P1[m] = mm(dr, e, P1[m]);
+                    P2[m] = mm(zr, e, P2[m]);
+                }
+            }
+        }
+        // F, H in both orientations, M's row and column sums
+        float dG = 0.0f;
+        f32x4 HH[4], Ft[4], F[4];
+        f32x4 QKt[4] = {}, QK[4] = {}, KK[4] = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag kf[NPI], qf[NPI];
+            rows_of(kp, p.k.plane, p.k.sl, own, ks, PI(), kf);
+            rows_of(qp, p.q.plane, p.q.sl, own, ks, PI(), qf);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                Frag kr[NPI];
+                rows_of(kp, p.k.plane, p.k.sl, 16 * m + row16, ks, PI(), kr);
+                KK[m] = mm(kr, kf, KK[m]);
+                if (m <= wave) QKt[m] = mm(kr, qf, QKt[m]);
+                if (m >= wave) {
+                    Frag qr[NPI];
+                    rows_of(qp, p.q.plane, p.q.sl, 16 * m + row16, ks, PI(), qr);
+                    QK[m] = mm(qr, kf, QK[m]);
+                }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int o = 16 * m + 4 * g4 + r;
+                const double Go = lds.G[o];
+                const float bo = lds.beta[o];
+                float ft = 0.0f, f = 0.0f, hh = 0.0f;
+                if (o <= own) {                              // this step reads what step o wrote
+                    const float D = __expf((float)(Gown - Go));
+                    ft = p.scale * D * bo * P1t[m][r];
+                    if (o < own) hh = -D * bown * bo * P2t[m][r];
+                    dG += ft * QKt[m][r] + hh * KK[m][r];
+                }
+                if (o >= own) {                              // step o reads what this step wrote
+                    const float D = __expf((float)(Go - Gown));
+                    f = p.scale * D * bown * P1[m][r];
+                    float hx = 0.0f;
+                    if (o > own) hx = -D * bown * bo * P2[m][r];
+                    dG -= f * QK[m][r] + hx * KK[m][r];
+                    hh += hx;
+                }
+                Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
+            }
+        // dQ += F K, dK += (H + H^T) K + F^T Q
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            Frag ft[NPF], f[NPF], hh[NPF];
+            split_tiles<NPF>(Ft[2 * x], Ft[2 * x + 1], ft);
+            split_tiles<NPF>(F[2 * x], F[2 * x + 1], f);
+            split_tiles<NPF>(HH[2 * x], HH[2 * x + 1], hh);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                Frag kt[NPI], qt[NPI];
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.kt[i][16 * m + row16][32 * x + 8 * g4]);
+                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.qt[i][16 * m + row16][32 * x + 8 * g4]);
+                }
+                dq[m] = mm(kt, ft, dq[m]);
+                dk[m] = mm(kt, hh, dk[m]);
+                dk[m] = mm(qt, f, dk[m]);
+            }
+        }
+        // the states' part
+        float ends = 0.0f, sdot = 0.0f;
+        {
+            f32x4 qs[MT], kr[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) qs[m] = kr[m] = f32x4{};
+            for (int ks = 0; ks < ksv; ++ks) {
+                Frag dO[NPI], z[NPE];
+                rows_of(dp, p.dout.plane, p.dout.sl, own, ks, PI(), dO);
+                rows_of(zp, eplane, estride, own, ks, PE(), z);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    Frag s[NPS];
+#pragma unroll
+                    for (int i = 0; i < NPS; ++i) s[i].v = *reinterpret_cast<const uint4 *>(s0p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
+                    qs[m] = mm(s, dO, qs[m]);
+                    kr[m] = mm(s, z, kr[m]);
+                }
+            }
+            const float cq = p.scale * gam, ck = -gam * bown;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                f32x4 qv = {}, kv = {};
+#pragma unroll
+                for (int i = NPI - 1; i >= 0; --i) {
+                    const uint2 a = *reinterpret_cast<const uint2 *>(qp + i * p.q.plane + own_row * p.q.sl + 16 * m + 4 * g4);
+                    const uint2 c = *reinterpret_cast<const uint2 *>(kp + i * p.k.plane + own_row * p.k.sl + 16 * m + 4 * g4);
+                    qv += f32x4{__uint_as_float(a.x << 16), hi_part(__uint_as_float(a.x)), __uint_as_float(a.y << 16), hi_part(__uint_as_float(a.y))};
+                    kv += f32x4{__uint_as_float(c.x << 16), hi_part(__uint_as_float(c.x)), __uint_as_float(c.y << 16), hi_part(__uint_as_float(c.y))};
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float a = cq * qs[m][r], c = ck * kr[m][r];
+                    dq[m][r] += a; dk[m][r] += c;
+                    dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) qs[m] = f32x4{};
+            for (int ks = 0; ks < ksv; ++ks) {
+                Frag e[NPE];
+                rows_of(ep, eplane, estride, own, ks, PE(), e);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    Frag s[NPS];
+#pragma unroll
+                    for (int i = 0; i < NPS; ++i) s[i].v = *reinterpret_cast<const uint4 *>(s1p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
+                    qs[m] = mm(s, e, qs[m]);
+                    if ((m & 3) == wave) {                   // <S0, dS1>: every wavefront a quarter of the rows
+                        Frag o[NPS];
+#pragma unroll
+                        for (int i = 0; i < NPS; ++i) o[i].v = *reinterpret_cast<const uint4 *>(s0p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
+#pragma unroll
+                            for (int i = NPS - 1; i >= 0; --i) {
+                                al += __uint_as_float(s[i].u[x] << 16); ah += hi_part(__uint_as_float(s[i].u[x]));
+                                cl += __uint_as_float(o[i].u[x] << 16); chh += hi_part(__uint_as_float(o[i].u[x]));
+                            }
+                            sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
+                        }
+                    }
+                }
+            }
+            const float cw = en * bown;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                f32x4 kv = {};
+#pragma unroll
+                for (int i = NPI - 1; i >= 0; --i) {
+                    const uint2 c = *reinterpret_cast<const uint2 *>(kp + i * p.k.plane + own_row * p.k.sl + 16 * m + 4 * g4);
+                    kv += f32x4{__uint_as_float(c.x << 16), hi_part(__uint_as_float(c.x)), __uint_as_float(c.y << 16), hi_part(__uint_as_float(c.y))};
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float a = cw * qs[m][r];
+                    dk[m][r] += a;
+                    ends = __builtin_fmaf(kv[r], a, ends);
+                }
+            }
+        }
+        dG -= ends;
+        if (!own_in) { dG = 0.0f; ends = 0.0f; }
+        // over the four lane groups of a step, then over the steps
+#pragma unroll
+        for (int m = 16; m < 64; m <<= 1) {
+            dG += __shfl_xor(dG, m, 64);
+            dbeta += __shfl_xor(dbeta, m, 64);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            ends += __shfl_xor(ends, m, 64);
+            sdot += __shfl_xor(sdot, m, 64);
+        }
+        if (lane < 16) {
+            lds.dG[own] = dG;
+            if (own_in) {
+                const int64_t i = (row0 + own) * p.Hv + h;
+                if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dbeta) + i, dbeta);
+                else store_io(reinterpret_cast<float *>(p.dbeta) + i, dbeta);
+            }
+        }
+        if (lane == 0) { lds.ends[wave] = ends; lds.dots[wave] = sdot; }
+        __syncthreads();
+        if (wave == 0) {
+            float x = lds.dG[lane];
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const float o = __shfl_down(x, m, 64);
+                if (lane + m < 64) x += o;
+            }
+            x += (lds.ends[0] + lds.ends[1]) + (lds.ends[2] + lds.ends[3]);
+            x += __expf((float)lds.G[63]) * ((lds.dots[0] + lds.dots[1]) + (lds.dots[2] + lds.dots[3]));
+            if (lane < n) {
+                const int64_t i = (row0 + lane) * p.Hv + h;
+                if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dg) + i, x);
+                else store_io(reinterpret_cast<float *>(p.dg) + i, x);
+            }
+        }
+    }
+    if (own_in) {
+        IO *qo = reinterpret_cast<IO *>(p.dq) + ((row0 + own) * p.Hk + hk) * p.dk, *ko = reinterpret_cast<IO *>(p.dkk) + ((row0 + own) * p.Hk + hk) * p.dk;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int d = 16 * m + 4 * g4;
+            if (p.dk % 4 == 0 && p.o_vec) {
+                if (d < p.dk) { store4(qo + d, dq[m]); store4(ko + d, dk[m]); }
+            } else
+#pragma unroll
+                for (int r = 0; r < 4; ++r) if (d + r < p.dk) { store_io(qo + d + r, dq[m][r]); store_io(ko + d + r, dk[m][r]); }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- launches
+template <int NPI, int NP, int DK, int NW> static hipError_t launch_adjoint_one(const DeltaParams &p, hipStream_t s) {
+    constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
+    constexpr size_t bytes = sizeof(AdjLds<NPI, NP, DK, NBUF>);
+    static_assert(bytes <= 160 * 1024, "LDS");
+    auto k = k_delta_adjoint<NPI, NP, DK, NW>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)((p.dvp / 16 + NW - 1) / NW), (unsigned)p.Hv, (unsigned)p.B), dim3(NW * 64), bytes, s, p);
+    return hipGetLastError();
+}
+template <int NPI, int NP, int DK> static hipError_t launch_adjoint_dk(const DeltaParams &p, hipStream_t s) {
+    if (p.wave_cols == 8) return launch_adjoint_one<NPI, NP, DK, 8>(p, s);
+    if (p.wave_cols == 4) return launch_adjoint_one<NPI, NP, DK, 4>(p, s);
+    return launch_adjoint_one<NPI, NP, DK, 2>(p, s);
+}
+hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
+    if (!p.io) return p.dk > 64 ? launch_adjoint_dk<3, 3, 128>(p, s) : launch_adjoint_dk<3, 3, 64>(p, s);
+    if (p.np == 3) return p.dk > 64 ? launch_adjoint_dk<1, 3, 128>(p, s) : launch_adjoint_dk<1, 3, 64>(p, s);
+    return p.dk > 64 ? launch_adjoint_dk<1, 2, 128>(p, s) : launch_adjoint_dk<1, 2, 64>(p, s);
+}
+template <class IO, int NPI, int DK> static hipError_t launch_grads_one(const DeltaParams &p, hipStream_t s) {
+    constexpr size_t bytes = sizeof(GradLds<NPI, DK>);
+    static_assert(bytes <= 160 * 1024, "LDS");
+    auto k = k_delta_grads<IO, NPI, DK>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3((unsigned)(p.nslots * p.Hk)), dim3(256), bytes, s, p);
+    return hipGetLastError();
+}
+hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s) {
+    if (!p.io) return p.dk > 64 ? launch_grads_one<float, 3, 128>(p, s) : launch_grads_one<float, 3, 64>(p, s);
+    return p.dk > 64 ? launch_grads_one<uint16_t, 1, 128>(p, s) : launch_grads_one<uint16_t, 1, 64>(p, s);
+}
+
+}  // namespace lrnnx

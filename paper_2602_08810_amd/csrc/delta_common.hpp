@@ -1,0 +1,143 @@
+// Device helpers of the gated delta rule: bfloat16 planes, matrix instructions, sequences and slots.
+//
+// Precision.  Matrix instructions take bfloat16 factors and add in float32.  A float32 number is the sum of three bfloat16 numbers (8 bits
+// of its mantissa each, split by truncation without loss), so a float32 product is six instructions (those of weight 2^-24 and below are left
+// out), and three where one factor is bfloat16 from the start.  At 16 cycles for 16 x 16 x 32 six of them take 96 cycles, the float32 matrix
+// instruction 256.  Where every result is rounded to bfloat16 two planes do (16 bits, relative error 2^-17).
+#pragma once
+#include "delta.hpp"
+#include "scan_common.hpp"
+
+namespace lrnnx {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Operand of a 16 x 16 x 32 matrix product: lane l holds row (or column) l % 16 and eight of the 32 terms of the sum.  Which eight is free as long
+// as both operands agree: operands from memory take them in order (8 (l / 16) ..), operands made from a result take 4 (l / 16) .. + 3 of either
+// half of 16, which is what the lane holds of two result tiles.
+union Frag {
+    uint32_t u[4];
+    uint2 h[2];
+    uint4 v;
+    bf16x8 b;
+};
+
+__device__ __forceinline__ f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
+}
+// product of operands in planes: terms below the smallest plane's weight are left out
+template <int NA, int NB> __device__ __forceinline__ f32x4 mm(const Frag (&a)[NA], const Frag (&b)[NB], f32x4 c) {
+    constexpr int M = NA > NB ? NA : NB;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < M) c = mfma(a[i], b[j], c);
+    return c;
+}
+
+__device__ __forceinline__ float hi_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_hi(float a, float b) {        // the upper halves of two numbers
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ uint32_t pack_rne(float a, float b) {
+    f32x2 x = {a, b};
+    union { bf16x2 b; uint32_t u; } r;
+    r.b = __builtin_convertvector(x, bf16x2);
+    return r.u;
+}
+// two numbers as NP planes: by truncation (exact with three), the last of fewer planes rounded to nearest
+template <int NP> __device__ __forceinline__ void split2(float a, float b, uint32_t (&out)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        if (i == NP - 1 && NP < 3) { out[i] = pack_rne(a, b); break; }
+        out[i] = pack_hi(a, b);
+        if (i < NP - 1) { a -= hi_part(a); b -= hi_part(b); }
+    }
+}
+// two result tiles as the operand of the next product
+template <int NP> __device__ __forceinline__ void split_tiles(const f32x4 &lo, const f32x4 &hi, Frag (&f)[NP]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t w[NP];
+        if (e < 2) split2<NP>(lo[2 * e], lo[2 * e + 1], w);
+        else split2<NP>(hi[2 * e - 4], hi[2 * e - 3], w);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f[i].u[e] = w[i];
+    }
+}
+template <int NP> __device__ __forceinline__ void zero_frags(Frag (&f)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) f[i].v = make_uint4(0, 0, 0, 0);
+}
+
+__device__ __forceinline__ float load_io(const float *p) { return *p; }
+__device__ __forceinline__ float load_io(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ void store_io(float *p, float x) { *p = x; }
+__device__ __forceinline__ void store_io(uint16_t *p, float x) { *p = (uint16_t)pack_rne(x, x); }
+// four elements; `vec`: the address takes one access
+__device__ __forceinline__ void store4(float *p, const f32x4 &x) { *reinterpret_cast<f32x4 *>(p) = x; }
+__device__ __forceinline__ void store4(uint16_t *p, const f32x4 &x) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_rne(x[0], x[1]), pack_rne(x[2], x[3]));
+}
+
+// g or beta of a step, in float32 or in the I/O type
+__device__ __forceinline__ float load_gate(const void *p, int64_t i, int io, int gate_io) {
+    return gate_io && io ? load_io(reinterpret_cast<const uint16_t *>(p) + i) : load_io(reinterpret_cast<const float *>(p) + i);
+}
+
+// Position of terms 4 q .. 4 q + 3 of a block of 32 in a row of LDS: what lane group g reads lies together (4 g .. and 16 + 4 g ..).
+__device__ __forceinline__ int quad_place(int q) { return ((q & 3) * 2 + (q >> 2)) * 4; }
+// four rows of four neighbouring elements -> four columns of four
+__device__ __forceinline__ void transpose_quad(const uint2 (&w)[4], uint2 (&c)[4]) {
+    c[0] = make_uint2(__builtin_amdgcn_perm(w[1].x, w[0].x, 0x05040100u), __builtin_amdgcn_perm(w[3].x, w[2].x, 0x05040100u));
+    c[1] = make_uint2(__builtin_amdgcn_perm(w[1].x, w[0].x, 0x07060302u), __builtin_amdgcn_perm(w[3].x, w[2].x, 0x07060302u));
+    c[2] = make_uint2(__builtin_amdgcn_perm(w[1].y, w[0].y, 0x05040100u), __builtin_amdgcn_perm(w[3].y, w[2].y, 0x05040100u));
+    c[3] = make_uint2(__builtin_amdgcn_perm(w[1].y, w[0].y, 0x07060302u), __builtin_amdgcn_perm(w[3].y, w[2].y, 0x07060302u));
+}
+
+struct DeltaSeq {
+    int64_t at, len;                     // first step on its time axis, steps
+    int64_t slot, row;                   // first slot; first row of the arrays [row, head, column] that the library lays out
+    int64_t ib;                          // batch entry of the caller's tensors
+};
+__device__ __forceinline__ int64_t delta_clamp(int64_t x, int64_t L) { return x < 0 ? 0 : x > L ? L : x; }
+__device__ __forceinline__ DeltaSeq delta_seq(const DeltaParams &p, int b) {
+    DeltaSeq s;
+    if (p.cu) {
+        const int64_t lo = delta_clamp(p.cu[b], p.L), hi = delta_clamp(p.cu[b + 1], p.L);
+        s.at = lo; s.len = hi > lo ? hi - lo : 0; s.slot = lo / kDeltaSlot + b; s.row = lo; s.ib = 0;
+    } else {
+        s.at = 0; s.len = p.L; s.slot = (int64_t)b * p.slots_each; s.row = (int64_t)b * p.L; s.ib = b;
+    }
+    return s;
+}
+// The sequence that a slot of a packed batch belongs to, by a 64-way search of ascending boundaries (whole wavefronts call it).
+__device__ __forceinline__ int delta_find(const DeltaParams &p, int64_t slot) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = p.B;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const bool before = i < hi && (lane == 0 || delta_clamp(p.cu[i], p.L) / kDeltaSlot + i <= slot);
+        const int n = __popcll(__ballot(before));
+        lo = lo + (n - 1) * step;
+        hi = hi < lo + step ? hi : lo + step;
+    }
+    return lo;
+}
+// Steps of a slot: its sequence, its first step within it and how many of the 64 there are (0: none).
+__device__ __forceinline__ int delta_slot(const DeltaParams &p, int64_t slot, DeltaSeq &s, int64_t &t0, int &b) {
+    b = p.cu ? delta_find(p, slot) : (int)(slot / p.slots_each);
+    s = delta_seq(p, b);
+    t0 = (slot - s.slot) * kDeltaSlot;
+    const int64_t n = t0 < 0 ? 0 : s.len - t0;
+    return n <= 0 ? 0 : n > kDeltaSlot ? kDeltaSlot : (int)n;
+}
+
+// Logarithm of a decay: -inf (forget everything) as a number whose sums stay finite; exp of it is 0 all the same.
+__device__ __forceinline__ double gate_log(float g) { return g < -1e5f ? -1e5 : (double)g; }
+
+}  // namespace lrnnx

@@ -1,0 +1,517 @@
+// Gated delta rule, forward.  With G the running sum of the log decays within a chunk of C = 32 steps and S0 the state before it:
+//     N_ij  = exp(G_i - G_j) k_i . k_j   (j < i)          A_ij = scale exp(G_i - G_j) q_i . k_j   (j <= i)
+//     E     = (I + N diag(beta))^-1 (V - diag(exp G) K S0)       the corrections: what the state does not yet say of each value
+//     U     = diag(beta) E
+//     O     = scale diag(exp G) Q S0 + A U
+//     S1    = exp(G_C) S0 + (diag(exp(G_C - G)) K)^T U
+// Every exponent is a sum of log decays, at most 0 for decays: nothing overflows, and differences are taken of sums in double precision.
+// k_delta_prep forms the inverse and A of every chunk, all chunks side by side; k_delta_scan then walks the chunks of a sequence.
+#include "delta_common.hpp"
+
+namespace lrnnx {
+
+// ---------------------------------------------------------------- operands in planes
+// A float32 operand, or rows that are not as the matrix kernels read them (width not padded, unaligned), as planes of aligned rows.
+__global__ __launch_bounds__(256) void k_delta_pack(const DeltaPack p) {
+    const int64_t per_row = (int64_t)p.H * (p.dp / 8), n = (int64_t)p.B * p.L * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per_row;
+        const int rest = (int)(i - row * per_row), h = rest / (p.dp / 8), c = rest % (p.dp / 8) * 8;
+        const int64_t b = row / p.L, t = row - b * p.L, from = b * p.sb + t * p.sl + h * p.sh + c;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = 0.0f;
+            if (c + e < p.d) x[e] = p.io ? load_io(reinterpret_cast<const uint16_t *>(p.src) + from + e)
+                                         : load_io(reinterpret_cast<const float *>(p.src) + from + e);
+        }
+        uint16_t *to = p.dst + (row * p.H + h) * p.dp + c;
+        Frag f[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t w[3];
+            split2<3>(x[2 * e], x[2 * e + 1], w);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) f[k].u[e] = w[k];
+        }
+        for (int k = 0; k < p.planes; ++k) *reinterpret_cast<uint4 *>(to + k * p.plane) = f[k].v;
+    }
+}
+hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s) {
+    const int64_t n = (int64_t)p.B * p.L * p.H * (p.dp / 8), blocks = (n + 255) / 256;
+    hipLaunchKernelGGL(k_delta_pack, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- the matrices of a chunk
+// One wavefront takes a slot (two chunks) of one value head.  Q K^T and K K^T come from matrix instructions on rows read straight from memory;
+// the inverse is solved a column to a lane, row by row (496 multiply-adds a lane, both chunks side by side): substitution is stable where
+// powers of N would cancel.
+template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) void k_delta_prep(const DeltaParams p) {
+    constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2;
+    __shared__ __align__(16) float Ns[2][32][W], As[2][32][W];
+    __shared__ double Gs[64];
+    __shared__ float Bs[64];
+    const int64_t slot = blockIdx.x / (unsigned)p.Hv;
+    const int h = (int)(blockIdx.x - slot * p.Hv), hk = h / (p.Hv / p.Hk);
+    const int lane = threadIdx.x, row16 = lane & 15, g4 = lane >> 4;
+    DeltaSeq sq;
+    int64_t t0;
+    int b;
+    const int n = delta_slot(p, slot, sq, t0, b);
+    if (n == 0) return;
+    const int64_t at = sq.at + t0;
+
+    // running sums of the log decays over each chunk
+    {
+        const bool in = lane < n;
+        const int64_t t = at + (in ? lane : 0);
+        const float gr = load_gate(p.g, sq.ib * p.g_sb + t * p.g_sl + h * p.g_sh, p.io, p.gate_io);
+        const float be = load_gate(p.beta, sq.ib * p.be_sb + t * p.be_sl + h * p.be_sh, p.io, p.gate_io);
+        double G = in ? gate_log(gr) : 0.0;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const double o = __shfl_up(G, m, 32);
+            if ((lane & 31) >= m) G += o;
+        }
+        const double end = __shfl(G, 31, 32);
+        const float bv = in ? be : 0.0f;
+        Gs[lane] = G; Bs[lane] = bv;
+        float *sc = p.scal + ((slot * p.Hv + h) * 2 + (lane >> 5)) * 96 + (lane & 31);
+        sc[0] = __expf((float)G); sc[32] = __expf((float)(end - G)); sc[64] = bv;
+    }
+    __syncthreads();
+
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const uint16_t *kp = p.k.p + sq.ib * p.k.sb + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + hk * p.q.sh;
+        f32x4 kk[3] = {}, qk[3] = {};                     // tiles (0,0), (1,0), (1,1)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag K[2][NPI], Q[2][NPI];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const int t = 32 * c + 16 * m + row16;
+                const bool in = t < n;
+                const int64_t tk = at + (in ? t : 0);
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    K[m][i].v = *reinterpret_cast<const uint4 *>(kp + i * p.k.plane + tk * p.k.sl + 32 * ks + 8 * g4);
+                    Q[m][i].v = *reinterpret_cast<const uint4 *>(qp + i * p.q.plane + tk * p.q.sl + 32 * ks + 8 * g4);
+                }
+                if (!in) { zero_frags(K[m]); zero_frags(Q[m]); }
+            }
+            kk[0] = mm(K[0], K[0], kk[0]); kk[1] = mm(K[1], K[0], kk[1]); kk[2] = mm(K[1], K[1], kk[2]);
+            qk[0] = mm(Q[0], K[0], qk[0]); qk[1] = mm(Q[1], K[0], qk[1]); qk[2] = mm(Q[1], K[1], qk[2]);
+        }
+#pragma unroll
+        for (int x = 0; x < 3; ++x) {
+            const int mi = x > 0, mj = x > 1, j = 16 * mj + row16;
+            const double Gj = Gs[32 * c + j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * mi + 4 * g4 + r;
+                const float d = j <= i ? __expf((float)(Gs[32 * c + i] - Gj)) : 0.0f;
+                Ns[c][i][j] = j < i ? d * kk[x][r] : 0.0f;
+                As[c][i][j] = j <= i ? p.scale * d * qk[x][r] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) As[c][4 * g4 + r][16 + row16] = 0.0f;
+    }
+    __syncthreads();
+
+    const int64_t mat = (slot * p.Hv + h) * 2;
+    auto by_rows = [&](const float (*M)[W], int m, auto np, uint16_t *to) {          // rows of the matrix along the lanes
+        constexpr int P = decltype(np)::value;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(&M[16 * m + row16][4 * g4]);
+        const f32x4 hi = *reinterpret_cast<const f32x4 *>(&M[16 * m + row16][16 + 4 * g4]);
+        Frag f[P];
+        split_tiles<P>(lo, hi, f);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4 *>(to + (m * P + i) * 512 + lane * 8) = f[i].v;
+    };
+    auto by_columns = [&](const float (*M)[W], int m, auto np, uint16_t *to) {       // columns along the lanes
+        constexpr int P = decltype(np)::value;
+        f32x4 lo, hi;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { lo[r] = M[4 * g4 + r][16 * m + row16]; hi[r] = M[16 + 4 * g4 + r][16 * m + row16]; }
+        Frag f[P];
+        split_tiles<P>(lo, hi, f);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4 *>(to + (m * P + i) * 512 + lane * 8) = f[i].v;
+    };
+    using ForA = std::integral_constant<int, NPA>;
+    using ForT = std::integral_constant<int, NP>;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            by_rows(As[c], m, ForA(), p.mat_a + (mat + c) * (2 * NPA * 512));
+            if (ADJ > 0) by_columns(As[c], m, ForA(), p.mat_at + (mat + c) * (2 * NPA * 512));
+        }
+    __syncthreads();
+
+    // X = (I + N diag(beta))^-1 (and (I + diag(beta) N)^-1): lane (c, j) solves for column j of chunk c
+    const int c = lane >> 5, j = lane & 31;
+    {
+        float y[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float acc = 0.0f;
+#pragma unroll
+            for (int l = 0; l < i; ++l) acc = __builtin_fmaf(Ns[c][i][l], y[l], acc);
+            const float x = (i == j ? 1.0f : 0.0f) - acc;
+            y[i] = Bs[32 * c + i] * x;
+            As[c][i][j] = x;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) by_rows(As[cc], m, ForT(), p.mat_t + (mat + cc) * (2 * NP * 512));
+    if constexpr (ADJ > 0) {
+        __syncthreads();
+        float x[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float acc = 0.0f;
+#pragma unroll
+            for (int l = 0; l < i; ++l) acc = __builtin_fmaf(Ns[c][i][l], x[l], acc);
+            x[i] = (i == j ? 1.0f : 0.0f) - Bs[32 * c + i] * acc;
+            As[c][i][j] = x[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) by_columns(As[cc], m, std::integral_constant<int, ADJ>(), p.mat_tt + (mat + cc) * (2 * ADJ * 512));
+    }
+}
+
+// ---------------------------------------------------------------- the walk over the chunks
+// A wavefront owns 16 columns of a head's state, dk x 16 in float32 accumulators, for the whole sequence.  A result tile of a matrix instruction
+// holds a column of four rows in each lane, which is what the second operand of the next instruction wants of its terms, so K S0 -> E -> U ->
+// K^T U runs from registers to registers: no exchange between lanes or wavefronts on the path that the next chunk waits for.  The wavefronts of
+// a workgroup share what is the same for all columns (K, Q, K^T, the chunk's matrices) in LDS.
+template <int NPI, int NP, int DK, int NBUF> struct ScanLds {
+    static constexpr int NPA = NPI == 3 ? 3 : 2;
+    struct Buf {
+        uint16_t k[NPI][32][DK + 8], q[NPI][32][DK + 8], kt[NPI][DK][40];
+        uint16_t t[2][NP][512], a[2][NPA][512];
+        float scal[96];
+    } buf[NBUF];
+};
+
+template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __launch_bounds__(NW * 64) void k_delta_scan(const DeltaParams p) {
+    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
+    constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
+    constexpr int NPO = NPI == 3 ? 3 : 2;                 // planes of what only enters o
+    extern __shared__ __align__(16) char lds_raw[];
+    using Lds = ScanLds<NPI, NP, DK, NBUF>;
+    Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row16 = lane & 15, g4 = lane >> 4;
+    const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
+    const DeltaSeq sq = delta_seq(p, b);
+    const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;     // this wavefront's columns, this lane's
+    const bool col_in = n0 < p.dv;
+    const int64_t nchunk = (sq.len + 31) / 32;
+
+    f32x4 S[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * m + 4 * g4 + r;
+            S[m][r] = p.s0 && col_in && d < p.dk ? p.s0[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] : 0.0f;
+        }
+
+    const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
+    const IO *vp = reinterpret_cast<const IO *>(p.v) + sq.ib * p.v_sb + sq.at * p.v_sl + h * p.v_sh + (col_in ? n0 : 0);
+    IO *op = reinterpret_cast<IO *>(p.o) + sq.ib * p.o_sb + sq.at * p.o_sl + h * p.o_sh + c0 + 4 * g4;
+
+    // what a thread brings into LDS
+    constexpr int QUADS = 8 * (DK / 4), QROWS = 32 * (DK / 8), MATS = (2 * NP + 2 * NPA) * 64;
+    constexpr int IQ = (QUADS + NT - 1) / NT, IR = (QROWS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
+    uint2 kreg[IQ][NPI][4];
+    uint4 qreg[IR][NPI], mreg[IM];
+    float sreg[2];
+    IO vreg[2][4];
+    auto fetch = [&](int64_t ch) {
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+#pragma unroll
+        for (int x = 0; x < IQ; ++x) {
+            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
+            if (QUADS % NT && i >= QUADS) break;
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = 4 * tq + e;
+                    kreg[x][pl][e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + (t0 + (t < n ? t : 0)) * p.k.sl + 4 * dq);
+                    if (t >= n) kreg[x][pl][e] = make_uint2(0, 0);
+                }
+        }
+#pragma unroll
+        for (int x = 0; x < IR; ++x) {
+            const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
+            if (QROWS % NT && i >= QROWS) break;
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl) {
+                qreg[x][pl] = *reinterpret_cast<const uint4 *>(qp + pl * p.q.plane + (t0 + (t < n ? t : 0)) * p.q.sl + 8 * d8);
+                if (t >= n) qreg[x][pl] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
+#pragma unroll
+        for (int x = 0; x < IM; ++x) {
+            const int i = tid + x * NT;
+            if (MATS % NT && i >= MATS) break;
+            const uint16_t *from = i < 128 * NP ? p.mat_t + mat * (2 * NP * 512) + i * 8 : p.mat_a + mat * (2 * NPA * 512) + (i - 128 * NP) * 8;
+            mreg[x] = *reinterpret_cast<const uint4 *>(from);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (tid + x * NT < 96) sreg[x] = p.scal[mat * 96 + tid + x * NT];
+    };
+    auto put = [&](typename Lds::Buf &B) {
+#pragma unroll
+        for (int x = 0; x < IQ; ++x) {
+            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
+            if (QUADS % NT && i >= QUADS) break;
+            const int col = (dq >> 3) * 32 + quad_place(dq & 7);
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl) {
+                const uint2 *w = kreg[x][pl];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = w[e];
+                uint2 c[4];
+                transpose_quad(kreg[x][pl], c);
+                const int place = quad_place(tq);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < IR; ++x) {
+            const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
+            if (QROWS % NT && i >= QROWS) break;
+            const int q0 = (2 * d8) & 7, base = (d8 >> 2) * 32;
+#pragma unroll
+            for (int pl = 0; pl < NPI; ++pl) {
+                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0)]) = make_uint2(qreg[x][pl].x, qreg[x][pl].y);
+                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0 + 1)]) = make_uint2(qreg[x][pl].z, qreg[x][pl].w);
+            }
+        }
+        uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
+#pragma unroll
+        for (int x = 0; x < IM; ++x) {
+            const int i = tid + x * NT;
+            if (MATS % NT && i >= MATS) break;
+            mats[i] = mreg[x];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (tid + x * NT < 96) B.scal[tid + x * NT] = sreg[x];
+    };
+    auto fetch_v = [&](int64_t ch) {
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * m + 4 * g4 + r;
+                vreg[m][r] = vp[(t0 + (t < n ? t : 0)) * p.v_sl];
+                if (t >= n || !col_in) vreg[m][r] = 0;
+            }
+    };
+
+    if (nchunk > 0) {
+        fetch(0);
+        fetch_v(0);
+        put(lds.buf[0]);
+    }
+    __syncthreads();
+    for (int64_t ch = 0; ch < nchunk; ++ch) {
+        const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
+        f32x4 V[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) V[m][r] = load_io(&vreg[m][r]);
+        if (ch + 1 < nchunk) { fetch(ch + 1); fetch_v(ch + 1); }
+
+        const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
+        if (SAVE && !(ch & 1) && c0 < p.dvp) {
+            uint16_t *to = p.states + sh * NPS * DK * p.dvp + n0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    uint32_t w[NPS];
+                    split2<NPS>(S[m][r], S[m][r + 1], w);
+#pragma unroll
+                    for (int i = 0; i < NPS; ++i) {
+                        uint16_t *q = to + ((int64_t)i * DK + 16 * m + 4 * g4 + r) * p.dvp;
+                        q[0] = (uint16_t)w[i];
+                        q[p.dvp] = (uint16_t)(w[i] >> 16);
+                    }
+                }
+        }
+
+        // K S0 and (transposed: a step to a lane) Q S0
+        f32x4 P[2] = {}, O[2] = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag s[NP], so[NPO];
+            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s);
+#pragma unroll
+            for (int i = 0; i < NPO; ++i) so[i] = s[i < NP ? i : NP - 1];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                Frag a[NPI], c[NPI];
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    a[i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
+                    c[i].v = *reinterpret_cast<const uint4 *>(&B.q[i][16 * m + row16][32 * ks + 8 * g4]);
+                }
+                P[m] = mm(a, s, P[m]);
+                O[m] = mm(so, c, O[m]);
+            }
+        }
+        // E = (I + N beta)^-1 (V - exp(G) K S0)
+        f32x4 R[2], E[2] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f32x4 gam = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[r], P[m][r], V[m][r]);
+        }
+        Frag rf[NP];
+        split_tiles<NP>(R[0], R[1], rf);
+        f32x4 Et[2] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            Frag t[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) t[i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+            E[m] = mm(t, rf, E[m]);
+            if (SAVE) Et[m] = mm(rf, t, Et[m]);                        // a step to a lane, for wide stores
+        }
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        if (SAVE && c0 < p.dvp) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const int t = 16 * m + row16;
+                uint32_t lo[NPE], hi[NPE];
+                split2<NPE>(Et[m][0], Et[m][1], lo);
+                split2<NPE>(Et[m][2], Et[m][3], hi);
+                if (t < n)
+#pragma unroll
+                    for (int i = 0; i < NPE; ++i)
+                        *reinterpret_cast<uint2 *>(p.err + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + t) * p.Hv + h) * p.dvp + c0 + 4 * g4) =
+                            make_uint2(lo[i], hi[i]);
+            }
+        }
+        // U = beta E, and U decayed to the end of the chunk
+        f32x4 U[2], D[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const f32x4 be = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]);
+            const f32x4 en = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { U[m][r] = be[r] * E[m][r]; D[m][r] = en[r] * U[m][r]; }
+        }
+        Frag uf[NPO], df[NP];
+        split_tiles<NPO>(U[0], U[1], uf);
+        split_tiles<NP>(D[0], D[1], df);
+        // S1
+        const float gend = B.scal[31];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            Frag a[NPI];
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][8 * g4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[m][r] *= gend;
+            S[m] = mm(a, df, S[m]);
+        }
+        // O
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            Frag a[NPA];
+#pragma unroll
+            for (int i = 0; i < NPA; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
+            const float gam = p.scale * B.scal[16 * m + row16];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) O[m][r] *= gam;
+            O[m] = mm(uf, a, O[m]);
+            const int t = 16 * m + row16, left = p.dv - c0 - 4 * g4;
+            if (t < n) {
+                IO *to = op + (t0 + t) * p.o_sl;
+                if (p.o_vec && left >= 4) store4(to, O[m]);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (r < left) store_io(to + r, O[m][r]);
+            }
+        }
+        if (NBUF == 1) __syncthreads();
+        if (ch + 1 < nchunk) put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0]);
+        __syncthreads();
+    }
+    if (p.s_last && col_in)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = 16 * m + 4 * g4 + r;
+                if (d < p.dk) p.s_last[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] = S[m][r];
+            }
+}
+
+// ---------------------------------------------------------------- launches
+template <int NPI, int NP, int ADJ> static hipError_t launch_prep(const DeltaParams &p, hipStream_t s) {
+    const dim3 grid((unsigned)(p.nslots * p.Hv)), block(64);
+    if (p.dk > 64) hipLaunchKernelGGL((k_delta_prep<NPI, NP, 128, ADJ>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_delta_prep<NPI, NP, 64, ADJ>), grid, block, 0, s, p);
+    return hipGetLastError();
+}
+hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s) {
+    if (!p.io) return p.mat_tt ? launch_prep<3, 3, 3>(p, s) : launch_prep<3, 3, 0>(p, s);
+    if (!p.mat_tt) return p.np == 3 ? launch_prep<1, 3, 0>(p, s) : launch_prep<1, 2, 0>(p, s);
+    if (p.np_adjoint == 3) return launch_prep<1, 3, 3>(p, s);
+    return p.np == 3 ? launch_prep<1, 3, 2>(p, s) : launch_prep<1, 2, 2>(p, s);
+}
+
+template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> static hipError_t launch_scan_one(const DeltaParams &p, hipStream_t s) {
+    constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
+    constexpr size_t bytes = sizeof(ScanLds<NPI, NP, DK, NBUF>);
+    static_assert(bytes <= 160 * 1024, "LDS");
+    auto k = k_delta_scan<IO, NPI, NP, DK, NW, SAVE>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((p.dvp / 16 + NW - 1) / NW), (unsigned)p.Hv, (unsigned)p.B);
+    hipLaunchKernelGGL(k, grid, dim3(NW * 64), bytes, s, p);
+    return hipGetLastError();
+}
+template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
+    if (p.states) {
+        if (p.wave_cols == 8) return launch_scan_one<IO, NPI, NP, DK, 8, true>(p, s);
+        if (p.wave_cols == 4) return launch_scan_one<IO, NPI, NP, DK, 4, true>(p, s);
+        return launch_scan_one<IO, NPI, NP, DK, 2, true>(p, s);
+    }
+    if (p.wave_cols == 8) return launch_scan_one<IO, NPI, NP, DK, 8, false>(p, s);
+    if (p.wave_cols == 4) return launch_scan_one<IO, NPI, NP, DK, 4, false>(p, s);
+    return launch_scan_one<IO, NPI, NP, DK, 2, false>(p, s);
+}
+hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s) {
+    if (!p.io) return p.dk > 64 ? launch_scan_dk<float, 3, 3, 128>(p, s) : launch_scan_dk<float, 3, 3, 64>(p, s);
+    if (p.np == 3) return p.dk > 64 ? launch_scan_dk<uint16_t, 1, 3, 128>(p, s) : launch_scan_dk<uint16_t, 1, 3, 64>(p, s);
+    return p.dk > 64 ? launch_scan_dk<uint16_t, 1, 2, 128>(p, s) : launch_scan_dk<uint16_t, 1, 2, 64>(p, s);
+}
+
+}  // namespace lrnnx
