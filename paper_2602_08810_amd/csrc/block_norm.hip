@@ -13,78 +13,69 @@
 
 namespace lrnnx {
 
-template <class T, int VEC> struct Piece;        // VEC neighbouring elements as one access
-template <> struct Piece<float, 4> {
-    static __device__ __forceinline__ void load(const float *p, float (&x)[4]) { const f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+// VEC neighbouring elements as one access, as they lie in memory (so that a row can be on its way while the one before is worked on) and in float32
+template <class T, int VEC> struct Piece {
+    static constexpr int W = VEC * (int)sizeof(T) / 4;            // words
+    uint32_t w[W > 0 ? W : 1];
+    __device__ __forceinline__ void load(Buffer b, uint32_t off) {
+        if constexpr (W == 0) w[0] = __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0);
+        else if constexpr (W == 1) w[0] = __builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0);
+        else if constexpr (W == 2) { const uint2 v = buffer_load8(b, off); w[0] = v.x; w[1] = v.y; }
+        else
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = v[e]; }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[4]) { *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]}; }
-};
-template <> struct Piece<uint16_t, 4> {
-    static __device__ __forceinline__ void load(const uint16_t *p, float (&x)[4]) {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        x[0] = __uint_as_float(v.x << 16); x[1] = hi_part(__uint_as_float(v.x)); x[2] = __uint_as_float(v.y << 16); x[3] = hi_part(__uint_as_float(v.y));
+            for (int i = 0; i < W; i += 4) {
+                const uint4 v = buffer_load16(b, off + 4 * i);
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
     }
-    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[4]) {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(pack_rne(x[0], x[1]), pack_rne(x[2], x[3]));
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     }
-};
-template <class T> struct Piece<T, 8> {
-    static __device__ __forceinline__ void load(const T *p, float (&x)[8]) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(p);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    static __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {
+        if constexpr (VEC == 1) store_io(p, x[0]);
+        else if constexpr (sizeof(T) == 4)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(w[e] << 16); x[2 * e + 1] = hi_part(__uint_as_float(w[e])); }
-        } else {
-            float a[4], b[4];
-            Piece<float, 4>::load(p, a); Piece<float, 4>::load(p + 4, b);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-        }
+            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<f32x4 *>(p + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        else if constexpr (VEC == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_rne(x[0], x[1]), pack_rne(x[2], x[3]));
+        else *reinterpret_cast<uint4 *>(p) = make_uint4(pack_rne(x[0], x[1]), pack_rne(x[2], x[3]), pack_rne(x[4], x[5]), pack_rne(x[6], x[7]));
     }
-    static __device__ __forceinline__ void store(T *p, const float (&x)[8]) {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4 *>(p) = make_uint4(pack_rne(x[0], x[1]), pack_rne(x[2], x[3]), pack_rne(x[4], x[5]), pack_rne(x[6], x[7]));
-        } else {
-            Piece<float, 4>::store(p, {x[0], x[1], x[2], x[3]});
-            Piece<float, 4>::store(p + 4, {x[4], x[5], x[6], x[7]});
-        }
-    }
-};
-template <class T> struct Piece<T, 1> {
-    static __device__ __forceinline__ void load(const T *p, float (&x)[1]) { x[0] = load_io(p); }
-    static __device__ __forceinline__ void store(T *p, const float (&x)[1]) { store_io(p, x[0]); }
 };
 
+// Sum over the wavefront, the same number in every lane: moves within rows of 16 lanes and from row to row, no LDS.
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m, 64);
-    return x;
+    x += dpp<0x111>(0.0f, x);                     // from 1, 2, 4, 8 lanes below within a row
+    x += dpp<0x112>(0.0f, x);
+    x += dpp<0x114>(0.0f, x);
+    x += dpp<0x118>(0.0f, x);
+    x += dpp<0x142, 0xA>(0.0f, x);                // the last lane of a row to the next, into rows 1 and 3
+    x += dpp<0x143, 0xC>(0.0f, x);                // and of the lower half to the upper
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
 }
-// Sum over the workgroup; `part`: a float of LDS per wavefront, free again after the next barrier.
+// Sum over the workgroup.  `part`: a float of LDS for each of eight wavefronts, taken in turn from a set (`Sums`) that is large enough for a
+// slot not to be written again before a barrier has passed since it was read: one barrier a sum.
 __device__ __forceinline__ float block_sum(float x, float *part) {
     x = wave_sum(x);
     const int waves = blockDim.x >> 6;
     if (waves == 1) return x;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float s = 0.0f;
-    for (int w = 0; w < waves; ++w) s += part[w];
-    __syncthreads();
+    lds_barrier();
+    float s = part[0];
+    for (int w = 1; w < waves; ++w) s += part[w];
     return s;
 }
+constexpr int kSumSlots = 8;                      // four sums a row, two rows
 
 // How the sum over a group is taken: over the workgroup (one group), over `lanes` neighbouring lanes (a power of two), or through LDS.
 enum : int { GROUP_ROW = 0, GROUP_LANES = 1, GROUP_LDS = 2 };
 
 // Sums over each thread's groups of `x[i]` (piece i of the row lies in one group), into x.
-template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], int how, int pieces, int per_group, float *lds) {
+template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], int how, int pieces, int per_group, float *lds, float *part) {
     if (how == GROUP_ROW) {
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) s += x[i];
-        s = block_sum(s, lds);
+        s = block_sum(s, part);
 #pragma unroll
         for (int i = 0; i < NV; ++i) x[i] = s;
     } else if (how == GROUP_LANES) {
@@ -95,56 +86,115 @@ template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], int
         const int nt = blockDim.x, groups = pieces / per_group;
 #pragma unroll
         for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; if (v < pieces) lds[v] = x[i]; }
-        __syncthreads();
+        lds_barrier();
         float *out = lds + pieces;
-        for (int g = threadIdx.x; g < groups; g += nt) {
-            float s = 0.0f;
-            for (int j = 0; j < per_group; ++j) s += lds[g * per_group + j];
-            out[g] = s;
-        }
-        __syncthreads();
+        if (per_group < 64)                       // a thread or a wavefront a group
+            for (int g = threadIdx.x; g < groups; g += nt) {
+                float s = 0.0f;
+                for (int j = 0; j < per_group; ++j) s += lds[g * per_group + j];
+                out[g] = s;
+            }
+        else
+            for (int g = threadIdx.x >> 6; g < groups; g += nt >> 6) {
+                float s = 0.0f;
+                for (int j = threadIdx.x & 63; j < per_group; j += 64) s += lds[g * per_group + j];
+                s = wave_sum(s);
+                if ((threadIdx.x & 63) == 0) out[g] = s;
+            }
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; x[i] = v < pieces ? out[v / per_group] : 0.0f; }
-        __syncthreads();
+        lds_barrier();
     }
 }
 
 template <bool FINE> __device__ __forceinline__ void gate_of(float z, int act, float &a, float &da) {
-    const float s = 1.0f / (1.0f + (FINE ? expf(-z) : __expf(-z)));
+    const float s = __builtin_amdgcn_rcpf(1.0f + (FINE ? expf(-z) : __expf(-z)));
     if (act) { a = s; da = s * (1.0f - s); }
     else { a = z * s; da = s * (1.0f + z * (1.0f - s)); }
 }
 
-template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bounds__(512) void k_block_norm(const NormParams p, int how) {
-    extern __shared__ float lds[];
-    const int nt = blockDim.x, pieces = p.D / VEC, per_group = p.width / VEC;
-    float *part = lds;
-    float w1[BWD ? NV : 1][VEC] = {}, w2[BWD ? NV : 1][VEC] = {}, w3[BWD ? NV : 1][VEC] = {};
-    const float by_width = 1.0f / (float)p.width, by_D = 1.0f / (float)p.D;
-    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
-        float x[NV][VEC], z[NV][VEC], r[NV][VEC], act[NV][VEC], r1[NV];
-        float dh[BWD ? NV : 1][VEC], dy[BWD ? NV : 1][VEC];
+// The row that a workgroup takes next, on its way from memory while it works on this one.  All loads go through buffer descriptors: what is past the
+// row, past the last row or not given at all reads as zero, with no branch in which the loads would have to be waited for.
+template <class IO, class RES, int VEC, int NV, bool BWD> struct NormRow {
+    Piece<IO, VEC> x[NV], z[NV], dy[BWD ? NV : 1];
+    Piece<RES, VEC> r[NV], dh[BWD ? NV : 1];
+    template <class T> static __device__ __forceinline__ Buffer row_of(const NormParams &p, const void *base, int64_t stride, int64_t row) {
+        return buffer_of(reinterpret_cast<const T *>(base) + row * stride, base && row < p.M ? p.D * (int)sizeof(T) : 0);
+    }
+    __device__ __forceinline__ void load(const NormParams &p, int64_t row) {
+        const Buffer bx = row_of<IO>(p, p.x, p.x_s, row), bz = row_of<IO>(p, p.gate, p.gate_s, row), br = row_of<RES>(p, p.res, p.res_s, row);
+        const Buffer bh = row_of<RES>(p, p.dh, p.dh_s, row), by = row_of<IO>(p, p.dy, p.dy_s, row);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = threadIdx.x + i * nt;
-            const bool in = v < pieces;
+            const uint32_t c = (threadIdx.x + i * blockDim.x) * VEC;
+            x[i].load(bx, c * sizeof(IO));
+            z[i].load(bz, c * sizeof(IO));
+            r[i].load(br, c * sizeof(RES));
+            if constexpr (BWD) { dh[i].load(bh, c * sizeof(RES)); dy[i].load(by, c * sizeof(IO)); }
+        }
+    }
+};
+
+template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bounds__(512) void k_block_norm(const NormParams p, int how) {
+    extern __shared__ __align__(16) float lds[];
+    const int nt = blockDim.x, pieces = p.D / VEC, per_group = p.width / VEC;
+    // LDS: slots of sums, the weights (a wait for them from memory would be a wait for the next row too), sums of groups
+    float *const w_post = lds + kSumSlots * 8, *const w_scale = w_post + (p.post ? p.post_shared ? (p.width + 3) & ~3 : (p.D + 3) & ~3 : 0);
+    float *const w_pre = w_scale + (p.scale ? (p.D + 3) & ~3 : 0), *const wide = w_pre + (p.pre ? (p.D + 3) & ~3 : 0);
+    int turn = 0;
+    auto slot = [&]() { turn = (turn + 1) % kSumSlots; return lds + turn * 8; };
+    float w1[BWD ? NV : 1][VEC] = {}, w2[BWD ? NV : 1][VEC] = {}, w3[BWD ? NV : 1][VEC] = {};
+    const float by_width = 1.0f / (float)p.width, by_D = 1.0f / (float)p.D;
+    int cp[NV];                                   // where a piece's part of post_weight starts
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) x[i][e] = z[i][e] = r[i][e] = 0.0f;
-            if (BWD)
+    for (int i = 0; i < NV; ++i) { const int c = (threadIdx.x + i * nt) * VEC; cp[i] = c >= p.D ? 0 : p.post_shared ? c % p.width : c; }
+    struct Weight { float w[VEC]; __device__ __forceinline__ float get(int e) const { return w[e]; } };
+    auto weight = [&](const float *w, int c) {
+        Weight r;
+        if (c >= p.D) c = 0;
+        if constexpr (VEC == 1) r.w[0] = w[c];
+        else
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) dh[i][e] = dy[i][e] = 0.0f;
-            if (in) {
-                const int64_t c = (int64_t)v * VEC;
-                Piece<IO, VEC>::load(reinterpret_cast<const IO *>(p.x) + row * p.x_s + c, x[i]);
-                if (p.gate) Piece<IO, VEC>::load(reinterpret_cast<const IO *>(p.gate) + row * p.gate_s + c, z[i]);
-                if (p.res) Piece<RES, VEC>::load(reinterpret_cast<const RES *>(p.res) + row * p.res_s + c, r[i]);
-                if constexpr (BWD) {
-                    if (p.dh) Piece<RES, VEC>::load(reinterpret_cast<const RES *>(p.dh) + row * p.dh_s + c, dh[i]);
-                    if (p.dy) Piece<IO, VEC>::load(reinterpret_cast<const IO *>(p.dy) + row * p.dy_s + c, dy[i]);
-                }
+            for (int e = 0; e < VEC; e += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(w + c + e);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) r.w[e + f] = v[f];
+            }
+        return r;
+    };
+    using Row = NormRow<IO, RES, VEC, NV, BWD>;
+    Row even, odd;
+    int64_t row = blockIdx.x;
+    even.load(p, row);
+    {
+        const Buffer bp = buffer_of(p.post, p.post ? (p.post_shared ? p.width : p.D) * 4 : 0), bs = buffer_of(p.scale, p.scale ? p.D * 4 : 0),
+                     br = buffer_of(p.pre, p.pre ? p.D * 4 : 0);
+        Piece<float, VEC> a[NV], b[NV], c[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t off = (threadIdx.x + i * nt) * VEC * 4;
+            a[i].load(bp, off); b[i].load(bs, off); c[i].load(br, off);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = (threadIdx.x + i * nt) * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                if (p.post && at < (p.post_shared ? p.width : p.D)) w_post[at + e] = a[i].get(e);
+                if (p.scale && at < p.D) w_scale[at + e] = b[i].get(e);
+                if (p.pre && at < p.D) w_pre[at + e] = c[i].get(e);
             }
         }
-        // n (in x), and h
+    }
+    lds_barrier();
+    auto take = [&](const Row &in) __attribute__((always_inline)) {
+        float x[NV][VEC], r1[NV], h[NV][VEC], ss = 0.0f;
+        float act[BWD ? NV : 1][VEC], dact[BWD ? NV : 1][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[i][e] = in.x[i].get(e);
         if (p.post) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -152,112 +202,162 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) r1[i] = __builtin_fmaf(x[i][e], x[i][e], r1[i]);
             }
-            group_sums<NV>(r1, how, pieces, per_group, part);
+            group_sums<NV>(r1, how, pieces, per_group, wide, slot());
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                r1[i] = 1.0f / sqrtf(__builtin_fmaf(r1[i], by_width, p.eps));
+                r1[i] = __builtin_amdgcn_rsqf(__builtin_fmaf(r1[i], by_width, p.eps));
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) x[i][e] *= r1[i];
+                for (int e = 0; e < VEC; ++e) x[i][e] *= r1[i];                  // n
             }
         }
-        float h[NV][VEC], ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = threadIdx.x + i * nt, c = v * VEC;
-            if (v < pieces) {
-                const int cp = p.post_shared ? c % p.width : c;
+            const int c = (threadIdx.x + i * nt) * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) h[i][e] = x[i][e];
+            if (p.post) {
+                const auto w = weight(w_post, cp[i]);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) h[i][e] *= w.get(e);
+            }
+            if (p.gate)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    float m = p.post ? p.post[cp + e] * x[i][e] : x[i][e];
-                    if (p.gate) { float da; gate_of<sizeof(IO) == 4>(z[i][e], p.gate_act, act[i][e], da); m *= act[i][e]; if (BWD) z[i][e] = da; }
-                    if (p.scale) m *= p.scale[c + e];
-                    h[i][e] = r[i][e] + m;
-                    ss = __builtin_fmaf(h[i][e], h[i][e], ss);
+                    float a, da;
+                    gate_of<sizeof(IO) == 4>(in.z[i].get(e), p.gate_act, a, da);
+                    h[i][e] *= a;
+                    if constexpr (BWD) { act[i][e] = a; dact[i][e] = da; }
                 }
+            else if constexpr (BWD)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) { act[i][e] = 1.0f; dact[i][e] = 0.0f; }
+            if (p.scale) {
+                const auto w = weight(w_scale, c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) h[i][e] *= w.get(e);
             }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { h[i][e] += in.r[i].get(e); ss = __builtin_fmaf(h[i][e], h[i][e], ss); }
         }
         float r2 = 0.0f;
-        if (p.pre) r2 = 1.0f / sqrtf(__builtin_fmaf(block_sum(ss, part), by_D, p.eps));
+        if (p.pre) r2 = __builtin_amdgcn_rsqf(__builtin_fmaf(block_sum(ss, slot()), by_D, p.eps));
         if constexpr (!BWD) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int v = threadIdx.x + i * nt, c = v * VEC;
-                if (v < pieces) {
+                const int c = (threadIdx.x + i * nt) * VEC;
+                if (c < p.D) {
                     Piece<RES, VEC>::store(reinterpret_cast<RES *>(p.h) + row * p.D + c, h[i]);
                     if (p.pre) {
+                        const auto w = weight(w_pre, c);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) h[i][e] *= r2 * p.pre[c + e];
+                        for (int e = 0; e < VEC; ++e) h[i][e] *= r2 * w.get(e);
                         Piece<IO, VEC>::store(reinterpret_cast<IO *>(p.y) + row * p.D + c, h[i]);
                     }
                 }
             }
         } else {
+            float g[NV][VEC];                         // the gradient on its way down: of y, h, m, n
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) g[i][e] = in.dh[i].get(e);
             if (p.pre) {
                 float dot = 0.0f;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    const int v = threadIdx.x + i * nt, c = v * VEC;
-                    if (v < pieces)
+                    const auto w = weight(w_pre, (threadIdx.x + i * nt) * VEC);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            h[i][e] *= r2;                                       // n2
-                            w3[i][e] = __builtin_fmaf(dy[i][e], h[i][e], w3[i][e]);
-                            dy[i][e] *= p.pre[c + e];
-                            dot = __builtin_fmaf(dy[i][e], h[i][e], dot);
-                        }
+                    for (int e = 0; e < VEC; ++e) {
+                        const float d = in.dy[i].get(e);
+                        h[i][e] *= r2;                                           // n2
+                        w3[i][e] = __builtin_fmaf(d, h[i][e], w3[i][e]);
+                        dot = __builtin_fmaf(d * w.get(e), h[i][e], dot);
+                    }
                 }
-                dot = block_sum(dot, part) * by_D;
+                dot = block_sum(dot, slot()) * by_D;
+                const float cd = p.D == 1 ? p.eps * r2 * r2 * r2 : r2, ch = p.D == 1 ? 0.0f : r2 * dot;
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (threadIdx.x + i * nt < pieces)
+                for (int i = 0; i < NV; ++i) {
+                    const auto w = weight(w_pre, (threadIdx.x + i * nt) * VEC);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e)
-                            dh[i][e] = __builtin_fmaf(r2, p.D == 1 ? dy[i][e] * p.eps * r2 * r2 : __builtin_fmaf(-h[i][e], dot, dy[i][e]), dh[i][e]);
+                    for (int e = 0; e < VEC; ++e) {
+                        g[i][e] = __builtin_fmaf(cd * w.get(e), in.dy[i].get(e), __builtin_fmaf(-ch, h[i][e], g[i][e]));
+                    }
+                }
             }
             float dots[NV];
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int v = threadIdx.x + i * nt, c = v * VEC;
+                const int c = (threadIdx.x + i * nt) * VEC;
                 dots[i] = 0.0f;
-                if (v < pieces) {
-                    if (p.dres) Piece<RES, VEC>::store(reinterpret_cast<RES *>(p.dres) + row * p.D + c, dh[i]);
-                    const int cp = p.post_shared ? c % p.width : c;
+                if (c < p.D) {
+                    if (p.dres) Piece<RES, VEC>::store(reinterpret_cast<RES *>(p.dres) + row * p.D + c, g[i]);
+                    Weight wp, ws;
+                    if (p.post) wp = weight(w_post, cp[i]);
+                    if (p.scale) ws = weight(w_scale, c);
                     float dz[VEC];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const float w = p.post ? p.post[cp + e] : 1.0f, m = w * x[i][e], a = p.gate ? act[i][e] : 1.0f;
-                        float dp = dh[i][e];
-                        if (p.scale) { w2[i][e] = __builtin_fmaf(dp, m * a, w2[i][e]); dp *= p.scale[c + e]; }
-                        dz[e] = p.gate ? dp * m * z[i][e] : 0.0f;
+                        const float w = p.post ? wp.get(e) : 1.0f, m = w * x[i][e];
+                        const float a = act[i][e];
+                        float dp = g[i][e];
+                        if (p.scale) { w2[i][e] = __builtin_fmaf(dp, m * a, w2[i][e]); dp *= ws.get(e); }
+                        dz[e] = dp * m * dact[i][e];
                         dp *= a;
                         if (p.post) w1[i][e] = __builtin_fmaf(dp, x[i][e], w1[i][e]);
-                        dh[i][e] = dp * w;
-                        dots[i] = __builtin_fmaf(dh[i][e], x[i][e], dots[i]);
+                        g[i][e] = dp * w;
+                        dots[i] = __builtin_fmaf(g[i][e], x[i][e], dots[i]);
                     }
                     if (p.dgate) Piece<IO, VEC>::store(reinterpret_cast<IO *>(p.dgate) + row * p.D + c, dz);
                 }
             }
-            if (p.post) group_sums<NV>(dots, how, pieces, per_group, part);
+            if (p.post) group_sums<NV>(dots, how, pieces, per_group, wide, slot());
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int v = threadIdx.x + i * nt, c = v * VEC;
-                if (v < pieces) {
-                    if (p.post)
+                const int c = (threadIdx.x + i * nt) * VEC;
+                if (c < p.D) {
+                    if (p.post) {
+                        const float cg = p.width == 1 ? p.eps * r1[i] * r1[i] * r1[i] : r1[i], cx = p.width == 1 ? 0.0f : r1[i] * dots[i] * by_width;
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e)
-                            dh[i][e] = r1[i] * (p.width == 1 ? dh[i][e] * p.eps * r1[i] * r1[i] : __builtin_fmaf(-x[i][e], dots[i] * by_width, dh[i][e]));
-                    Piece<IO, VEC>::store(reinterpret_cast<IO *>(p.dx) + row * p.D + c, dh[i]);
+                        for (int e = 0; e < VEC; ++e) g[i][e] = __builtin_fmaf(cg, g[i][e], -cx * x[i][e]);
+                    }
+                    Piece<IO, VEC>::store(reinterpret_cast<IO *>(p.dx) + row * p.D + c, g[i]);
                 }
             }
         }
+    };
+    while (row < p.M) {                           // two rows a round: the next row's registers are never copied, which would wait for them
+        odd.load(p, row + gridDim.x);
+        take(even);
+        row += gridDim.x;
+        if (row >= p.M) break;
+        even.load(p, row + gridDim.x);
+        take(odd);
+        row += gridDim.x;
     }
     if constexpr (BWD) {
         float *to = p.sums + (int64_t)blockIdx.x * 3 * p.D;
+        if (p.dpost && p.post_shared) {           // one weight for all groups: theirs are added up here
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (threadIdx.x + i * nt) * VEC;
+                if (c < p.D)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) wide[c + e] = w1[i][e];
+            }
+            lds_barrier();
+            for (int c = threadIdx.x; c < p.width; c += nt) {
+                float s = 0.0f;
+                for (int g = 0; g < p.groups; ++g) s += wide[g * p.width + c];
+                to[c] = s;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = threadIdx.x + i * nt, c = v * VEC;
-            if (v < pieces) {
-                if (p.dpost) Piece<float, VEC>::store(to + c, w1[i]);
+            const int c = (threadIdx.x + i * nt) * VEC;
+            if (c < p.D) {
+                if (p.dpost && !p.post_shared) Piece<float, VEC>::store(to + c, w1[i]);
                 if (p.dscale) Piece<float, VEC>::store(to + p.D + c, w2[i]);
                 if (p.dpre) Piece<float, VEC>::store(to + 2 * (int64_t)p.D + c, w3[i]);
             }
@@ -265,27 +365,28 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
     }
 }
 
-// Sums over workgroups (and over groups, of a shared weight): 16 columns by 16 parts of the workgroups, in a fixed order.
-__global__ __launch_bounds__(256) void k_norm_sums(const NormParams p) {
-    __shared__ float part[16][17];
+// Sums over workgroups: 16 columns by 64 parts of the workgroups, in a fixed order.
+__global__ __launch_bounds__(1024) void k_norm_sums(const NormParams p) {
+    __shared__ float part[64][17];
     const int which = blockIdx.y, cl = threadIdx.x & 15, q = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
     float *to = which == 0 ? p.dpost : which == 1 ? p.dscale : p.dpre;
     if (!to) return;
-    const bool shared = which == 0 && p.post_shared;
-    const int n = shared ? p.width : p.D, reps = shared ? p.groups : 1;
+    const int n = which == 0 && p.post_shared ? p.width : p.D;
     float s = 0.0f;
     if (c < n)
-        for (int b = q; b < p.blocks; b += 16)
-            for (int g = 0; g < reps; ++g) s += p.sums[((int64_t)b * 3 + which) * p.D + (int64_t)g * n + c];
+        for (int b = q; b < p.blocks; b += 64) s += p.sums[((int64_t)b * 3 + which) * p.D + c];
     part[q][cl] = s;
     __syncthreads();
-    if (q == 0 && c < n) {
-        for (int i = 1; i < 16; ++i) s += part[i][cl];
-        to[c] = s;
+    if (q < 4) {
+        for (int i = 1; i < 16; ++i) s += part[q + 4 * i][cl];
+        part[q][cl] = s;
     }
+    __syncthreads();
+    if (q == 0 && c < n) to[c] = (s + part[1][cl]) + (part[2][cl] + part[3][cl]);
 }
 
 // Shape of a launch: pieces of 16 bytes of the narrowest tensor where every row allows it, threads so that a thread has few pieces.
+static int up4(int x) { return (x + 3) & ~3; }
 struct NormShape { int vec, nt, nv, how; size_t lds; };
 static bool norm_rows_fit(const NormParams &p, int vec) {
     const int es = p.io ? 2 : 4, rs = p.res_io ? 2 : 4;
@@ -294,38 +395,45 @@ static bool norm_rows_fit(const NormParams &p, int vec) {
     };
     return p.D % vec == 0 && p.width % vec == 0 && fits(p.x, p.x_s, es) && fits(p.gate, p.gate_s, es) && fits(p.res, p.res_s, rs) &&
            fits(p.dh, p.dh_s, rs) && fits(p.dy, p.dy_s, es) && fits(p.h, p.D, rs) && fits(p.y, p.D, es) && fits(p.dx, p.D, es) &&
-           fits(p.dgate, p.D, es) && fits(p.dres, p.D, rs) && fits(p.sums, p.D, 4);
+           fits(p.dgate, p.D, es) && fits(p.dres, p.D, rs) && fits(p.sums, p.D, 4) &&
+           fits(p.post, 0, 4) && fits(p.scale, 0, 4) && fits(p.pre, 0, 4);
 }
 static NormShape norm_shape(const NormParams &p) {
     NormShape s;
-    s.vec = norm_rows_fit(p, 8) ? 8 : norm_rows_fit(p, 4) ? 4 : 1;
+    s.vec = p.io && norm_rows_fit(p, 8) ? 8 : norm_rows_fit(p, 4) ? 4 : 1;       // 16 bytes of x
     const int pieces = p.D / s.vec, per_group = p.width / s.vec;
-    const int most = 16 / s.vec;                     // pieces a thread: 16 elements of every tensor in its registers
-    s.nt = 64;
-    while (s.nt < 512 && s.nt * most < pieces) s.nt *= 2;
-    const int need = (pieces + s.nt - 1) / s.nt;
-    s.nv = 1;
-    while (s.nv < need) s.nv *= 2;
+    s.nv = 1;                                        // pieces a thread: as few as 512 threads allow
+    while ((pieces + s.nv - 1) / s.nv > 512) s.nv *= 2;
+    s.nt = ((pieces + s.nv - 1) / s.nv + 63) / 64 * 64;
     const bool pow2 = (per_group & (per_group - 1)) == 0;
     s.how = p.groups == 1 ? GROUP_ROW : pow2 && per_group <= 64 ? GROUP_LANES : GROUP_LDS;
-    s.lds = s.how == GROUP_LDS && p.post ? sizeof(float) * (size_t)(pieces + p.groups) : 0;
-    if (s.lds < 16 * sizeof(float)) s.lds = 16 * sizeof(float);
+    size_t wide = s.how == GROUP_LDS && p.post ? (size_t)(pieces + p.groups) : 0;
+    if (p.dpost && p.post_shared && wide < (size_t)p.D) wide = (size_t)p.D;
+    const size_t row = (size_t)up4(p.D);
+    s.lds = sizeof(float) * (kSumSlots * 8 + (p.post ? p.post_shared ? (size_t)up4(p.width) : row : 0) + (p.scale ? row : 0) + (p.pre ? row : 0) + wide);
     return s;
+}
+template <class IO, class RES, int VEC, int NV, bool BWD> static hipError_t launch_norm_one(const NormParams &p, const NormShape &s, unsigned blocks, hipStream_t st) {
+    auto k = k_block_norm<IO, RES, VEC, NV, BWD>;
+    if (s.lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)s.lds) != hipSuccess)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3(blocks), dim3(s.nt), s.lds, st, p, s.how);
+    return hipGetLastError();
 }
 template <class IO, class RES, int VEC, bool BWD> static hipError_t launch_norm_nv(const NormParams &p, const NormShape &s, unsigned blocks, hipStream_t st) {
     switch (s.nv) {
-        case 1: hipLaunchKernelGGL((k_block_norm<IO, RES, VEC, 1, BWD>), dim3(blocks), dim3(s.nt), s.lds, st, p, s.how); break;
-        case 2: hipLaunchKernelGGL((k_block_norm<IO, RES, VEC, 2, BWD>), dim3(blocks), dim3(s.nt), s.lds, st, p, s.how); break;
-        case 4: if constexpr (VEC <= 4) { hipLaunchKernelGGL((k_block_norm<IO, RES, VEC, 4, BWD>), dim3(blocks), dim3(s.nt), s.lds, st, p, s.how); break; }
-        case 8: if constexpr (VEC == 1) { hipLaunchKernelGGL((k_block_norm<IO, RES, VEC, 8, BWD>), dim3(blocks), dim3(s.nt), s.lds, st, p, s.how); break; }
-        case 16: if constexpr (VEC == 1) { hipLaunchKernelGGL((k_block_norm<IO, RES, VEC, 16, BWD>), dim3(blocks), dim3(s.nt), s.lds, st, p, s.how); break; }
-        default: return hipErrorInvalidValue;
+        case 1: return launch_norm_one<IO, RES, VEC, 1, BWD>(p, s, blocks, st);
+        case 2: return launch_norm_one<IO, RES, VEC, 2, BWD>(p, s, blocks, st);
+        case 4: if constexpr (VEC <= 4) return launch_norm_one<IO, RES, VEC, 4, BWD>(p, s, blocks, st); break;
+        case 8: if constexpr (VEC == 1) return launch_norm_one<IO, RES, VEC, 8, BWD>(p, s, blocks, st); break;
+        case 16: if constexpr (VEC == 1) return launch_norm_one<IO, RES, VEC, 16, BWD>(p, s, blocks, st); break;
     }
-    return hipGetLastError();
+    return hipErrorInvalidValue;
 }
 template <class IO, class RES, bool BWD> static hipError_t launch_norm_vec(const NormParams &p, unsigned blocks, hipStream_t st) {
     const NormShape s = norm_shape(p);
-    if (s.vec == 8) return launch_norm_nv<IO, RES, 8, BWD>(p, s, blocks, st);
+    if constexpr (sizeof(IO) == 2)
+        if (s.vec == 8) return launch_norm_nv<IO, RES, 8, BWD>(p, s, blocks, st);
     if (s.vec == 4) return launch_norm_nv<IO, RES, 4, BWD>(p, s, blocks, st);
     return launch_norm_nv<IO, RES, 1, BWD>(p, s, blocks, st);
 }
@@ -333,13 +441,18 @@ template <bool BWD> static hipError_t launch_norm(const NormParams &p, unsigned 
     if (p.io) return p.res_io ? launch_norm_vec<uint16_t, uint16_t, BWD>(p, blocks, st) : launch_norm_vec<uint16_t, float, BWD>(p, blocks, st);
     return launch_norm_vec<float, float, BWD>(p, blocks, st);
 }
-hipError_t launch_norm_fwd(const NormParams &p, hipStream_t s) { return launch_norm<false>(p, (unsigned)(p.M < 65536 ? p.M : 65536), s); }
-
-int norm_bwd_blocks(int64_t M, int) { return (int)(M < 1024 ? M : 1024); }
+// Workgroups: as many as run at once, 24 wavefronts a compute unit forward and 12 backward (registers), each going on to further rows with the next
+// one always under way; backward four rows at least, since a workgroup also leaves three rows of sums behind.
+static int norm_blocks(int64_t M, int waves, int waves_per_cu) {
+    const int64_t n = 256 * (waves_per_cu / waves);
+    return (int)(M < n ? M : n);
+}
+hipError_t launch_norm_fwd(const NormParams &p, hipStream_t s) { return launch_norm<false>(p, (unsigned)norm_blocks(p.M, norm_shape(p).nt / 64, 24), s); }
+int norm_bwd_blocks(int64_t M, int D) { return norm_blocks((M + 3) / 4, D <= 4096 ? (D + 511) / 512 : 8, 12); }
 hipError_t launch_norm_bwd(const NormParams &p, hipStream_t s) {
     hipError_t e = launch_norm<true>(p, (unsigned)p.blocks, s);
     if (e != hipSuccess || (!p.dpost && !p.dscale && !p.dpre)) return e;
-    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((p.D + 15) / 16), 3), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((p.D + 15) / 16), 3), dim3(1024), 0, s, p);
     return hipGetLastError();
 }
 

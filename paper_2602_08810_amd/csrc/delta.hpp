@@ -8,6 +8,9 @@ namespace lrnnx {
 constexpr int kDeltaSlot = 64;           // steps between saved states; a slot holds two chunks
 constexpr int kDeltaChunk = 32;          // steps whose corrections are solved for together
 
+// The matrices of a chunk, in 16-bit words: T (2 row tiles x planes x 512), A (likewise), then exp(G), exp(G_end - G), beta (3 x 32 floats).
+constexpr int chunk_words(int np, int npa) { return (2 * np + 2 * npa) * 512 + 192; }
+
 // Rows of a matrix operand in bfloat16: element (plane, batch, step, head, column) at plane * plane_stride + b * sb + t * sl + h * sh + column,
 // rows 16-byte aligned and zero beyond the head's width up to the padded one.  A float32 operand is the sum of three planes.
 struct DeltaRows {
@@ -29,9 +32,8 @@ struct DeltaParams {
     int64_t o_sb, o_sl, o_sh;
     int o_vec;                           // rows of o take stores of four elements
     float *s_last;
-    uint16_t *mat_t, *mat_a;             // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands
-    uint16_t *mat_tt, *mat_at;           // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
-    float *scal;                         // per slot, head and chunk: exp(G), exp(G_end - G), beta
+    uint16_t *mats;                      // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands, and the gates (chunk_words)
+    uint16_t *mats_adj;                  // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
     uint16_t *states, *err;              // saved for the backward pass; null: not wanted
     // backward
     const float *ds_last;
@@ -52,6 +54,7 @@ struct DeltaPack {                       // a strided operand copied into planes
 };
 
 hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s);
+hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s);       // copied as it is: planes and dp are not looked at
 hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s);

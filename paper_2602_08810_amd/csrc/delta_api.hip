@@ -43,9 +43,11 @@ template <class A> Shape shape_of(const A *a) {
 }
 inline int adjoint_planes(const Shape &s, bool s0) { return !s.bf16 || s0 ? 3 : 2; }
 
+// Rows that do not overlap and of which 32 span less than 2 GB.
+bool rows_near(const Shape &s, int width, int64_t sl) { return s.L == 1 || (sl >= width && sl < (int64_t)1 << 24); }
 // Strided rows of `width` elements that the matrix kernels can read as they lie.
 bool rows_in_place(const Shape &s, const void *p, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, int H) {
-    return s.bf16 && width == padded && on16(p) && (one_batch || s.B == 1 || sb % 8 == 0) && (s.L == 1 || sl % 8 == 0) && (H == 1 || sh % 8 == 0);
+    return s.bf16 && width == padded && on16(p) && rows_near(s, width, sl) && (one_batch || s.B == 1 || sb % 8 == 0) && (s.L == 1 || sl % 8 == 0) && (H == 1 || sh % 8 == 0);
 }
 
 // Lays arrays out one after the other, 256-byte aligned; with a null base it only counts.
@@ -64,16 +66,14 @@ inline int a_planes(const Shape &s) { return s.bf16 ? 2 : 3; }
 void lay_saved(const Shape &s, bool s0, Layout &l, DeltaParams &p) {
     p.states = l.take<uint16_t>(s.nslots * s.Hv * (s.bf16 ? 1 : 3) * s.dkp * s.dvp);
     p.err = l.take<uint16_t>((int64_t)(s.bf16 ? 2 : 3) * s.rows * s.Hv * s.dvp);
-    p.mat_tt = l.take<uint16_t>(mats(s) * 2 * adjoint_planes(s, s0) * 512);
-    p.mat_at = l.take<uint16_t>(mats(s) * 2 * a_planes(s) * 512);
-    p.scal = l.take<float>(mats(s) * 96);
+    p.mats_adj = l.take<uint16_t>(mats(s) * chunk_words(adjoint_planes(s, s0), a_planes(s)));
 }
 
 DeltaRows lay_rows(const Shape &s, Layout &l, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, bool &copied) {
     copied = !rows_in_place(s, src, width, padded, sb, sl, sh, one_batch, H);
     DeltaRows r;
     if (!copied) {
-        r.p = reinterpret_cast<const uint16_t *>(src); r.plane = 0; r.sb = sb; r.sl = sl; r.sh = sh;
+        r.p = reinterpret_cast<const uint16_t *>(src); r.plane = 0; r.sb = sb; r.sl = s.L == 1 ? padded : sl; r.sh = sh;
         return r;
     }
     r.plane = s.rows * H * padded;
@@ -108,7 +108,7 @@ int waves_of(const Shape &s) {
     return 2;
 }
 
-struct FwdPlan { DeltaParams p; bool copy_q, copy_k; size_t bytes, saved; };
+struct FwdPlan { DeltaParams p; bool copy_q, copy_k, copy_v; size_t bytes, saved; };
 FwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *saved) {
     FwdPlan f{};
     set_inputs(a, s, f.p);
@@ -119,10 +119,13 @@ FwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *
     Layout l{ws}, sv{saved};
     f.p.q = lay_rows(s, l, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, f.copy_q);
     f.p.k = lay_rows(s, l, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, f.copy_k);
-    f.p.mat_t = l.take<uint16_t>(mats(s) * 2 * f.p.np * 512);
-    f.p.mat_a = l.take<uint16_t>(mats(s) * 2 * a_planes(s) * 512);
+    f.copy_v = !rows_near(s, s.dv, a->v_stride_l);
+    if (f.copy_v) {                                   // v of rows that overlap or lie far apart, one after the other
+        f.p.v = l.take<char>(s.rows * s.Hv * s.dv * (int64_t)elem(a->io_dtype));
+        f.p.v_sb = s.L * s.Hv * s.dv; f.p.v_sl = (int64_t)s.Hv * s.dv; f.p.v_sh = s.dv;
+    } else if (s.L == 1) f.p.v_sl = s.dv;
+    f.p.mats = l.take<uint16_t>(mats(s) * chunk_words(f.p.np, a_planes(s)));
     if (a->saved || !ws) lay_saved(s, a->s0 != nullptr, sv, f.p);
-    if (!a->saved) f.p.scal = l.take<float>(mats(s) * 96);
     f.bytes = l.at; f.saved = sv.at;
     return f;
 }
@@ -182,6 +185,13 @@ int lrnnx_gated_delta_fwd(const lrnnx_delta_fwd_args *a) {
     const hipStream_t st = reinterpret_cast<hipStream_t>(a->stream);
     if (f.copy_q && copy_rows(s, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     if (f.copy_k && copy_rows(s, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if (f.copy_v) {
+        DeltaPack k{};
+        k.src = a->v; k.sb = a->v_stride_b; k.sl = a->v_stride_l; k.sh = a->v_stride_h;
+        k.dst = reinterpret_cast<uint16_t *>(const_cast<void *>(p.v));
+        k.B = one ? 1 : s.B; k.H = s.Hv; k.d = s.dv; k.io = s.bf16; k.L = s.L;
+        if (launch_delta_gather(k, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    }
     if (launch_delta_prep(p, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     return launch_delta_scan(p, st) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
 }

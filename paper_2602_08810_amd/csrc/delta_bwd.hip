@@ -26,13 +26,14 @@ template <int NPI, int NP, int DK, int NBUF> struct AdjLds {
     } buf[NBUF];
 };
 
-template <int NPI, int NP, int DK, int NW> __global__ __launch_bounds__(NW * 64) void k_delta_adjoint(const DeltaParams p) {
+template <int NPI, int NP, int DK, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_adjoint(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     extern __shared__ __align__(16) char lds_raw[];
     using Lds = AdjLds<NPI, NP, DK, NBUF>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
     const DeltaSeq sq = delta_seq(p, b);
     const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;
@@ -49,93 +50,74 @@ template <int NPI, int NP, int DK, int NW> __global__ __launch_bounds__(NW * 64)
         }
 
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
-    const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + sq.at * p.dout.sl + h * p.dout.sh + (mine ? n0 : 0);
+    const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + sq.at * p.dout.sl + h * p.dout.sh;
 
-    constexpr int QUADS = 8 * (DK / 4), MATS = (2 * NP + 2 * NPA) * 64;
+    constexpr int QUADS = 8 * (DK / 4), MATS = chunk_words(NP, NPA) / 8;
     constexpr int IQ = (QUADS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
     uint2 kreg[IQ][NPI][4], qreg[IQ][NPI][4];
     uint4 mreg[IM];
-    float sreg[2];
     uint16_t dreg[NPI][2][4];
+    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, drow = (uint32_t)p.dout.sl * 2;
+    const uint32_t doff = mine ? 4 * g4 * drow + n0 * 2u : kOutside;
     auto fetch = [&](int64_t ch) {
-        const int64_t t0 = ch * 32;
-        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        const int64_t t0 = ch * 32, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
 #pragma unroll
-        for (int x = 0; x < IQ; ++x) {
-            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
-            if (QUADS % NT && i >= QUADS) break;
+        for (int pl = 0; pl < NPI; ++pl) {
+            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, last * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, last * qrow + 2 * DK);
+            const Buffer db = buffer_of(dp + pl * p.dout.plane + t0 * p.dout.sl, last * drow + 2 * p.dvp);
 #pragma unroll
-            for (int pl = 0; pl < NPI; ++pl)
+            for (int x = 0; x < IQ; ++x) {
+                const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int t = 4 * tq + e;
-                    const int64_t row = t0 + (t < n ? t : 0);
-                    kreg[x][pl][e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + row * p.k.sl + 4 * dq);
-                    qreg[x][pl][e] = *reinterpret_cast<const uint2 *>(qp + pl * p.q.plane + row * p.q.sl + 4 * dq);
-                    if (t >= n) kreg[x][pl][e] = qreg[x][pl][e] = make_uint2(0, 0);
-                }
-        }
-        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
-#pragma unroll
-        for (int x = 0; x < IM; ++x) {
-            const int i = tid + x * NT;
-            if (MATS % NT && i >= MATS) break;
-            const uint16_t *from = i < 128 * NP ? p.mat_tt + mat * (2 * NP * 512) + i * 8 : p.mat_at + mat * (2 * NPA * 512) + (i - 128 * NP) * 8;
-            mreg[x] = *reinterpret_cast<const uint4 *>(from);
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (tid + x * NT < 96) sreg[x] = p.scal[mat * 96 + tid + x * NT];
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g4 + r;
-#pragma unroll
-                for (int pl = 0; pl < NPI; ++pl) {
-                    dreg[pl][m][r] = dp[pl * p.dout.plane + (t0 + (t < n ? t : 0)) * p.dout.sl];
-                    if (t >= n || !mine) dreg[pl][m][r] = 0;
+                    kreg[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
+                    qreg[x][pl][e] = buffer_load8(qb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * qrow + 8 * dq);
                 }
             }
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) buffer_load(db, doff + (16 * m + r) * drow, dreg[pl][m][r]);
+        }
+        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
+        const Buffer mb = buffer_of(p.mats_adj + mat * (MATS * 8), MATS * 16);
+#pragma unroll
+        for (int x = 0; x < IM; ++x) mreg[x] = buffer_load16(mb, (tid + x * NT) * 16);
     };
     auto put = [&](typename Lds::Buf &B) {
 #pragma unroll
         for (int x = 0; x < IQ; ++x) {
             const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
-            if (QUADS % NT && i >= QUADS) break;
+            if (QUADS % NT && i >= QUADS) continue;
             const int col = (dq >> 3) * 32 + quad_place(dq & 7), place = quad_place(tq);
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
-                uint2 c[4];
+                uint2 kc[4], qc[4];
+                transpose_quad(kreg[x][pl], kc);
+                transpose_quad(qreg[x][pl], qc);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
-                transpose_quad(kreg[x][pl], c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
-                transpose_quad(qreg[x][pl], c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.qt[pl][4 * dq + e][place]) = c[e];
+                for (int e = 0; e < 4; ++e) {
+                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
+                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = kc[e];
+                    *reinterpret_cast<uint2 *>(&B.qt[pl][4 * dq + e][place]) = qc[e];
+                }
             }
         }
         uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
 #pragma unroll
-        for (int x = 0; x < IM; ++x) {
-            const int i = tid + x * NT;
-            if (MATS % NT && i >= MATS) break;
-            mats[i] = mreg[x];
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (tid + x * NT < 96) B.scal[tid + x * NT] = sreg[x];
+        for (int x = 0; x < IM; ++x)
+            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = mreg[x];
     };
 
     if (nchunk > 0) {
         fetch(nchunk - 1);
         put(lds.buf[NBUF == 2 ? (nchunk - 1) & 1 : 0]);
     }
-    __syncthreads();
+    lds_barrier();
     for (int64_t ch = nchunk - 1; ch >= 0; --ch) {
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
         Frag dof[NPI];
         f32x4 dO[2] = {};
 #pragma unroll
@@ -193,8 +175,6 @@ template <int NPI, int NP, int DK, int NW> __global__ __launch_bounds__(NW * 64)
         }
         Frag uf[NP];
         split_tiles<NP>(X[0], X[1], uf);
-        const int64_t t0 = ch * 32;
-        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
         f32x4 R[2];                                         // exp(G) beta z
         f32x4 W[2];                                         // scale exp(G) dO
 #pragma unroll
@@ -232,9 +212,9 @@ template <int NPI, int NP, int DK, int NW> __global__ __launch_bounds__(NW * 64)
             S[m] = mm(a, rf, S[m]);
             S[m] = mm(c, wf, S[m]);
         }
-        if (NBUF == 1) __syncthreads();
+        if (NBUF == 1) lds_barrier();
         if (ch > 0) put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0]);
-        __syncthreads();
+        lds_barrier();
     }
     if (p.ds0 && col_in)
 #pragma unroll

@@ -74,6 +74,27 @@ template <int NP> __device__ __forceinline__ void zero_frags(Frag (&f)[NP]) {
     for (int i = 0; i < NP; ++i) f[i].v = make_uint4(0, 0, 0, 0);
 }
 
+// Rows of a chunk through a buffer descriptor: steps past the end of a sequence lie past the descriptor's end and read as zero, so nothing is
+// compared, cleared or branched around on the way, and offsets are 32 bits that stay the same from chunk to chunk.  The host sees to it that
+// rows do not overlap and that 32 of them span less than 2 GB.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void *p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+}
+constexpr uint32_t kOutside = 0x80000000u;                    // an offset past every descriptor's end
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 buffer_load8(Buffer b, uint32_t off) {
+    const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, off, 0, 0));
+    return make_uint2(v.x, v.y);
+}
+__device__ __forceinline__ uint4 buffer_load16(Buffer b, uint32_t off) {
+    const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void buffer_load(Buffer b, uint32_t off, uint16_t &x) { x = __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0); }
+__device__ __forceinline__ void buffer_load(Buffer b, uint32_t off, float &x) { x = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0)); }
+
 __device__ __forceinline__ float load_io(const float *p) { return *p; }
 __device__ __forceinline__ float load_io(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ __forceinline__ void store_io(float *p, float x) { *p = x; }
@@ -97,6 +118,14 @@ __device__ __forceinline__ void transpose_quad(const uint2 (&w)[4], uint2 (&c)[4
     c[1] = make_uint2(__builtin_amdgcn_perm(w[1].x, w[0].x, 0x07060302u), __builtin_amdgcn_perm(w[3].x, w[2].x, 0x07060302u));
     c[2] = make_uint2(__builtin_amdgcn_perm(w[1].y, w[0].y, 0x05040100u), __builtin_amdgcn_perm(w[3].y, w[2].y, 0x05040100u));
     c[3] = make_uint2(__builtin_amdgcn_perm(w[1].y, w[0].y, 0x07060302u), __builtin_amdgcn_perm(w[3].y, w[2].y, 0x07060302u));
+}
+
+// Barrier of a workgroup whose wavefronts exchange through LDS alone: accesses to global memory stay under way (__syncthreads would wait for
+// every store of results, about a microsecond each time).
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 struct DeltaSeq {

@@ -43,12 +43,28 @@ hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <class T> __global__ __launch_bounds__(256) void k_delta_gather(const DeltaPack p) {
+    const int64_t per_row = (int64_t)p.H * p.d, n = (int64_t)p.B * p.L * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per_row, b = row / p.L, t = row - b * p.L;
+        const int rest = (int)(i - row * per_row), h = rest / p.d;
+        reinterpret_cast<T *>(p.dst)[i] = reinterpret_cast<const T *>(p.src)[b * p.sb + t * p.sl + h * p.sh + (rest - h * p.d)];
+    }
+}
+hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s) {
+    const int64_t n = (int64_t)p.B * p.L * p.H * p.d, blocks = (n + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536));
+    if (p.io) hipLaunchKernelGGL(k_delta_gather<uint16_t>, grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(k_delta_gather<float>, grid, dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- the matrices of a chunk
 // One wavefront takes a slot (two chunks) of one value head.  Q K^T and K K^T come from matrix instructions on rows read straight from memory;
 // the inverse is solved a column to a lane, row by row (496 multiply-adds a lane, both chunks side by side): substitution is stable where
 // powers of N would cancel.
 template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) void k_delta_prep(const DeltaParams p) {
-    constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2;
+    constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, NPA);
     __shared__ __align__(16) float Ns[2][32][W], As[2][32][W];
     __shared__ double Gs[64];
     __shared__ float Bs[64];
@@ -77,8 +93,14 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
         const double end = __shfl(G, 31, 32);
         const float bv = in ? be : 0.0f;
         Gs[lane] = G; Bs[lane] = bv;
-        float *sc = p.scal + ((slot * p.Hv + h) * 2 + (lane >> 5)) * 96 + (lane & 31);
-        sc[0] = __expf((float)G); sc[32] = __expf((float)(end - G)); sc[64] = bv;
+        const float eg = __expf((float)G), ee = __expf((float)(end - G));
+        const int64_t mat = (slot * p.Hv + h) * 2 + (lane >> 5);
+        float *sc = reinterpret_cast<float *>(p.mats + (mat + 1) * MW - 192) + (lane & 31);
+        sc[0] = eg; sc[32] = ee; sc[64] = bv;
+        if constexpr (ADJ > 0) {
+            sc = reinterpret_cast<float *>(p.mats_adj + (mat + 1) * AW - 192) + (lane & 31);
+            sc[0] = eg; sc[32] = ee; sc[64] = bv;
+        }
     }
     __syncthreads();
 
@@ -147,8 +169,8 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            by_rows(As[c], m, ForA(), p.mat_a + (mat + c) * (2 * NPA * 512));
-            if (ADJ > 0) by_columns(As[c], m, ForA(), p.mat_at + (mat + c) * (2 * NPA * 512));
+            by_rows(As[c], m, ForA(), p.mats + (mat + c) * MW + 2 * NP * 512);
+            if (ADJ > 0) by_columns(As[c], m, ForA(), p.mats_adj + (mat + c) * AW + 2 * ADJ * 512);
         }
     __syncthreads();
 
@@ -170,7 +192,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
 #pragma unroll
     for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) by_rows(As[cc], m, ForT(), p.mat_t + (mat + cc) * (2 * NP * 512));
+        for (int m = 0; m < 2; ++m) by_rows(As[cc], m, ForT(), p.mats + (mat + cc) * MW);
     if constexpr (ADJ > 0) {
         __syncthreads();
         float x[32];
@@ -186,7 +208,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
 #pragma unroll
         for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) by_columns(As[cc], m, std::integral_constant<int, ADJ>(), p.mat_tt + (mat + cc) * (2 * ADJ * 512));
+            for (int m = 0; m < 2; ++m) by_columns(As[cc], m, std::integral_constant<int, ADJ>(), p.mats_adj + (mat + cc) * AW);
     }
 }
 
@@ -204,19 +226,21 @@ template <int NPI, int NP, int DK, int NBUF> struct ScanLds {
     } buf[NBUF];
 };
 
-template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __launch_bounds__(NW * 64) void k_delta_scan(const DeltaParams p) {
+template <class IO, int NPI, int NP, int DK, int NW, bool SAVE>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr int NPO = NPI == 3 ? 3 : 2;                 // planes of what only enters o
     extern __shared__ __align__(16) char lds_raw[];
     using Lds = ScanLds<NPI, NP, DK, NBUF>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row16 = lane & 15, g4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
     const DeltaSeq sq = delta_seq(p, b);
     const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;     // this wavefront's columns, this lane's
     const bool col_in = n0 < p.dv;
     const int64_t nchunk = (sq.len + 31) / 32;
+    const bool wide = p.o_vec && c0 + 16 <= p.dv;                      // o in stores of four elements
 
     f32x4 S[MT];
 #pragma unroll
@@ -228,76 +252,65 @@ template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __lau
         }
 
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
-    const IO *vp = reinterpret_cast<const IO *>(p.v) + sq.ib * p.v_sb + sq.at * p.v_sl + h * p.v_sh + (col_in ? n0 : 0);
+    const IO *vp = reinterpret_cast<const IO *>(p.v) + sq.ib * p.v_sb + sq.at * p.v_sl + h * p.v_sh;
     IO *op = reinterpret_cast<IO *>(p.o) + sq.ib * p.o_sb + sq.at * p.o_sl + h * p.o_sh + c0 + 4 * g4;
 
-    // what a thread brings into LDS
-    constexpr int QUADS = 8 * (DK / 4), QROWS = 32 * (DK / 8), MATS = (2 * NP + 2 * NPA) * 64;
+    // what a thread brings into LDS: quads of four steps by four columns of K, 16 bytes of Q, 16 bytes of the chunk's matrices
+    constexpr int QUADS = 8 * (DK / 4), QROWS = 32 * (DK / 8), MATS = chunk_words(NP, NPA) / 8;
     constexpr int IQ = (QUADS + NT - 1) / NT, IR = (QROWS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
     uint2 kreg[IQ][NPI][4];
     uint4 qreg[IR][NPI], mreg[IM];
-    float sreg[2];
     IO vreg[2][4];
+    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, vrow = (uint32_t)p.v_sl * sizeof(IO);
+    const uint32_t voff = col_in ? 4 * g4 * vrow + n0 * (uint32_t)sizeof(IO) : kOutside;
     auto fetch = [&](int64_t ch) {
-        const int64_t t0 = ch * 32;
-        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        const int64_t t0 = ch * 32, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
 #pragma unroll
-        for (int x = 0; x < IQ; ++x) {
-            const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
-            if (QUADS % NT && i >= QUADS) break;
+        for (int pl = 0; pl < NPI; ++pl) {
+            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, last * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, last * qrow + 2 * DK);
 #pragma unroll
-            for (int pl = 0; pl < NPI; ++pl)
+            for (int x = 0; x < IQ; ++x) {
+                const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int t = 4 * tq + e;
-                    kreg[x][pl][e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + (t0 + (t < n ? t : 0)) * p.k.sl + 4 * dq);
-                    if (t >= n) kreg[x][pl][e] = make_uint2(0, 0);
-                }
-        }
+                for (int e = 0; e < 4; ++e) kreg[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
+            }
 #pragma unroll
-        for (int x = 0; x < IR; ++x) {
-            const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
-            if (QROWS % NT && i >= QROWS) break;
-#pragma unroll
-            for (int pl = 0; pl < NPI; ++pl) {
-                qreg[x][pl] = *reinterpret_cast<const uint4 *>(qp + pl * p.q.plane + (t0 + (t < n ? t : 0)) * p.q.sl + 8 * d8);
-                if (t >= n) qreg[x][pl] = make_uint4(0, 0, 0, 0);
+            for (int x = 0; x < IR; ++x) {
+                const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
+                qreg[x][pl] = buffer_load16(qb, QROWS % NT && i >= QROWS ? kOutside : t * qrow + 16 * d8);
             }
         }
         const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
+        const Buffer mb = buffer_of(p.mats + mat * (MATS * 8), MATS * 16);
 #pragma unroll
-        for (int x = 0; x < IM; ++x) {
-            const int i = tid + x * NT;
-            if (MATS % NT && i >= MATS) break;
-            const uint16_t *from = i < 128 * NP ? p.mat_t + mat * (2 * NP * 512) + i * 8 : p.mat_a + mat * (2 * NPA * 512) + (i - 128 * NP) * 8;
-            mreg[x] = *reinterpret_cast<const uint4 *>(from);
-        }
+        for (int x = 0; x < IM; ++x) mreg[x] = buffer_load16(mb, (tid + x * NT) * 16);
+        const Buffer vb = buffer_of(vp + t0 * p.v_sl, last * vrow + p.dv * (int)sizeof(IO));
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (tid + x * NT < 96) sreg[x] = p.scal[mat * 96 + tid + x * NT];
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) buffer_load(vb, voff + (16 * m + r) * vrow, vreg[m][r]);
     };
     auto put = [&](typename Lds::Buf &B) {
 #pragma unroll
         for (int x = 0; x < IQ; ++x) {
             const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
-            if (QUADS % NT && i >= QUADS) break;
-            const int col = (dq >> 3) * 32 + quad_place(dq & 7);
+            if (QUADS % NT && i >= QUADS) continue;
+            const int col = (dq >> 3) * 32 + quad_place(dq & 7), place = quad_place(tq);
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
-                const uint2 *w = kreg[x][pl];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = w[e];
                 uint2 c[4];
                 transpose_quad(kreg[x][pl], c);
-                const int place = quad_place(tq);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
+                for (int e = 0; e < 4; ++e) {
+                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
+                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
+                }
             }
         }
 #pragma unroll
         for (int x = 0; x < IR; ++x) {
             const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
-            if (QROWS % NT && i >= QROWS) break;
+            if (QROWS % NT && i >= QROWS) continue;
             const int q0 = (2 * d8) & 7, base = (d8 >> 2) * 32;
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
@@ -307,34 +320,15 @@ template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __lau
         }
         uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
 #pragma unroll
-        for (int x = 0; x < IM; ++x) {
-            const int i = tid + x * NT;
-            if (MATS % NT && i >= MATS) break;
-            mats[i] = mreg[x];
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (tid + x * NT < 96) B.scal[tid + x * NT] = sreg[x];
-    };
-    auto fetch_v = [&](int64_t ch) {
-        const int64_t t0 = ch * 32;
-        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g4 + r;
-                vreg[m][r] = vp[(t0 + (t < n ? t : 0)) * p.v_sl];
-                if (t >= n || !col_in) vreg[m][r] = 0;
-            }
+        for (int x = 0; x < IM; ++x)
+            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = mreg[x];
     };
 
     if (nchunk > 0) {
         fetch(0);
-        fetch_v(0);
         put(lds.buf[0]);
     }
-    __syncthreads();
+    lds_barrier();
     for (int64_t ch = 0; ch < nchunk; ++ch) {
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
         f32x4 V[2];
@@ -342,7 +336,9 @@ template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __lau
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) V[m][r] = load_io(&vreg[m][r]);
-        if (ch + 1 < nchunk) { fetch(ch + 1); fetch_v(ch + 1); }
+        const int64_t t0 = ch * 32;
+        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        if (ch + 1 < nchunk) fetch(ch + 1);
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         if (SAVE && !(ch & 1) && c0 < p.dvp) {
@@ -401,8 +397,6 @@ template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __lau
             E[m] = mm(t, rf, E[m]);
             if (SAVE) Et[m] = mm(rf, t, Et[m]);                        // a step to a lane, for wide stores
         }
-        const int64_t t0 = ch * 32;
-        const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
         if (SAVE && c0 < p.dvp) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
@@ -450,19 +444,17 @@ template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> __global__ __lau
 #pragma unroll
             for (int r = 0; r < 4; ++r) O[m][r] *= gam;
             O[m] = mm(uf, a, O[m]);
-            const int t = 16 * m + row16, left = p.dv - c0 - 4 * g4;
-            if (t < n) {
-                IO *to = op + (t0 + t) * p.o_sl;
-                if (p.o_vec && left >= 4) store4(to, O[m]);
-                else
+            const int t = 16 * m + row16;
+            IO *to = op + (t0 + t) * p.o_sl;
+            if (wide) { if (t < n) store4(to, O[m]); }
+            else if (t < n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (r < left) store_io(to + r, O[m][r]);
-            }
+                for (int r = 0; r < 4; ++r)
+                    if (c0 + 4 * g4 + r < p.dv) store_io(to + r, O[m][r]);
         }
-        if (NBUF == 1) __syncthreads();
+        if (NBUF == 1) lds_barrier();
         if (ch + 1 < nchunk) put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0]);
-        __syncthreads();
+        lds_barrier();
     }
     if (p.s_last && col_in)
 #pragma unroll
@@ -482,8 +474,8 @@ template <int NPI, int NP, int ADJ> static hipError_t launch_prep(const DeltaPar
     return hipGetLastError();
 }
 hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s) {
-    if (!p.io) return p.mat_tt ? launch_prep<3, 3, 3>(p, s) : launch_prep<3, 3, 0>(p, s);
-    if (!p.mat_tt) return p.np == 3 ? launch_prep<1, 3, 0>(p, s) : launch_prep<1, 2, 0>(p, s);
+    if (!p.io) return p.mats_adj ? launch_prep<3, 3, 3>(p, s) : launch_prep<3, 3, 0>(p, s);
+    if (!p.mats_adj) return p.np == 3 ? launch_prep<1, 3, 0>(p, s) : launch_prep<1, 2, 0>(p, s);
     if (p.np_adjoint == 3) return launch_prep<1, 3, 3>(p, s);
     return p.np == 3 ? launch_prep<1, 3, 2>(p, s) : launch_prep<1, 2, 2>(p, s);
 }
