@@ -231,19 +231,28 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // of 16, and every product is arranged so that its results lie a step to a lane: gates are a number to a lane, F and H go from one product's
 // results into the next one's operand without leaving the lane, and rows of dQ and dK come out four neighbouring elements at a time.  Both
 // orientations of F and H are computed (one as products with the rows of others, one the other way round), which costs less than turning them.
+// The columns of v come through LDS 32 at a time (rows of dO, E, Z and of both states, the next ones under way meanwhile), then K and Q, as rows
+// and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.
 template <int NPI, int DK> struct GradLds {
-    uint16_t kt[NPI][DK][72], qt[NPI][DK][72];              // K^T, Q^T, steps placed as results of matrix instructions hold them
+    static constexpr int NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, ROWS = NPI == 3 ? 0 : 1;
+    union {
+        struct { uint16_t e[NPE][64][40], z[NPE][64][40], d[NPI][64][40], s0[NPS][DK][40], s1[NPS][DK][40]; } v;
+        struct { uint16_t kt[NPI][DK][72], qt[NPI][DK][72], kr[ROWS + 1][ROWS ? 64 : 1][DK + 8]; } k;      // kr: rows of K and of Q
+    };
     double G[64];
     float beta[64], dG[64], ends[4], dots[4];
 };
 
-template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_delta_grads(const DeltaParams p) {
+template <class IO, int NPI, int DK, bool SHARED>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 && !SHARED ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, NPF = NPI == 3 ? 3 : 2;
+    constexpr bool ROWS = NPI == 1;                         // rows of K and Q in LDS too; else from memory
+    constexpr int IS = DK / 64;                             // 16-byte pieces of 32 columns of a state to a thread
     extern __shared__ __align__(16) char lds_raw[];
     GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     const int64_t slot = blockIdx.x / (unsigned)p.Hk;
-    const int hk = (int)(blockIdx.x - slot * p.Hk), share = p.Hv / p.Hk;
+    const int hk = (int)(blockIdx.x - slot * p.Hk), share = SHARED ? p.Hv / p.Hk : 1;
     DeltaSeq sq;
     int64_t t0;
     int b;
@@ -251,43 +260,9 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
     if (n == 0) return;
     const int64_t at = sq.at + t0, row0 = sq.row + t0, rows = (int64_t)(p.cu ? 1 : p.B) * p.L;
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
-    const int own = 16 * wave + row16, own_row = own < n ? own : 0;
+    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, drow = (uint32_t)p.dout.sl * 2, erow = (uint32_t)p.Hv * p.dvp * 2;
+    const int own = 16 * wave + row16;
     const bool own_in = own < n;
-
-    // K^T and Q^T into LDS: 16 quads of steps by DK / 4 quads of columns
-    for (int i = tid; i < 16 * (DK / 4); i += 256) {
-        const int tq = i / (DK / 4), dq = i % (DK / 4), place = (tq >> 3) * 32 + quad_place(tq & 7);
-#pragma unroll
-        for (int pl = 0; pl < NPI; ++pl) {
-            uint2 kw[4], qw[4], c[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int t = 4 * tq + e;
-                kw[e] = *reinterpret_cast<const uint2 *>(kp + pl * p.k.plane + (t < n ? t : 0) * p.k.sl + 4 * dq);
-                qw[e] = *reinterpret_cast<const uint2 *>(qp + pl * p.q.plane + (t < n ? t : 0) * p.q.sl + 4 * dq);
-                if (t >= n) kw[e] = qw[e] = make_uint2(0, 0);
-            }
-            transpose_quad(kw, c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&lds.kt[pl][4 * dq + e][place]) = c[e];
-            transpose_quad(qw, c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint2 *>(&lds.qt[pl][4 * dq + e][place]) = c[e];
-        }
-    }
-    // rows of the slot as operands: step 16 m + row16, terms 32 ks + 8 g4 ..
-    auto rows_of = [&](const uint16_t *base, int64_t plane, int64_t stride, int t, int ks, auto np, Frag *f) {
-        constexpr int P = decltype(np)::value;
-        const bool in = t < n;
-        const uint16_t *q = base + (in ? t : 0) * stride + 32 * ks + 8 * g4;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            f[i].v = *reinterpret_cast<const uint4 *>(q + i * plane);
-            if (!in) f[i].v = make_uint4(0, 0, 0, 0);
-        }
-    };
-    using PI = std::integral_constant<int, NPI>;
-    using PE = std::integral_constant<int, NPE>;
 
     f32x4 dq[MT], dk[MT];
 #pragma unroll
@@ -297,11 +272,33 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
         const int h = hk * share + sh;
         const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
         const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
-        const int64_t eplane = rows * p.Hv * p.dvp, estride = (int64_t)p.Hv * p.dvp;
+        const int64_t eplane = rows * p.Hv * p.dvp;
         const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPS * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPS * DK * p.dvp;
         const int ksv = p.dvp / 32;
 
-        __syncthreads();                                    // the last head's sums have been read; K^T and Q^T are there
+        // 32 columns of v on their way: a thread brings 16 bytes of a row of dO, of each plane of E and Z, and of DK / 64 rows of the states
+        uint4 ereg[NPE], zreg[NPE], dreg[NPI], areg[NPS][IS], breg[NPS][IS];
+        const int tr = tid >> 2, tc = (tid & 3) * 16;
+        auto fetch = [&](int ks) {
+#pragma unroll
+            for (int i = 0; i < NPE; ++i) {
+                ereg[i] = buffer_load16(buffer_of(ep + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
+                zreg[i] = buffer_load16(buffer_of(zp + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
+            }
+#pragma unroll
+            for (int i = 0; i < NPI; ++i)
+                dreg[i] = buffer_load16(buffer_of(dp + i * p.dout.plane, (int64_t)(n - 1) * drow + 2 * p.dvp), tr * drow + 64 * ks + tc);
+#pragma unroll
+            for (int i = 0; i < NPS; ++i)
+#pragma unroll
+                for (int x = 0; x < IS; ++x) {
+                    const uint32_t off = (uint32_t)((tr + 64 * x) * p.dvp * 2 + 64 * ks + tc);
+                    areg[i][x] = buffer_load16(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+                    breg[i][x] = buffer_load16(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+                }
+        };
+        fetch(0);
+        lds_barrier();                                      // what the last head left in LDS has been read
         if (wave == 0) {
             const bool in = lane < n;
             const int64_t t = at + (in ? lane : 0);
@@ -316,18 +313,85 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
             lds.G[lane] = G;
             lds.beta[lane] = in ? be : 0.0f;
         }
-        __syncthreads();
-        const double Gown = lds.G[own];
-        const float bown = lds.beta[own], gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
 
-        // products over the columns of v: other steps' rows with this lane's step
         f32x4 P1t[4] = {}, P1[4] = {}, P2t[4] = {}, P2[4] = {};      // dO_own . e_j; dO_i . e_own; z_own . e_j; z_i . e_own
-        float dbeta = 0.0f;
+        f32x4 qs[MT], kr[MT], kw[MT];                                // S0 dO, S0 z, dS1 e of the lane's step
+#pragma unroll
+        for (int m = 0; m < MT; ++m) qs[m] = kr[m] = kw[m] = f32x4{};
+        float dbeta = 0.0f, sdot = 0.0f, bown = 0.0f;
         for (int ks = 0; ks < ksv; ++ks) {
+            if (ks > 0) lds_barrier();
+            auto &L = lds.v;
+#pragma unroll
+            for (int i = 0; i < NPE; ++i) {
+                *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = ereg[i];
+                *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = zreg[i];
+            }
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = dreg[i];
+#pragma unroll
+            for (int i = 0; i < NPS; ++i)
+#pragma unroll
+                for (int x = 0; x < IS; ++x) {
+                    *reinterpret_cast<uint4 *>(&L.s0[i][tr + 64 * x][tc / 2]) = areg[i][x];
+                    *reinterpret_cast<uint4 *>(&L.s1[i][tr + 64 * x][tc / 2]) = breg[i][x];
+                }
+            if (ks + 1 < ksv) fetch(ks + 1);
+            lds_barrier();
+            bown = lds.beta[own];
             Frag dO[NPI], e[NPE], z[NPE];
-            rows_of(dp, p.dout.plane, p.dout.sl, own, ks, PI(), dO);
-            rows_of(ep, eplane, estride, own, ks, PE(), e);
-            rows_of(zp, eplane, estride, own, ks, PE(), z);
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) dO[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][own][8 * g4]);
+#pragma unroll
+            for (int i = 0; i < NPE; ++i) {
+                e[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][own][8 * g4]);
+                z[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][own][8 * g4]);
+            }
+            // the states' products, and <S0, dS1> of a quarter of their rows
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                Frag s0[NPS], s1[NPS];
+#pragma unroll
+                for (int i = 0; i < NPS; ++i) {
+                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][8 * g4]);
+                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][8 * g4]);
+                }
+                qs[m] = mm(s0, dO, qs[m]);
+                kr[m] = mm(s0, z, kr[m]);
+                kw[m] = mm(s1, e, kw[m]);
+                if ((m & 3) == wave)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
+#pragma unroll
+                        for (int i = NPS - 1; i >= 0; --i) {
+                            al += __uint_as_float(s1[i].u[x] << 16); ah += hi_part(__uint_as_float(s1[i].u[x]));
+                            cl += __uint_as_float(s0[i].u[x] << 16); chh += hi_part(__uint_as_float(s0[i].u[x]));
+                        }
+                        sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
+                    }
+            }
+            // with the other steps
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                if (m <= wave) {
+                    Frag er[NPE];
+#pragma unroll
+                    for (int i = 0; i < NPE; ++i) er[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][16 * m + row16][8 * g4]);
+                    P1t[m] = mm(er, dO, P1t[m]);
+                    P2t[m] = mm(er, z, P2t[m]);
+                }
+                if (m >= wave) {
+                    Frag dr[NPI], zr[NPE];
+#pragma unroll
+                    for (int i = 0; i < NPI; ++i) dr[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][16 * m + row16][8 * g4]);
+#pragma unroll
+                    for (int i = 0; i < NPE; ++i) zr[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][16 * m + row16][8 * g4]);
+                    P1[m] = mm(dr, e, P1[m]);
+                    P2[m] = mm(zr, e, P2[m]);
+                }
+            }
+            // dV = beta z, dbeta = z . e
             f32x4 zs[2] = {}, es[2] = {};
 #pragma unroll
             for (int x = 0; x < 8; ++x)
@@ -336,9 +400,8 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
                     zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
                     es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
                 }
-            // dV = beta z
             const int c = 32 * ks + 8 * g4;
-            IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + own_row) * p.Hv + h) * p.dv + c;
+            IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + (own_in ? own : 0)) * p.Hv + h) * p.dv + c;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 f32x4 v;
@@ -351,69 +414,129 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
                         for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
                 }
             }
+        }
+        const double Gown = lds.G[own];
+        const float gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
+
+        // K and Q into LDS: 16 quads of steps by DK / 4 quads of columns, turned, and as rows
+        constexpr int IQ = DK / 64;
+        uint2 kw4[NPI][IQ * 4], qw4[NPI][IQ * 4];
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                if (m <= wave) {
-                    Frag er[NPE];
-                    rows_of(ep, eplane, estride, 16 * m + row16, ks, PE(), er);
-                    P1t[m] = mm(er, dO, P1t[m]);
-                    P2t[m] = mm(er, z, P2t[m]);
+        for (int pl = 0; pl < NPI; ++pl) {
+            const Buffer kb = buffer_of(kp + pl * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
+#pragma unroll
+            for (int x = 0; x < IQ; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4);
+                    kw4[pl][4 * x + e] = buffer_load8(kb, (4 * tq + e) * krow + 8 * dc);
+                    qw4[pl][4 * x + e] = buffer_load8(qb, (4 * tq + e) * qrow + 8 * dc);
                 }
-                if (m >= wave) {
-                    Frag dr[NPI], zr[NPE];
-                    rows_of(dp, p.dout.plane, p.dout.sl, 16 * m + row16, ks, PI(), dr);
-                    rows_of(zp, eplane, estride, 16 * m + row16, ks, PE(), zr);
-                    P1[m] = mm(dr, e, P1[m]);
-                    P2[m] = mm(zr, e, P2[m]);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int pl = 0; pl < NPI; ++pl)
+#pragma unroll
+            for (int x = 0; x < IQ; ++x) {
+                const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4), place = (tq >> 3) * 32 + quad_place(tq & 7);
+                uint2 w[4], u[4], c[4], d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { w[e] = kw4[pl][4 * x + e]; u[e] = qw4[pl][4 * x + e]; }
+                transpose_quad(w, c);
+                transpose_quad(u, d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    *reinterpret_cast<uint2 *>(&lds.k.kt[pl][4 * dc + e][place]) = c[e];
+                    *reinterpret_cast<uint2 *>(&lds.k.qt[pl][4 * dc + e][place]) = d[e];
+                    if constexpr (ROWS) {
+                        *reinterpret_cast<uint2 *>(&lds.k.kr[0][4 * tq + e][4 * dc]) = w[e];
+                        *reinterpret_cast<uint2 *>(&lds.k.kr[1][4 * tq + e][4 * dc]) = u[e];
+                    }
                 }
             }
+        lds_barrier();
+        // rows of K (which = 0) and Q as operands
+        auto row_of = [&](int which, int t, int ks, Frag (&f)[NPI]) {
+            if constexpr (ROWS) f[0].v = *reinterpret_cast<const uint4 *>(&lds.k.kr[which][t][32 * ks + 8 * g4]);
+            else
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
+                    f[i].v = buffer_load16(rb, t * (which ? qrow : krow) + 64 * ks + 16 * g4);
+                }
+        };
+        auto four_of = [&](int which, int m) -> f32x4 {      // of this lane's step, columns 16 m + 4 g4 ..
+            f32x4 v = {};
+#pragma unroll
+            for (int i = NPI - 1; i >= 0; --i) {
+                uint2 a;
+                if constexpr (ROWS) a = *reinterpret_cast<const uint2 *>(&lds.k.kr[which][own][16 * m + 4 * g4]);
+                else {
+                    const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
+                    a = buffer_load8(rb, own * (which ? qrow : krow) + 32 * m + 8 * g4);
+                }
+                v += f32x4{__uint_as_float(a.x << 16), hi_part(__uint_as_float(a.x)), __uint_as_float(a.y << 16), hi_part(__uint_as_float(a.y))};
+            }
+            return v;
+        };
+        // the states' part of dQ and dK
+        float dG = 0.0f, ends = 0.0f;
+        {
+            const float cq = p.scale * gam, ck = -gam * bown, cw = en * bown;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const f32x4 kv = four_of(0, m), qv = four_of(1, m);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float a = cq * qs[m][r], c = ck * kr[m][r], w = cw * kw[m][r];
+                    dq[m][r] += a; dk[m][r] += c + w;
+                    dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
+                    ends = __builtin_fmaf(kv[r], w, ends);
+                }
+            }
+            dG -= ends;
         }
         // F, H in both orientations, M's row and column sums
-        float dG = 0.0f;
         f32x4 HH[4], Ft[4], F[4];
-        f32x4 QKt[4] = {}, QK[4] = {}, KK[4] = {};
+        {
+            Frag kf[KS][NPI], qf[KS][NPI];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            Frag kf[NPI], qf[NPI];
-            rows_of(kp, p.k.plane, p.k.sl, own, ks, PI(), kf);
-            rows_of(qp, p.q.plane, p.q.sl, own, ks, PI(), qf);
+            for (int ks = 0; ks < KS; ++ks) { row_of(0, own, ks, kf[ks]); row_of(1, own, ks, qf[ks]); }
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-                Frag kr[NPI];
-                rows_of(kp, p.k.plane, p.k.sl, 16 * m + row16, ks, PI(), kr);
-                KK[m] = mm(kr, kf, KK[m]);
-                if (m <= wave) QKt[m] = mm(kr, qf, QKt[m]);
-                if (m >= wave) {
-                    Frag qr[NPI];
-                    rows_of(qp, p.q.plane, p.q.sl, 16 * m + row16, ks, PI(), qr);
-                    QK[m] = mm(qr, kf, QK[m]);
+                f32x4 QKt = {}, QK = {}, KK = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    Frag kx[NPI], qx[NPI];
+                    row_of(0, 16 * m + row16, ks, kx);
+                    row_of(1, 16 * m + row16, ks, qx);
+                    KK = mm(kx, kf[ks], KK);
+                    QKt = mm(kx, qf[ks], QKt);
+                    QK = mm(qx, kf[ks], QK);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int o = 16 * m + 4 * g4 + r;
+                    const double Go = lds.G[o];
+                    const float bo = lds.beta[o];
+                    float ft = 0.0f, f = 0.0f, hh = 0.0f;
+                    const float D = __expf((float)(o <= own ? Gown - Go : Go - Gown));
+                    if (o <= own) {                              // this step reads what step o wrote
+                        ft = p.scale * D * bo * P1t[m][r];
+                        if (o < own) hh = -D * bown * bo * P2t[m][r];
+                        dG += ft * QKt[r] + hh * KK[r];
+                    }
+                    if (o >= own) {                              // step o reads what this step wrote
+                        f = p.scale * D * bown * P1[m][r];
+                        float hx = 0.0f;
+                        if (o > own) hx = -D * bown * bo * P2[m][r];
+                        dG -= f * QK[r] + hx * KK[r];
+                        hh += hx;
+                    }
+                    Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
                 }
             }
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int o = 16 * m + 4 * g4 + r;
-                const double Go = lds.G[o];
-                const float bo = lds.beta[o];
-                float ft = 0.0f, f = 0.0f, hh = 0.0f;
-                if (o <= own) {                              // this step reads what step o wrote
-                    const float D = __expf((float)(Gown - Go));
-                    ft = p.scale * D * bo * P1t[m][r];
-                    if (o < own) hh = -D * bown * bo * P2t[m][r];
-                    dG += ft * QKt[m][r] + hh * KK[m][r];
-                }
-                if (o >= own) {                              // step o reads what this step wrote
-                    const float D = __expf((float)(Go - Gown));
-                    f = p.scale * D * bown * P1[m][r];
-                    float hx = 0.0f;
-                    if (o > own) hx = -D * bown * bo * P2[m][r];
-                    dG -= f * QK[m][r] + hx * KK[m][r];
-                    hh += hx;
-                }
-                Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
-            }
         // dQ += F K, dK += (H + H^T) K + F^T Q
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -426,97 +549,14 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
                 Frag kt[NPI], qt[NPI];
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) {
-                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.kt[i][16 * m + row16][32 * x + 8 * g4]);
-                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.qt[i][16 * m + row16][32 * x + 8 * g4]);
+                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.kt[i][16 * m + row16][32 * x + 8 * g4]);
+                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.qt[i][16 * m + row16][32 * x + 8 * g4]);
                 }
                 dq[m] = mm(kt, ft, dq[m]);
                 dk[m] = mm(kt, hh, dk[m]);
                 dk[m] = mm(qt, f, dk[m]);
             }
         }
-        // the states' part
-        float ends = 0.0f, sdot = 0.0f;
-        {
-            f32x4 qs[MT], kr[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) qs[m] = kr[m] = f32x4{};
-            for (int ks = 0; ks < ksv; ++ks) {
-                Frag dO[NPI], z[NPE];
-                rows_of(dp, p.dout.plane, p.dout.sl, own, ks, PI(), dO);
-                rows_of(zp, eplane, estride, own, ks, PE(), z);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    Frag s[NPS];
-#pragma unroll
-                    for (int i = 0; i < NPS; ++i) s[i].v = *reinterpret_cast<const uint4 *>(s0p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
-                    qs[m] = mm(s, dO, qs[m]);
-                    kr[m] = mm(s, z, kr[m]);
-                }
-            }
-            const float cq = p.scale * gam, ck = -gam * bown;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                f32x4 qv = {}, kv = {};
-#pragma unroll
-                for (int i = NPI - 1; i >= 0; --i) {
-                    const uint2 a = *reinterpret_cast<const uint2 *>(qp + i * p.q.plane + own_row * p.q.sl + 16 * m + 4 * g4);
-                    const uint2 c = *reinterpret_cast<const uint2 *>(kp + i * p.k.plane + own_row * p.k.sl + 16 * m + 4 * g4);
-                    qv += f32x4{__uint_as_float(a.x << 16), hi_part(__uint_as_float(a.x)), __uint_as_float(a.y << 16), hi_part(__uint_as_float(a.y))};
-                    kv += f32x4{__uint_as_float(c.x << 16), hi_part(__uint_as_float(c.x)), __uint_as_float(c.y << 16), hi_part(__uint_as_float(c.y))};
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float a = cq * qs[m][r], c = ck * kr[m][r];
-                    dq[m][r] += a; dk[m][r] += c;
-                    dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m) qs[m] = f32x4{};
-            for (int ks = 0; ks < ksv; ++ks) {
-                Frag e[NPE];
-                rows_of(ep, eplane, estride, own, ks, PE(), e);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    Frag s[NPS];
-#pragma unroll
-                    for (int i = 0; i < NPS; ++i) s[i].v = *reinterpret_cast<const uint4 *>(s1p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
-                    qs[m] = mm(s, e, qs[m]);
-                    if ((m & 3) == wave) {                   // <S0, dS1>: every wavefront a quarter of the rows
-                        Frag o[NPS];
-#pragma unroll
-                        for (int i = 0; i < NPS; ++i) o[i].v = *reinterpret_cast<const uint4 *>(s0p + ((int64_t)i * DK + 16 * m + row16) * p.dvp + 32 * ks + 8 * g4);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
-#pragma unroll
-                            for (int i = NPS - 1; i >= 0; --i) {
-                                al += __uint_as_float(s[i].u[x] << 16); ah += hi_part(__uint_as_float(s[i].u[x]));
-                                cl += __uint_as_float(o[i].u[x] << 16); chh += hi_part(__uint_as_float(o[i].u[x]));
-                            }
-                            sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
-                        }
-                    }
-                }
-            }
-            const float cw = en * bown;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                f32x4 kv = {};
-#pragma unroll
-                for (int i = NPI - 1; i >= 0; --i) {
-                    const uint2 c = *reinterpret_cast<const uint2 *>(kp + i * p.k.plane + own_row * p.k.sl + 16 * m + 4 * g4);
-                    kv += f32x4{__uint_as_float(c.x << 16), hi_part(__uint_as_float(c.x)), __uint_as_float(c.y << 16), hi_part(__uint_as_float(c.y))};
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float a = cw * qs[m][r];
-                    dk[m][r] += a;
-                    ends = __builtin_fmaf(kv[r], a, ends);
-                }
-            }
-        }
-        dG -= ends;
         if (!own_in) { dG = 0.0f; ends = 0.0f; }
         // over the four lane groups of a step, then over the steps
 #pragma unroll
@@ -538,7 +578,7 @@ template <class IO, int NPI, int DK> __global__ __launch_bounds__(256) void k_de
             }
         }
         if (lane == 0) { lds.ends[wave] = ends; lds.dots[wave] = sdot; }
-        __syncthreads();
+        lds_barrier();
         if (wave == 0) {
             float x = lds.dG[lane];
 #pragma unroll
@@ -592,7 +632,7 @@ hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
 template <class IO, int NPI, int DK> static hipError_t launch_grads_one(const DeltaParams &p, hipStream_t s) {
     constexpr size_t bytes = sizeof(GradLds<NPI, DK>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    auto k = k_delta_grads<IO, NPI, DK>;
+    auto k = p.Hv > p.Hk ? k_delta_grads<IO, NPI, DK, true> : k_delta_grads<IO, NPI, DK, false>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3((unsigned)(p.nslots * p.Hk)), dim3(256), bytes, s, p);
     return hipGetLastError();
