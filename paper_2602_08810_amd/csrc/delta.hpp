@@ -40,8 +40,11 @@ struct DeltaParams {
     float *ds0;
     uint16_t *dstates, *z;
     void *dq, *dkk, *dvv, *dg, *dbeta;
-    int wave_cols;                       // (launch) waves of 16 columns a workgroup
     int np, np_adjoint;                  // planes of the state chain, of its adjoint
+    // segments of the time axis that are walked side by side (one sequence of a batch entry alone does not fill the chip); 1: none
+    int nseg, seg_chunks, groups;        // segments, chunks of one (even); groups of columns (workgroups) of a head
+    float *entry;                        // [B,Hv,nseg,dkp,dvp] state entering each segment (adjoint: of the segment's end)
+    uint16_t *trans;                     // [B,Hv,nseg-1,planes,dkp,dkp] what a segment makes of the state that enters it
 };
 
 struct DeltaPack {                       // a strided operand copied into planes
@@ -58,6 +61,8 @@ hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s);       // copi
 hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s);
+hipError_t launch_delta_join(const DeltaParams &p, bool adjoint, hipStream_t s);
+constexpr int delta_waves(int dvp) { return dvp > 32 ? 4 : 2; }          // wavefronts of 16 columns a workgroup
 hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s);
 
 struct DeltaStepParams {

@@ -26,19 +26,27 @@ template <int NPI, int NP, int DK, int NBUF> struct AdjLds {
     } buf[NBUF];
 };
 
-template <int NPI, int NP, int DK, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_adjoint(const DeltaParams p) {
+// DEEP: loads two chunks ahead, for launches of at most a workgroup a compute unit, where registers are there for it and nothing else hides memory
+// (walk of 4 x 4096 steps, 16 heads of 128 x 128: 385 -> 346 us; the forward walk gains nothing by it).
+template <int NPI, int NP, int DK, int NW, bool AGG, bool DEEP>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 1 : 2, DEEP ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     extern __shared__ __align__(16) char lds_raw[];
     using Lds = AdjLds<NPI, NP, DK, NBUF>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
-    const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
+    DeltaUnit un;
+    if (!delta_unit(p, AGG ? p.nseg - 1 : p.nseg, un)) return;
+    const int h = un.h, hk = h / (p.Hv / p.Hk), b = un.b, seg = AGG ? un.seg + 1 : un.seg;
     const DeltaSeq sq = delta_seq(p, b);
-    const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;
+    const int c0 = (un.group * NW + wave) * 16, n0 = c0 + row16;
     const bool col_in = n0 < p.dv, mine = c0 < p.dvp;
-    const int64_t nchunk = (sq.len + 31) / 32;
+    const int64_t nchunk = (sq.len + 31) / 32, ch0 = p.nseg > 1 ? (int64_t)seg * p.seg_chunks : 0;
+    const int64_t ch1 = p.nseg > 1 && nchunk > ch0 + p.seg_chunks ? ch0 + p.seg_chunks : nchunk;
+    if (ch0 >= nchunk && seg > 0) return;
+    const int64_t head = (int64_t)b * p.Hv + h;
+    const NegId neg = neg_id();
 
     f32x4 S[MT];
 #pragma unroll
@@ -46,7 +54,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = 16 * m + 4 * g4 + r;
-            S[m][r] = p.ds_last && col_in && d < p.dk ? p.ds_last[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] : 0.0f;
+            if (AGG) S[m][r] = d == n0 - p.dvp ? 1.0f : 0.0f;
+            else if (ch1 < nchunk) S[m][r] = mine ? p.entry[((head * p.nseg + seg) * DK + d) * p.dvp + n0] : 0.0f;
+            else S[m][r] = p.ds_last && col_in && d < p.dk ? p.ds_last[(head * p.dk + d) * p.dv + n0] : 0.0f;
         }
 
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
@@ -54,37 +64,41 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
     constexpr int QUADS = 8 * (DK / 4), MATS = chunk_words(NP, NPA) / 8;
     constexpr int IQ = (QUADS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
-    uint2 kreg[IQ][NPI][4], qreg[IQ][NPI][4];
-    uint4 mreg[IM];
-    uint16_t dreg[NPI][2][4];
+    struct Stage {
+        uint2 k[IQ][NPI][4], q[IQ][NPI][4];
+        uint4 m[IM];
+        uint16_t d[NPI][2][4];
+    };
     const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, drow = (uint32_t)p.dout.sl * 2;
     const uint32_t doff = mine ? 4 * g4 * drow + n0 * 2u : kOutside;
-    auto fetch = [&](int64_t ch) {
-        const int64_t t0 = ch * 32, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
+    auto fetch = [&](int64_t ch, Stage &st) __attribute__((always_inline)) {
+        const bool in = ch >= ch0 && ch < ch1;
+        const int64_t t0 = in ? ch * 32 : 0, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
 #pragma unroll
         for (int pl = 0; pl < NPI; ++pl) {
-            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, last * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, last * qrow + 2 * DK);
-            const Buffer db = buffer_of(dp + pl * p.dout.plane + t0 * p.dout.sl, last * drow + 2 * p.dvp);
+            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, in ? last * krow + 2 * DK : 0);
+            const Buffer qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, in ? last * qrow + 2 * DK : 0);
+            const Buffer db = buffer_of(dp + pl * p.dout.plane + t0 * p.dout.sl, in ? last * drow + 2 * p.dvp : 0);
 #pragma unroll
             for (int x = 0; x < IQ; ++x) {
                 const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    kreg[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
-                    qreg[x][pl][e] = buffer_load8(qb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * qrow + 8 * dq);
+                    st.k[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
+                    st.q[x][pl][e] = buffer_load8(qb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * qrow + 8 * dq);
                 }
             }
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) buffer_load(db, doff + (16 * m + r) * drow, dreg[pl][m][r]);
+                for (int r = 0; r < 4; ++r) buffer_load(db, doff + (16 * m + r) * drow, st.d[pl][m][r]);
         }
-        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
-        const Buffer mb = buffer_of(p.mats_adj + mat * (MATS * 8), MATS * 16);
+        const int64_t mat = in ? ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1) : 0;
+        const Buffer mb = buffer_of(p.mats_adj + mat * (MATS * 8), in ? MATS * 16 : 0);
 #pragma unroll
-        for (int x = 0; x < IM; ++x) mreg[x] = buffer_load16(mb, (tid + x * NT) * 16);
+        for (int x = 0; x < IM; ++x) st.m[x] = buffer_load16(mb, (tid + x * NT) * 16);
     };
-    auto put = [&](typename Lds::Buf &B) {
+    auto put = [&](typename Lds::Buf &B, const Stage &st) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < IQ; ++x) {
             const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
@@ -93,28 +107,23 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
                 uint2 kc[4], qc[4];
-                transpose_quad(kreg[x][pl], kc);
-                transpose_quad(qreg[x][pl], qc);
+                transpose_quad(st.k[x][pl], kc);
+                transpose_quad(st.q[x][pl], qc);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
-                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = kc[e];
-                    *reinterpret_cast<uint2 *>(&B.qt[pl][4 * dq + e][place]) = qc[e];
+                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = st.k[x][pl][e];
+                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][turned(4 * dq, place)]) = kc[e];
+                    *reinterpret_cast<uint2 *>(&B.qt[pl][4 * dq + e][turned(4 * dq, place)]) = qc[e];
                 }
             }
         }
         uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
 #pragma unroll
         for (int x = 0; x < IM; ++x)
-            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = mreg[x];
+            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = st.m[x];
     };
 
-    if (nchunk > 0) {
-        fetch(nchunk - 1);
-        put(lds.buf[NBUF == 2 ? (nchunk - 1) & 1 : 0]);
-    }
-    lds_barrier();
-    for (int64_t ch = nchunk - 1; ch >= 0; --ch) {
+    auto step = [&](int64_t ch, Stage &cur, Stage &next) __attribute__((always_inline)) {
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
         const int64_t t0 = ch * 32;
         const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
@@ -125,104 +134,166 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dO[m][r] += load_io(&dreg[pl][m][r]);
+                for (int r = 0; r < 4; ++r) dO[m][r] += load_io(&cur.d[pl][m][r]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                dof[pl].u[e] = (uint32_t)dreg[pl][e >> 1][2 * (e & 1)] | (uint32_t)dreg[pl][e >> 1][2 * (e & 1) + 1] << 16;
+                dof[pl].u[e] = (uint32_t)cur.d[pl][e >> 1][2 * (e & 1)] | (uint32_t)cur.d[pl][e >> 1][2 * (e & 1) + 1] << 16;
         }
-        if (ch > 0) fetch(ch - 1);
+        fetch(ch - (DEEP ? 2 : 1), cur);
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
-        if (((ch & 1) || ch == nchunk - 1) && mine) {
-            uint16_t *to = p.dstates + sh * NPS * DK * p.dvp + n0;
+        if (!AGG && ((ch & 1) || ch == nchunk - 1) && mine) {
+            uint16_t *to = p.dstates + (sh * NPS * p.dvp + n0) * DK + 4 * g4;            // turned: a column to a row
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < MT; ++m) {
+                uint32_t lo[NPS], hi[NPS];
+                split2<NPS>(S[m][0], S[m][1], lo);
+                split2<NPS>(S[m][2], S[m][3], hi);
 #pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    uint32_t w[NPS];
-                    split2<NPS>(S[m][r], S[m][r + 1], w);
-#pragma unroll
-                    for (int i = 0; i < NPS; ++i) {
-                        uint16_t *q = to + ((int64_t)i * DK + 16 * m + 4 * g4 + r) * p.dvp;
-                        q[0] = (uint16_t)w[i];
-                        q[p.dvp] = (uint16_t)(w[i] >> 16);
-                    }
-                }
+                for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + (int64_t)i * p.dvp * DK + 16 * m) = make_uint2(lo[i], hi[i]);
+            }
         }
+        constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
+        Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NPA];
+        f32x4 gam[2], be[2], en[2];
+        if constexpr (EARLY)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) kf[ks][m][0].v = *reinterpret_cast<const uint4 *>(&B.k[0][16 * m + row16][32 * ks + 8 * g4]);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
+#pragma unroll
+            for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) tf[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+        }
+        if constexpr (EARLY) reads_first();
         // dU
-        f32x4 X[2] = {};
+        f32x4 X[2] = {}, Y[2] = {};
+#pragma unroll
+        for (int m = 0; m < 2; ++m) Y[m] = mm(af[m], dof, Y[m]);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             Frag s[NP];
-            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s);
+            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s, neg);
+            const int at = EARLY ? ks : 0;
+            if constexpr (!EARLY)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                Frag a[NPI];
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
-                X[m] = mm(a, s, X[m]);
+                    for (int i = 0; i < NPI; ++i) kf[0][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < NPI; ++j)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+                        if (i + j < NP) X[m] = mfma(kf[at][m][j], s[i], X[m]);
+        }
+        if constexpr (EARLY)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                ktf[m][0].v = *reinterpret_cast<const uint4 *>(&B.kt[0][16 * m + row16][turned(16 * m, 8 * g4)]);
+                qtf[m][0].v = *reinterpret_cast<const uint4 *>(&B.qt[0][16 * m + row16][turned(16 * m, 8 * g4)]);
             }
-        }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            const f32x4 en = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) X[m][r] *= en[r];
-            Frag a[NPA];
-#pragma unroll
-            for (int i = 0; i < NPA; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
-            X[m] = mm(a, dof, X[m]);
+            be[m] = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]);
+            gam[m] = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
         }
-        Frag uf[NP];
-        split_tiles<NP>(X[0], X[1], uf);
-        f32x4 R[2];                                         // exp(G) beta z
-        f32x4 W[2];                                         // scale exp(G) dO
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            Frag t[NP];
-#pragma unroll
-            for (int i = 0; i < NP; ++i) t[i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
-            const f32x4 z = mm(t, uf, f32x4{}), zt = mm(uf, t, f32x4{});
-            const int tt = 16 * m + row16;
-            uint32_t lo[NPE], hi[NPE];
-            split2<NPE>(zt[0], zt[1], lo);
-            split2<NPE>(zt[2], zt[3], hi);
-            if (tt < n && mine)
-#pragma unroll
-                for (int i = 0; i < NPE; ++i)
-                    *reinterpret_cast<uint2 *>(p.z + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + tt) * p.Hv + h) * p.dvp + c0 + 4 * g4) = make_uint2(lo[i], hi[i]);
-            const f32x4 be = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]), gam = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { R[m][r] = -gam[r] * be[r] * z[r]; W[m][r] = p.scale * gam[r] * dO[m][r]; }
-        }
-        Frag rf[NP], wf[NP];
-        split_tiles<NP>(R[0], R[1], rf);
-        split_tiles<NP>(W[0], W[1], wf);
         const float gend = B.scal[31];
+        if constexpr (EARLY) reads_first();
+        // scale exp(G) dO, which waits for nothing, into dS0 first
+        f32x4 W[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { W[m][r] = p.scale * gam[m][r] * dO[m][r]; X[m][r] = __builtin_fmaf(en[m][r], X[m][r], Y[m][r]); }
+        Frag uf[NP], wf[NP];
+        split_tiles<NP>(X[0], X[1], uf, neg);
+        split_tiles<NP>(W[0], W[1], wf, neg);
+        f32x4 Z[2] = {}, Zt[2] = {};
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                if (i + j < NP)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        Z[m] = mfma(tf[m][i], uf[j], Z[m]);
+                        if (!AGG) Zt[m] = mfma(uf[j], tf[m][i], Zt[m]);                      // a step to a lane, for wide stores
+                    }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            Frag a[NPI], c[NPI];
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                a[i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][8 * g4]);
-                c[i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][16 * m + row16][8 * g4]);
-            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[m][r] *= gend;
-            S[m] = mm(a, rf, S[m]);
-            S[m] = mm(c, wf, S[m]);
+            if constexpr (!EARLY)
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) qtf[0][i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+            S[m] = mm(qtf[EARLY ? m : 0], wf, S[m]);
+        }
+        f32x4 R[2];                                         // -exp(G) beta z
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R[m][r] = -gam[m][r] * be[m][r] * Z[m][r];
+        Frag rf[NP];
+        split_tiles<NP>(R[0], R[1], rf, neg);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if constexpr (!EARLY)
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+            S[m] = mm(ktf[EARLY ? m : 0], rf, S[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int t = 16 * m + row16;
+            uint32_t lo[NPE], hi[NPE];
+            split2<NPE>(Zt[m][0], Zt[m][1], lo);
+            split2<NPE>(Zt[m][2], Zt[m][3], hi);
+            if (!AGG && t < n && mine)
+#pragma unroll
+                for (int i = 0; i < NPE; ++i)
+                    *reinterpret_cast<uint2 *>(p.z + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + t) * p.Hv + h) * p.dvp + c0 + 4 * g4) = make_uint2(lo[i], hi[i]);
         }
         if (NBUF == 1) lds_barrier();
-        if (ch > 0) put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0]);
+        put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0], next);
         lds_barrier();
+    };
+    Stage one;
+    fetch(ch1 - 1, one);
+    put(lds.buf[NBUF == 2 ? (ch1 - 1) & 1 : 0], one);
+    if constexpr (DEEP) {
+        Stage two;
+        fetch(ch1 - 2, two);
+        lds_barrier();
+        for (int64_t ch = ch1 - 1; ch >= ch0;) {
+            step(ch, one, two);
+            if (--ch < ch0) break;
+            step(ch, two, one);
+            --ch;
+        }
+    } else {
+        lds_barrier();
+        for (int64_t ch = ch1 - 1; ch >= ch0; --ch) step(ch, one, one);
     }
-    if (p.ds0 && col_in)
+    if constexpr (AGG) {
+        if (mine) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p.entry[((head * p.nseg + un.seg) * DK + 16 * m + 4 * g4 + r) * p.dvp + n0] = S[m][r];
+        } else if (c0 < p.dvp + DK) store_trans<NP, DK>(S, p.trans + (head * (p.nseg - 1) + un.seg) * NP * DK * DK, n0 - p.dvp, g4);
+    } else if (p.ds0 && col_in && ch0 == 0)
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int d = 16 * m + 4 * g4 + r;
-                if (d < p.dk) p.ds0[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] = S[m][r];
+                if (d < p.dk) p.ds0[(head * p.dk + d) * p.dv + n0] = S[m][r];
             }
 }
 
@@ -247,7 +318,6 @@ template <class IO, int NPI, int DK, bool SHARED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 && !SHARED ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, NPF = NPI == 3 ? 3 : 2;
     constexpr bool ROWS = NPI == 1;                         // rows of K and Q in LDS too; else from memory
-    constexpr int IS = DK / 64;                             // 16-byte pieces of 32 columns of a state to a thread
     extern __shared__ __align__(16) char lds_raw[];
     GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
@@ -276,9 +346,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
         const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPS * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPS * DK * p.dvp;
         const int ksv = p.dvp / 32;
 
-        // 32 columns of v on their way: a thread brings 16 bytes of a row of dO, of each plane of E and Z, and of DK / 64 rows of the states
-        uint4 ereg[NPE], zreg[NPE], dreg[NPI], areg[NPS][IS], breg[NPS][IS];
-        const int tr = tid >> 2, tc = (tid & 3) * 16;
+        // 32 columns of v on their way: a thread brings 16 bytes of a row of dO and of each plane of E and Z, and of the states, which lie a column of v to
+        // a row, four rows by four elements (the first 2 DK threads)
+        uint4 ereg[NPE], zreg[NPE], dreg[NPI];
+        uint2 areg[NPS][4], breg[NPS][4];
+        const int tr = tid >> 2, tc = (tid & 3) * 16, sq4 = tid / (DK / 4), sd4 = tid % (DK / 4);
         auto fetch = [&](int ks) {
 #pragma unroll
             for (int i = 0; i < NPE; ++i) {
@@ -291,10 +363,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
 #pragma unroll
             for (int i = 0; i < NPS; ++i)
 #pragma unroll
-                for (int x = 0; x < IS; ++x) {
-                    const uint32_t off = (uint32_t)((tr + 64 * x) * p.dvp * 2 + 64 * ks + tc);
-                    areg[i][x] = buffer_load16(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
-                    breg[i][x] = buffer_load16(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * 2) : kOutside;
+                    areg[i][x] = buffer_load8(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+                    breg[i][x] = buffer_load8(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
                 }
         };
         fetch(0);
@@ -331,10 +403,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
             for (int i = 0; i < NPI; ++i) *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = dreg[i];
 #pragma unroll
             for (int i = 0; i < NPS; ++i)
+                if (tid < 2 * DK) {
+                    uint2 c[4], d[4];
+                    transpose_quad(areg[i], c);
+                    transpose_quad(breg[i], d);
 #pragma unroll
-                for (int x = 0; x < IS; ++x) {
-                    *reinterpret_cast<uint4 *>(&L.s0[i][tr + 64 * x][tc / 2]) = areg[i][x];
-                    *reinterpret_cast<uint4 *>(&L.s1[i][tr + 64 * x][tc / 2]) = breg[i][x];
+                    for (int x = 0; x < 4; ++x) {
+                        *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = c[x];
+                        *reinterpret_cast<uint2 *>(&L.s1[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = d[x];
+                    }
                 }
             if (ks + 1 < ksv) fetch(ks + 1);
             lds_barrier();
@@ -353,8 +430,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                 Frag s0[NPS], s1[NPS];
 #pragma unroll
                 for (int i = 0; i < NPS; ++i) {
-                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][8 * g4]);
-                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][8 * g4]);
+                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                 }
                 qs[m] = mm(s0, dO, qs[m]);
                 kr[m] = mm(s0, z, kr[m]);
@@ -446,8 +523,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                 transpose_quad(u, d);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<uint2 *>(&lds.k.kt[pl][4 * dc + e][place]) = c[e];
-                    *reinterpret_cast<uint2 *>(&lds.k.qt[pl][4 * dc + e][place]) = d[e];
+                    *reinterpret_cast<uint2 *>(&lds.k.kt[pl][4 * dc + e][turned(4 * dc, place)]) = c[e];
+                    *reinterpret_cast<uint2 *>(&lds.k.qt[pl][4 * dc + e][turned(4 * dc, place)]) = d[e];
                     if constexpr (ROWS) {
                         *reinterpret_cast<uint2 *>(&lds.k.kr[0][4 * tq + e][4 * dc]) = w[e];
                         *reinterpret_cast<uint2 *>(&lds.k.kr[1][4 * tq + e][4 * dc]) = u[e];
@@ -549,8 +626,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                 Frag kt[NPI], qt[NPI];
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) {
-                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.kt[i][16 * m + row16][32 * x + 8 * g4]);
-                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.qt[i][16 * m + row16][32 * x + 8 * g4]);
+                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.kt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
+                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.qt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
                 }
                 dq[m] = mm(kt, ft, dq[m]);
                 dk[m] = mm(kt, hh, dk[m]);
@@ -610,19 +687,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
 }
 
 // ---------------------------------------------------------------- launches
-template <int NPI, int NP, int DK, int NW> static hipError_t launch_adjoint_one(const DeltaParams &p, hipStream_t s) {
+template <int NPI, int NP, int DK, int NW, bool AGG> static hipError_t launch_adjoint_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr size_t bytes = sizeof(AdjLds<NPI, NP, DK, NBUF>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    auto k = k_delta_adjoint<NPI, NP, DK, NW>;
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3((unsigned)((p.dvp / 16 + NW - 1) / NW), (unsigned)p.Hv, (unsigned)p.B), dim3(NW * 64), bytes, s, p);
+    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + NW - 1) / NW;
+    const unsigned blocks = delta_blocks(p, AGG ? p.nseg - 1 : p.nseg);
+    auto k = blocks <= 256 ? k_delta_adjoint<NPI, NP, DK, NW, AGG, true> : k_delta_adjoint<NPI, NP, DK, NW, AGG, false>;
+    if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3(blocks), dim3(NW * 64), bytes, s, p);
     return hipGetLastError();
 }
+template <int NPI, int NP, int DK, int NW> static hipError_t launch_adjoint_nw(const DeltaParams &p, hipStream_t s) {
+    if (p.nseg > 1) {
+        if (const hipError_t e = launch_adjoint_one<NPI, NP, DK, NW, true>(p, s)) return e;
+        if (const hipError_t e = launch_delta_join(p, true, s)) return e;
+    }
+    return launch_adjoint_one<NPI, NP, DK, NW, false>(p, s);
+}
 template <int NPI, int NP, int DK> static hipError_t launch_adjoint_dk(const DeltaParams &p, hipStream_t s) {
-    if (p.wave_cols == 8) return launch_adjoint_one<NPI, NP, DK, 8>(p, s);
-    if (p.wave_cols == 4) return launch_adjoint_one<NPI, NP, DK, 4>(p, s);
-    return launch_adjoint_one<NPI, NP, DK, 2>(p, s);
+    return delta_waves(p.dvp) == 4 ? launch_adjoint_nw<NPI, NP, DK, 4>(p, s) : launch_adjoint_nw<NPI, NP, DK, 2>(p, s);
 }
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_adjoint_dk<3, 3, 128>(p, s) : launch_adjoint_dk<3, 3, 64>(p, s);

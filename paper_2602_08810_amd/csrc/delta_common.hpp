@@ -69,6 +69,34 @@ template <int NP> __device__ __forceinline__ void split_tiles(const f32x4 &lo, c
         for (int i = 0; i < NP; ++i) f[i].u[e] = w[i];
     }
 }
+// The same with the matrix unit taking off what a plane holds: x - plane as (-I) plane + x, exact like the subtraction, one instruction for a tile
+// where two vector instructions an element are eight.  (A wavefront alone on its SIMD is bound by the instructions it issues.)
+struct NegId { Frag lo, hi; };                               // -I for the terms of the lower and of the upper tile of an operand
+__device__ __forceinline__ NegId neg_id() {
+    NegId n;
+    const int lane = threadIdx.x & 63, at = (lane & 15) - 4 * (lane >> 4);          // this row's own term, if it is one of the lane's four
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t w = at == 2 * i ? 0xbf80u : at == 2 * i + 1 ? 0xbf800000u : 0u;
+        n.lo.u[i] = w; n.lo.u[i + 2] = 0;
+        n.hi.u[i] = 0; n.hi.u[i + 2] = w;
+    }
+    return n;
+}
+template <int NP> __device__ __forceinline__ void split_tiles(f32x4 lo, f32x4 hi, Frag (&f)[NP], const NegId &neg) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            f[i].u[e] = i == NP - 1 && NP < 3 ? pack_rne(lo[2 * e], lo[2 * e + 1]) : pack_hi(lo[2 * e], lo[2 * e + 1]);
+            f[i].u[e + 2] = i == NP - 1 && NP < 3 ? pack_rne(hi[2 * e], hi[2 * e + 1]) : pack_hi(hi[2 * e], hi[2 * e + 1]);
+        }
+        if (i < NP - 1) { lo = mfma(neg.lo, f[i], lo); hi = mfma(neg.hi, f[i], hi); }
+    }
+}
+// LDS reads before this stay before it (they are wanted early, registers or not)
+__device__ __forceinline__ void reads_first() { asm volatile("" ::: "memory"); }
+
 template <int NP> __device__ __forceinline__ void zero_frags(Frag (&f)[NP]) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) f[i].v = make_uint4(0, 0, 0, 0);
@@ -112,6 +140,9 @@ __device__ __forceinline__ float load_gate(const void *p, int64_t i, int io, int
 
 // Position of terms 4 q .. 4 q + 3 of a block of 32 in a row of LDS: what lane group g reads lies together (4 g .. and 16 + 4 g ..).
 __device__ __forceinline__ int quad_place(int q) { return ((q & 3) * 2 + (q >> 2)) * 4; }
+// Where a turned operand's 16-byte piece of a row lies: pieces of every 16 rows change places, so that a wavefront that writes a piece of every
+// fourth row reaches all banks.  (The pieces of a tile of 16 rows move together: a constant for who reads it.)
+__device__ __forceinline__ int turned(int row, int place) { return place ^ (((row >> 4) & 3) << 3); }
 // four rows of four neighbouring elements -> four columns of four
 __device__ __forceinline__ void transpose_quad(const uint2 (&w)[4], uint2 (&c)[4]) {
     c[0] = make_uint2(__builtin_amdgcn_perm(w[1].x, w[0].x, 0x05040100u), __builtin_amdgcn_perm(w[3].x, w[2].x, 0x05040100u));
@@ -126,6 +157,39 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Which workgroup does what: a unit is a segment of a head of a batch entry; the workgroups of its groups of columns, which read the same rows, are
+// 8 apart and so on one die.  False: none (the launch rounds up to whole eights).
+struct DeltaUnit { int group, h, b, seg; };
+__device__ __forceinline__ bool delta_unit(const DeltaParams &p, unsigned segs, DeltaUnit &u) {
+    const unsigned id = blockIdx.x, per = 8u * p.groups, heads = (unsigned)p.B * p.Hv;
+    const unsigned unit = id / per * 8 + (id & 7);
+    u.group = (int)(id % per >> 3);
+    if (unit >= heads * segs) return false;
+    u.seg = (int)(unit / heads);
+    const unsigned bh = unit - u.seg * heads;
+    u.b = (int)(bh / (unsigned)p.Hv);
+    u.h = (int)(bh - (unsigned)u.b * p.Hv);
+    return true;
+}
+
+inline unsigned delta_blocks(const DeltaParams &p, int segs) { return (unsigned)(((int64_t)p.B * p.Hv * segs + 7) / 8 * 8 * p.groups); }
+// A wavefront's 16 columns (this lane's: j) of a segment's transition, as planes [dk][dk].
+template <int NP, int DK> __device__ __forceinline__ void store_trans(const f32x4 (&S)[DK / 16], uint16_t *to, int j, int g4) {
+#pragma unroll
+    for (int m = 0; m < DK / 16; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+            uint32_t w[NP];
+            split2<NP>(S[m][r], S[m][r + 1], w);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                uint16_t *q = to + (i * DK + 16 * m + 4 * g4 + r) * DK + j;
+                q[0] = (uint16_t)w[i];
+                q[DK] = (uint16_t)(w[i] >> 16);
+            }
+        }
 }
 
 struct DeltaSeq {

@@ -226,7 +226,10 @@ template <int NPI, int NP, int DK, int NBUF> struct ScanLds {
     } buf[NBUF];
 };
 
-template <class IO, int NPI, int NP, int DK, int NW, bool SAVE>
+//
+// AGG: what a segment makes of the state that enters it, S -> M S + N, without outputs: N is the walk from a state of zero, and the columns of M, behind those
+// of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
+template <class IO, int NPI, int NP, int DK, int NW, bool SAVE, bool AGG>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
@@ -235,11 +238,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     using Lds = ScanLds<NPI, NP, DK, NBUF>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
-    const int h = blockIdx.y, hk = h / (p.Hv / p.Hk), b = blockIdx.z;
+    DeltaUnit un;
+    if (!delta_unit(p, AGG ? p.nseg - 1 : p.nseg, un)) return;
+    const int h = un.h, hk = h / (p.Hv / p.Hk), b = un.b;
     const DeltaSeq sq = delta_seq(p, b);
-    const int c0 = (blockIdx.x * NW + wave) * 16, n0 = c0 + row16;     // this wavefront's columns, this lane's
+    const int c0 = (un.group * NW + wave) * 16, n0 = c0 + row16;       // this wavefront's columns, this lane's
     const bool col_in = n0 < p.dv;
-    const int64_t nchunk = (sq.len + 31) / 32;
+    const int64_t nchunk = (sq.len + 31) / 32, ch0 = p.nseg > 1 ? (int64_t)un.seg * p.seg_chunks : 0;
+    const int64_t ch1 = p.nseg > 1 && nchunk > ch0 + p.seg_chunks ? ch0 + p.seg_chunks : nchunk;
+    if (ch0 >= nchunk && un.seg > 0) return;
+    const int64_t head = (int64_t)b * p.Hv + h;
+    const NegId neg = neg_id();
     const bool wide = p.o_vec && c0 + 16 <= p.dv;                      // o in stores of four elements
 
     f32x4 S[MT];
@@ -248,7 +257,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = 16 * m + 4 * g4 + r;
-            S[m][r] = p.s0 && col_in && d < p.dk ? p.s0[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] : 0.0f;
+            if (AGG) S[m][r] = d == n0 - p.dvp ? 1.0f : 0.0f;
+            else if (un.seg > 0) S[m][r] = c0 < p.dvp ? p.entry[((head * p.nseg + un.seg) * DK + d) * p.dvp + n0] : 0.0f;
+            else S[m][r] = p.s0 && col_in && d < p.dk ? p.s0[(head * p.dk + d) * p.dv + n0] : 0.0f;
         }
 
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
@@ -258,39 +269,44 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     // what a thread brings into LDS: quads of four steps by four columns of K, 16 bytes of Q, 16 bytes of the chunk's matrices
     constexpr int QUADS = 8 * (DK / 4), QROWS = 32 * (DK / 8), MATS = chunk_words(NP, NPA) / 8;
     constexpr int IQ = (QUADS + NT - 1) / NT, IR = (QROWS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
-    uint2 kreg[IQ][NPI][4];
-    uint4 qreg[IR][NPI], mreg[IM];
-    IO vreg[2][4];
+    struct Stage {
+        uint2 k[IQ][NPI][4];
+        uint4 q[IR][NPI], m[IM];
+    };
+    struct Values { IO v[2][4]; };                          // rows of v, wanted late in their own chunk
     const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, vrow = (uint32_t)p.v_sl * sizeof(IO);
     const uint32_t voff = col_in ? 4 * g4 * vrow + n0 * (uint32_t)sizeof(IO) : kOutside;
-    auto fetch = [&](int64_t ch) {
-        const int64_t t0 = ch * 32, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
+    // (a chunk past the segment's end: nothing is read, without a branch that would have to wait for the registers)
+    auto fetch = [&](int64_t ch, Stage &st, Values &vs) __attribute__((always_inline)) {
+        const bool in = ch < ch1;
+        const int64_t t0 = in ? ch * 32 : 0, last = (sq.len - t0 < 32 ? sq.len - t0 : 32) - 1;
 #pragma unroll
         for (int pl = 0; pl < NPI; ++pl) {
-            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, last * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, last * qrow + 2 * DK);
+            const Buffer kb = buffer_of(kp + pl * p.k.plane + t0 * p.k.sl, in ? last * krow + 2 * DK : 0);
+            const Buffer qb = buffer_of(qp + pl * p.q.plane + t0 * p.q.sl, in ? last * qrow + 2 * DK : 0);
 #pragma unroll
             for (int x = 0; x < IQ; ++x) {
                 const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) kreg[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
+                for (int e = 0; e < 4; ++e) st.k[x][pl][e] = buffer_load8(kb, QUADS % NT && i >= QUADS ? kOutside : (4 * tq + e) * krow + 8 * dq);
             }
 #pragma unroll
-            for (int x = 0; x < IR; ++x) {
+            for (int x = 0; x < (AGG ? 0 : IR); ++x) {
                 const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
-                qreg[x][pl] = buffer_load16(qb, QROWS % NT && i >= QROWS ? kOutside : t * qrow + 16 * d8);
+                st.q[x][pl] = buffer_load16(qb, QROWS % NT && i >= QROWS ? kOutside : t * qrow + 16 * d8);
             }
         }
-        const int64_t mat = ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1);
-        const Buffer mb = buffer_of(p.mats + mat * (MATS * 8), MATS * 16);
+        const int64_t mat = in ? ((sq.slot + (ch >> 1)) * p.Hv + h) * 2 + (ch & 1) : 0;
+        const Buffer mb = buffer_of(p.mats + mat * (MATS * 8), in ? MATS * 16 : 0);
 #pragma unroll
-        for (int x = 0; x < IM; ++x) mreg[x] = buffer_load16(mb, (tid + x * NT) * 16);
-        const Buffer vb = buffer_of(vp + t0 * p.v_sl, last * vrow + p.dv * (int)sizeof(IO));
+        for (int x = 0; x < IM; ++x) st.m[x] = buffer_load16(mb, (tid + x * NT) * 16);
+        const Buffer vb = buffer_of(vp + t0 * p.v_sl, in ? last * vrow + p.dv * (int)sizeof(IO) : 0);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) buffer_load(vb, voff + (16 * m + r) * vrow, vreg[m][r]);
+            for (int r = 0; r < 4; ++r) buffer_load(vb, voff + (16 * m + r) * vrow, vs.v[m][r]);
     };
-    auto put = [&](typename Lds::Buf &B) {
+    auto put = [&](typename Lds::Buf &B, const Stage &st) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < IQ; ++x) {
             const int i = tid + x * NT, tq = i / (DK / 4), dq = i % (DK / 4);
@@ -299,103 +315,150 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
                 uint2 c[4];
-                transpose_quad(kreg[x][pl], c);
+                transpose_quad(st.k[x][pl], c);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = kreg[x][pl][e];
-                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][place]) = c[e];
+                    *reinterpret_cast<uint2 *>(&B.k[pl][4 * tq + e][col]) = st.k[x][pl][e];
+                    *reinterpret_cast<uint2 *>(&B.kt[pl][4 * dq + e][turned(4 * dq, place)]) = c[e];
                 }
             }
         }
 #pragma unroll
-        for (int x = 0; x < IR; ++x) {
+        for (int x = 0; x < (AGG ? 0 : IR); ++x) {
             const int i = tid + x * NT, t = i / (DK / 8), d8 = i % (DK / 8);
             if (QROWS % NT && i >= QROWS) continue;
             const int q0 = (2 * d8) & 7, base = (d8 >> 2) * 32;
 #pragma unroll
             for (int pl = 0; pl < NPI; ++pl) {
-                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0)]) = make_uint2(qreg[x][pl].x, qreg[x][pl].y);
-                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0 + 1)]) = make_uint2(qreg[x][pl].z, qreg[x][pl].w);
+                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0)]) = make_uint2(st.q[x][pl].x, st.q[x][pl].y);
+                *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0 + 1)]) = make_uint2(st.q[x][pl].z, st.q[x][pl].w);
             }
         }
         uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
 #pragma unroll
         for (int x = 0; x < IM; ++x)
-            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = mreg[x];
+            if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = st.m[x];
     };
 
-    if (nchunk > 0) {
-        fetch(0);
-        put(lds.buf[0]);
-    }
-    lds_barrier();
-    for (int64_t ch = 0; ch < nchunk; ++ch) {
+    auto step = [&](int64_t ch, Stage &st, const Values &v, Values &vnext) __attribute__((always_inline)) {
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
-        f32x4 V[2];
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) V[m][r] = load_io(&vreg[m][r]);
         const int64_t t0 = ch * 32;
         const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
-        if (ch + 1 < nchunk) fetch(ch + 1);
+        f32x4 V[2];                                         // (with SAVE there are no registers for a second set of rows under way)
+        if constexpr (SAVE)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) V[m][r] = load_io(&v.v[m][r]);
+        fetch(ch + 1, st, vnext);
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         if (SAVE && !(ch & 1) && c0 < p.dvp) {
-            uint16_t *to = p.states + sh * NPS * DK * p.dvp + n0;
+            uint16_t *to = p.states + (sh * NPS * p.dvp + n0) * DK + 4 * g4;             // turned: a column to a row
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < MT; ++m) {
+                uint32_t lo[NPS], hi[NPS];
+                split2<NPS>(S[m][0], S[m][1], lo);
+                split2<NPS>(S[m][2], S[m][3], hi);
 #pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    uint32_t w[NPS];
-                    split2<NPS>(S[m][r], S[m][r + 1], w);
-#pragma unroll
-                    for (int i = 0; i < NPS; ++i) {
-                        uint16_t *q = to + ((int64_t)i * DK + 16 * m + 4 * g4 + r) * p.dvp;
-                        q[0] = (uint16_t)w[i];
-                        q[p.dvp] = (uint16_t)(w[i] >> 16);
-                    }
-                }
+                for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + (int64_t)i * p.dvp * DK + 16 * m) = make_uint2(lo[i], hi[i]);
+            }
         }
 
         // K S0 and (transposed: a step to a lane) Q S0
+        constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
+        Frag kf[EARLY ? KS : 1][2][NPI], qf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], af[2][NPA];
+        f32x4 gam[2], be[2], en[2];
+        auto read_kq = [&](int ks, int at) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    kf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
+                    if constexpr (!AGG) qf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.q[i][16 * m + row16][32 * ks + 8 * g4]);
+                }
+        };
+        if constexpr (EARLY)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) read_kq(ks, ks);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            gam[m] = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) tf[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+        }
+        if constexpr (EARLY) reads_first();
         f32x4 P[2] = {}, O[2] = {};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            Frag s[NP], so[NPO];
-            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s);
+            Frag s[NP];
+            split_tiles<NP>(S[2 * ks], S[2 * ks + 1], s, neg);
+            const int at = EARLY ? ks : 0;
+            if constexpr (!EARLY) read_kq(ks, 0);
 #pragma unroll
-            for (int i = 0; i < NPO; ++i) so[i] = s[i < NP ? i : NP - 1];
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                Frag a[NPI], c[NPI];
+                for (int j = 0; j < NPI; ++j)
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    a[i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
-                    c[i].v = *reinterpret_cast<const uint4 *>(&B.q[i][16 * m + row16][32 * ks + 8 * g4]);
-                }
-                P[m] = mm(a, s, P[m]);
-                O[m] = mm(so, c, O[m]);
-            }
+                    for (int m = 0; m < 2; ++m) {
+                        if (i + j < NP) P[m] = mfma(kf[at][m][j], s[i], P[m]);
+                        if (!AGG && i < NPO && i + j < NPO) O[m] = mfma(s[i], qf[at][m][j], O[m]);
+                    }
         }
+        if constexpr (EARLY) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) ktf[m][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            be[m] = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]);
+            en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
+            if constexpr (!AGG)
+#pragma unroll
+                for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
+        }
+        if constexpr (EARLY) reads_first();
         // E = (I + N beta)^-1 (V - exp(G) K S0)
-        f32x4 R[2], E[2] = {};
+        f32x4 R[2], E[2] = {}, Et[2] = {};
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f32x4 gam = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[r], P[m][r], V[m][r]);
-        }
+            for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[m][r], P[m][r], SAVE ? V[m][r] : load_io(&v.v[m][r]));
         Frag rf[NP];
-        split_tiles<NP>(R[0], R[1], rf);
-        f32x4 Et[2] = {};
+        split_tiles<NP>(R[0], R[1], rf, neg);
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            Frag t[NP];
+        for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int i = 0; i < NP; ++i) t[i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
-            E[m] = mm(t, rf, E[m]);
-            if (SAVE) Et[m] = mm(rf, t, Et[m]);                        // a step to a lane, for wide stores
+            for (int j = 0; j < NP; ++j)
+                if (i + j < NP)
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        E[m] = mfma(tf[m][i], rf[j], E[m]);
+                        if (SAVE) Et[m] = mfma(rf[j], tf[m][i], Et[m]);            // a step to a lane, for wide stores
+                    }
+        // U = beta E, and U decayed to the end of the chunk
+        f32x4 U[2], D[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { U[m][r] = be[m][r] * E[m][r]; D[m][r] = en[m][r] * U[m][r]; }
+        Frag uf[NPO], df[NP];
+        split_tiles<NP>(D[0], D[1], df, neg);
+        if constexpr (!AGG) split_tiles<NPO>(U[0], U[1], uf, neg);
+        // S1
+        const float gend = B.scal[31];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[m][r] *= gend;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if constexpr (!EARLY)
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+            S[m] = mm(ktf[EARLY ? m : 0], df, S[m]);
         }
         if (SAVE && c0 < p.dvp) {
 #pragma unroll
@@ -411,39 +474,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                             make_uint2(lo[i], hi[i]);
             }
         }
-        // U = beta E, and U decayed to the end of the chunk
-        f32x4 U[2], D[2];
+        if constexpr (!AGG)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const f32x4 be = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]);
-            const f32x4 en = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
+        for (int m = 0; m < 2; ++m) {                       // O
+            const float gs = p.scale * B.scal[16 * m + row16];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { U[m][r] = be[r] * E[m][r]; D[m][r] = en[r] * U[m][r]; }
-        }
-        Frag uf[NPO], df[NP];
-        split_tiles<NPO>(U[0], U[1], uf);
-        split_tiles<NP>(D[0], D[1], df);
-        // S1
-        const float gend = B.scal[31];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            Frag a[NPI];
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][8 * g4]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[m][r] *= gend;
-            S[m] = mm(a, df, S[m]);
-        }
-        // O
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            Frag a[NPA];
-#pragma unroll
-            for (int i = 0; i < NPA; ++i) a[i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
-            const float gam = p.scale * B.scal[16 * m + row16];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) O[m][r] *= gam;
-            O[m] = mm(uf, a, O[m]);
+            for (int r = 0; r < 4; ++r) O[m][r] *= gs;
+            O[m] = mm(uf, af[m], O[m]);
             const int t = 16 * m + row16;
             IO *to = op + (t0 + t) * p.o_sl;
             if (wide) { if (t < n) store4(to, O[m]); }
@@ -453,17 +490,120 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     if (c0 + 4 * g4 + r < p.dv) store_io(to + r, O[m][r]);
         }
         if (NBUF == 1) lds_barrier();
-        if (ch + 1 < nchunk) put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0]);
+        put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0], st);
         lds_barrier();
-    }
-    if (p.s_last && col_in)
+    };
+    Stage st;
+    Values va, vb;
+    fetch(ch0, st, va);
+    put(lds.buf[0], st);                                    // (segments have an even number of chunks)
+    lds_barrier();
+    if constexpr (SAVE)
+        for (int64_t ch = ch0; ch < ch1; ++ch) step(ch, st, va, va);
+    else
+        for (int64_t ch = ch0; ch < ch1;) {                 // two chunks a round, so that no register is copied while it is loaded
+            step(ch, st, va, vb);
+            if (++ch >= ch1) break;
+            step(ch, st, vb, va);
+            ++ch;
+        }
+    if constexpr (AGG) {
+        if (c0 < p.dvp) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p.entry[((head * p.nseg + un.seg + 1) * DK + 16 * m + 4 * g4 + r) * p.dvp + n0] = S[m][r];
+        } else if (c0 < p.dvp + DK) store_trans<NP, DK>(S, p.trans + (head * (p.nseg - 1) + un.seg) * NP * DK * DK, n0 - p.dvp, g4);
+    } else if (p.s_last && col_in && ch1 == nchunk)
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int d = 16 * m + 4 * g4 + r;
-                if (d < p.dk) p.s_last[(((int64_t)b * p.Hv + h) * p.dk + d) * p.dv + n0] = S[m][r];
+                if (d < p.dk) p.s_last[(head * p.dk + d) * p.dv + n0] = S[m][r];
             }
+}
+
+// ---------------------------------------------------------------- chaining segments
+// entry[s + 1] <- M_s entry[s] + N_s in the order of time (N_s lies in entry[s + 1]; entry[0] is s0), for the adjoint entry[s - 1] <- M_s entry[s] + N_s
+// against it.  A workgroup takes 32 columns, a wavefront 16 rows of them: its rows of M and of N are under way two segments ahead, and only the state
+// itself, in planes through LDS, is waited for (21 us a segment with a wavefront for all rows of 16 columns, 1.5 so).
+template <int NP, int DK, bool ADJ> __global__ __launch_bounds__(DK * 4) void k_delta_join(const DeltaParams p) {
+    constexpr int KS = DK / 32;
+    __shared__ __align__(16) uint16_t st[2][NP][32][DK + 8];
+    const int lane = threadIdx.x & 63, m = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row16 = lane & 15, g4 = lane >> 4;
+    const int n0 = blockIdx.x * 32 + row16, h = blockIdx.y, b = blockIdx.z;
+    const int64_t head = (int64_t)b * p.Hv + h, plane = DK * p.dvp;
+    const float *first = ADJ ? p.ds_last : p.s0;
+    f32x4 S[2];
+    struct Part { f32x4 N[2]; Frag M[KS][NP]; } even, odd;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = 16 * m + 4 * g4 + r, n = n0 + 16 * c;
+            S[c][r] = first && n < p.dv && d < p.dk ? first[(head * p.dk + d) * p.dv + n] : 0.0f;
+        }
+    auto place = [&](int i) { return p.entry + (head * p.nseg + (ADJ ? p.nseg - 2 - i : i + 1)) * plane + (16 * m + 4 * g4) * p.dvp + n0; };
+    auto fetch = [&](int i, Part &a) __attribute__((always_inline)) {
+        if (i > p.nseg - 2) i = p.nseg - 2;                  // (past the end: the last one again, no branch around the loads)
+        const uint16_t *t = p.trans + (head * (p.nseg - 1) + (ADJ ? p.nseg - 2 - i : i)) * NP * DK * DK + (16 * m + row16) * DK + 8 * g4;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) a.M[ks][k].v = *reinterpret_cast<const uint4 *>(t + k * DK * DK + 32 * ks);
+        const float *at = place(i);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) a.N[c][r] = at[r * p.dvp + 16 * c];
+    };
+    auto step = [&](int i, Part &a) __attribute__((always_inline)) {
+        auto &L = st[i & 1];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            uint32_t lo[NP], hi[NP];
+            split2<NP>(S[c][0], S[c][1], lo);
+            split2<NP>(S[c][2], S[c][3], hi);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) *reinterpret_cast<uint2 *>(&L[k][16 * c + row16][16 * m + 4 * g4]) = make_uint2(lo[k], hi[k]);
+            S[c] = a.N[c];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                Frag s[NP];
+#pragma unroll
+                for (int k = 0; k < NP; ++k) s[k].v = *reinterpret_cast<const uint4 *>(&L[k][16 * c + row16][32 * ks + 8 * g4]);
+                S[c] = mm(a.M[ks], s, S[c]);
+            }
+        fetch(i + 2, a);
+        float *at = place(i);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) at[r * p.dvp + 16 * c] = S[c][r];
+    };
+    fetch(0, even);
+    fetch(1, odd);
+    for (int i = 0; i < p.nseg - 1;) {
+        step(i, even);
+        if (++i >= p.nseg - 1) break;
+        step(i, odd);
+        ++i;
+    }
+}
+template <int NP, bool ADJ> static hipError_t launch_join(const DeltaParams &p, hipStream_t s) {
+    const dim3 grid((unsigned)(p.dvp / 32), (unsigned)p.Hv, (unsigned)p.B);
+    if (p.dk > 64) hipLaunchKernelGGL((k_delta_join<NP, 128, ADJ>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((k_delta_join<NP, 64, ADJ>), grid, dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+hipError_t launch_delta_join(const DeltaParams &p, bool adjoint, hipStream_t s) {
+    if (adjoint) return p.np == 3 ? launch_join<3, true>(p, s) : launch_join<2, true>(p, s);
+    return p.np == 3 ? launch_join<3, false>(p, s) : launch_join<2, false>(p, s);
 }
 
 // ---------------------------------------------------------------- launches
@@ -480,25 +620,26 @@ hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s) {
     return p.np == 3 ? launch_prep<1, 3, 2>(p, s) : launch_prep<1, 2, 2>(p, s);
 }
 
-template <class IO, int NPI, int NP, int DK, int NW, bool SAVE> static hipError_t launch_scan_one(const DeltaParams &p, hipStream_t s) {
+template <class IO, int NPI, int NP, int DK, int NW, bool SAVE, bool AGG> static hipError_t launch_scan_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr size_t bytes = sizeof(ScanLds<NPI, NP, DK, NBUF>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    auto k = k_delta_scan<IO, NPI, NP, DK, NW, SAVE>;
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((p.dvp / 16 + NW - 1) / NW), (unsigned)p.Hv, (unsigned)p.B);
-    hipLaunchKernelGGL(k, grid, dim3(NW * 64), bytes, s, p);
+    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + NW - 1) / NW;
+    auto k = k_delta_scan<IO, NPI, NP, DK, NW, SAVE, AGG>;
+    if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k, dim3(delta_blocks(p, AGG ? p.nseg - 1 : p.nseg)), dim3(NW * 64), bytes, s, p);
     return hipGetLastError();
 }
-template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
-    if (p.states) {
-        if (p.wave_cols == 8) return launch_scan_one<IO, NPI, NP, DK, 8, true>(p, s);
-        if (p.wave_cols == 4) return launch_scan_one<IO, NPI, NP, DK, 4, true>(p, s);
-        return launch_scan_one<IO, NPI, NP, DK, 2, true>(p, s);
+template <class IO, int NPI, int NP, int DK, int NW> static hipError_t launch_scan_nw(const DeltaParams &p, hipStream_t s) {
+    if (p.nseg > 1) {
+        if (const hipError_t e = launch_scan_one<IO, NPI, NP, DK, NW, false, true>(p, s)) return e;
+        if (const hipError_t e = launch_delta_join(p, false, s)) return e;
     }
-    if (p.wave_cols == 8) return launch_scan_one<IO, NPI, NP, DK, 8, false>(p, s);
-    if (p.wave_cols == 4) return launch_scan_one<IO, NPI, NP, DK, 4, false>(p, s);
-    return launch_scan_one<IO, NPI, NP, DK, 2, false>(p, s);
+    return p.states ? launch_scan_one<IO, NPI, NP, DK, NW, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, NW, false, false>(p, s);
+}
+template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
+    return delta_waves(p.dvp) == 4 ? launch_scan_nw<IO, NPI, NP, DK, 4>(p, s) : launch_scan_nw<IO, NPI, NP, DK, 2>(p, s);
 }
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_scan_dk<float, 3, 3, 128>(p, s) : launch_scan_dk<float, 3, 3, 64>(p, s);
