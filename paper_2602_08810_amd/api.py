@@ -235,7 +235,9 @@ def lib():
         _binding.bind(_check, L.lrnnx_ckpt_interval(), tuple(ctypes.cast(getattr(L, "lrnnx_" + n), _vp).value for n in (
             "selective_scan_fwd", "selective_scan_bwd", "selective_scan_bwd_workspace_bytes", "selective_scan_fwd_complex",
             "selective_scan_bwd_complex", "selective_step", "selective_step_complex", "lti_diag_scan", "lti_diag_scan_bwd",
-            "diag_scan", "diag_scan_bwd", "workspace_bytes")))
+            "diag_scan", "diag_scan_bwd", "workspace_bytes", "gated_delta_fwd", "gated_delta_fwd_workspace_bytes", "gated_delta_saved_bytes",
+            "gated_delta_bwd", "gated_delta_bwd_workspace_bytes", "gated_delta_step", "block_norm_fwd", "block_norm_bwd",
+            "block_norm_bwd_workspace_bytes")))
         _lib = L
         _native = _binding
     return _lib
@@ -1070,7 +1072,7 @@ def _scratch(workspace, nbytes, device, name="workspace"):
     return workspace
 
 
-@_device_checked
+@_native_first
 def lrnnx_gated_delta_fwd(q, k, v, g, beta, scale=None, s0=None, cu_seqlens=None, return_last_state=False, return_saved=False,
                           out=None, workspace=None):
     """o [B,L,Hv,dv] of the gated delta rule, and optionally the last state [B,Hv,dk,dv] float32 and `saved`, the opaque
@@ -1102,7 +1104,7 @@ def lrnnx_gated_delta_fwd(q, k, v, g, beta, scale=None, s0=None, cu_seqlens=None
     return res[0] if len(res) == 1 else res
 
 
-@_device_checked
+@_native_first
 def lrnnx_gated_delta_bwd(q, k, v, g, beta, do, saved, scale=None, s0=None, ds_last=None, want_ds0=False, cu_seqlens=None,
                           workspace=None):
     """Gradients of sum(do * o) (and sum(ds_last * s_last)) as a dict: dq, dk, dv in the I/O type, dg, dbeta in the gates'
@@ -1133,7 +1135,7 @@ def lrnnx_gated_delta_bwd(q, k, v, g, beta, do, saved, scale=None, s0=None, ds_l
     return res
 
 
-@_device_checked
+@_native_first
 def lrnnx_gated_delta_step(q, k, v, g, beta, state, scale=None, out=None):
     """One token: updates state [B,Hv,dk,dv] float32 in place and returns o [B,Hv,dv]; q, k [B,Hk,dk], v [B,Hv,dv], g, beta
     [B,Hv]; see lrnnx_delta_step_args."""
@@ -1198,7 +1200,7 @@ def _io_dtype_of(dtype):
     return BF16 if dtype == torch.bfloat16 else F32
 
 
-@_device_checked
+@_native_first
 def lrnnx_block_norm_fwd(x, post_weight=None, groups=1, gate=None, gate_act="silu", residual=None, res_scale=None, pre_weight=None,
                          eps=1e-6, out=None):
     """(h, y): the norm, gate and residual sum after a block and the norm before the next; see lrnnx_norm_fwd_args.
@@ -1216,7 +1218,7 @@ def lrnnx_block_norm_fwd(x, post_weight=None, groups=1, gate=None, gate_act="sil
     return h, y
 
 
-@_device_checked
+@_native_first
 def lrnnx_block_norm_bwd(x, dh=None, dy=None, post_weight=None, groups=1, gate=None, gate_act="silu", residual=None, res_scale=None,
                          pre_weight=None, eps=1e-6, workspace=None):
     """Gradients of sum(dh * h) + sum(dy * y) as a dict: dx, and dgate, dresidual, dpost_weight, dres_scale, dpre_weight for

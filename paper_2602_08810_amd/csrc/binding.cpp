@@ -24,6 +24,7 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "../../include/lrnnx.h"
@@ -44,6 +45,15 @@ struct {
     decltype(&lrnnx_diag_scan) diag;
     decltype(&lrnnx_diag_scan_bwd) diag_bwd;
     decltype(&lrnnx_workspace_bytes) bytes;
+    decltype(&lrnnx_gated_delta_fwd) delta_fwd;
+    decltype(&lrnnx_gated_delta_fwd_workspace_bytes) delta_fwd_bytes;
+    decltype(&lrnnx_gated_delta_saved_bytes) delta_saved_bytes;
+    decltype(&lrnnx_gated_delta_bwd) delta_bwd;
+    decltype(&lrnnx_gated_delta_bwd_workspace_bytes) delta_bwd_bytes;
+    decltype(&lrnnx_gated_delta_step) delta_step;
+    decltype(&lrnnx_block_norm_fwd) norm_fwd;
+    decltype(&lrnnx_block_norm_bwd) norm_bwd;
+    decltype(&lrnnx_block_norm_bwd_workspace_bytes) norm_bwd_bytes;
 } lib = {};
 constexpr int kEntries = sizeof(lib) / sizeof(void *);
 int64_t ckpt_interval = 0;
@@ -70,6 +80,15 @@ Names kLti = {8, {"lam", "v", "x0", "return_last_state", "out", "workspace", "pa
 Names kLtiBwd = {8, {"lam", "x", "gx", "x0", "want_dx0", "out", "workspace", "chain_status"}, {}};
 Names kDiag = {7, {"a", "b", "x0", "return_last_state", "out", "workspace", "chain_status"}, {}};
 Names kDiagBwd = {7, {"a", "x", "gx", "x0", "want_dx0", "workspace", "chain_status"}, {}};
+
+enum { G_Q, G_K, G_V, G_G, G_BETA, G_SCALE, G_S0, G_CU, G_LAST, G_SAVED, G_OUT, G_WS };
+Names kDeltaFwd = {12, {"q", "k", "v", "g", "beta", "scale", "s0", "cu_seqlens", "return_last_state", "return_saved", "out", "workspace"}, {}};
+enum { H_DO = 5, H_SAVED, H_SCALE, H_S0, H_DS_LAST, H_DS0, H_CU, H_WS };
+Names kDeltaBwd = {13, {"q", "k", "v", "g", "beta", "do", "saved", "scale", "s0", "ds_last", "want_ds0", "cu_seqlens", "workspace"}, {}};
+Names kDeltaStep = {8, {"q", "k", "v", "g", "beta", "state", "scale", "out"}, {}};
+enum { N_X, N_POST, N_GROUPS, N_GATE, N_ACT, N_RES, N_SCALE, N_PRE, N_EPS, N_OUT };
+Names kNormFwd = {10, {"x", "post_weight", "groups", "gate", "gate_act", "residual", "res_scale", "pre_weight", "eps", "out"}, {}};
+Names kNormBwd = {12, {"x", "dh", "dy", "post_weight", "groups", "gate", "gate_act", "residual", "res_scale", "pre_weight", "eps", "workspace"}, {}};
 
 // The arguments by position of their names (null: not given).  False for anything that the list of names does not
 // cover: unknown, doubled or surplus arguments.
@@ -118,6 +137,15 @@ bool steps(PyObject *o, int64_t &value) {
     int overflow = 0;
     value = PyLong_AsLongLongAndOverflow(o, &overflow);
     return overflow == 0;
+}
+
+// a number given as a Python float, or its default
+bool number(PyObject *o, double otherwise, float &value) {
+    value = (float)otherwise;
+    if (absent(o)) return true;
+    if (!PyFloat_CheckExact(o)) return false;
+    value = (float)PyFloat_AS_DOUBLE(o);
+    return true;
 }
 
 using Shape = c10::SmallVector<int64_t, 5>;
@@ -491,6 +519,239 @@ template <bool LTI> PyObject *chain_bwd(PyObject *args, PyObject *kwargs) {
     return res;
 }
 
+// ---------------------------------------------------------------- gated delta rule and block norms
+// [B,H,d] or [B,L,H,d] with a contiguous last axis: its memory and the strides of the axes before it (b, l, h; l is skipped for a step)
+template <class Ptr> void heads(Call &c, const at::Tensor *t, c10::ScalarType type, c10::IntArrayRef shape, Ptr &p, std::initializer_list<int64_t *> strides) {
+    p = nullptr;
+    if (!t || !c.good) return;
+    if (t->scalar_type() != type || t->sizes() != shape || (t->stride(-1) != 1 && shape.back() > 1)) { c.good = false; return; }
+    p = t->data_ptr();
+    int i = 0;
+    for (int64_t *s : strides) *s = t->stride(i++);
+}
+template <class Ptr> void gates(Call &c, const at::Tensor *t, c10::ScalarType type, c10::IntArrayRef shape, Ptr &p, std::initializer_list<int64_t *> strides) {
+    p = nullptr;
+    if (!t || !c.good) return;
+    if (t->scalar_type() != type || t->sizes() != shape) { c.good = false; return; }
+    p = t->data_ptr();
+    int i = 0;
+    for (int64_t *s : strides) *s = t->stride(i++);
+}
+
+// What the calls over a batch of sequences have in common (packed batches go the general way).
+struct Delta {
+    Shape q, v, g, state;
+    c10::ScalarType io, gate;
+    template <class Args> void read(Call &c, Args &a, PyObject **o, PyObject *scale, PyObject *s0) {
+        const at::Tensor *tq = c.needed(o[G_Q]), *tk = c.needed(o[G_K]), *tv = c.needed(o[G_V]), *tg = c.needed(o[G_G]), *tb = c.needed(o[G_BETA]);
+        const at::Tensor *ts = c.tensor(s0);
+        if (!c.good || tq->dim() != 4 || tv->dim() != 4) { c.good = false; return; }
+        const int64_t B = tq->size(0), L = tq->size(1), Hk = tq->size(2), dk = tq->size(3), Hv = tv->size(2), dv = tv->size(3);
+        io = tv->scalar_type(); gate = tg->scalar_type();
+        if ((io != at::kBFloat16 && io != at::kFloat) || (gate != at::kFloat && gate != io) || !fits32(B) || !fits32(Hk) || !fits32(Hv) || !fits32(dk) || !fits32(dv) ||
+            dk < 1 || !number(scale, 1.0 / std::sqrt((double)dk), a.scale)) { c.good = false; return; }
+        q = {B, L, Hk, dk}; v = {B, L, Hv, dv}; g = {B, L, Hv}; state = {B, Hv, dk, dv};
+        a.struct_size = sizeof(a);
+        a.B = (int32_t)B; a.Hk = (int32_t)Hk; a.Hv = (int32_t)Hv; a.dk = (int32_t)dk; a.dv = (int32_t)dv; a.L = L;
+        a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        a.gate_dtype = gate == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        heads(c, tq, io, q, a.q, {&a.q_stride_b, &a.q_stride_l, &a.q_stride_h});
+        heads(c, tk, io, q, a.k, {&a.k_stride_b, &a.k_stride_l, &a.k_stride_h});
+        heads(c, tv, io, v, a.v, {&a.v_stride_b, &a.v_stride_l, &a.v_stride_h});
+        gates(c, tg, gate, g, a.g, {&a.g_stride_b, &a.g_stride_l, &a.g_stride_h});
+        gates(c, tb, gate, g, a.beta, {&a.beta_stride_b, &a.beta_stride_l, &a.beta_stride_h});
+        c.data(ts, at::kFloat, state, a.s0);
+    }
+};
+
+PyObject *delta_forward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_delta_fwd_args a = {};
+    Call c;
+    bool want_last, want_saved;
+    if (!c.good || !gather(kDeltaFwd, args, kwargs, o) || !absent(o[G_CU]) || !absent(o[G_OUT]) || !absent(o[G_WS]) || !flag(o[G_LAST], false, want_last) ||
+        !flag(o[G_SAVED], false, want_saved)) Py_RETURN_NONE;
+    Delta d;
+    d.read(c, a, o, o[G_SCALE], o[G_S0]);
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor y = c.make(d.v, d.io), last, saved, ws;
+    heads(c, &y, d.io, d.v, a.o, {&a.o_stride_b, &a.o_stride_l, &a.o_stride_h});
+    if (want_last) { last = c.make(d.state, at::kFloat); c.data(&last, at::kFloat, d.state, a.s_last); }
+    if (want_saved) {
+        a.saved_bytes = lib.delta_saved_bytes(&a);
+        saved = c.make({(int64_t)std::max<size_t>(a.saved_bytes, 16)}, at::kByte);
+        a.saved = saved.data_ptr();
+    }
+    ws = c.scratch(a, std::max<size_t>(lib.delta_fwd_bytes(&a), 16));
+    a.stream = c.stream();
+    if (!launched(lib.delta_fwd, a)) return nullptr;
+    if (!want_last && !want_saved) return wrap(y);
+    PyObject *res = PyTuple_New(1 + want_last + want_saved);
+    PyTuple_SET_ITEM(res, 0, wrap(y));
+    if (want_last) PyTuple_SET_ITEM(res, 1, wrap(last));
+    if (want_saved) PyTuple_SET_ITEM(res, 1 + want_last, wrap(saved));
+    return res;
+}
+
+// a dict of new tensors by name
+struct Results {
+    struct { const char *name; at::Tensor t; } outs[8];
+    int n = 0;
+    void *add(const Call &c, const char *name, c10::IntArrayRef shape, c10::ScalarType type) {
+        outs[n].name = name;
+        outs[n].t = c.make(shape, type);
+        return outs[n++].t.data_ptr();
+    }
+    PyObject *dict() {
+        PyObject *res = PyDict_New();
+        for (int i = 0; res && i < n; ++i) {
+            PyObject *t = wrap(outs[i].t);
+            if (!t || PyDict_SetItemString(res, outs[i].name, t) < 0) Py_CLEAR(res);
+            Py_XDECREF(t);
+        }
+        return res;
+    }
+};
+
+PyObject *delta_backward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_delta_bwd_args a = {};
+    Call c;
+    bool want_ds0;
+    if (!c.good || !gather(kDeltaBwd, args, kwargs, o) || !absent(o[H_CU]) || !absent(o[H_WS]) || !flag(o[H_DS0], false, want_ds0)) Py_RETURN_NONE;
+    Delta d;
+    d.read(c, a, o, o[H_SCALE], o[H_S0]);
+    const at::Tensor *dout = c.needed(o[H_DO]), *saved = c.needed(o[H_SAVED]), *dl = c.tensor(o[H_DS_LAST]);
+    if (c.good) {
+        heads(c, dout, d.io, d.v, a.dout, {&a.dout_stride_b, &a.dout_stride_l, &a.dout_stride_h});
+        c.data(saved, at::kByte, {saved->numel()}, a.saved);
+        a.saved_bytes = (size_t)saved->numel();
+        c.data(dl, at::kFloat, d.state, a.ds_last);
+    }
+    if (!c.good) Py_RETURN_NONE;
+    Results r;
+    a.dq = r.add(c, "dq", d.q, d.io);
+    a.dkey = r.add(c, "dk", d.q, d.io);
+    a.dval = r.add(c, "dv", d.v, d.io);
+    a.dg = r.add(c, "dg", d.g, d.gate);
+    a.dbeta = r.add(c, "dbeta", d.g, d.gate);
+    if (want_ds0) a.ds0 = static_cast<float *>(r.add(c, "ds0", d.state, at::kFloat));
+    at::Tensor ws = c.scratch(a, std::max<size_t>(lib.delta_bwd_bytes(&a), 16));
+    a.stream = c.stream();
+    return launched(lib.delta_bwd, a) ? r.dict() : nullptr;
+}
+
+PyObject *delta_step(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_delta_step_args a = {};
+    Call c;
+    if (!c.good || !gather(kDeltaStep, args, kwargs, o) || !absent(o[7])) Py_RETURN_NONE;
+    const at::Tensor *q = c.needed(o[0]), *k = c.needed(o[1]), *v = c.needed(o[2]), *g = c.needed(o[3]), *b = c.needed(o[4]), *s = c.needed(o[5]);
+    if (!c.good || q->dim() != 3 || v->dim() != 3) Py_RETURN_NONE;
+    const int64_t B = q->size(0), Hk = q->size(1), dk = q->size(2), Hv = v->size(1), dv = v->size(2);
+    const c10::ScalarType io = v->scalar_type(), gate = g->scalar_type();
+    if ((io != at::kBFloat16 && io != at::kFloat) || (gate != at::kFloat && gate != io) || !fits32(B) || !fits32(Hk) || !fits32(Hv) || !fits32(dk) || !fits32(dv) ||
+        dk < 1 || !number(o[6], 1.0 / std::sqrt((double)dk), a.scale)) Py_RETURN_NONE;
+    a.struct_size = sizeof(a);
+    a.B = (int32_t)B; a.Hk = (int32_t)Hk; a.Hv = (int32_t)Hv; a.dk = (int32_t)dk; a.dv = (int32_t)dv;
+    a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+    a.gate_dtype = gate == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+    const int64_t qs[] = {B, Hk, dk}, vs[] = {B, Hv, dv}, gs[] = {B, Hv}, ss[] = {B, Hv, dk, dv};
+    heads(c, q, io, qs, a.q, {&a.q_stride_b, &a.q_stride_h});
+    heads(c, k, io, qs, a.k, {&a.k_stride_b, &a.k_stride_h});
+    heads(c, v, io, vs, a.v, {&a.v_stride_b, &a.v_stride_h});
+    gates(c, g, gate, gs, a.g, {&a.g_stride_b, &a.g_stride_h});
+    gates(c, b, gate, gs, a.beta, {&a.beta_stride_b, &a.beta_stride_h});
+    c.data(s, at::kFloat, ss, a.state);
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor y = c.make(vs, io);
+    heads(c, &y, io, vs, a.o, {&a.o_stride_b, &a.o_stride_h});
+    a.stream = c.stream();
+    return launched(lib.delta_step, a) ? wrap(y) : nullptr;
+}
+
+// The inputs of both passes of the block norm: contiguous rows.
+struct Norm {
+    int64_t M = 0, D = 0, groups = 1;
+    c10::ScalarType io, res;
+    bool shared = false;
+    Shape rows, post;
+    template <class Ptr> void row(Call &c, const at::Tensor *t, c10::ScalarType type, Ptr &p, int64_t &stride) {
+        c.data(t, type, rows, p);
+        stride = p ? D : 0;
+    }
+    // o: x, post_weight, groups, gate, gate_act, residual, res_scale, pre_weight, eps; like: what h's type follows without a residual
+    template <class Args> void read(Call &c, Args &a, PyObject *const (&o)[9], const at::Tensor *like) {
+        const at::Tensor *x = c.needed(o[0]), *w = c.tensor(o[1]), *gate = c.tensor(o[3]), *r = c.tensor(o[5]), *scale = c.tensor(o[6]), *pre = c.tensor(o[7]);
+        if (!c.good || x->dim() < 1 || !steps(o[2], groups) || !mode(o[4], {"silu", "sigmoid"}, a.gate_act) || !number(o[8], 1e-6, a.eps)) { c.good = false; return; }
+        if (!o[2]) groups = 1;
+        io = x->scalar_type();
+        res = r ? r->scalar_type() : like ? like->scalar_type() : io;
+        D = x->size(-1);
+        if ((io != at::kBFloat16 && io != at::kFloat) || (res != at::kFloat && res != io) || D < 1 || !fits32(D) || groups < 1 || groups > D || D % groups) { c.good = false; return; }
+        M = x->numel() / D;
+        rows.append(x->sizes().begin(), x->sizes().end());
+        shared = w && groups > 1 && w->dim() == 1 && w->size(0) == D / groups;
+        post = {shared ? D / groups : D};
+        a.struct_size = sizeof(a);
+        a.M = M; a.D = (int32_t)D; a.groups = (int32_t)groups; a.post_shared = shared;
+        a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        a.res_dtype = res == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        row(c, x, io, a.x, a.x_stride);
+        row(c, gate, io, a.gate, a.gate_stride);
+        row(c, r, res, a.residual, a.residual_stride);
+        const int64_t d[] = {D};
+        c.data(w, at::kFloat, post, a.post_weight);
+        c.data(scale, at::kFloat, d, a.res_scale);
+        c.data(pre, at::kFloat, d, a.pre_weight);
+    }
+};
+
+PyObject *norm_forward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_norm_fwd_args a = {};
+    Call c;
+    if (!c.good || !gather(kNormFwd, args, kwargs, o) || !absent(o[N_OUT])) Py_RETURN_NONE;
+    Norm n;
+    n.read(c, a, {o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7], o[8]}, nullptr);
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor h = c.make(n.rows, n.res), y;
+    a.h = h.data_ptr();
+    if (a.pre_weight) { y = c.make(n.rows, n.io); a.y = y.data_ptr(); }
+    a.stream = c.stream();
+    if (!launched(lib.norm_fwd, a)) return nullptr;
+    PyObject *res = PyTuple_New(2);
+    PyTuple_SET_ITEM(res, 0, wrap(h));
+    PyTuple_SET_ITEM(res, 1, a.y ? wrap(y) : given(Py_None));
+    return res;
+}
+
+PyObject *norm_backward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_norm_bwd_args a = {};
+    Call c;
+    if (!c.good || !gather(kNormBwd, args, kwargs, o) || !absent(o[11])) Py_RETURN_NONE;
+    const at::Tensor *dh = c.tensor(o[1]), *dy = c.tensor(o[2]);
+    if (!dh && !dy) Py_RETURN_NONE;
+    Norm n;
+    n.read(c, a, {o[0], o[3], o[4], o[5], o[6], o[7], o[8], o[9], o[10]}, dh);
+    if (c.good) {
+        n.row(c, dh, n.res, a.dh, a.dh_stride);
+        n.row(c, dy, n.io, a.dy, a.dy_stride);
+    }
+    if (!c.good) Py_RETURN_NONE;
+    Results r;
+    a.dx = r.add(c, "dx", n.rows, n.io);
+    if (a.gate) a.dgate = r.add(c, "dgate", n.rows, n.io);
+    if (a.residual) a.dresidual = r.add(c, "dresidual", n.rows, n.res);
+    if (a.post_weight) a.dpost_weight = static_cast<float *>(r.add(c, "dpost_weight", n.post, at::kFloat));
+    if (a.res_scale) a.dres_scale = static_cast<float *>(r.add(c, "dres_scale", {n.D}, at::kFloat));
+    if (a.pre_weight) a.dpre_weight = static_cast<float *>(r.add(c, "dpre_weight", {n.D}, at::kFloat));
+    at::Tensor ws = c.scratch(a, std::max<size_t>(lib.norm_bwd_bytes(n.M, n.D), 16));
+    a.stream = c.stream();
+    return launched(lib.norm_bwd, a) ? r.dict() : nullptr;
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *)> PyObject *entry(PyObject *, PyObject *const *p, Py_ssize_t n) {
     if (n != 2 || !PyTuple_CheckExact(p[0]) || !PyDict_CheckExact(p[1]) || !check_status) Py_RETURN_NONE;
     HANDLE_TH_ERRORS
@@ -530,13 +791,18 @@ PyMethodDef methods[] = {
     method("lrnnx_lti_diag_scan_bwd", entry<chain_bwd<true>>),
     method("lrnnx_diag_scan", entry<chain<false>>),
     method("lrnnx_diag_scan_bwd", entry<chain_bwd<false>>),
+    method("lrnnx_gated_delta_fwd", entry<delta_forward>),
+    method("lrnnx_gated_delta_bwd", entry<delta_backward>),
+    method("lrnnx_gated_delta_step", entry<delta_step>),
+    method("lrnnx_block_norm_fwd", entry<norm_forward>),
+    method("lrnnx_block_norm_bwd", entry<norm_backward>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "usual forms of the entry points' calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__binding() {
-    for (Names *n : {&kFwd, &kFwdComplex, &kBwd, &kStep, &kLti, &kLtiBwd, &kDiag, &kDiagBwd})
+    for (Names *n : {&kFwd, &kFwdComplex, &kBwd, &kStep, &kLti, &kLtiBwd, &kDiag, &kDiagBwd, &kDeltaFwd, &kDeltaBwd, &kDeltaStep, &kNormFwd, &kNormBwd})
         for (int i = 0; i < n->count; ++i)
             if (!(n->key[i] = PyUnicode_InternFromString(n->text[i]))) return nullptr;
     return PyModule_Create(&module);
