@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "kernels.hpp"
 
 namespace lrnnx {
 
@@ -47,17 +48,30 @@ struct DeltaParams {
     uint16_t *trans;                     // [B,Hv,nseg-1,planes,dkp,dkp] what a segment makes of the state that enters it
 };
 
-struct DeltaPack {                       // a strided operand copied into planes
+struct DeltaPack {                       // a strided operand copied into planes, [B,L,H,dp]
     const void *src;
     int64_t sb, sl, sh;
     uint16_t *dst;
     int64_t plane;
-    int B, H, d, dp, planes, io;
+    int H, d, dp, vec;                   // vec: eight elements at a time may be read as 16-byte pieces
+    unsigned items, rows;                // pieces of eight elements a step, steps a workgroup takes at once
+    Divider by_items, by_head;
+};
+struct DeltaPacks {                      // all operands of a call that need it
+    DeltaPack p[3];
+    int n = 0, B, planes, io;
+    int64_t L;
+};
+struct DeltaGather {                     // rows copied one after the other as they are
+    const void *src;
+    int64_t sb, sl, sh;
+    void *dst;
+    int B, H, d, io;
     int64_t L;
 };
 
-hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s);
-hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s);       // copied as it is: planes and dp are not looked at
+hipError_t launch_delta_pack(const DeltaPacks &p, hipStream_t s);
+hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s);
 hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s);

@@ -81,12 +81,17 @@ DeltaRows lay_rows(const Shape &s, Layout &l, const void *src, int H, int width,
     r.sb = s.L * H * padded; r.sl = (int64_t)H * padded; r.sh = padded;
     return r;
 }
-hipError_t copy_rows(const Shape &s, const DeltaRows &r, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, hipStream_t st) {
-    DeltaPack k{};
+void add_pack(const Shape &s, DeltaPacks &all, const DeltaRows &r, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch) {
+    DeltaPack &k = all.p[all.n++];
     k.src = src; k.sb = sb; k.sl = sl; k.sh = sh;
     k.dst = const_cast<uint16_t *>(r.p); k.plane = r.plane;
-    k.B = one_batch ? 1 : s.B; k.H = H; k.d = width; k.dp = padded; k.planes = s.planes; k.io = s.bf16; k.L = s.L;
-    return launch_delta_pack(k, st);
+    k.H = H; k.d = width; k.dp = padded;
+    const int64_t each = s.bf16 ? 8 : 4;                  // elements of 16 bytes
+    k.vec = on16(src) && (one_batch || s.B == 1 || sb % each == 0) && (s.L == 1 || sl % each == 0) && (H == 1 || sh % each == 0);
+    k.items = (unsigned)(H * (padded / 8));
+    k.rows = k.items < 256 ? 256 / k.items : 1;
+    k.by_items = Divider(k.items); k.by_head = Divider((unsigned)(padded / 8));
+    all.B = one_batch ? 1 : s.B; all.planes = s.planes; all.io = s.bf16; all.L = s.L;
 }
 
 template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
@@ -117,9 +122,9 @@ void plan_segments(const Shape &s, bool packed, Layout &l, DeltaParams &p) {
     p.trans = l.take<uint16_t>(heads * (p.nseg - 1) * p.np * s.dkp * s.dkp);
 }
 
-struct FwdPlan { DeltaParams p; bool copy_q, copy_k, copy_v; size_t bytes, saved; };
-FwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *saved) {
-    FwdPlan f{};
+struct DeltaFwdPlan { DeltaParams p; bool copy_q, copy_k, copy_v; size_t bytes, saved; };
+DeltaFwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *saved) {
+    DeltaFwdPlan f{};
     set_inputs(a, s, f.p);
     const bool one = a->cu_seqlens != nullptr;
     f.p.np = !s.bf16 || a->s0 || a->s_last ? 3 : 2;
@@ -139,9 +144,9 @@ FwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, char *
     return f;
 }
 
-struct BwdPlan { DeltaParams p; bool copy_q, copy_k, copy_d; size_t bytes, saved; };
-BwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, char *saved) {
-    BwdPlan f{};
+struct DeltaBwdPlan { DeltaParams p; bool copy_q, copy_k, copy_d; size_t bytes, saved; };
+DeltaBwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, char *saved) {
+    DeltaBwdPlan f{};
     set_inputs(a, s, f.p);
     const bool one = a->cu_seqlens != nullptr;
     f.p.np = adjoint_planes(s, a->s0 != nullptr);
@@ -184,7 +189,7 @@ int lrnnx_gated_delta_fwd(const lrnnx_delta_fwd_args *a) {
     const size_t es = elem(a->io_dtype);
     if (!inputs_on_elements(a) || !on_elem(a->o, es) || !on_elem(a->s_last, 4) || !on16(a->saved) || !on16(a->workspace)) return LRNNX_ERR_INVALID_ARG;
     const Shape s = shape_of(a);
-    FwdPlan f = plan_fwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(a->saved));
+    DeltaFwdPlan f = plan_fwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(a->saved));
     if (!a->workspace || a->workspace_bytes < f.bytes || (a->saved && a->saved_bytes < f.saved)) return LRNNX_ERR_WORKSPACE;
     DeltaParams &p = f.p;
     p.o = a->o; p.o_sb = a->o_stride_b; p.o_sl = a->o_stride_l; p.o_sh = a->o_stride_h; p.s_last = a->s_last;
@@ -192,12 +197,14 @@ int lrnnx_gated_delta_fwd(const lrnnx_delta_fwd_args *a) {
     p.o_vec = (reinterpret_cast<uintptr_t>(a->o) & (4 * es - 1)) == 0 && (one || s.B == 1 || a->o_stride_b % 4 == 0) &&
               (s.L == 1 || a->o_stride_l % 4 == 0) && (s.Hv == 1 || a->o_stride_h % 4 == 0);
     const hipStream_t st = reinterpret_cast<hipStream_t>(a->stream);
-    if (f.copy_q && copy_rows(s, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
-    if (f.copy_k && copy_rows(s, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    DeltaPacks packs;
+    if (f.copy_q) add_pack(s, packs, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one);
+    if (f.copy_k) add_pack(s, packs, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one);
+    if (packs.n && launch_delta_pack(packs, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     if (f.copy_v) {
-        DeltaPack k{};
+        DeltaGather k{};
         k.src = a->v; k.sb = a->v_stride_b; k.sl = a->v_stride_l; k.sh = a->v_stride_h;
-        k.dst = reinterpret_cast<uint16_t *>(const_cast<void *>(p.v));
+        k.dst = const_cast<void *>(p.v);
         k.B = one ? 1 : s.B; k.H = s.Hv; k.d = s.dv; k.io = s.bf16; k.L = s.L;
         if (launch_delta_gather(k, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
@@ -219,7 +226,7 @@ int lrnnx_gated_delta_bwd(const lrnnx_delta_bwd_args *a) {
         !on_elem(a->dval, es) || !on_elem(a->dg, gs) || !on_elem(a->dbeta, gs) || !on_elem(a->ds0, 4) || !on16(a->workspace))
         return LRNNX_ERR_INVALID_ARG;
     const Shape s = shape_of(a);
-    BwdPlan f = plan_bwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(const_cast<void *>(a->saved)));
+    DeltaBwdPlan f = plan_bwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(const_cast<void *>(a->saved)));
     if (!a->workspace || a->workspace_bytes < f.bytes || a->saved_bytes < f.saved) return LRNNX_ERR_WORKSPACE;
     DeltaParams &p = f.p;
     p.ds_last = a->ds_last; p.ds0 = a->ds0;
@@ -228,10 +235,11 @@ int lrnnx_gated_delta_bwd(const lrnnx_delta_bwd_args *a) {
     p.dq = a->dq; p.dkk = a->dkey; p.dvv = a->dval; p.dg = a->dg; p.dbeta = a->dbeta;
     const bool one = a->cu_seqlens != nullptr;
     const hipStream_t st = reinterpret_cast<hipStream_t>(a->stream);
-    if (f.copy_q && copy_rows(s, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
-    if (f.copy_k && copy_rows(s, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
-    if (f.copy_d && copy_rows(s, p.dout, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one, st) != hipSuccess)
-        return LRNNX_ERR_LAUNCH;
+    DeltaPacks packs;
+    if (f.copy_q) add_pack(s, packs, p.q, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one);
+    if (f.copy_k) add_pack(s, packs, p.k, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one);
+    if (f.copy_d) add_pack(s, packs, p.dout, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one);
+    if (packs.n && launch_delta_pack(packs, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     if (launch_delta_adjoint(p, st) != hipSuccess) return LRNNX_ERR_LAUNCH;
     return launch_delta_grads(p, st) == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH;
 }

@@ -11,39 +11,59 @@
 namespace lrnnx {
 
 // ---------------------------------------------------------------- operands in planes
-// A float32 operand, or rows that are not as the matrix kernels read them (width not padded, unaligned), as planes of aligned rows.
-__global__ __launch_bounds__(256) void k_delta_pack(const DeltaPack p) {
-    const int64_t per_row = (int64_t)p.H * (p.dp / 8), n = (int64_t)p.B * p.L * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per_row;
-        const int rest = (int)(i - row * per_row), h = rest / (p.dp / 8), c = rest % (p.dp / 8) * 8;
-        const int64_t b = row / p.L, t = row - b * p.L, from = b * p.sb + t * p.sl + h * p.sh + c;
-        float x[8];
+// A float32 operand, or rows that are not as the matrix kernels read them (width not padded, unaligned), as planes of aligned rows: one launch for
+// all operands of a call, eight elements a thread.
+template <class IO> __global__ __launch_bounds__(256) void k_delta_pack(const DeltaPacks all) {
+    const DeltaPack &p = all.p[blockIdx.z];
+    const unsigned sub = p.rows > 1 ? p.by_items(threadIdx.x) : 0, first = threadIdx.x - sub * p.items;
+    if (sub >= p.rows) return;
+    const int64_t b = blockIdx.y, step = (int64_t)gridDim.x * p.rows;
+    for (int64_t t = (int64_t)blockIdx.x * p.rows + sub; t < all.L; t += step)
+        for (unsigned rest = first; rest < p.items; rest += 256) {
+            const unsigned h = p.by_head(rest), c = (rest - h * (p.dp / 8)) * 8;
+            const int64_t from = b * p.sb + t * p.sl + h * p.sh + c;
+            float x[8] = {};
+            const IO *f = reinterpret_cast<const IO *>(p.src) + from;
+            if (p.vec && c + 8 <= (unsigned)p.d) {
+                uint32_t u[2 * sizeof(IO)];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = 0.0f;
-            if (c + e < p.d) x[e] = p.io ? load_io(reinterpret_cast<const uint16_t *>(p.src) + from + e)
-                                         : load_io(reinterpret_cast<const float *>(p.src) + from + e);
+                for (int i = 0; i < (int)sizeof(IO) / 2; ++i) {
+                    const uint4 v = reinterpret_cast<const uint4 *>(f)[i];
+                    u[4 * i] = v.x; u[4 * i + 1] = v.y; u[4 * i + 2] = v.z; u[4 * i + 3] = v.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(sizeof(IO) == 4 ? u[e % (2 * sizeof(IO))] : e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+            } else if (c < (unsigned)p.d) {
+                IO raw[8];                                   // (all loads under way before the first is looked at)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) raw[e] = f[c + e < (unsigned)p.d ? e : 0];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = c + e < (unsigned)p.d ? load_io(&raw[e]) : 0.0f;
+            }
+            uint16_t *to = p.dst + ((b * all.L + t) * p.H + h) * p.dp + c;
+            Frag g[3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t u[3];
+                split2<3>(x[2 * e], x[2 * e + 1], u);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) g[k].u[e] = u[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) if (k < all.planes) *reinterpret_cast<uint4 *>(to + k * p.plane) = g[k].v;
         }
-        uint16_t *to = p.dst + (row * p.H + h) * p.dp + c;
-        Frag f[3];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t w[3];
-            split2<3>(x[2 * e], x[2 * e + 1], w);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) f[k].u[e] = w[k];
-        }
-        for (int k = 0; k < p.planes; ++k) *reinterpret_cast<uint4 *>(to + k * p.plane) = f[k].v;
-    }
 }
-hipError_t launch_delta_pack(const DeltaPack &p, hipStream_t s) {
-    const int64_t n = (int64_t)p.B * p.L * p.H * (p.dp / 8), blocks = (n + 255) / 256;
-    hipLaunchKernelGGL(k_delta_pack, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, p);
+hipError_t launch_delta_pack(const DeltaPacks &p, hipStream_t s) {
+    unsigned rows = 256;
+    for (int i = 0; i < p.n; ++i) rows = p.p[i].rows < rows ? p.p[i].rows : rows;
+    const int64_t blocks = (p.L + rows - 1) / rows;
+    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)p.B, (unsigned)p.n);
+    if (p.io) hipLaunchKernelGGL(k_delta_pack<uint16_t>, grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(k_delta_pack<float>, grid, dim3(256), 0, s, p);
     return hipGetLastError();
 }
 
-template <class T> __global__ __launch_bounds__(256) void k_delta_gather(const DeltaPack p) {
+template <class T> __global__ __launch_bounds__(256) void k_delta_gather(const DeltaGather p) {
     const int64_t per_row = (int64_t)p.H * p.d, n = (int64_t)p.B * p.L * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / per_row, b = row / p.L, t = row - b * p.L;
@@ -51,7 +71,7 @@ template <class T> __global__ __launch_bounds__(256) void k_delta_gather(const D
         reinterpret_cast<T *>(p.dst)[i] = reinterpret_cast<const T *>(p.src)[b * p.sb + t * p.sl + h * p.sh + (rest - h * p.d)];
     }
 }
-hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s) {
+hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s) {
     const int64_t n = (int64_t)p.B * p.L * p.H * p.d, blocks = (n + 255) / 256;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536));
     if (p.io) hipLaunchKernelGGL(k_delta_gather<uint16_t>, grid, dim3(256), 0, s, p);
@@ -60,14 +80,15 @@ hipError_t launch_delta_gather(const DeltaPack &p, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- the matrices of a chunk
-// One wavefront takes a slot (two chunks) of one value head.  Q K^T and K K^T come from matrix instructions on rows read straight from memory;
-// the inverse is solved a column to a lane, row by row (496 multiply-adds a lane, both chunks side by side): substitution is stable where
-// powers of N would cancel.
+// One wavefront takes a slot (two chunks) of one value head, rows read straight from memory.  Products K K^T and Q K^T are taken in the orientation in
+// which their tiles are operands as they come (A: a step to a lane, its terms in the lane), for the adjoint in the other one too; only N goes through
+// LDS, for the solve: a row of the inverse to a lane, both chunks side by side, each element found and at once taken off the ones before it (496
+// multiply-adds a lane that do not wait for each other).  Substitution is stable where powers of N would cancel.
 template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) void k_delta_prep(const DeltaParams p) {
     constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, NPA);
-    __shared__ __align__(16) float Ns[2][32][W], As[2][32][W];
+    __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][2][32][W];        // N by rows; by columns
     __shared__ double Gs[64];
-    __shared__ float Bs[64];
+    __shared__ __align__(16) float Bs[64];
     const int64_t slot = blockIdx.x / (unsigned)p.Hv;
     const int h = (int)(blockIdx.x - slot * p.Hv), hk = h / (p.Hv / p.Hk);
     const int lane = threadIdx.x, row16 = lane & 15, g4 = lane >> 4;
@@ -76,14 +97,44 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
     int b;
     const int n = delta_slot(p, slot, sq, t0, b);
     if (n == 0) return;
-    const int64_t at = sq.at + t0;
+    const int64_t at = sq.at + t0, mat = (slot * p.Hv + h) * 2;
+    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2;
+    const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
+    const bool in = lane < n;
+    const int64_t tg = at + (in ? lane : 0);
+    const float gr = load_gate(p.g, sq.ib * p.g_sb + tg * p.g_sl + h * p.g_sh, p.io, p.gate_io);
+    const float be = load_gate(p.beta, sq.ib * p.be_sb + tg * p.be_sl + h * p.be_sh, p.io, p.gate_io);
 
+    // tiles of K K^T and Q K^T of each chunk: [step written j][step reading i], and [i][j] for the adjoint
+    f32x4 kk[2][3] = {}, qk[2][3] = {}, qa[2][3] = {}, ka[2] = {};
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        Frag K[KS][2][NPI], Q[KS][2][NPI];
+#pragma unroll
+        for (int i = 0; i < NPI; ++i) {
+            const Buffer kb = buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const uint32_t t = 32 * c + 16 * m + row16;
+                    K[ks][m][i].v = buffer_load16(kb, t * krow + 64 * ks + 16 * g4);
+                    Q[ks][m][i].v = buffer_load16(qb, t * qrow + 64 * ks + 16 * g4);
+                }
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {                     // (0,0), (0,1), (1,1)
+                kk[c][x] = mm(K[ks][x > 1], K[ks][x > 0], kk[c][x]);
+                qk[c][x] = mm(K[ks][x > 1], Q[ks][x > 0], qk[c][x]);
+                if (ADJ > 0) qa[c][x] = mm(Q[ks][x > 0], K[ks][x > 1], qa[c][x]);
+            }
+            if (ADJ > 0) ka[c] = mm(K[ks][1], K[ks][0], ka[c]);   // (the tiles on the diagonal are their own transposes)
+        }
+    }
     // running sums of the log decays over each chunk
     {
-        const bool in = lane < n;
-        const int64_t t = at + (in ? lane : 0);
-        const float gr = load_gate(p.g, sq.ib * p.g_sb + t * p.g_sl + h * p.g_sh, p.io, p.gate_io);
-        const float be = load_gate(p.beta, sq.ib * p.be_sb + t * p.be_sl + h * p.be_sh, p.io, p.gate_io);
         double G = in ? gate_log(gr) : 0.0;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
@@ -91,124 +142,111 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
             if ((lane & 31) >= m) G += o;
         }
         const double end = __shfl(G, 31, 32);
-        const float bv = in ? be : 0.0f;
+        const float bv = in ? be : 0.0f, eg = __expf((float)G), ee = __expf((float)(end - G));
         Gs[lane] = G; Bs[lane] = bv;
-        const float eg = __expf((float)G), ee = __expf((float)(end - G));
-        const int64_t mat = (slot * p.Hv + h) * 2 + (lane >> 5);
-        float *sc = reinterpret_cast<float *>(p.mats + (mat + 1) * MW - 192) + (lane & 31);
+        float *sc = reinterpret_cast<float *>(p.mats + (mat + (lane >> 5) + 1) * MW - 192) + (lane & 31);
         sc[0] = eg; sc[32] = ee; sc[64] = bv;
         if constexpr (ADJ > 0) {
-            sc = reinterpret_cast<float *>(p.mats_adj + (mat + 1) * AW - 192) + (lane & 31);
+            sc = reinterpret_cast<float *>(p.mats_adj + (mat + (lane >> 5) + 1) * AW - 192) + (lane & 31);
             sc[0] = eg; sc[32] = ee; sc[64] = bv;
         }
     }
-    __syncthreads();
-
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const uint16_t *kp = p.k.p + sq.ib * p.k.sb + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + hk * p.q.sh;
-        f32x4 kk[3] = {}, qk[3] = {};                     // tiles (0,0), (1,0), (1,1)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            Frag K[2][NPI], Q[2][NPI];
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const int t = 32 * c + 16 * m + row16;
-                const bool in = t < n;
-                const int64_t tk = at + (in ? t : 0);
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    K[m][i].v = *reinterpret_cast<const uint4 *>(kp + i * p.k.plane + tk * p.k.sl + 32 * ks + 8 * g4);
-                    Q[m][i].v = *reinterpret_cast<const uint4 *>(qp + i * p.q.plane + tk * p.q.sl + 32 * ks + 8 * g4);
-                }
-                if (!in) { zero_frags(K[m]); zero_frags(Q[m]); }
-            }
-            kk[0] = mm(K[0], K[0], kk[0]); kk[1] = mm(K[1], K[0], kk[1]); kk[2] = mm(K[1], K[1], kk[2]);
-            qk[0] = mm(Q[0], K[0], qk[0]); qk[1] = mm(Q[1], K[0], qk[1]); qk[2] = mm(Q[1], K[1], qk[2]);
-        }
-#pragma unroll
-        for (int x = 0; x < 3; ++x) {
-            const int mi = x > 0, mj = x > 1, j = 16 * mj + row16;
-            const double Gj = Gs[32 * c + j];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * mi + 4 * g4 + r;
-                const float d = j <= i ? __expf((float)(Gs[32 * c + i] - Gj)) : 0.0f;
-                Ns[c][i][j] = j < i ? d * kk[x][r] : 0.0f;
-                As[c][i][j] = j <= i ? p.scale * d * qk[x][r] : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) As[c][4 * g4 + r][16 + row16] = 0.0f;
-    }
-    __syncthreads();
-
-    const int64_t mat = (slot * p.Hv + h) * 2;
-    auto by_rows = [&](const float (*M)[W], int m, auto np, uint16_t *to) {          // rows of the matrix along the lanes
+    lds_barrier();
+    auto store = [&](const f32x4 &lo, const f32x4 &hi, int m, auto np, uint16_t *to) {
         constexpr int P = decltype(np)::value;
-        const f32x4 lo = *reinterpret_cast<const f32x4 *>(&M[16 * m + row16][4 * g4]);
-        const f32x4 hi = *reinterpret_cast<const f32x4 *>(&M[16 * m + row16][16 + 4 * g4]);
-        Frag f[P];
-        split_tiles<P>(lo, hi, f);
-#pragma unroll
-        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4 *>(to + (m * P + i) * 512 + lane * 8) = f[i].v;
-    };
-    auto by_columns = [&](const float (*M)[W], int m, auto np, uint16_t *to) {       // columns along the lanes
-        constexpr int P = decltype(np)::value;
-        f32x4 lo, hi;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { lo[r] = M[4 * g4 + r][16 * m + row16]; hi[r] = M[16 + 4 * g4 + r][16 * m + row16]; }
         Frag f[P];
         split_tiles<P>(lo, hi, f);
 #pragma unroll
         for (int i = 0; i < P; ++i) *reinterpret_cast<uint4 *>(to + (m * P + i) * 512 + lane * 8) = f[i].v;
     };
     using ForA = std::integral_constant<int, NPA>;
-    using ForT = std::integral_constant<int, NP>;
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < 2; ++c) {
+        f32x4 A[3], At[3];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            by_rows(As[c], m, ForA(), p.mats + (mat + c) * MW + 2 * NP * 512);
-            if (ADJ > 0) by_columns(As[c], m, ForA(), p.mats_adj + (mat + c) * AW + 2 * ADJ * 512);
+        for (int x = 0; x < 3; ++x) {
+            {                                                // a reading step to a lane
+                const int i = 16 * (x > 0) + row16, j0 = 16 * (x > 1) + 4 * g4;
+                const double Gi = Gs[32 * c + i];
+                f32x4 N;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float d = j0 + r <= i ? __expf((float)(Gi - Gs[32 * c + j0 + r])) : 0.0f;
+                    N[r] = j0 + r < i ? d * kk[c][x][r] : 0.0f;
+                    A[x][r] = j0 + r <= i ? p.scale * d * qk[c][x][r] : 0.0f;
+                }
+                *reinterpret_cast<f32x4 *>(&Ns[0][c][i][j0]) = N;
+            }
+            if constexpr (ADJ > 0) {                         // a written step to a lane
+                const int j = 16 * (x > 1) + row16, i0 = 16 * (x > 0) + 4 * g4;
+                const double Gj = Gs[32 * c + j];
+                f32x4 N;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float d = j <= i0 + r ? __expf((float)(Gs[32 * c + i0 + r] - Gj)) : 0.0f;
+                    N[r] = j < i0 + r ? d * (x == 1 ? ka[c][r] : kk[c][x][r]) : 0.0f;
+                    At[x][r] = j <= i0 + r ? p.scale * d * qa[c][x][r] : 0.0f;
+                }
+                *reinterpret_cast<f32x4 *>(&Ns[1][c][j][i0]) = N;
+            }
         }
-    __syncthreads();
-
-    // X = (I + N diag(beta))^-1 (and (I + diag(beta) N)^-1): lane (c, j) solves for column j of chunk c
-    const int c = lane >> 5, j = lane & 31;
-    {
-        float y[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float acc = 0.0f;
-#pragma unroll
-            for (int l = 0; l < i; ++l) acc = __builtin_fmaf(Ns[c][i][l], y[l], acc);
-            const float x = (i == j ? 1.0f : 0.0f) - acc;
-            y[i] = Bs[32 * c + i] * x;
-            As[c][i][j] = x;
+        const f32x4 none = {};
+        uint16_t *to = p.mats + (mat + c) * MW + 2 * NP * 512;
+        store(A[0], none, 0, ForA(), to);
+        store(A[1], A[2], 1, ForA(), to);
+        if constexpr (ADJ > 0) {
+            to = p.mats_adj + (mat + c) * AW + 2 * ADJ * 512;
+            store(At[0], At[1], 0, ForA(), to);
+            store(none, At[2], 1, ForA(), to);
         }
     }
-    __syncthreads();
+    lds_barrier();
+
+    // rows of the inverses: lane (c, i) solves for row i of chunk c
+    const int c = lane >> 5, own = lane & 31;
+    auto emit = [&](float (&x)[32], float (*N)[32][W], auto np, uint16_t *to, int64_t words) {       // through LDS into the operands' order
+        lds_barrier();
 #pragma unroll
-    for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-        for (int m = 0; m < 2; ++m) by_rows(As[cc], m, ForT(), p.mats + (mat + cc) * MW);
-    if constexpr (ADJ > 0) {
-        __syncthreads();
-        float x[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float acc = 0.0f;
-#pragma unroll
-            for (int l = 0; l < i; ++l) acc = __builtin_fmaf(Ns[c][i][l], x[l], acc);
-            x[i] = (i == j ? 1.0f : 0.0f) - Bs[32 * c + i] * acc;
-            As[c][i][j] = x[i];
-        }
-        __syncthreads();
+        for (int j = 0; j < 32; j += 4) *reinterpret_cast<f32x4 *>(&N[c][own][j]) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+        lds_barrier();
 #pragma unroll
         for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) by_columns(As[cc], m, std::integral_constant<int, ADJ>(), p.mats_adj + (mat + cc) * AW);
+            for (int m = 0; m < 2; ++m)
+                store(*reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][4 * g4]), *reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][16 + 4 * g4]),
+                      m, np, to + (mat + cc) * words);
+    };
+    {                                                        // X (I + N diag(beta)) = I, from the last column to the first
+        float x[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = 0.0f;            // the sums over later columns first, then the element
+#pragma unroll
+        for (int l = 31; l >= 0; --l) {
+            x[l] = (l == own ? 1.0f : 0.0f) - Bs[32 * c + l] * x[l];
+#pragma unroll
+            for (int j = 0; j < l; j += 4) {
+                const f32x4 N = *reinterpret_cast<const f32x4 *>(&Ns[0][c][l][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (j + e < l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
+            }
+        }
+        emit(x, Ns[0], std::integral_constant<int, NP>(), p.mats, MW);
+    }
+    if constexpr (ADJ > 0) {                                 // X (I + N^T diag(beta)) = I, from the first column to the last
+        float x[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = 0.0f;
+#pragma unroll
+        for (int l = 0; l < 32; ++l) {
+            x[l] = (l == own ? 1.0f : 0.0f) - Bs[32 * c + l] * x[l];
+#pragma unroll
+            for (int j = (l + 1) & ~3; j < 32; j += 4) {
+                const f32x4 N = *reinterpret_cast<const f32x4 *>(&Ns[1][c][l][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (j + e > l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
+            }
+        }
+        emit(x, Ns[1], std::integral_constant<int, ADJ>(), p.mats_adj, AW);
     }
 }
 
@@ -366,7 +404,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
 
         // K S0 and (transposed: a step to a lane) Q S0
-        constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
+        constexpr bool EARLY = NPI == 1 || DK == 64;        // operands read well before they are used
         Frag kf[EARLY ? KS : 1][2][NPI], qf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], af[2][NPA];
         f32x4 gam[2], be[2], en[2];
         auto read_kq = [&](int ks, int at) {
