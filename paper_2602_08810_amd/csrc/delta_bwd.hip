@@ -226,14 +226,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
                         if (!AGG) Zt[m] = mfma(uf[j], tf[m][i], Zt[m]);                      // a step to a lane, for wide stores
                     }
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[m][r] *= gend;
-            if constexpr (!EARLY)
+        if constexpr (EARLY) mm_each(qtf, wf, S);
+        else
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) qtf[0][i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-            S[m] = mm(qtf[EARLY ? m : 0], wf, S[m]);
-        }
+                S[m] = mm(qtf[0], wf, S[m]);
+            }
         f32x4 R[2];                                         // -exp(G) beta z
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -241,13 +244,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
             for (int r = 0; r < 4; ++r) R[m][r] = -gam[m][r] * be[m][r] * Z[m][r];
         Frag rf[NP];
         split_tiles<NP>(R[0], R[1], rf, neg);
+        if constexpr (EARLY) mm_each(ktf, rf, S);
+        else
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if constexpr (!EARLY)
+            for (int m = 0; m < MT; ++m) {
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-            S[m] = mm(ktf[EARLY ? m : 0], rf, S[m]);
-        }
+                S[m] = mm(ktf[0], rf, S[m]);
+            }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             const int t = 16 * m + row16;

@@ -39,6 +39,18 @@ template <int NA, int NB> __device__ __forceinline__ f32x4 mm(const Frag (&a)[NA
     return c;
 }
 
+// the same for several results with one operand in common, product by product: neighbours do not wait for each other's sums
+template <int N, int NA, int NB> __device__ __forceinline__ void mm_each(const Frag (&a)[N][NA], const Frag (&b)[NB], f32x4 (&c)[N]) {
+    constexpr int M = NA > NB ? NA : NB;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < M)
+#pragma unroll
+                for (int m = 0; m < N; ++m) c[m] = mfma(a[m][i], b[j], c[m]);
+}
+
 __device__ __forceinline__ float hi_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack_hi(float a, float b) {        // the upper halves of two numbers
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);

@@ -491,13 +491,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[m][r] *= gend;
+        if constexpr (EARLY) mm_each(ktf, df, S);
+        else
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if constexpr (!EARLY)
+            for (int m = 0; m < MT; ++m) {
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-            S[m] = mm(ktf[EARLY ? m : 0], df, S[m]);
-        }
+                S[m] = mm(ktf[0], df, S[m]);
+            }
         if (SAVE && c0 < p.dvp) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
@@ -512,13 +513,24 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                             make_uint2(lo[i], hi[i]);
             }
         }
+        if constexpr (!AGG) {                               // O
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const float gs = p.scale * B.scal[16 * m + row16];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) O[m][r] *= gs;
+            }
+#pragma unroll
+            for (int i = 0; i < NPO; ++i)
+#pragma unroll
+                for (int j = 0; j < NPA; ++j)
+                    if (i + j < (NPO > NPA ? NPO : NPA))
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) O[m] = mfma(uf[i], af[m][j], O[m]);
+        }
         if constexpr (!AGG)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {                       // O
-            const float gs = p.scale * B.scal[16 * m + row16];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) O[m][r] *= gs;
-            O[m] = mm(uf, af[m], O[m]);
+        for (int m = 0; m < 2; ++m) {
             const int t = 16 * m + row16;
             IO *to = op + (t0 + t) * p.o_sl;
             if (wide) { if (t < n) store4(to, O[m]); }
