@@ -36,10 +36,12 @@ struct DeltaParams {
     uint16_t *mats;                      // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands, and the gates (chunk_words)
     uint16_t *mats_adj;                  // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
     uint16_t *states, *err;              // saved for the backward pass; null: not wanted
+    float *units;                        // and with bfloat16 I/O the powers of two of their blocks of 16 columns: S0 (G), E (2 chunks by G) of a slot's head
     // backward
     const float *ds_last;
     float *ds0;
     uint16_t *dstates, *z;
+    float *dunits;                       // likewise S1's (G), Z's (2 G)
     void *dq, *dkk, *dvv, *dg, *dbeta;
     int np, np_adjoint;                  // planes of the state chain, of its adjoint
     // segments of the time axis that are walked side by side (one sequence of a batch entry alone does not fill the chip); 1: none

@@ -64,8 +64,9 @@ inline int64_t mats(const Shape &s) { return s.nslots * s.Hv * 2; }
 inline int a_planes(const Shape &s) { return s.bf16 ? 2 : 3; }
 
 void lay_saved(const Shape &s, bool s0, Layout &l, DeltaParams &p) {
-    p.states = l.take<uint16_t>(s.nslots * s.Hv * (s.bf16 ? 1 : 3) * s.dkp * s.dvp);
-    p.err = l.take<uint16_t>((int64_t)(s.bf16 ? 2 : 3) * s.rows * s.Hv * s.dvp);
+    p.states = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
+    p.err = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
+    if (s.bf16) p.units = l.take<float>(s.nslots * s.Hv * 3 * (s.dvp / 16));
     p.mats_adj = l.take<uint16_t>(mats(s) * chunk_words(adjoint_planes(s, s0), a_planes(s)));
 }
 
@@ -155,8 +156,9 @@ DeltaBwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, c
     f.p.k = lay_rows(s, l, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, f.copy_k);
     f.p.dout = lay_rows(s, l, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one, f.copy_d);
     lay_saved(s, a->s0 != nullptr, sv, f.p);
-    f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * (s.bf16 ? 1 : 3) * s.dkp * s.dvp);
-    f.p.z = l.take<uint16_t>((int64_t)(s.bf16 ? 2 : 3) * s.rows * s.Hv * s.dvp);
+    f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
+    f.p.z = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
+    if (s.bf16) f.p.dunits = l.take<float>(s.nslots * s.Hv * 3 * (s.dvp / 16));
     plan_segments(s, one, l, f.p);
     f.bytes = l.at; f.saved = sv.at;
     return f;

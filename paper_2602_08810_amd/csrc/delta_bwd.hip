@@ -30,7 +30,7 @@ template <int NPI, int NP, int DK, int NBUF> struct AdjLds {
 // (walk of 4 x 4096 steps, 16 heads of 128 x 128: 385 -> 346 us; the forward walk gains nothing by it).
 template <int NPI, int NP, int DK, int NW, bool AGG, bool DEEP>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 1 : 2, DEEP ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
-    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
+    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     extern __shared__ __align__(16) char lds_raw[];
     using Lds = AdjLds<NPI, NP, DK, NBUF>;
@@ -142,17 +142,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
         fetch(ch - (DEEP ? 2 : 1), cur);
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
-        if (!AGG && ((ch & 1) || ch == nchunk - 1) && mine) {
-            uint16_t *to = p.dstates + (sh * NPS * p.dvp + n0) * DK + 4 * g4;            // turned: a column to a row
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                uint32_t lo[NPS], hi[NPS];
-                split2<NPS>(S[m][0], S[m][1], lo);
-                split2<NPS>(S[m][2], S[m][3], hi);
-#pragma unroll
-                for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + (int64_t)i * p.dvp * DK + 16 * m) = make_uint2(lo[i], hi[i]);
-            }
-        }
+        const int G = p.dvp / 16;
+        float *units = p.dunits + sh * 3 * G + c0 / 16;
+        if (!AGG && ((ch & 1) || ch == nchunk - 1) && mine)
+            save_state<NPS, DK>(S, p.dstates + (sh * NPS * p.dvp + n0) * DK + 4 * g4, (int64_t)p.dvp * DK, units);
         constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
         Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NPA];
         f32x4 gam[2], be[2], en[2];
@@ -252,17 +245,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
                 for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                 S[m] = mm(ktf[0], rf, S[m]);
             }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int t = 16 * m + row16;
-            uint32_t lo[NPE], hi[NPE];
-            split2<NPE>(Zt[m][0], Zt[m][1], lo);
-            split2<NPE>(Zt[m][2], Zt[m][3], hi);
-            if (!AGG && t < n && mine)
-#pragma unroll
-                for (int i = 0; i < NPE; ++i)
-                    *reinterpret_cast<uint2 *>(p.z + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + t) * p.Hv + h) * p.dvp + c0 + 4 * g4) = make_uint2(lo[i], hi[i]);
-        }
+        if (!AGG && mine)
+            save_rows<NPS>(Zt, p.z + ((sq.row + t0 + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n, units + (1 + (ch & 1)) * G);
         if (NBUF == 1) lds_barrier();
         put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0], next);
         lds_barrier();
@@ -309,18 +294,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 // The columns of v come through LDS 32 at a time (rows of dO, E, Z and of both states, the next ones under way meanwhile), then K and Q, as rows
 // and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.
 template <int NPI, int DK> struct GradLds {
-    static constexpr int NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, ROWS = NPI == 3 ? 0 : 1;
+    static constexpr int ROWS = NPI == 3 ? 0 : 1;
     union {
-        struct { uint16_t e[NPE][64][40], z[NPE][64][40], d[NPI][64][40], s0[NPS][DK][40], s1[NPS][DK][40]; } v;
+        struct { uint16_t e[NPI][64][40], z[NPI][64][40], d[NPI][64][40], s0[NPI][DK][40], s1[NPI][DK][40]; } v;
         struct { uint16_t kt[NPI][DK][72], qt[NPI][DK][72], kr[ROWS + 1][ROWS ? 64 : 1][DK + 8]; } k;      // kr: rows of K and of Q
     };
     double G[64];
-    float beta[64], dG[64], ends[4], dots[4];
+    float beta[64], dG[64], ends[4], dots[4], most[4];
 };
 
 template <class IO, int NPI, int DK, bool SHARED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 && !SHARED ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
-    constexpr int KS = DK / 32, MT = DK / 16, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2, NPF = NPI == 3 ? 3 : 2;
+    constexpr int KS = DK / 32, MT = DK / 16, NPF = NPI == 3 ? 3 : 2;
+    constexpr bool UNITS = NPI == 1;                        // E, Z, the states and here dO too: 16-bit floating point with a power of two a block
     constexpr bool ROWS = NPI == 1;                         // rows of K and Q in LDS too; else from memory
     extern __shared__ __align__(16) char lds_raw[];
     GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
@@ -347,17 +333,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
         const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
         const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
         const int64_t eplane = rows * p.Hv * p.dvp;
-        const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPS * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPS * DK * p.dvp;
+        const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPI * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPI * DK * p.dvp;
         const int ksv = p.dvp / 32;
 
         // 32 columns of v on their way: a thread brings 16 bytes of a row of dO and of each plane of E and Z, and of the states, which lie a column of v to
         // a row, four rows by four elements (the first 2 DK threads)
-        uint4 ereg[NPE], zreg[NPE], dreg[NPI];
-        uint2 areg[NPS][4], breg[NPS][4];
+        uint4 ereg[NPI], zreg[NPI], dreg[NPI];
+        uint2 areg[NPI][4], breg[NPI][4];
         const int tr = tid >> 2, tc = (tid & 3) * 16, sq4 = tid / (DK / 4), sd4 = tid % (DK / 4);
         auto fetch = [&](int ks) {
 #pragma unroll
-            for (int i = 0; i < NPE; ++i) {
+            for (int i = 0; i < NPI; ++i) {
                 ereg[i] = buffer_load16(buffer_of(ep + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
                 zreg[i] = buffer_load16(buffer_of(zp + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
             }
@@ -365,7 +351,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
             for (int i = 0; i < NPI; ++i)
                 dreg[i] = buffer_load16(buffer_of(dp + i * p.dout.plane, (int64_t)(n - 1) * drow + 2 * p.dvp), tr * drow + 64 * ks + tc);
 #pragma unroll
-            for (int i = 0; i < NPS; ++i)
+            for (int i = 0; i < NPI; ++i)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * 2) : kOutside;
@@ -373,8 +359,35 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                     breg[i][x] = buffer_load8(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
                 }
         };
+        // the blocks' units: a slot's largest of each kind, and the others' share of it
+        float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
+        const int G = p.dvp / 16;
+        if constexpr (UNITS) {
+            const float *fu = p.units + (slot * p.Hv + h) * 3 * G, *bu = p.dunits + (slot * p.Hv + h) * 3 * G;
+            const int in = (n > 32 ? 2 : 1) * G;
+            buffer_load(buffer_of(fu, 4 * G), 4 * lane, rA);
+            buffer_load(buffer_of(fu + G, 4 * in), 4 * lane, rE);
+            buffer_load(buffer_of(bu, 4 * G), 4 * lane, rB);
+            buffer_load(buffer_of(bu + G, 4 * in), 4 * lane, rZ);
+        }
         fetch(0);
-        lds_barrier();                                      // what the last head left in LDS has been read
+        if constexpr (UNITS) {
+            // the largest of dO, whose rows are read once more for it
+            const Buffer db = buffer_of(dp, (int64_t)(n - 1) * drow + 2 * p.dvp);
+            uint32_t most = 0;
+            for (int ks = 0; ks < ksv; ks += 4) {
+                uint4 d[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) d[x] = buffer_load16(db, ks + x < ksv ? tr * drow + 64 * (ks + x) + tc : kOutside);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) most = max_halves(max_halves(most, max_halves(d[x].x, d[x].y)), max_halves(d[x].z, d[x].w));
+            }
+            most = most << 16 > (most & 0x7fff0000u) ? most << 16 : most & 0x7fff0000u;
+            const float whole = wave_max(__uint_as_float(most));
+            if (lane == 0) lds.most[wave] = whole;
+            uA = wave_max(rA); uE = wave_max(rE); uB = wave_max(rB); uZ = wave_max(rZ);
+            rA *= inverse_unit(uA); rE *= inverse_unit(uE); rB *= inverse_unit(uB); rZ *= inverse_unit(uZ);
+        }
         if (wave == 0) {
             const bool in = lane < n;
             const int64_t t = at + (in ? lane : 0);
@@ -390,104 +403,162 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
             lds.beta[lane] = in ? be : 0.0f;
         }
 
-        f32x4 P1t[4] = {}, P1[4] = {}, P2t[4] = {}, P2[4] = {};      // dO_own . e_j; dO_i . e_own; z_own . e_j; z_i . e_own
+        // Products with 16 others' steps at a time: earlier ones wrote what this wavefront's read (e_j . dO_own, e_j . z_own), later ones read what it wrote
+        // (dO_i . e_own, z_i . e_own); its own 16 are both, the second kind of them apart.
+        f32x4 P1[4] = {}, P2[4] = {}, P1own = {}, P2own = {};
         f32x4 qs[MT], kr[MT], kw[MT];                                // S0 dO, S0 z, dS1 e of the lane's step
 #pragma unroll
         for (int m = 0; m < MT; ++m) qs[m] = kr[m] = kw[m] = f32x4{};
+        auto mv = [](const Frag (&a)[NPI], const Frag (&b)[NPI], f32x4 c) __attribute__((always_inline)) -> f32x4 {
+            if constexpr (UNITS) return mfma16(a[0], b[0], c);
+            else return mm(a, b, c);
+        };
         float dbeta = 0.0f, sdot = 0.0f, bown = 0.0f;
-        for (int ks = 0; ks < ksv; ++ks) {
-            if (ks > 0) lds_barrier();
-            auto &L = lds.v;
+        // K and Q of the slot, 16 quads of steps by DK / 4 quads of columns, under way during the last 32 columns
+        constexpr int IQ = DK / 64;
+        uint2 kw4[NPI][IQ * 4], qw4[NPI][IQ * 4];
+        auto fetch_kq = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < NPE; ++i) {
-                *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = ereg[i];
-                *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = zreg[i];
+            for (int pl = 0; pl < NPI; ++pl) {
+                const Buffer kb = buffer_of(kp + pl * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
+#pragma unroll
+                for (int x = 0; x < IQ; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4);
+                        kw4[pl][4 * x + e] = buffer_load8(kb, (4 * tq + e) * krow + 8 * dc);
+                        qw4[pl][4 * x + e] = buffer_load8(qb, (4 * tq + e) * qrow + 8 * dc);
+                    }
+            }
+        };
+        auto columns = [&](int ks, auto last) __attribute__((always_inline)) {
+            lds_barrier();                                  // what was there in LDS has been read
+            auto &L = lds.v;
+            if constexpr (UNITS) uD = block_unit(fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3])));
+            uint32_t pE = 0, pZ = 0, pA = 0, pB = 0;
+            if constexpr (UNITS) {                          // brought to the slot's units
+                const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 5) * G, gs = 2 * ks + (sq4 >> 2 & 1);
+                const float fE = __shfl(rE, ge, 64), fZ = __shfl(rZ, ge, 64), fA = __shfl(rA, gs, 64), fB = __shfl(rB, gs, 64);
+                pE = pack_f16(fE, fE); pZ = pack_f16(fZ, fZ); pA = pack_f16(fA, fA); pB = pack_f16(fB, fB);
+            }
+            auto times = [&](uint32_t x, uint32_t f) __attribute__((always_inline)) -> uint32_t {
+                return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f)) : x;
+            };
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                const uint4 e = ereg[i], z = zreg[i];
+                *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
+                *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = make_uint4(times(z.x, pZ), times(z.y, pZ), times(z.z, pZ), times(z.w, pZ));
             }
 #pragma unroll
-            for (int i = 0; i < NPI; ++i) *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = dreg[i];
+            for (int i = 0; i < NPI; ++i) {
+                uint4 d = dreg[i];
+                if constexpr (UNITS) {
+                    const float inv = inverse_unit(uD);
+                    auto conv = [&](uint32_t x) __attribute__((always_inline)) { return pack_f16(__uint_as_float(x << 16) * inv, hi_part(__uint_as_float(x)) * inv); };
+                    d = make_uint4(conv(d.x), conv(d.y), conv(d.z), conv(d.w));
+                }
+                *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = d;
+            }
 #pragma unroll
-            for (int i = 0; i < NPS; ++i)
+            for (int i = 0; i < NPI; ++i)
                 if (tid < 2 * DK) {
                     uint2 c[4], d[4];
                     transpose_quad(areg[i], c);
                     transpose_quad(breg[i], d);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = c[x];
-                        *reinterpret_cast<uint2 *>(&L.s1[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = d[x];
+                        *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(c[x].x, pA), times(c[x].y, pA));
+                        *reinterpret_cast<uint2 *>(&L.s1[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(d[x].x, pB), times(d[x].y, pB));
                     }
                 }
-            if (ks + 1 < ksv) fetch(ks + 1);
+            if constexpr (last) fetch_kq();
+            else fetch(ks + 1);
             lds_barrier();
             bown = lds.beta[own];
-            Frag dO[NPI], e[NPE], z[NPE];
+            Frag dO[NPI], e[NPI], z[NPI];
 #pragma unroll
             for (int i = 0; i < NPI; ++i) dO[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][own][8 * g4]);
 #pragma unroll
-            for (int i = 0; i < NPE; ++i) {
+            for (int i = 0; i < NPI; ++i) {
                 e[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][own][8 * g4]);
                 z[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][own][8 * g4]);
             }
             // the states' products, and <S0, dS1> of a quarter of their rows
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                Frag s0[NPS], s1[NPS];
+                Frag s0[NPI], s1[NPI];
 #pragma unroll
-                for (int i = 0; i < NPS; ++i) {
+                for (int i = 0; i < NPI; ++i) {
                     s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                     s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                 }
-                qs[m] = mm(s0, dO, qs[m]);
-                kr[m] = mm(s0, z, kr[m]);
-                kw[m] = mm(s1, e, kw[m]);
-                if ((m & 3) == wave)
+                qs[m] = mv(s0, dO, qs[m]);
+                kr[m] = mv(s0, z, kr[m]);
+                kw[m] = mv(s1, e, kw[m]);
+                if (m & 1) reads_first();
+            }
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
+            for (int y = 0; y < MT / 4; ++y) {
+                const int m = 4 * y + wave;
+                Frag s0[NPI], s1[NPI];
+#pragma unroll
+                for (int i = 0; i < NPI; ++i) {
+                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    if constexpr (UNITS) sdot = __builtin_amdgcn_fdot2(s0[0].p16[x], s1[0].p16[x], sdot, false);
+                    else {
                         float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
 #pragma unroll
-                        for (int i = NPS - 1; i >= 0; --i) {
+                        for (int i = NPI - 1; i >= 0; --i) {
                             al += __uint_as_float(s1[i].u[x] << 16); ah += hi_part(__uint_as_float(s1[i].u[x]));
                             cl += __uint_as_float(s0[i].u[x] << 16); chh += hi_part(__uint_as_float(s0[i].u[x]));
                         }
                         sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
                     }
+                }
             }
             // with the other steps
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-                if (m <= wave) {
-                    Frag er[NPE];
+                Frag r1[NPI], r2[NPI], c1[NPI], c2[NPI];
 #pragma unroll
-                    for (int i = 0; i < NPE; ++i) er[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][16 * m + row16][8 * g4]);
-                    P1t[m] = mm(er, dO, P1t[m]);
-                    P2t[m] = mm(er, z, P2t[m]);
+                for (int i = 0; i < NPI; ++i) {
+                    r1[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.d)[i][16 * m + row16][8 * g4]);
+                    r2[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.z)[i][16 * m + row16][8 * g4]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) { c1[i].u[x] = m <= wave ? dO[i].u[x] : e[i].u[x]; c2[i].u[x] = m <= wave ? z[i].u[x] : e[i].u[x]; }
                 }
-                if (m >= wave) {
-                    Frag dr[NPI], zr[NPE];
-#pragma unroll
-                    for (int i = 0; i < NPI; ++i) dr[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][16 * m + row16][8 * g4]);
-#pragma unroll
-                    for (int i = 0; i < NPE; ++i) zr[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][16 * m + row16][8 * g4]);
-                    P1[m] = mm(dr, e, P1[m]);
-                    P2[m] = mm(zr, e, P2[m]);
-                }
+                P1[m] = mv(r1, c1, P1[m]);
+                P2[m] = mv(r2, c2, P2[m]);
             }
+            P1own = mv(dO, e, P1own);
+            P2own = mv(z, e, P2own);
             // dV = beta z, dbeta = z . e
             f32x4 zs[2] = {}, es[2] = {};
+            if constexpr (UNITS) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
+                for (int x = 0; x < 4; ++x) dbeta = __builtin_amdgcn_fdot2(z[0].p16[x], e[0].p16[x], dbeta, false);
 #pragma unroll
-                for (int i = NPE - 1; i >= 0; --i) {
-                    zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
-                    es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
-                }
+                for (int x = 0; x < 8; ++x) zs[x >> 2][x & 3] = (float)z[0].h16[x] * uZ;
+            } else
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+#pragma unroll
+                    for (int i = NPI - 1; i >= 0; --i) {
+                        zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
+                        es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
+                    }
             const int c = 32 * ks + 8 * g4;
             IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + (own_in ? own : 0)) * p.Hv + h) * p.dv + c;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 f32x4 v;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) { dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
+                for (int r = 0; r < 4; ++r) { if (!UNITS) dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
                 if (own_in) {
                     if (p.o_vec && c + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
                     else
@@ -495,25 +566,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                         for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
                 }
             }
-        }
+        };
+#pragma unroll 1
+        for (int ks = 0; ks < ksv - 1; ++ks) columns(ks, std::false_type{});
+        columns(ksv - 1, std::true_type{});
+        if constexpr (UNITS) { dbeta = dbeta * uZ * uE; sdot = sdot * uA * uB; }
         const double Gown = lds.G[own];
         const float gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
 
-        // K and Q into LDS: 16 quads of steps by DK / 4 quads of columns, turned, and as rows
-        constexpr int IQ = DK / 64;
-        uint2 kw4[NPI][IQ * 4], qw4[NPI][IQ * 4];
-#pragma unroll
-        for (int pl = 0; pl < NPI; ++pl) {
-            const Buffer kb = buffer_of(kp + pl * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
-#pragma unroll
-            for (int x = 0; x < IQ; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4);
-                    kw4[pl][4 * x + e] = buffer_load8(kb, (4 * tq + e) * krow + 8 * dc);
-                    qw4[pl][4 * x + e] = buffer_load8(qb, (4 * tq + e) * qrow + 8 * dc);
-                }
-        }
+        // K and Q into LDS, turned, and as rows
         lds_barrier();
 #pragma unroll
         for (int pl = 0; pl < NPI; ++pl)
@@ -563,13 +624,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
         // the states' part of dQ and dK
         float dG = 0.0f, ends = 0.0f;
         {
-            const float cq = p.scale * gam, ck = -gam * bown, cw = en * bown;
+            const float cq = p.scale * gam, ck = -gam * bown, cw = en * bown, vq = uA * uD, vk = uA * uZ, vw = uB * uE;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const f32x4 kv = four_of(0, m), qv = four_of(1, m);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float a = cq * qs[m][r], c = ck * kr[m][r], w = cw * kw[m][r];
+                    const float a = cq * (vq * qs[m][r]), c = ck * (vk * kr[m][r]), w = cw * (vw * kw[m][r]);
                     dq[m][r] += a; dk[m][r] += c + w;
                     dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
                     ends = __builtin_fmaf(kv[r], w, ends);
@@ -580,6 +641,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
         // F, H in both orientations, M's row and column sums
         f32x4 HH[4], Ft[4], F[4];
         {
+            const float vf = uD * uE, vh = uZ * uE;
             Frag kf[KS][NPI], qf[KS][NPI];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) { row_of(0, own, ks, kf[ks]); row_of(1, own, ks, qf[ks]); }
@@ -600,20 +662,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
                     const int o = 16 * m + 4 * g4 + r;
                     const double Go = lds.G[o];
                     const float bo = lds.beta[o];
-                    float ft = 0.0f, f = 0.0f, hh = 0.0f;
                     const float D = __expf((float)(o <= own ? Gown - Go : Go - Gown));
-                    if (o <= own) {                              // this step reads what step o wrote
-                        ft = p.scale * D * bo * P1t[m][r];
-                        if (o < own) hh = -D * bown * bo * P2t[m][r];
-                        dG += ft * QKt[r] + hh * KK[r];
-                    }
-                    if (o >= own) {                              // step o reads what this step wrote
-                        f = p.scale * D * bown * P1[m][r];
-                        float hx = 0.0f;
-                        if (o > own) hx = -D * bown * bo * P2[m][r];
-                        dG -= f * QK[r] + hx * KK[r];
-                        hh += hx;
-                    }
+                    const float ds = p.scale * D * vf, db = -D * bown * bo * vh;
+                    const float ft = o <= own ? ds * bo * P1[m][r] : 0.0f;          // this step reads what step o wrote
+                    const float f = o >= own ? ds * bown * (m == wave ? P1own[r] : P1[m][r]) : 0.0f;        // step o reads what this step wrote
+                    const float hl = o < own ? db * P2[m][r] : 0.0f, hx = o > own ? db * (m == wave ? P2own[r] : P2[m][r]) : 0.0f;
+                    const float hh = hl + hx;
+                    dG += ft * QKt[r] + hl * KK[r];
+                    dG -= f * QK[r] + hx * KK[r];
                     Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
                 }
             }

@@ -14,6 +14,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Operand of a 16 x 16 x 32 matrix product: lane l holds row (or column) l % 16 and eight of the 32 terms of the sum.  Which eight is free as long
 // as both operands agree: operands from memory take them in order (8 (l / 16) ..), operands made from a result take 4 (l / 16) .. + 3 of either
@@ -23,10 +25,15 @@ union Frag {
     uint2 h[2];
     uint4 v;
     bf16x8 b;
+    f16x8 h16;
+    f16x2 p16[4];
 };
 
 __device__ __forceinline__ f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(const Frag &a, const Frag &b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h16, b.h16, c, 0, 0, 0);
 }
 // product of operands in planes: terms below the smallest plane's weight are left out
 template <int NA, int NB> __device__ __forceinline__ f32x4 mm(const Frag (&a)[NA], const Frag (&b)[NB], f32x4 c) {
@@ -70,6 +77,91 @@ template <int NP> __device__ __forceinline__ void split2(float a, float b, uint3
         if (i < NP - 1) { a -= hi_part(a); b -= hi_part(b); }
     }
 }
+// What the backward pass is left of bfloat16 operands' states, errors and gradients: 16-bit floating point with a common power of two a block, 11 bits of
+// mantissa (what the results are rounded to has 8) for numbers down to 2^-29 of the block's largest, which the power brings to 2^14 .. 2^15.
+// The power's inverse, from the largest magnitude (an infinity leaves its block only infinities and zeros):
+__device__ __forceinline__ float block_unit(float largest) {
+    const uint32_t e = __float_as_uint(largest) >> 23;
+    return __uint_as_float(((e > 15 ? e : 15) - 14) << 23);
+}
+__device__ __forceinline__ float inverse_unit(float unit) { return __uint_as_float((254u << 23) - __float_as_uint(unit)); }
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+}
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {          // magnitudes of bfloat16 pairs
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7fff7fffu), __builtin_bit_cast(u16x2, b & 0x7fff7fffu)));
+}
+template <int N> __device__ __forceinline__ float largest_of(const f32x4 (&x)[N]) {
+    float m[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m[i & 1] = fmaxf(m[i & 1], fabsf(x[i][r]));
+    return fmaxf(m[0], m[1]);
+}
+template <int CTRL, int ROW_MASK = 0xF> __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xF, false);
+    return x > y ? x : y;
+}
+__device__ __forceinline__ float wave_max(float m) {          // of numbers that are not negative: they compare as their bits do
+    uint32_t x = __float_as_uint(m);
+    x = dpp_max<0x111>(x);                                    // row_shr 1, 2, 4, 8
+    x = dpp_max<0x112>(x);
+    x = dpp_max<0x114>(x);
+    x = dpp_max<0x118>(x);
+    x = dpp_max<0x142, 0xA>(x);                               // lane 15 of a row to the next row, lane 31 to the upper half
+    x = dpp_max<0x143, 0xC>(x);
+    return __uint_as_float(__builtin_amdgcn_readlane(x, 63));
+}
+// a state's 16 columns as they are saved, a column to a row of DK: planes, or 16 bits with their unit
+template <int NPS, int DK> __device__ __forceinline__ void save_state(const f32x4 (&S)[DK / 16], uint16_t *to, int64_t plane, float *unit) {
+    float inv = 0.0f;
+    if constexpr (NPS == 1) {
+        const float u = block_unit(wave_max(largest_of(S)));
+        inv = inverse_unit(u);
+        if ((threadIdx.x & 63) == 0) *unit = u;
+    }
+#pragma unroll
+    for (int m = 0; m < DK / 16; ++m) {
+        uint32_t lo[NPS], hi[NPS];
+        if constexpr (NPS == 1) {
+            lo[0] = pack_f16(S[m][0] * inv, S[m][1] * inv);
+            hi[0] = pack_f16(S[m][2] * inv, S[m][3] * inv);
+        } else {
+            split2<NPS>(S[m][0], S[m][1], lo);
+            split2<NPS>(S[m][2], S[m][3], hi);
+        }
+#pragma unroll
+        for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + i * plane + 16 * m) = make_uint2(lo[i], hi[i]);
+    }
+}
+// 16 columns of 32 steps of E or Z, a step to a lane (`row`: this lane's of the first 16 steps, 16 of them `rows16` apart; n: steps of the chunk)
+template <int NPE> __device__ __forceinline__ void save_rows(const f32x4 (&X)[2], uint16_t *row, int64_t rows16, int64_t plane, int n, float *unit) {
+    const int row16 = threadIdx.x & 15;
+    float inv = 0.0f;
+    if constexpr (NPE == 1) {
+        const float u = block_unit(wave_max(largest_of(X)));
+        inv = inverse_unit(u);
+        if ((threadIdx.x & 63) == 0) *unit = u;
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        uint32_t lo[NPE], hi[NPE];
+        if constexpr (NPE == 1) {
+            lo[0] = pack_f16(X[m][0] * inv, X[m][1] * inv);
+            hi[0] = pack_f16(X[m][2] * inv, X[m][3] * inv);
+        } else {
+            split2<NPE>(X[m][0], X[m][1], lo);
+            split2<NPE>(X[m][2], X[m][3], hi);
+        }
+        if (16 * m + row16 < n)
+#pragma unroll
+            for (int i = 0; i < NPE; ++i) *reinterpret_cast<uint2 *>(row + i * plane + m * rows16) = make_uint2(lo[i], hi[i]);
+    }
+}
+
 // two result tiles as the operand of the next product
 template <int NP> __device__ __forceinline__ void split_tiles(const f32x4 &lo, const f32x4 &hi, Frag (&f)[NP]) {
 #pragma unroll

@@ -269,7 +269,7 @@ template <int NPI, int NP, int DK, int NBUF> struct ScanLds {
 // of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
 template <class IO, int NPI, int NP, int DK, int NW, bool SAVE, bool AGG>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
-    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI == 3 ? 3 : 1, NPE = NPI == 3 ? 3 : 2;
+    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr int NPO = NPI == 3 ? 3 : 2;                 // planes of what only enters o
     extern __shared__ __align__(16) char lds_raw[];
@@ -392,15 +392,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         if (SAVE && !(ch & 1) && c0 < p.dvp) {
-            uint16_t *to = p.states + (sh * NPS * p.dvp + n0) * DK + 4 * g4;             // turned: a column to a row
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                uint32_t lo[NPS], hi[NPS];
-                split2<NPS>(S[m][0], S[m][1], lo);
-                split2<NPS>(S[m][2], S[m][3], hi);
-#pragma unroll
-                for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + (int64_t)i * p.dvp * DK + 16 * m) = make_uint2(lo[i], hi[i]);
-            }
+            const int G = p.dvp / 16;
+            save_state<NPS, DK>(S, p.states + (sh * NPS * p.dvp + n0) * DK + 4 * g4, (int64_t)p.dvp * DK, p.units + sh * 3 * G + c0 / 16);
         }
 
         // K S0 and (transposed: a step to a lane) Q S0
@@ -500,18 +493,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 S[m] = mm(ktf[0], df, S[m]);
             }
         if (SAVE && c0 < p.dvp) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const int t = 16 * m + row16;
-                uint32_t lo[NPE], hi[NPE];
-                split2<NPE>(Et[m][0], Et[m][1], lo);
-                split2<NPE>(Et[m][2], Et[m][3], hi);
-                if (t < n)
-#pragma unroll
-                    for (int i = 0; i < NPE; ++i)
-                        *reinterpret_cast<uint2 *>(p.err + (((int64_t)i * (p.cu ? 1 : p.B) * p.L + sq.row + t0 + t) * p.Hv + h) * p.dvp + c0 + 4 * g4) =
-                            make_uint2(lo[i], hi[i]);
-            }
+            const int G = p.dvp / 16;
+            save_rows<NPS>(Et, p.err + ((sq.row + t0 + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n, p.units + (sh * 3 + 1 + (ch & 1)) * G + c0 / 16);
         }
         if constexpr (!AGG) {                               // O
 #pragma unroll
