@@ -36,12 +36,12 @@ struct DeltaParams {
     uint16_t *mats;                      // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands, and the gates (chunk_words)
     uint16_t *mats_adj;                  // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
     uint16_t *states, *err;              // saved for the backward pass; null: not wanted
-    float *units;                        // and with bfloat16 I/O the powers of two of their blocks of 16 columns: S0 (G), E (2 chunks by G) of a slot's head
+    float *units;                        // and with bfloat16 I/O the powers of two of their blocks of 16 columns: S0 (2 halves of its rows by G), E (4 times 16 steps by G) of a slot's head
     // backward
     const float *ds_last;
     float *ds0;
     uint16_t *dstates, *z;
-    float *dunits;                       // likewise S1's (G), Z's (2 G)
+    float *dunits;                       // likewise S1's (2 G), Z's (4 G)
     void *dq, *dkk, *dvv, *dg, *dbeta;
     int np, np_adjoint;                  // planes of the state chain, of its adjoint
     // segments of the time axis that are walked side by side (one sequence of a batch entry alone does not fill the chip); 1: none
@@ -78,7 +78,6 @@ hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s);
 hipError_t launch_delta_join(const DeltaParams &p, bool adjoint, hipStream_t s);
-constexpr int delta_waves(int dvp) { return dvp > 32 ? 4 : 2; }          // wavefronts of 16 columns a workgroup
 hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s);
 
 struct DeltaStepParams {

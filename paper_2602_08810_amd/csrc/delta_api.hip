@@ -66,7 +66,7 @@ inline int a_planes(const Shape &s) { return s.bf16 ? 2 : 3; }
 void lay_saved(const Shape &s, bool s0, Layout &l, DeltaParams &p) {
     p.states = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
     p.err = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
-    if (s.bf16) p.units = l.take<float>(s.nslots * s.Hv * 3 * (s.dvp / 16));
+    if (s.bf16) p.units = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
     p.mats_adj = l.take<uint16_t>(mats(s) * chunk_words(adjoint_planes(s, s0), a_planes(s)));
 }
 
@@ -111,8 +111,7 @@ template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
 // in two segments 57 + 13 + 81.
 void plan_segments(const Shape &s, bool packed, Layout &l, DeltaParams &p) {
     p.nseg = 1; p.seg_chunks = 0; p.entry = nullptr; p.trans = nullptr;
-    const int waves = delta_waves(s.dvp);
-    const int64_t heads = (int64_t)s.B * s.Hv, wgs = heads * ((s.dvp / 16 + waves - 1) / waves), slots = s.slots_each;
+    const int64_t heads = (int64_t)s.B * s.Hv, wgs = heads * ((s.dvp + 63) / 64), slots = s.slots_each;
     if (packed) return;
     int64_t n = 256 / wgs;                            // a workgroup a compute unit
     if (n > slots / 4) n = slots / 4;                 // of 256 steps at least
@@ -158,7 +157,7 @@ DeltaBwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, c
     lay_saved(s, a->s0 != nullptr, sv, f.p);
     f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
     f.p.z = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
-    if (s.bf16) f.p.dunits = l.take<float>(s.nslots * s.Hv * 3 * (s.dvp / 16));
+    if (s.bf16) f.p.dunits = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
     plan_segments(s, one, l, f.p);
     f.bytes = l.at; f.saved = sv.at;
     return f;

@@ -17,30 +17,33 @@ namespace lrnnx {
 
 // ---------------------------------------------------------------- the walk backwards
 // As in the forward walk a wavefront owns 16 columns of dS, and everything it computes of them stays in its registers.
-template <int NPI, int NP, int DK, int NBUF> struct AdjLds {
+template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
     static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
         uint16_t k[NPI][32][DK + 8], kt[NPI][DK][40], qt[NPI][DK][40];
         uint16_t t[2][NP][512], a[2][NPA][512];
         float scal[96];
     } buf[NBUF];
+    f32x4 halves[DS == 2 ? 8 : 1][64];
 };
 
 // DEEP: loads two chunks ahead, for launches of at most a workgroup a compute unit, where registers are there for it and nothing else hides memory
 // (walk of 4 x 4096 steps, 16 heads of 128 x 128: 385 -> 346 us; the forward walk gains nothing by it).
-template <int NPI, int NP, int DK, int NW, bool AGG, bool DEEP>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 1 : 2, DEEP ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
-    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI;
+template <int NPI, int NP, int DK, int DS, bool AGG, bool DEEP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS == 1 || NPI == 3) ? 1 : 2, DEEP && (DS == 1 || NPI == 3) ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
+    constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
+    constexpr int NPA = NPI == 3 ? 3 : 2, NPS = NPI;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     extern __shared__ __align__(16) char lds_raw[];
-    using Lds = AdjLds<NPI, NP, DK, NBUF>;
+    using Lds = AdjLds<NPI, NP, DK, NBUF, DS>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     DeltaUnit un;
     if (!delta_unit(p, AGG ? p.nseg - 1 : p.nseg, un)) return;
     const int h = un.h, hk = h / (p.Hv / p.Hk), b = un.b, seg = AGG ? un.seg + 1 : un.seg;
     const DeltaSeq sq = delta_seq(p, b);
-    const int c0 = (un.group * NW + wave) * 16, n0 = c0 + row16;
+    const int dh = DS == 2 ? wave & 1 : 0, d0 = dh * (DK / 2), first = DS == 2 ? dh : 0;
+    const int c0 = (un.group * CW + wave / DS) * 16, n0 = c0 + row16;
     const bool col_in = n0 < p.dv, mine = c0 < p.dvp;
     const int64_t nchunk = (sq.len + 31) / 32, ch0 = p.nseg > 1 ? (int64_t)seg * p.seg_chunks : 0;
     const int64_t ch1 = p.nseg > 1 && nchunk > ch0 + p.seg_chunks ? ch0 + p.seg_chunks : nchunk;
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * m + 4 * g4 + r;
+            const int d = d0 + 16 * m + 4 * g4 + r;
             if (AGG) S[m][r] = d == n0 - p.dvp ? 1.0f : 0.0f;
             else if (ch1 < nchunk) S[m][r] = mine ? p.entry[((head * p.nseg + seg) * DK + d) * p.dvp + n0] : 0.0f;
             else S[m][r] = p.ds_last && col_in && d < p.dk ? p.ds_last[(head * p.dk + d) * p.dv + n0] : 0.0f;
@@ -143,17 +146,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         const int G = p.dvp / 16;
-        float *units = p.dunits + sh * 3 * G + c0 / 16;
+        float *units = p.dunits + sh * 6 * G + c0 / 16;
         if (!AGG && ((ch & 1) || ch == nchunk - 1) && mine)
-            save_state<NPS, DK>(S, p.dstates + (sh * NPS * p.dvp + n0) * DK + 4 * g4, (int64_t)p.dvp * DK, units);
+            save_state<NPS, DK>(S, p.dstates + (sh * NPS * p.dvp + n0) * DK + d0 + 4 * g4, (int64_t)p.dvp * DK, units + dh * G, G);
         constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
-        Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NPA];
+        Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NPA], tt[OT][NP];
         f32x4 gam[2], be[2], en[2];
         if constexpr (EARLY)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) kf[ks][m][0].v = *reinterpret_cast<const uint4 *>(&B.k[0][16 * m + row16][32 * ks + 8 * g4]);
+                for (int m = 0; m < 2; ++m) kf[ks][m][0].v = *reinterpret_cast<const uint4 *>(&B.k[0][16 * m + row16][d0 + 32 * ks + 8 * g4]);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int i = 0; i < NPI; ++i) kf[0][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
+                    for (int i = 0; i < NPI; ++i) kf[0][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][d0 + 32 * ks + 8 * g4]);
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
@@ -185,11 +188,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
                     for (int m = 0; m < 2; ++m)
                         if (i + j < NP) X[m] = mfma(kf[at][m][j], s[i], X[m]);
         }
+        if constexpr (DS == 2) {
+            lds.halves[2 * wave][lane] = X[0];
+            lds.halves[2 * wave + 1][lane] = X[1];
+            lds_barrier();
+            X[0] += lds.halves[2 * (wave ^ 1)][lane];
+            X[1] += lds.halves[2 * (wave ^ 1) + 1][lane];
+        }
+        if constexpr (!AGG)
+#pragma unroll
+            for (int m = 0; m < OT; ++m)
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    if constexpr (DS == 2) tt[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[dh][i][lane * 8]);
+                    else tt[m][i] = tf[m][i];
+                }
         if constexpr (EARLY)
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                ktf[m][0].v = *reinterpret_cast<const uint4 *>(&B.kt[0][16 * m + row16][turned(16 * m, 8 * g4)]);
-                qtf[m][0].v = *reinterpret_cast<const uint4 *>(&B.qt[0][16 * m + row16][turned(16 * m, 8 * g4)]);
+                ktf[m][0].v = *reinterpret_cast<const uint4 *>(&B.kt[0][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
+                qtf[m][0].v = *reinterpret_cast<const uint4 *>(&B.qt[0][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
             }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -207,7 +225,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
         Frag uf[NP], wf[NP];
         split_tiles<NP>(X[0], X[1], uf, neg);
         split_tiles<NP>(W[0], W[1], wf, neg);
-        f32x4 Z[2] = {}, Zt[2] = {};
+        f32x4 Z[2] = {}, Zt[OT] = {};
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
@@ -216,7 +234,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         Z[m] = mfma(tf[m][i], uf[j], Z[m]);
-                        if (!AGG) Zt[m] = mfma(uf[j], tf[m][i], Zt[m]);                      // a step to a lane, for wide stores
+                        if (!AGG && m < OT) Zt[m] = mfma(uf[j], tt[m][i], Zt[m]);                      // a step to a lane, for wide stores
                     }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -227,7 +245,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) qtf[0][i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                for (int i = 0; i < NPI; ++i) qtf[0][i].v = *reinterpret_cast<const uint4 *>(&B.qt[i][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
                 S[m] = mm(qtf[0], wf, S[m]);
             }
         f32x4 R[2];                                         // -exp(G) beta z
@@ -242,12 +260,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
                 S[m] = mm(ktf[0], rf, S[m]);
             }
         if (!AGG && mine)
-            save_rows<NPS>(Zt, p.z + ((sq.row + t0 + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
-                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n, units + (1 + (ch & 1)) * G);
+            save_rows<NPS>(Zt, p.z + ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n - 16 * first, units + (2 + 2 * (ch & 1) + first) * G, G);
         if (NBUF == 1) lds_barrier();
         put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0], next);
         lds_barrier();
@@ -281,7 +299,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(DEEP ? 
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 16 * m + 4 * g4 + r;
+                const int d = d0 + 16 * m + 4 * g4 + r;
                 if (d < p.dk) p.ds0[(head * p.dk + d) * p.dv + n0] = S[m][r];
             }
 }
@@ -363,12 +381,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
         float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
         const int G = p.dvp / 16;
         if constexpr (UNITS) {
-            const float *fu = p.units + (slot * p.Hv + h) * 3 * G, *bu = p.dunits + (slot * p.Hv + h) * 3 * G;
-            const int in = (n > 32 ? 2 : 1) * G;
-            buffer_load(buffer_of(fu, 4 * G), 4 * lane, rA);
-            buffer_load(buffer_of(fu + G, 4 * in), 4 * lane, rE);
-            buffer_load(buffer_of(bu, 4 * G), 4 * lane, rB);
-            buffer_load(buffer_of(bu + G, 4 * in), 4 * lane, rZ);
+            const float *fu = p.units + (slot * p.Hv + h) * 6 * G, *bu = p.dunits + (slot * p.Hv + h) * 6 * G;
+            const int in = (n > 32 ? 4 : 2) * G;
+            buffer_load(buffer_of(fu, 8 * G), 4 * lane, rA);
+            buffer_load(buffer_of(fu + 2 * G, 4 * in), 4 * lane, rE);
+            buffer_load(buffer_of(bu, 8 * G), 4 * lane, rB);
+            buffer_load(buffer_of(bu + 2 * G, 4 * in), 4 * lane, rZ);
         }
         fetch(0);
         if constexpr (UNITS) {
@@ -437,7 +455,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
             if constexpr (UNITS) uD = block_unit(fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3])));
             uint32_t pE = 0, pZ = 0, pA = 0, pB = 0;
             if constexpr (UNITS) {                          // brought to the slot's units
-                const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 5) * G, gs = 2 * ks + (sq4 >> 2 & 1);
+                const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 4) * G, gs = 2 * ks + (sq4 >> 2 & 1) + (8 * sd4 >= DK ? G : 0);
                 const float fE = __shfl(rE, ge, 64), fZ = __shfl(rZ, ge, 64), fA = __shfl(rA, gs, 64), fB = __shfl(rB, gs, 64);
                 pE = pack_f16(fE, fE); pZ = pack_f16(fZ, fZ); pA = pack_f16(fA, fA); pB = pack_f16(fB, fB);
             }
@@ -747,27 +765,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
 }
 
 // ---------------------------------------------------------------- launches
-template <int NPI, int NP, int DK, int NW, bool AGG> static hipError_t launch_adjoint_one(DeltaParams p, hipStream_t s) {
+template <int NPI, int NP, int DK, int DS, bool AGG> static hipError_t launch_adjoint_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
-    constexpr size_t bytes = sizeof(AdjLds<NPI, NP, DK, NBUF>);
+    constexpr size_t bytes = sizeof(AdjLds<NPI, NP, DK, NBUF, DS>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + NW - 1) / NW;
+    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + 4 / DS - 1) / (4 / DS);
     const unsigned blocks = delta_blocks(p, AGG ? p.nseg - 1 : p.nseg);
-    auto k = blocks <= 256 ? k_delta_adjoint<NPI, NP, DK, NW, AGG, true> : k_delta_adjoint<NPI, NP, DK, NW, AGG, false>;
+    auto k = blocks <= 256 ? k_delta_adjoint<NPI, NP, DK, DS, AGG, true> : k_delta_adjoint<NPI, NP, DK, DS, AGG, false>;
     if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3(blocks), dim3(NW * 64), bytes, s, p);
+    hipLaunchKernelGGL(k, dim3(blocks), dim3(256), bytes, s, p);
     return hipGetLastError();
 }
-template <int NPI, int NP, int DK, int NW> static hipError_t launch_adjoint_nw(const DeltaParams &p, hipStream_t s) {
+template <int NPI, int NP, int DK> static hipError_t launch_adjoint_dk(const DeltaParams &p, hipStream_t s) {
     if (p.nseg > 1) {
-        if (const hipError_t e = launch_adjoint_one<NPI, NP, DK, NW, true>(p, s)) return e;
+        if (const hipError_t e = launch_adjoint_one<NPI, NP, DK, 1, true>(p, s)) return e;
         if (const hipError_t e = launch_delta_join(p, true, s)) return e;
     }
-    return launch_adjoint_one<NPI, NP, DK, NW, false>(p, s);
-}
-template <int NPI, int NP, int DK> static hipError_t launch_adjoint_dk(const DeltaParams &p, hipStream_t s) {
-    return delta_waves(p.dvp) == 4 ? launch_adjoint_nw<NPI, NP, DK, 4>(p, s) : launch_adjoint_nw<NPI, NP, DK, 2>(p, s);
+    return delta_rows_split(p) ? launch_adjoint_one<NPI, NP, DK, 2, false>(p, s) : launch_adjoint_one<NPI, NP, DK, 1, false>(p, s);
 }
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_adjoint_dk<3, 3, 128>(p, s) : launch_adjoint_dk<3, 3, 64>(p, s);

@@ -115,16 +115,19 @@ __device__ __forceinline__ float wave_max(float m) {          // of numbers that
     x = dpp_max<0x143, 0xC>(x);
     return __uint_as_float(__builtin_amdgcn_readlane(x, 63));
 }
-// a state's 16 columns as they are saved, a column to a row of DK: planes, or 16 bits with their unit
-template <int NPS, int DK> __device__ __forceinline__ void save_state(const f32x4 (&S)[DK / 16], uint16_t *to, int64_t plane, float *unit) {
+// MT tiles of a state's 16 columns as they are saved, a column to a row of DK: planes, or 16 bits with their unit (a unit each half of the rows)
+template <int NPS, int DK, int MT> __device__ __forceinline__ void save_state(const f32x4 (&S)[MT], uint16_t *to, int64_t plane, float *unit, int G) {
     float inv = 0.0f;
     if constexpr (NPS == 1) {
         const float u = block_unit(wave_max(largest_of(S)));
         inv = inverse_unit(u);
-        if ((threadIdx.x & 63) == 0) *unit = u;
+        if ((threadIdx.x & 63) == 0) {
+            *unit = u;
+            if (MT == DK / 16) unit[G] = u;
+        }
     }
 #pragma unroll
-    for (int m = 0; m < DK / 16; ++m) {
+    for (int m = 0; m < MT; ++m) {
         uint32_t lo[NPS], hi[NPS];
         if constexpr (NPS == 1) {
             lo[0] = pack_f16(S[m][0] * inv, S[m][1] * inv);
@@ -137,17 +140,20 @@ template <int NPS, int DK> __device__ __forceinline__ void save_state(const f32x
         for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + i * plane + 16 * m) = make_uint2(lo[i], hi[i]);
     }
 }
-// 16 columns of 32 steps of E or Z, a step to a lane (`row`: this lane's of the first 16 steps, 16 of them `rows16` apart; n: steps of the chunk)
-template <int NPE> __device__ __forceinline__ void save_rows(const f32x4 (&X)[2], uint16_t *row, int64_t rows16, int64_t plane, int n, float *unit) {
+// 16 columns of N tiles of 16 steps of E or Z, a step to a lane (`row`: this lane's of the first, the next ones' rows16 elements on; n: steps there
+// are from the first tile on; a unit a tile, G apart)
+template <int NPE, int N> __device__ __forceinline__ void save_rows(const f32x4 (&X)[N], uint16_t *row, int64_t rows16, int64_t plane, int n, float *unit, int G) {
     const int row16 = threadIdx.x & 15;
     float inv = 0.0f;
     if constexpr (NPE == 1) {
         const float u = block_unit(wave_max(largest_of(X)));
         inv = inverse_unit(u);
-        if ((threadIdx.x & 63) == 0) *unit = u;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int m = 0; m < N; ++m) unit[m * G] = u;
     }
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
+    for (int m = 0; m < N; ++m) {
         uint32_t lo[NPE], hi[NPE];
         if constexpr (NPE == 1) {
             lo[0] = pack_f16(X[m][0] * inv, X[m][1] * inv);
@@ -279,6 +285,8 @@ __device__ __forceinline__ bool delta_unit(const DeltaParams &p, unsigned segs, 
 }
 
 inline unsigned delta_blocks(const DeltaParams &p, int segs) { return (unsigned)(((int64_t)p.B * p.Hv * segs + 7) / 8 * 8 * p.groups); }
+// Two wavefronts to 16 columns: where one each would leave half of the compute units without a workgroup, or half of a workgroup without columns.
+inline bool delta_rows_split(const DeltaParams &p) { return p.dvp <= 32 || (int64_t)p.B * p.Hv * p.nseg * ((p.dvp + 63) / 64) <= 128; }
 // A wavefront's 16 columns (this lane's: j) of a segment's transition, as planes [dk][dk].
 template <int NP, int DK> __device__ __forceinline__ void store_trans(const f32x4 (&S)[DK / 16], uint16_t *to, int j, int g4) {
 #pragma unroll

@@ -255,32 +255,37 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
 // holds a column of four rows in each lane, which is what the second operand of the next instruction wants of its terms, so K S0 -> E -> U ->
 // K^T U runs from registers to registers: no exchange between lanes or wavefronts on the path that the next chunk waits for.  The wavefronts of
 // a workgroup share what is the same for all columns (K, Q, K^T, the chunk's matrices) in LDS.
-template <int NPI, int NP, int DK, int NBUF> struct ScanLds {
+template <int NPI, int NP, int DK, int NBUF, int DS> struct ScanLds {
     static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
         uint16_t k[NPI][32][DK + 8], q[NPI][32][DK + 8], kt[NPI][DK][40];
         uint16_t t[2][NP][512], a[2][NPA][512];
         float scal[96];
     } buf[NBUF];
+    f32x4 halves[DS == 2 ? 12 : 1][64];
 };
 
 //
+// DS = 2: two wavefronts share 16 columns, each with half of the rows of S: half of the products and registers each, for one exchange through LDS (the
+// halves of K S0 and Q S0 are added) and twice the workgroups, which pays where heads are few.
 // AGG: what a segment makes of the state that enters it, S -> M S + N, without outputs: N is the walk from a state of zero, and the columns of M, behind those
 // of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
-template <class IO, int NPI, int NP, int DK, int NW, bool SAVE, bool AGG>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
-    constexpr int KS = DK / 32, MT = DK / 16, NT = NW * 64, NPA = NPI == 3 ? 3 : 2, NPS = NPI;
+template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
+    constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
+    constexpr int NPA = NPI == 3 ? 3 : 2, NPS = NPI;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr int NPO = NPI == 3 ? 3 : 2;                 // planes of what only enters o
     extern __shared__ __align__(16) char lds_raw[];
-    using Lds = ScanLds<NPI, NP, DK, NBUF>;
+    using Lds = ScanLds<NPI, NP, DK, NBUF, DS>;
     Lds &lds = *reinterpret_cast<Lds *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     DeltaUnit un;
     if (!delta_unit(p, AGG ? p.nseg - 1 : p.nseg, un)) return;
     const int h = un.h, hk = h / (p.Hv / p.Hk), b = un.b;
     const DeltaSeq sq = delta_seq(p, b);
-    const int c0 = (un.group * NW + wave) * 16, n0 = c0 + row16;       // this wavefront's columns, this lane's
+    const int dh = DS == 2 ? wave & 1 : 0, d0 = dh * (DK / 2);         // this wavefront's half of the rows of S
+    const int c0 = (un.group * CW + wave / DS) * 16, n0 = c0 + row16;  // this wavefront's columns, this lane's
     const bool col_in = n0 < p.dv;
     const int64_t nchunk = (sq.len + 31) / 32, ch0 = p.nseg > 1 ? (int64_t)un.seg * p.seg_chunks : 0;
     const int64_t ch1 = p.nseg > 1 && nchunk > ch0 + p.seg_chunks ? ch0 + p.seg_chunks : nchunk;
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * m + 4 * g4 + r;
+            const int d = d0 + 16 * m + 4 * g4 + r;
             if (AGG) S[m][r] = d == n0 - p.dvp ? 1.0f : 0.0f;
             else if (un.seg > 0) S[m][r] = c0 < p.dvp ? p.entry[((head * p.nseg + un.seg) * DK + d) * p.dvp + n0] : 0.0f;
             else S[m][r] = p.s0 && col_in && d < p.dk ? p.s0[(head * p.dk + d) * p.dv + n0] : 0.0f;
@@ -382,8 +387,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
         const int64_t t0 = ch * 32;
         const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
+        constexpr bool ONE = SAVE && DS == 1;
         f32x4 V[2];                                         // (with SAVE there are no registers for a second set of rows under way)
-        if constexpr (SAVE)
+        if constexpr (ONE)
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -393,20 +399,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         if (SAVE && !(ch & 1) && c0 < p.dvp) {
             const int G = p.dvp / 16;
-            save_state<NPS, DK>(S, p.states + (sh * NPS * p.dvp + n0) * DK + 4 * g4, (int64_t)p.dvp * DK, p.units + sh * 3 * G + c0 / 16);
+            save_state<NPS, DK>(S, p.states + (sh * NPS * p.dvp + n0) * DK + d0 + 4 * g4, (int64_t)p.dvp * DK, p.units + (sh * 6 + dh) * G + c0 / 16, G);
         }
 
         // K S0 and (transposed: a step to a lane) Q S0
         constexpr bool EARLY = NPI == 1 || DK == 64;        // operands read well before they are used
-        Frag kf[EARLY ? KS : 1][2][NPI], qf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], af[2][NPA];
+        Frag kf[EARLY ? KS : 1][2][NPI], qf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], af[OT][NPA], tt[OT][NP];
         f32x4 gam[2], be[2], en[2];
         auto read_kq = [&](int ks, int at) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int i = 0; i < NPI; ++i) {
-                    kf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][32 * ks + 8 * g4]);
-                    if constexpr (!AGG) qf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.q[i][16 * m + row16][32 * ks + 8 * g4]);
+                    kf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.k[i][16 * m + row16][d0 + 32 * ks + 8 * g4]);
+                    if constexpr (!AGG) qf[at][m][i].v = *reinterpret_cast<const uint4 *>(&B.q[i][16 * m + row16][d0 + 32 * ks + 8 * g4]);
                 }
         };
         if constexpr (EARLY)
@@ -436,27 +442,50 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                         if (!AGG && i < NPO && i + j < NPO) O[m] = mfma(s[i], qf[at][m][j], O[m]);
                     }
         }
+        f32x4 Oown[OT];                                     // and the tiles of the chunk's steps whose o (and E) it writes
+        const int first = DS == 2 ? dh : 0;
+        if constexpr (DS == 2) {
+            lds.halves[3 * wave][lane] = P[0];
+            lds.halves[3 * wave + 1][lane] = P[1];
+            if constexpr (!AGG) lds.halves[3 * wave + 2][lane] = dh ? O[0] : O[1];
+            lds_barrier();
+            P[0] += lds.halves[3 * (wave ^ 1)][lane];
+            P[1] += lds.halves[3 * (wave ^ 1) + 1][lane];
+            Oown[0] = dh ? O[1] : O[0];
+            if constexpr (!AGG) Oown[0] += lds.halves[3 * (wave ^ 1) + 2][lane];
+        } else
+#pragma unroll
+            for (int m = 0; m < OT; ++m) Oown[m] = O[m];
         if constexpr (EARLY) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) ktf[m][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                for (int i = 0; i < NPI; ++i) ktf[m][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             be[m] = *reinterpret_cast<const f32x4 *>(&B.scal[64 + 16 * m + 4 * g4]);
             en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
-            if constexpr (!AGG)
-#pragma unroll
-                for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
         }
+        if constexpr (!AGG)
+#pragma unroll
+            for (int m = 0; m < OT; ++m) {
+#pragma unroll
+                for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[first + m][i][lane * 8]);
+                if constexpr (SAVE)
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) {
+                        if constexpr (DS == 2) tt[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[dh][i][lane * 8]);
+                        else tt[m][i] = tf[m][i];
+                    }
+            }
         if constexpr (EARLY) reads_first();
         // E = (I + N beta)^-1 (V - exp(G) K S0)
-        f32x4 R[2], E[2] = {}, Et[2] = {};
+        f32x4 R[2], E[2] = {}, Et[OT] = {};
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[m][r], P[m][r], SAVE ? V[m][r] : load_io(&v.v[m][r]));
+            for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[m][r], P[m][r], ONE ? V[m][r] : load_io(&v.v[m][r]));
         Frag rf[NP];
         split_tiles<NP>(R[0], R[1], rf, neg);
 #pragma unroll
@@ -467,7 +496,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         E[m] = mfma(tf[m][i], rf[j], E[m]);
-                        if (SAVE) Et[m] = mfma(rf[j], tf[m][i], Et[m]);            // a step to a lane, for wide stores
+                        if (SAVE && m < OT) Et[m] = mfma(rf[j], tt[m][i], Et[m]);  // a step to a lane, for wide stores
                     }
         // U = beta E, and U decayed to the end of the chunk
         f32x4 U[2], D[2];
@@ -489,20 +518,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
 #pragma unroll
-                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                for (int i = 0; i < NPI; ++i) ktf[0][i].v = *reinterpret_cast<const uint4 *>(&B.kt[i][d0 + 16 * m + row16][turned(d0 + 16 * m, 8 * g4)]);
                 S[m] = mm(ktf[0], df, S[m]);
             }
         if (SAVE && c0 < p.dvp) {
             const int G = p.dvp / 16;
-            save_rows<NPS>(Et, p.err + ((sq.row + t0 + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
-                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n, p.units + (sh * 3 + 1 + (ch & 1)) * G + c0 / 16);
+            save_rows<NPS>(Et, p.err + ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n - 16 * first, p.units + (sh * 6 + 2 + 2 * (ch & 1) + first) * G + c0 / 16, G);
         }
         if constexpr (!AGG) {                               // O
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const float gs = p.scale * B.scal[16 * m + row16];
+            for (int m = 0; m < OT; ++m) {
+                const float gs = p.scale * B.scal[16 * (first + m) + row16];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) O[m][r] *= gs;
+                for (int r = 0; r < 4; ++r) Oown[m][r] *= gs;
             }
 #pragma unroll
             for (int i = 0; i < NPO; ++i)
@@ -510,18 +539,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 for (int j = 0; j < NPA; ++j)
                     if (i + j < (NPO > NPA ? NPO : NPA))
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) O[m] = mfma(uf[i], af[m][j], O[m]);
-        }
-        if constexpr (!AGG)
+                        for (int m = 0; m < OT; ++m) Oown[m] = mfma(uf[i], af[m][j], Oown[m]);
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int t = 16 * m + row16;
-            IO *to = op + (t0 + t) * p.o_sl;
-            if (wide) { if (t < n) store4(to, O[m]); }
-            else if (t < n)
+            for (int m = 0; m < OT; ++m) {
+                const int t = 16 * (first + m) + row16;
+                IO *to = op + (t0 + t) * p.o_sl;
+                if (wide) { if (t < n) store4(to, Oown[m]); }
+                else if (t < n)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (c0 + 4 * g4 + r < p.dv) store_io(to + r, O[m][r]);
+                    for (int r = 0; r < 4; ++r)
+                        if (c0 + 4 * g4 + r < p.dv) store_io(to + r, Oown[m][r]);
+            }
         }
         if (NBUF == 1) lds_barrier();
         put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0], st);
@@ -532,7 +560,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     fetch(ch0, st, va);
     put(lds.buf[0], st);                                    // (segments have an even number of chunks)
     lds_barrier();
-    if constexpr (SAVE)
+    if constexpr (SAVE && DS == 1)
         for (int64_t ch = ch0; ch < ch1; ++ch) step(ch, st, va, va);
     else
         for (int64_t ch = ch0; ch < ch1;) {                 // two chunks a round, so that no register is copied while it is loaded
@@ -553,7 +581,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 16 * m + 4 * g4 + r;
+                const int d = d0 + 16 * m + 4 * g4 + r;
                 if (d < p.dk) p.s_last[(head * p.dk + d) * p.dv + n0] = S[m][r];
             }
 }
@@ -654,26 +682,24 @@ hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s) {
     return p.np == 3 ? launch_prep<1, 3, 2>(p, s) : launch_prep<1, 2, 2>(p, s);
 }
 
-template <class IO, int NPI, int NP, int DK, int NW, bool SAVE, bool AGG> static hipError_t launch_scan_one(DeltaParams p, hipStream_t s) {
+template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG> static hipError_t launch_scan_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
-    constexpr size_t bytes = sizeof(ScanLds<NPI, NP, DK, NBUF>);
+    constexpr size_t bytes = sizeof(ScanLds<NPI, NP, DK, NBUF, DS>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + NW - 1) / NW;
-    auto k = k_delta_scan<IO, NPI, NP, DK, NW, SAVE, AGG>;
+    p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + 4 / DS - 1) / (4 / DS);
+    auto k = k_delta_scan<IO, NPI, NP, DK, DS, SAVE, AGG>;
     if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3(delta_blocks(p, AGG ? p.nseg - 1 : p.nseg)), dim3(NW * 64), bytes, s, p);
+    hipLaunchKernelGGL(k, dim3(delta_blocks(p, AGG ? p.nseg - 1 : p.nseg)), dim3(256), bytes, s, p);
     return hipGetLastError();
 }
-template <class IO, int NPI, int NP, int DK, int NW> static hipError_t launch_scan_nw(const DeltaParams &p, hipStream_t s) {
+template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
     if (p.nseg > 1) {
-        if (const hipError_t e = launch_scan_one<IO, NPI, NP, DK, NW, false, true>(p, s)) return e;
+        if (const hipError_t e = launch_scan_one<IO, NPI, NP, DK, 1, false, true>(p, s)) return e;
         if (const hipError_t e = launch_delta_join(p, false, s)) return e;
     }
-    return p.states ? launch_scan_one<IO, NPI, NP, DK, NW, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, NW, false, false>(p, s);
-}
-template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
-    return delta_waves(p.dvp) == 4 ? launch_scan_nw<IO, NPI, NP, DK, 4>(p, s) : launch_scan_nw<IO, NPI, NP, DK, 2>(p, s);
+    if (delta_rows_split(p)) return p.states ? launch_scan_one<IO, NPI, NP, DK, 2, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 2, false, false>(p, s);
+    return p.states ? launch_scan_one<IO, NPI, NP, DK, 1, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 1, false, false>(p, s);
 }
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_scan_dk<float, 3, 3, 128>(p, s) : launch_scan_dk<float, 3, 3, 64>(p, s);
