@@ -43,6 +43,7 @@ struct DeltaParams {
     uint16_t *dstates, *z;
     float *dunits;                       // likewise S1's (2 G), Z's (4 G)
     void *dq, *dkk, *dvv, *dg, *dbeta;
+    float *part;                         // with shared key heads: [2,rows,Hv,dkp] every value head's share of dq and of dk
     int np, np_adjoint;                  // planes of the state chain, of its adjoint
     // segments of the time axis that are walked side by side (one sequence of a batch entry alone does not fill the chip); 1: none
     int nseg, seg_chunks, groups;        // segments, chunks of one (even); groups of columns (workgroups) of a head

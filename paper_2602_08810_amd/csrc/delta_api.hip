@@ -157,6 +157,7 @@ DeltaBwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, c
     lay_saved(s, a->s0 != nullptr, sv, f.p);
     f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
     f.p.z = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
+    if (s.Hv > s.Hk) f.p.part = l.take<float>(2 * s.rows * s.Hv * s.dkp);
     if (s.bf16) f.p.dunits = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
     plan_segments(s, one, l, f.p);
     f.bytes = l.at; f.saved = sv.at;

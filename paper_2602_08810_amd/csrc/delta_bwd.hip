@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
 }
 
 // ---------------------------------------------------------------- the gradients of a slot
-// A workgroup takes the 64 steps of a slot and a key head, value head by value head; a wavefront owns 16 of the steps, one to a lane of each group
+// A workgroup takes the 64 steps of a slot and a value head (where value heads share a key head, k_delta_share adds up their parts of dQ and dK); a wavefront owns 16 of the steps, one to a lane of each group
 // of 16, and every product is arranged so that its results lie a step to a lane: gates are a number to a lane, F and H go from one product's
 // results into the next one's operand without leaving the lane, and rows of dQ and dK come out four neighbouring elements at a time.  Both
 // orientations of F and H are computed (one as products with the rows of others, one the other way round), which costs less than turning them.
@@ -321,16 +321,16 @@ template <int NPI, int DK> struct GradLds {
     float beta[64], dG[64], ends[4], dots[4], most[4];
 };
 
-template <class IO, int NPI, int DK, bool SHARED>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 && !SHARED ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
+template <class IO, int NPI, int DK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NPF = NPI == 3 ? 3 : 2;
     constexpr bool UNITS = NPI == 1;                        // E, Z, the states and here dO too: 16-bit floating point with a power of two a block
     constexpr bool ROWS = NPI == 1;                         // rows of K and Q in LDS too; else from memory
     extern __shared__ __align__(16) char lds_raw[];
     GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
-    const int64_t slot = blockIdx.x / (unsigned)p.Hk;
-    const int hk = (int)(blockIdx.x - slot * p.Hk), share = SHARED ? p.Hv / p.Hk : 1;
+    const int64_t slot = blockIdx.x / (unsigned)p.Hv;
+    const int h = (int)(blockIdx.x - slot * p.Hv), hk = h / (p.Hv / p.Hk);
     DeltaSeq sq;
     int64_t t0;
     int b;
@@ -346,421 +346,450 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 &&
 #pragma unroll
     for (int m = 0; m < MT; ++m) dq[m] = dk[m] = f32x4{};
 
-    for (int sh = 0; sh < share; ++sh) {
-        const int h = hk * share + sh;
-        const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
-        const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
-        const int64_t eplane = rows * p.Hv * p.dvp;
-        const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPI * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPI * DK * p.dvp;
-        const int ksv = p.dvp / 32;
+    const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
+    const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
+    const int64_t eplane = rows * p.Hv * p.dvp;
+    const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPI * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPI * DK * p.dvp;
+    const int ksv = p.dvp / 32;
 
-        // 32 columns of v on their way: a thread brings 16 bytes of a row of dO and of each plane of E and Z, and of the states, which lie a column of v to
-        // a row, four rows by four elements (the first 2 DK threads)
-        uint4 ereg[NPI], zreg[NPI], dreg[NPI];
-        uint2 areg[NPI][4], breg[NPI][4];
-        const int tr = tid >> 2, tc = (tid & 3) * 16, sq4 = tid / (DK / 4), sd4 = tid % (DK / 4);
-        auto fetch = [&](int ks) {
+    // 32 columns of v on their way: a thread brings 16 bytes of a row of dO and of each plane of E and Z, and of the states, which lie a column of v to
+    // a row, four rows by four elements (the first 2 DK threads)
+    uint4 ereg[NPI], zreg[NPI], dreg[NPI];
+    uint2 areg[NPI][4], breg[NPI][4];
+    const int tr = tid >> 2, tc = (tid & 3) * 16, sq4 = tid / (DK / 4), sd4 = tid % (DK / 4);
+    auto fetch = [&](int ks) {
 #pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                ereg[i] = buffer_load16(buffer_of(ep + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
-                zreg[i] = buffer_load16(buffer_of(zp + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
-            }
-#pragma unroll
-            for (int i = 0; i < NPI; ++i)
-                dreg[i] = buffer_load16(buffer_of(dp + i * p.dout.plane, (int64_t)(n - 1) * drow + 2 * p.dvp), tr * drow + 64 * ks + tc);
-#pragma unroll
-            for (int i = 0; i < NPI; ++i)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * 2) : kOutside;
-                    areg[i][x] = buffer_load8(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
-                    breg[i][x] = buffer_load8(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
-                }
-        };
-        // the blocks' units: a slot's largest of each kind, and the others' share of it
-        float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
-        const int G = p.dvp / 16;
-        if constexpr (UNITS) {
-            const float *fu = p.units + (slot * p.Hv + h) * 6 * G, *bu = p.dunits + (slot * p.Hv + h) * 6 * G;
-            const int in = (n > 32 ? 4 : 2) * G;
-            buffer_load(buffer_of(fu, 8 * G), 4 * lane, rA);
-            buffer_load(buffer_of(fu + 2 * G, 4 * in), 4 * lane, rE);
-            buffer_load(buffer_of(bu, 8 * G), 4 * lane, rB);
-            buffer_load(buffer_of(bu + 2 * G, 4 * in), 4 * lane, rZ);
+        for (int i = 0; i < NPI; ++i) {
+            ereg[i] = buffer_load16(buffer_of(ep + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
+            zreg[i] = buffer_load16(buffer_of(zp + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
         }
-        fetch(0);
-        if constexpr (UNITS) {
-            // the largest of dO, whose rows are read once more for it
-            const Buffer db = buffer_of(dp, (int64_t)(n - 1) * drow + 2 * p.dvp);
-            uint32_t most = 0;
-            for (int ks = 0; ks < ksv; ks += 4) {
-                uint4 d[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) d[x] = buffer_load16(db, ks + x < ksv ? tr * drow + 64 * (ks + x) + tc : kOutside);
+        for (int i = 0; i < NPI; ++i)
+            dreg[i] = buffer_load16(buffer_of(dp + i * p.dout.plane, (int64_t)(n - 1) * drow + 2 * p.dvp), tr * drow + 64 * ks + tc);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) most = max_halves(max_halves(most, max_halves(d[x].x, d[x].y)), max_halves(d[x].z, d[x].w));
+        for (int i = 0; i < NPI; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * 2) : kOutside;
+                areg[i][x] = buffer_load8(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+                breg[i][x] = buffer_load8(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
             }
-            most = most << 16 > (most & 0x7fff0000u) ? most << 16 : most & 0x7fff0000u;
-            const float whole = wave_max(__uint_as_float(most));
-            if (lane == 0) lds.most[wave] = whole;
-            uA = wave_max(rA); uE = wave_max(rE); uB = wave_max(rB); uZ = wave_max(rZ);
-            rA *= inverse_unit(uA); rE *= inverse_unit(uE); rB *= inverse_unit(uB); rZ *= inverse_unit(uZ);
+    };
+    // the blocks' units: a slot's largest of each kind, and the others' share of it
+    float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
+    const int G = p.dvp / 16;
+    if constexpr (UNITS) {
+        const float *fu = p.units + (slot * p.Hv + h) * 6 * G, *bu = p.dunits + (slot * p.Hv + h) * 6 * G;
+        const int in = (n > 32 ? 4 : 2) * G;
+        buffer_load(buffer_of(fu, 8 * G), 4 * lane, rA);
+        buffer_load(buffer_of(fu + 2 * G, 4 * in), 4 * lane, rE);
+        buffer_load(buffer_of(bu, 8 * G), 4 * lane, rB);
+        buffer_load(buffer_of(bu + 2 * G, 4 * in), 4 * lane, rZ);
+    }
+    fetch(0);
+    if constexpr (UNITS) {
+        // the largest of dO, whose rows are read once more for it
+        const Buffer db = buffer_of(dp, (int64_t)(n - 1) * drow + 2 * p.dvp);
+        uint32_t most = 0;
+        for (int ks = 0; ks < ksv; ks += 4) {
+            uint4 d[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) d[x] = buffer_load16(db, ks + x < ksv ? tr * drow + 64 * (ks + x) + tc : kOutside);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) most = max_halves(max_halves(most, max_halves(d[x].x, d[x].y)), max_halves(d[x].z, d[x].w));
         }
-        if (wave == 0) {
-            const bool in = lane < n;
-            const int64_t t = at + (in ? lane : 0);
-            const float gr = load_gate(p.g, sq.ib * p.g_sb + t * p.g_sl + h * p.g_sh, p.io, p.gate_io);
-            const float be = load_gate(p.beta, sq.ib * p.be_sb + t * p.be_sl + h * p.be_sh, p.io, p.gate_io);
-            double G = in ? gate_log(gr) : 0.0;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const double o = __shfl_up(G, m, 64);
-                if (lane >= m) G += o;
-            }
-            lds.G[lane] = G;
-            lds.beta[lane] = in ? be : 0.0f;
-        }
-
-        // Products with 16 others' steps at a time: earlier ones wrote what this wavefront's read (e_j . dO_own, e_j . z_own), later ones read what it wrote
-        // (dO_i . e_own, z_i . e_own); its own 16 are both, the second kind of them apart.
-        f32x4 P1[4] = {}, P2[4] = {}, P1own = {}, P2own = {};
-        f32x4 qs[MT], kr[MT], kw[MT];                                // S0 dO, S0 z, dS1 e of the lane's step
-#pragma unroll
-        for (int m = 0; m < MT; ++m) qs[m] = kr[m] = kw[m] = f32x4{};
-        auto mv = [](const Frag (&a)[NPI], const Frag (&b)[NPI], f32x4 c) __attribute__((always_inline)) -> f32x4 {
-            if constexpr (UNITS) return mfma16(a[0], b[0], c);
-            else return mm(a, b, c);
-        };
-        float dbeta = 0.0f, sdot = 0.0f, bown = 0.0f;
-        // K and Q of the slot, 16 quads of steps by DK / 4 quads of columns, under way during the last 32 columns
-        constexpr int IQ = DK / 64;
-        uint2 kw4[NPI][IQ * 4], qw4[NPI][IQ * 4];
-        auto fetch_kq = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int pl = 0; pl < NPI; ++pl) {
-                const Buffer kb = buffer_of(kp + pl * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
-#pragma unroll
-                for (int x = 0; x < IQ; ++x)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4);
-                        kw4[pl][4 * x + e] = buffer_load8(kb, (4 * tq + e) * krow + 8 * dc);
-                        qw4[pl][4 * x + e] = buffer_load8(qb, (4 * tq + e) * qrow + 8 * dc);
-                    }
-            }
-        };
-        auto columns = [&](int ks, auto last) __attribute__((always_inline)) {
-            lds_barrier();                                  // what was there in LDS has been read
-            auto &L = lds.v;
-            if constexpr (UNITS) uD = block_unit(fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3])));
-            uint32_t pE = 0, pZ = 0, pA = 0, pB = 0;
-            if constexpr (UNITS) {                          // brought to the slot's units
-                const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 4) * G, gs = 2 * ks + (sq4 >> 2 & 1) + (8 * sd4 >= DK ? G : 0);
-                const float fE = __shfl(rE, ge, 64), fZ = __shfl(rZ, ge, 64), fA = __shfl(rA, gs, 64), fB = __shfl(rB, gs, 64);
-                pE = pack_f16(fE, fE); pZ = pack_f16(fZ, fZ); pA = pack_f16(fA, fA); pB = pack_f16(fB, fB);
-            }
-            auto times = [&](uint32_t x, uint32_t f) __attribute__((always_inline)) -> uint32_t {
-                return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f)) : x;
-            };
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                const uint4 e = ereg[i], z = zreg[i];
-                *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
-                *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = make_uint4(times(z.x, pZ), times(z.y, pZ), times(z.z, pZ), times(z.w, pZ));
-            }
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                uint4 d = dreg[i];
-                if constexpr (UNITS) {
-                    const float inv = inverse_unit(uD);
-                    auto conv = [&](uint32_t x) __attribute__((always_inline)) { return pack_f16(__uint_as_float(x << 16) * inv, hi_part(__uint_as_float(x)) * inv); };
-                    d = make_uint4(conv(d.x), conv(d.y), conv(d.z), conv(d.w));
-                }
-                *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = d;
-            }
-#pragma unroll
-            for (int i = 0; i < NPI; ++i)
-                if (tid < 2 * DK) {
-                    uint2 c[4], d[4];
-                    transpose_quad(areg[i], c);
-                    transpose_quad(breg[i], d);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(c[x].x, pA), times(c[x].y, pA));
-                        *reinterpret_cast<uint2 *>(&L.s1[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(d[x].x, pB), times(d[x].y, pB));
-                    }
-                }
-            if constexpr (last) fetch_kq();
-            else fetch(ks + 1);
-            lds_barrier();
-            bown = lds.beta[own];
-            Frag dO[NPI], e[NPI], z[NPI];
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) dO[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][own][8 * g4]);
-#pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                e[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][own][8 * g4]);
-                z[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][own][8 * g4]);
-            }
-            // the states' products, and <S0, dS1> of a quarter of their rows
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                Frag s0[NPI], s1[NPI];
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-                }
-                qs[m] = mv(s0, dO, qs[m]);
-                kr[m] = mv(s0, z, kr[m]);
-                kw[m] = mv(s1, e, kw[m]);
-                if (m & 1) reads_first();
-            }
-#pragma unroll
-            for (int y = 0; y < MT / 4; ++y) {
-                const int m = 4 * y + wave;
-                Frag s0[NPI], s1[NPI];
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-                    s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    if constexpr (UNITS) sdot = __builtin_amdgcn_fdot2(s0[0].p16[x], s1[0].p16[x], sdot, false);
-                    else {
-                        float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
-#pragma unroll
-                        for (int i = NPI - 1; i >= 0; --i) {
-                            al += __uint_as_float(s1[i].u[x] << 16); ah += hi_part(__uint_as_float(s1[i].u[x]));
-                            cl += __uint_as_float(s0[i].u[x] << 16); chh += hi_part(__uint_as_float(s0[i].u[x]));
-                        }
-                        sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
-                    }
-                }
-            }
-            // with the other steps
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                Frag r1[NPI], r2[NPI], c1[NPI], c2[NPI];
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    r1[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.d)[i][16 * m + row16][8 * g4]);
-                    r2[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.z)[i][16 * m + row16][8 * g4]);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) { c1[i].u[x] = m <= wave ? dO[i].u[x] : e[i].u[x]; c2[i].u[x] = m <= wave ? z[i].u[x] : e[i].u[x]; }
-                }
-                P1[m] = mv(r1, c1, P1[m]);
-                P2[m] = mv(r2, c2, P2[m]);
-            }
-            P1own = mv(dO, e, P1own);
-            P2own = mv(z, e, P2own);
-            // dV = beta z, dbeta = z . e
-            f32x4 zs[2] = {}, es[2] = {};
-            if constexpr (UNITS) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) dbeta = __builtin_amdgcn_fdot2(z[0].p16[x], e[0].p16[x], dbeta, false);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) zs[x >> 2][x & 3] = (float)z[0].h16[x] * uZ;
-            } else
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-#pragma unroll
-                    for (int i = NPI - 1; i >= 0; --i) {
-                        zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
-                        es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
-                    }
-            const int c = 32 * ks + 8 * g4;
-            IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + (own_in ? own : 0)) * p.Hv + h) * p.dv + c;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                f32x4 v;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) { if (!UNITS) dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
-                if (own_in) {
-                    if (p.o_vec && c + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
-                    else
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
-                }
-            }
-        };
-#pragma unroll 1
-        for (int ks = 0; ks < ksv - 1; ++ks) columns(ks, std::false_type{});
-        columns(ksv - 1, std::true_type{});
-        if constexpr (UNITS) { dbeta = dbeta * uZ * uE; sdot = sdot * uA * uB; }
-        const double Gown = lds.G[own];
-        const float gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
-
-        // K and Q into LDS, turned, and as rows
-        lds_barrier();
-#pragma unroll
-        for (int pl = 0; pl < NPI; ++pl)
-#pragma unroll
-            for (int x = 0; x < IQ; ++x) {
-                const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4), place = (tq >> 3) * 32 + quad_place(tq & 7);
-                uint2 w[4], u[4], c[4], d[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { w[e] = kw4[pl][4 * x + e]; u[e] = qw4[pl][4 * x + e]; }
-                transpose_quad(w, c);
-                transpose_quad(u, d);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    *reinterpret_cast<uint2 *>(&lds.k.kt[pl][4 * dc + e][turned(4 * dc, place)]) = c[e];
-                    *reinterpret_cast<uint2 *>(&lds.k.qt[pl][4 * dc + e][turned(4 * dc, place)]) = d[e];
-                    if constexpr (ROWS) {
-                        *reinterpret_cast<uint2 *>(&lds.k.kr[0][4 * tq + e][4 * dc]) = w[e];
-                        *reinterpret_cast<uint2 *>(&lds.k.kr[1][4 * tq + e][4 * dc]) = u[e];
-                    }
-                }
-            }
-        lds_barrier();
-        // rows of K (which = 0) and Q as operands
-        auto row_of = [&](int which, int t, int ks, Frag (&f)[NPI]) {
-            if constexpr (ROWS) f[0].v = *reinterpret_cast<const uint4 *>(&lds.k.kr[which][t][32 * ks + 8 * g4]);
-            else
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
-                    f[i].v = buffer_load16(rb, t * (which ? qrow : krow) + 64 * ks + 16 * g4);
-                }
-        };
-        auto four_of = [&](int which, int m) -> f32x4 {      // of this lane's step, columns 16 m + 4 g4 ..
-            f32x4 v = {};
-#pragma unroll
-            for (int i = NPI - 1; i >= 0; --i) {
-                uint2 a;
-                if constexpr (ROWS) a = *reinterpret_cast<const uint2 *>(&lds.k.kr[which][own][16 * m + 4 * g4]);
-                else {
-                    const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
-                    a = buffer_load8(rb, own * (which ? qrow : krow) + 32 * m + 8 * g4);
-                }
-                v += f32x4{__uint_as_float(a.x << 16), hi_part(__uint_as_float(a.x)), __uint_as_float(a.y << 16), hi_part(__uint_as_float(a.y))};
-            }
-            return v;
-        };
-        // the states' part of dQ and dK
-        float dG = 0.0f, ends = 0.0f;
-        {
-            const float cq = p.scale * gam, ck = -gam * bown, cw = en * bown, vq = uA * uD, vk = uA * uZ, vw = uB * uE;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const f32x4 kv = four_of(0, m), qv = four_of(1, m);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float a = cq * (vq * qs[m][r]), c = ck * (vk * kr[m][r]), w = cw * (vw * kw[m][r]);
-                    dq[m][r] += a; dk[m][r] += c + w;
-                    dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
-                    ends = __builtin_fmaf(kv[r], w, ends);
-                }
-            }
-            dG -= ends;
-        }
-        // F, H in both orientations, M's row and column sums
-        f32x4 HH[4], Ft[4], F[4];
-        {
-            const float vf = uD * uE, vh = uZ * uE;
-            Frag kf[KS][NPI], qf[KS][NPI];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) { row_of(0, own, ks, kf[ks]); row_of(1, own, ks, qf[ks]); }
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                f32x4 QKt = {}, QK = {}, KK = {};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    Frag kx[NPI], qx[NPI];
-                    row_of(0, 16 * m + row16, ks, kx);
-                    row_of(1, 16 * m + row16, ks, qx);
-                    KK = mm(kx, kf[ks], KK);
-                    QKt = mm(kx, qf[ks], QKt);
-                    QK = mm(qx, kf[ks], QK);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int o = 16 * m + 4 * g4 + r;
-                    const double Go = lds.G[o];
-                    const float bo = lds.beta[o];
-                    const float D = __expf((float)(o <= own ? Gown - Go : Go - Gown));
-                    const float ds = p.scale * D * vf, db = -D * bown * bo * vh;
-                    const float ft = o <= own ? ds * bo * P1[m][r] : 0.0f;          // this step reads what step o wrote
-                    const float f = o >= own ? ds * bown * (m == wave ? P1own[r] : P1[m][r]) : 0.0f;        // step o reads what this step wrote
-                    const float hl = o < own ? db * P2[m][r] : 0.0f, hx = o > own ? db * (m == wave ? P2own[r] : P2[m][r]) : 0.0f;
-                    const float hh = hl + hx;
-                    dG += ft * QKt[r] + hl * KK[r];
-                    dG -= f * QK[r] + hx * KK[r];
-                    Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
-                }
-            }
-        }
-        // dQ += F K, dK += (H + H^T) K + F^T Q
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            Frag ft[NPF], f[NPF], hh[NPF];
-            split_tiles<NPF>(Ft[2 * x], Ft[2 * x + 1], ft);
-            split_tiles<NPF>(F[2 * x], F[2 * x + 1], f);
-            split_tiles<NPF>(HH[2 * x], HH[2 * x + 1], hh);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                Frag kt[NPI], qt[NPI];
-#pragma unroll
-                for (int i = 0; i < NPI; ++i) {
-                    kt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.kt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
-                    qt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.qt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
-                }
-                dq[m] = mm(kt, ft, dq[m]);
-                dk[m] = mm(kt, hh, dk[m]);
-                dk[m] = mm(qt, f, dk[m]);
-            }
-        }
-        if (!own_in) { dG = 0.0f; ends = 0.0f; }
-        // over the four lane groups of a step, then over the steps
-#pragma unroll
-        for (int m = 16; m < 64; m <<= 1) {
-            dG += __shfl_xor(dG, m, 64);
-            dbeta += __shfl_xor(dbeta, m, 64);
-        }
+        most = most << 16 > (most & 0x7fff0000u) ? most << 16 : most & 0x7fff0000u;
+        const float whole = wave_max(__uint_as_float(most));
+        if (lane == 0) lds.most[wave] = whole;
+        uA = wave_max(rA); uE = wave_max(rE); uB = wave_max(rB); uZ = wave_max(rZ);
+        rA *= inverse_unit(uA); rE *= inverse_unit(uE); rB *= inverse_unit(uB); rZ *= inverse_unit(uZ);
+    }
+    if (wave == 0) {
+        const bool in = lane < n;
+        const int64_t t = at + (in ? lane : 0);
+        const float gr = load_gate(p.g, sq.ib * p.g_sb + t * p.g_sl + h * p.g_sh, p.io, p.gate_io);
+        const float be = load_gate(p.beta, sq.ib * p.be_sb + t * p.be_sl + h * p.be_sh, p.io, p.gate_io);
+        double G = in ? gate_log(gr) : 0.0;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
-            ends += __shfl_xor(ends, m, 64);
-            sdot += __shfl_xor(sdot, m, 64);
+            const double o = __shfl_up(G, m, 64);
+            if (lane >= m) G += o;
         }
-        if (lane < 16) {
-            lds.dG[own] = dG;
-            if (own_in) {
-                const int64_t i = (row0 + own) * p.Hv + h;
-                if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dbeta) + i, dbeta);
-                else store_io(reinterpret_cast<float *>(p.dbeta) + i, dbeta);
-            }
-        }
-        if (lane == 0) { lds.ends[wave] = ends; lds.dots[wave] = sdot; }
-        lds_barrier();
-        if (wave == 0) {
-            float x = lds.dG[lane];
+        lds.G[lane] = G;
+        lds.beta[lane] = in ? be : 0.0f;
+    }
+
+    // Products with 16 others' steps at a time: earlier ones wrote what this wavefront's read (e_j . dO_own, e_j . z_own), later ones read what it wrote
+    // (dO_i . e_own, z_i . e_own); its own 16 are both, the second kind of them apart.
+    f32x4 P1[4] = {}, P2[4] = {}, P1own = {}, P2own = {};
+    f32x4 qs[MT], kr[MT], kw[MT];                                // S0 dO, S0 z, dS1 e of the lane's step
 #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const float o = __shfl_down(x, m, 64);
-                if (lane + m < 64) x += o;
+    for (int m = 0; m < MT; ++m) qs[m] = kr[m] = kw[m] = f32x4{};
+    auto mv = [](const Frag (&a)[NPI], const Frag (&b)[NPI], f32x4 c) __attribute__((always_inline)) -> f32x4 {
+        if constexpr (UNITS) return mfma16(a[0], b[0], c);
+        else return mm(a, b, c);
+    };
+    float dbeta = 0.0f, sdot = 0.0f, bown = 0.0f;
+    // K and Q of the slot, 16 quads of steps by DK / 4 quads of columns, under way during the last 32 columns
+    constexpr int IQ = DK / 64;
+    uint2 kw4[NPI][IQ * 4], qw4[NPI][IQ * 4];
+    auto fetch_kq = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int pl = 0; pl < NPI; ++pl) {
+            const Buffer kb = buffer_of(kp + pl * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + pl * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
+#pragma unroll
+            for (int x = 0; x < IQ; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4);
+                    kw4[pl][4 * x + e] = buffer_load8(kb, (4 * tq + e) * krow + 8 * dc);
+                    qw4[pl][4 * x + e] = buffer_load8(qb, (4 * tq + e) * qrow + 8 * dc);
+                }
+        }
+    };
+    auto columns = [&](int ks, auto last) __attribute__((always_inline)) {
+        lds_barrier();                                  // what was there in LDS has been read
+        auto &L = lds.v;
+        if constexpr (UNITS) uD = block_unit(fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3])));
+        uint32_t pE = 0, pZ = 0, pA = 0, pB = 0;
+        if constexpr (UNITS) {                          // brought to the slot's units
+            const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 4) * G, gs = 2 * ks + (sq4 >> 2 & 1) + (8 * sd4 >= DK ? G : 0);
+            const float fE = __shfl(rE, ge, 64), fZ = __shfl(rZ, ge, 64), fA = __shfl(rA, gs, 64), fB = __shfl(rB, gs, 64);
+            pE = pack_f16(fE, fE); pZ = pack_f16(fZ, fZ); pA = pack_f16(fA, fA); pB = pack_f16(fB, fB);
+        }
+        auto times = [&](uint32_t x, uint32_t f) __attribute__((always_inline)) -> uint32_t {
+            return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f)) : x;
+        };
+#pragma unroll
+        for (int i = 0; i < NPI; ++i) {
+            const uint4 e = ereg[i], z = zreg[i];
+            *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
+            *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = make_uint4(times(z.x, pZ), times(z.y, pZ), times(z.z, pZ), times(z.w, pZ));
+        }
+#pragma unroll
+        for (int i = 0; i < NPI; ++i) {
+            uint4 d = dreg[i];
+            if constexpr (UNITS) {
+                const float inv = inverse_unit(uD);
+                auto conv = [&](uint32_t x) __attribute__((always_inline)) { return pack_f16(__uint_as_float(x << 16) * inv, hi_part(__uint_as_float(x)) * inv); };
+                d = make_uint4(conv(d.x), conv(d.y), conv(d.z), conv(d.w));
             }
-            x += (lds.ends[0] + lds.ends[1]) + (lds.ends[2] + lds.ends[3]);
-            x += __expf((float)lds.G[63]) * ((lds.dots[0] + lds.dots[1]) + (lds.dots[2] + lds.dots[3]));
-            if (lane < n) {
-                const int64_t i = (row0 + lane) * p.Hv + h;
-                if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dg) + i, x);
-                else store_io(reinterpret_cast<float *>(p.dg) + i, x);
+            *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = d;
+        }
+#pragma unroll
+        for (int i = 0; i < NPI; ++i)
+            if (tid < 2 * DK) {
+                uint2 c[4], d[4];
+                transpose_quad(areg[i], c);
+                transpose_quad(breg[i], d);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(c[x].x, pA), times(c[x].y, pA));
+                    *reinterpret_cast<uint2 *>(&L.s1[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(d[x].x, pB), times(d[x].y, pB));
+                }
+            }
+        if constexpr (last) fetch_kq();
+        else fetch(ks + 1);
+        lds_barrier();
+        bown = lds.beta[own];
+        Frag dO[NPI], e[NPI], z[NPI];
+#pragma unroll
+        for (int i = 0; i < NPI; ++i) dO[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][own][8 * g4]);
+#pragma unroll
+        for (int i = 0; i < NPI; ++i) {
+            e[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][own][8 * g4]);
+            z[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][own][8 * g4]);
+        }
+        // the states' products, and <S0, dS1> of a quarter of their rows
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            Frag s0[NPI], s1[NPI];
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+            }
+            qs[m] = mv(s0, dO, qs[m]);
+            kr[m] = mv(s0, z, kr[m]);
+            kw[m] = mv(s1, e, kw[m]);
+            if (m & 1) reads_first();
+        }
+#pragma unroll
+        for (int y = 0; y < MT / 4; ++y) {
+            const int m = 4 * y + wave;
+            Frag s0[NPI], s1[NPI];
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+                s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if constexpr (UNITS) sdot = __builtin_amdgcn_fdot2(s0[0].p16[x], s1[0].p16[x], sdot, false);
+                else {
+                    float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
+#pragma unroll
+                    for (int i = NPI - 1; i >= 0; --i) {
+                        al += __uint_as_float(s1[i].u[x] << 16); ah += hi_part(__uint_as_float(s1[i].u[x]));
+                        cl += __uint_as_float(s0[i].u[x] << 16); chh += hi_part(__uint_as_float(s0[i].u[x]));
+                    }
+                    sdot = __builtin_fmaf(al, cl, __builtin_fmaf(ah, chh, sdot));
+                }
+            }
+        }
+        // with the other steps
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            Frag r1[NPI], r2[NPI], c1[NPI], c2[NPI];
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                r1[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.d)[i][16 * m + row16][8 * g4]);
+                r2[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.z)[i][16 * m + row16][8 * g4]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) { c1[i].u[x] = m <= wave ? dO[i].u[x] : e[i].u[x]; c2[i].u[x] = m <= wave ? z[i].u[x] : e[i].u[x]; }
+            }
+            P1[m] = mv(r1, c1, P1[m]);
+            P2[m] = mv(r2, c2, P2[m]);
+        }
+        P1own = mv(dO, e, P1own);
+        P2own = mv(z, e, P2own);
+        // dV = beta z, dbeta = z . e
+        f32x4 zs[2] = {}, es[2] = {};
+        if constexpr (UNITS) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) dbeta = __builtin_amdgcn_fdot2(z[0].p16[x], e[0].p16[x], dbeta, false);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) zs[x >> 2][x & 3] = (float)z[0].h16[x] * uZ;
+        } else
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+#pragma unroll
+                for (int i = NPI - 1; i >= 0; --i) {
+                    zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
+                    es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
+                }
+        const int c = 32 * ks + 8 * g4;
+        IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + (own_in ? own : 0)) * p.Hv + h) * p.dv + c;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            f32x4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { if (!UNITS) dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
+            if (own_in) {
+                if (p.o_vec && c + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
+            }
+        }
+    };
+#pragma unroll 1
+    for (int ks = 0; ks < ksv - 1; ++ks) columns(ks, std::false_type{});
+    columns(ksv - 1, std::true_type{});
+    if constexpr (UNITS) { dbeta = dbeta * uZ * uE; sdot = sdot * uA * uB; }
+    const double Gown = lds.G[own];
+    const float gam = __expf((float)Gown), en = __expf((float)(lds.G[63] - Gown));
+
+    // K and Q into LDS, turned, and as rows
+    lds_barrier();
+#pragma unroll
+    for (int pl = 0; pl < NPI; ++pl)
+#pragma unroll
+        for (int x = 0; x < IQ; ++x) {
+            const int i = tid + 256 * x, tq = i / (DK / 4), dc = i % (DK / 4), place = (tq >> 3) * 32 + quad_place(tq & 7);
+            uint2 w[4], u[4], c[4], d[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { w[e] = kw4[pl][4 * x + e]; u[e] = qw4[pl][4 * x + e]; }
+            transpose_quad(w, c);
+            transpose_quad(u, d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                *reinterpret_cast<uint2 *>(&lds.k.kt[pl][4 * dc + e][turned(4 * dc, place)]) = c[e];
+                *reinterpret_cast<uint2 *>(&lds.k.qt[pl][4 * dc + e][turned(4 * dc, place)]) = d[e];
+                if constexpr (ROWS) {
+                    *reinterpret_cast<uint2 *>(&lds.k.kr[0][4 * tq + e][4 * dc]) = w[e];
+                    *reinterpret_cast<uint2 *>(&lds.k.kr[1][4 * tq + e][4 * dc]) = u[e];
+                }
+            }
+        }
+    lds_barrier();
+    // rows of K (which = 0) and Q as operands
+    auto row_of = [&](int which, int t, int ks, Frag (&f)[NPI]) {
+        if constexpr (ROWS) f[0].v = *reinterpret_cast<const uint4 *>(&lds.k.kr[which][t][32 * ks + 8 * g4]);
+        else
+#pragma unroll
+            for (int i = 0; i < NPI; ++i) {
+                const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
+                f[i].v = buffer_load16(rb, t * (which ? qrow : krow) + 64 * ks + 16 * g4);
+            }
+    };
+    auto four_of = [&](int which, int m) -> f32x4 {      // of this lane's step, columns 16 m + 4 g4 ..
+        f32x4 v = {};
+#pragma unroll
+        for (int i = NPI - 1; i >= 0; --i) {
+            uint2 a;
+            if constexpr (ROWS) a = *reinterpret_cast<const uint2 *>(&lds.k.kr[which][own][16 * m + 4 * g4]);
+            else {
+                const Buffer rb = which ? buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK) : buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK);
+                a = buffer_load8(rb, own * (which ? qrow : krow) + 32 * m + 8 * g4);
+            }
+            v += f32x4{__uint_as_float(a.x << 16), hi_part(__uint_as_float(a.x)), __uint_as_float(a.y << 16), hi_part(__uint_as_float(a.y))};
+        }
+        return v;
+    };
+    // the states' part of dQ and dK
+    float dG = 0.0f, ends = 0.0f;
+    {
+        const float cq = p.scale * gam, ck = -gam * bown, cw = en * bown, vq = uA * uD, vk = uA * uZ, vw = uB * uE;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const f32x4 kv = four_of(0, m), qv = four_of(1, m);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float a = cq * (vq * qs[m][r]), c = ck * (vk * kr[m][r]), w = cw * (vw * kw[m][r]);
+                dq[m][r] += a; dk[m][r] += c + w;
+                dG = __builtin_fmaf(qv[r], a, __builtin_fmaf(kv[r], c, dG));
+                ends = __builtin_fmaf(kv[r], w, ends);
+            }
+        }
+        dG -= ends;
+    }
+    // F, H in both orientations, M's row and column sums
+    f32x4 HH[4], Ft[4], F[4];
+    {
+        const float vf = uD * uE, vh = uZ * uE;
+        Frag kf[KS][NPI], qf[KS][NPI];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) { row_of(0, own, ks, kf[ks]); row_of(1, own, ks, qf[ks]); }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            f32x4 QKt = {}, QK = {}, KK = {};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                Frag kx[NPI], qx[NPI];
+                row_of(0, 16 * m + row16, ks, kx);
+                row_of(1, 16 * m + row16, ks, qx);
+                KK = mm(kx, kf[ks], KK);
+                QKt = mm(kx, qf[ks], QKt);
+                QK = mm(qx, kf[ks], QK);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int o = 16 * m + 4 * g4 + r;
+                const double Go = lds.G[o];
+                const float bo = lds.beta[o];
+                const float D = __expf((float)(o <= own ? Gown - Go : Go - Gown));
+                const float ds = p.scale * D * vf, db = -D * bown * bo * vh;
+                const float ft = o <= own ? ds * bo * P1[m][r] : 0.0f;          // this step reads what step o wrote
+                const float f = o >= own ? ds * bown * (m == wave ? P1own[r] : P1[m][r]) : 0.0f;        // step o reads what this step wrote
+                const float hl = o < own ? db * P2[m][r] : 0.0f, hx = o > own ? db * (m == wave ? P2own[r] : P2[m][r]) : 0.0f;
+                const float hh = hl + hx;
+                dG += ft * QKt[r] + hl * KK[r];
+                dG -= f * QK[r] + hx * KK[r];
+                Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
             }
         }
     }
-    if (own_in) {
-        IO *qo = reinterpret_cast<IO *>(p.dq) + ((row0 + own) * p.Hk + hk) * p.dk, *ko = reinterpret_cast<IO *>(p.dkk) + ((row0 + own) * p.Hk + hk) * p.dk;
+    // dQ += F K, dK += (H + H^T) K + F^T Q
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        Frag ft[NPF], f[NPF], hh[NPF];
+        split_tiles<NPF>(Ft[2 * x], Ft[2 * x + 1], ft);
+        split_tiles<NPF>(F[2 * x], F[2 * x + 1], f);
+        split_tiles<NPF>(HH[2 * x], HH[2 * x + 1], hh);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const int d = 16 * m + 4 * g4;
-            if (p.dk % 4 == 0 && p.o_vec) {
-                if (d < p.dk) { store4(qo + d, dq[m]); store4(ko + d, dk[m]); }
-            } else
+            Frag kt[NPI], qt[NPI];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) if (d + r < p.dk) { store_io(qo + d + r, dq[m][r]); store_io(ko + d + r, dk[m][r]); }
+            for (int i = 0; i < NPI; ++i) {
+                kt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.kt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
+                qt[i].v = *reinterpret_cast<const uint4 *>(&lds.k.qt[i][16 * m + row16][turned(16 * m, 32 * x + 8 * g4)]);
+            }
+            dq[m] = mm(kt, ft, dq[m]);
+            dk[m] = mm(kt, hh, dk[m]);
+            dk[m] = mm(qt, f, dk[m]);
         }
+    }
+    if (!own_in) { dG = 0.0f; ends = 0.0f; }
+    // over the four lane groups of a step, then over the steps
+#pragma unroll
+    for (int m = 16; m < 64; m <<= 1) {
+        dG += __shfl_xor(dG, m, 64);
+        dbeta += __shfl_xor(dbeta, m, 64);
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        ends += __shfl_xor(ends, m, 64);
+        sdot += __shfl_xor(sdot, m, 64);
+    }
+    if (lane < 16) {
+        lds.dG[own] = dG;
+        if (own_in) {
+            const int64_t i = (row0 + own) * p.Hv + h;
+            if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dbeta) + i, dbeta);
+            else store_io(reinterpret_cast<float *>(p.dbeta) + i, dbeta);
+        }
+    }
+    if (lane == 0) { lds.ends[wave] = ends; lds.dots[wave] = sdot; }
+    lds_barrier();
+    if (wave == 0) {
+        float x = lds.dG[lane];
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const float o = __shfl_down(x, m, 64);
+            if (lane + m < 64) x += o;
+        }
+        x += (lds.ends[0] + lds.ends[1]) + (lds.ends[2] + lds.ends[3]);
+        x += __expf((float)lds.G[63]) * ((lds.dots[0] + lds.dots[1]) + (lds.dots[2] + lds.dots[3]));
+        if (lane < n) {
+            const int64_t i = (row0 + lane) * p.Hv + h;
+            if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(p.dg) + i, x);
+            else store_io(reinterpret_cast<float *>(p.dg) + i, x);
+        }
+    }
+    if (!own_in) return;
+    if (p.part) {
+        float *qo = p.part + ((row0 + own) * p.Hv + h) * DK + 4 * g4, *ko = qo + rows * p.Hv * DK;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) { store4(qo + 16 * m, dq[m]); store4(ko + 16 * m, dk[m]); }
+        return;
+    }
+    IO *qo = reinterpret_cast<IO *>(p.dq) + ((row0 + own) * p.Hk + hk) * p.dk, *ko = reinterpret_cast<IO *>(p.dkk) + ((row0 + own) * p.Hk + hk) * p.dk;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int d = 16 * m + 4 * g4;
+        if (p.dk % 4 == 0 && p.o_vec) {
+            if (d < p.dk) { store4(qo + d, dq[m]); store4(ko + d, dk[m]); }
+        } else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (d + r < p.dk) { store_io(qo + d + r, dq[m][r]); store_io(ko + d + r, dk[m][r]); }
+    }
+}
+
+// dQ and dK of a shared key head: its value heads' parts in their order.  A workgroup takes a quarter of a slot's steps and a key head, a thread four columns; bound
+// by the parts' bytes.  (With a workgroup for all value heads of a key head no parts would be written, but the registers of both sums do not fit
+// beside the rest, and where heads are few the chip is left empty: float32, 239 steps of 12 value heads on 4 of 128 x 128, 2 entries: 280 us a
+// training step so, 170 now.)
+template <class IO, int DK> __global__ __launch_bounds__(256) void k_delta_share(const DeltaParams p) {
+    const int64_t slot = blockIdx.x / (unsigned)p.Hk;
+    const int hk = (int)(blockIdx.x - slot * p.Hk), d = threadIdx.x % (DK / 4) * 4, share = p.Hv / p.Hk;
+    DeltaSeq sq;
+    int64_t t0;
+    int b;
+    const int n = delta_slot(p, slot, sq, t0, b);
+    const float *part = p.part + (blockIdx.y & 1 ? (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * DK : 0);
+    void *out = blockIdx.y & 1 ? p.dkk : p.dq;
+    for (int t = (blockIdx.y >> 1) * (1024 / DK) + threadIdx.x / (DK / 4); t < n; t += 4 * (1024 / DK)) {
+        const int64_t row = sq.row + t0 + t;
+        const float *from = part + (row * p.Hv + hk * share) * DK + d;
+        IO *to = reinterpret_cast<IO *>(out) + (row * p.Hk + hk) * p.dk + d;
+        f32x4 x = {};
+        for (int i = 0; i < share; ++i) x += *reinterpret_cast<const f32x4 *>(from + i * DK);
+        if (p.dk % 4 == 0 && p.o_vec) {
+            if (d < p.dk) store4(to, x);
+        } else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (d + r < p.dk) store_io(to + r, x[r]);
     }
 }
 
@@ -792,9 +821,11 @@ hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
 template <class IO, int NPI, int DK> static hipError_t launch_grads_one(const DeltaParams &p, hipStream_t s) {
     constexpr size_t bytes = sizeof(GradLds<NPI, DK>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    auto k = p.Hv > p.Hk ? k_delta_grads<IO, NPI, DK, true> : k_delta_grads<IO, NPI, DK, false>;
+    auto k = k_delta_grads<IO, NPI, DK>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k, dim3((unsigned)(p.nslots * p.Hk)), dim3(256), bytes, s, p);
+    hipLaunchKernelGGL(k, dim3((unsigned)(p.nslots * p.Hv)), dim3(256), bytes, s, p);
+    if (const hipError_t e = hipGetLastError()) return e;
+    if (p.part) hipLaunchKernelGGL((k_delta_share<IO, DK>), dim3((unsigned)(p.nslots * p.Hk), 8), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s) {
