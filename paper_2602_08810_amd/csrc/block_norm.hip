@@ -53,24 +53,24 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
 }
 // Sum over the workgroup.  `part`: a float of LDS for each of eight wavefronts, taken in turn from a set (`Sums`) that is large enough for a
-// slot not to be written again before a barrier has passed since it was read: one barrier a sum.
+// slot not to be written again before a barrier has passed since it was read: one barrier a sum.  Wavefronts that are not there have left zeros.
 __device__ __forceinline__ float block_sum(float x, float *part) {
     x = wave_sum(x);
     const int waves = blockDim.x >> 6;
     if (waves == 1) return x;
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     lds_barrier();
-    float s = part[0];
-    for (int w = 1; w < waves; ++w) s += part[w];
-    return s;
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(part), b = *reinterpret_cast<const f32x4 *>(part + 4);
+    return ((a[0] + a[1]) + (a[2] + a[3])) + ((b[0] + b[1]) + (b[2] + b[3]));
 }
 constexpr int kSumSlots = 8;                      // four sums a row, two rows
 
 // How the sum over a group is taken: over the workgroup (one group), over `lanes` neighbouring lanes (a power of two), or through LDS.
 enum : int { GROUP_ROW = 0, GROUP_LANES = 1, GROUP_LDS = 2 };
 
-// Sums over each thread's groups of `x[i]` (piece i of the row lies in one group), into x.
-template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], int how, int pieces, int per_group, float *lds, float *part) {
+// Sums over each thread's groups of `x[i]` (piece i of the row lies in one group, `of[i]`), into x.  Through LDS a power of two of neighbouring lanes
+// takes a group, as many as the workgroup has for it (32 groups of 49, training, 2442 rows in bfloat16: 94 us with a lane a group, 70 so).
+template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], const int (&of)[NV], int how, int pieces, int per_group, float *lds, float *part) {
     if (how == GROUP_ROW) {
         float s = 0.0f;
 #pragma unroll
@@ -88,22 +88,21 @@ template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], int
         for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; if (v < pieces) lds[v] = x[i]; }
         lds_barrier();
         float *out = lds + pieces;
-        if (per_group < 64)                       // a thread or a wavefront a group
-            for (int g = threadIdx.x; g < groups; g += nt) {
-                float s = 0.0f;
-                for (int j = 0; j < per_group; ++j) s += lds[g * per_group + j];
-                out[g] = s;
-            }
-        else
-            for (int g = threadIdx.x >> 6; g < groups; g += nt >> 6) {
-                float s = 0.0f;
-                for (int j = threadIdx.x & 63; j < per_group; j += 64) s += lds[g * per_group + j];
-                s = wave_sum(s);
-                if ((threadIdx.x & 63) == 0) out[g] = s;
-            }
+        const int room = nt / groups, lanes = room >= 64 ? 64 : room > 1 ? 1 << (31 - __builtin_clz(room)) : 1;
+        const int at = threadIdx.x & (lanes - 1), g0 = threadIdx.x / lanes;                   // (a power of two: a shift)
+        for (int first = 0; first < groups; first += nt / lanes) {
+            const int g = first + g0;
+            float s = 0.0f;
+            if (g < groups)
+                for (int j = at; j < per_group; j += lanes) s += lds[g * per_group + j];
+            if (lanes == 64) s = wave_sum(s);
+            else
+                for (int m = 1; m < lanes; m <<= 1) s += __shfl_xor(s, m, 64);
+            if (at == 0 && g < groups) out[g] = s;
+        }
         lds_barrier();
 #pragma unroll
-        for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; x[i] = v < pieces ? out[v / per_group] : 0.0f; }
+        for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; x[i] = v < pieces ? out[of[i]] : 0.0f; }
         lds_barrier();
     }
 }
@@ -146,9 +145,9 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
     auto slot = [&]() { turn = (turn + 1) % kSumSlots; return lds + turn * 8; };
     float w1[BWD ? NV : 1][VEC] = {}, w2[BWD ? NV : 1][VEC] = {}, w3[BWD ? NV : 1][VEC] = {};
     const float by_width = 1.0f / (float)p.width, by_D = 1.0f / (float)p.D;
-    int cp[NV];                                   // where a piece's part of post_weight starts
+    int of[NV], cp[NV];                                   // where a piece's part of post_weight starts
 #pragma unroll
-    for (int i = 0; i < NV; ++i) { const int c = (threadIdx.x + i * nt) * VEC; cp[i] = c >= p.D ? 0 : p.post_shared ? c % p.width : c; }
+    for (int i = 0; i < NV; ++i) { const int c = (threadIdx.x + i * nt) * VEC; of[i] = how == GROUP_LDS ? c / p.width : 0; cp[i] = c >= p.D ? 0 : p.post_shared ? c % p.width : c; }
     struct Weight { float w[VEC]; __device__ __forceinline__ float get(int e) const { return w[e]; } };
     auto weight = [&](const float *w, int c) {
         Weight r;
@@ -167,6 +166,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
     Row even, odd;
     int64_t row = blockIdx.x;
     even.load(p, row);
+    if (threadIdx.x < kSumSlots * 8) lds[threadIdx.x] = 0.0f;
     {
         const Buffer bp = buffer_of(p.post, p.post ? (p.post_shared ? p.width : p.D) * 4 : 0), bs = buffer_of(p.scale, p.scale ? p.D * 4 : 0),
                      br = buffer_of(p.pre, p.pre ? p.D * 4 : 0);
@@ -202,7 +202,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) r1[i] = __builtin_fmaf(x[i][e], x[i][e], r1[i]);
             }
-            group_sums<NV>(r1, how, pieces, per_group, wide, slot());
+            group_sums<NV>(r1, of, how, pieces, per_group, wide, slot());
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 r1[i] = __builtin_amdgcn_rsqf(__builtin_fmaf(r1[i], by_width, p.eps));
@@ -311,7 +311,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
                     if (p.dgate) Piece<IO, VEC>::store(reinterpret_cast<IO *>(p.dgate) + row * p.D + c, dz);
                 }
             }
-            if (p.post) group_sums<NV>(dots, how, pieces, per_group, wide, slot());
+            if (p.post) group_sums<NV>(dots, of, how, pieces, per_group, wide, slot());
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (threadIdx.x + i * nt) * VEC;
@@ -442,14 +442,17 @@ template <bool BWD> static hipError_t launch_norm(const NormParams &p, unsigned 
     return launch_norm_vec<float, float, BWD>(p, blocks, st);
 }
 // Workgroups: as many as run at once, 24 wavefronts a compute unit forward and 12 backward (registers), each going on to further rows with the next
-// one always under way; backward four rows at least, since a workgroup also leaves three rows of sums behind.
+// one always under way; backward four rows at least once every compute unit has one, since a workgroup also leaves three rows of sums behind.
 static int norm_blocks(int64_t M, int waves, int waves_per_cu) {
     const int64_t n = 256 * (waves_per_cu / waves);
     return (int)(M < n ? M : n);
 }
 hipError_t launch_norm_fwd(const NormParams &p, hipStream_t s) { return launch_norm<false>(p, (unsigned)norm_blocks(p.M, norm_shape(p).nt / 64, 24), s); }
-int norm_bwd_blocks(int64_t M, int D) { return norm_blocks((M + 3) / 4, D <= 4096 ? (D + 511) / 512 : 8, 12); }
-hipError_t launch_norm_bwd(const NormParams &p, hipStream_t s) {
+int norm_bwd_blocks(int64_t M, int D) { return norm_blocks(M <= 256 ? M : M <= 1024 ? 256 : (M + 3) / 4, D <= 4096 ? (D + 511) / 512 : 8, 12); }
+hipError_t launch_norm_bwd(NormParams p, hipStream_t s) {
+    const NormShape shape = norm_shape(p);        // fewer than there is room for, where narrow pieces make a row's workgroup larger
+    const int each = shape.nv * shape.vec, waves = shape.nt / 64, room = (each >= 16 ? 8 : each >= 8 || shape.nv >= 4 ? 12 : 20) / waves;
+    if (p.blocks > 256 * (room > 1 ? room : 1)) p.blocks = 256 * (room > 1 ? room : 1);
     hipError_t e = launch_norm<true>(p, (unsigned)p.blocks, s);
     if (e != hipSuccess || (!p.dpost && !p.dscale && !p.dpre)) return e;
     hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((p.D + 15) / 16), 3), dim3(1024), 0, s, p);

@@ -26,7 +26,7 @@ struct NormParams {
 };
 
 hipError_t launch_norm_fwd(const NormParams &p, hipStream_t s);
-hipError_t launch_norm_bwd(const NormParams &p, hipStream_t s);
+hipError_t launch_norm_bwd(NormParams p, hipStream_t s);
 int norm_bwd_blocks(int64_t M, int D);
 
 }  // namespace lrnnx
