@@ -9,8 +9,9 @@ namespace lrnnx {
 constexpr int kDeltaSlot = 64;           // steps between saved states; a slot holds two chunks
 constexpr int kDeltaChunk = 32;          // steps whose corrections are solved for together
 
-// The matrices of a chunk, in 16-bit words: T (2 row tiles x planes x 512), A (likewise), then exp(G), exp(G_end - G), beta (3 x 32 floats).
-constexpr int chunk_words(int np, int npa) { return (2 * np + 2 * npa) * 512 + 192; }
+// The matrices of a chunk, in 16-bit words: T, then A, of planes each two tiles of 16 rows, first the one of whose two 16 x 16 blocks one is zero (the
+// other block alone, 256 a plane), then the whole one (512 a plane); then exp(G), exp(G_end - G), beta (3 x 32 floats).
+constexpr int chunk_words(int np, int npa) { return (np + npa) * 768 + 192; }
 
 // Rows of a matrix operand in bfloat16: element (plane, batch, step, head, column) at plane * plane_stride + b * sb + t * sl + h * sh + column,
 // rows 16-byte aligned and zero beyond the head's width up to the padded one.  A float32 operand is the sum of three planes.

@@ -21,7 +21,7 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
     static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
         uint16_t k[NPI][32][DK + 8], kt[NPI][DK][40], qt[NPI][DK][40];
-        uint16_t t[2][NP][512], a[2][NPA][512];
+        uint16_t th[NP][256], tw[NP][512], ah[NPA][256], aw[NPA][512];         // (as they lie in memory)
         float scal[96];
     } buf[NBUF];
     f32x4 halves[DS == 2 ? 8 : 1][64];
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
                 }
             }
         }
-        uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
+        uint4 *mats = reinterpret_cast<uint4 *>(&B.th[0][0]);
 #pragma unroll
         for (int x = 0; x < IM; ++x)
             if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = st.m[x];
@@ -161,9 +161,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
         for (int m = 0; m < 2; ++m) {
             en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
 #pragma unroll
-            for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[m][i][lane * 8]);
+            for (int i = 0; i < NPA; ++i) af[m][i] = m ? half_tile<true>(B.ah[i], lane) : whole_tile(B.aw[i], lane);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) tf[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+            for (int i = 0; i < NP; ++i) tf[m][i] = m ? half_tile<true>(B.th[i], lane) : whole_tile(B.tw[i], lane);
         }
         if constexpr (EARLY) reads_first();
         // dU
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
             for (int m = 0; m < OT; ++m)
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
-                    if constexpr (DS == 2) tt[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[dh][i][lane * 8]);
+                    if constexpr (DS == 2) triangle_tile<true>(dh == 1, B.th[i], B.tw[i], lane, tt[m][i]);
                     else tt[m][i] = tf[m][i];
                 }
         if constexpr (EARLY)

@@ -204,6 +204,25 @@ template <int NP> __device__ __forceinline__ void split_tiles(f32x4 lo, f32x4 hi
         if (i < NP - 1) { lo = mfma(neg.lo, f[i], lo); hi = mfma(neg.hi, f[i], hi); }
     }
 }
+// Tiles of a chunk's triangular matrices as they lie in memory and LDS: UP: of T^T and A^T, whose second tile of rows has no first block; else of T and
+// A, whose first has no second.  `half`: that tile.
+template <bool UP> __device__ __forceinline__ void triangle_tile(bool half, const uint16_t *halves, const uint16_t *wholes, int lane, Frag &f) {
+    const uint16_t *p = half ? halves + 4 * lane : wholes + 8 * lane;
+    const uint2 a = *reinterpret_cast<const uint2 *>(p), b = *reinterpret_cast<const uint2 *>(p + (UP && half ? 0 : 4));
+    f.h[0] = UP && half ? make_uint2(0, 0) : a;
+    f.h[1] = !UP && half ? make_uint2(0, 0) : b;
+}
+template <bool UP> __device__ __forceinline__ Frag half_tile(const uint16_t *halves, int lane) {
+    Frag f;
+    f.h[UP] = *reinterpret_cast<const uint2 *>(halves + 4 * lane);
+    f.h[!UP] = make_uint2(0, 0);
+    return f;
+}
+__device__ __forceinline__ Frag whole_tile(const uint16_t *wholes, int lane) {
+    Frag f;
+    f.v = *reinterpret_cast<const uint4 *>(wholes + 8 * lane);
+    return f;
+}
 // LDS reads before this stay before it (they are wanted early, registers or not)
 __device__ __forceinline__ void reads_first() { asm volatile("" ::: "memory"); }
 

@@ -152,12 +152,15 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
         }
     }
     lds_barrier();
-    auto store = [&](const f32x4 &lo, const f32x4 &hi, int m, auto np, uint16_t *to) {
+    auto store = [&](const f32x4 &lo, const f32x4 &hi, int m, auto np, auto up, uint16_t *to) {       // tile m of an operand (triangle_tile)
         constexpr int P = decltype(np)::value;
+        constexpr bool UP = decltype(up)::value;
         Frag f[P];
         split_tiles<P>(lo, hi, f);
 #pragma unroll
-        for (int i = 0; i < P; ++i) *reinterpret_cast<uint4 *>(to + (m * P + i) * 512 + lane * 8) = f[i].v;
+        for (int i = 0; i < P; ++i)
+            if (m == UP) *reinterpret_cast<uint2 *>(to + i * 256 + lane * 4) = f[i].h[UP];
+            else *reinterpret_cast<uint4 *>(to + (P + 2 * i) * 256 + lane * 8) = f[i].v;
     };
     using ForA = std::integral_constant<int, NPA>;
 #pragma unroll
@@ -191,20 +194,20 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
             }
         }
         const f32x4 none = {};
-        uint16_t *to = p.mats + (mat + c) * MW + 2 * NP * 512;
-        store(A[0], none, 0, ForA(), to);
-        store(A[1], A[2], 1, ForA(), to);
+        uint16_t *to = p.mats + (mat + c) * MW + NP * 768;
+        store(A[0], none, 0, ForA(), std::false_type(), to);
+        store(A[1], A[2], 1, ForA(), std::false_type(), to);
         if constexpr (ADJ > 0) {
-            to = p.mats_adj + (mat + c) * AW + 2 * ADJ * 512;
-            store(At[0], At[1], 0, ForA(), to);
-            store(none, At[2], 1, ForA(), to);
+            to = p.mats_adj + (mat + c) * AW + ADJ * 768;
+            store(At[0], At[1], 0, ForA(), std::true_type(), to);
+            store(none, At[2], 1, ForA(), std::true_type(), to);
         }
     }
     lds_barrier();
 
     // rows of the inverses: lane (c, i) solves for row i of chunk c
     const int c = lane >> 5, own = lane & 31;
-    auto emit = [&](float (&x)[32], float (*N)[32][W], auto np, uint16_t *to, int64_t words) {       // through LDS into the operands' order
+    auto emit = [&](float (&x)[32], float (*N)[32][W], auto np, auto up, uint16_t *to, int64_t words) {       // through LDS into the operands' order
         lds_barrier();
 #pragma unroll
         for (int j = 0; j < 32; j += 4) *reinterpret_cast<f32x4 *>(&N[c][own][j]) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
@@ -214,7 +217,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
 #pragma unroll
             for (int m = 0; m < 2; ++m)
                 store(*reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][4 * g4]), *reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][16 + 4 * g4]),
-                      m, np, to + (mat + cc) * words);
+                      m, np, up, to + (mat + cc) * words);
     };
     {                                                        // X (I + N diag(beta)) = I, from the last column to the first
         float x[32];
@@ -230,7 +233,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
                 for (int e = 0; e < 4; ++e) if (j + e < l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
             }
         }
-        emit(x, Ns[0], std::integral_constant<int, NP>(), p.mats, MW);
+        emit(x, Ns[0], std::integral_constant<int, NP>(), std::false_type(), p.mats, MW);
     }
     if constexpr (ADJ > 0) {                                 // X (I + N^T diag(beta)) = I, from the first column to the last
         float x[32];
@@ -246,7 +249,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
                 for (int e = 0; e < 4; ++e) if (j + e > l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
             }
         }
-        emit(x, Ns[1], std::integral_constant<int, ADJ>(), p.mats_adj, AW);
+        emit(x, Ns[1], std::integral_constant<int, ADJ>(), std::true_type(), p.mats_adj, AW);
     }
 }
 
@@ -259,7 +262,7 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct ScanLds {
     static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
         uint16_t k[NPI][32][DK + 8], q[NPI][32][DK + 8], kt[NPI][DK][40];
-        uint16_t t[2][NP][512], a[2][NPA][512];
+        uint16_t th[NP][256], tw[NP][512], ah[NPA][256], aw[NPA][512];         // (as they lie in memory)
         float scal[96];
     } buf[NBUF];
     f32x4 halves[DS == 2 ? 12 : 1][64];
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 *reinterpret_cast<uint2 *>(&B.q[pl][t][base + quad_place(q0 + 1)]) = make_uint2(st.q[x][pl].z, st.q[x][pl].w);
             }
         }
-        uint4 *mats = reinterpret_cast<uint4 *>(&B.t[0][0][0]);
+        uint4 *mats = reinterpret_cast<uint4 *>(&B.th[0][0]);
 #pragma unroll
         for (int x = 0; x < IM; ++x)
             if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = st.m[x];
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int m = 0; m < 2; ++m) {
             gam[m] = *reinterpret_cast<const f32x4 *>(&B.scal[16 * m + 4 * g4]);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) tf[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[m][i][lane * 8]);
+            for (int i = 0; i < NP; ++i) tf[m][i] = m ? whole_tile(B.tw[i], lane) : half_tile<false>(B.th[i], lane);
         }
         if constexpr (EARLY) reads_first();
         f32x4 P[2] = {}, O[2] = {};
@@ -471,11 +474,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
             for (int m = 0; m < OT; ++m) {
 #pragma unroll
-                for (int i = 0; i < NPA; ++i) af[m][i].v = *reinterpret_cast<const uint4 *>(&B.a[first + m][i][lane * 8]);
+                for (int i = 0; i < NPA; ++i) triangle_tile<false>(first + m == 0, B.ah[i], B.aw[i], lane, af[m][i]);
                 if constexpr (SAVE)
 #pragma unroll
                     for (int i = 0; i < NP; ++i) {
-                        if constexpr (DS == 2) tt[m][i].v = *reinterpret_cast<const uint4 *>(&B.t[dh][i][lane * 8]);
+                        if constexpr (DS == 2) triangle_tile<false>(dh == 0, B.th[i], B.tw[i], lane, tt[m][i]);
                         else tt[m][i] = tf[m][i];
                     }
             }
