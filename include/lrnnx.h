@@ -519,7 +519,8 @@ int lrnnx_lti_step(const lrnnx_lti_step_args *args);
  * lrnnx_gated_delta_saved_bytes(args) bytes, opaque, 16-byte aligned, to be handed to the backward call unchanged together
  * with the same inputs.  workspace: lrnnx_gated_delta_fwd_workspace_bytes(args) bytes, 16-byte aligned.
  * Accumulation, states and gates are float32; products run on matrix units whose factors are bfloat16 numbers or sums of
- * two (results rounded to bfloat16) or three (float32 results) of them.  Results are bitwise reproducible.            */
+ * two (results rounded to bfloat16) or three (float32 results) of them.  A bfloat16 call saves states and corrections
+ * once rounded, to 16-bit floating point with a power of two for every block.  Results are bitwise reproducible.         */
 typedef struct lrnnx_delta_fwd_args {
     size_t struct_size;
     int32_t B, Hk, Hv, dk, dv;
@@ -550,7 +551,7 @@ size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *args);
  * [B,L,Hv] in gate_dtype, ds0 [B,Hv,dk,dv] float (optional), all contiguous ([L,H,...] for a packed batch; rows of steps
  * outside every sequence are not written).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
  * Gradients of g are those of the log decay.  With bfloat16 I/O and float32 gates dg and dbeta are as accurate as
- * products of factors in 16 bits leave them (about 1e-3 of their norm); ds0 is accurate to float32 if s0 was given.   */
+ * what was saved in 11 bits of mantissa leaves them (a few 1e-4 of their norm); ds0 is accurate to float32 if s0 was given. */
 typedef struct lrnnx_delta_bwd_args {
     size_t struct_size;
     int32_t B, Hk, Hv, dk, dv;

@@ -8,6 +8,8 @@
 // (of a norm over one element the difference is dn eps / (x^2 + eps), which is formed so: as a difference nothing of it would be left)
 // and over all rows dpre_weight = sum dy n2, dres_scale = sum dh m, dpost_weight = sum dp act(gate) n: a workgroup adds up the rows it takes in
 // registers and leaves them in the workspace, a second launch adds up the workgroups in a fixed order.
+// 16384 rows of 2560, bfloat16 with the residual stream in float32: forward 503 MB in 84 us, backward 755 MB in 172 and 7 of sums; gated heads, 16 of 128:
+// 201 MB in 41 and 335 in 72 and 6 (a plain copy does 4.9 TB/s).  Few rows: latency, 5.3 us for 16.
 #include "block_norm.hpp"
 #include "delta_common.hpp"
 

@@ -107,8 +107,8 @@ template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
 }
 
 // Segments of the time axis: walked side by side where the heads alone leave the chip part empty, at the price of a walk with dk more columns before and
-// of chaining (4 us a segment).  32768 steps of 8 heads of 128 x 128, bfloat16: 1870 us in one walk, 16 segments 155 + 62 + 150; 4 x 2048 of 16 heads: 134,
-// in two segments 57 + 13 + 81.
+// of chaining (4 us a segment).  32768 steps of 8 heads of 128 x 128, bfloat16: 1640 us in one walk, 16 segments 149 + 62 + 144; 4 x 2048 of 16 heads:
+// 120, in two segments 57 + 13 + 81.
 void plan_segments(const Shape &s, bool packed, Layout &l, DeltaParams &p) {
     p.nseg = 1; p.seg_chunks = 0; p.entry = nullptr; p.trans = nullptr;
     const int64_t heads = (int64_t)s.B * s.Hv, wgs = heads * ((s.dvp + 63) / 64), slots = s.slots_each;

@@ -10,13 +10,14 @@
 //     dbeta_t = z_t . e_t,     dg_t = sum of dG_i over i >= t,
 //     dG_i = sum_j M_ij - sum_j M_ji + q_i . (state part of dQ_i) + k_i . (-.. Z S0^T part) - k_i . (U dS1^T part),   M = F o Q K^T + H o K K^T
 //     and at the slot's last step also the sum of k . (U dS1^T part) and exp(G_C) <S0, dS1>.
-// M is formed once and added to rows and subtracted from columns in float32, so that what cancels in the sums of dG does so exactly.
+// Row and column sums of M are taken in float32, without the diagonal, which cancels.
 #include "delta_common.hpp"
 
 namespace lrnnx {
 
 // ---------------------------------------------------------------- the walk backwards
-// As in the forward walk a wavefront owns 16 columns of dS, and everything it computes of them stays in its registers.
+// As in the forward walk a wavefront owns 16 columns of dS, or two share them, and everything it computes of them stays in its registers.  Bound by the
+// latency of a chunk: 4 x 4096 steps of 16 heads of 128 x 128, bfloat16, 128 chunks in 257 us (351 with one wavefront to 16 columns).
 template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
     static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
@@ -28,7 +29,7 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
 };
 
 // DEEP: loads two chunks ahead, for launches of at most a workgroup a compute unit, where registers are there for it and nothing else hides memory
-// (walk of 4 x 4096 steps, 16 heads of 128 x 128: 385 -> 346 us; the forward walk gains nothing by it).
+// (the same with one wavefront to 16 columns: 385 -> 346 us; the forward walk gains nothing by it, with one or two).
 template <int NPI, int NP, int DK, int DS, bool AGG, bool DEEP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS == 1 || NPI == 3) ? 1 : 2, DEEP && (DS == 1 || NPI == 3) ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
     constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
@@ -305,12 +306,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
 }
 
 // ---------------------------------------------------------------- the gradients of a slot
-// A workgroup takes the 64 steps of a slot and a value head (where value heads share a key head, k_delta_share adds up their parts of dQ and dK); a wavefront owns 16 of the steps, one to a lane of each group
-// of 16, and every product is arranged so that its results lie a step to a lane: gates are a number to a lane, F and H go from one product's
+// A workgroup takes the 64 steps of a slot and a value head (where value heads share a key head, k_delta_share adds up their parts of dQ and dK); a
+// wavefront owns 16 of the steps, one to a lane of each group of 16, and every product is arranged so that its results lie a step to a lane: gates are a number to a lane, F and H go from one product's
 // results into the next one's operand without leaving the lane, and rows of dQ and dK come out four neighbouring elements at a time.  Both
 // orientations of F and H are computed (one as products with the rows of others, one the other way round), which costs less than turning them.
 // The columns of v come through LDS 32 at a time (rows of dO, E, Z and of both states, the next ones under way meanwhile), then K and Q, as rows
-// and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.
+// and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.  Bound by memory: 4 x 4096 steps of 16 heads of
+// 128 x 128, 783 MB in 224 us (3.5 TB/s; a copy would take 158).
 template <int NPI, int DK> struct GradLds {
     static constexpr int ROWS = NPI == 3 ? 0 : 1;
     union {
@@ -390,14 +392,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
     if constexpr (UNITS) {
         // the largest of dO, whose rows are read once more for it
         const Buffer db = buffer_of(dp, (int64_t)(n - 1) * drow + 2 * p.dvp);
-        uint32_t most = 0;
+        uint32_t most = 0x00800080u;
         for (int ks = 0; ks < ksv; ks += 4) {
             uint4 d[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) d[x] = buffer_load16(db, ks + x < ksv ? tr * drow + 64 * (ks + x) + tc : kOutside);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) most = max_halves(max_halves(most, max_halves(d[x].x, d[x].y)), max_halves(d[x].z, d[x].w));
+            for (int x = 0; x < 4; ++x) most = max_finite(max_finite(max_finite(max_finite(most, d[x].x), d[x].y), d[x].z), d[x].w);
         }
+        most -= 0x00800080u;
         most = most << 16 > (most & 0x7fff0000u) ? most << 16 : most & 0x7fff0000u;
         const float whole = wave_max(__uint_as_float(most));
         if (lane == 0) lds.most[wave] = whole;
@@ -684,8 +687,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
                 const float f = o >= own ? ds * bown * (m == wave ? P1own[r] : P1[m][r]) : 0.0f;        // step o reads what this step wrote
                 const float hl = o < own ? db * P2[m][r] : 0.0f, hx = o > own ? db * (m == wave ? P2own[r] : P2[m][r]) : 0.0f;
                 const float hh = hl + hx;
-                dG += ft * QKt[r] + hl * KK[r];
-                dG -= f * QK[r] + hx * KK[r];
+                dG += (o < own ? ft * QKt[r] : 0.0f) + hl * KK[r];            // (a step's own term would be added and taken off again)
+                dG -= (o > own ? f * QK[r] : 0.0f) + hx * KK[r];
                 Ft[m][r] = ft; F[m][r] = f; HH[m][r] = hh;
             }
         }

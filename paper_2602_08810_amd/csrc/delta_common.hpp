@@ -79,7 +79,7 @@ template <int NP> __device__ __forceinline__ void split2(float a, float b, uint3
 }
 // What the backward pass is left of bfloat16 operands' states, errors and gradients: 16-bit floating point with a common power of two a block, 11 bits of
 // mantissa (what the results are rounded to has 8) for numbers down to 2^-29 of the block's largest, which the power brings to 2^14 .. 2^15.
-// The power's inverse, from the largest magnitude (an infinity leaves its block only infinities and zeros):
+// What is not finite stays so and has no part in it.  The power's inverse, from the largest magnitude:
 __device__ __forceinline__ float block_unit(float largest) {
     const uint32_t e = __float_as_uint(largest) >> 23;
     return __uint_as_float(((e > 15 ? e : 15) - 14) << 23);
@@ -90,15 +90,20 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
 }
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {          // magnitudes of bfloat16 pairs
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7fff7fffu), __builtin_bit_cast(u16x2, b & 0x7fff7fffu)));
+// The larger magnitudes of bfloat16 pairs, as bits plus 0x80, by which what is not finite comes out smallest.
+__device__ __forceinline__ uint32_t max_finite(uint32_t most, uint32_t pair) {
+    const uint32_t x = ((pair & 0x7fff7fffu) + 0x00800080u) & 0x7fff7fffu;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, x)));
 }
-template <int N> __device__ __forceinline__ float largest_of(const f32x4 (&x)[N]) {
+template <int N, bool FINITE = false> __device__ __forceinline__ float largest_of(const f32x4 (&x)[N]) {
     float m[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) m[i & 1] = fmaxf(m[i & 1], fabsf(x[i][r]));
+        for (int r = 0; r < 4; ++r) {
+            const float v = fabsf(x[i][r]);
+            m[i & 1] = fmaxf(m[i & 1], FINITE && v == INFINITY ? 0.0f : v);
+        }
     return fmaxf(m[0], m[1]);
 }
 template <int CTRL, int ROW_MASK = 0xF> __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
@@ -115,11 +120,17 @@ __device__ __forceinline__ float wave_max(float m) {          // of numbers that
     x = dpp_max<0x143, 0xC>(x);
     return __uint_as_float(__builtin_amdgcn_readlane(x, 63));
 }
+// the unit of a wavefront's numbers, by the largest that is finite
+template <int N> __device__ __forceinline__ float unit_of(const f32x4 (&x)[N]) {
+    float m = wave_max(largest_of(x));
+    if (m == INFINITY) m = wave_max(largest_of<N, true>(x));
+    return block_unit(m);
+}
 // MT tiles of a state's 16 columns as they are saved, a column to a row of DK: planes, or 16 bits with their unit (a unit each half of the rows)
 template <int NPS, int DK, int MT> __device__ __forceinline__ void save_state(const f32x4 (&S)[MT], uint16_t *to, int64_t plane, float *unit, int G) {
     float inv = 0.0f;
     if constexpr (NPS == 1) {
-        const float u = block_unit(wave_max(largest_of(S)));
+        const float u = unit_of(S);
         inv = inverse_unit(u);
         if ((threadIdx.x & 63) == 0) {
             *unit = u;
@@ -146,7 +157,7 @@ template <int NPE, int N> __device__ __forceinline__ void save_rows(const f32x4 
     const int row16 = threadIdx.x & 15;
     float inv = 0.0f;
     if constexpr (NPE == 1) {
-        const float u = block_unit(wave_max(largest_of(X)));
+        const float u = unit_of(X);
         inv = inverse_unit(u);
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -304,7 +315,8 @@ __device__ __forceinline__ bool delta_unit(const DeltaParams &p, unsigned segs, 
 }
 
 inline unsigned delta_blocks(const DeltaParams &p, int segs) { return (unsigned)(((int64_t)p.B * p.Hv * segs + 7) / 8 * 8 * p.groups); }
-// Two wavefronts to 16 columns: where one each would leave half of the compute units without a workgroup, or half of a workgroup without columns.
+// Two wavefronts to 16 columns: where one each would leave half of the compute units without a workgroup, or half of a workgroup without columns.  At 128
+// workgroups of one each the walk forward takes 120 us for 133, backward 260 for 351; at 256 the 512 of two each would come in two rounds.
 inline bool delta_rows_split(const DeltaParams &p) { return p.dvp <= 32 || (int64_t)p.B * p.Hv * p.nseg * ((p.dvp + 63) / 64) <= 128; }
 // A wavefront's 16 columns (this lane's: j) of a segment's transition, as planes [dk][dk].
 template <int NP, int DK> __device__ __forceinline__ void store_trans(const f32x4 (&S)[DK / 16], uint16_t *to, int j, int g4) {

@@ -12,7 +12,7 @@ namespace lrnnx {
 
 // ---------------------------------------------------------------- operands in planes
 // A float32 operand, or rows that are not as the matrix kernels read them (width not padded, unaligned), as planes of aligned rows: one launch for
-// all operands of a call, eight elements a thread.
+// all operands of a call, eight elements a thread (q, k and the gradient of 3 x 531 steps of 6 heads in float32: 6 us, a latency).
 template <class IO> __global__ __launch_bounds__(256) void k_delta_pack(const DeltaPacks all) {
     const DeltaPack &p = all.p[blockIdx.z];
     const unsigned sub = p.rows > 1 ? p.by_items(threadIdx.x) : 0, first = threadIdx.x - sub * p.items;
@@ -84,6 +84,8 @@ hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s) {
 // which their tiles are operands as they come (A: a step to a lane, its terms in the lane), for the adjoint in the other one too; only N goes through
 // LDS, for the solve: a row of the inverse to a lane, both chunks side by side, each element found and at once taken off the ones before it (496
 // multiply-adds a lane that do not wait for each other).  Substitution is stable where powers of N would cancel.
+// Bound by latency and what it writes: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 20 at the rate of a copy; 4 x 4096 with the
+// adjoint's matrices 71 us where 241 MB are 49.
 template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) void k_delta_prep(const DeltaParams p) {
     constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, NPA);
     __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][2][32][W];        // N by rows; by columns
@@ -268,9 +270,10 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct ScanLds {
     f32x4 halves[DS == 2 ? 12 : 1][64];
 };
 
-//
+// Bound by the latency of a chunk's chain of products and of the rows it brings: 4 x 2048 steps of 16 heads of 128 x 128, bfloat16 with the last state in
+// float32, 64 chunks in 120 us; 4 x 4096 with what the backward pass is left, 269 us where 540 MB are 110 at the rate of a copy.
 // DS = 2: two wavefronts share 16 columns, each with half of the rows of S: half of the products and registers each, for one exchange through LDS (the
-// halves of K S0 and Q S0 are added) and twice the workgroups, which pays where heads are few.
+// halves of K S0 and Q S0 are added) and twice the workgroups (the two cases above with one wavefront: 133 and 340 us).
 // AGG: what a segment makes of the state that enters it, S -> M S + N, without outputs: N is the walk from a state of zero, and the columns of M, behind those
 // of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
 template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG>
@@ -592,7 +595,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // ---------------------------------------------------------------- chaining segments
 // entry[s + 1] <- M_s entry[s] + N_s in the order of time (N_s lies in entry[s + 1]; entry[0] is s0), for the adjoint entry[s - 1] <- M_s entry[s] + N_s
 // against it.  A workgroup takes 32 columns, a wavefront 16 rows of them: its rows of M and of N are under way two segments ahead, and only the state
-// itself, in planes through LDS, is waited for (21 us a segment with a wavefront for all rows of 16 columns, 1.5 so).
+// itself, in planes through LDS, is waited for (21 us a segment with a wavefront for all rows of 16 columns, 4 so: what a compute unit reads of M).
 template <int NP, int DK, bool ADJ> __global__ __launch_bounds__(DK * 4) void k_delta_join(const DeltaParams p) {
     constexpr int KS = DK / 32;
     __shared__ __align__(16) uint16_t st[2][NP][32][DK + 8];
