@@ -80,46 +80,48 @@ hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------- the matrices of a chunk
-// One wavefront takes a slot (two chunks) of one value head, rows read straight from memory.  Products K K^T and Q K^T are taken in the orientation in
-// which their tiles are operands as they come (A: a step to a lane, its terms in the lane), for the adjoint in the other one too; only N goes through
-// LDS, for the solve: a row of the inverse to a lane, both chunks side by side, each element found and at once taken off the ones before it (496
-// multiply-adds a lane that do not wait for each other).  Substitution is stable where powers of N would cancel.
-// Bound by latency and what it writes: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 20 at the rate of a copy; 4 x 4096 with the
-// adjoint's matrices 71 us where 241 MB are 49.
-template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) void k_delta_prep(const DeltaParams p) {
+// One wavefront takes a chunk of one value head, rows read straight from memory.  Products K K^T and Q K^T are taken in the orientation in which their
+// tiles are operands as they come (A: a step to a lane, its terms in the lane), for the adjoint in the other one too; only N goes through LDS, for the
+// solve: a row of the inverse to a lane, each element found and at once taken off the ones before it (496 multiply-adds a lane that do not wait for each
+// other).  Substitution is stable where powers of N would cancel.  The upper 32 lanes solve for the adjoint's inverse, which is the same with the steps
+// counted from the chunk's end.
+// Bound by what it reads and writes, few chunks by latency: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 20 at the rate of a copy;
+// 4 x 4096 with the adjoint's matrices 61 us of 49 (71 with a wavefront for two chunks); 2 x 77 steps of 6 heads, float32, 9 (11).
+template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NPI == 3 ? 2 : 4))) void k_delta_prep(const DeltaParams p) {
     constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, NPA);
-    __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][2][32][W];        // N by rows; by columns
-    __shared__ double Gs[64];
-    __shared__ __align__(16) float Bs[64];
-    const int64_t slot = blockIdx.x / (unsigned)p.Hv;
-    const int h = (int)(blockIdx.x - slot * p.Hv), hk = h / (p.Hv / p.Hk);
-    const int lane = threadIdx.x, row16 = lane & 15, g4 = lane >> 4;
+    __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][32][W];           // N by rows; by columns, both counted from the end
+    __shared__ double Gs[32];
+    __shared__ __align__(16) float Bs[32];
+    const int c = blockIdx.x & 1;
+    const int64_t unit = blockIdx.x >> 1, slot = unit / (unsigned)p.Hv;
+    const int h = (int)(unit - slot * p.Hv), hk = h / (p.Hv / p.Hk);
+    const int lane = threadIdx.x, row16 = lane & 15, g4 = lane >> 4, own = lane & 31;
+    const bool up = lane >= 32;
     DeltaSeq sq;
     int64_t t0;
     int b;
-    const int n = delta_slot(p, slot, sq, t0, b);
-    if (n == 0) return;
-    const int64_t at = sq.at + t0, mat = (slot * p.Hv + h) * 2;
+    const int n = delta_slot(p, slot, sq, t0, b) - 32 * c;   // steps from the chunk's first on
+    if (n <= 0) return;
+    const int64_t at = sq.at + t0 + 32 * c, mat = unit * 2 + c;
     const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2;
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
-    const bool in = lane < n;
-    const int64_t tg = at + (in ? lane : 0);
+    const bool in = own < n;
+    const int64_t tg = at + (in ? own : 0), last = (n < 32 ? n : 32) - 1;
     const float gr = load_gate(p.g, sq.ib * p.g_sb + tg * p.g_sl + h * p.g_sh, p.io, p.gate_io);
     const float be = load_gate(p.beta, sq.ib * p.be_sb + tg * p.be_sl + h * p.be_sh, p.io, p.gate_io);
 
-    // tiles of K K^T and Q K^T of each chunk: [step written j][step reading i], and [i][j] for the adjoint
-    f32x4 kk[2][3] = {}, qk[2][3] = {}, qa[2][3] = {}, ka[2] = {};
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    // tiles of K K^T and Q K^T: [step written j][step reading i], and [i][j] for the adjoint
+    f32x4 kk[3] = {}, qk[3] = {}, qa[3] = {}, ka = {};
+    {
         Frag K[KS][2][NPI], Q[KS][2][NPI];
 #pragma unroll
         for (int i = 0; i < NPI; ++i) {
-            const Buffer kb = buffer_of(kp + i * p.k.plane, (int64_t)(n - 1) * krow + 2 * DK), qb = buffer_of(qp + i * p.q.plane, (int64_t)(n - 1) * qrow + 2 * DK);
+            const Buffer kb = buffer_of(kp + i * p.k.plane, last * krow + 2 * DK), qb = buffer_of(qp + i * p.q.plane, last * qrow + 2 * DK);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    const uint32_t t = 32 * c + 16 * m + row16;
+                    const uint32_t t = 16 * m + row16;
                     K[ks][m][i].v = buffer_load16(kb, t * krow + 64 * ks + 16 * g4);
                     Q[ks][m][i].v = buffer_load16(qb, t * qrow + 64 * ks + 16 * g4);
                 }
@@ -128,35 +130,36 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
             for (int x = 0; x < 3; ++x) {                     // (0,0), (0,1), (1,1)
-                kk[c][x] = mm(K[ks][x > 1], K[ks][x > 0], kk[c][x]);
-                qk[c][x] = mm(K[ks][x > 1], Q[ks][x > 0], qk[c][x]);
-                if (ADJ > 0) qa[c][x] = mm(Q[ks][x > 0], K[ks][x > 1], qa[c][x]);
+                kk[x] = mm(K[ks][x > 1], K[ks][x > 0], kk[x]);
+                qk[x] = mm(K[ks][x > 1], Q[ks][x > 0], qk[x]);
+                if (ADJ > 0) qa[x] = mm(Q[ks][x > 0], K[ks][x > 1], qa[x]);
             }
-            if (ADJ > 0) ka[c] = mm(K[ks][1], K[ks][0], ka[c]);   // (the tiles on the diagonal are their own transposes)
+            if (ADJ > 0) ka = mm(K[ks][1], K[ks][0], ka);     // (the tiles on the diagonal are their own transposes)
         }
     }
-    // running sums of the log decays over each chunk
+    // running sums of the log decays, the same in both halves of the wavefront
     {
         double G = in ? gate_log(gr) : 0.0;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
             const double o = __shfl_up(G, m, 32);
-            if ((lane & 31) >= m) G += o;
+            if (own >= m) G += o;
         }
         const double end = __shfl(G, 31, 32);
         const float bv = in ? be : 0.0f, eg = __expf((float)G), ee = __expf((float)(end - G));
-        Gs[lane] = G; Bs[lane] = bv;
-        float *sc = reinterpret_cast<float *>(p.mats + (mat + (lane >> 5) + 1) * MW - 192) + (lane & 31);
-        sc[0] = eg; sc[32] = ee; sc[64] = bv;
-        if constexpr (ADJ > 0) {
-            sc = reinterpret_cast<float *>(p.mats_adj + (mat + (lane >> 5) + 1) * AW - 192) + (lane & 31);
+        if (!up) {
+            Gs[own] = G; Bs[own] = bv;
+            float *sc = reinterpret_cast<float *>(p.mats + (mat + 1) * MW - 192) + own;
+            sc[0] = eg; sc[32] = ee; sc[64] = bv;
+        } else if constexpr (ADJ > 0) {
+            float *sc = reinterpret_cast<float *>(p.mats_adj + (mat + 1) * AW - 192) + own;
             sc[0] = eg; sc[32] = ee; sc[64] = bv;
         }
     }
     lds_barrier();
-    auto store = [&](const f32x4 &lo, const f32x4 &hi, int m, auto np, auto up, uint16_t *to) {       // tile m of an operand (triangle_tile)
+    auto store = [&](const f32x4 &lo, const f32x4 &hi, int m, auto np, auto upper, uint16_t *to) {       // tile m of an operand (triangle_tile)
         constexpr int P = decltype(np)::value;
-        constexpr bool UP = decltype(up)::value;
+        constexpr bool UP = decltype(upper)::value;
         Frag f[P];
         split_tiles<P>(lo, hi, f);
 #pragma unroll
@@ -165,93 +168,78 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) voi
             else *reinterpret_cast<uint4 *>(to + (P + 2 * i) * 256 + lane * 8) = f[i].v;
     };
     using ForA = std::integral_constant<int, NPA>;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    {
         f32x4 A[3], At[3];
 #pragma unroll
         for (int x = 0; x < 3; ++x) {
             {                                                // a reading step to a lane
                 const int i = 16 * (x > 0) + row16, j0 = 16 * (x > 1) + 4 * g4;
-                const double Gi = Gs[32 * c + i];
+                const double Gi = Gs[i];
                 f32x4 N;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float d = j0 + r <= i ? __expf((float)(Gi - Gs[32 * c + j0 + r])) : 0.0f;
-                    N[r] = j0 + r < i ? d * kk[c][x][r] : 0.0f;
-                    A[x][r] = j0 + r <= i ? p.scale * d * qk[c][x][r] : 0.0f;
+                    const float d = j0 + r <= i ? __expf((float)(Gi - Gs[j0 + r])) : 0.0f;
+                    N[r] = j0 + r < i ? d * kk[x][r] : 0.0f;
+                    A[x][r] = j0 + r <= i ? p.scale * d * qk[x][r] : 0.0f;
                 }
-                *reinterpret_cast<f32x4 *>(&Ns[0][c][i][j0]) = N;
+                *reinterpret_cast<f32x4 *>(&Ns[0][i][j0]) = N;
             }
             if constexpr (ADJ > 0) {                         // a written step to a lane
                 const int j = 16 * (x > 1) + row16, i0 = 16 * (x > 0) + 4 * g4;
-                const double Gj = Gs[32 * c + j];
+                const double Gj = Gs[j];
                 f32x4 N;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float d = j <= i0 + r ? __expf((float)(Gs[32 * c + i0 + r] - Gj)) : 0.0f;
-                    N[r] = j < i0 + r ? d * (x == 1 ? ka[c][r] : kk[c][x][r]) : 0.0f;
-                    At[x][r] = j <= i0 + r ? p.scale * d * qa[c][x][r] : 0.0f;
+                    const float d = j <= i0 + r ? __expf((float)(Gs[i0 + r] - Gj)) : 0.0f;
+                    N[3 - r] = j < i0 + r ? d * (x == 1 ? ka[r] : kk[x][r]) : 0.0f;
+                    At[x][r] = j <= i0 + r ? p.scale * d * qa[x][r] : 0.0f;
                 }
-                *reinterpret_cast<f32x4 *>(&Ns[1][c][j][i0]) = N;
+                *reinterpret_cast<f32x4 *>(&Ns[1][31 - j][28 - i0]) = N;
             }
         }
         const f32x4 none = {};
-        uint16_t *to = p.mats + (mat + c) * MW + NP * 768;
+        uint16_t *to = p.mats + mat * MW + NP * 768;
         store(A[0], none, 0, ForA(), std::false_type(), to);
         store(A[1], A[2], 1, ForA(), std::false_type(), to);
         if constexpr (ADJ > 0) {
-            to = p.mats_adj + (mat + c) * AW + ADJ * 768;
+            to = p.mats_adj + mat * AW + ADJ * 768;
             store(At[0], At[1], 0, ForA(), std::true_type(), to);
             store(none, At[2], 1, ForA(), std::true_type(), to);
         }
     }
     lds_barrier();
 
-    // rows of the inverses: lane (c, i) solves for row i of chunk c
-    const int c = lane >> 5, own = lane & 31;
-    auto emit = [&](float (&x)[32], float (*N)[32][W], auto np, auto up, uint16_t *to, int64_t words) {       // through LDS into the operands' order
-        lds_barrier();
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) *reinterpret_cast<f32x4 *>(&N[c][own][j]) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
-        lds_barrier();
-#pragma unroll
-        for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-                store(*reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][4 * g4]), *reinterpret_cast<const f32x4 *>(&N[cc][16 * m + row16][16 + 4 * g4]),
-                      m, np, up, to + (mat + cc) * words);
-    };
-    {                                                        // X (I + N diag(beta)) = I, from the last column to the first
+    // X (I + N diag(beta)) = I, from the last column to the first; row `own`, of the adjoint counted from the end
+    const int from = ADJ > 0 && up ? 32 * W : 0;
+    const float *N = &Ns[0][0][0] + from;
+    {
         float x[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = 0.0f;            // the sums over later columns first, then the element
 #pragma unroll
         for (int l = 31; l >= 0; --l) {
-            x[l] = (l == own ? 1.0f : 0.0f) - Bs[32 * c + l] * x[l];
+            x[l] = (l == own ? 1.0f : 0.0f) - Bs[ADJ > 0 && up ? 31 - l : l] * x[l];
 #pragma unroll
             for (int j = 0; j < l; j += 4) {
-                const f32x4 N = *reinterpret_cast<const f32x4 *>(&Ns[0][c][l][j]);
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(N + l * W + j);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) if (j + e < l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
+                for (int e = 0; e < 4; ++e) if (j + e < l) x[j + e] = __builtin_fmaf(x[l], v[e], x[j + e]);
             }
         }
-        emit(x, Ns[0], std::integral_constant<int, NP>(), std::false_type(), p.mats, MW);
+        lds_barrier();                                       // through LDS into the operands' order
+        float *row = &Ns[0][0][0] + (ADJ > 0 && up ? (32 + 31 - own) * W : own * W);
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const f32x4 v = {x[j], x[j + 1], x[j + 2], x[j + 3]};
+            *reinterpret_cast<f32x4 *>(row + (ADJ > 0 && up ? 28 - j : j)) = ADJ > 0 && up ? f32x4{v[3], v[2], v[1], v[0]} : v;
+        }
     }
-    if constexpr (ADJ > 0) {                                 // X (I + N^T diag(beta)) = I, from the first column to the last
-        float x[32];
+    lds_barrier();
+    auto half = [&](int which, int m, int k) { return *reinterpret_cast<const f32x4 *>(&Ns[which][16 * m + row16][16 * k + 4 * g4]); };
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] = 0.0f;
-#pragma unroll
-        for (int l = 0; l < 32; ++l) {
-            x[l] = (l == own ? 1.0f : 0.0f) - Bs[32 * c + l] * x[l];
-#pragma unroll
-            for (int j = (l + 1) & ~3; j < 32; j += 4) {
-                const f32x4 N = *reinterpret_cast<const f32x4 *>(&Ns[1][c][l][j]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) if (j + e > l) x[j + e] = __builtin_fmaf(x[l], N[e], x[j + e]);
-            }
-        }
-        emit(x, Ns[1], std::integral_constant<int, ADJ>(), std::true_type(), p.mats_adj, AW);
+    for (int m = 0; m < 2; ++m) {
+        store(half(0, m, 0), half(0, m, 1), m, std::integral_constant<int, NP>(), std::false_type(), p.mats + mat * MW);
+        if constexpr (ADJ > 0) store(half(1, m, 0), half(1, m, 1), m, std::integral_constant<int, ADJ>(), std::true_type(), p.mats_adj + mat * AW);
     }
 }
 
@@ -676,7 +664,7 @@ hipError_t launch_delta_join(const DeltaParams &p, bool adjoint, hipStream_t s) 
 
 // ---------------------------------------------------------------- launches
 template <int NPI, int NP, int ADJ> static hipError_t launch_prep(const DeltaParams &p, hipStream_t s) {
-    const dim3 grid((unsigned)(p.nslots * p.Hv)), block(64);
+    const dim3 grid((unsigned)(2 * p.nslots * p.Hv)), block(64);
     if (p.dk > 64) hipLaunchKernelGGL((k_delta_prep<NPI, NP, 128, ADJ>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((k_delta_prep<NPI, NP, 64, ADJ>), grid, block, 0, s, p);
     return hipGetLastError();
