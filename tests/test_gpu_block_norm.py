@@ -180,3 +180,12 @@ def test_refusals(api):
     with pytest.raises(api.LrnnxError) as e:
         api.lrnnx_block_norm_bwd(dh=dh, dy=dy, **a, workspace=torch.empty(32, dtype=torch.uint8, device="cuda"))
     assert e.value.code == 3
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("M,D,groups", [(3, 2731, 1), (600, 4097, 1), (2, 5001, 1), (700, 6145, 5), (300, 8190, 3), (520, 8191, 1), (1100, 288, 32),
+                                        (600, 1568, 32), (257, 1026, 2)])
+def test_widths_that_nothing_divides(api, io, M, D, groups):
+    """Rows that are read an element at a time, several rows a workgroup, and groups that are neither the row nor a power of two of its pieces."""
+    a, dh, dy = _make(M + D, M, D, io, groups=groups, gate="sigmoid")
+    _both(api, a, dh, dy)
