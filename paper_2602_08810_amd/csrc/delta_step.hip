@@ -1,7 +1,7 @@
 // Gated delta rule, one step of a carried state S [dk,dv] of every batch entry and head, in place:
 //     u = beta (v - exp(g) S^T k),   S <- exp(g) S + k u^T,   o = scale S^T q = scale (exp(g) S^T q + (k . q) u)
 // Both products with the old state are taken in one pass, so the state is read once and written once from registers: the bytes of the state are
-// what a call costs (4096 states of 128 x 128: 540 MB in 112 us, 97 % of the rate of a copy), and with few states the latency of one pass (16: 3.5 us).
+// what a call costs (4096 states of 128 x 128: 540 MB in 112 us, 97 % of the rate of a copy), and with few states the latency of one pass (16: 4.4 us).
 // A workgroup takes 32 columns of one state: 8 threads of four columns each side by side, 32 threads along the rows.
 #include "delta_common.hpp"
 
