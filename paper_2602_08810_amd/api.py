@@ -1207,10 +1207,12 @@ def lrnnx_block_norm_fwd(x, post_weight=None, groups=1, gate=None, gate_act="sil
 
     x, gate [..., D]; post_weight [D] or [D // groups] (one for all groups), res_scale, pre_weight [D] float32; residual
     [..., D] float32 or the I/O type, which is h's type too (x's without a residual).  y is None without pre_weight.  `out`
-    takes h (it may be the residual)."""
+    takes h: contiguous, in the residual's type if there is one (it may be the residual)."""
     res_dtype = residual.dtype if residual is not None else out.dtype if out is not None else x.dtype
     head = _norm_head(x, post_weight, groups, gate, gate_act, residual, res_scale, pre_weight, eps, _NORM_FWD_SIZE, res_dtype)
     h = torch.empty(x.shape, dtype=res_dtype, device=x.device) if out is None else out
+    if h.dtype != res_dtype:
+        raise TypeError(f"out: dtype {h.dtype}, expected {res_dtype}")
     if h.shape != x.shape or not h.is_contiguous():
         raise ValueError(f"out: expected a contiguous tensor of shape {tuple(x.shape)}")
     y = None if pre_weight is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
