@@ -2,6 +2,8 @@
 //     n = x / rms(x), group by group;   m = post_weight n act(gate);   h = residual + res_scale m;   y = pre_weight h / rms(h)
 // every part but x optional.  A row stays in the registers of a workgroup from the first load to the last store: one read of every input, one
 // write of every output, which is what bounds it.  Sums of squares are taken in float32 over lanes and wavefronts.
+// Lanes past the end of the row bring zeros into its sums: their groups' sum is taken as 1 (with eps = 0 their norm would be 0 / 0), their weights are
+// zeros behind the row's own in LDS.
 // Backward, with everything of the forward pass formed again from its inputs (which the gradients need anyway; nothing is saved):
 //     dn2 = dy pre_weight;  dh += (dn2 - n2 mean(dn2 n2)) / rms(h);   dresidual = dh;   dp = dh res_scale;   dgate = dp n post_weight act'(gate)
 //     dn1 = dp act(gate) post_weight;   dx = (dn1 - n mean(dn1 n)) / rms(x)
@@ -66,11 +68,13 @@ __device__ __forceinline__ float block_sum(float x, float *part) {
     return ((a[0] + a[1]) + (a[2] + a[3])) + ((b[0] + b[1]) + (b[2] + b[3]));
 }
 constexpr int kSumSlots = 8;                      // four sums a row, two rows
+// Floats of LDS for a weight of n elements, whole pieces of it and a piece of zeros.
+__host__ __device__ constexpr int weight_room(int n) { return ((n + 3) & ~3) + 8; }
 
 // How the sum over a group is taken: over the workgroup (one group), over `lanes` neighbouring lanes (a power of two), or through LDS.
 enum : int { GROUP_ROW = 0, GROUP_LANES = 1, GROUP_LDS = 2 };
 
-// Sums over each thread's groups of `x[i]` (piece i of the row lies in one group, `of[i]`), into x.  Through LDS a power of two of neighbouring lanes
+// Sums over each thread's groups of `x[i]` (piece i of the row lies in one group, `of[i]`), into x (1 past the end of the row).  Through LDS a power of two of neighbouring lanes
 // takes a group, as many as the workgroup has for it (32 groups of 49, training, 2442 rows in bfloat16: 94 us with a lane a group, 70 so).
 template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], const int (&of)[NV], int how, int pieces, int per_group, float *lds, float *part) {
     if (how == GROUP_ROW) {
@@ -84,6 +88,8 @@ template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], con
         for (int m = 1; m < per_group; m <<= 1)
 #pragma unroll
             for (int i = 0; i < NV; ++i) x[i] += __shfl_xor(x[i], m, 64);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = (int)(threadIdx.x + i * blockDim.x) < pieces ? x[i] : 1.0f;
     } else {
         const int nt = blockDim.x, groups = pieces / per_group;
 #pragma unroll
@@ -104,7 +110,7 @@ template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], con
         }
         lds_barrier();
 #pragma unroll
-        for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; x[i] = v < pieces ? out[of[i]] : 0.0f; }
+        for (int i = 0; i < NV; ++i) { const int v = threadIdx.x + i * nt; x[i] = v < pieces ? out[of[i]] : 1.0f; }
         lds_barrier();
     }
 }
@@ -141,19 +147,20 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
     extern __shared__ __align__(16) float lds[];
     const int nt = blockDim.x, pieces = p.D / VEC, per_group = p.width / VEC;
     // LDS: slots of sums, the weights (a wait for them from memory would be a wait for the next row too), sums of groups
-    float *const w_post = lds + kSumSlots * 8, *const w_scale = w_post + (p.post ? p.post_shared ? (p.width + 3) & ~3 : (p.D + 3) & ~3 : 0);
-    float *const w_pre = w_scale + (p.scale ? (p.D + 3) & ~3 : 0), *const wide = w_pre + (p.pre ? (p.D + 3) & ~3 : 0);
+    const int n_post = p.post_shared ? p.width : p.D;
+    float *const w_post = lds + kSumSlots * 8, *const w_scale = w_post + (p.post ? weight_room(n_post) : 0);
+    float *const w_pre = w_scale + (p.scale ? weight_room(p.D) : 0), *const wide = w_pre + (p.pre ? weight_room(p.D) : 0);
     int turn = 0;
     auto slot = [&]() { turn = (turn + 1) % kSumSlots; return lds + turn * 8; };
     float w1[BWD ? NV : 1][VEC] = {}, w2[BWD ? NV : 1][VEC] = {}, w3[BWD ? NV : 1][VEC] = {};
     const float by_width = 1.0f / (float)p.width, by_D = 1.0f / (float)p.D;
     int of[NV], cp[NV];                                   // where a piece's part of post_weight starts
 #pragma unroll
-    for (int i = 0; i < NV; ++i) { const int c = (threadIdx.x + i * nt) * VEC; of[i] = how == GROUP_LDS ? c / p.width : 0; cp[i] = c >= p.D ? 0 : p.post_shared ? c % p.width : c; }
+    for (int i = 0; i < NV; ++i) { const int c = (threadIdx.x + i * nt) * VEC; of[i] = how == GROUP_LDS ? c / p.width : 0; cp[i] = c >= p.D ? n_post : p.post_shared ? c % p.width : c; }
     struct Weight { float w[VEC]; __device__ __forceinline__ float get(int e) const { return w[e]; } };
     auto weight = [&](const float *w, int c) {
         Weight r;
-        if (c >= p.D) c = 0;
+        if (c >= p.D) c = p.D;
         if constexpr (VEC == 1) r.w[0] = w[c];
         else
 #pragma unroll
@@ -169,8 +176,13 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
     int64_t row = blockIdx.x;
     even.load(p, row);
     if (threadIdx.x < kSumSlots * 8) lds[threadIdx.x] = 0.0f;
+    if (threadIdx.x < VEC) {
+        if (p.post) w_post[n_post + threadIdx.x] = 0.0f;
+        if (p.scale) w_scale[p.D + threadIdx.x] = 0.0f;
+        if (p.pre) w_pre[p.D + threadIdx.x] = 0.0f;
+    }
     {
-        const Buffer bp = buffer_of(p.post, p.post ? (p.post_shared ? p.width : p.D) * 4 : 0), bs = buffer_of(p.scale, p.scale ? p.D * 4 : 0),
+        const Buffer bp = buffer_of(p.post, p.post ? n_post * 4 : 0), bs = buffer_of(p.scale, p.scale ? p.D * 4 : 0),
                      br = buffer_of(p.pre, p.pre ? p.D * 4 : 0);
         Piece<float, VEC> a[NV], b[NV], c[NV];
 #pragma unroll
@@ -183,7 +195,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
             const int at = (threadIdx.x + i * nt) * VEC;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                if (p.post && at < (p.post_shared ? p.width : p.D)) w_post[at + e] = a[i].get(e);
+                if (p.post && at < n_post) w_post[at + e] = a[i].get(e);
                 if (p.scale && at < p.D) w_scale[at + e] = b[i].get(e);
                 if (p.pre && at < p.D) w_pre[at + e] = c[i].get(e);
             }
@@ -394,7 +406,6 @@ __global__ __launch_bounds__(1024) void k_norm_sums(const NormParams p) {
 }
 
 // Shape of a launch: pieces of 16 bytes of the narrowest tensor where every row allows it, threads so that a thread has few pieces.
-static int up4(int x) { return (x + 3) & ~3; }
 struct NormShape { int vec, nt, nv, how; size_t lds; };
 static bool norm_rows_fit(const NormParams &p, int vec) {
     const int es = p.io ? 2 : 4, rs = p.res_io ? 2 : 4;
@@ -417,8 +428,8 @@ static NormShape norm_shape(const NormParams &p) {
     s.how = p.groups == 1 ? GROUP_ROW : pow2 && per_group <= 64 ? GROUP_LANES : GROUP_LDS;
     size_t wide = s.how == GROUP_LDS && p.post ? (size_t)(pieces + p.groups) : 0;
     if (p.dpost && p.post_shared && wide < (size_t)p.D) wide = (size_t)p.D;
-    const size_t row = (size_t)up4(p.D);
-    s.lds = sizeof(float) * (kSumSlots * 8 + (p.post ? p.post_shared ? (size_t)up4(p.width) : row : 0) + (p.scale ? row : 0) + (p.pre ? row : 0) + wide);
+    const size_t row = (size_t)weight_room(p.D);
+    s.lds = sizeof(float) * (kSumSlots * 8 + (p.post ? p.post_shared ? (size_t)weight_room(p.width) : row : 0) + (p.scale ? row : 0) + (p.pre ? row : 0) + wide);
     return s;
 }
 template <class IO, class RES, int VEC, int NV, bool BWD> static hipError_t launch_norm_one(const NormParams &p, const NormShape &s, unsigned blocks, hipStream_t st) {
