@@ -1,7 +1,7 @@
 // Norms around a block, with its gate and the scale of its residual:
 //     n = x / rms(x), group by group;   m = post_weight n act(gate);   h = residual + res_scale m;   y = pre_weight h / rms(h)
 // every part but x optional.  A row stays in the registers of a workgroup from the first load to the last store: one read of every input, one
-// write of every output, which is what bounds it.  Sums of squares are taken in float32 over lanes and wavefronts.
+// write of every output, which is what bounds it.  Sums of squares are taken in float32 over lanes and wavefronts; roots are taken to 1 ulp, of subnormal means too.
 // Lanes past the end of the row bring zeros into its sums: their groups' sum is taken as 1 (with eps = 0 their norm would be 0 / 0), their weights are
 // zeros behind the row's own in LDS.
 // Backward, with everything of the forward pass formed again from its inputs (which the gradients need anyway; nothing is saved):
@@ -219,7 +219,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
             group_sums<NV>(r1, of, how, pieces, per_group, wide, slot());
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                r1[i] = __builtin_amdgcn_rsqf(__builtin_fmaf(r1[i], by_width, p.eps));
+                r1[i] = rsqrtf(__builtin_fmaf(r1[i], by_width, p.eps));
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) x[i][e] *= r1[i];                  // n
             }
@@ -254,7 +254,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
             for (int e = 0; e < VEC; ++e) { h[i][e] += in.r[i].get(e); ss = __builtin_fmaf(h[i][e], h[i][e], ss); }
         }
         float r2 = 0.0f;
-        if (p.pre) r2 = __builtin_amdgcn_rsqf(__builtin_fmaf(block_sum(ss, slot()), by_D, p.eps));
+        if (p.pre) r2 = rsqrtf(__builtin_fmaf(block_sum(ss, slot()), by_D, p.eps));
         if constexpr (!BWD) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {

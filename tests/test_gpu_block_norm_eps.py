@@ -30,6 +30,17 @@ def test_eps(api, io, eps, M, D, groups):  # noqa: F811
             _check(r[n], want[n], n)
 
 
+@pytest.mark.parametrize("scale", [1e-18, 1e-20])
+def test_tiny_rows_without_eps(api, scale):  # noqa: F811
+    """Means of squares of 1e-36, and of 1e-40, which is subnormal (8 bits are left of it: 4e-3 of the norm)."""
+    import torch
+    x = torch.randn(4, 96, generator=torch.Generator().manual_seed(1)).cuda()
+    _, want = api.lrnnx_block_norm_fwd(x, pre_weight=torch.ones(96, device="cuda"), eps=0.0)
+    h, y = api.lrnnx_block_norm_fwd(x * scale, pre_weight=torch.ones(96, device="cuda"), eps=0.0)
+    assert bool(torch.isfinite(y).all())
+    assert np.linalg.norm(_h(y) - _h(want)) <= (5e-6 if scale > 1e-19 else 4e-3) * np.linalg.norm(_h(want))
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("M,D,groups", SHAPES)
 @pytest.mark.parametrize("which", ["post_weight", "res_scale"])
