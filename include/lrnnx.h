@@ -517,7 +517,7 @@ int lrnnx_lti_step(const lrnnx_lti_step_args *args);
  * of a sequence without steps is its first.
  * saved (optional): what lrnnx_gated_delta_bwd needs from this call (states every 64 steps, corrections e, solved matrices),
  * lrnnx_gated_delta_saved_bytes(args) bytes, opaque, 16-byte aligned, to be handed to the backward call unchanged together
- * with the same inputs.  workspace: lrnnx_gated_delta_fwd_workspace_bytes(args) bytes, 16-byte aligned.
+ * with the same inputs and with that very size (saved_bytes there; what another call left is refused where its size differs).  workspace: lrnnx_gated_delta_fwd_workspace_bytes(args) bytes, 16-byte aligned.
  * Accumulation, states and gates are float32; products run on matrix units whose factors are bfloat16 numbers or sums of
  * two (results rounded to bfloat16) or three (float32 results) of them.  A bfloat16 call saves states and corrections
  * once rounded, to 16-bit floating point with a power of two for every block.  Results are bitwise reproducible.         */

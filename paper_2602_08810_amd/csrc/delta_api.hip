@@ -229,7 +229,7 @@ int lrnnx_gated_delta_bwd(const lrnnx_delta_bwd_args *a) {
         return LRNNX_ERR_INVALID_ARG;
     const Shape s = shape_of(a);
     DeltaBwdPlan f = plan_bwd(a, s, reinterpret_cast<char *>(a->workspace), reinterpret_cast<char *>(const_cast<void *>(a->saved)));
-    if (!a->workspace || a->workspace_bytes < f.bytes || a->saved_bytes < f.saved) return LRNNX_ERR_WORKSPACE;
+    if (!a->workspace || a->workspace_bytes < f.bytes || a->saved_bytes != f.saved) return LRNNX_ERR_WORKSPACE;      // (its layout goes by its size)
     DeltaParams &p = f.p;
     p.ds_last = a->ds_last; p.ds0 = a->ds0;
     auto on4 = [&](const void *q) { return (reinterpret_cast<uintptr_t>(q) & (4 * es - 1)) == 0; };
