@@ -519,8 +519,10 @@ int lrnnx_lti_step(const lrnnx_lti_step_args *args);
  * lrnnx_gated_delta_saved_bytes(args) bytes, opaque, 16-byte aligned, to be handed to the backward call unchanged together
  * with the same inputs and with that very size (saved_bytes there; what another call left is refused where its size differs).  workspace: lrnnx_gated_delta_fwd_workspace_bytes(args) bytes, 16-byte aligned.
  * Accumulation, states and gates are float32; products run on matrix units whose factors are bfloat16 numbers or sums of
- * two (results rounded to bfloat16) or three (float32 results) of them.  A bfloat16 call saves states and corrections
- * once rounded, to 16-bit floating point with a power of two for every block.  Results are bitwise reproducible.         */
+ * two (results rounded to bfloat16) or three (float32 results) of them.  What is saved is float32 with float32 gates, so
+ * that every float32 result is as accurate as that; with bfloat16 I/O and gates it is rounded once, to 16-bit floating point
+ * with a power of two for every block, and its gradients are rounded to bfloat16.  With bfloat16 I/O and gates o may
+ * differ in its last bit with the states that are given or asked for.  Results are bitwise reproducible.                 */
 typedef struct lrnnx_delta_fwd_args {
     size_t struct_size;
     int32_t B, Hk, Hv, dk, dv;
@@ -550,8 +552,8 @@ size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *args);
  * (of s_last): dq, dk [B,L,Hk,dk] (summed over the value heads that share them), dv [B,L,Hv,dv] in io_dtype, dg, dbeta
  * [B,L,Hv] in gate_dtype, ds0 [B,Hv,dk,dv] float (optional), all contiguous ([L,H,...] for a packed batch; rows of steps
  * outside every sequence are not written).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
- * Gradients of g are those of the log decay.  With bfloat16 I/O and float32 gates dg and dbeta are as accurate as
- * what was saved in 11 bits of mantissa leaves them (a few 1e-4 of their norm); ds0 is accurate to float32 if s0 was given. */
+ * Gradients of g are those of the log decay.  Float32 gradients are accurate to some 1e-7 of their norm, whatever the I/O
+ * type; but ds0 of a call without s0, with bfloat16 I/O and gates, to 5e-6.                                              */
 typedef struct lrnnx_delta_bwd_args {
     size_t struct_size;
     int32_t B, Hk, Hv, dk, dv;

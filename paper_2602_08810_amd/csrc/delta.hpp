@@ -9,7 +9,7 @@ namespace lrnnx {
 constexpr int kDeltaSlot = 64;           // steps between saved states; a slot holds two chunks
 constexpr int kDeltaChunk = 32;          // steps whose corrections are solved for together
 
-// The matrices of a chunk, in 16-bit words: T, then A, of planes each two tiles of 16 rows, first the one of whose two 16 x 16 blocks one is zero (the
+// The matrices of a chunk, in 16-bit words: T, then A, of np and npa planes (the adjoint's of the same number), of planes each two tiles of 16 rows, first the one of whose two 16 x 16 blocks one is zero (the
 // other block alone, 256 a plane), then the whole one (512 a plane); then exp(G), exp(G_end - G), beta (3 x 32 floats).
 constexpr int chunk_words(int np, int npa) { return (np + npa) * 768 + 192; }
 
@@ -36,12 +36,13 @@ struct DeltaParams {
     float *s_last;
     uint16_t *mats;                      // per slot, head and chunk: (I + N beta)^-1 and A as matrix operands, and the gates (chunk_words)
     uint16_t *mats_adj;                  // the same for the adjoint: ((I + beta N)^-1)^T and A^T; null: not wanted
-    uint16_t *states, *err;              // saved for the backward pass; null: not wanted
-    float *units;                        // and with bfloat16 I/O the powers of two of their blocks of 16 columns: S0 (2 halves of its rows by G), E (4 times 16 steps by G) of a slot's head
+    int exact;                           // what is saved is float32; else 16-bit floating point
+    void *states, *err;                  // saved for the backward pass, by slot and head a column to a row [nslots,Hv,dvp,dkp], by step [rows,Hv,dvp]; null: not wanted
+    float *units;                        // and in 16 bits the powers of two of their blocks of 16 columns: S0 (2 halves of its rows by G), E (4 times 16 steps by G) of a slot's head
     // backward
     const float *ds_last;
     float *ds0;
-    uint16_t *dstates, *z;
+    void *dstates, *z;
     float *dunits;                       // likewise S1's (2 G), Z's (4 G)
     void *dq, *dkk, *dvv, *dg, *dbeta;
     float *part;                         // with shared key heads: [2,rows,Hv,dkp] every value head's share of dq and of dk

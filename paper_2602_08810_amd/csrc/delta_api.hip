@@ -15,7 +15,8 @@ inline size_t elem(int dtype) { return dtype == LRNNX_BF16 ? 2 : 4; }
 
 // What the forward and the backward call have in common.
 struct Shape {
-    int B, Hk, Hv, dk, dv, dkp, dvp, bf16, planes;       // planes: bfloat16 numbers that a factor read from memory is the sum of
+    int B, Hk, Hv, dk, dv, dkp, dvp, bf16, planes;       // planes: bfloat16 numbers that an input is the sum of
+    int exact;                                           // a gradient of the gates is float32, and so what it comes from
     int64_t L, rows, nslots, slots_each;
 };
 
@@ -35,13 +36,13 @@ template <class A> Shape shape_of(const A *a) {
     Shape s;
     s.B = a->B; s.Hk = a->Hk; s.Hv = a->Hv; s.dk = a->dk; s.dv = a->dv; s.L = a->L;
     s.dkp = a->dk > 64 ? 128 : 64; s.dvp = (int)up(a->dv, 32);
-    s.bf16 = a->io_dtype == LRNNX_BF16; s.planes = s.bf16 ? 1 : 3;
+    s.bf16 = a->io_dtype == LRNNX_BF16; s.planes = s.bf16 ? 1 : 3; s.exact = a->gate_dtype == LRNNX_F32;
     s.rows = (a->cu_seqlens ? 1 : (int64_t)a->B) * a->L;
     s.slots_each = (a->L + kDeltaSlot - 1) / kDeltaSlot;
     s.nslots = a->cu_seqlens ? a->L / kDeltaSlot + a->B : a->B * s.slots_each;
     return s;
 }
-inline int adjoint_planes(const Shape &s, bool s0) { return !s.bf16 || s0 ? 3 : 2; }
+inline int adjoint_planes(const Shape &s, bool s0) { return s.exact || s0 ? 3 : 2; }
 
 // Rows that do not overlap and of which 32 span less than 2 GB.
 bool rows_near(const Shape &s, int width, int64_t sl) { return s.L == 1 || (sl >= width && sl < (int64_t)1 << 24); }
@@ -63,11 +64,16 @@ struct Layout {
 inline int64_t mats(const Shape &s) { return s.nslots * s.Hv * 2; }
 inline int a_planes(const Shape &s) { return s.bf16 ? 2 : 3; }
 
+// States by slot and rows by step, float32 or 16 bits with the units of their blocks.
+void lay_kept(const Shape &s, Layout &l, void *&states, void *&rows, float *&units) {
+    const int64_t size = s.exact ? 4 : 2;
+    states = l.take<char>(s.nslots * s.Hv * s.dkp * s.dvp * size);
+    rows = l.take<char>(s.rows * s.Hv * s.dvp * size);
+    if (!s.exact) units = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
+}
 void lay_saved(const Shape &s, bool s0, Layout &l, DeltaParams &p) {
-    p.states = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
-    p.err = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
-    if (s.bf16) p.units = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
-    p.mats_adj = l.take<uint16_t>(mats(s) * chunk_words(adjoint_planes(s, s0), a_planes(s)));
+    lay_kept(s, l, p.states, p.err, p.units);
+    p.mats_adj = l.take<uint16_t>(mats(s) * chunk_words(adjoint_planes(s, s0), adjoint_planes(s, s0)));
 }
 
 DeltaRows lay_rows(const Shape &s, Layout &l, const void *src, int H, int width, int padded, int64_t sb, int64_t sl, int64_t sh, bool one_batch, bool &copied) {
@@ -98,7 +104,7 @@ void add_pack(const Shape &s, DeltaPacks &all, const DeltaRows &r, const void *s
 template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
     p.B = s.B; p.Hk = s.Hk; p.Hv = s.Hv; p.dk = s.dk; p.dv = s.dv; p.dvp = s.dvp;
     p.L = s.L; p.nslots = s.nslots; p.slots_each = s.slots_each; p.scale = a->scale;
-    p.io = s.bf16; p.gate_io = a->gate_dtype == LRNNX_BF16; p.cu = a->cu_seqlens;
+    p.io = s.bf16; p.gate_io = a->gate_dtype == LRNNX_BF16; p.exact = s.exact; p.cu = a->cu_seqlens;
     p.v = a->v; p.g = a->g; p.beta = a->beta;
     p.v_sb = a->v_stride_b; p.v_sl = a->v_stride_l; p.v_sh = a->v_stride_h;
     p.g_sb = a->g_stride_b; p.g_sl = a->g_stride_l; p.g_sh = a->g_stride_h;
@@ -127,7 +133,7 @@ DeltaFwdPlan plan_fwd(const lrnnx_delta_fwd_args *a, const Shape &s, char *ws, c
     DeltaFwdPlan f{};
     set_inputs(a, s, f.p);
     const bool one = a->cu_seqlens != nullptr;
-    f.p.np = !s.bf16 || a->s0 || a->s_last ? 3 : 2;
+    f.p.np = s.exact || a->s0 || a->s_last ? 3 : 2;
     f.p.np_adjoint = adjoint_planes(s, a->s0 != nullptr);
     Layout l{ws}, sv{saved};
     f.p.q = lay_rows(s, l, a->q, s.Hk, s.dk, s.dkp, a->q_stride_b, a->q_stride_l, a->q_stride_h, one, f.copy_q);
@@ -155,10 +161,8 @@ DeltaBwdPlan plan_bwd(const lrnnx_delta_bwd_args *a, const Shape &s, char *ws, c
     f.p.k = lay_rows(s, l, a->k, s.Hk, s.dk, s.dkp, a->k_stride_b, a->k_stride_l, a->k_stride_h, one, f.copy_k);
     f.p.dout = lay_rows(s, l, a->dout, s.Hv, s.dv, s.dvp, a->dout_stride_b, a->dout_stride_l, a->dout_stride_h, one, f.copy_d);
     lay_saved(s, a->s0 != nullptr, sv, f.p);
-    f.p.dstates = l.take<uint16_t>(s.nslots * s.Hv * s.planes * s.dkp * s.dvp);
-    f.p.z = l.take<uint16_t>((int64_t)s.planes * s.rows * s.Hv * s.dvp);
+    lay_kept(s, l, f.p.dstates, f.p.z, f.p.dunits);
     if (s.Hv > s.Hk) f.p.part = l.take<float>(2 * s.rows * s.Hv * s.dkp);
-    if (s.bf16) f.p.dunits = l.take<float>(s.nslots * s.Hv * 6 * (s.dvp / 16));
     plan_segments(s, one, l, f.p);
     f.bytes = l.at; f.saved = sv.at;
     return f;

@@ -19,10 +19,9 @@ namespace lrnnx {
 // As in the forward walk a wavefront owns 16 columns of dS, or two share them, and everything it computes of them stays in its registers.  Bound by the
 // latency of a chunk: 4 x 4096 steps of 16 heads of 128 x 128, bfloat16, 128 chunks in 257 us (351 with one wavefront to 16 columns).
 template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
-    static constexpr int NPA = NPI == 3 ? 3 : 2;
     struct Buf {
         uint16_t k[NPI][32][DK + 8], kt[NPI][DK][40], qt[NPI][DK][40];
-        uint16_t th[NP][256], tw[NP][512], ah[NPA][256], aw[NPA][512];         // (as they lie in memory)
+        uint16_t th[NP][256], tw[NP][512], ah[NP][256], aw[NP][512];           // (as they lie in memory)
         float scal[96];
     } buf[NBUF];
     f32x4 halves[DS == 2 ? 8 : 1][64];
@@ -30,10 +29,9 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
 
 // DEEP: loads two chunks ahead, for launches of at most a workgroup a compute unit, where registers are there for it and nothing else hides memory
 // (the same with one wavefront to 16 columns: 385 -> 346 us; the forward walk gains nothing by it, with one or two).
-template <int NPI, int NP, int DK, int DS, bool AGG, bool DEEP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS == 1 || NPI == 3) ? 1 : 2, DEEP && (DS == 1 || NPI == 3) ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
+template <int NPI, int NP, int DK, int DS, bool EXACT, bool AGG, bool DEEP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS == 1 || NP == 3) ? 1 : 2, DEEP && (DS == 1 || NP == 3) ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
     constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
-    constexpr int NPA = NPI == 3 ? 3 : 2, NPS = NPI;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     extern __shared__ __align__(16) char lds_raw[];
     using Lds = AdjLds<NPI, NP, DK, NBUF, DS>;
@@ -66,7 +64,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + sq.at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + sq.at * p.q.sl + hk * p.q.sh;
     const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + sq.at * p.dout.sl + h * p.dout.sh;
 
-    constexpr int QUADS = 8 * (DK / 4), MATS = chunk_words(NP, NPA) / 8;
+    constexpr int QUADS = 8 * (DK / 4), MATS = chunk_words(NP, NP) / 8;
     constexpr int IQ = (QUADS + NT - 1) / NT, IM = (MATS + NT - 1) / NT;
     struct Stage {
         uint2 k[IQ][NPI][4], q[IQ][NPI][4];
@@ -149,9 +147,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
         const int G = p.dvp / 16;
         float *units = p.dunits + sh * 6 * G + c0 / 16;
         if (!AGG && ((ch & 1) || ch == nchunk - 1) && mine)
-            save_state<NPS, DK>(S, p.dstates + (sh * NPS * p.dvp + n0) * DK + d0 + 4 * g4, (int64_t)p.dvp * DK, units + dh * G, G);
+            save_state<EXACT, DK>(S, p.dstates, (sh * p.dvp + n0) * DK + d0 + 4 * g4, units + dh * G, G);
         constexpr bool EARLY = NPI == 1;                    // operands read well before they are used
-        Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NPA], tt[OT][NP];
+        Frag kf[EARLY ? KS : 1][2][NPI], tf[2][NP], ktf[EARLY ? MT : 1][NPI], qtf[EARLY ? MT : 1][NPI], af[2][NP], tt[OT][NP];
         f32x4 gam[2], be[2], en[2];
         if constexpr (EARLY)
 #pragma unroll
@@ -162,7 +160,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
         for (int m = 0; m < 2; ++m) {
             en[m] = *reinterpret_cast<const f32x4 *>(&B.scal[32 + 16 * m + 4 * g4]);
 #pragma unroll
-            for (int i = 0; i < NPA; ++i) af[m][i] = m ? half_tile<true>(B.ah[i], lane) : whole_tile(B.aw[i], lane);
+            for (int i = 0; i < NP; ++i) af[m][i] = m ? half_tile<true>(B.ah[i], lane) : whole_tile(B.aw[i], lane);
 #pragma unroll
             for (int i = 0; i < NP; ++i) tf[m][i] = m ? half_tile<true>(B.th[i], lane) : whole_tile(B.tw[i], lane);
         }
@@ -265,8 +263,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
                 S[m] = mm(ktf[0], rf, S[m]);
             }
         if (!AGG && mine)
-            save_rows<NPS>(Zt, p.z + ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
-                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n - 16 * first, units + (2 + 2 * (ch & 1) + first) * G, G);
+            save_rows<EXACT>(Zt, p.z, ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                             n - 16 * first, units + (2 + 2 * (ch & 1) + first) * G, G);
         if (NBUF == 1) lds_barrier();
         put(lds.buf[NBUF == 2 ? (ch - 1) & 1 : 0], next);
         lds_barrier();
@@ -313,23 +311,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
 // The columns of v come through LDS 32 at a time (rows of dO, E, Z and of both states, the next ones under way meanwhile), then K and Q, as rows
 // and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.  Bound by memory: 4 x 4096 steps of 16 heads of
 // 128 x 128, 783 MB in 224 us (3.5 TB/s; a copy would take 158).
-template <int NPI, int DK> struct GradLds {
+template <int NPI, int NPE, int DK> struct GradLds {
     static constexpr int ROWS = NPI == 3 ? 0 : 1;
     union {
-        struct { uint16_t e[NPI][64][40], z[NPI][64][40], d[NPI][64][40], s0[NPI][DK][40], s1[NPI][DK][40]; } v;
+        struct { uint16_t e[NPE][64][40], z[NPE][64][40], d[NPI][64][40], s0[NPE][DK][40], s1[NPE][DK][40]; } v;
         struct { uint16_t kt[NPI][DK][72], qt[NPI][DK][72], kr[ROWS + 1][ROWS ? 64 : 1][DK + 8]; } k;      // kr: rows of K and of Q
     };
     double G[64];
     float beta[64], dG[64], ends[4], dots[4], most[4];
 };
 
-template <class IO, int NPI, int DK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
+// NPI: planes of an input, NPE: of E, Z and the states, which lie in memory as float32 (3) or as 16-bit floating point with a power of two a block (1; dO too
+// is brought to that here).
+template <class IO, int NPI, int NPE, int DK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 2 : 1, 2))) void k_delta_grads(const DeltaParams p) {
     constexpr int KS = DK / 32, MT = DK / 16, NPF = NPI == 3 ? 3 : 2;
-    constexpr bool UNITS = NPI == 1;                        // E, Z, the states and here dO too: 16-bit floating point with a power of two a block
+    constexpr bool UNITS = NPE == 1;
+    using Kept = std::conditional_t<UNITS, uint16_t, float>;
+    constexpr int KE = sizeof(Kept) / 2;
     constexpr bool ROWS = NPI == 1;                         // rows of K and Q in LDS too; else from memory
     extern __shared__ __align__(16) char lds_raw[];
-    GradLds<NPI, DK> &lds = *reinterpret_cast<GradLds<NPI, DK> *>(lds_raw);
+    GradLds<NPI, NPE, DK> &lds = *reinterpret_cast<GradLds<NPI, NPE, DK> *>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row16 = lane & 15, g4 = lane >> 4;
     const int64_t slot = blockIdx.x / (unsigned)p.Hv;
     const int h = (int)(blockIdx.x - slot * p.Hv), hk = h / (p.Hv / p.Hk);
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
     if (n == 0) return;
     const int64_t at = sq.at + t0, row0 = sq.row + t0, rows = (int64_t)(p.cu ? 1 : p.B) * p.L;
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
-    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, drow = (uint32_t)p.dout.sl * 2, erow = (uint32_t)p.Hv * p.dvp * 2;
+    const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, drow = (uint32_t)p.dout.sl * 2, erow = (uint32_t)p.Hv * p.dvp * (uint32_t)sizeof(Kept);
     const int own = 16 * wave + row16;
     const bool own_in = own < n;
 
@@ -349,33 +351,41 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
     for (int m = 0; m < MT; ++m) dq[m] = dk[m] = f32x4{};
 
     const uint16_t *dp = p.dout.p + sq.ib * p.dout.sb + at * p.dout.sl + h * p.dout.sh;
-    const uint16_t *ep = p.err + (row0 * p.Hv + h) * p.dvp, *zp = p.z + (row0 * p.Hv + h) * p.dvp;
-    const int64_t eplane = rows * p.Hv * p.dvp;
-    const uint16_t *s0p = p.states + (slot * p.Hv + h) * NPI * DK * p.dvp, *s1p = p.dstates + (slot * p.Hv + h) * NPI * DK * p.dvp;
+    // E's and Z's rows: in float32 those of the wavefront's 16 steps (all 64 of a slot may span more than a descriptor does)
+    const int from = UNITS ? 0 : 16 * wave, to = UNITS || n < from + 16 ? n : from + 16;
+    const int64_t first = ((row0 + from) * p.Hv + h) * p.dvp;
+    const int64_t ebytes = to > from ? (to - from - 1) * (int64_t)erow + p.dvp * (int64_t)sizeof(Kept) : 0;
+    const Kept *ep = reinterpret_cast<const Kept *>(p.err) + first, *zp = reinterpret_cast<const Kept *>(p.z) + first;
+    const Kept *s0p = reinterpret_cast<const Kept *>(p.states) + (slot * p.Hv + h) * DK * p.dvp;
+    const Kept *s1p = reinterpret_cast<const Kept *>(p.dstates) + (slot * p.Hv + h) * DK * p.dvp;
     const int ksv = p.dvp / 32;
 
-    // 32 columns of v on their way: a thread brings 16 bytes of a row of dO and of each plane of E and Z, and of the states, which lie a column of v to
+    // 32 columns of v on their way: a thread brings eight elements of a row of dO (of each plane), E and Z, and of the states, which lie a column of v to
     // a row, four rows by four elements (the first 2 DK threads)
-    uint4 ereg[NPI], zreg[NPI], dreg[NPI];
-    uint2 areg[NPI][4], breg[NPI][4];
+    uint4 ereg[KE], zreg[KE], dreg[NPI];
+    uint2 areg[KE][4], breg[KE][4];
     const int tr = tid >> 2, tc = (tid & 3) * 16, sq4 = tid / (DK / 4), sd4 = tid % (DK / 4);
     auto fetch = [&](int ks) {
 #pragma unroll
-        for (int i = 0; i < NPI; ++i) {
-            ereg[i] = buffer_load16(buffer_of(ep + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
-            zreg[i] = buffer_load16(buffer_of(zp + i * eplane, (int64_t)(n - 1) * erow + 2 * p.dvp), tr * erow + 64 * ks + tc);
+        for (int i = 0; i < KE; ++i) {
+            const uint32_t off = (UNITS ? tr : tr & 15) * erow + KE * (64 * ks + tc) + 16 * i;
+            ereg[i] = buffer_load16(buffer_of(ep, ebytes), off);
+            zreg[i] = buffer_load16(buffer_of(zp, ebytes), off);
         }
 #pragma unroll
         for (int i = 0; i < NPI; ++i)
             dreg[i] = buffer_load16(buffer_of(dp + i * p.dout.plane, (int64_t)(n - 1) * drow + 2 * p.dvp), tr * drow + 64 * ks + tc);
 #pragma unroll
-        for (int i = 0; i < NPI; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * 2) : kOutside;
-                areg[i][x] = buffer_load8(buffer_of(s0p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
-                breg[i][x] = buffer_load8(buffer_of(s1p + (int64_t)i * DK * p.dvp, DK * p.dvp * 2), off);
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t off = tid < 2 * DK ? (uint32_t)(((32 * ks + 4 * sq4 + x) * DK + 4 * sd4) * (int)sizeof(Kept)) : kOutside;
+            const Buffer ab = buffer_of(s0p, DK * p.dvp * (int)sizeof(Kept)), bb = buffer_of(s1p, DK * p.dvp * (int)sizeof(Kept));
+            if constexpr (UNITS) { areg[0][x] = buffer_load8(ab, off); breg[0][x] = buffer_load8(bb, off); }
+            else {
+                const uint4 a = buffer_load16(ab, off), b = buffer_load16(bb, off);
+                areg[0][x] = make_uint2(a.x, a.y); areg[KE - 1][x] = make_uint2(a.z, a.w);
+                breg[0][x] = make_uint2(b.x, b.y); breg[KE - 1][x] = make_uint2(b.z, b.w);
             }
+        }
     };
     // the blocks' units: a slot's largest of each kind, and the others' share of it
     float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
@@ -428,7 +438,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
     f32x4 qs[MT], kr[MT], kw[MT];                                // S0 dO, S0 z, dS1 e of the lane's step
 #pragma unroll
     for (int m = 0; m < MT; ++m) qs[m] = kr[m] = kw[m] = f32x4{};
-    auto mv = [](const Frag (&a)[NPI], const Frag (&b)[NPI], f32x4 c) __attribute__((always_inline)) -> f32x4 {
+    auto mv = [](const auto &a, const auto &b, f32x4 c) __attribute__((always_inline)) -> f32x4 {
         if constexpr (UNITS) return mfma16(a[0], b[0], c);
         else return mm(a, b, c);
     };
@@ -463,11 +473,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
         auto times = [&](uint32_t x, uint32_t f) __attribute__((always_inline)) -> uint32_t {
             return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f)) : x;
         };
+        if constexpr (UNITS) {
+            const uint4 e = ereg[0], z = zreg[0];
+            *reinterpret_cast<uint4 *>(&L.e[0][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
+            *reinterpret_cast<uint4 *>(&L.z[0][tr][tc / 2]) = make_uint4(times(z.x, pZ), times(z.y, pZ), times(z.z, pZ), times(z.w, pZ));
+        } else {
+            auto planes = [](const uint4 &lo, const uint4 &hi, uint32_t (&w)[4][NPE]) __attribute__((always_inline)) {
+                split2<NPE>(__uint_as_float(lo.x), __uint_as_float(lo.y), w[0]);
+                split2<NPE>(__uint_as_float(lo.z), __uint_as_float(lo.w), w[1]);
+                split2<NPE>(__uint_as_float(hi.x), __uint_as_float(hi.y), w[2]);
+                split2<NPE>(__uint_as_float(hi.z), __uint_as_float(hi.w), w[3]);
+            };
+            uint32_t e[4][NPE], z[4][NPE];
+            planes(ereg[0], ereg[KE - 1], e);
+            planes(zreg[0], zreg[KE - 1], z);
 #pragma unroll
-        for (int i = 0; i < NPI; ++i) {
-            const uint4 e = ereg[i], z = zreg[i];
-            *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
-            *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = make_uint4(times(z.x, pZ), times(z.y, pZ), times(z.z, pZ), times(z.w, pZ));
+            for (int i = 0; i < NPE; ++i) {
+                *reinterpret_cast<uint4 *>(&L.e[i][tr][tc / 2]) = make_uint4(e[0][i], e[1][i], e[2][i], e[3][i]);
+                *reinterpret_cast<uint4 *>(&L.z[i][tr][tc / 2]) = make_uint4(z[0][i], z[1][i], z[2][i], z[3][i]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < NPI; ++i) {
@@ -479,12 +503,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
             }
             *reinterpret_cast<uint4 *>(&L.d[i][tr][tc / 2]) = d;
         }
+        uint2 ap[NPE][4], bp[NPE][4];
 #pragma unroll
-        for (int i = 0; i < NPI; ++i)
+        for (int x = 0; x < 4; ++x) {
+            if constexpr (UNITS) { ap[0][x] = areg[0][x]; bp[0][x] = breg[0][x]; }
+            else {
+                uint32_t a[2][NPE], b[2][NPE];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    split2<NPE>(__uint_as_float(areg[y * (KE - 1)][x].x), __uint_as_float(areg[y * (KE - 1)][x].y), a[y]);
+                    split2<NPE>(__uint_as_float(breg[y * (KE - 1)][x].x), __uint_as_float(breg[y * (KE - 1)][x].y), b[y]);
+                }
+#pragma unroll
+                for (int i = 0; i < NPE; ++i) { ap[i][x] = make_uint2(a[0][i], a[1][i]); bp[i][x] = make_uint2(b[0][i], b[1][i]); }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NPE; ++i)
             if (tid < 2 * DK) {
                 uint2 c[4], d[4];
-                transpose_quad(areg[i], c);
-                transpose_quad(breg[i], d);
+                transpose_quad(ap[i], c);
+                transpose_quad(bp[i], d);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     *reinterpret_cast<uint2 *>(&L.s0[i][4 * sd4 + x][turned(4 * sd4, 4 * sq4)]) = make_uint2(times(c[x].x, pA), times(c[x].y, pA));
@@ -495,20 +534,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
         else fetch(ks + 1);
         lds_barrier();
         bown = lds.beta[own];
-        Frag dO[NPI], e[NPI], z[NPI];
+        Frag dO[NPI], e[NPE], z[NPE];
 #pragma unroll
         for (int i = 0; i < NPI; ++i) dO[i].v = *reinterpret_cast<const uint4 *>(&L.d[i][own][8 * g4]);
 #pragma unroll
-        for (int i = 0; i < NPI; ++i) {
+        for (int i = 0; i < NPE; ++i) {
             e[i].v = *reinterpret_cast<const uint4 *>(&L.e[i][own][8 * g4]);
             z[i].v = *reinterpret_cast<const uint4 *>(&L.z[i][own][8 * g4]);
         }
         // the states' products, and <S0, dS1> of a quarter of their rows
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            Frag s0[NPI], s1[NPI];
+            Frag s0[NPE], s1[NPE];
 #pragma unroll
-            for (int i = 0; i < NPI; ++i) {
+            for (int i = 0; i < NPE; ++i) {
                 s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                 s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
             }
@@ -520,9 +559,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
 #pragma unroll
         for (int y = 0; y < MT / 4; ++y) {
             const int m = 4 * y + wave;
-            Frag s0[NPI], s1[NPI];
+            Frag s0[NPE], s1[NPE];
 #pragma unroll
-            for (int i = 0; i < NPI; ++i) {
+            for (int i = 0; i < NPE; ++i) {
                 s0[i].v = *reinterpret_cast<const uint4 *>(&L.s0[i][16 * m + row16][turned(16 * m, 8 * g4)]);
                 s1[i].v = *reinterpret_cast<const uint4 *>(&L.s1[i][16 * m + row16][turned(16 * m, 8 * g4)]);
             }
@@ -532,7 +571,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
                 else {
                     float al = 0.0f, ah = 0.0f, cl = 0.0f, chh = 0.0f;
 #pragma unroll
-                    for (int i = NPI - 1; i >= 0; --i) {
+                    for (int i = NPE - 1; i >= 0; --i) {
                         al += __uint_as_float(s1[i].u[x] << 16); ah += hi_part(__uint_as_float(s1[i].u[x]));
                         cl += __uint_as_float(s0[i].u[x] << 16); chh += hi_part(__uint_as_float(s0[i].u[x]));
                     }
@@ -543,15 +582,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
         // with the other steps
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            Frag r1[NPI], r2[NPI], c1[NPI], c2[NPI];
+            Frag r1[NPE], r2[NPE], c1[NPE], c2[NPE];
 #pragma unroll
-            for (int i = 0; i < NPI; ++i) {
-                r1[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.d)[i][16 * m + row16][8 * g4]);
+            for (int i = 0; i < NPE; ++i) {
+                const int j = i < NPI ? i : 0;              // (of one plane each product of E with dO takes it)
+                r1[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.d)[NPI == NPE || m <= wave ? i : j][16 * m + row16][8 * g4]);
                 r2[i].v = *reinterpret_cast<const uint4 *>(&(m <= wave ? L.e : L.z)[i][16 * m + row16][8 * g4]);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) { c1[i].u[x] = m <= wave ? dO[i].u[x] : e[i].u[x]; c2[i].u[x] = m <= wave ? z[i].u[x] : e[i].u[x]; }
+                for (int x = 0; x < 4; ++x) { c1[i].u[x] = m <= wave ? dO[j].u[x] : e[i].u[x]; c2[i].u[x] = m <= wave ? z[i].u[x] : e[i].u[x]; }
             }
-            P1[m] = mv(r1, c1, P1[m]);
+            if constexpr (NPI == NPE) P1[m] = mv(r1, c1, P1[m]);
+            else
+#pragma unroll
+                for (int i = 0; i < NPE; ++i) P1[m] = mfma(r1[i], c1[i], P1[m]);
             P2[m] = mv(r2, c2, P2[m]);
         }
         P1own = mv(dO, e, P1own);
@@ -567,7 +610,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPI == 1 ? 
 #pragma unroll
             for (int x = 0; x < 8; ++x)
 #pragma unroll
-                for (int i = NPI - 1; i >= 0; --i) {
+                for (int i = NPE - 1; i >= 0; --i) {
                     zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
                     es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
                 }
@@ -797,13 +840,13 @@ template <class IO, int DK> __global__ __launch_bounds__(256) void k_delta_share
 }
 
 // ---------------------------------------------------------------- launches
-template <int NPI, int NP, int DK, int DS, bool AGG> static hipError_t launch_adjoint_one(DeltaParams p, hipStream_t s) {
+template <int NPI, int NP, int DK, int DS, bool EXACT, bool AGG> static hipError_t launch_adjoint_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr size_t bytes = sizeof(AdjLds<NPI, NP, DK, NBUF, DS>);
     static_assert(bytes <= 160 * 1024, "LDS");
     p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + 4 / DS - 1) / (4 / DS);
     const unsigned blocks = delta_blocks(p, AGG ? p.nseg - 1 : p.nseg);
-    auto k = blocks <= 256 ? k_delta_adjoint<NPI, NP, DK, DS, AGG, true> : k_delta_adjoint<NPI, NP, DK, DS, AGG, false>;
+    auto k = blocks <= 256 ? k_delta_adjoint<NPI, NP, DK, DS, EXACT, AGG, true> : k_delta_adjoint<NPI, NP, DK, DS, EXACT, AGG, false>;
     if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3(blocks), dim3(256), bytes, s, p);
@@ -811,20 +854,25 @@ template <int NPI, int NP, int DK, int DS, bool AGG> static hipError_t launch_ad
 }
 template <int NPI, int NP, int DK> static hipError_t launch_adjoint_dk(const DeltaParams &p, hipStream_t s) {
     if (p.nseg > 1) {
-        if (const hipError_t e = launch_adjoint_one<NPI, NP, DK, 1, true>(p, s)) return e;
+        if (const hipError_t e = launch_adjoint_one<NPI, NP, DK, 1, false, true>(p, s)) return e;
         if (const hipError_t e = launch_delta_join(p, true, s)) return e;
     }
-    return delta_rows_split(p) ? launch_adjoint_one<NPI, NP, DK, 2, false>(p, s) : launch_adjoint_one<NPI, NP, DK, 1, false>(p, s);
+    const bool split = delta_rows_split(p);
+    if constexpr (NP == 3)
+        if (p.exact) return split ? launch_adjoint_one<NPI, NP, DK, 2, true, false>(p, s) : launch_adjoint_one<NPI, NP, DK, 1, true, false>(p, s);
+    if constexpr (NPI == 1)
+        if (!p.exact) return split ? launch_adjoint_one<NPI, NP, DK, 2, false, false>(p, s) : launch_adjoint_one<NPI, NP, DK, 1, false, false>(p, s);
+    return hipErrorInvalidValue;
 }
 hipError_t launch_delta_adjoint(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_adjoint_dk<3, 3, 128>(p, s) : launch_adjoint_dk<3, 3, 64>(p, s);
     if (p.np == 3) return p.dk > 64 ? launch_adjoint_dk<1, 3, 128>(p, s) : launch_adjoint_dk<1, 3, 64>(p, s);
     return p.dk > 64 ? launch_adjoint_dk<1, 2, 128>(p, s) : launch_adjoint_dk<1, 2, 64>(p, s);
 }
-template <class IO, int NPI, int DK> static hipError_t launch_grads_one(const DeltaParams &p, hipStream_t s) {
-    constexpr size_t bytes = sizeof(GradLds<NPI, DK>);
+template <class IO, int NPI, int NPE, int DK> static hipError_t launch_grads_one(const DeltaParams &p, hipStream_t s) {
+    constexpr size_t bytes = sizeof(GradLds<NPI, NPE, DK>);
     static_assert(bytes <= 160 * 1024, "LDS");
-    auto k = k_delta_grads<IO, NPI, DK>;
+    auto k = k_delta_grads<IO, NPI, NPE, DK>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3((unsigned)(p.nslots * p.Hv)), dim3(256), bytes, s, p);
     if (const hipError_t e = hipGetLastError()) return e;
@@ -832,8 +880,9 @@ template <class IO, int NPI, int DK> static hipError_t launch_grads_one(const De
     return hipGetLastError();
 }
 hipError_t launch_delta_grads(const DeltaParams &p, hipStream_t s) {
-    if (!p.io) return p.dk > 64 ? launch_grads_one<float, 3, 128>(p, s) : launch_grads_one<float, 3, 64>(p, s);
-    return p.dk > 64 ? launch_grads_one<uint16_t, 1, 128>(p, s) : launch_grads_one<uint16_t, 1, 64>(p, s);
+    if (!p.io) return p.dk > 64 ? launch_grads_one<float, 3, 3, 128>(p, s) : launch_grads_one<float, 3, 3, 64>(p, s);
+    if (p.exact) return p.dk > 64 ? launch_grads_one<uint16_t, 1, 3, 128>(p, s) : launch_grads_one<uint16_t, 1, 3, 64>(p, s);
+    return p.dk > 64 ? launch_grads_one<uint16_t, 1, 1, 128>(p, s) : launch_grads_one<uint16_t, 1, 1, 64>(p, s);
 }
 
 }  // namespace lrnnx

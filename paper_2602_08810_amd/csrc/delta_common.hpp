@@ -3,7 +3,8 @@
 // Precision.  Matrix instructions take bfloat16 factors and add in float32.  A float32 number is the sum of three bfloat16 numbers (8 bits
 // of its mantissa each, split by truncation without loss), so a float32 product is six instructions (those of weight 2^-24 and below are left
 // out), and three where one factor is bfloat16 from the start.  At 16 cycles for 16 x 16 x 32 six of them take 96 cycles, the float32 matrix
-// instruction 256.  Where every result is rounded to bfloat16 two planes do (16 bits, relative error 2^-17).
+// instruction 256.  Where every result is rounded to bfloat16 two planes do (16 bits, relative error 2^-17): with bfloat16 inputs and gates and no first or
+// last state.  A gradient of the first state that is asked for without one is the exception: float32, from two planes (5e-6 of its norm, 2e-7 from three).
 #pragma once
 #include "delta.hpp"
 #include "scan_common.hpp"
@@ -77,8 +78,10 @@ template <int NP> __device__ __forceinline__ void split2(float a, float b, uint3
         if (i < NP - 1) { a -= hi_part(a); b -= hi_part(b); }
     }
 }
-// What the backward pass is left of bfloat16 operands' states, errors and gradients: 16-bit floating point with a common power of two a block, 11 bits of
-// mantissa (what the results are rounded to has 8) for numbers down to 2^-29 of the block's largest, which the power brings to 2^14 .. 2^15.
+// What the backward pass is left of states, errors and their gradients: float32 where a result is float32, which is that of the gates with float32 gates.
+// Where inputs and gates are bfloat16, and so all results but the states' gradients (which come from none of it): 16-bit floating point with a common
+// power of two a block, 11 bits of mantissa (the results keep 8) for numbers down to 2^-29 of the block's largest, which the power brings to 2^14 .. 2^15.
+// 4 x 4096 steps of 16 heads of 128 x 128, training: 803 us so, 1177 in float32 (with three planes in both walks too).
 // What is not finite stays so and has no part in it.  The power's inverse, from the largest magnitude:
 __device__ __forceinline__ float block_unit(float largest) {
     const uint32_t e = __float_as_uint(largest) >> 23;
@@ -126,37 +129,30 @@ template <int N> __device__ __forceinline__ float unit_of(const f32x4 (&x)[N]) {
     if (m == INFINITY) m = wave_max(largest_of<N, true>(x));
     return block_unit(m);
 }
-// MT tiles of a state's 16 columns as they are saved, a column to a row of DK: planes, or 16 bits with their unit (a unit each half of the rows)
-template <int NPS, int DK, int MT> __device__ __forceinline__ void save_state(const f32x4 (&S)[MT], uint16_t *to, int64_t plane, float *unit, int G) {
-    float inv = 0.0f;
-    if constexpr (NPS == 1) {
-        const float u = unit_of(S);
-        inv = inverse_unit(u);
+// MT tiles of a state's 16 columns as they are saved, a column to a row of DK (this lane's part starts at element `at`): float32, or 16 bits with
+// their unit (a unit each half of the rows)
+template <bool EXACT, int DK, int MT> __device__ __forceinline__ void save_state(const f32x4 (&S)[MT], void *states, int64_t at, float *unit, int G) {
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(states) + at + 16 * m) = S[m];
+    } else {
+        const float u = unit_of(S), inv = inverse_unit(u);
         if ((threadIdx.x & 63) == 0) {
             *unit = u;
             if (MT == DK / 16) unit[G] = u;
         }
-    }
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        uint32_t lo[NPS], hi[NPS];
-        if constexpr (NPS == 1) {
-            lo[0] = pack_f16(S[m][0] * inv, S[m][1] * inv);
-            hi[0] = pack_f16(S[m][2] * inv, S[m][3] * inv);
-        } else {
-            split2<NPS>(S[m][0], S[m][1], lo);
-            split2<NPS>(S[m][2], S[m][3], hi);
-        }
-#pragma unroll
-        for (int i = 0; i < NPS; ++i) *reinterpret_cast<uint2 *>(to + i * plane + 16 * m) = make_uint2(lo[i], hi[i]);
+        for (int m = 0; m < MT; ++m)
+            *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(states) + at + 16 * m) =
+                make_uint2(pack_f16(S[m][0] * inv, S[m][1] * inv), pack_f16(S[m][2] * inv, S[m][3] * inv));
     }
 }
-// 16 columns of N tiles of 16 steps of E or Z, a step to a lane (`row`: this lane's of the first, the next ones' rows16 elements on; n: steps there
+// 16 columns of N tiles of 16 steps of E or Z, a step to a lane (`at`: this lane's element of the first, the next ones' rows16 on; n: steps there
 // are from the first tile on; a unit a tile, G apart)
-template <int NPE, int N> __device__ __forceinline__ void save_rows(const f32x4 (&X)[N], uint16_t *row, int64_t rows16, int64_t plane, int n, float *unit, int G) {
+template <bool EXACT, int N> __device__ __forceinline__ void save_rows(const f32x4 (&X)[N], void *rows, int64_t at, int64_t rows16, int n, float *unit, int G) {
     const int row16 = threadIdx.x & 15;
     float inv = 0.0f;
-    if constexpr (NPE == 1) {
+    if constexpr (!EXACT) {
         const float u = unit_of(X);
         inv = inverse_unit(u);
         if ((threadIdx.x & 63) == 0)
@@ -164,19 +160,12 @@ template <int NPE, int N> __device__ __forceinline__ void save_rows(const f32x4 
             for (int m = 0; m < N; ++m) unit[m * G] = u;
     }
 #pragma unroll
-    for (int m = 0; m < N; ++m) {
-        uint32_t lo[NPE], hi[NPE];
-        if constexpr (NPE == 1) {
-            lo[0] = pack_f16(X[m][0] * inv, X[m][1] * inv);
-            hi[0] = pack_f16(X[m][2] * inv, X[m][3] * inv);
-        } else {
-            split2<NPE>(X[m][0], X[m][1], lo);
-            split2<NPE>(X[m][2], X[m][3], hi);
+    for (int m = 0; m < N; ++m)
+        if (16 * m + row16 < n) {
+            if constexpr (EXACT) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(rows) + at + m * rows16) = X[m];
+            else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(rows) + at + m * rows16) =
+                     make_uint2(pack_f16(X[m][0] * inv, X[m][1] * inv), pack_f16(X[m][2] * inv, X[m][3] * inv));
         }
-        if (16 * m + row16 < n)
-#pragma unroll
-            for (int i = 0; i < NPE; ++i) *reinterpret_cast<uint2 *>(row + i * plane + m * rows16) = make_uint2(lo[i], hi[i]);
-    }
 }
 
 // two result tiles as the operand of the next product

@@ -88,7 +88,7 @@ hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s) {
 // Bound by what it reads and writes, few chunks by latency: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 20 at the rate of a copy;
 // 4 x 4096 with the adjoint's matrices 61 us of 49 (71 with a wavefront for two chunks); 2 x 77 steps of 6 heads, float32, 9 (11).
 template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NPI == 3 ? 2 : 4))) void k_delta_prep(const DeltaParams p) {
-    constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, NPA);
+    constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, ADJ);
     __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][32][W];           // N by rows; by columns, both counted from the end
     __shared__ double Gs[32];
     __shared__ __align__(16) float Bs[32];
@@ -203,8 +203,8 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __a
         store(A[1], A[2], 1, ForA(), std::false_type(), to);
         if constexpr (ADJ > 0) {
             to = p.mats_adj + mat * AW + ADJ * 768;
-            store(At[0], At[1], 0, ForA(), std::true_type(), to);
-            store(none, At[2], 1, ForA(), std::true_type(), to);
+            store(At[0], At[1], 0, std::integral_constant<int, ADJ>(), std::true_type(), to);
+            store(none, At[2], 1, std::integral_constant<int, ADJ>(), std::true_type(), to);
         }
     }
     lds_barrier();
@@ -264,10 +264,10 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct ScanLds {
 // halves of K S0 and Q S0 are added) and twice the workgroups (the two cases above with one wavefront: 133 and 340 us).
 // AGG: what a segment makes of the state that enters it, S -> M S + N, without outputs: N is the walk from a state of zero, and the columns of M, behind those
 // of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
-template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG>
+template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool EXACT, bool AGG>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(const DeltaParams p) {
     constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
-    constexpr int NPA = NPI == 3 ? 3 : 2, NPS = NPI;
+    constexpr int NPA = NPI == 3 ? 3 : 2;
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr int NPO = NPI == 3 ? 3 : 2;                 // planes of what only enters o
     extern __shared__ __align__(16) char lds_raw[];
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const int64_t sh = (sq.slot + (ch >> 1)) * p.Hv + h;
         if (SAVE && !(ch & 1) && c0 < p.dvp) {
             const int G = p.dvp / 16;
-            save_state<NPS, DK>(S, p.states + (sh * NPS * p.dvp + n0) * DK + d0 + 4 * g4, (int64_t)p.dvp * DK, p.units + (sh * 6 + dh) * G + c0 / 16, G);
+            save_state<EXACT, DK>(S, p.states, (sh * p.dvp + n0) * DK + d0 + 4 * g4, p.units + (sh * 6 + dh) * G + c0 / 16, G);
         }
 
         // K S0 and (transposed: a step to a lane) Q S0
@@ -517,8 +517,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
         if (SAVE && c0 < p.dvp) {
             const int G = p.dvp / 16;
-            save_rows<NPS>(Et, p.err + ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
-                           (int64_t)(p.cu ? 1 : p.B) * p.L * p.Hv * p.dvp, n - 16 * first, p.units + (sh * 6 + 2 + 2 * (ch & 1) + first) * G + c0 / 16, G);
+            save_rows<EXACT>(Et, p.err, ((sq.row + t0 + 16 * first + row16) * p.Hv + h) * p.dvp + c0 + 4 * g4, (int64_t)16 * p.Hv * p.dvp,
+                             n - 16 * first, p.units + (sh * 6 + 2 + 2 * (ch & 1) + first) * G + c0 / 16, G);
         }
         if constexpr (!AGG) {                               // O
 #pragma unroll
@@ -676,12 +676,12 @@ hipError_t launch_delta_prep(const DeltaParams &p, hipStream_t s) {
     return p.np == 3 ? launch_prep<1, 3, 2>(p, s) : launch_prep<1, 2, 2>(p, s);
 }
 
-template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG> static hipError_t launch_scan_one(DeltaParams p, hipStream_t s) {
+template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool EXACT, bool AGG> static hipError_t launch_scan_one(DeltaParams p, hipStream_t s) {
     constexpr int NBUF = NPI == 3 && DK == 128 ? 1 : 2;
     constexpr size_t bytes = sizeof(ScanLds<NPI, NP, DK, NBUF, DS>);
     static_assert(bytes <= 160 * 1024, "LDS");
     p.groups = ((AGG ? p.dvp + DK : p.dvp) / 16 + 4 / DS - 1) / (4 / DS);
-    auto k = k_delta_scan<IO, NPI, NP, DK, DS, SAVE, AGG>;
+    auto k = k_delta_scan<IO, NPI, NP, DK, DS, SAVE, EXACT, AGG>;
     if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(k, dim3(delta_blocks(p, AGG ? p.nseg - 1 : p.nseg)), dim3(256), bytes, s, p);
@@ -689,11 +689,16 @@ template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool AGG> static
 }
 template <class IO, int NPI, int NP, int DK> static hipError_t launch_scan_dk(const DeltaParams &p, hipStream_t s) {
     if (p.nseg > 1) {
-        if (const hipError_t e = launch_scan_one<IO, NPI, NP, DK, 1, false, true>(p, s)) return e;
+        if (const hipError_t e = launch_scan_one<IO, NPI, NP, DK, 1, false, false, true>(p, s)) return e;
         if (const hipError_t e = launch_delta_join(p, false, s)) return e;
     }
-    if (delta_rows_split(p)) return p.states ? launch_scan_one<IO, NPI, NP, DK, 2, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 2, false, false>(p, s);
-    return p.states ? launch_scan_one<IO, NPI, NP, DK, 1, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 1, false, false>(p, s);
+    const bool split = delta_rows_split(p);
+    if (!p.states) return split ? launch_scan_one<IO, NPI, NP, DK, 2, false, false, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 1, false, false, false>(p, s);
+    if constexpr (NP == 3)
+        if (p.exact) return split ? launch_scan_one<IO, NPI, NP, DK, 2, true, true, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 1, true, true, false>(p, s);
+    if constexpr (NPI == 1)
+        if (!p.exact) return split ? launch_scan_one<IO, NPI, NP, DK, 2, true, false, false>(p, s) : launch_scan_one<IO, NPI, NP, DK, 1, true, false, false>(p, s);
+    return hipErrorInvalidValue;
 }
 hipError_t launch_delta_scan(const DeltaParams &p, hipStream_t s) {
     if (!p.io) return p.dk > 64 ? launch_scan_dk<float, 3, 3, 128>(p, s) : launch_scan_dk<float, 3, 3, 64>(p, s);

@@ -25,7 +25,7 @@ def test_a_buffer_of_a_call_with_a_first_state_is_refused_without(api):  # noqa:
         assert _call(api, "lrnnx_gated_delta_bwd", a) == WORKSPACE, over
 
 
-@pytest.mark.parametrize("other", [dict(L=164), dict(B=3), dict(Hv=6), dict(dv=128), dict(io_dtype=0)])
+@pytest.mark.parametrize("other", [dict(L=164), dict(B=3), dict(Hv=6), dict(dv=128), dict(dk=128)])
 def test_a_larger_call_s_buffer_is_refused(api, other):  # noqa: F811
     size = _saved(api, **other)
     assert size > _saved(api)
