@@ -511,6 +511,9 @@ int lrnnx_lti_step(const lrnnx_lti_step_args *args);
  * 64 or 128 elements (dk) at 16-byte steps are read in place, others are first copied into the workspace.
  * s0, s_last: [B,Hv,dk,dv] float, contiguous, optional.  1 <= dk <= 128, 1 <= dv <= 256; B, Hv <= 65535; any L >= 1.
  * The keys are used as they are: a recurrence with beta |k|^2 > 2 grows, as its definition says.
+ * What is not finite in k, g (+infinity or NaN) or beta of a step is seen by o of that step and of later ones of the head, in
+ * v by its column of them, in q by that step alone, in s0 by its column; no other o and no other column of s_last changes.
+ * (Where float32 overflows though the inputs are finite, o of up to 31 steps before may be NaN too.)
  * Packed variable-length batches: with cu_seqlens != NULL (device memory [B+1], ascending) q, k, v, g, beta, o are [L,H,...]
  * (batch strides ignored) and sequence b is steps cu_seqlens[b] .. cu_seqlens[b+1]-1; s0 and s_last stay [B,Hv,dk,dv].
  * Boundaries are clamped to [0,L]; steps outside every sequence are neither read as part of one nor written.  The last state

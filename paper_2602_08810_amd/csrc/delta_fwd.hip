@@ -169,6 +169,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __a
     };
     using ForA = std::integral_constant<int, NPA>;
     {
+        float rows[2] = {0.0f, 0.0f};                        // of the lane's row of either half: 0, or NaN
         f32x4 A[3], At[3];
 #pragma unroll
         for (int x = 0; x < 3; ++x) {
@@ -181,6 +182,7 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __a
                     const float d = j0 + r <= i ? __expf((float)(Gi - Gs[j0 + r])) : 0.0f;
                     N[r] = j0 + r < i ? d * kk[x][r] : 0.0f;
                     A[x][r] = j0 + r <= i ? p.scale * d * qk[x][r] : 0.0f;
+                    rows[x > 0] = __builtin_fmaf(N[r], 0.0f, rows[x > 0]);
                 }
                 *reinterpret_cast<f32x4 *>(&Ns[0][i][j0]) = N;
             }
@@ -205,6 +207,19 @@ template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __a
             to = p.mats_adj + mat * AW + ADJ * 768;
             store(At[0], At[1], 0, std::integral_constant<int, ADJ>(), std::true_type(), to);
             store(none, At[2], 1, std::integral_constant<int, ADJ>(), std::true_type(), to);
+        }
+        const uint64_t lower = __ballot(rows[0] != 0.0f), upper = __ballot(rows[1] != 0.0f), strong = __ballot(Bs[own] - Bs[own] != 0.0f);
+        if (lower | upper | strong) {                        // rows from the first that is not finite on: none of N, the walk finds NaN in exp(G)
+            auto fold = [](uint64_t m) { return (uint32_t)(m | m >> 16 | m >> 32 | m >> 48) & 0xffffu; };
+            const int sound = __builtin_ctz(fold(lower) | fold(upper) << 16 | (uint32_t)strong);
+            lds_barrier();
+            if (!up && own >= sound) {
+                Bs[own] = 0.0f;
+                for (int j = 0; j < 32; ++j) Ns[0][own][j] = 0.0f;
+                *(reinterpret_cast<float *>(p.mats + (mat + 1) * MW - 192) + own) = __builtin_nanf("");
+            }
+            if (ADJ > 0 && up)
+                for (int j = 0; j < 32; ++j) Ns[ADJ > 0][own][j] = __builtin_nanf("");
         }
     }
     lds_barrier();
@@ -310,7 +325,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         uint2 k[IQ][NPI][4];
         uint4 q[IR][NPI], m[IM];
     };
-    struct Values { IO v[2][4]; };                          // rows of v, wanted late in their own chunk
+    constexpr bool LATE = NPI == 1 && (AGG || DK == 64 || (DS == 2 && !(SAVE && NP == 3)));
+    struct Values { IO v[2][4]; float gend; };             // rows of v and exp(G_C), wanted in their own chunk
     const uint32_t krow = (uint32_t)p.k.sl * 2, qrow = (uint32_t)p.q.sl * 2, vrow = (uint32_t)p.v_sl * sizeof(IO);
     const uint32_t voff = col_in ? 4 * g4 * vrow + n0 * (uint32_t)sizeof(IO) : kOutside;
     // (a chunk past the segment's end: nothing is read, without a branch that would have to wait for the registers)
@@ -342,6 +358,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) buffer_load(vb, voff + (16 * m + r) * vrow, vs.v[m][r]);
+        if constexpr (!LATE) buffer_load(mb, MATS * 16 - 4 * (96 - 31), vs.gend);
     };
     auto put = [&](typename Lds::Buf &B, const Stage &st) __attribute__((always_inline)) {
 #pragma unroll
@@ -377,7 +394,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             if (MATS % NT == 0 || tid + x * NT < MATS) mats[tid + x * NT] = st.m[x];
     };
 
-    auto step = [&](int64_t ch, Stage &st, const Values &v, Values &vnext) __attribute__((always_inline)) {
+    // What is not finite in v, k or the gates of the chunk (there exp(G) is NaN) must not meet the zeros that stand in T and A for later steps: from a
+    // column's first such step on R and beta, and so U, are taken as zeros, o, what is saved and the state after the chunk as NaN.  LATE: looked for in R;
+    // else at the start of the step, in v and exp(G_C), which then is another copy of the code (`rare`): a branch amid a step costs up to 3 % and 30 registers,
+    // and where they spill 8 % (8 heads of 128 x 128 on 32768 steps, the second walk 151 -> 163 us) or, in float32, 80 %; the other way costs 2 to 4 %.
+    auto step = [&](int64_t ch, Stage &st, const Values &v, Values &vnext, auto rare) __attribute__((always_inline)) {
         const typename Lds::Buf &B = lds.buf[NBUF == 2 ? ch & 1 : 0];
         const int64_t t0 = ch * 32;
         const int n = (int)(sq.len - t0 < 32 ? sq.len - t0 : 32);
@@ -480,6 +501,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) R[m][r] = __builtin_fmaf(-gam[m][r], P[m][r], ONE ? V[m][r] : load_io(&v.v[m][r]));
+        float gend = B.scal[31];
+        bool fix = decltype(rare)::value;
+        if constexpr (LATE) fix = __any(!__builtin_isfinite(((R[0][0] + R[0][1]) + (R[0][2] + R[0][3])) + ((R[1][0] + R[1][1]) + (R[1][2] + R[1][3]))));
+        if (__builtin_expect(fix, 0)) {
+            int bad = 32;
+#pragma unroll
+            for (int t = 7; t >= 0; --t) bad = __builtin_isfinite(R[t >> 2][t & 3]) ? bad : 16 * (t >> 2) + 4 * g4 + (t & 3);
+            bad = min(bad, __shfl_xor(bad, 16, 64));
+            bad = min(bad, __shfl_xor(bad, 32, 64));
+            if (bad < 32) gend = __builtin_nanf("");
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (16 * (t >> 2) + 4 * g4 + (t & 3) >= bad) { R[t >> 2][t & 3] = 0.0f; be[t >> 2][t & 3] = 0.0f; }
+            if constexpr (!AGG)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int column = __shfl(bad, 4 * g4 + r, 64);
+#pragma unroll
+                    for (int m = 0; m < OT; ++m)
+                        if (16 * (first + m) + row16 >= column) Oown[m][r] = Et[m][r] = __builtin_nanf("");
+                }
+        }
         Frag rf[NP];
         split_tiles<NP>(R[0], R[1], rf, neg);
 #pragma unroll
@@ -502,7 +545,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         split_tiles<NP>(D[0], D[1], df, neg);
         if constexpr (!AGG) split_tiles<NPO>(U[0], U[1], uf, neg);
         // S1
-        const float gend = B.scal[31];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -549,18 +591,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         put(lds.buf[NBUF == 2 ? (ch + 1) & 1 : 0], st);
         lds_barrier();
     };
+    auto walk = [&](int64_t ch, Stage &st, const Values &v, Values &vnext) __attribute__((always_inline)) {
+        if constexpr (!LATE) {
+            float whole[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) whole[r] = load_io(&v.v[0][r]) + load_io(&v.v[1][r]);
+            if (__builtin_expect(__any(!__builtin_isfinite(((whole[0] + whole[1]) + (whole[2] + whole[3])) + v.gend)), 0)) return step(ch, st, v, vnext, std::true_type{});
+        }
+        step(ch, st, v, vnext, std::false_type{});
+    };
     Stage st;
     Values va, vb;
     fetch(ch0, st, va);
     put(lds.buf[0], st);                                    // (segments have an even number of chunks)
     lds_barrier();
     if constexpr (SAVE && DS == 1)
-        for (int64_t ch = ch0; ch < ch1; ++ch) step(ch, st, va, va);
+        for (int64_t ch = ch0; ch < ch1; ++ch) walk(ch, st, va, va);
     else
         for (int64_t ch = ch0; ch < ch1;) {                 // two chunks a round, so that no register is copied while it is loaded
-            step(ch, st, va, vb);
+            walk(ch, st, va, vb);
             if (++ch >= ch1) break;
-            step(ch, st, vb, va);
+            walk(ch, st, vb, va);
             ++ch;
         }
     if constexpr (AGG) {
