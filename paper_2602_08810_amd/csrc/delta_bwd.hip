@@ -388,6 +388,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
         }
     };
     // the blocks' units: a slot's largest of each kind, and the others' share of it
+    float zunit = 1.0f;
     float uE = 1.0f, uZ = 1.0f, uD = 1.0f, uA = 1.0f, uB = 1.0f, rE = 1.0f, rZ = 1.0f, rA = 1.0f, rB = 1.0f;
     const int G = p.dvp / 16;
     if constexpr (UNITS) {
@@ -415,6 +416,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
         const float whole = wave_max(__uint_as_float(most));
         if (lane == 0) lds.most[wave] = whole;
         uA = wave_max(rA); uE = wave_max(rE); uB = wave_max(rB); uZ = wave_max(rZ);
+        zunit = rZ;
         rA *= inverse_unit(uA); rE *= inverse_unit(uE); rB *= inverse_unit(uB); rZ *= inverse_unit(uZ);
     }
     if (wave == 0) {
@@ -464,15 +466,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
         lds_barrier();                                  // what was there in LDS has been read
         auto &L = lds.v;
         if constexpr (UNITS) uD = block_unit(fmaxf(fmaxf(lds.most[0], lds.most[1]), fmaxf(lds.most[2], lds.most[3])));
-        uint32_t pE = 0, pZ = 0, pA = 0, pB = 0;
-        if constexpr (UNITS) {                          // brought to the slot's units
-            const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 4) * G, gs = 2 * ks + (sq4 >> 2 & 1) + (8 * sd4 >= DK ? G : 0);
-            const float fE = __shfl(rE, ge, 64), fZ = __shfl(rZ, ge, 64), fA = __shfl(rA, gs, 64), fB = __shfl(rB, gs, 64);
-            pE = pack_f16(fE, fE); pZ = pack_f16(fZ, fZ); pA = pack_f16(fA, fA); pB = pack_f16(fB, fB);
+        uint2 pE = {}, pZ = {}, pA = {}, pB = {};
+        const int ge = 2 * ks + ((tid >> 1) & 1) + (tr >> 4) * G;
+        // Brought to the slot's units, where 11 bits are left of numbers down to 2^-29 of the slot's largest and nothing below 2^-39 (a sum in float32 has
+        // lost such a term by 2^-24).  The power itself may be below what 16 bits hold: two factors, of 2^-14 and 2^-24 at least.
+        if constexpr (UNITS) {
+            const int gs = 2 * ks + (sq4 >> 2 & 1) + (8 * sd4 >= DK ? G : 0);
+            auto factors = [](float f) __attribute__((always_inline)) -> uint2 {
+                const float a = fmaxf(f, 0x1p-14f), b = fminf(f * 0x1p14f, 1.0f);
+                return make_uint2(pack_f16(a, a), pack_f16(b, b));
+            };
+            pE = factors(__shfl(rE, ge, 64)); pZ = factors(__shfl(rZ, ge, 64)); pA = factors(__shfl(rA, gs, 64)); pB = factors(__shfl(rB, gs, 64));
         }
-        auto times = [&](uint32_t x, uint32_t f) __attribute__((always_inline)) -> uint32_t {
-            return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f)) : x;
+        auto times = [&](uint32_t x, uint2 f) __attribute__((always_inline)) -> uint32_t {
+            return UNITS ? __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, f.x) * __builtin_bit_cast(f16x2, f.y)) : x;
         };
+        // dV = beta z, a row's eight columns a thread: of 16 bits as they lie in memory, with their own block's unit
+        auto put_dv = [&](int row, int column, const f32x4 (&z)[2], float f) __attribute__((always_inline)) {
+            if (row >= n) return;
+            IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + row) * p.Hv + h) * p.dv + column;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const f32x4 v = z[x] * f;
+                if (p.o_vec && column + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) if (column + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
+            }
+        };
+        if constexpr (UNITS) {
+            Frag z;
+            z.v = zreg[0];
+            f32x4 zs[2];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) zs[x >> 2][x & 3] = (float)z.h16[x];
+            put_dv(tr, 32 * ks + 8 * (tid & 3), zs, lds.beta[tr] * __shfl(zunit, ge, 64));
+        }
         if constexpr (UNITS) {
             const uint4 e = ereg[0], z = zreg[0];
             *reinterpret_cast<uint4 *>(&L.e[0][tr][tc / 2]) = make_uint4(times(e.x, pE), times(e.y, pE), times(e.z, pE), times(e.w, pE));
@@ -599,14 +628,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
         }
         P1own = mv(dO, e, P1own);
         P2own = mv(z, e, P2own);
-        // dV = beta z, dbeta = z . e
-        f32x4 zs[2] = {}, es[2] = {};
+        // dbeta = z . e
         if constexpr (UNITS) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) dbeta = __builtin_amdgcn_fdot2(z[0].p16[x], e[0].p16[x], dbeta, false);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) zs[x >> 2][x & 3] = (float)z[0].h16[x] * uZ;
-        } else
+        } else {
+            f32x4 zs[2] = {}, es[2] = {};
 #pragma unroll
             for (int x = 0; x < 8; ++x)
 #pragma unroll
@@ -614,19 +641,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
                     zs[x >> 2][x & 3] += __uint_as_float(x & 1 ? z[i].u[x >> 1] & 0xffff0000u : z[i].u[x >> 1] << 16);
                     es[x >> 2][x & 3] += __uint_as_float(x & 1 ? e[i].u[x >> 1] & 0xffff0000u : e[i].u[x >> 1] << 16);
                 }
-        const int c = 32 * ks + 8 * g4;
-        IO *to = reinterpret_cast<IO *>(p.dvv) + ((row0 + (own_in ? own : 0)) * p.Hv + h) * p.dv + c;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            f32x4 v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { if (!UNITS) dbeta = __builtin_fmaf(zs[x][r], es[x][r], dbeta); v[r] = bown * zs[x][r]; }
-            if (own_in) {
-                if (p.o_vec && c + 4 * x + 4 <= p.dv) store4(to + 4 * x, v);
-                else
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) if (c + 4 * x + r < p.dv) store_io(to + 4 * x + r, v[r]);
-            }
+            for (int x = 0; x < 8; ++x) dbeta = __builtin_fmaf(zs[x >> 2][x & 3], es[x >> 2][x & 3], dbeta);
+            put_dv(own, 32 * ks + 8 * g4, zs, bown);
         }
     };
 #pragma unroll 1
