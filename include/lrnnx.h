@@ -554,7 +554,7 @@ size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *args);
 /* Reverse-mode derivative of lrnnx_gated_delta_fwd for upstream gradients dout (of o, strided as o) and, optionally, ds_last
  * (of s_last): dq, dk [B,L,Hk,dk] (summed over the value heads that share them), dv [B,L,Hv,dv] in io_dtype, dg, dbeta
  * [B,L,Hv] in gate_dtype, ds0 [B,Hv,dk,dv] float (optional), all contiguous ([L,H,...] for a packed batch; rows of steps
- * outside every sequence are not written).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
+ * outside every sequence are zeros).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
  * Gradients of g are those of the log decay.  Float32 gradients are accurate to some 1e-7 of their norm, whatever the I/O
  * type; but ds0 of a call without s0, with bfloat16 I/O and gates, to 5e-6.                                              */
 typedef struct lrnnx_delta_bwd_args {

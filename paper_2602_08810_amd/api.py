@@ -1080,7 +1080,8 @@ def lrnnx_gated_delta_fwd(q, k, v, g, beta, scale=None, s0=None, cu_seqlens=None
 
     q, k [B,L,Hk,dk], v [B,L,Hv,dv] float32 or bfloat16, any strides with a contiguous last axis; g (log decay), beta
     [B,L,Hv] float32 or the I/O type; scale: dk ** -0.5 by default.  With `cu_seqlens` (int64 [S+1] on the device) the
-    batch is packed: q, k, v, g, beta, o without the batch axis, s0 and the last state [S,Hv,dk,dv]."""
+    batch is packed: q, k, v, g, beta, o without the batch axis, s0 and the last state [S,Hv,dk,dv]; rows of o outside every
+    sequence are not written (a new o holds anything there)."""
     packed, io = cu_seqlens is not None, v.dtype
     q, k, v, lead, B, Hk, Hv, dk, dv, scale = _delta_head(q, k, v, cu_seqlens, scale)
     code = _io_dtype(v)
@@ -1109,7 +1110,7 @@ def lrnnx_gated_delta_bwd(q, k, v, g, beta, do, saved, scale=None, s0=None, ds_l
                           workspace=None):
     """Gradients of sum(do * o) (and sum(ds_last * s_last)) as a dict: dq, dk, dv in the I/O type, dg, dbeta in the gates'
     type, ds0 float32 if wanted; see lrnnx_delta_bwd_args.  Inputs, scale, s0 and cu_seqlens as in the forward call that
-    returned `saved`."""
+    returned `saved`.  Gradients of steps outside every sequence of a packed batch are zeros."""
     packed, io = cu_seqlens is not None, v.dtype
     gdt, device = g.dtype, v.device
     q, k, v, lead, B, Hk, Hv, dk, dv, scale = _delta_head(q, k, v, cu_seqlens, scale)

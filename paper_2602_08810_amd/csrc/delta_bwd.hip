@@ -321,6 +321,28 @@ template <int NPI, int NPE, int DK> struct GradLds {
     float beta[64], dG[64], ends[4], dots[4], most[4];
 };
 
+// Rows of a packed axis outside every sequence, zeros in the gradients: there are at most as many as slots have steps, and a slot's workgroup clears the 64 of
+// them that come at its place in their order.
+template <class IO> __device__ void clear_outside(const DeltaParams &p, int64_t slot, int h, int hk) {
+    const int64_t lo = delta_clamp(p.cu[0], p.L), end = delta_clamp(p.cu[p.B], p.L), hi = end > lo ? end : lo, count = lo + (p.L - hi) - slot * kDeltaSlot;
+    const bool keys = h % (p.Hv / p.Hk) == 0;
+    for (int i = threadIdx.x >> 6; i < (count < kDeltaSlot ? count : kDeltaSlot); i += 4) {
+        const int64_t at = slot * kDeltaSlot + i, row = at < lo ? at : hi + (at - lo);
+        const int lane = threadIdx.x & 63;
+        for (int c = lane; c < p.dv; c += 64) store_io(reinterpret_cast<IO *>(p.dvv) + (row * p.Hv + h) * p.dv + c, 0.0f);
+        if (keys)
+            for (int c = lane; c < p.dk; c += 64) {
+                store_io(reinterpret_cast<IO *>(p.dq) + (row * p.Hk + hk) * p.dk + c, 0.0f);
+                store_io(reinterpret_cast<IO *>(p.dkk) + (row * p.Hk + hk) * p.dk + c, 0.0f);
+            }
+        if (lane == 0)
+            for (void *gate : {p.dg, p.dbeta}) {
+                if (p.gate_io && p.io) store_io(reinterpret_cast<uint16_t *>(gate) + row * p.Hv + h, 0.0f);
+                else store_io(reinterpret_cast<float *>(gate) + row * p.Hv + h, 0.0f);
+            }
+    }
+}
+
 // NPI: planes of an input, NPE: of E, Z and the states, which lie in memory as float32 (3) or as 16-bit floating point with a power of two a block (1; dO too
 // is brought to that here).
 template <class IO, int NPI, int NPE, int DK>
@@ -339,6 +361,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
     int64_t t0;
     int b;
     const int n = delta_slot(p, slot, sq, t0, b);
+    if (p.cu) clear_outside<IO>(p, slot, h, hk);
     if (n == 0) return;
     const int64_t at = sq.at + t0, row0 = sq.row + t0, rows = (int64_t)(p.cu ? 1 : p.B) * p.L;
     const uint16_t *kp = p.k.p + sq.ib * p.k.sb + at * p.k.sl + hk * p.k.sh, *qp = p.q.p + sq.ib * p.q.sb + at * p.q.sl + hk * p.q.sh;
