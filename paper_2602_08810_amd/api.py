@@ -1039,7 +1039,7 @@ def _out_rows(t, name, shape, dtype):
         if count > 1:
             if stride < need:
                 raise ValueError(f"{name}: output rows overlap")
-            need = stride * count
+            need += stride * (count - 1)
     return r
 
 
