@@ -26,7 +26,7 @@ class GatedDelta(torch.autograd.Function):
     @staticmethod
     def backward(ctx, do):
         *inputs, saved = ctx.saved_tensors
-        r = api.lrnnx_gated_delta_bwd(*inputs, do, saved)
+        r = api.lrnnx_gated_delta_bwd(*inputs, do.contiguous(), saved)
         return r["dq"], r["dk"], r["dv"], r["dg"], r["dbeta"]
 
 
