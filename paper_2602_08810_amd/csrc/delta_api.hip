@@ -113,17 +113,23 @@ template <class A> void set_inputs(const A *a, const Shape &s, DeltaParams &p) {
 }
 
 // Segments of the time axis: walked side by side where the heads alone leave the chip part empty, at the price of a walk with dk more columns before and
-// of chaining (4 us a segment).  32768 steps of 8 heads of 128 x 128, bfloat16: 1640 us in one walk, 16 segments 149 + 62 + 144; 4 x 2048 of 16 heads:
-// 120, in two segments 57 + 13 + 81.
+// of chaining (4 us a segment).  32768 steps of 8 heads of 128 x 128, bfloat16: 1640 us in one walk, 16 segments 149 + 62 + 144.
+// Taken where both walks (the first over as many turns of the chip as its workgroups need, each chunk 1.15 times a single walk's, in float32 1.25) and the
+// chaining, counted in chunks, come to less than one walk's chunks.  Whole calls for prompts, one walk / segments, us, of 128 x 128 in bfloat16: 8 heads 768
+// steps 54 / 61 (one), 1024 68 / 65, 2048 122 / 83; 40 heads 1024 steps 73 / 94 (one), 2048 131 / 136 (one), 4096 246 / 231; float32 8 heads 1024 steps
+// 120 / 97, 40 heads 137 / 178 (one), 4096 575 / 576; 64 x 64 of 64 heads 768 steps 51 / 53 (one), 2048 111 / 86, of 84 heads in float32 4096 steps
+// 469 / 487 (one).
 void plan_segments(const Shape &s, bool packed, Layout &l, DeltaParams &p) {
     p.nseg = 1; p.seg_chunks = 0; p.entry = nullptr; p.trans = nullptr;
     const int64_t heads = (int64_t)s.B * s.Hv, wgs = heads * ((s.dvp + 63) / 64), slots = s.slots_each;
     if (packed) return;
     int64_t n = 256 / wgs;                            // a workgroup a compute unit
-    if (n > slots / 4) n = slots / 4;                 // of 256 steps at least
-    if (n < 3) return;                                // two walks of a half each cost what one walk does
-    const int64_t each = (slots + n - 1) / n;
-    p.nseg = (int)((slots + each - 1) / each); p.seg_chunks = (int)(2 * each);
+    if (n > slots / 4) n = slots / 4;                 // of 256 steps at least (8 heads of 128 x 128, 1024 steps: 4 segments 65 us, 8 of 128 steps 71)
+    if (n < 2) return;
+    const int64_t each = (slots + n - 1) / n, segs = (slots + each - 1) / each;
+    const double turns = (double)(heads * (segs - 1) * ((s.dvp + s.dkp + 63) / 64)) / (s.bf16 && s.dkp == 64 ? 512 : 256);
+    if ((1 + (turns > 1 ? turns : 1)) * 2 * each * (s.bf16 ? 1.15 : 1.25) + 2 * segs + 3 >= 2 * slots) return;
+    p.nseg = (int)segs; p.seg_chunks = (int)(2 * each);
     p.entry = l.take<float>(heads * p.nseg * s.dkp * s.dvp);
     p.trans = l.take<uint16_t>(heads * (p.nseg - 1) * p.np * s.dkp * s.dkp);
 }

@@ -7,7 +7,7 @@ import pytest
 from test_gpu_gated_delta import BF16, F32, _make, _near, _reference, _state, api  # noqa: F401
 
 pytestmark = pytest.mark.gpu
-SHAPES = [(1, 1290, 48, 48, 16, 64), (1, 1290, 12, 48, 96, 33), (2, 1100, 21, 21, 128, 40)]
+SHAPES = [(1, 2570, 24, 24, 16, 64), (1, 2570, 6, 24, 96, 33), (2, 1700, 12, 12, 128, 40)]
 
 
 def _launches(B, L, Hv, dk, dv):
@@ -16,6 +16,8 @@ def _launches(B, L, Hv, dk, dv):
     n = min(256 // (B * Hv * ((dvp + 63) // 64)), slots // 4)
     each = (slots + n - 1) // n
     nseg = (slots + each - 1) // each
+    turns = B * Hv * (nseg - 1) * ((dvp + dkp + 63) // 64) / 256
+    assert (1 + max(1, turns)) * 2 * each * 1.25 + 2 * nseg + 3 < 2 * slots
     return nseg, B * Hv * nseg * ((dvp + 63) // 64), (B * Hv * (nseg - 1) + 7) // 8 * 8 * (((dvp + dkp) // 16 + 3) // 4)
 
 
