@@ -555,6 +555,8 @@ size_t lrnnx_gated_delta_saved_bytes(const lrnnx_delta_fwd_args *args);
  * (of s_last): dq, dk [B,L,Hk,dk] (summed over the value heads that share them), dv [B,L,Hv,dv] in io_dtype, dg, dbeta
  * [B,L,Hv] in gate_dtype, ds0 [B,Hv,dk,dv] float (optional), all contiguous ([L,H,...] for a packed batch; rows of steps
  * outside every sequence are zeros).  Inputs, s0 and cu_seqlens as in the forward call, saved as it left it.
+ * What is not finite in an input, dout or ds_last makes the gradients that come from it not finite, and may make any other
+ * of the head's gradients in the same 64 steps of its sequence NaN (what is in v or dout of a column leaves dv of others).
  * Gradients of g are those of the log decay.  Float32 gradients are accurate to some 1e-7 of their norm, whatever the I/O
  * type; but ds0 of a call without s0, with bfloat16 I/O and gates, to 5e-6.                                              */
 typedef struct lrnnx_delta_bwd_args {

@@ -10,8 +10,8 @@
 // (of a norm over one element the difference is dn eps / (x^2 + eps), which is formed so: as a difference nothing of it would be left)
 // and over all rows dpre_weight = sum dy n2, dres_scale = sum dh m, dpost_weight = sum dp act(gate) n: a workgroup adds up the rows it takes in
 // registers and leaves them in the workspace, a second launch adds up the workgroups in a fixed order.
-// 16384 rows of 2560, bfloat16 with the residual stream in float32: forward 503 MB in 84 us, backward 755 MB in 172 and 7 of sums; gated heads, 16 of 128:
-// 201 MB in 41 and 335 in 72 and 6 (a plain copy does 4.9 TB/s).  Few rows: latency, 5.3 us for 16.
+// 16384 rows of 2560, bfloat16 with the residual stream in float32: forward 503 MB in 85 us (5.9 TB/s), backward 755 MB in 172 (4.4) and 7 of sums; gated
+// heads, 16 of 128: 201 MB in 43 (4.7) and 335 in 74 (4.5) and 6; a copy of these sizes does 5.3 TB/s.  Few rows: latency, 5.0 us for 16.
 #include "block_norm.hpp"
 #include "delta_common.hpp"
 
@@ -75,7 +75,7 @@ __host__ __device__ constexpr int weight_room(int n) { return ((n + 3) & ~3) + 8
 enum : int { GROUP_ROW = 0, GROUP_LANES = 1, GROUP_LDS = 2 };
 
 // Sums over each thread's groups of `x[i]` (piece i of the row lies in one group, `of[i]`), into x (1 past the end of the row).  Through LDS a power of two of neighbouring lanes
-// takes a group, as many as the workgroup has for it (32 groups of 49, training, 2442 rows in bfloat16: 94 us with a lane a group, 70 so).
+// takes a group, as many as the workgroup has for it (2442 rows of 32 groups of 49, gated, bfloat16: 30 us forward and 69 backward with a lane a group, 24 and 48 so).
 template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], const int (&of)[NV], int how, int pieces, int per_group, float *lds, float *part) {
     if (how == GROUP_ROW) {
         float s = 0.0f;
@@ -115,6 +115,7 @@ template <int NV> __device__ __forceinline__ void group_sums(float (&x)[NV], con
     }
 }
 
+// (the reciprocal is the hardware's, 1 ulp)
 template <bool FINE> __device__ __forceinline__ void gate_of(float z, int act, float &a, float &da) {
     const float s = __builtin_amdgcn_rcpf(1.0f + (FINE ? expf(-z) : __expf(-z)));
     if (act) { a = s; da = s * (1.0f - s); }
@@ -340,7 +341,7 @@ template <class IO, class RES, int VEC, int NV, bool BWD> __global__ __launch_bo
             }
         }
     };
-    if constexpr (VEC == 1 && NV > 8) {           // no registers for a second row (4000 rows of 5001: backward 960 us with one, 270 without)
+    if constexpr (VEC == 1 && NV > 8) {           // no registers for a second row (4000 rows of 5001, bfloat16: backward 330 us with one, 178 without)
         for (; row < p.M; row += gridDim.x) {
             take(even);
             even.load(p, row + gridDim.x);

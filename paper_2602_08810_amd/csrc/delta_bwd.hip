@@ -17,7 +17,7 @@ namespace lrnnx {
 
 // ---------------------------------------------------------------- the walk backwards
 // As in the forward walk a wavefront owns 16 columns of dS, or two share them, and everything it computes of them stays in its registers.  Bound by the
-// latency of a chunk: 4 x 4096 steps of 16 heads of 128 x 128, bfloat16, 128 chunks in 257 us (351 with one wavefront to 16 columns).
+// latency of a chunk: 4 x 4096 steps of 16 heads of 128 x 128, bfloat16, 128 chunks in 254 us (343 with one wavefront to 16 columns).
 template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
     struct Buf {
         uint16_t k[NPI][32][DK + 8], kt[NPI][DK][40], qt[NPI][DK][40];
@@ -28,7 +28,7 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct AdjLds {
 };
 
 // DEEP: loads two chunks ahead, for launches of at most a workgroup a compute unit, where registers are there for it and nothing else hides memory
-// (the same with one wavefront to 16 columns: 385 -> 346 us; the forward walk gains nothing by it, with one or two).
+// (the same case: 285 us without; the forward walk gains nothing by it, with one or two wavefronts to 16 columns).
 template <int NPI, int NP, int DK, int DS, bool EXACT, bool AGG, bool DEEP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS == 1 || NP == 3) ? 1 : 2, DEEP && (DS == 1 || NP == 3) ? 1 : 2))) void k_delta_adjoint(const DeltaParams p) {
     constexpr int NT = 256, CW = 4 / DS, KS = DK / 32 / DS, MT = DK / 16 / DS, OT = 2 / DS;          // tiles that are a wavefront's own
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DEEP && (DS
 // orientations of F and H are computed (one as products with the rows of others, one the other way round), which costs less than turning them.
 // The columns of v come through LDS 32 at a time (rows of dO, E, Z and of both states, the next ones under way meanwhile), then K and Q, as rows
 // and turned, in the same place: 72 KB for dk = 128 in bfloat16, two workgroups a compute unit.  Bound by memory: 4 x 4096 steps of 16 heads of
-// 128 x 128, 783 MB in 224 us (3.5 TB/s; a copy would take 158).
+// 128 x 128, 805 MB in 227 us (3.5 TB/s; a copy would take 152); with what is kept in float32 1.21 GB in 466, one workgroup a compute unit (98 KB).
 template <int NPI, int NPE, int DK> struct GradLds {
     static constexpr int ROWS = NPI == 3 ? 0 : 1;
     union {
@@ -855,7 +855,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NPE == 1 ? 
 // dQ and dK of a shared key head: its value heads' parts in their order.  A workgroup takes a quarter of a slot's steps and a key head, a thread four columns; bound
 // by the parts' bytes.  (With a workgroup for all value heads of a key head no parts would be written, but the registers of both sums do not fit
 // beside the rest, and where heads are few the chip is left empty: float32, 239 steps of 12 value heads on 4 of 128 x 128, 2 entries: 280 us a
-// training step so, 170 now.)
+// training step so, 170 with parts.)
 template <class IO, int DK> __global__ __launch_bounds__(256) void k_delta_share(const DeltaParams p) {
     const int64_t slot = blockIdx.x / (unsigned)p.Hk;
     const int hk = (int)(blockIdx.x - slot * p.Hk), d = threadIdx.x % (DK / 4) * 4, share = p.Hv / p.Hk;

@@ -85,8 +85,8 @@ hipError_t launch_delta_gather(const DeltaGather &p, hipStream_t s) {
 // solve: a row of the inverse to a lane, each element found and at once taken off the ones before it (496 multiply-adds a lane that do not wait for each
 // other).  Substitution is stable where powers of N would cancel.  The upper 32 lanes solve for the adjoint's inverse, which is the same with the steps
 // counted from the chunk's end.
-// Bound by what it reads and writes, few chunks by latency: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 20 at the rate of a copy;
-// 4 x 4096 with the adjoint's matrices 61 us of 49 (71 with a wavefront for two chunks); 2 x 77 steps of 6 heads, float32, 9 (11).
+// Bound by what it reads and writes, few chunks by latency: 4 x 2048 steps of 16 heads of 128, bfloat16, 23 us where 100 MB are 19 at the rate of a copy;
+// 4 x 4096 with the adjoint's matrices 61 us of 46 (71 with a wavefront for two chunks); 2 x 77 steps of 6 heads, float32, 9 (11).
 template <int NPI, int NP, int DK, int ADJ> __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NPI == 3 ? 2 : 4))) void k_delta_prep(const DeltaParams p) {
     constexpr int KS = DK / 32, W = 36, NPA = NPI == 3 ? 3 : 2, MW = chunk_words(NP, NPA), AW = chunk_words(ADJ, ADJ);
     __shared__ __align__(16) float Ns[ADJ > 0 ? 2 : 1][32][W];           // N by rows; by columns, both counted from the end
@@ -274,9 +274,9 @@ template <int NPI, int NP, int DK, int NBUF, int DS> struct ScanLds {
 };
 
 // Bound by the latency of a chunk's chain of products and of the rows it brings: 4 x 2048 steps of 16 heads of 128 x 128, bfloat16 with the last state in
-// float32, 64 chunks in 120 us; 4 x 4096 with what the backward pass is left, 269 us where 540 MB are 110 at the rate of a copy.
+// float32, 64 chunks in 124 us; 4 x 4096 with what the backward pass is left, 260 us where 540 MB are 102 at the rate of a copy.
 // DS = 2: two wavefronts share 16 columns, each with half of the rows of S: half of the products and registers each, for one exchange through LDS (the
-// halves of K S0 and Q S0 are added) and twice the workgroups (the two cases above with one wavefront: 133 and 340 us).
+// halves of K S0 and Q S0 are added) and twice the workgroups (the two cases above with one wavefront: 139 and 335 us).
 // AGG: what a segment makes of the state that enters it, S -> M S + N, without outputs: N is the walk from a state of zero, and the columns of M, behind those
 // of v, are walks from the columns of I with v = 0.  k_delta_join then chains the segments, and each is walked again from its true state.
 template <class IO, int NPI, int NP, int DK, int DS, bool SAVE, bool EXACT, bool AGG>
