@@ -1079,7 +1079,7 @@ def lrnnx_gated_delta_fwd(q, k, v, g, beta, scale=None, s0=None, cu_seqlens=None
     buffer that lrnnx_gated_delta_bwd takes; see lrnnx_delta_fwd_args.
 
     q, k [B,L,Hk,dk], v [B,L,Hv,dv] float32 or bfloat16, any strides with a contiguous last axis; g (log decay), beta
-    [B,L,Hv] float32 or the I/O type; scale: dk ** -0.5 by default.  With `cu_seqlens` (int64 [S+1] on the device) the
+    [B,L,Hv] float32 or the I/O type (`saved` is then float32, or with bfloat16 gates 16 bits); scale: dk ** -0.5 by default.  With `cu_seqlens` (int64 [S+1] on the device) the
     batch is packed: q, k, v, g, beta, o without the batch axis, s0 and the last state [S,Hv,dk,dv]; rows of o outside every
     sequence are not written (a new o holds anything there)."""
     packed, io = cu_seqlens is not None, v.dtype

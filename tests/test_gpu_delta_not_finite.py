@@ -111,3 +111,35 @@ def test_what_is_saved_of_earlier_steps(api, io):  # noqa: F811
         assert torch.equal(a["dq"][:, :at], b["dq"][:, :at]) and torch.equal(a["dq"][:, :, 0], b["dq"][:, :, 0])
         assert torch.equal(a["dk"][:, :at], b["dk"][:, :at])
         assert not bool(torch.isfinite(b["dq"][0, at:, 1]).any())
+
+
+@pytest.mark.parametrize("io,gates,states", [("bf16", "io", False), ("bf16", "io", True), ("bf16", None, True), ("f32", None, True), ("f32", None, False)])
+@pytest.mark.parametrize("save", [False, True])
+@pytest.mark.parametrize("B,L,Hk,Hv,dk,dv", [(2, 70, 70, 70, 64, 64), (2, 70, 70, 70, 128, 64), (1, 100, 2, 2, 64, 64), (1, 100, 2, 2, 128, 48), (1, 1100, 1, 1, 64, 96),
+                                            (1, 2570, 24, 24, 16, 64)])
+def test_every_form_of_the_walk(api, io, gates, states, save, B, L, Hk, Hv, dk, dv):  # noqa: F811
+    """With and without states (bfloat16 gates then take two planes), one wavefront to 16 columns or two, in segments of either."""
+    import torch
+    t, s0 = _make(9, (B, L), Hk, Hv, dk, dv, io, gates), _state(10, B, Hv, dk, dv) if states else None
+
+    def run(t):
+        r = api.lrnnx_gated_delta_fwd(**t, s0=s0, return_last_state=states, return_saved=save)
+        return r[0] if isinstance(r, tuple) else r
+
+    clean = run(t)
+    for at in (0, 20, 31, 50, L - 1):
+        for name, what in (("v", NAN), ("v", INF), ("k", NAN), ("beta", INF), ("g", NAN)):
+            bad = {**t, name: t[name].clone()}
+            same = torch.ones_like(clean, dtype=torch.bool)
+            if name == "v":
+                bad["v"][0, at, Hv - 1, dv // 2] = what
+                same[0, at:, Hv - 1, dv // 2] = False
+            elif name == "k":
+                bad["k"][0, at, Hk - 1, dk - 1] = what
+                same[0, at:, Hv - Hv // Hk:] = False
+            else:
+                bad[name][0, at, Hv - 1] = what
+                same[0, at:, Hv - 1] = False
+            o = run(bad)
+            assert torch.equal(o[same], clean[same]), (name, what, at)
+            assert not bool(torch.isfinite(o[~same]).any()), (name, what, at)
