@@ -672,6 +672,166 @@ typedef struct lrnnx_norm_bwd_args {
 int lrnnx_block_norm_bwd(const lrnnx_norm_bwd_args *args);
 size_t lrnnx_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
 
+/* ------------------------------------------------------------------ short causal convolution
+ * What lies before a recurrence: every channel's own convolution over the last W inputs, and an activation,
+ *     pre[b,l,d] = bias[d] + sum_{j < W} weight[d,j] x[b,l-(W-1)+j,d],    y = pre sigmoid(pre)  (act 0)  or  pre  (act 1).
+ * Inputs before the first step are x0[b,l+W-1,d] (l < 0; the last inputs of what came before) or 0.  x_last [B,W-1,D] are the last
+ * W - 1 inputs, x0's among them where there are fewer steps: the x0 of what follows, and the state of lrnnx_short_conv_step.
+ * Two layouts: time_last = 0, x and y [B,L,D] with the channels contiguous (as the gated delta rule takes them; strides of batch entry and
+ * step), or 1, [B,D,L] with the time axis contiguous (as the selective scan does; strides of batch entry and channel).  x, x0, x_last and y in
+ * io_dtype, weight [D,W] and bias [D] (optional) float; x0, x_last contiguous, optional.  2 <= W <= 4; 1 <= D <= 65536; B <= 65535; any L >= 1.
+ * Accesses are made at element alignment.  y must not overlap an input.
+ * Packed variable-length batches: with cu_seqlens != NULL (device memory [B+1], ascending) x and y are one axis of L steps (batch strides
+ * ignored) and sequence b is its steps cu_seqlens[b] .. cu_seqlens[b+1]-1; x0 and x_last stay [B,W-1,D].  Boundaries are clamped to [0,L];
+ * steps outside every sequence are neither read as part of one nor written.  A sequence without steps has x0 (or zeros) for its x_last.
+ * Sums are float32.  Results are bitwise reproducible.                                                                  */
+typedef struct lrnnx_conv_fwd_args {
+    size_t struct_size;
+    int32_t B, D, W;
+    int32_t time_last, act, io_dtype;
+    int64_t L;
+    const int64_t *cu_seqlens;
+    const void *x;      int64_t x_stride_b, x_stride_s;            /* stride_s: of a step (time_last 0) or a channel (1) */
+    const float *weight;
+    const float *bias;                                             /* [D] or NULL */
+    const void *x0;                                                /* [B,W-1,D] or NULL */
+    void *y;            int64_t y_stride_b, y_stride_s;
+    void *x_last;                                                  /* [B,W-1,D] out or NULL */
+    void *stream;
+} lrnnx_conv_fwd_args;
+
+int lrnnx_short_conv_fwd(const lrnnx_conv_fwd_args *args);
+
+/* Its reverse-mode derivative for upstream gradients dy (of y, strided as x is) and, optionally, dx_last (of x_last, contiguous): dx strided as y was,
+ * dweight [D,W] and dbias [D] (optional) float, dx0 [B,W-1,D] in io_dtype (optional; also of a call without x0).  Inputs as in the
+ * forward call, from which pre is formed again.  dx of steps outside every sequence of a packed batch is zero.  The weights' gradients
+ * are summed in a fixed order through the workspace: lrnnx_short_conv_bwd_workspace_bytes(args) bytes, 16-byte aligned.   */
+typedef struct lrnnx_conv_bwd_args {
+    size_t struct_size;
+    int32_t B, D, W;
+    int32_t time_last, act, io_dtype;
+    int64_t L;
+    const int64_t *cu_seqlens;
+    const void *x;      int64_t x_stride_b, x_stride_s;
+    const float *weight;
+    const float *bias;
+    const void *x0;
+    const void *dy;     int64_t dy_stride_b, dy_stride_s;
+    const void *dx_last;                                           /* [B,W-1,D] or NULL */
+    void *dx;           int64_t dx_stride_b, dx_stride_s;
+    float *dweight;
+    float *dbias;                                                  /* [D] out or NULL */
+    void *dx0;                                                     /* [B,W-1,D] out or NULL */
+    void *workspace;    size_t workspace_bytes;
+    void *stream;
+} lrnnx_conv_bwd_args;
+
+int lrnnx_short_conv_bwd(const lrnnx_conv_bwd_args *args);
+size_t lrnnx_short_conv_bwd_workspace_bytes(const lrnnx_conv_bwd_args *args);
+
+/* One step of it (generation): state [B,W-1,D] in io_dtype, contiguous, the last W - 1 inputs, moved on by x IN PLACE; x, y [B,D] with any strides
+ * (y may be x).  L calls give what the forward call gives on L steps.                                                   */
+typedef struct lrnnx_conv_step_args {
+    size_t struct_size;
+    int32_t B, D, W;
+    int32_t act, io_dtype, reserved;
+    const void *x;      int64_t x_stride_b, x_stride_d;
+    const float *weight;
+    const float *bias;
+    void *state;                                                   /* [B,W-1,D] in/out */
+    void *y;            int64_t y_stride_b, y_stride_d;
+    void *stream;
+} lrnnx_conv_step_args;
+
+int lrnnx_short_conv_step(const lrnnx_conv_step_args *args);
+
+/* ------------------------------------------------------------------ loss over a vocabulary
+ * Softmax cross entropy of T rows over V words whose logits are a product, without the logits in memory:
+ *     z[t,v] = sum_k h[t,k] weight[v,k],   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t,target[t]].
+ * h [T,K] and weight [V,K] in io_dtype with row strides, target [T] int64, loss and lse [T] float.  A row whose target is negative has
+ * no loss (0; its lse is there all the same); one whose target is V or more has NaN.  T, V <= 2^27, K <= 2^20.  Rows of 16-byte pieces at
+ * 16-byte steps (bfloat16) are read in place, others are first copied into the workspace, a piece of the vocabulary at a time.
+ * lrnnx_vocab_loss_fwd_workspace_bytes(args) bytes of workspace, 256-byte aligned.  Products run on matrix units and are summed in float32; a float32
+ * number is taken as the sum of three bfloat16 ones, and a product as six of theirs (relative error about 2^-23 of the factors' sizes; their
+ * magnitudes must stay below 3.3e38, what is smaller than 1e-30 loses accuracy).  Results are bitwise reproducible.      */
+typedef struct lrnnx_vocab_fwd_args {
+    size_t struct_size;
+    int64_t T, V;
+    int32_t K, io_dtype;
+    const void *h;          int64_t h_stride;
+    const void *weight;     int64_t weight_stride;
+    const int64_t *target;
+    float *loss;                                                   /* [T] out */
+    float *lse;                                                    /* [T] out */
+    void *workspace;        size_t workspace_bytes;
+    void *stream;
+} lrnnx_vocab_fwd_args;
+
+int lrnnx_vocab_loss_fwd(const lrnnx_vocab_fwd_args *args);
+size_t lrnnx_vocab_loss_fwd_workspace_bytes(const lrnnx_vocab_fwd_args *args);
+
+/* Its reverse-mode derivative for upstream gradients dloss [T] float (element stride dloss_stride; 0: one number for all rows):
+ *     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz weight,   dweight = dz^T h,
+ * dh [T,K] and dweight [V,K] in io_dtype, contiguous; either may be NULL.  Inputs as in the forward call, lse as it left it.  z is
+ * formed again a piece of the vocabulary at a time; a piece of dz, in bfloat16 (with float32 inputs as the sum of three), lies in the
+ * workspace: lrnnx_vocab_loss_bwd_workspace_bytes(args) bytes, 256-byte aligned.  Rows without a target take no part: their dh is zero, and nothing
+ * in them, finite or not, reaches dweight.  Sums are taken in a fixed order: results are bitwise reproducible.            */
+typedef struct lrnnx_vocab_bwd_args {
+    size_t struct_size;
+    int64_t T, V;
+    int32_t K, io_dtype;
+    const void *h;          int64_t h_stride;
+    const void *weight;     int64_t weight_stride;
+    const int64_t *target;
+    const float *lse;
+    const float *dloss;     int64_t dloss_stride;
+    void *dh;                                                      /* [T,K] out or NULL */
+    void *dweight;                                                 /* [V,K] out or NULL */
+    void *workspace;        size_t workspace_bytes;
+    void *stream;
+} lrnnx_vocab_bwd_args;
+
+int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *args);
+size_t lrnnx_vocab_loss_bwd_workspace_bytes(const lrnnx_vocab_bwd_args *args);
+
+/* ------------------------------------------------------------------ norm and clipping of a model's gradients
+ * lrnnx_grad_norm: norm[0] = sqrt(sum of the squares of all elements of all tensors), summed in double precision in a fixed order.
+ * lrnnx_grad_clip: out_i = scale grad_i, scale = min(1, max_norm / (norm[0] + eps)), where norm[0] is what lrnnx_grad_norm left or any other
+ * device float (a norm over several processes).  A norm that is NaN makes everything NaN; an infinite one makes scale 0.
+ * grads, numel, dtype, out, out_dtype are HOST arrays of `count` entries, read before the call returns: device pointers (each on its element size; NULL
+ * where numel is 0), numbers of elements, lrnnx_dtype of each (LRNNX_F32 or LRNNX_BF16).  out NULL: in place (nothing is read or
+ * written where scale is 1); else the types of out may be LRNNX_F32 for any tensor, or the tensor's.  The tensors of out must not overlap each other (a tensor
+ * given twice would be scaled twice) nor another tensor's grad.
+ * lrnnx_grad_norm_workspace_bytes(args) bytes of workspace, 16-byte aligned.  eps >= 0, max_norm >= 0.                */
+typedef struct lrnnx_grad_norm_args {
+    size_t struct_size;
+    int64_t count;
+    const void *const *grads;
+    const int64_t *numel;
+    const int32_t *dtype;
+    float *norm;                                                   /* [1] out, device */
+    void *workspace;        size_t workspace_bytes;
+    void *stream;
+} lrnnx_grad_norm_args;
+
+int lrnnx_grad_norm(const lrnnx_grad_norm_args *args);
+size_t lrnnx_grad_norm_workspace_bytes(const lrnnx_grad_norm_args *args);
+
+typedef struct lrnnx_grad_clip_args {
+    size_t struct_size;
+    int64_t count;
+    void *const *grads;
+    const int64_t *numel;
+    const int32_t *dtype;
+    void *const *out;                                              /* or NULL: in place */
+    const int32_t *out_dtype;                                      /* with out */
+    const float *norm;                                             /* [1] device */
+    float max_norm, eps;
+    void *stream;
+} lrnnx_grad_clip_args;
+
+int lrnnx_grad_clip(const lrnnx_grad_clip_args *args);
+
 /* ------------------------------------------------------------------ queries (host only, no GPU needed) */
 typedef enum { LRNNX_WS_FWD = 0, LRNNX_WS_BWD = 1, LRNNX_WS_LTI = 2, LRNNX_WS_LTI_BWD = 3, LRNNX_WS_DIAG = 4,
                LRNNX_WS_DIAG_BWD = 5, LRNNX_WS_BWD_COMPLEX = 6,

@@ -159,6 +159,48 @@ class NormBwdArgs(ctypes.Structure):              # lrnnx_norm_bwd_args
                 + [(n, _vp) for n in ("dx", "dgate", "dresidual", "dpost_weight", "dres_scale", "dpre_weight")] + _SCRATCH)
 
 
+_CONV_HEAD = [("struct_size", _sz), ("B", _i32), ("D", _i32), ("W", _i32), ("time_last", _i32), ("act", _i32), ("io_dtype", _i32),
+              ("L", _i64), ("cu_seqlens", _vp), *_strided("x", "bs"), ("weight", _vp), ("bias", _vp), ("x0", _vp)]
+
+
+class ConvFwdArgs(ctypes.Structure):              # lrnnx_conv_fwd_args
+    _fields_ = _CONV_HEAD + _strided("y", "bs") + [("x_last", _vp), ("stream", _vp)]
+
+
+class ConvBwdArgs(ctypes.Structure):              # lrnnx_conv_bwd_args
+    _fields_ = (_CONV_HEAD + _strided("dy", "bs") + [("dx_last", _vp)] + _strided("dx", "bs")
+                + [(n, _vp) for n in ("dweight", "dbias", "dx0")] + _SCRATCH)
+
+
+class ConvStepArgs(ctypes.Structure):             # lrnnx_conv_step_args
+    _fields_ = [("struct_size", _sz), ("B", _i32), ("D", _i32), ("W", _i32), ("act", _i32), ("io_dtype", _i32), ("reserved", _i32),
+                *_strided("x", "bd"), ("weight", _vp), ("bias", _vp), ("state", _vp), *_strided("y", "bd"), ("stream", _vp)]
+
+
+_VOCAB_HEAD = [("struct_size", _sz), ("T", _i64), ("V", _i64), ("K", _i32), ("io_dtype", _i32), ("h", _vp), ("h_stride", _i64),
+               ("weight", _vp), ("weight_stride", _i64), ("target", _vp)]
+
+
+class VocabFwdArgs(ctypes.Structure):             # lrnnx_vocab_fwd_args
+    _fields_ = _VOCAB_HEAD + [("loss", _vp), ("lse", _vp)] + _SCRATCH
+
+
+class VocabBwdArgs(ctypes.Structure):             # lrnnx_vocab_bwd_args
+    _fields_ = _VOCAB_HEAD + [("lse", _vp), ("dloss", _vp), ("dloss_stride", _i64), ("dh", _vp), ("dweight", _vp)] + _SCRATCH
+
+
+_GRAD_HEAD = [("struct_size", _sz), ("count", _i64), ("grads", _vp), ("numel", _vp), ("dtype", _vp)]
+
+
+class GradNormArgs(ctypes.Structure):             # lrnnx_grad_norm_args
+    _fields_ = _GRAD_HEAD + [("norm", _vp)] + _SCRATCH
+
+
+class GradClipArgs(ctypes.Structure):             # lrnnx_grad_clip_args
+    _fields_ = _GRAD_HEAD + [("out", _vp), ("out_dtype", _vp), ("norm", _vp), ("max_norm", ctypes.c_float), ("eps", ctypes.c_float),
+                             ("stream", _vp)]
+
+
 def _packer(cls):
     """Packs the values of an argument struct's fields in order (0, not None, stands for NULL).  One call of 0.6 us, where 34
     attributes set one by one take 3.7: the general path of the forward call of 16 rows of 256 steps takes 15.3 us, of a generated
@@ -172,6 +214,9 @@ def _packer(cls):
 _pack_fwd, _pack_bwd, _pack_step = _packer(FwdArgs), _packer(BwdArgs), _packer(StepArgs)
 _pack_delta_fwd, _pack_delta_bwd, _pack_delta_step = _packer(DeltaFwdArgs), _packer(DeltaBwdArgs), _packer(DeltaStepArgs)
 _pack_norm_fwd, _pack_norm_bwd = _packer(NormFwdArgs), _packer(NormBwdArgs)
+_pack_conv_fwd, _pack_conv_bwd, _pack_conv_step = _packer(ConvFwdArgs), _packer(ConvBwdArgs), _packer(ConvStepArgs)
+_pack_vocab_fwd, _pack_vocab_bwd = _packer(VocabFwdArgs), _packer(VocabBwdArgs)
+_pack_grad_norm, _pack_grad_clip = _packer(GradNormArgs), _packer(GradClipArgs)
 _FWD_SIZE, _BWD_SIZE, _STEP_SIZE = ctypes.sizeof(FwdArgs), ctypes.sizeof(BwdArgs), ctypes.sizeof(StepArgs)
 
 _lib = None
@@ -224,10 +269,13 @@ def lib():
         L.lrnnx_status_string.restype = ctypes.c_char_p
         of_bytes, size_of_bytes = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_char_p), ctypes.CFUNCTYPE(_sz, ctypes.c_char_p)
         for n in ("lrnnx_selective_scan_fwd", "lrnnx_selective_scan_bwd", "lrnnx_selective_step", "lrnnx_gated_delta_fwd",
-                  "lrnnx_gated_delta_bwd", "lrnnx_gated_delta_step", "lrnnx_block_norm_fwd", "lrnnx_block_norm_bwd"):
+                  "lrnnx_gated_delta_bwd", "lrnnx_gated_delta_step", "lrnnx_block_norm_fwd", "lrnnx_block_norm_bwd",
+                  "lrnnx_short_conv_fwd", "lrnnx_short_conv_bwd", "lrnnx_short_conv_step", "lrnnx_vocab_loss_fwd", "lrnnx_vocab_loss_bwd",
+                  "lrnnx_grad_norm", "lrnnx_grad_clip"):
             _packed[n] = of_bytes((n, L))
         for n in ("lrnnx_selective_scan_bwd_workspace_bytes", "lrnnx_gated_delta_fwd_workspace_bytes",
-                  "lrnnx_gated_delta_saved_bytes", "lrnnx_gated_delta_bwd_workspace_bytes"):
+                  "lrnnx_gated_delta_saved_bytes", "lrnnx_gated_delta_bwd_workspace_bytes", "lrnnx_short_conv_bwd_workspace_bytes",
+                  "lrnnx_vocab_loss_fwd_workspace_bytes", "lrnnx_vocab_loss_bwd_workspace_bytes", "lrnnx_grad_norm_workspace_bytes"):
             _packed[n] = size_of_bytes((n, L))
         L.lrnnx_block_norm_bwd_workspace_bytes.argtypes = [_i64, _i64]
         L.lrnnx_block_norm_bwd_workspace_bytes.restype = _sz
@@ -1245,3 +1293,247 @@ def lrnnx_block_norm_bwd(x, dh=None, dy=None, post_weight=None, groups=1, gate=N
         *head, *_matrix(dh, "dh", x.shape, (res_dtype,)), *_matrix(dy, "dy", x.shape, (x.dtype,)), *ptrs,
         workspace.data_ptr(), workspace.numel(), _stream())))
     return grads
+
+
+def _on_current(t, name):
+    """Work is enqueued on the current device's stream: tensors of another GPU are refused."""
+    if t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+# ---------------------------------------------------------------- short causal convolution
+CONV_ACT = {"silu": 0, "none": 1}
+CONV_LAYOUT = {"bld": 0, "bdl": 1}
+_CONV_FWD_SIZE, _CONV_BWD_SIZE, _CONV_STEP_SIZE = (ctypes.sizeof(c) for c in (ConvFwdArgs, ConvBwdArgs, ConvStepArgs))
+
+
+def _conv_rows(t, name, shape, io, out=False):
+    """(ptr, stride of a batch entry, of a row) of [B,L,D] or [B,D,L] with a contiguous last axis."""
+    ptr, sb, ss = (_out_rows if out else _rows)(t, name, shape, io)
+    return ptr, sb, ss
+
+
+def _state(t, name, shape, io):
+    """Pointer of optional carried inputs, contiguous in the I/O type."""
+    if t is None:
+        return 0
+    if t.dtype != io or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous {io} tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _conv_head(size, x, weight, bias, act, x0, cu_seqlens, layout):
+    """What the calls over a sequence have in common; the packed form gets a batch axis of one.  x, shape, sequences, W - 1, head."""
+    if x.dim() != (3 if cu_seqlens is None else 2):
+        raise ValueError("x: expected three axes, or two with cu_seqlens")
+    _on_current(x, "x")
+    S = _check_cu(cu_seqlens) if cu_seqlens is not None else None
+    if S is not None:
+        x = x.unsqueeze(0)
+    time_last, io = _code(layout, CONV_LAYOUT), x.dtype
+    shape = x.shape
+    L, D = (shape[2], shape[1]) if time_last else (shape[1], shape[2])
+    B = S if S is not None else shape[0]
+    if weight.dim() != 2:
+        raise ValueError("weight: expected [D,W]")
+    W = weight.shape[1]
+    return x, shape, B, (B, max(W - 1, 0), D), (
+        size, B, D, W, time_last, _code(act, CONV_ACT), _io_dtype(x), L, 0 if S is None else cu_seqlens.data_ptr(),
+        *_conv_rows(x, "x", shape, io), _f32c(weight, "weight", (D, W)), _f32c(bias, "bias", (D,)), _state(x0, "x0", (B, max(W - 1, 0), D), io))
+
+
+@_device_checked
+def lrnnx_short_conv_fwd(x, weight, bias=None, act="silu", x0=None, cu_seqlens=None, layout="bld", return_last_state=False, out=None):
+    """y, and optionally the last W - 1 inputs [B,W-1,D], of the short causal convolution; see lrnnx_conv_fwd_args.
+
+    x [B,L,D] (layout "bld", channels contiguous) or [B,D,L] ("bdl", time axis contiguous) float32 or bfloat16, views of wider tensors
+    among them; weight [D,W] (W = 2 .. 4) and bias [D] float32; act "silu" or "none"; x0 [B,W-1,D] in x's type, the inputs before
+    the first.  With `cu_seqlens` (int64 [S+1] on the device) the batch is packed: x and y without the batch axis, x0 and the last inputs
+    [S,W-1,D]; steps of y outside every sequence are not written (a new y holds anything there).  y must not overlap an input."""
+    packed = cu_seqlens is not None
+    io, device = x.dtype, x.device
+    x, shape, B, state, head = _conv_head(_CONV_FWD_SIZE, x, weight, bias, act, x0, cu_seqlens, layout)
+    y = torch.empty(shape, dtype=io, device=device) if out is None else out.unsqueeze(0) if packed else out
+    last = torch.empty(state, dtype=io, device=device) if return_last_state else None
+    _check(_call("lrnnx_short_conv_fwd", _pack_conv_fwd(*head, *_conv_rows(y, "out", shape, io, out=True), 0 if last is None else last.data_ptr(), _stream())))
+    y = y[0] if packed else y
+    return (y, last) if return_last_state else y
+
+
+@_device_checked
+def lrnnx_short_conv_bwd(x, weight, dy, bias=None, act="silu", x0=None, dx_last=None, want_dx0=False, cu_seqlens=None, layout="bld",
+                         out=None, workspace=None):
+    """Gradients of sum(dy * y) (and sum(dx_last * x_last)) as a dict: dx in x's type (in `out`, if given), dweight and with a bias dbias
+    float32, dx0 in x's type if wanted; see lrnnx_conv_bwd_args.  Inputs as in the forward call.  dx of steps outside every sequence of a
+    packed batch is zero."""
+    packed = cu_seqlens is not None
+    io, device = x.dtype, x.device
+    x, shape, B, state, head = _conv_head(_CONV_BWD_SIZE, x, weight, bias, act, x0, cu_seqlens, layout)
+    pdy = _conv_rows(dy.unsqueeze(0) if packed else dy, "dy", shape, io)
+    dx = torch.empty(shape, dtype=io, device=device) if out is None else out.unsqueeze(0) if packed else out
+    pdx = _conv_rows(dx, "out", shape, io, out=True)
+    res = dict(dx=dx[0] if packed else dx, dweight=torch.empty_like(weight))
+    if bias is not None:
+        res["dbias"] = torch.empty_like(bias)
+    if want_dx0:
+        res["dx0"] = torch.empty(state, dtype=io, device=device)
+    args = (*head, *pdy, _state(dx_last, "dx_last", state, io), *pdx, *(res[n].data_ptr() if n in res else 0 for n in ("dweight", "dbias", "dx0")))
+    workspace = _scratch(workspace, 0 if workspace is not None else _call("lrnnx_short_conv_bwd_workspace_bytes", _pack_conv_bwd(*args, 0, 0, 0)), device)
+    _check(_call("lrnnx_short_conv_bwd", _pack_conv_bwd(*args, workspace.data_ptr(), workspace.numel(), _stream())))
+    return res
+
+
+@_device_checked
+def lrnnx_short_conv_step(x, weight, state, bias=None, act="silu", out=None):
+    """One token: moves the last inputs, state [B,W-1,D] in x's type, on by x in place and returns y [B,D]; see lrnnx_conv_step_args."""
+    io = x.dtype
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x, weight: expected [B,D] and [D,W]")
+    _on_current(x, "x")
+    (B, D), W = x.shape, weight.shape[1]
+    y = torch.empty((B, D), dtype=io, device=x.device) if out is None else out
+    if y.shape != x.shape:
+        raise ValueError(f"out: expected shape {(B, D)}, got {tuple(y.shape)}")
+    if state is None:
+        raise TypeError("state: expected a tensor")
+    _check(_call("lrnnx_short_conv_step", _pack_conv_step(
+        _CONV_STEP_SIZE, B, D, W, _code(act, CONV_ACT), _io_dtype(x), 0, *_bd(x, "x", io), _f32c(weight, "weight", (D, W)),
+        _f32c(bias, "bias", (D,)), _state(state, "state", (B, max(W - 1, 0), D), io), *_bd(y, "out", io), _stream())))
+    return y
+
+
+# ---------------------------------------------------------------- loss over a vocabulary
+_VOCAB_FWD_SIZE, _VOCAB_BWD_SIZE = ctypes.sizeof(VocabFwdArgs), ctypes.sizeof(VocabBwdArgs)
+
+
+def _vocab_head(size, h, weight, target):
+    if h.dim() < 1 or weight.dim() != 2 or weight.shape[1] != h.shape[-1]:
+        raise ValueError("h, weight: expected [..., K] and [V,K]")
+    _on_current(h, "h")
+    if target.dtype != torch.int64 or not target.is_contiguous():
+        raise TypeError("target: expected a contiguous int64 tensor")
+    if target.shape != h.shape[:-1]:
+        raise ValueError(f"target: expected shape {tuple(h.shape[:-1])}, got {tuple(target.shape)}")
+    return (size, target.numel(), weight.shape[0], weight.shape[1], _io_dtype(h), *_matrix(h, "h", h.shape, (h.dtype,)),
+            *_matrix(weight, "weight", weight.shape, (h.dtype,)), target.data_ptr())
+
+
+def _vocab_scratch(name, pack, args, workspace, device):
+    if workspace is None:
+        return torch.empty(max(_call(name, pack(*args, 0, 0, 0)), 16), dtype=torch.uint8, device=device)
+    return _scratch(workspace, 0, device)
+
+
+@_device_checked
+def lrnnx_vocab_loss_fwd(h, weight, target, workspace=None):
+    """(loss, lse): softmax cross entropy of h [..., K] over the words of weight [V,K] (logits h weight^T, which are not kept), and the
+    logarithm of the sum that lrnnx_vocab_loss_bwd takes; see lrnnx_vocab_fwd_args.
+
+    h, weight float32 or bfloat16 with evenly spaced rows; target [...] int64: rows whose target is negative have no loss (0), rows whose
+    target is V or more NaN.  loss and lse [...] float32."""
+    args = _vocab_head(_VOCAB_FWD_SIZE, h, weight, target)
+    loss, lse = (torch.empty(target.shape, dtype=torch.float32, device=h.device) for _ in range(2))
+    args = (*args, loss.data_ptr(), lse.data_ptr())
+    workspace = _vocab_scratch("lrnnx_vocab_loss_fwd_workspace_bytes", _pack_vocab_fwd, args, workspace, h.device)
+    _check(_call("lrnnx_vocab_loss_fwd", _pack_vocab_fwd(*args, workspace.data_ptr(), workspace.numel(), _stream())))
+    return loss, lse
+
+
+@_device_checked
+def lrnnx_vocab_loss_bwd(h, weight, target, lse, dloss, want_dh=True, want_dweight=True, workspace=None):
+    """Gradients of sum(dloss * loss) as a dict: dh [..., K] and dweight [V,K] in the I/O type (each if wanted); see
+    lrnnx_vocab_bwd_args.  h, weight and target as in the forward call, lse as it returned it; dloss [...] float32, contiguous or one
+    number expanded.  dh of rows without a target is zero."""
+    args = _vocab_head(_VOCAB_BWD_SIZE, h, weight, target)
+    if dloss.dtype != torch.float32:
+        raise TypeError("dloss: expected a float32 tensor")
+    if dloss.shape != target.shape:
+        raise ValueError(f"dloss: expected shape {tuple(target.shape)}, got {tuple(dloss.shape)}")
+    if not any(dloss.stride()) and dloss.numel() > 0:
+        step = 0
+    elif dloss.is_contiguous():
+        step = 1
+    else:
+        raise ValueError("dloss: expected a contiguous tensor, or one number expanded")
+    if not want_dh and not want_dweight:
+        raise ValueError("want_dh, want_dweight: one of them is needed")
+    res = {}
+    if want_dh:
+        res["dh"] = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    if want_dweight:
+        res["dweight"] = torch.empty(weight.shape, dtype=h.dtype, device=h.device)
+    args = (*args, _f32c(lse, "lse", target.shape), dloss.data_ptr(), step, *(res[n].data_ptr() if n in res else 0 for n in ("dh", "dweight")))
+    workspace = _vocab_scratch("lrnnx_vocab_loss_bwd_workspace_bytes", _pack_vocab_bwd, args, workspace, h.device)
+    _check(_call("lrnnx_vocab_loss_bwd", _pack_vocab_bwd(*args, workspace.data_ptr(), workspace.numel(), _stream())))
+    return res
+
+
+# ---------------------------------------------------------------- norm and clipping of gradients
+_GRAD_NORM_SIZE, _GRAD_CLIP_SIZE = ctypes.sizeof(GradNormArgs), ctypes.sizeof(GradClipArgs)
+
+
+def _grad_list(grads, name, device=None):
+    """The tensors as a list, with host arrays of their pointers, sizes and types."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError(f"{name}: expected one tensor at least")
+    for t in grads:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected tensors")
+        if device is None:
+            device = t.device
+        if not t.is_cuda or t.device != device:
+            raise TypeError(f"{name}: a tensor is on {t.device}; the library needs tensors of one GPU")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous tensors")
+    _on_current(grads[0], name)
+    n = len(grads)
+    return grads, ((_vp * n)(*(t.data_ptr() for t in grads)), (_i64 * n)(*(t.numel() for t in grads)), (_i32 * n)(*(_io_dtype(t) for t in grads)))
+
+
+def _apart(grads, name):
+    """Tensors that are written must not overlap."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in grads if t.numel())
+    for (_, end), (start, _) in zip(spans, spans[1:]):
+        if start < end:
+            raise ValueError(f"{name}: tensors overlap")
+
+
+@_device_checked
+def lrnnx_grad_norm(grads, workspace=None):
+    """The 2-norm of all elements of a list of tensors together, a float32 tensor without axes; see lrnnx_grad_norm_args.
+    Tensors contiguous, float32 or bfloat16, mixed as they are."""
+    grads, arrays = _grad_list(grads, "grads")
+    device = grads[0].device
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    args = (_GRAD_NORM_SIZE, len(grads), *(ctypes.addressof(a) for a in arrays), norm.data_ptr())
+    workspace = _scratch(workspace, 0 if workspace is not None else _call("lrnnx_grad_norm_workspace_bytes", _pack_grad_norm(*args, 0, 0, 0)), device)
+    _check(_call("lrnnx_grad_norm", _pack_grad_norm(*args, workspace.data_ptr(), workspace.numel(), _stream())))
+    return norm
+
+
+@_device_checked
+def lrnnx_grad_clip(grads, norm, max_norm, eps=1e-6, out=None):
+    """Scales all tensors by min(1, max_norm / (norm + eps)), in place or into the tensors `out` (float32, or each in its type), and returns
+    them; see lrnnx_grad_clip_args.  norm: a float32 tensor of one element, what lrnnx_grad_norm returned or any other (a norm over
+    several processes).  No tensor is waited for."""
+    grads, arrays = _grad_list(grads, "grads")
+    if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != grads[0].device:
+        raise TypeError("norm: expected a float32 tensor of one element on the device of the gradients")
+    outs, to = grads, (0, 0)
+    if out is not None:
+        outs, more = _grad_list(out, "out", grads[0].device)
+        if len(outs) != len(grads):
+            raise ValueError("out: expected as many tensors as grads")
+        for g, o in zip(grads, outs):
+            if o.shape != g.shape:
+                raise ValueError(f"out: expected shape {tuple(g.shape)}, got {tuple(o.shape)}")
+            if o.dtype not in (torch.float32, g.dtype):
+                raise TypeError(f"out: dtype {o.dtype}, expected torch.float32 or {g.dtype}")
+        to = (ctypes.addressof(more[0]), ctypes.addressof(more[2]))
+    _apart(outs, "grads" if out is None else "out")
+    _check(_call("lrnnx_grad_clip", _pack_grad_clip(
+        _GRAD_CLIP_SIZE, len(grads), *(ctypes.addressof(a) for a in arrays), *to, norm.data_ptr(), float(max_norm), float(eps), _stream())))
+    return outs

@@ -1,0 +1,341 @@
+// C ABI of the short causal convolution, the loss over a vocabulary, and the norm and clipping of gradients: argument checks, layout of workspaces, launches.
+// Nothing here allocates, frees or synchronises; see include/lrnnx.h for the contract.
+#include "../../include/lrnnx.h"
+#include "conv.hpp"
+#include "grad_clip.hpp"
+#include "vocab_loss.hpp"
+
+using namespace lrnnx;
+
+namespace {
+
+inline int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline bool on(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline size_t elem(int dtype) { return dtype == LRNNX_BF16 ? 2 : 4; }
+inline bool io_type(int dtype) { return dtype == LRNNX_F32 || dtype == LRNNX_BF16; }
+inline int status(hipError_t e) { return e == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH; }
+
+// ---------------------------------------------------------------- short causal convolution
+template <class A> int conv_checks(const A *a) {
+    if (a->B < 1 || a->D < 1 || a->L < 1 || a->W < 1 || a->act < 0 || a->act > 1 || a->time_last < 0 || a->time_last > 1 || !io_type(a->io_dtype)) return LRNNX_ERR_INVALID_ARG;
+    if (a->W < 2 || a->W > 4 || a->D > 65536 || a->B > 65535) return LRNNX_ERR_UNSUPPORTED;
+    // elements stay countable in tiles of four steps, which are counted in 32 bits
+    if (a->L > ((int64_t)1 << 32) / (a->cu_seqlens ? 1 : a->B)) return LRNNX_ERR_UNSUPPORTED;
+    return LRNNX_OK;
+}
+template <class A> bool conv_inputs(const A *a) {
+    const size_t es = elem(a->io_dtype);
+    return a->x && a->weight && on(a->x, es) && on(a->weight, 4) && on(a->bias, 4) && on(a->x0, es) && on(a->cu_seqlens, 8);
+}
+template <class A> ConvParams conv_params(const A *a, bool backward) {
+    ConvParams p{};
+    p.seqs = a->B; p.B = a->cu_seqlens ? 1 : a->B; p.D = a->D; p.W = a->W; p.L = a->L;
+    p.io = a->io_dtype == LRNNX_BF16; p.act = a->act; p.time_last = a->time_last; p.cu = a->cu_seqlens;
+    p.x = a->x; p.x_b = a->x_stride_b;
+    p.x_l = a->time_last ? 1 : a->x_stride_s; p.x_d = a->time_last ? a->x_stride_s : 1;
+    p.w = a->weight; p.bias = a->bias; p.x0 = a->x0;
+    plan_conv(p, backward);
+    return p;
+}
+size_t conv_sums_bytes(const ConvParams &p) { return (size_t)p.blocks * (p.W + 1) * p.D * sizeof(float); }
+
+}  // namespace
+
+extern "C" {
+
+int lrnnx_short_conv_fwd(const lrnnx_conv_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_conv_fwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = conv_checks(a)) return e;
+    const size_t es = elem(a->io_dtype);
+    if (!conv_inputs(a) || !a->y || !on(a->y, es) || !on(a->x_last, es)) return LRNNX_ERR_INVALID_ARG;
+    ConvParams p = conv_params(a, false);
+    p.y = a->y; p.y_b = a->y_stride_b; p.y_l = a->time_last ? 1 : a->y_stride_s; p.y_d = a->time_last ? a->y_stride_s : 1;
+    p.x_last = a->x_last;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    return status(a->time_last ? launch_conv_time_fwd(p, s) : launch_conv_rows_fwd(p, s));
+}
+
+size_t lrnnx_short_conv_bwd_workspace_bytes(const lrnnx_conv_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_conv_bwd_args) || conv_checks(a) != LRNNX_OK) return 0;
+    return conv_sums_bytes(conv_params(a, true));
+}
+
+int lrnnx_short_conv_bwd(const lrnnx_conv_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_conv_bwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = conv_checks(a)) return e;
+    const size_t es = elem(a->io_dtype);
+    if (!conv_inputs(a) || !a->dy || !a->dx || !a->dweight || (a->dbias && !a->bias)) return LRNNX_ERR_INVALID_ARG;
+    if (!on(a->dy, es) || !on(a->dx, es) || !on(a->dx_last, es) || !on(a->dx0, es) || !on(a->dweight, 4) || !on(a->dbias, 4) || !on(a->workspace, 16)) return LRNNX_ERR_INVALID_ARG;
+    ConvParams p = conv_params(a, true);
+    if (!a->workspace || a->workspace_bytes < conv_sums_bytes(p)) return LRNNX_ERR_WORKSPACE;
+    p.dy = a->dy; p.dy_b = a->dy_stride_b; p.dy_l = a->time_last ? 1 : a->dy_stride_s; p.dy_d = a->time_last ? a->dy_stride_s : 1;
+    p.dx = a->dx; p.y_b = a->dx_stride_b; p.y_l = a->time_last ? 1 : a->dx_stride_s; p.y_d = a->time_last ? a->dx_stride_s : 1;
+    p.dx_last = a->dx_last; p.dx0 = a->dx0; p.dw = a->dweight; p.db = a->dbias;
+    p.sums = reinterpret_cast<float *>(a->workspace);
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    if ((a->time_last ? launch_conv_time_bwd(p, s) : launch_conv_rows_bwd(p, s)) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    return status(launch_conv_sums(p, s));
+}
+
+int lrnnx_short_conv_step(const lrnnx_conv_step_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_conv_step_args)) return LRNNX_ERR_INVALID_ARG;
+    if (a->B < 1 || a->D < 1 || a->W < 1 || a->act < 0 || a->act > 1 || !io_type(a->io_dtype)) return LRNNX_ERR_INVALID_ARG;
+    if (a->W < 2 || a->W > 4 || a->D > 65536 || a->B > 65535) return LRNNX_ERR_UNSUPPORTED;
+    const size_t es = elem(a->io_dtype);
+    if (!a->x || !a->weight || !a->state || !a->y || !on(a->x, es) || !on(a->state, es) || !on(a->y, es) || !on(a->weight, 4) || !on(a->bias, 4)) return LRNNX_ERR_INVALID_ARG;
+    ConvStepParams p{};
+    p.B = a->B; p.D = a->D; p.W = a->W; p.io = a->io_dtype == LRNNX_BF16; p.act = a->act;
+    p.x = a->x; p.x_b = a->x_stride_b; p.x_d = a->x_stride_d; p.w = a->weight; p.bias = a->bias; p.state = a->state;
+    p.y = a->y; p.y_b = a->y_stride_b; p.y_d = a->y_stride_d;
+    return status(launch_conv_step(p, reinterpret_cast<hipStream_t>(a->stream)));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- loss over a vocabulary
+namespace {
+
+template <class A> int vocab_checks(const A *a) {
+    if (a->T < 1 || a->V < 1 || a->K < 1 || !io_type(a->io_dtype)) return LRNNX_ERR_INVALID_ARG;
+    if (a->T > (1 << 27) || a->V > (1 << 27) || a->K > (1 << 20)) return LRNNX_ERR_UNSUPPORTED;
+    if (((a->V + kVocabTile - 1) / kVocabTile) * ((a->T + kVocabTile - 1) / kVocabTile) > (1 << 30)) return LRNNX_ERR_UNSUPPORTED;     // workgroups of a launch
+    return LRNNX_OK;
+}
+template <class A> bool vocab_inputs(const A *a) {
+    const size_t es = elem(a->io_dtype);
+    return a->h && a->weight && a->target && on(a->h, es) && on(a->weight, es) && on(a->target, 8);
+}
+// Rows that the matrix kernels can read as they lie: whole 16-byte pieces at 16-byte steps, 256 of them within 31 bits.
+bool rows_in_place(const void *p, int64_t ld, int K, int io) { return io == LRNNX_BF16 && on(p, 16) && K % 8 == 0 && ld % 8 == 0 && ld >= K && ld <= 1 << 21; }
+
+struct Layout {
+    char *base;
+    size_t at = 0;
+    template <class T> T *take(int64_t count) {
+        const size_t here = (at + 255) / 256 * 256;
+        at = here + (size_t)count * sizeof(T);
+        return base ? reinterpret_cast<T *>(base + here) : nullptr;
+    }
+};
+
+struct VocabPlan {
+    VocabParams p;
+    VocabPack h, w;                      // copies; src null: read in place
+    VocabRows rows;
+    int64_t each;                        // words of a piece
+    size_t bytes;
+};
+
+// The vocabulary is taken in as few pieces as lie in 1 GiB of workspace (a piece's dz; of a copied vocabulary its copy): of whole tiles.
+constexpr int64_t kVocabRoom = (int64_t)1 << 30;
+int64_t piece_of(int64_t words, int64_t bytes_each) {
+    int64_t n = bytes_each > 0 ? kVocabRoom / bytes_each / kVocabTile * kVocabTile : words;
+    if (n > 1 << 21) n = 1 << 21;
+    if (n < kVocabTile) n = kVocabTile;
+    return n < words ? n : words;
+}
+
+template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
+    VocabPlan f{};
+    const int io = a->io_dtype == LRNNX_BF16, planes = io ? 1 : 3;
+    const int64_t Kp = up(a->K, 8);
+    Layout l{ws};
+    VocabParams &p = f.p;
+    p.T = a->T; p.K = a->K; p.planes = planes; p.io = io; p.words = a->V; p.target = a->target;
+    auto copy = [&](VocabPack &k, VocabFactor &to, const void *src, int64_t ld, int64_t rows, bool must) {
+        if (!must && rows_in_place(src, ld, a->K, a->io_dtype)) { to = {reinterpret_cast<const uint16_t *>(src), 0, ld}; return; }
+        k.src = src; k.ld = ld; k.rows = rows; k.plane = rows * Kp; k.K = a->K; k.Kp = (int)Kp; k.io = io; k.planes = planes;
+        k.dst = l.take<uint16_t>(planes * k.plane);
+        to = {k.dst, k.plane, Kp};
+    };
+    const bool copied = !rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype);
+    int64_t each = piece_of(a->V, copied ? planes * Kp * 2 : 0);
+    if (backward) {
+        const int64_t of_dz = piece_of(a->V, planes * a->T * 2);
+        each = of_dz < each ? of_dz : each;
+    }
+    f.each = each;
+    copy(f.h, p.h, a->h, a->h_stride, a->T, backward);
+    copy(f.w, p.w, a->weight, a->weight_stride, each, copied);
+    if (!backward) {
+        p.parts = (a->V + kVocabTile - 1) / kVocabTile;
+        p.part = l.take<float>(2 * p.parts * a->T);
+        p.hit = l.take<float>(a->T);
+    } else {
+        p.ldz = up(each, kVocabTile);
+        p.dz.ld = p.ldz; p.dz.plane = a->T * p.ldz;
+        p.dz.p = l.take<uint16_t>(planes * p.dz.plane);
+        f.rows.index = l.take<int>(a->T);
+        f.rows.place = l.take<int>(a->T);
+        f.rows.count = l.take<int>(1);
+        f.rows.row_lse = l.take<float>(a->T);
+        f.rows.row_scale = l.take<float>(a->T);
+        f.rows.row_target = l.take<int>(a->T);
+        // Stretches of the words that dh is summed over side by side: as many as fill whole turns of the 256 compute units best, each an addition of its part
+        const int64_t tiles = up(a->K, kVocabTile) / kVocabTile * (up(a->T, kVocabTile) / kVocabTile), steps = up(each, kVocabStep) / kVocabStep;
+        double best = 0;
+        p.splits = 1;
+        for (int s = 1; s <= 64 && s * 8 <= steps; ++s) {
+            const double turns = (double)((tiles * s + 255) / 256), use = tiles * s / (256.0 * turns) / (1 + 0.01 * s);
+            if (use > best) { best = use; p.splits = s; }
+        }
+        p.dh_part = l.take<float>(p.splits * a->T * a->K);
+        p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
+        f.h.index = f.rows.index; f.h.count = f.rows.count;
+        f.rows.T = a->T; f.rows.V = a->V; f.rows.target = a->target;
+    }
+    f.bytes = l.at;
+    return f;
+}
+// The piece of the vocabulary from word v0 on, copied if it has to be.
+int vocab_piece(VocabPlan &f, const void *weight, int64_t stride, int64_t v0, hipStream_t s) {
+    VocabParams &p = f.p;
+    p.v0 = v0;
+    p.V = p.words - v0 < f.each ? p.words - v0 : f.each;
+    p.first = v0 == 0;
+    const char *from = reinterpret_cast<const char *>(weight) + v0 * stride * (p.io ? 2 : 4);
+    if (!f.w.src) { p.w.p = reinterpret_cast<const uint16_t *>(from); return LRNNX_OK; }
+    f.w.src = from; f.w.rows = p.V;
+    return status(launch_vocab_pack(f.w, s));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lrnnx_vocab_loss_fwd_workspace_bytes(const lrnnx_vocab_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_vocab_fwd_args) || vocab_checks(a) != LRNNX_OK) return 0;
+    return plan_vocab(a, nullptr, false).bytes;
+}
+
+int lrnnx_vocab_loss_fwd(const lrnnx_vocab_fwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_vocab_fwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = vocab_checks(a)) return e;
+    if (!vocab_inputs(a) || !a->loss || !a->lse || !on(a->loss, 4) || !on(a->lse, 4) || !on(a->workspace, 256)) return LRNNX_ERR_INVALID_ARG;
+    VocabPlan f = plan_vocab(a, reinterpret_cast<char *>(a->workspace), false);
+    if (!a->workspace || a->workspace_bytes < f.bytes) return LRNNX_ERR_WORKSPACE;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    if (f.h.src && launch_vocab_pack(f.h, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    for (int64_t v0 = 0; v0 < a->V; v0 += f.each) {
+        if (const int e = vocab_piece(f, a->weight, a->weight_stride, v0, s)) return e;
+        if (launch_vocab_logits(f.p, false, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    }
+    const VocabLoss end{a->T, a->V, f.p.parts, a->target, f.p.part, f.p.hit, a->loss, a->lse};
+    return status(launch_vocab_loss(end, s));
+}
+
+size_t lrnnx_vocab_loss_bwd_workspace_bytes(const lrnnx_vocab_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_vocab_bwd_args) || vocab_checks(a) != LRNNX_OK) return 0;
+    return plan_vocab(a, nullptr, true).bytes;
+}
+
+int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_vocab_bwd_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = vocab_checks(a)) return e;
+    const size_t es = elem(a->io_dtype);
+    if (!vocab_inputs(a) || !a->lse || !a->dloss || (!a->dh && !a->dweight)) return LRNNX_ERR_INVALID_ARG;
+    if (!on(a->lse, 4) || !on(a->dloss, 4) || !on(a->dh, es) || !on(a->dweight, es) || !on(a->workspace, 256)) return LRNNX_ERR_INVALID_ARG;
+    VocabPlan f = plan_vocab(a, reinterpret_cast<char *>(a->workspace), true);
+    if (!a->workspace || a->workspace_bytes < f.bytes) return LRNNX_ERR_WORKSPACE;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    f.rows.lse = a->lse; f.rows.dloss = a->dloss; f.rows.dloss_stride = a->dloss_stride;
+    if (launch_vocab_rows(f.rows, s) != hipSuccess || launch_vocab_pack(f.h, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    f.p.dw = a->dweight;
+    for (int64_t v0 = 0; v0 < a->V; v0 += f.each) {
+        if (const int e = vocab_piece(f, a->weight, a->weight_stride, v0, s)) return e;
+        if (launch_vocab_logits(f.p, true, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+        if (a->dh && launch_vocab_dh(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+        if (a->dweight && launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    }
+    if (!a->dh) return LRNNX_OK;
+    const VocabDh end{a->T, a->K, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
+    return status(launch_vocab_dh_out(end, s));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- norm and clipping
+namespace {
+
+// Elements of a piece: about 4096 pieces in all, of 8192 elements at least (few pieces for the second launch to add, 16 workgroups a compute unit).
+int64_t grad_piece(const int64_t *numel, int64_t count, int64_t &pieces) {
+    int64_t total = 0;
+    for (int64_t i = 0; i < count; ++i) total += numel[i];
+    int64_t n = up(total / 4096, 2048);
+    n = n < 8192 ? 8192 : n > 1 << 24 ? 1 << 24 : n;
+    pieces = 0;
+    for (int64_t i = 0; i < count; ++i) pieces += (numel[i] + n - 1) / n;
+    return n;
+}
+template <class A> int grad_checks(const A *a) {
+    if (a->count < 1 || !a->grads || !a->numel || !a->dtype) return LRNNX_ERR_INVALID_ARG;
+    int64_t total = 0;
+    for (int64_t i = 0; i < a->count; ++i) {
+        if (a->numel[i] < 0 || !io_type(a->dtype[i])) return LRNNX_ERR_INVALID_ARG;
+        if (a->numel[i] > ((int64_t)1 << 44) || (total += a->numel[i]) > ((int64_t)1 << 44)) return LRNNX_ERR_UNSUPPORTED;
+        if (a->numel[i] && (!a->grads[i] || !on(a->grads[i], elem(a->dtype[i])))) return LRNNX_ERR_INVALID_ARG;
+    }
+    return LRNNX_OK;
+}
+// `launch` on lists of the tensors that have elements; false if it fails
+template <class A, class F> bool grad_lists(const A *a, void *const *out, const int32_t *out_dtype, int64_t piece, F launch) {
+    GradList l;
+    l.count = 0; l.piece = (int)piece; l.base = 0; l.first[0] = 0;
+    for (int64_t i = 0; i < a->count; ++i) {
+        if (a->numel[i]) {
+            const int k = l.count++;
+            l.g[k] = a->grads[i];
+            l.out[k] = out ? out[i] : const_cast<void *>(static_cast<const void *>(a->grads[i]));
+            l.n[k] = a->numel[i];
+            l.io[k] = (uint8_t)((a->dtype[i] == LRNNX_BF16 ? 1 : 0) | ((out ? out_dtype[i] : a->dtype[i]) == LRNNX_BF16 ? 2 : 0));
+            l.first[k + 1] = l.first[k] + (uint32_t)((a->numel[i] + piece - 1) / piece);
+        }
+        if (l.count == kGradTensors || (i + 1 == a->count && l.count)) {
+            if (launch(l) != hipSuccess) return false;
+            l.base += l.first[l.count];
+            l.count = 0;
+        }
+    }
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lrnnx_grad_norm_workspace_bytes(const lrnnx_grad_norm_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_grad_norm_args) || a->count < 1 || !a->numel) return 0;
+    int64_t pieces;
+    grad_piece(a->numel, a->count, pieces);
+    return (size_t)pieces * sizeof(double);
+}
+
+int lrnnx_grad_norm(const lrnnx_grad_norm_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_grad_norm_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = grad_checks(a)) return e;
+    if (!a->norm || !on(a->norm, 4) || !on(a->workspace, 16)) return LRNNX_ERR_INVALID_ARG;
+    int64_t pieces;
+    const int64_t piece = grad_piece(a->numel, a->count, pieces);
+    if (pieces && (!a->workspace || a->workspace_bytes < (size_t)pieces * sizeof(double))) return LRNNX_ERR_WORKSPACE;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    double *sums = reinterpret_cast<double *>(a->workspace);
+    if (!grad_lists(a, nullptr, nullptr, piece, [&](const GradList &l) { return launch_grad_squares(l, sums, s); })) return LRNNX_ERR_LAUNCH;
+    return status(launch_grad_total(sums, (uint32_t)pieces, a->norm, s));
+}
+
+int lrnnx_grad_clip(const lrnnx_grad_clip_args *a) {
+    if (!a || a->struct_size != sizeof(lrnnx_grad_clip_args)) return LRNNX_ERR_INVALID_ARG;
+    if (const int e = grad_checks(a)) return e;
+    if (!a->norm || !on(a->norm, 4) || !(a->max_norm >= 0.0f) || !(a->eps >= 0.0f) || (a->out && !a->out_dtype)) return LRNNX_ERR_INVALID_ARG;
+    if (a->out)
+        for (int64_t i = 0; i < a->count; ++i) {
+            if (a->out_dtype[i] != LRNNX_F32 && a->out_dtype[i] != a->dtype[i]) return LRNNX_ERR_INVALID_ARG;
+            if (a->numel[i] && (!a->out[i] || !on(a->out[i], elem(a->out_dtype[i])))) return LRNNX_ERR_INVALID_ARG;
+        }
+    int64_t pieces;
+    const int64_t piece = grad_piece(a->numel, a->count, pieces);
+    const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    return grad_lists(a, a->out, a->out_dtype, piece, [&](const GradList &l) { return launch_grad_scale(l, a->norm, a->max_norm, a->eps, !a->out, s); }) ? LRNNX_OK : LRNNX_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,76 @@
+// Host-visible parameter blocks and launcher declarations of the loss over a vocabulary.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lrnnx {
+
+constexpr int kVocabTile = 256;          // rows and columns of a product's tile
+constexpr int kVocabStep = 64;           // terms of its sums taken at a time
+
+// A factor of a matrix product in bfloat16, `planes` numbers to an element (a float32 element is the sum of three): element (plane, row, column) at
+// plane * plane_stride + row * ld + column.  16-byte aligned rows of whole 16-byte pieces.
+struct VocabFactor {
+    const uint16_t *p;
+    int64_t plane, ld;
+};
+
+struct VocabParams {
+    int64_t T, V, K, ldz;                // V: words of this piece; ldz: row stride of dz, V up to whole tiles
+    int planes, io;                      // io 1: bfloat16
+    const int *count;                    // device: rows that have a target (null: all T)
+    VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]
+    int64_t v0, words;                   // first word of this piece, words in all
+    // forward
+    float *part;                         // [T, tiles of all words, 2]: largest, sum
+    int64_t parts;
+    float *hit;                          // [T] z of the target
+    const int64_t *target;
+    // backward, by row among those that have a target
+    const float *row_lse, *row_scale;
+    const int *row_target;               // -1: beyond the vocabulary
+    float *dh_part;                      // [splits,T,K]
+    int splits, first;                   // first piece: the parts are set, not added to
+    void *dw;                            // [words,K]
+};
+hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s);
+hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s);
+hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s);
+
+// [rows,K] strided elements as a factor with Kp columns, zeros behind the K-th; `index`: the source's row of each (and `count` rows)
+struct VocabPack {
+    const void *src; int64_t ld;
+    uint16_t *dst; int64_t plane, rows;
+    int K, Kp, io, planes;
+    const int *index, *count;
+};
+hipError_t launch_vocab_pack(const VocabPack &p, hipStream_t s);
+
+struct VocabRows {
+    int64_t T, V;
+    const int64_t *target;
+    const float *lse, *dloss; int64_t dloss_stride;
+    int *index, *place, *count;          // row of the T that the i-th with a target is; place: the other way, -1: none
+    float *row_lse, *row_scale;
+    int *row_target;
+};
+hipError_t launch_vocab_rows(const VocabRows &p, hipStream_t s);
+
+struct VocabLoss {
+    int64_t T, V, parts;
+    const int64_t *target;
+    const float *part, *hit;
+    float *loss, *lse;
+};
+hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s);
+
+struct VocabDh {
+    int64_t T;
+    int K, io, splits;
+    const float *part;
+    const int *place;
+    void *dh;
+};
+hipError_t launch_vocab_dh_out(const VocabDh &p, hipStream_t s);
+
+}  // namespace lrnnx

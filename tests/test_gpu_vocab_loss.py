@@ -1,0 +1,164 @@
+"""GPU tests of the loss over a vocabulary against a plain implementation in 64 bits on the same (rounded) inputs.
+
+Tolerances, of the 2-norm of each tensor.  A logit is a sum of up to 771 products in float32 on the matrix units (32 at a time): 6e-8 * sqrt(771 / 32) of
+its terms' size, 3e-7; its exponential is off by as much and by the hardware's 1e-7 (1 + |z|), |z| < 10, their logarithm's sum by less: lse and loss 2e-6.
+Gradients in float32: the exponentials' 1.5e-6, sums like the logits': held to 5e-6.  In bfloat16 dz is rounded (rms 1.7e-3 of it, independent errors) and the
+result too: 1.7e-3 * sqrt(2) = 2.4e-3, held to 4e-3."""
+import pytest
+
+from _train_ref import vocab
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def api():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2602_08810_amd import api as _api
+    _api.lib()
+    return _api
+
+
+def _make(seed, T, V, K, io, none=0.3):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    w = (torch.randn(V, K, generator=g) * 1.5 * K ** -0.5).to(dt)
+    target = torch.randint(0, V, (T,), generator=g)
+    h = (torch.randn(T, K, generator=g) + 3 * torch.rand(T, 1, generator=g) * w[target].float()).to(dt)
+    target[torch.rand(T, generator=g) < none] = -100
+    return h, w, target, torch.rand(T, generator=g) + 0.1
+
+
+def _check(got, want, name, tol=None):
+    import torch
+    tol = tol or (4e-3 if got.dtype == torch.bfloat16 else 5e-6 if name.startswith("d") else 2e-6)
+    got = got.double().cpu()
+    assert got.shape == want.shape, name
+    e = ((got - want).norm() / want.norm().clamp(min=1e-300)).item()
+    assert e <= tol, f"{name}: relative error {e:.2e}, tolerance {tol:g}"
+
+
+def _both(api, h, w, target, dloss):
+    loss, lse = api.lrnnx_vocab_loss_fwd(h.cuda(), w.cuda(), target.cuda())
+    r = api.lrnnx_vocab_loss_bwd(h.cuda(), w.cuda(), target.cuda(), lse, dloss.cuda())
+    want = vocab(h.double(), w.double(), target, dloss.double())
+    for n, got, ref in zip(("loss", "lse", "dh", "dweight"), (loss, lse, r["dh"], r["dweight"]), want):
+        _check(got, ref, n)
+    return loss, lse, r
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,K", [(1, 1, 1), (1, 300, 64), (3, 5, 7), (5, 256, 8), (17, 257, 72), (64, 1000, 128), (255, 255, 136), (257, 513, 64),
+                                   (300, 771, 200), (70, 2000, 771), (600, 300, 330), (33, 3500, 65)])
+def test_sizes(api, io, T, V, K):
+    _both(api, *_make(T + V + K, T, V, K, io))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("none", [0.0, 1.0, 0.97])
+def test_rows_without_a_target(api, io, none):
+    h, w, target, dloss = _make(1, 270, 300, 96, io, none)
+    loss, lse, r = _both(api, h, w, target, dloss)
+    there = (target >= 0).cuda()
+    assert not bool(loss[~there].any()) and not bool(r["dh"][~there].any())
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_what_is_not_finite_stays_in_its_row(api, io):
+    import torch
+    h, w, target, dloss = _make(2, 40, 300, 64, io)
+    clean = _both(api, h, w, target, dloss)
+    target[7], target[9] = -1, -5
+    without = _both(api, h, w, target, dloss)
+    h[7], h[9], dloss[9] = float("nan"), float("inf"), float("nan")              # rows without a target
+    loss, lse = api.lrnnx_vocab_loss_fwd(h.cuda(), w.cuda(), target.cuda())
+    r = api.lrnnx_vocab_loss_bwd(h.cuda(), w.cuda(), target.cuda(), lse, dloss.cuda())
+    keep = [i for i in range(40) if i not in (7, 9)]
+    assert torch.equal(loss, without[0]) and torch.equal(lse[keep], without[1][keep])
+    assert torch.equal(r["dh"], without[2]["dh"]) and torch.equal(r["dweight"], without[2]["dweight"])
+    h, w, target, dloss = _make(2, 40, 300, 64, io)
+    target[3] = 300                                        # beyond the vocabulary: its row is lost, no other
+    loss, lse = api.lrnnx_vocab_loss_fwd(h.cuda(), w.cuda(), target.cuda())
+    r = api.lrnnx_vocab_loss_bwd(h.cuda(), w.cuda(), target.cuda(), lse, dloss.cuda())
+    keep = [i for i in range(40) if i != 3]
+    assert torch.equal(loss[keep], clean[0][keep]) and torch.equal(lse, clean[1]) and bool(torch.isnan(loss[3]))
+    assert torch.equal(r["dh"][keep], clean[2]["dh"][keep]) and bool(torch.isnan(r["dh"][3]).all()) and bool(torch.isnan(r["dweight"]).all())
+
+
+def test_logits_far_apart(api):
+    import torch
+    w = torch.zeros(600, 8, dtype=torch.bfloat16)
+    w[:, 0] = torch.linspace(-300, 300, 600)
+    h = torch.zeros(3, 8, dtype=torch.bfloat16)
+    h[0, 0], h[1, 0], h[2, 0] = 1.0, -256.0, 0.0
+    target = torch.tensor([599, 5, 17])
+    _both(api, h, w, target, torch.ones(3))
+
+
+def test_strided_rows_and_one_gradient(api):
+    import torch
+    for io in ("f32", "bf16"):
+        h, w, target, dloss = (t.cuda() for t in _make(3, 24, 520, 72, io))
+        loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+        want = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
+        for room, at in ((80, 8), (100, 3)):
+            hs, ws = (torch.full((t.shape[0], room), float("nan"), dtype=t.dtype, device="cuda")[:, at:at + 72] for t in (h, w))
+            hs.copy_(h)
+            ws.copy_(w)
+            l2, e2 = api.lrnnx_vocab_loss_fwd(hs, ws, target)
+            assert torch.equal(l2, loss) and torch.equal(e2, lse)
+            one = api.lrnnx_vocab_loss_bwd(hs, ws, target, lse, dloss, want_dweight=False)
+            other = api.lrnnx_vocab_loss_bwd(hs, ws, target, lse, dloss, want_dh=False)
+            assert set(one) == {"dh"} and set(other) == {"dweight"}
+            assert torch.equal(one["dh"], want["dh"]) and torch.equal(other["dweight"], want["dweight"])
+        l3, e3 = api.lrnnx_vocab_loss_fwd(h.view(4, 6, 72), w, target.view(4, 6))
+        assert l3.shape == (4, 6) and torch.equal(l3.view(24), loss)
+        mean = torch.full((), 0.125, device="cuda").expand(24)
+        full = api.lrnnx_vocab_loss_bwd(h, w, target, lse, mean.contiguous())
+        assert all(torch.equal(v, full[n]) for n, v in api.lrnnx_vocab_loss_bwd(h, w, target, lse, mean).items())
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_reproducible_on_another_stream_and_in_a_graph(api, io):
+    import torch
+    h, w, target, dloss = (t.cuda() for t in _make(5, 300, 700, 100, io))
+
+    def run():
+        loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+        return [loss, lse, *api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss).values()]
+    first = run()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        again = run()
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(first, again))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for i in range(3):
+        h.copy_(torch.randn(h.shape, device="cuda"))
+        target.copy_(torch.randint(-200, 700, target.shape, device="cuda"))       # another number of rows with a target
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), i
+
+
+def test_gradients_are_differences(api):
+    """Central differences of the loss in float32 along random directions: the loss is off by 2e-6 of 30 rows' sum (about 1e-4 at a step of 0.05 either way: 1e-3 of the
+    difference quotient, whose curvature adds as much)."""
+    import torch
+    h, w, target, dloss = _make(6, 30, 400, 48, "f32")
+    run = lambda a, b: (api.lrnnx_vocab_loss_fwd(a.cuda(), b.cuda(), target.cuda())[0].double().cpu() * dloss).sum()
+    lse = api.lrnnx_vocab_loss_fwd(h.cuda(), w.cuda(), target.cuda())[1]
+    r = api.lrnnx_vocab_loss_bwd(h.cuda(), w.cuda(), target.cuda(), lse, dloss.cuda())
+    for n, t in (("dh", h), ("dweight", w)):
+        d = r[n].cpu() / r[n].cpu().norm()                 # along the gradient itself
+        step = 0.05
+        up, down = ((h + s * d, w) if n == "dh" else (h, w + s * d) for s in (step, -step))
+        want = (r[n].cpu().double() * d).sum()
+        assert abs((run(*up) - run(*down)) / (2 * step) - want) < 4e-3 * want, n
