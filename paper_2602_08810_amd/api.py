@@ -285,7 +285,9 @@ def lib():
             "selective_scan_bwd_complex", "selective_step", "selective_step_complex", "lti_diag_scan", "lti_diag_scan_bwd",
             "diag_scan", "diag_scan_bwd", "workspace_bytes", "gated_delta_fwd", "gated_delta_fwd_workspace_bytes", "gated_delta_saved_bytes",
             "gated_delta_bwd", "gated_delta_bwd_workspace_bytes", "gated_delta_step", "block_norm_fwd", "block_norm_bwd",
-            "block_norm_bwd_workspace_bytes")))
+            "block_norm_bwd_workspace_bytes", "short_conv_fwd", "short_conv_bwd", "short_conv_bwd_workspace_bytes", "short_conv_step",
+            "vocab_loss_fwd", "vocab_loss_fwd_workspace_bytes", "vocab_loss_bwd", "vocab_loss_bwd_workspace_bytes", "grad_norm",
+            "grad_norm_workspace_bytes", "grad_clip")))
         _lib = L
         _native = _binding
     return _lib
@@ -1344,7 +1346,7 @@ def _conv_head(size, x, weight, bias, act, x0, cu_seqlens, layout):
         *_conv_rows(x, "x", shape, io), _f32c(weight, "weight", (D, W)), _f32c(bias, "bias", (D,)), _state(x0, "x0", (B, max(W - 1, 0), D), io))
 
 
-@_device_checked
+@_native_first
 def lrnnx_short_conv_fwd(x, weight, bias=None, act="silu", x0=None, cu_seqlens=None, layout="bld", return_last_state=False, out=None):
     """y, and optionally the last W - 1 inputs [B,W-1,D], of the short causal convolution; see lrnnx_conv_fwd_args.
 
@@ -1362,7 +1364,7 @@ def lrnnx_short_conv_fwd(x, weight, bias=None, act="silu", x0=None, cu_seqlens=N
     return (y, last) if return_last_state else y
 
 
-@_device_checked
+@_native_first
 def lrnnx_short_conv_bwd(x, weight, dy, bias=None, act="silu", x0=None, dx_last=None, want_dx0=False, cu_seqlens=None, layout="bld",
                          out=None, workspace=None):
     """Gradients of sum(dy * y) (and sum(dx_last * x_last)) as a dict: dx in x's type (in `out`, if given), dweight and with a bias dbias
@@ -1385,7 +1387,7 @@ def lrnnx_short_conv_bwd(x, weight, dy, bias=None, act="silu", x0=None, dx_last=
     return res
 
 
-@_device_checked
+@_native_first
 def lrnnx_short_conv_step(x, weight, state, bias=None, act="silu", out=None):
     """One token: moves the last inputs, state [B,W-1,D] in x's type, on by x in place and returns y [B,D]; see lrnnx_conv_step_args."""
     io = x.dtype
@@ -1426,7 +1428,7 @@ def _vocab_scratch(name, pack, args, workspace, device):
     return _scratch(workspace, 0, device)
 
 
-@_device_checked
+@_native_first
 def lrnnx_vocab_loss_fwd(h, weight, target, workspace=None):
     """(loss, lse): softmax cross entropy of h [..., K] over the words of weight [V,K] (logits h weight^T, which are not kept), and the
     logarithm of the sum that lrnnx_vocab_loss_bwd takes; see lrnnx_vocab_fwd_args.
@@ -1441,7 +1443,7 @@ def lrnnx_vocab_loss_fwd(h, weight, target, workspace=None):
     return loss, lse
 
 
-@_device_checked
+@_native_first
 def lrnnx_vocab_loss_bwd(h, weight, target, lse, dloss, want_dh=True, want_dweight=True, workspace=None):
     """Gradients of sum(dloss * loss) as a dict: dh [..., K] and dweight [V,K] in the I/O type (each if wanted); see
     lrnnx_vocab_bwd_args.  h, weight and target as in the forward call, lse as it returned it; dloss [...] float32, contiguous or one
@@ -1501,7 +1503,7 @@ def _apart(grads, name):
             raise ValueError(f"{name}: tensors overlap")
 
 
-@_device_checked
+@_native_first
 def lrnnx_grad_norm(grads, workspace=None):
     """The 2-norm of all elements of a list of tensors together, a float32 tensor without axes; see lrnnx_grad_norm_args.
     Tensors contiguous, float32 or bfloat16, mixed as they are."""
@@ -1514,7 +1516,7 @@ def lrnnx_grad_norm(grads, workspace=None):
     return norm
 
 
-@_device_checked
+@_native_first
 def lrnnx_grad_clip(grads, norm, max_norm, eps=1e-6, out=None):
     """Scales all tensors by min(1, max_norm / (norm + eps)), in place or into the tensors `out` (float32, or each in its type), and returns
     them; see lrnnx_grad_clip_args.  norm: a float32 tensor of one element, what lrnnx_grad_norm returned or any other (a norm over

@@ -4,7 +4,7 @@
 // What bounds it: small calls are bound by the host, since their kernels take 3 to 6 us.  Marshalled in Python, the
 // forward call of 16 rows of 256 steps took 15.7 us and a generated token of 64 x 1536 channels 11.2, here 6.6 and 5.0 (its
 // kernel's time); training steps, forward and backward: 16 rows of 256 steps 58.6 and 27.4, packed 76 and 35, complex 54 and 35; the
-// chained scans and their adjoints 28 and 18.  What is left is the allocation of the outputs and the launches.
+// chained scans and their adjoints 28 and 18; a token of the short convolution 9.9 and ?; norm and clipping of 26 tensors 72 and ?.  What is left is the allocation of the outputs and the launches.
 //
 // A call is taken only where every argument has the usual form: plain strided GPU tensors on the current device with the
 // expected types and shapes, contiguous where the general path looks no further, no caller-supplied scratch,
@@ -26,6 +26,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <utility>
+#include <vector>
 
 #include "../../include/lrnnx.h"
 
@@ -54,6 +56,17 @@ struct {
     decltype(&lrnnx_block_norm_fwd) norm_fwd;
     decltype(&lrnnx_block_norm_bwd) norm_bwd;
     decltype(&lrnnx_block_norm_bwd_workspace_bytes) norm_bwd_bytes;
+    decltype(&lrnnx_short_conv_fwd) conv_fwd;
+    decltype(&lrnnx_short_conv_bwd) conv_bwd;
+    decltype(&lrnnx_short_conv_bwd_workspace_bytes) conv_bwd_bytes;
+    decltype(&lrnnx_short_conv_step) conv_step;
+    decltype(&lrnnx_vocab_loss_fwd) vocab_fwd;
+    decltype(&lrnnx_vocab_loss_fwd_workspace_bytes) vocab_fwd_bytes;
+    decltype(&lrnnx_vocab_loss_bwd) vocab_bwd;
+    decltype(&lrnnx_vocab_loss_bwd_workspace_bytes) vocab_bwd_bytes;
+    decltype(&lrnnx_grad_norm) grad_norm;
+    decltype(&lrnnx_grad_norm_workspace_bytes) grad_norm_bytes;
+    decltype(&lrnnx_grad_clip) grad_clip;
 } lib = {};
 constexpr int kEntries = sizeof(lib) / sizeof(void *);
 int64_t ckpt_interval = 0;
@@ -89,6 +102,14 @@ Names kDeltaStep = {8, {"q", "k", "v", "g", "beta", "state", "scale", "out"}, {}
 enum { N_X, N_POST, N_GROUPS, N_GATE, N_ACT, N_RES, N_SCALE, N_PRE, N_EPS, N_OUT };
 Names kNormFwd = {10, {"x", "post_weight", "groups", "gate", "gate_act", "residual", "res_scale", "pre_weight", "eps", "out"}, {}};
 Names kNormBwd = {12, {"x", "dh", "dy", "post_weight", "groups", "gate", "gate_act", "residual", "res_scale", "pre_weight", "eps", "workspace"}, {}};
+enum { V_X, V_W, V_BIAS, V_ACT, V_X0, V_CU, V_LAYOUT, V_LAST, V_OUT };
+Names kConvFwd = {9, {"x", "weight", "bias", "act", "x0", "cu_seqlens", "layout", "return_last_state", "out"}, {}};
+Names kConvBwd = {11, {"x", "weight", "dy", "bias", "act", "x0", "dx_last", "want_dx0", "cu_seqlens", "layout", "out"}, {}};
+Names kConvStep = {6, {"x", "weight", "state", "bias", "act", "out"}, {}};
+Names kVocabFwd = {3, {"h", "weight", "target"}, {}};
+Names kVocabBwd = {7, {"h", "weight", "target", "lse", "dloss", "want_dh", "want_dweight"}, {}};
+Names kGradNorm = {1, {"grads"}, {}};
+Names kGradClip = {5, {"grads", "norm", "max_norm", "eps", "out"}, {}};
 
 // The arguments by position of their names (null: not given).  False for anything that the list of names does not
 // cover: unknown, doubled or surplus arguments.
@@ -752,6 +773,251 @@ PyObject *norm_backward(PyObject *args, PyObject *kwargs) {
     return launched(lib.norm_bwd, a) ? r.dict() : nullptr;
 }
 
+// ---------------------------------------------------------------- short causal convolution, loss over a vocabulary, clipping
+// What both passes of the convolution have in common.
+struct Conv {
+    c10::ScalarType io;
+    Shape rows, state, wide, one;
+    // o: x, weight, bias, act, x0, cu_seqlens, layout
+    template <class Args> void read(Call &c, Args &a, PyObject *const (&o)[7]) {
+        const at::Tensor *x = c.needed(o[0]), *w = c.needed(o[1]), *bias = c.tensor(o[2]), *x0 = c.tensor(o[4]), *cu = c.tensor(o[5]);
+        if (!c.good || x->dim() != (cu ? 2 : 3) || w->dim() != 2 || !mode(o[3], {"silu", "none"}, a.act) || !mode(o[6], {"bld", "bdl"}, a.time_last)) { c.good = false; return; }
+        if (cu) {
+            c.good = cu->scalar_type() == at::kLong && cu->dim() == 1 && cu->is_contiguous() && cu->numel() >= 2;
+            if (!c.good) return;
+            a.cu_seqlens = static_cast<const int64_t *>(cu->data_ptr());
+        }
+        io = x->scalar_type();
+        const int64_t B = cu ? cu->numel() - 1 : x->size(0), L = x->size(a.time_last ? -1 : -2), D = x->size(a.time_last ? -2 : -1), W = w->size(1);
+        if ((io != at::kBFloat16 && io != at::kFloat) || !fits32(B) || !fits32(D) || W < 2 || W > 4) { c.good = false; return; }
+        a.struct_size = sizeof(a);
+        a.B = (int32_t)B; a.D = (int32_t)D; a.W = (int32_t)W; a.L = L;
+        a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        rows.append(x->sizes().begin(), x->sizes().end());
+        state = {B, W - 1, D}; wide = {D, W}; one = {D};
+        row(c, x, a.x, a.x_stride_b, a.x_stride_s);
+        c.data(w, at::kFloat, wide, a.weight);
+        c.data(bias, at::kFloat, one, a.bias);
+        c.data(x0, io, state, a.x0);
+    }
+    template <class Ptr> void row(Call &c, const at::Tensor *t, Ptr &p, int64_t &sb, int64_t &ss) const {
+        p = nullptr;
+        if (!t || !c.good) return;
+        if (t->scalar_type() != io || t->sizes() != c10::IntArrayRef(rows) || (t->stride(-1) != 1 && rows.back() > 1)) { c.good = false; return; }
+        p = t->data_ptr();
+        ss = t->stride(-2);
+        sb = t->dim() == 3 ? t->stride(0) : 0;
+    }
+};
+
+PyObject *conv_forward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_conv_fwd_args a = {};
+    Call c;
+    bool want_last;
+    if (!c.good || !gather(kConvFwd, args, kwargs, o) || !absent(o[V_OUT]) || !flag(o[V_LAST], false, want_last)) Py_RETURN_NONE;
+    Conv v;
+    v.read(c, a, {o[V_X], o[V_W], o[V_BIAS], o[V_ACT], o[V_X0], o[V_CU], o[V_LAYOUT]});
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor y = c.make(v.rows, v.io), last;
+    v.row(c, &y, a.y, a.y_stride_b, a.y_stride_s);
+    if (want_last) { last = c.make(v.state, v.io); a.x_last = last.data_ptr(); }
+    a.stream = c.stream();
+    if (!launched(lib.conv_fwd, a)) return nullptr;
+    if (!want_last) return wrap(y);
+    PyObject *res = PyTuple_New(2);
+    PyTuple_SET_ITEM(res, 0, wrap(y));
+    PyTuple_SET_ITEM(res, 1, wrap(last));
+    return res;
+}
+
+PyObject *conv_backward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_conv_bwd_args a = {};
+    Call c;
+    bool want_dx0;
+    if (!c.good || !gather(kConvBwd, args, kwargs, o) || !absent(o[10]) || !flag(o[7], false, want_dx0)) Py_RETURN_NONE;
+    Conv v;
+    v.read(c, a, {o[0], o[1], o[3], o[4], o[5], o[8], o[9]});
+    const at::Tensor *dy = c.needed(o[2]), *dl = c.tensor(o[6]);
+    if (c.good) {
+        v.row(c, dy, a.dy, a.dy_stride_b, a.dy_stride_s);
+        c.data(dl, v.io, v.state, a.dx_last);
+    }
+    if (!c.good) Py_RETURN_NONE;
+    Results r;
+    r.add(c, "dx", v.rows, v.io);
+    v.row(c, &r.outs[0].t, a.dx, a.dx_stride_b, a.dx_stride_s);
+    a.dweight = static_cast<float *>(r.add(c, "dweight", v.wide, at::kFloat));
+    if (a.bias) a.dbias = static_cast<float *>(r.add(c, "dbias", v.one, at::kFloat));
+    if (want_dx0) a.dx0 = r.add(c, "dx0", v.state, v.io);
+    at::Tensor ws = c.scratch(a, std::max<size_t>(lib.conv_bwd_bytes(&a), 16));
+    a.stream = c.stream();
+    return launched(lib.conv_bwd, a) ? r.dict() : nullptr;
+}
+
+PyObject *conv_step(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_conv_step_args a = {};
+    Call c;
+    if (!c.good || !gather(kConvStep, args, kwargs, o) || !absent(o[5]) || !mode(o[4], {"silu", "none"}, a.act)) Py_RETURN_NONE;
+    const at::Tensor *x = c.needed(o[0]), *w = c.needed(o[1]), *state = c.needed(o[2]), *bias = c.tensor(o[3]);
+    if (!c.good || x->dim() != 2 || w->dim() != 2) Py_RETURN_NONE;
+    const int64_t B = x->size(0), D = x->size(1), W = w->size(1);
+    const c10::ScalarType io = x->scalar_type();
+    if ((io != at::kBFloat16 && io != at::kFloat) || !fits32(B) || !fits32(D) || W < 2 || W > 4) Py_RETURN_NONE;
+    a.struct_size = sizeof(a);
+    a.B = (int32_t)B; a.D = (int32_t)D; a.W = (int32_t)W;
+    a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+    const int64_t bd[] = {B, D}, carried[] = {B, W - 1, D}, wide[] = {D, W}, one[] = {D};
+    c.row(x, io, bd, a.x, a.x_stride_b, a.x_stride_d);
+    c.data(w, at::kFloat, wide, a.weight);
+    c.data(state, io, carried, a.state);
+    c.data(bias, at::kFloat, one, a.bias);
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor y = c.make(bd, io);
+    c.row(&y, io, bd, a.y, a.y_stride_b, a.y_stride_d);
+    a.stream = c.stream();
+    return launched(lib.conv_step, a) ? wrap(y) : nullptr;
+}
+
+// What both passes of the loss have in common: contiguous rows.
+struct Vocab {
+    c10::ScalarType io;
+    Shape rows, words, targets;
+    template <class Args> void read(Call &c, Args &a, PyObject **o) {
+        const at::Tensor *h = c.needed(o[0]), *w = c.needed(o[1]), *t = c.needed(o[2]);
+        if (!c.good || h->dim() < 1 || w->dim() != 2 || w->size(1) != h->size(-1) || !fits32(w->size(1))) { c.good = false; return; }
+        io = h->scalar_type();
+        if (io != at::kBFloat16 && io != at::kFloat) { c.good = false; return; }
+        rows.append(h->sizes().begin(), h->sizes().end());
+        words.append(w->sizes().begin(), w->sizes().end());
+        targets.append(h->sizes().begin(), h->sizes().end() - 1);
+        a.struct_size = sizeof(a);
+        a.T = t->numel(); a.V = w->size(0); a.K = (int32_t)w->size(1);
+        a.io_dtype = io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32;
+        a.h_stride = a.weight_stride = a.K;
+        c.data(h, io, rows, a.h);
+        c.data(w, io, words, a.weight);
+        c.data(t, at::kLong, targets, a.target);
+    }
+};
+
+PyObject *vocab_forward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_vocab_fwd_args a = {};
+    Call c;
+    if (!c.good || !gather(kVocabFwd, args, kwargs, o)) Py_RETURN_NONE;
+    Vocab v;
+    v.read(c, a, o);
+    if (!c.good) Py_RETURN_NONE;
+    at::Tensor loss = c.make(v.targets, at::kFloat), lse = c.make(v.targets, at::kFloat);
+    a.loss = static_cast<float *>(loss.data_ptr());
+    a.lse = static_cast<float *>(lse.data_ptr());
+    at::Tensor ws = c.scratch(a, std::max<size_t>(lib.vocab_fwd_bytes(&a), 16));
+    a.stream = c.stream();
+    if (!launched(lib.vocab_fwd, a)) return nullptr;
+    PyObject *res = PyTuple_New(2);
+    PyTuple_SET_ITEM(res, 0, wrap(loss));
+    PyTuple_SET_ITEM(res, 1, wrap(lse));
+    return res;
+}
+
+PyObject *vocab_backward(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_vocab_bwd_args a = {};
+    Call c;
+    bool want_dh, want_dw;
+    if (!c.good || !gather(kVocabBwd, args, kwargs, o) || !flag(o[5], true, want_dh) || !flag(o[6], true, want_dw) || (!want_dh && !want_dw)) Py_RETURN_NONE;
+    Vocab v;
+    v.read(c, a, o);
+    const at::Tensor *lse = c.needed(o[3]), *up = c.needed(o[4]);
+    if (!c.good || up->scalar_type() != at::kFloat || up->sizes() != c10::IntArrayRef(v.targets)) Py_RETURN_NONE;
+    c.data(lse, at::kFloat, v.targets, a.lse);
+    if (up->is_contiguous()) a.dloss_stride = 1;
+    else for (const int64_t s : up->strides()) c.good = c.good && s == 0;         // one number, expanded
+    a.dloss = static_cast<const float *>(up->data_ptr());
+    if (!c.good) Py_RETURN_NONE;
+    Results r;
+    if (want_dh) a.dh = r.add(c, "dh", v.rows, v.io);
+    if (want_dw) a.dweight = r.add(c, "dweight", v.words, v.io);
+    at::Tensor ws = c.scratch(a, std::max<size_t>(lib.vocab_bwd_bytes(&a), 16));
+    a.stream = c.stream();
+    return launched(lib.vocab_bwd, a) ? r.dict() : nullptr;
+}
+
+// A list or tuple of contiguous tensors on the current device.
+struct Tensors {
+    std::vector<void *> p;
+    std::vector<int64_t> n;
+    std::vector<int32_t> type;
+    void read(Call &c, PyObject *o) {
+        if (!o || !(PyList_CheckExact(o) || PyTuple_CheckExact(o)) || PySequence_Fast_GET_SIZE(o) < 1) { c.good = false; return; }
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(o);
+        p.reserve(count); n.reserve(count); type.reserve(count);
+        for (Py_ssize_t i = 0; i < count && c.good; ++i) {
+            const at::Tensor *t = c.needed(PySequence_Fast_GET_ITEM(o, i));
+            if (!c.good) return;
+            const c10::ScalarType io = t->scalar_type();
+            if ((io != at::kBFloat16 && io != at::kFloat) || !t->is_contiguous()) { c.good = false; return; }
+            p.push_back(t->data_ptr()); n.push_back(t->numel()); type.push_back(io == at::kBFloat16 ? LRNNX_BF16 : LRNNX_F32);
+        }
+    }
+    template <class Args> void give(Args &a) const {
+        a.struct_size = sizeof(a);
+        a.count = (int64_t)p.size(); a.grads = p.data(); a.numel = n.data(); a.dtype = type.data();
+    }
+    bool apart() const {
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        spans.reserve(p.size());
+        for (size_t i = 0; i < p.size(); ++i)
+            if (n[i]) spans.emplace_back((uintptr_t)p[i], (uintptr_t)p[i] + n[i] * (type[i] == LRNNX_BF16 ? 2 : 4));
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second) return false;
+        return true;
+    }
+};
+
+PyObject *grad_norm(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_grad_norm_args a = {};
+    Call c;
+    Tensors g;
+    if (!c.good || !gather(kGradNorm, args, kwargs, o)) Py_RETURN_NONE;
+    g.read(c, o[0]);
+    if (!c.good) Py_RETURN_NONE;
+    g.give(a);
+    at::Tensor norm = c.make({}, at::kFloat), ws = c.scratch(a, std::max<size_t>(lib.grad_norm_bytes(&a), 16));
+    a.norm = static_cast<float *>(norm.data_ptr());
+    a.stream = c.stream();
+    return launched(lib.grad_norm, a) ? wrap(norm) : nullptr;
+}
+
+PyObject *grad_clip(PyObject *args, PyObject *kwargs) {
+    PyObject *o[kMaxArgs];
+    lrnnx_grad_clip_args a = {};
+    Call c;
+    Tensors g, to;
+    if (!c.good || !gather(kGradClip, args, kwargs, o) || !o[2] || !number(o[2], 0.0, a.max_norm) || !number(o[3], 1e-6, a.eps)) Py_RETURN_NONE;
+    g.read(c, o[0]);
+    const at::Tensor *norm = c.needed(o[1]);
+    const bool out = !absent(o[4]);
+    if (out) to.read(c, o[4]);
+    if (!c.good || norm->scalar_type() != at::kFloat || norm->numel() != 1 || !(out ? to : g).apart()) Py_RETURN_NONE;
+    g.give(a);
+    a.norm = static_cast<const float *>(norm->data_ptr());
+    if (out) {
+        if (to.p.size() != g.p.size()) Py_RETURN_NONE;
+        for (size_t i = 0; i < g.p.size(); ++i)
+            if ((to.type[i] != LRNNX_F32 && to.type[i] != g.type[i]) ||
+                THPVariable_Unpack(PySequence_Fast_GET_ITEM(o[4], i)).sizes() != THPVariable_Unpack(PySequence_Fast_GET_ITEM(o[0], i)).sizes()) Py_RETURN_NONE;
+        a.out = to.p.data(); a.out_dtype = to.type.data();
+    }
+    a.stream = c.stream();
+    return launched(lib.grad_clip, a) ? PySequence_List(out ? o[4] : o[0]) : nullptr;
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *)> PyObject *entry(PyObject *, PyObject *const *p, Py_ssize_t n) {
     if (n != 2 || !PyTuple_CheckExact(p[0]) || !PyDict_CheckExact(p[1]) || !check_status) Py_RETURN_NONE;
     HANDLE_TH_ERRORS
@@ -796,13 +1062,21 @@ PyMethodDef methods[] = {
     method("lrnnx_gated_delta_step", entry<delta_step>),
     method("lrnnx_block_norm_fwd", entry<norm_forward>),
     method("lrnnx_block_norm_bwd", entry<norm_backward>),
+    method("lrnnx_short_conv_fwd", entry<conv_forward>),
+    method("lrnnx_short_conv_bwd", entry<conv_backward>),
+    method("lrnnx_short_conv_step", entry<conv_step>),
+    method("lrnnx_vocab_loss_fwd", entry<vocab_forward>),
+    method("lrnnx_vocab_loss_bwd", entry<vocab_backward>),
+    method("lrnnx_grad_norm", entry<grad_norm>),
+    method("lrnnx_grad_clip", entry<grad_clip>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "usual forms of the entry points' calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__binding() {
-    for (Names *n : {&kFwd, &kFwdComplex, &kBwd, &kStep, &kLti, &kLtiBwd, &kDiag, &kDiagBwd, &kDeltaFwd, &kDeltaBwd, &kDeltaStep, &kNormFwd, &kNormBwd})
+    for (Names *n : {&kFwd, &kFwdComplex, &kBwd, &kStep, &kLti, &kLtiBwd, &kDiag, &kDiagBwd, &kDeltaFwd, &kDeltaBwd, &kDeltaStep, &kNormFwd, &kNormBwd, &kConvFwd, &kConvBwd, &kConvStep,
+                     &kVocabFwd, &kVocabBwd, &kGradNorm, &kGradClip})
         for (int i = 0; i < n->count; ++i)
             if (!(n->key[i] = PyUnicode_InternFromString(n->text[i]))) return nullptr;
     return PyModule_Create(&module);

@@ -135,21 +135,25 @@ int64_t piece_of(int64_t words, int64_t bytes_each) {
     return n < words ? n : words;
 }
 
+// Rows and columns of a product's tiles: 256, but 128 where tiles of 256 leave compute units without any, and with float32 inputs.
+int tile_side(int planes, int64_t m, int64_t n) { return planes == 1 && (up(m, kVocabTile) / kVocabTile) * (up(n, kVocabTile) / kVocabTile) >= 128 ? kVocabTile : kVocabTile / 2; }
+
 template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     VocabPlan f{};
     const int io = a->io_dtype == LRNNX_BF16, planes = io ? 1 : 3;
-    const int64_t Kp = up(a->K, 8);
+    // rows of a copy start on 128 bytes, and not all in the same channel of memory
+    const int64_t Kp = up(a->K, 8), ldd = up(a->K, 64) + 64;
     Layout l{ws};
     VocabParams &p = f.p;
-    p.T = a->T; p.K = a->K; p.planes = planes; p.io = io; p.words = a->V; p.target = a->target;
+    p.T = a->T; p.K = a->K; p.Kp = Kp; p.planes = planes; p.io = io; p.words = a->V; p.target = a->target;
     auto copy = [&](VocabPack &k, VocabFactor &to, const void *src, int64_t ld, int64_t rows, bool must) {
         if (!must && rows_in_place(src, ld, a->K, a->io_dtype)) { to = {reinterpret_cast<const uint16_t *>(src), 0, ld}; return; }
-        k.src = src; k.ld = ld; k.rows = rows; k.plane = rows * Kp; k.K = a->K; k.Kp = (int)Kp; k.io = io; k.planes = planes;
+        k.src = src; k.ld = ld; k.rows = rows; k.ldd = ldd; k.plane = rows * ldd; k.K = a->K; k.Kp = (int)Kp; k.io = io; k.planes = planes;
         k.dst = l.take<uint16_t>(planes * k.plane);
-        to = {k.dst, k.plane, Kp};
+        to = {k.dst, k.plane, ldd};
     };
     const bool copied = !rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype);
-    int64_t each = piece_of(a->V, copied ? planes * Kp * 2 : 0);
+    int64_t each = piece_of(a->V, copied ? planes * ldd * 2 : 0);
     if (backward) {
         const int64_t of_dz = piece_of(a->V, planes * a->T * 2);
         each = of_dz < each ? of_dz : each;
@@ -158,12 +162,14 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     copy(f.h, p.h, a->h, a->h_stride, a->T, backward);
     copy(f.w, p.w, a->weight, a->weight_stride, each, copied);
     if (!backward) {
-        p.parts = (a->V + kVocabTile - 1) / kVocabTile;
+        p.side_z = tile_side(planes, each, a->T);
+        p.parts = up(a->V, planes == 1 ? p.side_z : kVocabTile) / (planes == 1 ? p.side_z : kVocabTile);
         p.part = l.take<float>(2 * p.parts * a->T);
         p.hit = l.take<float>(a->T);
     } else {
-        p.ldz = up(each, kVocabTile);
-        p.dz.ld = p.ldz; p.dz.plane = a->T * p.ldz;
+        p.side_z = tile_side(planes, each, a->T); p.side_h = tile_side(planes, a->K, a->T); p.side_w = tile_side(planes, a->K, each);
+        // whole tiles, and rows that do not all start in the same channel of memory
+        p.dz.ld = up(each, kVocabTile) + 128; p.dz.plane = a->T * p.dz.ld;
         p.dz.p = l.take<uint16_t>(planes * p.dz.plane);
         f.rows.index = l.take<int>(a->T);
         f.rows.place = l.take<int>(a->T);
@@ -171,15 +177,15 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
-        // Stretches of the words that dh is summed over side by side: as many as fill whole turns of the 256 compute units best, each an addition of its part
-        const int64_t tiles = up(a->K, kVocabTile) / kVocabTile * (up(a->T, kVocabTile) / kVocabTile), steps = up(each, kVocabStep) / kVocabStep;
+        // Stretches of the words that dh is summed over side by side: as many as fill whole turns of the compute units best, each an addition of its part
+        const int64_t wide = planes == 1 ? p.side_h : kVocabTile, tiles = up(a->K, wide) / wide * (up(a->T, p.side_h) / p.side_h), steps = (each + 63) / 64, units = p.side_h == kVocabTile || planes == 3 ? 256 : 512;
         double best = 0;
         p.splits = 1;
         for (int s = 1; s <= 64 && s * 8 <= steps; ++s) {
-            const double turns = (double)((tiles * s + 255) / 256), use = tiles * s / (256.0 * turns) / (1 + 0.01 * s);
+            const double turns = (double)((tiles * s + units - 1) / units), use = tiles * s / (units * turns) / (1 + 0.01 * s);
             if (use > best) { best = use; p.splits = s; }
         }
-        p.dh_part = l.take<float>(p.splits * a->T * a->K);
+        p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
         f.h.index = f.rows.index; f.h.count = f.rows.count;
         f.rows.T = a->T; f.rows.V = a->V; f.rows.target = a->target;
@@ -248,7 +254,7 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
         if (a->dweight && launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
     if (!a->dh) return LRNNX_OK;
-    const VocabDh end{a->T, a->K, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
+    const VocabDh end{a->T, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
     return status(launch_vocab_dh_out(end, s));
 }
 

@@ -5,41 +5,54 @@
 // as large as the results' own) and from there into both products.  Rows without a target are left out before the products: they cost nothing and
 // nothing in them, finite or not, reaches a gradient.
 // Float32 inputs: every factor is the sum of three bfloat16 numbers, a product six of theirs (terms of 2^-24 and below are left out), summed in float32.
-// Bound by the matrix units.  The core: tiles of 256 x 256, 64 terms at a time, eight wavefronts of 128 x 64, two stages of LDS of 64 KB filled from memory
-// without registers between.
+// Bound by the matrix units.
 #include "vocab_loss.hpp"
 #include "conv_common.hpp"
 
 namespace lrnnx {
 
-constexpr int kVT = kVocabTile, kVS = kVocabStep, kVocabThreads = 512;
-constexpr int kOperand = kVT * kVS * 2, kStage = 2 * kOperand;           // bytes of LDS
+// The tile of a product and its wavefronts: M x N, WM wavefronts along m, each 16 NI x 64 of it; STEP terms a stage, STAGES of them in LDS.
+// Large: 256 x 256, eight wavefronts of 128 x 64 (128 KB of LDS). Small: 128 x 128, four of 64 x 64, two workgroups a compute unit.
+// Of three planes: 256 x 128, eight of 64 x 64; all planes of a stage lie in LDS together (72 KB), so that each is loaded and read once for its six products
+// (997 x 5003, 771 terms: ? us; as six sums of a product each, tiles of 128 x 128: 100; tiles of 128 x 128, four wavefronts with all planes, three stages: 85).
+template <int M_, int N_, int WM_, int PLANES_> struct VocabSize {
+    static constexpr int M = M_, N = N_, WM = WM_, PLANES = PLANES_, STEP = PLANES == 1 ? 64 : 32;
+    static constexpr int NI = M / WM / 16, NJ = 4, WAVES = WM * (N / 64), THREADS = WAVES * 64;
+    static constexpr int PLANE_A = M * STEP * 2, PLANE_B = N * STEP * 2, OPERAND_A = PLANES * PLANE_A, STAGE = OPERAND_A + PLANES * PLANE_B;        // bytes of LDS
+    static constexpr int LOADS = STAGE / (THREADS * 16);                              // of a thread and a stage
+    static constexpr int PER_UNIT = M == 256 ? 1 : 2;                                 // workgroups a compute unit
+};
 
 // One factor of a tile.  ALONG: rows of the source are the tile's rows (columns: the terms of the sum); else rows of the source are the terms.
-// LDS, ALONG: [256 rows][64 terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), so that the 16 rows of a fragment, read at one place each, lie in
-// all banks.  Else [64 terms][256], pairs of pieces (16 columns, what a transposing read takes of a row) exchanged by pair ^ (bits 3, 4 and 0, 1 of the
-// row): the 16 rows that such a read touches then differ in all four bits.
-template <bool ALONG> struct VocabOperand {
-    const char *base;                    // of the next step
-    int64_t step, left;                  // bytes from step to step; terms left
+// LDS, ALONG: [ROWS rows][STEP terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), or of rows of four ^ (row / 4 & 3), so that the 16 rows of a fragment,
+// read at one place each, lie in all banks.  Else [STEP terms][ROWS], pairs of pieces (16 columns, what a transposing read takes of a row) exchanged by pair ^ (bits 3, 4 and 0, 1 of the
+// row): the 16 rows that such a read touches then lie in different banks, too.
+template <class S, int ROWS, bool ALONG> struct VocabOperand {
+    static constexpr int PLANE = ROWS * S::STEP * 2, LOADS = PLANE / (S::THREADS * 16);
+    const char *base;                    // of the next stage
+    int64_t step, left;                  // bytes from stage to stage; terms left
     int64_t ld, outer;                   // bytes of a row; rows (ALONG) or columns of the source from the tile's first on
-    uint32_t off[4];                     // this thread's pieces
-    __device__ __forceinline__ void start(const VocabFactor &f, int plane, int64_t first, int64_t outer_end, int64_t k, int64_t k_end) {
+    int64_t plane;                       // bytes from plane to plane
+    uint32_t off[LOADS];                 // this thread's pieces
+    static constexpr int PIECES = S::STEP / 8;            // of a row, ALONG
+    static __device__ __forceinline__ int turned(int row) { return S::STEP == 64 ? row & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int mixed(int row) { return ((row >> 3 & 3) << 2 | (row & 3)) & (ROWS / 16 - 1); }
+    __device__ __forceinline__ void start(const VocabFactor &f, int64_t first, int64_t outer_end, int64_t k, int64_t k_end) {
         ld = f.ld * 2;
+        plane = f.plane * 2;
         outer = outer_end - first;
         left = k_end - k;
-        base = reinterpret_cast<const char *>(f.p + plane * f.plane) + (ALONG ? first * ld + k * 2 : k * ld + first * 2);
-        step = ALONG ? kVS * 2 : kVS * ld;
-    }
-    __device__ __forceinline__ void place() {
+        base = reinterpret_cast<const char *>(f.p) + (ALONG ? first * ld + k * 2 : k * ld + first * 2);
+        step = ALONG ? S::STEP * 2 : S::STEP * ld;
         const int tid = threadIdx.x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             if (ALONG) {
-                const int row = (tid >> 3) + 64 * j, piece = (tid & 7) ^ (row & 7);
+                const int row = tid / PIECES + S::THREADS / PIECES * j, piece = (tid % PIECES) ^ turned(row);
                 off[j] = (uint32_t)(row * ld) + piece * 16;
             } else {
-                const int row = (tid >> 5) + 16 * j, at = tid & 31, pair = (at >> 1) ^ ((row >> 3 & 3) << 2 | (row & 3)), col = pair * 16 + (at & 1) * 8;
+                constexpr int ROW = ROWS / 8;             // pieces of a row
+                const int row = tid / ROW + S::THREADS / ROW * j, at = tid % ROW, col = ((at >> 1) ^ mixed(row)) * 16 + (at & 1) * 8;
                 off[j] = col < outer ? (uint32_t)(row * ld) + col * 2 : kOutside;
             }
         }
@@ -48,231 +61,394 @@ template <bool ALONG> struct VocabOperand {
     __device__ __forceinline__ void load(char *lds) {
         int64_t bytes = ALONG ? (outer - 1) * ld + (left + 7) / 8 * 16 : (left - 1) * ld + (outer + 7) / 8 * 16;
         bytes = left <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes;
-        const Buffer b = buffer_of(base, bytes);
-        const int wave = threadIdx.x >> 6;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t o = off[j];
-            if (ALONG) o = ((threadIdx.x & 7) ^ (threadIdx.x >> 3 & 7)) * 8 < left ? o : kOutside;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void *)(lds + (j * 512 + wave * 64) * 16), 16, o, 0, 0, 0);
+        for (int q = 0; q < S::PLANES; ++q) {
+            const Buffer b = buffer_of(base + q * plane, bytes);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                uint32_t o = off[j];
+                if (ALONG) o = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * 8 < left ? o : kOutside;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void *)(lds + q * PLANE + (j * S::THREADS + wave * 64) * 16), 16, o, 0, 0, 0);
+            }
         }
         base += step;
-        left -= kVS;
+        left -= S::STEP;
     }
     // the fragments of N times 16 rows from `row` on, of the 32 terms from 32 kk on
     template <int N> static __device__ __forceinline__ void read(const char *lds, int row, int kk, Frag (&f)[N]) {
         const int lane = threadIdx.x & 63, g = lane >> 4;
         if (ALONG) {
-            const char *at = lds + (row + (lane & 15)) * 128 + (((kk * 4 + g) ^ (lane & 7)) << 4);
+            constexpr int ROW = S::STEP * 2;
+            const char *at = lds + (row + (lane & 15)) * ROW + (((kk * 4 + g) ^ turned(lane & 15)) << 4);
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i].v = *reinterpret_cast<const uint4 *>(at + i * 2048);
+            for (int i = 0; i < N; ++i) f[i].v = *reinterpret_cast<const uint4 *>(at + i * 16 * ROW);
         } else {
             typedef short half4 __attribute__((ext_vector_type(4)));
-            const int r = (lane & 15) >> 2, mix = g << 2 | r;
+            constexpr int ROW = ROWS * 2;
+            const int r = (lane & 15) >> 2, mix = mixed(g << 3 | r);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const char *at = lds + (kk * 32 + g * 8 + r) * 512 + ((((row >> 4) + i) ^ mix) << 5) + (lane & 3) * 8;
+                const char *at = lds + (kk * 32 + g * 8 + r) * ROW + ((((row >> 4) + i) ^ mix) << 5) + (lane & 3) * 8;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    f[i].h[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) half4 *)(at + h * 2048)));
+                for (int h = 0; h < 2; ++h)       // four lanes a row of four terms: a lane gets its column's
+                    f[i].h[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) half4 *)(at + h * 4 * ROW)));
             }
         }
     }
 };
 
 struct VocabTile { int64_t m, n; };
-// Tile of a workgroup.  Workgroups go to the eight dies in turn: a die takes a stretch of the tiles, eight rows of tiles at a time, so that what its 32 workgroups
-// read together is in its cache.
-__device__ __forceinline__ VocabTile vocab_tile(unsigned id, unsigned mt, unsigned nt) {
-    const unsigned total = mt * nt, each = total / 8, rest = total % 8, die = id % 8;
-    unsigned at = die * each + (die < rest ? die : rest) + id / 8;
-    const unsigned width = 8 * nt, group = at / width, first = group * 8, rows = mt - first < 8 ? mt - first : 8;
-    at -= group * width;
-    return {(int64_t)(first + at % rows) * kVT, (int64_t)(at / rows) * kVT};
-}
+// The tiles of a product in the order in which they are taken.  Workgroups go to the eight dies in turn: a die takes a stretch of the tiles, four rows of tiles at
+// a time, so that what its 32 compute units read together (4 x 8 tiles) is in its cache: 32768 x 8192 with 2048 terms 1172 TFLOP/s, eight rows 1007.
+template <class S> struct VocabTiles {
+    unsigned mt, nt, total;
+    __device__ __forceinline__ VocabTiles(int64_t m, int64_t n) : mt((unsigned)((m + S::M - 1) / S::M)), nt((unsigned)((n + S::N - 1) / S::N)), total(mt * nt) {}
+    // first tile and number of tiles of a die
+    __device__ __forceinline__ unsigned first(unsigned die) const { const unsigned rest = total % 8; return die * (total / 8) + (die < rest ? die : rest); }
+    __device__ __forceinline__ unsigned count(unsigned die) const { return total / 8 + (die < total % 8 ? 1 : 0); }
+    __device__ __forceinline__ VocabTile tile(unsigned at) const {
+        const unsigned width = 4 * nt, group = at / width, row = group * 4, rows = mt - row < 4 ? mt - row : 4;
+        at -= group * width;
+        return {(int64_t)(row + at % rows) * S::M, (int64_t)(at / rows) * S::N};
+    }
+};
 
-// acc[i][j] += sum over terms [k, k_end) of a[16 i + ..] b[16 j + ..], for this wavefront's 128 x 64 of the tile at (m, n); acc: column (n) lane % 16, rows
-// (m) 4 (lane / 16) .. + 3.
-template <bool AA, bool BA> __device__ __forceinline__ void vocab_product(const VocabFactor &fa, const VocabFactor &fb, int planes, VocabTile t, int64_t m_end, int64_t n_end,
-                                                                          int64_t k, int64_t k_end, char *lds, f32x4 (&acc)[8][4]) {
-    const int wave = threadIdx.x >> 6, wm = (wave & 1) * 128, wn = (wave >> 1) * 64;
-    VocabOperand<AA> a;
-    VocabOperand<BA> b;
-    const int per = (int)((k_end - k + kVS - 1) / kVS), pairs = planes == 1 ? 1 : 6, steps = per * pairs;
-    if (steps <= 0) return;
-    int pair = 0;
-    auto begin = [&]() {                                  // of planes: (0,2) (1,1) (2,0) (0,1) (1,0) (0,0), smallest products first
-        const int pa = pairs == 1 ? 0 : (0x012010 >> (20 - 4 * pair)) & 15, pb = pairs == 1 ? 0 : (0x210100 >> (20 - 4 * pair)) & 15;
-        a.start(fa, pa, t.m, m_end, k, k_end);
-        b.start(fb, pb, t.n, n_end, k, k_end);
-    };
-    begin();
-    a.place();
-    b.place();
-    a.load(lds);
-    b.load(lds + kOperand);
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    int in_pair = 1;
-    for (int s = 0; s < steps; ++s) {
-        const char *now = lds + (s & 1) * kStage;
-        if (s + 1 < steps) {
-            if (in_pair == per) { in_pair = 0; ++pair; begin(); }
-            ++in_pair;
-            char *next = lds + ((s + 1) & 1) * kStage;
-            a.load(next);
-            b.load(next + kOperand);
-        }
+// The factors of a workgroup's tiles, a stage after the other: of one tile, then of the next; behind the last, zeros.
+template <class S, bool AA, bool BA> struct VocabFeed {
+    VocabFactor fa, fb;
+    int64_t m_end, n_end, k, k_end;
+    int stages, coming;                  // of a tile; the next stage
+    VocabTile t;
+    VocabOperand<S, S::M, AA> a;
+    VocabOperand<S, S::N, BA> b;
+    __device__ __forceinline__ VocabFeed(const VocabFactor &fa, const VocabFactor &fb, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end)
+        : fa(fa), fb(fb), m_end(m_end), n_end(n_end), k(k), k_end(k_end), stages((int)((k_end - k + S::STEP - 1) / S::STEP)) {}
+    __device__ __forceinline__ void start() {
+        a.start(fa, t.m, m_end, k, k_end);
+        b.start(fb, t.n, n_end, k, k_end);
+        coming = 0;
+    }
+    // `next`: sets t to the next tile, false if there is none
+    template <class F> __device__ __forceinline__ void fetch(char *lds, F next) {
+        if (coming == stages && next()) start();
+        ++coming;
+        a.load(lds);
+        b.load(lds + S::OPERAND_A);
+    }
+};
+
+// acc[i][j] += sum over the terms of a[16 i + ..] b[16 j + ..], for this wavefront's part of the tile; acc: column (n) lane % 16, rows (m) 4 (lane / 16) .. + 3.
+// Two stages of LDS; fragments are read half a stage ahead of the instructions that use them, and a stage's memory is filled again as soon as its second half
+// is in registers, two halves before it is read: one barrier a stage.  (Fragments read where they are used: 839 TFLOP/s where this does 1070 to 1190; four stages of 32
+// terms so: 1000 to 1100.)  With four wavefronts of 128 x 128 the reads of LDS, which take most of the time that the matrix units do, would be a third
+// fewer, but 256 sums and two sets of fragments do not fit the registers (890).
+// MIX: reads spread between matrix instructions by hand, which pays with transposing reads (1110 -> 1240) and costs without (1195 -> 1167).
+template <class S, bool AA, bool BA, bool MIX, int PLANES = S::PLANES> struct VocabPipe {
+    char *lds;
+    int wm, wn, now;                     // rows and columns of this wavefront; the stage whose first half is in x0, y0
+    Frag x0[S::NI], y0[S::NJ];
+    __device__ __forceinline__ VocabPipe(char *lds) : lds(lds), now(0) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = wave % S::WM * (S::M / S::WM);
+        wn = wave / S::WM * 64;
+    }
+    __device__ __forceinline__ void read(int stage, int kk, Frag (&x)[S::NI], Frag (&y)[S::NJ]) {
+        const char *at = lds + stage * S::STAGE;
+        VocabOperand<S, S::N, BA>::read(at + S::OPERAND_A, wn, kk, y);
+        VocabOperand<S, S::M, AA>::read(at, wm, kk, x);
+    }
+    static __device__ __forceinline__ void sums(const Frag (&x)[S::NI], const Frag (&y)[S::NJ], f32x4 (&acc)[S::NI][S::NJ]) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag x[8], y[4];
-            VocabOperand<BA>::read(now + kOperand, wn, kk, y);
-            VocabOperand<AA>::read(now, wm, kk, x);
+        for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[i], y[j], acc[i][j]);
+    }
+    template <int LOADS> static __device__ __forceinline__ void spread() {
+        if constexpr (MIX) {
+            constexpr int MATRIX = S::NI * S::NJ, READS = (AA ? S::NI : 2 * S::NI) + (BA ? S::NJ : 2 * S::NJ), PER = MATRIX / READS;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma(x[i], y[j], acc[i][j]);
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, MATRIX - PER * READS, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     }
+    template <class Fetch> __device__ __forceinline__ void prime(Fetch fetch) {
+        fetch(lds);
+        __builtin_amdgcn_sched_barrier(0);        // (the wait counts the second stage's loads)
+        fetch(lds + S::STAGE);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::LOADS) : "memory");
+        read(0, 0, x0, y0);
+    }
+    template <class Fetch> __device__ __forceinline__ void run(int stages, f32x4 (&acc)[S::NI][S::NJ], Fetch fetch) {
+        for (int s = 0; s < stages; ++s) {
+            Frag x1[S::NI], y1[S::NJ];
+            read(now, 1, x1, y1);
+            sums(x0, y0, acc);
+            spread<0>();
+            // the other stage has come, and this one is in everyone's registers
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            read(now ^ 1, 0, x0, y0);
+            fetch(lds + now * S::STAGE);
+            sums(x1, y1, acc);
+            spread<S::LOADS>();
+            now ^= 1;
+        }
+    }
+    // nothing on its way, and LDS free for the whole workgroup
+    __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+};
+
+// Of three planes: a stage is one set of fragments, six products of 16 matrix instructions each, smallest first.  The next stage's fragments are read as this one's are
+// used up, so that both fit the registers but for one plane of each factor; a stage's memory is filled again when it is in everyone's registers.
+template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 3> {
+    struct Set { Frag x[3][S::NI], y[3][S::NJ]; };
+    char *lds;
+    int wm, wn, now;                     // the stage that is in `f`
+    Set f;
+    using A = VocabOperand<S, S::M, AA>;
+    using B = VocabOperand<S, S::N, BA>;
+    __device__ __forceinline__ VocabPipe(char *lds) : lds(lds), now(0) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = wave % S::WM * (S::M / S::WM);
+        wn = wave / S::WM * 64;
+    }
+    template <class Fetch> __device__ __forceinline__ void prime(Fetch fetch) {
+        fetch(lds);
+        __builtin_amdgcn_sched_barrier(0);        // (the wait counts the second stage's loads)
+        fetch(lds + S::STAGE);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::LOADS) : "memory");
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            B::read(lds + S::OPERAND_A + q * S::PLANE_B, wn, 0, f.y[q]);
+            A::read(lds + q * S::PLANE_A, wm, 0, f.x[q]);
+        }
+    }
+    static __device__ __forceinline__ void product(const Set &s, int pa, int pb, f32x4 (&acc)[S::NI][S::NJ]) {
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(s.x[pa][i], s.y[pb][j], acc[i][j]);
+    }
+    template <class Fetch> __device__ __forceinline__ void stage(const Set &s, Set &to, f32x4 (&acc)[S::NI][S::NJ], Fetch fetch) {
+        product(s, 0, 2, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        // the other stage has come, and this one is in everyone's registers
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const char *a = lds + (now ^ 1) * S::STAGE, *b = a + S::OPERAND_A;
+        fetch(lds + now * S::STAGE);
+        B::read(b + 2 * S::PLANE_B, wn, 0, to.y[2]);
+        product(s, 1, 1, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        A::read(a, wm, 0, to.x[0]);
+        product(s, 2, 0, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        A::read(a + 2 * S::PLANE_A, wm, 0, to.x[2]);
+        product(s, 0, 1, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        B::read(b + S::PLANE_B, wn, 0, to.y[1]);
+        product(s, 1, 0, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        A::read(a + S::PLANE_A, wm, 0, to.x[1]);
+        B::read(b, wn, 0, to.y[0]);
+        product(s, 0, 0, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        now ^= 1;
+    }
+    template <class Fetch> __device__ __forceinline__ void run(int stages, f32x4 (&acc)[S::NI][S::NJ], Fetch fetch) {
+        for (int s = 0; s < stages; ++s) {
+            Set next;
+            stage(f, next, acc, fetch);
+            f = next;
+        }
+    }
+    __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+};
+
+// One tile's product.
+template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void vocab_product(const VocabFactor &fa, const VocabFactor &fb, VocabTile t, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
+    VocabFeed<S, AA, BA> feed(fa, fb, m_end, n_end, k, k_end);
+    if (feed.stages <= 0) return;
+    feed.t = t;
+    feed.start();
+    VocabPipe<S, AA, BA, MIX> pipe(lds);
+    auto fetch = [&](char *to) __attribute__((always_inline)) { feed.fetch(to, [] { return false; }); };
+    pipe.prime(fetch);
+    pipe.run(feed.stages, acc, fetch);
+    pipe.end();
 }
 
 // What exponents are taken relative to: the largest number, 0 where there is none but -infinity (words behind the last are -infinity too).
 __device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
 
-// z of a tile, words along m, rows along n
-template <bool BWD> __global__ __launch_bounds__(kVocabThreads) void k_vocab_logits(const VocabParams p) {
-    __shared__ __align__(16) char lds[2 * kStage];
-    const unsigned mt = (unsigned)((p.V + kVT - 1) / kVT), nt = (unsigned)((p.T + kVT - 1) / kVT);
-    const VocabTile t = vocab_tile(blockIdx.x, mt, nt);
-    const int64_t T = p.count ? *p.count : p.T;
-    if (t.n >= T) return;
-    f32x4 acc[8][4] = {};
-    vocab_product<true, true>(p.w, p.h, p.planes, t, p.V, T, 0, p.K, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
-    const int64_t v0 = t.m + (wave & 1) * 128 + 4 * g, n0 = t.n + (wave >> 1) * 64 + (lane & 15);       // this lane's first word and row
-    if constexpr (!BWD) {
-        float *sums = reinterpret_cast<float *>(lds);     // [2][256][2]
-        const int64_t left = p.V - v0;
-        float most[4], sum[4];
+// The place of this wavefront in a tile, and this lane's first row and column of it
+template <class S> struct VocabPlace {
+    int wave, m, n;
+    __device__ __forceinline__ VocabPlace() {
+        const int lane = threadIdx.x & 63;
+        wave = threadIdx.x >> 6;
+        m = wave % S::WM * (S::M / S::WM) + 4 * (lane >> 4);
+        n = wave / S::WM * 64 + (lane & 15);
+    }
+};
+// What comes of a tile of z, words along m, rows along n: forward, the largest number and the sum of exponentials of every row
+template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams &p, VocabTile t, int64_t T, float2 *sums, f32x4 (&acc)[S::NI][S::NJ]) {
+    const VocabPlace<S> at;
+    const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t row = n0 + j * 16;
-            const int64_t hit = (row < T ? p.target[row] : -1) - p.v0 - v0;
-            float m = -INFINITY, z = 0.0f;
+    for (int j = 0; j < S::NJ; ++j) {
+        const int64_t row = n0 + j * 16;
+        const int64_t hit = (row < T ? p.target[row] : -1) - p.v0 - v0;
+        float m = -INFINITY, z = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (16 * i + r >= left) acc[i][j][r] = -INFINITY;
-                    m = fmaxf(m, acc[i][j][r]);
-                    z = hit == 16 * i + r ? acc[i][j][r] : z;
-                }
-            if (hit >= 0 && hit < 128 && (hit & 15) < 4 && hit < left) p.hit[row] = z;
-            m = fmaxf(m, __shfl_xor(m, 16, 64));
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            float e = 0.0f;
-            const float base = vocab_base(m);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) e += __expf(acc[i][j][r] - base);
-            e += __shfl_xor(e, 16, 64);
-            e += __shfl_xor(e, 32, 64);
-            most[j] = m;
-            sum[j] = e;
-        }
-        if ((wave & 1) && g == 0)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int at = (wave >> 1) * 64 + j * 16 + lane;
-                sums[2 * at] = most[j]; sums[2 * at + 1] = sum[j];
+            for (int r = 0; r < 4; ++r) {
+                if (16 * i + r >= left) acc[i][j][r] = -INFINITY;
+                m = fmaxf(m, acc[i][j][r]);
+                z = hit == 16 * i + r ? acc[i][j][r] : z;
             }
-        __syncthreads();
-        if (!(wave & 1) && g == 0)
+        if (hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4 && hit < left) p.hit[row] = z;
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        float e = 0.0f;
+        const float base = vocab_base(m);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int at = (wave >> 1) * 64 + j * 16 + lane;
-                const float m2 = sums[2 * at], e2 = sums[2 * at + 1], m = fmaxf(most[j], m2), base = vocab_base(m);
-                const float e = sum[j] * __expf(most[j] - base) + e2 * __expf(m2 - base);
-                if (t.n + at < T) {
-                    float *to = p.part + ((t.n + at) * p.parts + (p.v0 + t.m) / kVT) * 2;
-                    to[0] = m; to[1] = e;
-                }
+        for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) e += __expf(acc[i][j][r] - base);
+        e += __shfl_xor(e, 16, 64);
+        e += __shfl_xor(e, 32, 64);
+        if ((threadIdx.x & 48) == 0) sums[at.wave % S::WM * S::N + at.n + j * 16] = make_float2(m, e);
+    }
+    lds_barrier();
+    const int n = threadIdx.x;
+    if (n < S::N && t.n + n < T) {
+        float m = sums[n].x, e = 0.0f;
+#pragma unroll
+        for (int w = 1; w < S::WM; ++w) m = fmaxf(m, sums[w * S::N + n].x);
+        const float base = vocab_base(m);
+#pragma unroll
+        for (int w = 0; w < S::WM; ++w) e += sums[w * S::N + n].y * __expf(sums[w * S::N + n].x - base);
+        reinterpret_cast<float2 *>(p.part)[(t.n + n) * p.parts + (p.v0 + t.m) / S::M] = make_float2(m, e);
+    }
+}
+// and backward, dz
+template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p, VocabTile t, int64_t T, f32x4 (&acc)[S::NI][S::NJ]) {
+    const VocabPlace<S> at;
+    const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) {
+        const int64_t row = n0 + j * 16;
+        if (row >= T) continue;
+        const float lse = p.row_lse[row], scale = p.row_scale[row];
+        const int64_t hit = (int64_t)p.row_target[row] - p.v0 - v0;
+        uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0;
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i) {
+            float d[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                d[r] = __expf(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
+                d[r] = 16 * i + r < left ? d[r] * scale : 0.0f;
             }
-    } else {
-        const int64_t left = p.V - v0;
+            if (S::PLANES == 1) *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(pack_rne(d[0], d[1]), pack_rne(d[2], d[3]));
+            else {
+                uint32_t a[3], b[3];
+                split2<3>(d[0], d[1], a);
+                split2<3>(d[2], d[3], b);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t row = n0 + j * 16;
-            if (row >= T) continue;
-            const float lse = p.row_lse[row], scale = p.row_scale[row];
-            const int64_t hit = (int64_t)p.row_target[row] - p.v0 - v0;
-            uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.ldz + v0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float d[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    d[r] = __expf(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
-                    d[r] = 16 * i + r < left ? d[r] * scale : 0.0f;
-                }
-                if (p.planes == 1) *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(pack_rne(d[0], d[1]), pack_rne(d[2], d[3]));
-                else {
-                    uint32_t a[3], b[3];
-                    split2<3>(d[0], d[1], a);
-                    split2<3>(d[2], d[3], b);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2 *>(to + q * p.dz.plane + 16 * i) = make_uint2(a[q], b[q]);
-                }
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2 *>(to + q * p.dz.plane + 16 * i) = make_uint2(a[q], b[q]);
             }
         }
     }
 }
+// A workgroup stays and takes a tile after the other; the next one's factors are on their way while it works on what comes of the one before.
+template <class S, bool BWD> __global__ __launch_bounds__(S::THREADS) void k_vocab_logits(const VocabParams p) {
+    __shared__ __align__(16) char lds[2 * S::STAGE];
+    __shared__ float2 sums[S::WM * S::N];
+    const int64_t T = p.count ? *p.count : p.T;
+    const VocabTiles<S> tiles(p.V, T);
+    const unsigned die = blockIdx.x & 7, first = tiles.first(die), count = tiles.count(die), turn = gridDim.x / 8;
+    unsigned at = blockIdx.x >> 3, coming = at;
+    if (at >= count) return;
+    VocabFeed<S, true, true> feed(p.w, p.h, p.V, T, 0, p.K);
+    feed.t = tiles.tile(first + at);
+    feed.start();
+    VocabPipe<S, true, true, false> pipe(lds);
+    auto next = [&]() __attribute__((always_inline)) {
+        coming += turn;
+        if (coming >= count) return false;
+        feed.t = tiles.tile(first + coming);
+        return true;
+    };
+    auto fetch = [&](char *to) __attribute__((always_inline)) { feed.fetch(to, next); };
+    pipe.prime(fetch);
+    for (; at < count; at += turn) {
+        f32x4 acc[S::NI][S::NJ] = {};
+        pipe.run(feed.stages, acc, fetch);
+        const VocabTile t = tiles.tile(first + at);
+        if constexpr (BWD) vocab_dz<S>(p, t, T, acc);
+        else vocab_sums<S>(p, t, T, sums, acc);
+    }
+    pipe.end();
+}
 
 // dh: columns of h along m, rows along n, words summed; a workgroup takes one of `splits` stretches of the words
-__global__ __launch_bounds__(kVocabThreads) void k_vocab_dh(const VocabParams p) {
-    __shared__ __align__(16) char lds[2 * kStage];
-    const unsigned mt = (unsigned)((p.K + kVT - 1) / kVT), nt = (unsigned)((p.T + kVT - 1) / kVT), split = blockIdx.x / (mt * nt);
-    const VocabTile t = vocab_tile(blockIdx.x - split * mt * nt, mt, nt);
+template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(const VocabParams p) {
+    __shared__ __align__(16) char lds[2 * S::STAGE];
     const int64_t T = p.count ? *p.count : p.T;
-    if (t.n >= T) return;
-    const int64_t each = ((p.V + kVS - 1) / kVS + p.splits - 1) / p.splits * kVS, k = split * each, end = k + each < p.V ? k + each : p.V;
-    f32x4 acc[8][4] = {};
-    vocab_product<false, true>(p.w, p.dz, p.planes, t, p.K, T, k, end, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c0 = t.m + (wave & 1) * 128 + 4 * (lane >> 4), n0 = t.n + (wave >> 1) * 64 + (lane & 15);
+    const VocabTiles<S> tiles(p.K, T);
+    const unsigned die = blockIdx.x & 7, at = blockIdx.x >> 3;
+    // (stretches of a tile one after the other: every die has the same tiles of all stretches)
+    const unsigned count = tiles.count(die);
+    if (at >= count * p.splits) return;
+    const unsigned split = at / count;
+    const VocabTile t = tiles.tile(tiles.first(die) + at % count);
+    const int64_t each = ((p.V + S::STEP - 1) / S::STEP + p.splits - 1) / p.splits * S::STEP, k = split * each, end = k + each < p.V ? k + each : p.V;
+    f32x4 acc[S::NI][S::NJ] = {};
+    vocab_product<S, false, true, true>(p.w, p.dz, t, p.K, T, k, end, lds, acc);
+    const VocabPlace<S> place;
+    const int64_t c0 = t.m + place.m, n0 = t.n + place.n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
         if (row >= T) continue;
-        float *to = p.dh_part + (split * p.T + row) * p.K + c0;
+        float *to = p.dh_part + (split * p.T + row) * p.Kp + c0;        // rows of whole 32-byte pieces: four columns are there or not
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (c0 + 16 * i + r < p.K) to[16 * i + r] = p.first ? acc[i][j][r] : to[16 * i + r] + acc[i][j][r];
-        }
+        for (int i = 0; i < S::NI; ++i)
+            if (c0 + 16 * i < p.Kp) {
+                f32x4 *q = reinterpret_cast<f32x4 *>(to + 16 * i);
+                *q = p.first ? acc[i][j] : *q + acc[i][j];
+            }
     }
 }
 
 // dw: columns of h along m, words along n, rows summed
-__global__ __launch_bounds__(kVocabThreads) void k_vocab_dw(const VocabParams p) {
-    __shared__ __align__(16) char lds[2 * kStage];
-    const unsigned mt = (unsigned)((p.K + kVT - 1) / kVT), nt = (unsigned)((p.V + kVT - 1) / kVT);
-    const VocabTile t = vocab_tile(blockIdx.x, mt, nt);
+template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dw(const VocabParams p) {
+    __shared__ __align__(16) char lds[2 * S::STAGE];
+    const VocabTiles<S> tiles(p.K, p.V);
+    const unsigned die = blockIdx.x & 7, at_die = blockIdx.x >> 3;
+    if (at_die >= tiles.count(die)) return;
+    const VocabTile t = tiles.tile(tiles.first(die) + at_die);
     const int64_t T = p.count ? *p.count : p.T;
-    f32x4 acc[8][4] = {};
-    vocab_product<false, false>(p.h, p.dz, p.planes, t, p.K, p.V, 0, T, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c0 = t.m + (wave & 1) * 128 + 4 * (lane >> 4), n0 = t.n + (wave >> 1) * 64 + (lane & 15);
+    f32x4 acc[S::NI][S::NJ] = {};
+    vocab_product<S, false, false, true>(p.h, p.dz, t, p.K, p.V, 0, T, lds, acc);
+    const VocabPlace<S> place;
+    const int64_t c0 = t.m + place.m, n0 = t.n + place.n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < S::NJ; ++j) {
         const int64_t word = n0 + j * 16;
         if (word >= p.V) continue;
         const int64_t at = (p.v0 + word) * p.K + c0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < S::NI; ++i) {
             const float d[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
             if (c0 + 16 * i + 4 <= p.K) {
                 if (p.io) Few<uint16_t, 4>::store(reinterpret_cast<uint16_t *>(p.dw) + at + 16 * i, d);
@@ -288,19 +464,38 @@ __global__ __launch_bounds__(kVocabThreads) void k_vocab_dw(const VocabParams p)
     }
 }
 
-hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s) {
-    const dim3 grid((unsigned)((p.V + kVT - 1) / kVT * ((p.T + kVT - 1) / kVT))), block(kVocabThreads);
-    if (backward) hipLaunchKernelGGL(k_vocab_logits<true>, grid, block, 0, s, p);
-    else hipLaunchKernelGGL(k_vocab_logits<false>, grid, block, 0, s, p);
+using VocabLarge = VocabSize<256, 256, 2, 1>;
+using VocabSmall = VocabSize<128, 128, 2, 1>;
+using VocabPlanes = VocabSize<256, 128, 4, 3>;
+template <class S> int64_t vocab_tiles(int64_t m, int64_t n) { return ((m + S::M - 1) / S::M) * ((n + S::N - 1) / S::N); }
+inline unsigned whole_dies(int64_t n) { return (unsigned)((n + 7) / 8 * 8); }
+
+template <class S> hipError_t run_logits(const VocabParams &p, bool backward, hipStream_t s) {
+    const int64_t tiles = vocab_tiles<S>(p.V, p.T), most = 256 * S::PER_UNIT;
+    const dim3 grid(whole_dies(tiles < most ? tiles : most)), block(S::THREADS);
+    if (backward) hipLaunchKernelGGL((k_vocab_logits<S, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_vocab_logits<S, false>), grid, block, 0, s, p);
     return hipGetLastError();
+}
+template <class S> hipError_t run_dh(const VocabParams &p, hipStream_t s) {
+    hipLaunchKernelGGL(k_vocab_dh<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.T)) * p.splits), dim3(S::THREADS), 0, s, p);
+    return hipGetLastError();
+}
+template <class S> hipError_t run_dw(const VocabParams &p, hipStream_t s) {
+    hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V))), dim3(S::THREADS), 0, s, p);
+    return hipGetLastError();
+}
+hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s) {
+    if (p.planes == 3) return run_logits<VocabPlanes>(p, backward, s);
+    return p.side_z == VocabLarge::M ? run_logits<VocabLarge>(p, backward, s) : run_logits<VocabSmall>(p, backward, s);
 }
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dh, dim3((unsigned)((p.K + kVT - 1) / kVT * ((p.T + kVT - 1) / kVT) * p.splits)), dim3(kVocabThreads), 0, s, p);
-    return hipGetLastError();
+    if (p.planes == 3) return run_dh<VocabPlanes>(p, s);
+    return p.side_h == VocabLarge::M ? run_dh<VocabLarge>(p, s) : run_dh<VocabSmall>(p, s);
 }
 hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dw, dim3((unsigned)((p.K + kVT - 1) / kVT * ((p.V + kVT - 1) / kVT))), dim3(kVocabThreads), 0, s, p);
-    return hipGetLastError();
+    if (p.planes == 3) return run_dw<VocabPlanes>(p, s);
+    return p.side_w == VocabLarge::M ? run_dw<VocabLarge>(p, s) : run_dw<VocabSmall>(p, s);
 }
 
 // ---------------------------------------------------------------- copies, rows, ends
@@ -323,7 +518,7 @@ template <class IO, int NP> __global__ __launch_bounds__(256) void k_vocab_pack(
 #pragma unroll
         for (int e = 0; e < 4; ++e) split2<NP>(x[2 * e], x[2 * e + 1], w[e]);
 #pragma unroll
-        for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4 *>(p.dst + q * p.plane + row * p.Kp + c) = make_uint4(w[0][q], w[1][q], w[2][q], w[3][q]);
+        for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4 *>(p.dst + q * p.plane + row * p.ldd + c) = make_uint4(w[0][q], w[1][q], w[2][q], w[3][q]);
     }
 }
 hipError_t launch_vocab_pack(const VocabPack &p, hipStream_t s) {
@@ -399,7 +594,7 @@ __global__ __launch_bounds__(256) void k_vocab_dh_out(const VocabDh p) {
         const int at = p.place[row];
         float s = 0.0f;
         if (at >= 0)
-            for (int q = 0; q < p.splits; ++q) s += p.part[((int64_t)q * p.T + at) * p.K + (i - row * p.K)];
+            for (int q = 0; q < p.splits; ++q) s += p.part[((int64_t)q * p.T + at) * p.Kp + (i - row * p.K)];
         if (p.io) store_io(reinterpret_cast<uint16_t *>(p.dh) + i, s);
         else store_io(reinterpret_cast<float *>(p.dh) + i, s);
     }

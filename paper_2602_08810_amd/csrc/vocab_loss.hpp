@@ -5,8 +5,7 @@
 
 namespace lrnnx {
 
-constexpr int kVocabTile = 256;          // rows and columns of a product's tile
-constexpr int kVocabStep = 64;           // terms of its sums taken at a time
+constexpr int kVocabTile = 256;          // rows and columns of a product's largest tile
 
 // A factor of a matrix product in bfloat16, `planes` numbers to an element (a float32 element is the sum of three): element (plane, row, column) at
 // plane * plane_stride + row * ld + column.  16-byte aligned rows of whole 16-byte pieces.
@@ -16,7 +15,8 @@ struct VocabFactor {
 };
 
 struct VocabParams {
-    int64_t T, V, K, ldz;                // V: words of this piece; ldz: row stride of dz, V up to whole tiles
+    int64_t T, V, K, Kp;                 // V: words of this piece; Kp: K up to whole 16-byte pieces
+    int side_z, side_h, side_w;          // rows and columns of a tile of z, dh, dw
     int planes, io;                      // io 1: bfloat16
     const int *count;                    // device: rows that have a target (null: all T)
     VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]
@@ -29,7 +29,7 @@ struct VocabParams {
     // backward, by row among those that have a target
     const float *row_lse, *row_scale;
     const int *row_target;               // -1: beyond the vocabulary
-    float *dh_part;                      // [splits,T,K]
+    float *dh_part;                      // [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
     void *dw;                            // [words,K]
 };
@@ -37,10 +37,10 @@ hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t 
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s);
 hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s);
 
-// [rows,K] strided elements as a factor with Kp columns, zeros behind the K-th; `index`: the source's row of each (and `count` rows)
+// [rows,K] strided elements as a factor with Kp columns in rows of ldd, zeros behind the K-th; `index`: the source's row of each (and `count` rows)
 struct VocabPack {
     const void *src; int64_t ld;
-    uint16_t *dst; int64_t plane, rows;
+    uint16_t *dst; int64_t plane, ldd, rows;
     int K, Kp, io, planes;
     const int *index, *count;
 };
@@ -66,7 +66,7 @@ hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s);
 
 struct VocabDh {
     int64_t T;
-    int K, io, splits;
+    int K, Kp, io, splits;
     const float *part;
     const int *place;
     void *dh;
