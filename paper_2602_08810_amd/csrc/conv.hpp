@@ -23,10 +23,8 @@ struct ConvParams {
     int shift;                           // log2 of a workgroup's threads side by side along the contiguous axis
 };
 
-hipError_t launch_conv_rows_fwd(const ConvParams &p, hipStream_t s);
-hipError_t launch_conv_rows_bwd(const ConvParams &p, hipStream_t s);
-hipError_t launch_conv_time_fwd(const ConvParams &p, hipStream_t s);
-hipError_t launch_conv_time_bwd(const ConvParams &p, hipStream_t s);
+hipError_t launch_conv_rows(const ConvParams &p, bool backward, hipStream_t s);
+hipError_t launch_conv_time(const ConvParams &p, bool backward, hipStream_t s);
 hipError_t launch_conv_sums(const ConvParams &p, hipStream_t s);
 // Tiles, workgroups and shift of a call (host only; sizes decide).
 void plan_conv(ConvParams &p, bool backward);

@@ -29,7 +29,23 @@ template <class T, int VEC> struct Few {
         if constexpr (VEC == 1) w[0] = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t *>(p) : *reinterpret_cast<const uint16_t *>(p);
         else if constexpr (W == 1) w[0] = *reinterpret_cast<const one *>(p);
         else if constexpr (W == 2) { const u32x2 v = *reinterpret_cast<const two *>(p); w[0] = v.x; w[1] = v.y; }
-        else { const u32x4 v = *reinterpret_cast<const four *>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+        else
+#pragma unroll
+            for (int i = 0; i < W; i += 4) {
+                const u32x4 v = *reinterpret_cast<const four *>(p + i * 4 / (int)sizeof(T));
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
+    }
+    // the first n elements, zeros behind them
+    __device__ __forceinline__ void load_some(const T *p, int n) {
+#pragma unroll
+        for (int i = 0; i < (W > 0 ? W : 1); ++i) w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e < n) {
+                if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t *>(p + e);
+                else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + e) << (e & 1) * 16;
+            }
     }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
@@ -37,9 +53,13 @@ template <class T, int VEC> struct Few {
     }
     static __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {
         if constexpr (VEC == 1) store_io(p, x[0]);
-        else if constexpr (sizeof(T) == 4) *reinterpret_cast<four *>(p) = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+        else if constexpr (sizeof(T) == 4)
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) *reinterpret_cast<four *>(p + i) = u32x4{__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])};
         else if constexpr (VEC == 4) *reinterpret_cast<two *>(p) = u32x2{pack_rne(x[0], x[1]), pack_rne(x[2], x[3])};
-        else *reinterpret_cast<four *>(p) = u32x4{pack_rne(x[0], x[1]), pack_rne(x[2], x[3]), pack_rne(x[4], x[5]), pack_rne(x[6], x[7])};
+        else
+#pragma unroll
+            for (int i = 0; i < VEC; i += 8) *reinterpret_cast<four *>(p + i) = u32x4{pack_rne(x[i], x[i + 1]), pack_rne(x[i + 2], x[i + 3]), pack_rne(x[i + 4], x[i + 5]), pack_rne(x[i + 6], x[i + 7])};
     }
 };
 template <class IO> constexpr int kFew = 16 / (int)sizeof(IO);    // elements of a 16-byte access
@@ -49,9 +69,9 @@ template <class IO> constexpr int kFew = 16 / (int)sizeof(IO);    // elements of
 template <class IO> __device__ __forceinline__ float conv_sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + (sizeof(IO) == 4 ? expf(-z) : __expf(-z)));
 }
-template <class IO> __device__ __forceinline__ float conv_act(float z, int act) { return act ? z : z * conv_sigmoid<IO>(z); }
-template <class IO> __device__ __forceinline__ float conv_dact(float z, int act) {
-    if (act) return 1.0f;
+template <class IO, bool SILU> __device__ __forceinline__ float conv_act(float z) { return SILU ? z * conv_sigmoid<IO>(z) : z; }
+template <class IO, bool SILU> __device__ __forceinline__ float conv_dact(float z) {
+    if constexpr (!SILU) return 1.0f;
     const float s = conv_sigmoid<IO>(z);
     return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
 }
@@ -109,7 +129,7 @@ template <class IO, int W> __device__ __forceinline__ void conv_last(const ConvP
 }
 // Gradients of the carried inputs: dx0[i] = sum_{j <= i} w[i-j] g[j] over the sequence's first steps, and of a sequence of fewer than W - 1 steps what dx_last
 // says of those that are still there.
-template <class IO, int W> __device__ __forceinline__ void conv_dx0(const ConvParams &p, int64_t first, int64_t stride) {
+template <class IO, int W, bool SILU> __device__ __forceinline__ void conv_dx0(const ConvParams &p, int64_t first, int64_t stride) {
     const int64_t n = (int64_t)p.seqs * p.D;
     for (int64_t i = first; i < n; i += stride) {
         const int d = (int)(i % p.D), seq = (int)(i / p.D), b = p.cu ? 0 : seq;
@@ -120,7 +140,7 @@ template <class IO, int W> __device__ __forceinline__ void conv_dx0(const ConvPa
         for (int j = 0; j < W - 1; ++j)
             if (j < steps) {
                 const float g = load_io(reinterpret_cast<const IO *>(p.dy) + b * p.dy_b + (s.lo + j) * p.dy_l + d * p.dy_d) *
-                                conv_dact<IO>(conv_pre<IO, W>(p, s, b, s.lo + j, d), p.act);
+                                conv_dact<IO, SILU>(conv_pre<IO, W>(p, s, b, s.lo + j, d));
 #pragma unroll
                 for (int k = j; k < W - 1; ++k) out[k] = __builtin_fmaf(p.w[(int64_t)d * W + k - j], g, out[k]);
             }

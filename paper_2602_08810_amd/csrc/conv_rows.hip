@@ -34,7 +34,39 @@ template <class IO, int W, int VEC> __device__ __forceinline__ void conv_before(
     }
 }
 
-template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_conv_rows_fwd(const ConvParams p) {
+// Steps l .. l + kConvAhead - 1 of a row, the last one before `end` for those behind it
+template <class IO, int VEC> struct RowsAhead {
+    Few<IO, VEC> v[kConvAhead];
+    __device__ __forceinline__ void load(const IO *x, int64_t stride, int64_t l) {
+#pragma unroll
+        for (int u = 0; u < kConvAhead; ++u) v[u].load(x + (l + u) * stride);
+    }
+    __device__ __forceinline__ void load(const IO *x, int64_t stride, int64_t l, int64_t end) {
+#pragma unroll
+        for (int u = 0; u < kConvAhead; ++u) v[u].load(x + (l + u < end ? l + u : end - 1) * stride);
+    }
+};
+// WHOLE: all steps lie before `end`.
+template <class IO, int W, int VEC, bool SILU, bool WHOLE> __device__ __forceinline__ void rows_fwd_steps(const ConvParams &p, const ConvWeights<IO, W, VEC> &k, const RowsAhead<IO, VEC> &in, IO *y, int64_t l,
+                                                                                                         int64_t end, float (&seen)[W - 1][VEC]) {
+#pragma unroll
+    for (int u = 0; u < kConvAhead; ++u) {
+        float out[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float now = in.v[u].get(e);
+            float z = k.b[e];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) z = __builtin_fmaf(k.w[j][e], seen[j][e], z);
+            out[e] = conv_act<IO, SILU>(__builtin_fmaf(k.w[W - 1][e], now, z));
+#pragma unroll
+            for (int j = 0; j + 1 < W - 1; ++j) seen[j][e] = seen[j + 1][e];
+            seen[W - 2][e] = now;
+        }
+        if (WHOLE || l + u < end) Few<IO, VEC>::store(y + (l + u) * p.y_l, out);
+    }
+}
+template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256) void k_conv_rows_fwd(const ConvParams p) {
     const int tid = threadIdx.x, c = (blockIdx.y << p.shift) + (tid & ((1 << p.shift) - 1));
     if ((int)blockIdx.x >= p.blocks) {
         conv_last<IO, W>(p, ((int64_t)(blockIdx.x - p.blocks) * gridDim.y + blockIdx.y) * 256 + tid, (int64_t)(gridDim.x - p.blocks) * gridDim.y * 256);
@@ -43,7 +75,7 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
     const int64_t slot = (int64_t)blockIdx.x * (256 >> p.shift) + (tid >> p.shift);
     if (slot >= p.tiles || (int64_t)c * VEC >= p.D) return;
     const int d = c * VEC + VEC <= p.D ? c * VEC : p.D - VEC;            // the last piece overlaps the one before
-    const int b = p.cu ? 0 : (int)(slot / p.tiles_each);
+    const int b = p.cu ? 0 : (int)((unsigned)slot / (unsigned)p.tiles_each);
     const int64_t t0 = (slot - (int64_t)b * p.tiles_each) * p.tile, t1 = t0 + p.tile < p.L ? t0 + p.tile : p.L;
     const IO *x = reinterpret_cast<const IO *>(p.x) + b * p.x_b + d;
     IO *y = reinterpret_cast<IO *>(p.y) + b * p.y_b + d;
@@ -55,46 +87,85 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
         if (!s.in) { l = end; continue; }
         float seen[W - 1][VEC];
         conv_before<IO, W, VEC>(p, s, x, l, d, seen);
+        RowsAhead<IO, VEC> in, next;                      // what comes after is on its way while this is worked on
+        in.load(x, p.x_l, l, end);
+        for (; l + 2 * kConvAhead <= end; l += kConvAhead) {
+            next.load(x, p.x_l, l + kConvAhead);
+            rows_fwd_steps<IO, W, VEC, SILU, true>(p, k, in, y, l, end, seen);
+            in = next;
+        }
         for (; l < end; l += kConvAhead) {
-            Few<IO, VEC> in[kConvAhead];
-#pragma unroll
-            for (int u = 0; u < kConvAhead; ++u) in[u].load(x + (l + u < end ? l + u : end - 1) * p.x_l);
-#pragma unroll
-            for (int u = 0; u < kConvAhead; ++u) {
-                float out[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float now = in[u].get(e);
-                    float z = k.b[e];
-#pragma unroll
-                    for (int j = 0; j < W - 1; ++j) z = __builtin_fmaf(k.w[j][e], seen[j][e], z);
-                    out[e] = conv_act<IO>(__builtin_fmaf(k.w[W - 1][e], now, z), p.act);
-#pragma unroll
-                    for (int j = 0; j + 1 < W - 1; ++j) seen[j][e] = seen[j + 1][e];
-                    seen[W - 2][e] = now;
-                }
-                if (l + u < end) Few<IO, VEC>::store(y + (l + u) * p.y_l, out);
-            }
+            rows_fwd_steps<IO, W, VEC, SILU, false>(p, k, in, y, l, end, seen);
+            in.load(x, p.x_l, l + kConvAhead, end);
         }
         l = end;
     }
 }
 
-template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_conv_rows_bwd(const ConvParams p) {
+// What a walk back carries along: the last inputs, the last g (g[i]: of the step i - (W - 1) from now), and the weights' gradients
+template <int W, int VEC> struct RowsBack {
+    float seen[W - 1][VEC], g[W][VEC], dw[W + 1][VEC];
+};
+// Steps l .. l + kConvAhead - 1 of the steps [first, end) of sequence `s`; INSIDE: they and the steps whose dx they complete are all of these, and none of the sequence's last W - 1.
+template <class IO, int W, int VEC, bool SILU, bool INSIDE> __device__ __forceinline__ void rows_bwd_steps(const ConvParams &p, const ConvWeights<IO, W, VEC> &k, const ConvSpan &s, const RowsAhead<IO, VEC> &in,
+                                                                                                          const RowsAhead<IO, VEC> &up, IO *dx, int d, int64_t l, int64_t first, int64_t end, RowsBack<W, VEC> &r) {
+#pragma unroll
+    for (int u = 0; u < kConvAhead; ++u) {
+        const bool within = INSIDE || l + u < s.hi, mine = INSIDE || l + u < end;
+        float out[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float now = in.v[u].get(e);
+            float z = k.b[e];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) z = __builtin_fmaf(k.w[j][e], r.seen[j][e], z);
+            z = __builtin_fmaf(k.w[W - 1][e], now, z);
+            float h = up.v[u].get(e) * conv_dact<IO, SILU>(z);
+            h = within ? h : 0.0f;
+#pragma unroll
+            for (int j = 0; j + 1 < W; ++j) r.g[j][e] = r.g[j + 1][e];
+            r.g[W - 1][e] = h;
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) r.dw[j][e] = __builtin_fmaf(h, r.seen[j][e], r.dw[j][e]);
+                r.dw[W - 1][e] = __builtin_fmaf(h, now, r.dw[W - 1][e]);
+                r.dw[W][e] += h;
+            }
+#pragma unroll
+            for (int j = 0; j + 1 < W - 1; ++j) r.seen[j][e] = r.seen[j + 1][e];
+            r.seen[W - 2][e] = now;
+            float a = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) a = __builtin_fmaf(k.w[j][e], r.g[W - 1 - j][e], a);
+            out[e] = a;
+        }
+        const int64_t t = l + u - (W - 1);
+        if (INSIDE || (t >= first && t < end)) {
+            if (!INSIDE && p.dx_last && t >= s.hi - (W - 1)) {
+                Few<IO, VEC> v;
+                v.load(reinterpret_cast<const IO *>(p.dx_last) + ((int64_t)s.seq * (W - 1) + (t - (s.hi - (W - 1)))) * p.D + d);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) out[e] += v.get(e);
+            }
+            Few<IO, VEC>::store(dx + t * p.y_l, out);
+        }
+    }
+}
+template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256, 3) void k_conv_rows_bwd(const ConvParams p) {
     __shared__ float lds[256 * VEC];
     const int tid = threadIdx.x, across = 1 << p.shift, c = (blockIdx.y << p.shift) + (tid & (across - 1));
     if ((int)blockIdx.x >= p.blocks) {
-        conv_dx0<IO, W>(p, ((int64_t)(blockIdx.x - p.blocks) * gridDim.y + blockIdx.y) * 256 + tid, (int64_t)(gridDim.x - p.blocks) * gridDim.y * 256);
+        conv_dx0<IO, W, SILU>(p, ((int64_t)(blockIdx.x - p.blocks) * gridDim.y + blockIdx.y) * 256 + tid, (int64_t)(gridDim.x - p.blocks) * gridDim.y * 256);
         return;
     }
     const bool there = (int64_t)c * VEC < p.D;
     const int d = c * VEC + VEC <= p.D ? c * VEC : p.D - VEC;
-    float dw[W + 1][VEC] = {};
+    RowsBack<W, VEC> r = {};
     if (there) {
         ConvWeights<IO, W, VEC> k;
         k.load(p, d);
         for (int64_t slot = (int64_t)blockIdx.x * (256 >> p.shift) + (tid >> p.shift); slot < p.tiles; slot += (int64_t)p.blocks * (256 >> p.shift)) {
-            const int b = p.cu ? 0 : (int)(slot / p.tiles_each);
+            const int b = p.cu ? 0 : (int)((unsigned)slot / (unsigned)p.tiles_each);
             const int64_t t0 = (slot - (int64_t)b * p.tiles_each) * p.tile, t1 = t0 + p.tile < p.L ? t0 + p.tile : p.L;
             const IO *x = reinterpret_cast<const IO *>(p.x) + b * p.x_b + d, *dy = reinterpret_cast<const IO *>(p.dy) + b * p.dy_b + d;
             IO *dx = reinterpret_cast<IO *>(p.dx) + b * p.y_b + d;
@@ -107,57 +178,31 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
                     first = end;
                     continue;
                 }
-                float seen[W - 1][VEC], g[W][VEC] = {};   // g[i]: of the step i - (W - 1) from now
-                conv_before<IO, W, VEC>(p, s, x, first, d, seen);
-                for (int64_t l = first; l < end + (W - 1); l += kConvAhead) {
-                    Few<IO, VEC> in[kConvAhead], up[kConvAhead];
+                conv_before<IO, W, VEC>(p, s, x, first, d, r.seen);
 #pragma unroll
-                    for (int u = 0; u < kConvAhead; ++u) {
-                        const int64_t t = l + u < s.hi ? l + u : s.hi - 1;
-                        in[u].load(x + t * p.x_l);
-                        up[u].load(dy + t * p.dy_l);
-                    }
+                for (int j = 0; j < W; ++j)
 #pragma unroll
-                    for (int u = 0; u < kConvAhead; ++u) {
-                        const bool within = l + u < s.hi, mine = l + u < end;
-                        float out[VEC];
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            const float now = in[u].get(e);
-                            float z = k.b[e];
-#pragma unroll
-                            for (int j = 0; j < W - 1; ++j) z = __builtin_fmaf(k.w[j][e], seen[j][e], z);
-                            z = __builtin_fmaf(k.w[W - 1][e], now, z);
-                            const float h = within ? up[u].get(e) * conv_dact<IO>(z, p.act) : 0.0f;
-#pragma unroll
-                            for (int j = 0; j + 1 < W; ++j) g[j][e] = g[j + 1][e];
-                            g[W - 1][e] = h;
-                            if (mine) {
-#pragma unroll
-                                for (int j = 0; j < W - 1; ++j) dw[j][e] = __builtin_fmaf(h, seen[j][e], dw[j][e]);
-                                dw[W - 1][e] = __builtin_fmaf(h, now, dw[W - 1][e]);
-                                dw[W][e] += h;
-                            }
-#pragma unroll
-                            for (int j = 0; j + 1 < W - 1; ++j) seen[j][e] = seen[j + 1][e];
-                            seen[W - 2][e] = now;
-                            float a = 0.0f;
-#pragma unroll
-                            for (int j = 0; j < W; ++j) a = __builtin_fmaf(k.w[j][e], g[W - 1 - j][e], a);
-                            out[e] = a;
-                        }
-                        const int64_t t = l + u - (W - 1);
-                        if (t >= first && t < end) {
-                            if (p.dx_last && t >= s.hi - (W - 1)) {
-                                Few<IO, VEC> v;
-                                v.load(reinterpret_cast<const IO *>(p.dx_last) + ((int64_t)s.seq * (W - 1) + (t - (s.hi - (W - 1)))) * p.D + d);
-#pragma unroll
-                                for (int e = 0; e < VEC; ++e) out[e] += v.get(e);
-                            }
-                            Few<IO, VEC>::store(dx + t * p.y_l, out);
-                        }
-                    }
+                    for (int e = 0; e < VEC; ++e) r.g[j][e] = 0.0f;
+                // the first steps complete nothing, the last are another tile's or none
+                RowsAhead<IO, VEC> in, up, in2, up2;
+                int64_t l = first;
+                in.load(x, p.x_l, l, s.hi);
+                up.load(dy, p.dy_l, l, s.hi);
+                auto edge = [&]() {
+                    rows_bwd_steps<IO, W, VEC, SILU, false>(p, k, s, in, up, dx, d, l, first, end, r);
+                    l += kConvAhead;
+                    in.load(x, p.x_l, l, s.hi);
+                    up.load(dy, p.dy_l, l, s.hi);
+                };
+                edge();
+                for (; l + 2 * kConvAhead <= end; l += kConvAhead) {
+                    in2.load(x, p.x_l, l + kConvAhead);
+                    up2.load(dy, p.dy_l, l + kConvAhead);
+                    rows_bwd_steps<IO, W, VEC, SILU, true>(p, k, s, in, up, dx, d, l, first, end, r);
+                    in = in2;
+                    up = up2;
                 }
+                while (l < end + (W - 1)) edge();
                 first = end;
             }
         }
@@ -167,11 +212,11 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
 #pragma unroll
     for (int j = 0; j <= W; ++j) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) lds[(tid >> p.shift) * cols + column * VEC + e] = dw[j][e];
+        for (int e = 0; e < VEC; ++e) lds[(tid >> p.shift) * cols + column * VEC + e] = r.dw[j][e];
         __syncthreads();
         for (int i = tid; i < cols; i += 256) {
             float sum = 0.0f;
-            for (int r = 0; r < 256 >> p.shift; ++r) sum += lds[r * cols + i];
+            for (int q = 0; q < 256 >> p.shift; ++q) sum += lds[q * cols + i];
             const int64_t piece = ((int64_t)blockIdx.y << p.shift) + i / VEC, at = piece * VEC + VEC <= p.D ? piece * VEC : (int64_t)p.D - VEC, ch = at + i % VEC;
             if (piece * VEC < p.D && ch >= piece * VEC) p.sums[((int64_t)blockIdx.x * (W + 1) + j) * p.D + ch] = sum;       // (what overlaps is the piece before's)
         }
@@ -179,47 +224,55 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
     }
 }
 
-// dw [D,W] and dbias [D] from the parts: 64 channels a workgroup, four rows of parts side by side.
-__global__ __launch_bounds__(256) void k_conv_sums(const ConvParams p) {
-    __shared__ float lds[4][64];
+// dw [D,W] and dbias [D] from the parts: 64 channels a workgroup, 16 rows of parts side by side.
+__global__ __launch_bounds__(1024) void k_conv_sums(const ConvParams p) {
+    __shared__ float lds[16][64];
     const int j = blockIdx.y, lane = threadIdx.x & 63, row = threadIdx.x >> 6;
     const int64_t d = (int64_t)blockIdx.x * 64 + lane;
     float s = 0.0f;
     if (d < p.D)
-        for (int i = row; i < p.blocks; i += 4) s += p.sums[((int64_t)i * (p.W + 1) + j) * p.D + d];
+#pragma unroll 4
+        for (int i = row; i < p.blocks; i += 16) s += p.sums[((int64_t)i * (p.W + 1) + j) * p.D + d];
     lds[row][lane] = s;
     __syncthreads();
     if (row == 0 && d < p.D) {
-        s = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += lds[i][lane];
         if (j < p.W) p.dw[d * p.W + j] = s;
         else p.db[d] = s;
     }
 }
 hipError_t launch_conv_sums(const ConvParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_conv_sums, dim3((unsigned)(((int64_t)p.D + 63) / 64), (unsigned)(p.W + (p.db ? 1 : 0))), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(k_conv_sums, dim3((unsigned)(((int64_t)p.D + 63) / 64), (unsigned)(p.W + (p.db ? 1 : 0))), dim3(1024), 0, s, p);
     return hipGetLastError();
 }
 
-template <class IO, int W, int VEC> hipError_t run_rows(const ConvParams &p, bool bwd, hipStream_t s) {
+template <class IO, int W, int VEC, bool SILU, bool BWD> hipError_t run_rows(const ConvParams &p, hipStream_t s) {
     const int64_t pieces = (p.D + VEC - 1) / VEC;
     const unsigned y = (unsigned)((pieces + (1 << p.shift) - 1) >> p.shift);
-    const unsigned more = bwd ? (p.dx0 ? conv_blocks((int64_t)p.seqs * p.D) : 0) : (p.x_last ? conv_blocks((int64_t)p.seqs * (W - 1) * p.D) : 0);
+    const unsigned more = BWD ? (p.dx0 ? conv_blocks((int64_t)p.seqs * p.D) : 0) : (p.x_last ? conv_blocks((int64_t)p.seqs * (W - 1) * p.D) : 0);
     const dim3 grid((unsigned)p.blocks + (more + y - 1) / y, y);
-    if (bwd) hipLaunchKernelGGL((k_conv_rows_bwd<IO, W, VEC>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((k_conv_rows_fwd<IO, W, VEC>), grid, dim3(256), 0, s, p);
+    if constexpr (BWD) hipLaunchKernelGGL((k_conv_rows_bwd<IO, W, VEC, SILU>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((k_conv_rows_fwd<IO, W, VEC, SILU>), grid, dim3(256), 0, s, p);
     return hipGetLastError();
 }
-template <class IO> hipError_t rows(const ConvParams &p, bool bwd, hipStream_t s) {
-    constexpr int V = kFew<IO>;
-    const bool vec = p.D >= V;
+template <class IO, int V, bool SILU, bool BWD> hipError_t rows_of(const ConvParams &p, hipStream_t s) {
     switch (p.W) {
-    case 2: return vec ? run_rows<IO, 2, V>(p, bwd, s) : run_rows<IO, 2, 1>(p, bwd, s);
-    case 3: return vec ? run_rows<IO, 3, V>(p, bwd, s) : run_rows<IO, 3, 1>(p, bwd, s);
-    default: return vec ? run_rows<IO, 4, V>(p, bwd, s) : run_rows<IO, 4, 1>(p, bwd, s);
+    case 2: return run_rows<IO, 2, V, SILU, BWD>(p, s);
+    case 3: return run_rows<IO, 3, V, SILU, BWD>(p, s);
+    default: return run_rows<IO, 4, V, SILU, BWD>(p, s);
     }
 }
-hipError_t launch_conv_rows_fwd(const ConvParams &p, hipStream_t s) { return p.io ? rows<uint16_t>(p, false, s) : rows<float>(p, false, s); }
-hipError_t launch_conv_rows_bwd(const ConvParams &p, hipStream_t s) { return p.io ? rows<uint16_t>(p, true, s) : rows<float>(p, true, s); }
+template <class IO, bool SILU> hipError_t rows(const ConvParams &p, bool bwd, hipStream_t s) {
+    constexpr int V = kFew<IO>;
+    if (p.D < V) return bwd ? rows_of<IO, 1, SILU, true>(p, s) : rows_of<IO, 1, SILU, false>(p, s);
+    return bwd ? rows_of<IO, 4, SILU, true>(p, s) : rows_of<IO, V, SILU, false>(p, s);
+}
+hipError_t launch_conv_rows(const ConvParams &p, bool bwd, hipStream_t s) {
+    if (p.act) return p.io ? rows<uint16_t, false>(p, bwd, s) : rows<float, false>(p, bwd, s);
+    return p.io ? rows<uint16_t, true>(p, bwd, s) : rows<float, true>(p, bwd, s);
+}
 
 // One token: VEC channels of a batch entry a thread; the carried inputs move on by one in place.
 template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_conv_step(const ConvStepParams p) {
@@ -238,7 +291,7 @@ template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_con
         float z = p.bias ? p.bias[d + e] : 0.0f;
 #pragma unroll
         for (int j = 0; j < W; ++j) z = __builtin_fmaf(p.w[(int64_t)(d + e) * W + j], in[j].get(e), z);
-        out[e] = conv_act<IO>(z, p.act);
+        out[e] = p.act ? conv_act<IO, false>(z) : conv_act<IO, true>(z);
     }
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {

@@ -28,7 +28,7 @@ template <int CTRL, int ROW_MASK = 0xF>
 __device__ __forceinline__ float dpp(float old, float src) {
     return i2f(__builtin_amdgcn_update_dpp(f2i(old), f2i(src), CTRL, ROW_MASK, 0xF, false));
 }
-constexpr int DPP_WAVE_SHR1 = 0x138;
+constexpr int DPP_WAVE_SHR1 = 0x138, DPP_WAVE_SHL1 = 0x130;
 constexpr int DPP_ROW_BCAST15 = 0x142, DPP_ROW_BCAST31 = 0x143;
 
 __device__ __forceinline__ float readlane(float x, int lane) { return i2f(__builtin_amdgcn_readlane(f2i(x), lane)); }

@@ -52,7 +52,7 @@ int lrnnx_short_conv_fwd(const lrnnx_conv_fwd_args *a) {
     p.y = a->y; p.y_b = a->y_stride_b; p.y_l = a->time_last ? 1 : a->y_stride_s; p.y_d = a->time_last ? a->y_stride_s : 1;
     p.x_last = a->x_last;
     const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
-    return status(a->time_last ? launch_conv_time_fwd(p, s) : launch_conv_rows_fwd(p, s));
+    return status(a->time_last ? launch_conv_time(p, false, s) : launch_conv_rows(p, false, s));
 }
 
 size_t lrnnx_short_conv_bwd_workspace_bytes(const lrnnx_conv_bwd_args *a) {
@@ -73,7 +73,7 @@ int lrnnx_short_conv_bwd(const lrnnx_conv_bwd_args *a) {
     p.dx_last = a->dx_last; p.dx0 = a->dx0; p.dw = a->dweight; p.db = a->dbias;
     p.sums = reinterpret_cast<float *>(a->workspace);
     const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
-    if ((a->time_last ? launch_conv_time_bwd(p, s) : launch_conv_rows_bwd(p, s)) != hipSuccess) return LRNNX_ERR_LAUNCH;
+    if ((a->time_last ? launch_conv_time(p, true, s) : launch_conv_rows(p, true, s)) != hipSuccess) return LRNNX_ERR_LAUNCH;
     return status(launch_conv_sums(p, s));
 }
 
