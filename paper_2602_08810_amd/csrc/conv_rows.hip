@@ -9,15 +9,17 @@
 namespace lrnnx {
 
 constexpr int kConvAhead = 4;                             // steps loaded at a time
+// workgroups of a step, two a compute unit: 256 entries of 8192 channels 6.3 us, with 1024 7.1, 4096 (an entry a thread) 8.6; 1024 entries 21, 22, 24
+constexpr int kStepBlocks = 512;
 
 template <class IO, int W, int VEC> struct ConvWeights {
     float w[W][VEC], b[VEC];
-    __device__ __forceinline__ void load(const ConvParams &p, int d) {
+    __device__ __forceinline__ void load(const float *weight, const float *bias, int d) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            b[e] = p.bias ? p.bias[d + e] : 0.0f;
+            b[e] = bias ? bias[d + e] : 0.0f;
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[j][e] = p.w[(int64_t)(d + e) * W + j];
+            for (int j = 0; j < W; ++j) w[j][e] = weight[(int64_t)(d + e) * W + j];
         }
     }
 };
@@ -80,7 +82,7 @@ template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256)
     const IO *x = reinterpret_cast<const IO *>(p.x) + b * p.x_b + d;
     IO *y = reinterpret_cast<IO *>(p.y) + b * p.y_b + d;
     ConvWeights<IO, W, VEC> k;
-    k.load(p, d);
+    k.load(p.w, p.bias, d);
     for (int64_t l = t0; l < t1;) {
         const ConvSpan s = conv_span(p, b, l);
         const int64_t end = s.hi < t1 ? s.hi : t1;
@@ -163,7 +165,7 @@ template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256,
     RowsBack<W, VEC> r = {};
     if (there) {
         ConvWeights<IO, W, VEC> k;
-        k.load(p, d);
+        k.load(p.w, p.bias, d);
         for (int64_t slot = (int64_t)blockIdx.x * (256 >> p.shift) + (tid >> p.shift); slot < p.tiles; slot += (int64_t)p.blocks * (256 >> p.shift)) {
             const int b = p.cu ? 0 : (int)((unsigned)slot / (unsigned)p.tiles_each);
             const int64_t t0 = (slot - (int64_t)b * p.tiles_each) * p.tile, t1 = t0 + p.tile < p.L ? t0 + p.tile : p.L;
@@ -274,41 +276,45 @@ hipError_t launch_conv_rows(const ConvParams &p, bool bwd, hipStream_t s) {
     return p.io ? rows<uint16_t, true>(p, bwd, s) : rows<float, true>(p, bwd, s);
 }
 
-// One token: VEC channels of a batch entry a thread; the carried inputs move on by one in place.
+// One token: VEC channels of a batch entry a thread, and of the entries gridDim.y further on, for which it has the weights already (they are more bytes than an
+// entry's inputs); the carried inputs move on by one in place.
 template <class IO, int W, int VEC> __global__ __launch_bounds__(256) void k_conv_step(const ConvStepParams p) {
-    const int c = blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
+    const int c = blockIdx.x * 256 + threadIdx.x;
     if ((int64_t)c * VEC >= p.D) return;
     const int d = c * VEC;
-    IO *state = reinterpret_cast<IO *>(p.state) + (int64_t)b * (W - 1) * p.D + d;
-    const IO *x = reinterpret_cast<const IO *>(p.x) + b * p.x_b + d * p.x_d;
-    Few<IO, VEC> in[W];
+    ConvWeights<IO, W, VEC> k;
+    k.load(p.w, p.bias, d);
+    for (int b = blockIdx.y; b < p.B; b += gridDim.y) {
+        IO *state = reinterpret_cast<IO *>(p.state) + (int64_t)b * (W - 1) * p.D + d;
+        Few<IO, VEC> in[W];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) in[j].load(state + (int64_t)j * p.D);
-    in[W - 1].load(x);
-    float out[VEC];
+        for (int j = 0; j < W - 1; ++j) in[j].load(state + (int64_t)j * p.D);
+        in[W - 1].load(reinterpret_cast<const IO *>(p.x) + b * p.x_b + d * p.x_d);
+        float out[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        float z = p.bias ? p.bias[d + e] : 0.0f;
+        for (int e = 0; e < VEC; ++e) {
+            float z = k.b[e];
 #pragma unroll
-        for (int j = 0; j < W; ++j) z = __builtin_fmaf(p.w[(int64_t)(d + e) * W + j], in[j].get(e), z);
-        out[e] = p.act ? conv_act<IO, false>(z) : conv_act<IO, true>(z);
+            for (int j = 0; j < W; ++j) z = __builtin_fmaf(k.w[j][e], in[j].get(e), z);
+            out[e] = p.act ? conv_act<IO, false>(z) : conv_act<IO, true>(z);
+        }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            float v[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = in[j + 1].get(e);
+            Few<IO, VEC>::store(state + (int64_t)j * p.D, v);
+        }
+        Few<IO, VEC>::store(reinterpret_cast<IO *>(p.y) + b * p.y_b + d * p.y_d, out);
     }
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-        float v[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = in[j + 1].get(e);
-        Few<IO, VEC>::store(state + (int64_t)j * p.D, v);
-    }
-    Few<IO, VEC>::store(reinterpret_cast<IO *>(p.y) + b * p.y_b + d * p.y_d, out);
+}
+template <class IO, int W, int V> hipError_t step_of(const ConvStepParams &p, hipStream_t s) {
+    const int x = (p.D / V + 255) / 256, most = kStepBlocks / x < 1 ? 1 : kStepBlocks / x;
+    hipLaunchKernelGGL((k_conv_step<IO, W, V>), dim3((unsigned)x, (unsigned)(p.B < most ? p.B : most)), dim3(256), 0, s, p);
+    return hipGetLastError();
 }
 template <class IO, int W> hipError_t run_step(const ConvStepParams &p, hipStream_t s) {
-    constexpr int V = 4;
-    const bool vec = p.D % V == 0 && p.x_d == 1 && p.y_d == 1;
-    const dim3 grid((unsigned)(((int64_t)p.D / (vec ? V : 1) + 255) / 256), (unsigned)p.B);
-    if (vec) hipLaunchKernelGGL((k_conv_step<IO, W, V>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((k_conv_step<IO, W, 1>), grid, dim3(256), 0, s, p);
-    return hipGetLastError();
+    return p.x_d == 1 && p.y_d == 1 && p.D % 4 == 0 ? step_of<IO, W, 4>(p, s) : step_of<IO, W, 1>(p, s);
 }
 hipError_t launch_conv_step(const ConvStepParams &p, hipStream_t s) {
     switch (p.W) {

@@ -135,8 +135,20 @@ int64_t piece_of(int64_t words, int64_t bytes_each) {
     return n < words ? n : words;
 }
 
-// Rows and columns of a product's tiles: 256, but 128 where tiles of 256 leave compute units without any, and with float32 inputs.
-int tile_side(int planes, int64_t m, int64_t n) { return planes == 1 && (up(m, kVocabTile) / kVocabTile) * (up(n, kVocabTile) / kVocabTile) >= 128 ? kVocabTile : kVocabTile / 2; }
+// Rows and columns of a product's tiles: 256, but 128 where tiles of 256 leave compute units without any or would be half empty, and with float32 inputs.
+int tile_side(int planes, int64_t m, int64_t n) { return planes == 1 && m > 128 && n > 128 && (up(m, kVocabTile) / kVocabTile) * (up(n, kVocabTile) / kVocabTile) >= 128 ? kVocabTile : kVocabTile / 2; }
+
+// Stretches of a sum's terms that are taken side by side: as many as fill whole turns of the compute units best, each an addition of its part, of 512 terms at least.
+int splits_of(int planes, int side, int64_t m, int64_t n, int64_t terms) {
+    const int64_t wide = planes == 1 ? side : kVocabTile, tiles = up(m, wide) / wide * (up(n, side) / side), steps = (terms + 63) / 64, units = side == kVocabTile || planes == 3 ? 256 : 512;
+    double best = 0;
+    int splits = 1;
+    for (int s = 1; s <= 256 && s * 8 <= steps; ++s) {
+        const double turns = (double)((tiles * s + units - 1) / units), use = tiles * s / (units * turns) / (1 + 0.01 * s);
+        if (use > best) { best = use; splits = s; }
+    }
+    return splits;
+}
 
 template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     VocabPlan f{};
@@ -177,14 +189,9 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
-        // Stretches of the words that dh is summed over side by side: as many as fill whole turns of the compute units best, each an addition of its part
-        const int64_t wide = planes == 1 ? p.side_h : kVocabTile, tiles = up(a->K, wide) / wide * (up(a->T, p.side_h) / p.side_h), steps = (each + 63) / 64, units = p.side_h == kVocabTile || planes == 3 ? 256 : 512;
-        double best = 0;
-        p.splits = 1;
-        for (int s = 1; s <= 64 && s * 8 <= steps; ++s) {
-            const double turns = (double)((tiles * s + units - 1) / units), use = tiles * s / (units * turns) / (1 + 0.01 * s);
-            if (use > best) { best = use; p.splits = s; }
-        }
+        p.splits = splits_of(planes, p.side_h, a->K, a->T, each);
+        p.splits_w = splits_of(planes, p.side_w, a->K, each, a->T);
+        if (p.splits_w > 1) p.dw_part = l.take<float>(p.splits_w * each * Kp);
         p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
         f.h.index = f.rows.index; f.h.count = f.rows.count;
@@ -251,11 +258,15 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
         if (const int e = vocab_piece(f, a->weight, a->weight_stride, v0, s)) return e;
         if (launch_vocab_logits(f.p, true, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (a->dh && launch_vocab_dh(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
-        if (a->dweight && launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+        if (!a->dweight) continue;
+        if (launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+        if (f.p.splits_w == 1) continue;
+        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
+        if (launch_vocab_add(parts, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
     if (!a->dh) return LRNNX_OK;
-    const VocabDh end{a->T, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
-    return status(launch_vocab_dh_out(end, s));
+    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
+    return status(launch_vocab_add(end, s));
 }
 
 }  // extern "C"

@@ -287,6 +287,13 @@ template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void v
 // What exponents are taken relative to: the largest number, 0 where there is none but -infinity (words behind the last are -infinity too).
 __device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// four elements, or as many of them as are left
+template <class IO> __device__ __forceinline__ void store_part(IO *to, const float (&x)[4], int64_t left) {
+    if (left >= 4) Few<IO, 4>::store(to, x);
+    else
+#pragma unroll
+        for (int r = 0; r < 4; ++r) if (r < left) store_io(to + r, x[r]);
+}
 // The place of this wavefront in a tile, and this lane's first row and column of it
 template <class S> struct VocabPlace {
     int wave, m, n;
@@ -400,27 +407,42 @@ template <class S, bool BWD> __global__ __launch_bounds__(S::THREADS) void k_voc
     pipe.end();
 }
 
-// dh: columns of h along m, rows along n, words summed; a workgroup takes one of `splits` stretches of the words
+// A sum over stretches of its terms side by side: which tile and stretch a workgroup takes.  The tiles of a stretch read the same rows and so stay on few dies.
+template <class S> struct VocabUnit {
+    VocabTile t;
+    int64_t split, k, end;
+    bool there;
+    __device__ __forceinline__ VocabUnit(int64_t m, int64_t n, int splits, int64_t terms) {
+        VocabTiles<S> units(m, n);
+        const unsigned tiles = units.total;
+        units.total = tiles * splits;
+        const unsigned die = blockIdx.x & 7, at = blockIdx.x >> 3;
+        there = at < units.count(die);
+        if (!there) return;
+        const unsigned unit = units.first(die) + at;
+        split = unit / tiles;
+        t = units.tile(unit % tiles);
+        const int64_t each = ((terms + S::STEP - 1) / S::STEP + splits - 1) / splits * S::STEP;
+        k = split * each;
+        end = k + each < terms ? k + each : terms;
+    }
+};
+
+// dh: columns of h along m, rows along n, words summed
 template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(const VocabParams p) {
     __shared__ __align__(16) char lds[2 * S::STAGE];
     const int64_t T = p.count ? *p.count : p.T;
-    const VocabTiles<S> tiles(p.K, T);
-    const unsigned die = blockIdx.x & 7, at = blockIdx.x >> 3;
-    // (stretches of a tile one after the other: every die has the same tiles of all stretches)
-    const unsigned count = tiles.count(die);
-    if (at >= count * p.splits) return;
-    const unsigned split = at / count;
-    const VocabTile t = tiles.tile(tiles.first(die) + at % count);
-    const int64_t each = ((p.V + S::STEP - 1) / S::STEP + p.splits - 1) / p.splits * S::STEP, k = split * each, end = k + each < p.V ? k + each : p.V;
+    const VocabUnit<S> u(p.K, T, p.splits, p.V);
+    if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, false, true, true>(p.w, p.dz, t, p.K, T, k, end, lds, acc);
+    vocab_product<S, false, true, true>(p.w, p.dz, u.t, p.K, T, u.k, u.end, lds, acc);
     const VocabPlace<S> place;
-    const int64_t c0 = t.m + place.m, n0 = t.n + place.n;
+    const int64_t c0 = u.t.m + place.m, n0 = u.t.n + place.n;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
         if (row >= T) continue;
-        float *to = p.dh_part + (split * p.T + row) * p.Kp + c0;        // rows of whole 32-byte pieces: four columns are there or not
+        float *to = p.dh_part + (u.split * p.T + row) * p.Kp + c0;       // rows of whole 32-byte pieces: four columns are there or not
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
             if (c0 + 16 * i < p.Kp) {
@@ -430,36 +452,33 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     }
 }
 
-// dw: columns of h along m, words along n, rows summed
+// dw: columns of h along m, words along n, rows summed; of one stretch as results, of several as parts
 template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dw(const VocabParams p) {
     __shared__ __align__(16) char lds[2 * S::STAGE];
-    const VocabTiles<S> tiles(p.K, p.V);
-    const unsigned die = blockIdx.x & 7, at_die = blockIdx.x >> 3;
-    if (at_die >= tiles.count(die)) return;
-    const VocabTile t = tiles.tile(tiles.first(die) + at_die);
     const int64_t T = p.count ? *p.count : p.T;
+    const VocabUnit<S> u(p.K, p.V, p.splits_w, T);
+    if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, false, false, true>(p.h, p.dz, t, p.K, p.V, 0, T, lds, acc);
+    vocab_product<S, false, false, true>(p.h, p.dz, u.t, p.K, p.V, u.k, u.end, lds, acc);
     const VocabPlace<S> place;
-    const int64_t c0 = t.m + place.m, n0 = t.n + place.n;
+    const int64_t c0 = u.t.m + place.m, n0 = u.t.n + place.n;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t word = n0 + j * 16;
         if (word >= p.V) continue;
+        if (p.splits_w > 1) {
+            float *to = p.dw_part + (u.split * p.V + word) * p.Kp + c0;
+#pragma unroll
+            for (int i = 0; i < S::NI; ++i)
+                if (c0 + 16 * i < p.Kp) *reinterpret_cast<f32x4 *>(to + 16 * i) = acc[i][j];
+            continue;
+        }
         const int64_t at = (p.v0 + word) * p.K + c0;
 #pragma unroll
         for (int i = 0; i < S::NI; ++i) {
             const float d[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (c0 + 16 * i + 4 <= p.K) {
-                if (p.io) Few<uint16_t, 4>::store(reinterpret_cast<uint16_t *>(p.dw) + at + 16 * i, d);
-                else Few<float, 4>::store(reinterpret_cast<float *>(p.dw) + at + 16 * i, d);
-            } else
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (c0 + 16 * i + r < p.K) {
-                        if (p.io) store_io(reinterpret_cast<uint16_t *>(p.dw) + at + 16 * i + r, d[r]);
-                        else store_io(reinterpret_cast<float *>(p.dw) + at + 16 * i + r, d[r]);
-                    }
+            if (p.io) store_part(reinterpret_cast<uint16_t *>(p.dw) + at + 16 * i, d, p.K - c0 - 16 * i);
+            else store_part(reinterpret_cast<float *>(p.dw) + at + 16 * i, d, p.K - c0 - 16 * i);
         }
     }
 }
@@ -478,11 +497,11 @@ template <class S> hipError_t run_logits(const VocabParams &p, bool backward, hi
     return hipGetLastError();
 }
 template <class S> hipError_t run_dh(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dh<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.T)) * p.splits), dim3(S::THREADS), 0, s, p);
+    hipLaunchKernelGGL(k_vocab_dh<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.T) * p.splits)), dim3(S::THREADS), 0, s, p);
     return hipGetLastError();
 }
 template <class S> hipError_t run_dw(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V))), dim3(S::THREADS), 0, s, p);
+    hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V) * p.splits_w)), dim3(S::THREADS), 0, s, p);
     return hipGetLastError();
 }
 hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s) {
@@ -529,26 +548,42 @@ hipError_t launch_vocab_pack(const VocabPack &p, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The rows with a target, in their order (one workgroup: 1024 rows at a time).  A target beyond the vocabulary makes its row's gradients NaN.
+// The rows with a target, in their order (one workgroup: 4096 rows at a time).  A target beyond the vocabulary makes its row's gradients NaN.
 __global__ __launch_bounds__(1024) void k_vocab_rows(const VocabRows p) {
+    constexpr int R = 4;
     __shared__ int part[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int base = 0;
-    for (int64_t first = 0; first < p.T; first += 1024) {
-        const int64_t t = first + threadIdx.x;
-        const int64_t target = t < p.T ? p.target[t] : -1;
-        const uint64_t have = __ballot(target >= 0);
-        if (lane == 0) part[wave] = __popcll(have);
+    for (int64_t first = 0; first < p.T; first += 1024 * R) {
+        int64_t target[R];
+        float lse[R], scale[R];
+        uint64_t have[R];
+        int mine = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t t = first + (wave * R + r) * 64 + lane;
+            target[r] = t < p.T ? p.target[t] : -1;
+            lse[r] = t < p.T ? p.lse[t] : 0.0f;
+            scale[r] = t < p.T ? p.dloss[t * p.dloss_stride] : 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) { have[r] = __ballot(target[r] >= 0); mine += __popcll(have[r]); }
+        if (lane == 0) part[wave] = mine;
         __syncthreads();
-        int at = base + __popcll(have & ((1ull << lane) - 1)), all = 0;
-        for (int w = 0; w < 16; ++w) { if (w < wave) at += part[w]; all += part[w]; }
-        base += all;
-        if (t < p.T) p.place[t] = target >= 0 ? at : -1;
-        if (target >= 0) {
-            p.index[at] = (int)t;
-            p.row_lse[at] = p.lse[t];
-            p.row_scale[at] = target < p.V ? p.dloss[t * p.dloss_stride] : __builtin_nanf("");
-            p.row_target[at] = target < p.V ? (int)target : -1;
+        int at = base;
+        for (int w = 0; w < 16; ++w) { if (w < wave) at += part[w]; base += part[w]; }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t t = first + (wave * R + r) * 64 + lane;
+            const int to = at + __popcll(have[r] & ((1ull << lane) - 1));
+            if (t < p.T) p.place[t] = target[r] >= 0 ? to : -1;
+            if (target[r] >= 0) {
+                p.index[to] = (int)t;
+                p.row_lse[to] = lse[r];
+                p.row_scale[to] = target[r] < p.V ? scale[r] : __builtin_nanf("");
+                p.row_target[to] = target[r] < p.V ? (int)target[r] : -1;
+            }
+            at += __popcll(have[r]);
         }
         __syncthreads();
     }
@@ -586,23 +621,45 @@ hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s) {
     return hipGetLastError();
 }
 
-// dh of all rows from the parts: zeros for rows without a target
-__global__ __launch_bounds__(256) void k_vocab_dh_out(const VocabDh p) {
-    const int64_t n = p.T * p.K;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / p.K;
-        const int at = p.place[row];
-        float s = 0.0f;
-        if (at >= 0)
-            for (int q = 0; q < p.splits; ++q) s += p.part[((int64_t)q * p.T + at) * p.Kp + (i - row * p.K)];
-        if (p.io) store_io(reinterpret_cast<uint16_t *>(p.dh) + i, s);
-        else store_io(reinterpret_cast<float *>(p.dh) + i, s);
+// Rows of a result from the parts of its sum, four columns a thread; PARTS threads take a stretch of the parts each where there are many.  `place`: where a row's lie, -1:
+// nowhere, and the row is zero.
+template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_add(const VocabAdd p) {
+    constexpr int ITEMS = 256 / PARTS;
+    __shared__ f32x4 lds[PARTS > 1 ? 256 : 1];
+    const int64_t pieces = p.Kp / 4, n = p.rows * pieces, step = (int64_t)gridDim.x * ITEMS;
+    const int mine = threadIdx.x % ITEMS, q0 = threadIdx.x / ITEMS;
+    for (int64_t first = (int64_t)blockIdx.x * ITEMS; first < n; first += step) {
+        const int64_t i = first + mine, row = i / pieces;
+        const int c = (int)(i - row * pieces) * 4;
+        const int64_t at = i < n ? p.place ? p.place[row] : row : -1;
+        f32x4 s = {};
+        if (at >= 0) {
+            const float *from = p.part + at * p.Kp + c;
+#pragma unroll 4
+            for (int q = q0; q < p.splits; q += PARTS) s += *reinterpret_cast<const f32x4 *>(from + q * p.plane);
+        }
+        if constexpr (PARTS > 1) {
+            lds[threadIdx.x] = s;
+            __syncthreads();
+            if (q0 == 0)
+#pragma unroll
+                for (int q = 1; q < PARTS; ++q) s += lds[q * ITEMS + mine];
+            __syncthreads();
+        }
+        if (q0 == 0 && i < n) {
+            const float x[4] = {s[0], s[1], s[2], s[3]};
+            store_part(reinterpret_cast<IO *>(p.out) + row * p.K + c, x, p.K - c);
+        }
     }
 }
-hipError_t launch_vocab_dh_out(const VocabDh &p, hipStream_t s) {
-    const int64_t blocks = (p.T * p.K + 255) / 256;
-    hipLaunchKernelGGL(k_vocab_dh_out, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, p);
+template <class IO> hipError_t run_add(const VocabAdd &p, hipStream_t s) {
+    const bool many = p.splits >= 16;
+    const int64_t blocks = (p.rows * (p.Kp / 4) + (many ? 32 : 256) - 1) / (many ? 32 : 256);
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384)), block(256);
+    if (many) hipLaunchKernelGGL((k_vocab_add<IO, 8>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_vocab_add<IO, 1>), grid, block, 0, s, p);
     return hipGetLastError();
 }
+hipError_t launch_vocab_add(const VocabAdd &p, hipStream_t s) { return p.io ? run_add<uint16_t>(p, s) : run_add<float>(p, s); }
 
 }  // namespace lrnnx

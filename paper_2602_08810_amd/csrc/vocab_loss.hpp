@@ -31,6 +31,8 @@ struct VocabParams {
     const int *row_target;               // -1: beyond the vocabulary
     float *dh_part;                      // [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
+    float *dw_part;                      // [splits_w,V,Kp], if there are several
+    int splits_w;
     void *dw;                            // [words,K]
 };
 hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s);
@@ -64,13 +66,13 @@ struct VocabLoss {
 };
 hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s);
 
-struct VocabDh {
-    int64_t T;
+struct VocabAdd {
+    int64_t rows, plane;                 // rows of the result; elements from part to part
     int K, Kp, io, splits;
     const float *part;
-    const int *place;
-    void *dh;
+    const int *place;                    // or null
+    void *out;                           // [rows,K]
 };
-hipError_t launch_vocab_dh_out(const VocabDh &p, hipStream_t s);
+hipError_t launch_vocab_add(const VocabAdd &p, hipStream_t s);
 
 }  // namespace lrnnx

@@ -51,7 +51,8 @@ def _both(api, h, w, target, dloss):
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("T,V,K", [(1, 1, 1), (1, 300, 64), (3, 5, 7), (5, 256, 8), (17, 257, 72), (64, 1000, 128), (255, 255, 136), (257, 513, 64),
-                                   (300, 771, 200), (70, 2000, 771), (600, 300, 330), (33, 3500, 65)])
+                                   (300, 771, 200), (70, 2000, 771), (600, 300, 330), (33, 3500, 65),
+                                   (2500, 130, 40), (4500, 60, 24), (5, 9000, 40), (1, 5000, 300), (700, 2100, 136)])
 def test_sizes(api, io, T, V, K):
     _both(api, *_make(T + V + K, T, V, K, io))
 
@@ -162,3 +163,50 @@ def test_gradients_are_differences(api):
         up, down = ((h + s * d, w) if n == "dh" else (h, w + s * d) for s in (step, -step))
         want = (r[n].cpu().double() * d).sum()
         assert abs((run(*up) - run(*down)) / (2 * step) - want) < 4e-3 * want, n
+
+
+@pytest.mark.parametrize("io,K", [("bf16", 64), ("bf16", 61), ("f32", 40)])
+def test_a_vocabulary_in_pieces(api, io, K):
+    """Rows and words whose dz does not lie in the workspace at once: the reference is taken on the GPU, in 64 bits."""
+    import torch
+    T, V = (16384, 33300) if io == "bf16" else (8192, 22100)
+    h, w, target, dloss = (t.cuda() for t in _make(8, T, V, K, io))
+    loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+    r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
+    hd, wd = h.double(), w.double()
+    want = dict(loss=torch.zeros(T, dtype=torch.float64, device="cuda"), lse=torch.zeros(T, dtype=torch.float64, device="cuda"), dh=torch.zeros_like(hd), dweight=torch.zeros_like(wd))
+    for lo in range(0, T, 2048):
+        rows, t = slice(lo, lo + 2048), target[lo:lo + 2048]
+        z = hd[rows] @ wd.t().contiguous()
+        want["lse"][rows] = torch.logsumexp(z, 1)
+        there = t >= 0
+        pick = z.gather(1, t.clamp(min=0)[:, None])[:, 0]
+        want["loss"][rows] = torch.where(there, want["lse"][rows] - pick, 0.0)
+        dz = torch.exp(z - want["lse"][rows, None])
+        dz.scatter_add_(1, t.clamp(min=0)[:, None], torch.full((len(t), 1), -1.0, dtype=torch.float64, device="cuda"))
+        dz *= torch.where(there, dloss[rows].double(), 0.0)[:, None]
+        want["dh"][rows] = dz @ wd
+        want["dweight"] += dz.t().contiguous() @ hd[rows]
+    for n, got in dict(r, loss=loss, lse=lse).items():
+        _check(got, want[n].cpu(), n)
+
+
+def test_a_copied_vocabulary_in_pieces(api):
+    """Rows that cannot be read in place, and whose copy is larger than the workspace may be: forward and backward, 64 bits on the GPU."""
+    import torch
+    T, V, K = 3, 108000, 5001
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.randn(V, K, generator=g, device="cuda") * K ** -0.5).bfloat16()
+    h = torch.randn(T, K, generator=g, device="cuda").bfloat16()
+    target, dloss = torch.tensor([107999, -1, 5], device="cuda"), torch.tensor([1.0, 2.0, 0.5], device="cuda")
+    loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+    r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
+    z = h.double() @ w.double().t().contiguous()
+    want = torch.logsumexp(z, 1)
+    dz = torch.exp(z - want[:, None])
+    dz[0, 107999] -= 1
+    dz[2, 5] -= 1
+    dz *= torch.tensor([1.0, 0.0, 0.5], device="cuda", dtype=torch.float64)[:, None]
+    _check(lse, want.cpu(), "lse", 5e-6)          # sums of 5001 products: 6e-8 * sqrt(5001 / 32) * 4 of a logit
+    _check(r["dh"], (dz @ w.double()).cpu(), "dh")
+    _check(r["dweight"], (dz.t().contiguous() @ h.double()).cpu(), "dweight")
