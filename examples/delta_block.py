@@ -1,9 +1,10 @@
 """A small language model of gated delta rule blocks: training steps, then generation token by token from the carried states.
 
-    y = norm(x);  q, k, v, gate, decay, strength = y W_in;  o = gated delta rule;  m = norm of each head's o, gated;  x += scale norm(m W_out)
+    y = norm(x);  q, k, v, gate, decay, strength = y W_in;  q, k, v = silu(short convolution);  o = gated delta rule;
+    m = norm of each head's o, gated;  x += scale norm(m W_out);  after the last block the loss over the vocabulary
 
-The recurrence, the norm and gate of the heads and the boundary between two blocks are the library's calls, forward, backward and for single tokens;
-the dense products are torch's.  Run on an MI355X: `python examples/delta_block.py`."""
+The convolution (of `conv` steps, 0: none), the recurrence, the norm and gate of the heads, the boundary between two blocks, the loss and the clipping of the
+gradients are the library's calls, forward, backward and for single tokens; the dense products are torch's.  Run on an MI355X: `python examples/delta_block.py`."""
 import math
 import os
 import sys
@@ -46,6 +47,43 @@ class BlockNorm(torch.autograd.Function):
         return r["dx"], r.get("dpost_weight"), None, r.get("dgate"), r.get("dresidual"), r.get("dres_scale"), r.get("dpre_weight")
 
 
+class ShortConv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        ctx.save_for_backward(x, weight)
+        return api.lrnnx_short_conv_fwd(x, weight)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight = ctx.saved_tensors
+        r = api.lrnnx_short_conv_bwd(x, weight, dy.contiguous())
+        return r["dx"], r["dweight"]
+
+
+class VocabLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, weight, target):
+        loss, lse = api.lrnnx_vocab_loss_fwd(h, weight, target)
+        ctx.save_for_backward(h, weight, target, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        h, weight, target, lse = ctx.saved_tensors
+        r = api.lrnnx_vocab_loss_bwd(h, weight, target, lse, dloss.contiguous())
+        return r["dh"], r["dweight"], None
+
+
+def short_conv(x, weight):
+    """silu of the causal convolution of x [B,L,D], a filter for every channel."""
+    return ShortConv.apply(x, weight)
+
+
+def vocab_loss(h, weight, target):
+    """Cross entropy of every row of h [..., K] over the words of weight [V,K]; 0 where the target is negative."""
+    return VocabLoss.apply(h, weight, target)
+
+
 def gated_delta(q, k, v, g, beta):
     return GatedDelta.apply(q, k, v, g, beta)
 
@@ -57,10 +95,10 @@ def block_norm(x, post=None, groups=1, gate=None, residual=None, scale=None, pre
 class Model:
     """Parameters in float32 (`params`, by name), activations in `io`, the residual stream in float32."""
 
-    def __init__(self, vocab=64, width=256, key_heads=2, value_heads=4, dk=64, dv=64, layers=2, io=torch.bfloat16, device="cuda", seed=0):
+    def __init__(self, vocab=64, width=256, key_heads=2, value_heads=4, dk=64, dv=64, layers=2, io=torch.bfloat16, device="cuda", seed=0, conv=0):
         gen = torch.Generator().manual_seed(seed)
         self.sizes = (key_heads, value_heads, dk, dv)
-        self.layers, self.io = layers, io
+        self.layers, self.io, self.conv = layers, io, conv
         self.parts = [key_heads * dk, key_heads * dk, value_heads * dv, value_heads * dv, value_heads, value_heads]
         p = dict(embed=torch.randn(vocab, width, generator=gen) * width ** -0.5, pre0=torch.ones(width))
         for i in range(layers):
@@ -69,46 +107,66 @@ class Model:
             p[f"rate{i}"] = torch.linspace(-5.0, -1.0, value_heads)
             p[f"head{i}"], p[f"post{i}"], p[f"pre{i + 1}"] = torch.ones(dv), torch.ones(width), torch.ones(width)
             p[f"scale{i}"] = torch.full((width,), 0.5)
+            if conv:
+                p[f"conv{i}"] = torch.randn(sum(self.parts[:3]), conv, generator=gen) * conv ** -0.5
         self.params = {n: t.to(device).requires_grad_() for n, t in p.items()}
 
-    def _inputs(self, i, y):
+    def _inputs(self, i, y, convolve):
         """What the recurrence of layer i takes, from the normed residual stream: q, k, v, g, beta, and the heads' gate."""
         Hk, Hv, dk, dv = self.sizes
-        q, k, v, gate, a, b = (y @ self.params[f"in{i}"].to(y.dtype)).split(self.parts, dim=-1)
+        z, n = y @ self.params[f"in{i}"].to(y.dtype), sum(self.parts[:3])
+        q, k, v = (convolve(i, z[..., :n]) if self.conv else z[..., :n]).split(self.parts[:3], dim=-1)
+        gate, a, b = z[..., n:].split(self.parts[3:], dim=-1)
         q, k = (F.normalize(t.unflatten(-1, (Hk, dk)), dim=-1) for t in (q, k))
         g = -F.softplus(a + self.params[f"rate{i}"].to(a.dtype))
         return q, k, v.unflatten(-1, (Hv, dv)), g, torch.sigmoid(b), gate
 
-    def _run(self, tokens, recurrence):
+    def _run(self, tokens, recurrence, convolve):
+        """The normed residual stream behind the last block."""
         p, (_, Hv, _, dv) = self.params, self.sizes
         h, y = block_norm(p["embed"][tokens].to(self.io), pre=p["pre0"])
         h = h.to(p["embed"].dtype)
         for i in range(self.layers):
-            *inputs, gate = self._inputs(i, y)
+            *inputs, gate = self._inputs(i, y, convolve)
             o = recurrence(i, *inputs)
             m, _ = block_norm(o.flatten(-2), post=p[f"head{i}"], groups=Hv, gate=gate)
             h, y = block_norm(m @ p[f"out{i}"].to(m.dtype), post=p[f"post{i}"], residual=h, scale=p[f"scale{i}"], pre=p[f"pre{i + 1}"])
-        return y @ p["embed"].to(y.dtype).T
+        return y
+
+    def _head(self, y):
+        return y @ self.params["embed"].to(y.dtype).T
+
+    def _train(self, tokens):
+        return self._run(tokens, lambda i, *inputs: gated_delta(*inputs), lambda i, x: short_conv(x, self.params[f"conv{i}"]))
 
     def logits(self, tokens):
-        """[B,L,vocab] for training."""
-        return self._run(tokens, lambda i, *inputs: gated_delta(*inputs))
+        """[B,L,vocab]."""
+        return self._head(self._train(tokens))
+
+    def losses(self, tokens, targets):
+        """Cross entropy [B,L] of the word that follows each token, 0 where the target is negative; the logits are never in memory."""
+        y = self._train(tokens)
+        return vocab_loss(y, self.params["embed"].to(y.dtype), targets)
 
     @torch.no_grad()
     def prompt(self, tokens):
-        """Logits of the prompt and the state of every layer after it."""
-        states = []
+        """Logits of the prompt and the states of every layer after it."""
+        states = [[None, None] for _ in range(self.layers)]
+
+        def convolve(i, x):
+            y, states[i][0] = api.lrnnx_short_conv_fwd(x, self.params[f"conv{i}"], return_last_state=True)
+            return y
 
         def recurrence(i, *inputs):
-            o, s = api.lrnnx_gated_delta_fwd(*inputs, return_last_state=True)
-            states.append(s)
+            o, states[i][1] = api.lrnnx_gated_delta_fwd(*inputs, return_last_state=True)
             return o
-        return self._run(tokens, recurrence), states
+        return self._head(self._run(tokens, recurrence, convolve)), states
 
     @torch.no_grad()
     def step(self, tokens, states):
         """Logits [B,vocab] of one more token, tokens [B]; the states move on in place."""
-        return self._run(tokens, lambda i, *inputs: api.lrnnx_gated_delta_step(*inputs, states[i]))
+        return self._head(self._run(tokens, lambda i, *inputs: api.lrnnx_gated_delta_step(*inputs, states[i][1]),
+                                    lambda i, x: api.lrnnx_short_conv_step(x, self.params[f"conv{i}"], states[i][0])))
 
 
 def repeats(batch, length, vocab, gen):
@@ -119,11 +177,12 @@ def repeats(batch, length, vocab, gen):
 
 def loss_of(model, tokens):
     half = tokens.shape[1] // 2
-    logits = model.logits(tokens[:, :-1])[:, half - 1:].float()
-    return F.cross_entropy(logits.flatten(0, 1), tokens[:, half:].flatten())
+    targets = tokens[:, 1:].clone()
+    targets[:, :half - 1] = -1                   # the first half cannot be known
+    return model.losses(tokens[:, :-1], targets).sum() / (targets.shape[0] * (targets.shape[1] - half + 1))
 
 
-def train(model, steps, batch=64, length=24, rate=5e-3, seed=1, device="cuda", every=0):
+def train(model, steps, batch=64, length=24, rate=5e-3, seed=1, device="cuda", every=0, clip=1.0):
     gen = torch.Generator().manual_seed(seed)
     vocab = model.params["embed"].shape[0]
     opt = torch.optim.AdamW(model.params.values(), lr=rate, weight_decay=0.0)
@@ -132,6 +191,8 @@ def train(model, steps, batch=64, length=24, rate=5e-3, seed=1, device="cuda", e
         loss = loss_of(model, repeats(batch, length, vocab, gen).to(device))
         opt.zero_grad()
         loss.backward()
+        grads = [t.grad for t in model.params.values()]
+        api.lrnnx_grad_clip(grads, api.lrnnx_grad_norm(grads), clip)
         opt.step()
         losses.append(loss.detach())
         if every and i % every == 0:
@@ -150,7 +211,7 @@ def generate(model, tokens, count):
 
 
 def main():
-    model = Model(vocab=32)
+    model = Model(vocab=32, conv=4)
     train(model, 3001, every=500)
     tokens = repeats(64, 24, model.params["embed"].shape[0], torch.Generator().manual_seed(99)).cuda()
     half = tokens.shape[1] // 2
