@@ -53,10 +53,11 @@ template <class T, int VEC> struct Few {
     }
     static __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {
         if constexpr (VEC == 1) store_io(p, x[0]);
+        else if constexpr (sizeof(T) == 4 && VEC == 2) *reinterpret_cast<two *>(p) = u32x2{__float_as_uint(x[0]), __float_as_uint(x[1])};
         else if constexpr (sizeof(T) == 4)
 #pragma unroll
             for (int i = 0; i < VEC; i += 4) *reinterpret_cast<four *>(p + i) = u32x4{__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])};
-        else if constexpr (VEC == 4) *reinterpret_cast<two *>(p) = u32x2{pack_rne(x[0], x[1]), pack_rne(x[2], x[3])};
+        else if constexpr (VEC == 4 && sizeof(T) == 2) *reinterpret_cast<two *>(p) = u32x2{pack_rne(x[0], x[1]), pack_rne(x[2], x[3])};
         else
 #pragma unroll
             for (int i = 0; i < VEC; i += 8) *reinterpret_cast<four *>(p + i) = u32x4{pack_rne(x[i], x[i + 1]), pack_rne(x[i + 2], x[i + 3]), pack_rne(x[i + 4], x[i + 5]), pack_rne(x[i + 6], x[i + 7])};

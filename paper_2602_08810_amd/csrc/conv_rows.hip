@@ -269,7 +269,7 @@ template <class IO, int V, bool SILU, bool BWD> hipError_t rows_of(const ConvPar
 template <class IO, bool SILU> hipError_t rows(const ConvParams &p, bool bwd, hipStream_t s) {
     constexpr int V = kFew<IO>;
     if (p.D < V) return bwd ? rows_of<IO, 1, SILU, true>(p, s) : rows_of<IO, 1, SILU, false>(p, s);
-    return bwd ? rows_of<IO, 4, SILU, true>(p, s) : rows_of<IO, V, SILU, false>(p, s);
+    return bwd ? rows_of<IO, V / 2, SILU, true>(p, s) : rows_of<IO, V, SILU, false>(p, s);
 }
 hipError_t launch_conv_rows(const ConvParams &p, bool bwd, hipStream_t s) {
     if (p.act) return p.io ? rows<uint16_t, false>(p, bwd, s) : rows<float, false>(p, bwd, s);

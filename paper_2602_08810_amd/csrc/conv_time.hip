@@ -248,7 +248,7 @@ static int log2_up(int64_t n, int most) {
     return s;
 }
 void plan_conv(ConvParams &p, bool backward) {
-    const int64_t along = p.time_last ? p.L : p.D, wide = p.io ? 8 : 4, each = along < wide ? 1 : !backward ? wide : p.time_last ? 2 * wide : 4, pieces = (along + each - 1) / each;
+    const int64_t along = p.time_last ? p.L : p.D, wide = p.io ? 8 : 4, each = along < wide ? 1 : !backward ? wide : p.time_last ? 2 * wide : wide / 2, pieces = (along + each - 1) / each;
     p.shift = log2_up(pieces, 6);
     const int side = 256 >> p.shift;
     int64_t groups;                                        // workgroups of a tile

@@ -274,6 +274,7 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
 // ---------------------------------------------------------------- norm and clipping
 namespace {
 
+constexpr int64_t kGradMost = (int64_t)1 << 44;        // elements in all
 // Elements of a piece: about 4096 pieces in all, of 8192 elements at least (few pieces for the second launch to add, 16 workgroups a compute unit).
 int64_t grad_piece(const int64_t *numel, int64_t count, int64_t &pieces) {
     int64_t total = 0;
@@ -289,7 +290,7 @@ template <class A> int grad_checks(const A *a) {
     int64_t total = 0;
     for (int64_t i = 0; i < a->count; ++i) {
         if (a->numel[i] < 0 || !io_type(a->dtype[i])) return LRNNX_ERR_INVALID_ARG;
-        if (a->numel[i] > ((int64_t)1 << 44) || (total += a->numel[i]) > ((int64_t)1 << 44)) return LRNNX_ERR_UNSUPPORTED;
+        if (a->numel[i] > kGradMost || (total += a->numel[i]) > kGradMost) return LRNNX_ERR_UNSUPPORTED;
         if (a->numel[i] && (!a->grads[i] || !on(a->grads[i], elem(a->dtype[i])))) return LRNNX_ERR_INVALID_ARG;
     }
     return LRNNX_OK;
@@ -322,7 +323,9 @@ extern "C" {
 
 size_t lrnnx_grad_norm_workspace_bytes(const lrnnx_grad_norm_args *a) {
     if (!a || a->struct_size != sizeof(lrnnx_grad_norm_args) || a->count < 1 || !a->numel) return 0;
-    int64_t pieces;
+    int64_t pieces, total = 0;
+    for (int64_t i = 0; i < a->count; ++i)
+        if (a->numel[i] < 0 || a->numel[i] > kGradMost || (total += a->numel[i]) > kGradMost) return 0;
     grad_piece(a->numel, a->count, pieces);
     return (size_t)pieces * sizeof(double);
 }
