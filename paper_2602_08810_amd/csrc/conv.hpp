@@ -18,8 +18,8 @@ struct ConvParams {
     int64_t y_b, y_l, y_d;
     float *dw, *db, *sums;               // sums [blocks,W+1,D]: parts of the weights' gradients
     int blocks;                          // workgroups along the time axis (backward: parts)
-    int tile;                            // steps a thread walks, or the lanes of a row take, at a time
-    int64_t tiles_each, tiles;           // tiles of a batch entry; in all
+    int tile, tile_log2;                 // steps a thread walks, or (a power of two) the lanes of a row take, at a time
+    int64_t tiles_each, tiles;           // tiles of a batch entry; in all (a packed time axis: slots)
     int shift;                           // log2 of a workgroup's threads side by side along the contiguous axis
 };
 

@@ -36,16 +36,24 @@ template <class T, int VEC> struct Few {
                 w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
             }
     }
-    // the first n elements, zeros behind them
+    // the first n elements, zeros behind them; all loads at once (where each is branched around, each is waited for)
     __device__ __forceinline__ void load_some(const T *p, int n) {
 #pragma unroll
         for (int i = 0; i < (W > 0 ? W : 1); ++i) w[i] = 0;
+        if (n <= 0) return;
+        uint32_t v[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (e < n) {
-                if constexpr (sizeof(T) == 4) w[e] = *reinterpret_cast<const uint32_t *>(p + e);
-                else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + e) << (e & 1) * 16;
-            }
+        for (int e = 0; e < VEC; ++e) {
+            const T *at = p + (e < n ? e : n - 1);
+            if constexpr (sizeof(T) == 4) v[e] = *reinterpret_cast<const uint32_t *>(at);
+            else v[e] = *reinterpret_cast<const uint16_t *>(at);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            v[e] = e < n ? v[e] : 0;
+            if constexpr (sizeof(T) == 4) w[e] = v[e];
+            else w[e >> 1] |= v[e] << (e & 1) * 16;
+        }
     }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
@@ -80,12 +88,28 @@ template <class IO, bool SILU> __device__ __forceinline__ float conv_dact(float 
 // The sequence that step l lies in: lo <= l < hi; or none, and then `hi` is where the next one may start (past l, so that a walk always ends,
 // whatever the boundaries hold).  Boundaries ascend and are clamped to the axis.
 struct ConvSpan { int64_t lo, hi; int seq; bool in; };
-__device__ __forceinline__ ConvSpan conv_span(const ConvParams &p, int b, int64_t l) {
+// `after`: the sequences before that one start at l or before (0: not known).
+__device__ __forceinline__ ConvSpan conv_span(const ConvParams &p, int b, int64_t l, int after = 0) {
     if (!p.cu) return {0, p.L, b, true};
     int lo = -1, hi = p.seqs;                              // the last sequence that starts at l or before
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (delta_clamp(p.cu[mid], p.L) <= l) lo = mid; else hi = mid;
+    if (after) {                                           // (a walk's next: a few further on)
+        lo = after - 1;
+        while (lo + 1 < hi && delta_clamp(p.cu[lo + 1], p.L) <= l) ++lo;
+        hi = lo + 1;
+    }
+    while (hi - lo > 1) {                                  // eight boundaries at a time: a wait for memory for three steps of a search by halves
+        const int step = (hi - lo - 1 + 7) / 8;
+        int64_t at[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const int k = lo + (i + 1) * step; at[i] = p.cu[k < hi ? k : hi - 1]; }
+        int found = lo, next = hi;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const int k = lo + (i + 1) * step;
+            if (k < hi && found == lo) { if (delta_clamp(at[i], p.L) <= l) found = k; else next = k; }
+        }
+        lo = found;
+        hi = next;
     }
     if (lo >= 0) {
         const int64_t s = delta_clamp(p.cu[lo], p.L), e = delta_clamp(p.cu[lo + 1], p.L);

@@ -83,8 +83,10 @@ template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256)
     IO *y = reinterpret_cast<IO *>(p.y) + b * p.y_b + d;
     ConvWeights<IO, W, VEC> k;
     k.load(p.w, p.bias, d);
+    int after = 0;
     for (int64_t l = t0; l < t1;) {
-        const ConvSpan s = conv_span(p, b, l);
+        const ConvSpan s = conv_span(p, b, l, after);
+        after = s.seq + 1;
         const int64_t end = s.hi < t1 ? s.hi : t1;
         if (!s.in) { l = end; continue; }
         float seen[W - 1][VEC];
@@ -171,8 +173,10 @@ template <class IO, int W, int VEC, bool SILU> __global__ __launch_bounds__(256,
             const int64_t t0 = (slot - (int64_t)b * p.tiles_each) * p.tile, t1 = t0 + p.tile < p.L ? t0 + p.tile : p.L;
             const IO *x = reinterpret_cast<const IO *>(p.x) + b * p.x_b + d, *dy = reinterpret_cast<const IO *>(p.dy) + b * p.dy_b + d;
             IO *dx = reinterpret_cast<IO *>(p.dx) + b * p.y_b + d;
+            int after = 0;
             for (int64_t first = t0; first < t1;) {
-                const ConvSpan s = conv_span(p, b, first);
+                const ConvSpan s = conv_span(p, b, first, after);
+                after = s.seq + 1;
                 const int64_t end = s.hi < t1 ? s.hi : t1;
                 if (!s.in) {                              // steps outside every sequence
                     const float none[VEC] = {};
