@@ -107,6 +107,7 @@ template <class A> bool vocab_inputs(const A *a) {
 }
 // Rows that the matrix kernels can read as they lie: whole 16-byte pieces at 16-byte steps, 256 of them within 31 bits.
 bool rows_in_place(const void *p, int64_t ld, int K, int io) { return io == LRNNX_BF16 && on(p, 16) && K % 8 == 0 && ld % 8 == 0 && ld >= K && ld <= 1 << 21; }
+bool wide_in_place(const void *p, int64_t ld, int K) { return on(p, 16) && K % 4 == 0 && ld % 4 == 0 && ld >= K && ld <= 1 << 21; }
 
 struct Layout {
     char *base;
@@ -126,6 +127,8 @@ struct VocabPlan {
     size_t bytes;
 };
 
+// Float32 inputs of so few rows: the weight is split where it is read instead of copied.
+constexpr int kVocabFew = 64;
 // The vocabulary is taken in as few pieces as lie in 1 GiB of workspace (a piece's dz; of a copied vocabulary its copy): of whole tiles.
 constexpr int64_t kVocabRoom = (int64_t)1 << 30;
 int64_t piece_of(int64_t words, int64_t bytes_each) {
@@ -135,19 +138,25 @@ int64_t piece_of(int64_t words, int64_t bytes_each) {
     return n < words ? n : words;
 }
 
-// Rows and columns of a product's tiles: 256, but 128 where tiles of 256 leave compute units without any or would be half empty, and with float32 inputs.
-int tile_side(int planes, int64_t m, int64_t n) { return planes == 1 && m > 128 && n > 128 && (up(m, kVocabTile) / kVocabTile) * (up(n, kVocabTile) / kVocabTile) >= 128 ? kVocabTile : kVocabTile / 2; }
-
-// Stretches of a sum's terms that are taken side by side: as many as fill whole turns of the compute units best, each an addition of its part, of 512 terms at least.
-int splits_of(int planes, int side, int64_t m, int64_t n, int64_t terms) {
-    const int64_t wide = planes == 1 ? side : kVocabTile, tiles = up(m, wide) / wide * (up(n, side) / side), steps = (terms + 63) / 64, units = side == kVocabTile || planes == 3 ? 256 : 512;
-    double best = 0;
-    int splits = 1;
-    for (int s = 1; s <= 256 && s * 8 <= steps; ++s) {
-        const double turns = (double)((tiles * s + units - 1) / units), use = tiles * s / (units * turns) / (1 + 0.01 * s);
-        if (use > best) { best = use; splits = s; }
+// First side of a product's tiles and the stretches of its terms that are taken side by side (`most` at most, of 512 terms at least): what takes the least time.  Tiles are
+// 256 x 256 or 128 x 128, two a compute unit; of three planes 256 x 128 or 128 x 64, two a compute unit; of a wide factor 128 x 64 or 64 x 64, two.  A whole turn of the smaller
+// tiles takes 0.67 of the larger ones' time; 0.6 of three planes; 0.8 of a wide factor.  (z of 997 rows, 5003 words, 771 terms in float32: 73 us with the larger ones, 87 with the smaller;
+// of 200 rows, 15179 words, 768 terms 67 and 51; in bfloat16 of 300 rows, 32000 words, 1024 terms 34 and 38, of 100, 32768, 2048 61 and 42.)
+struct VocabShape { int side, splits; };
+VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, int most) {
+    const int large = wide ? kVocabTile / 2 : kVocabTile, units = wide ? 512 : 256;
+    const double part = wide ? 0.8 : planes == 1 ? 0.67 : 0.6;
+    VocabShape best{};
+    double least = 0;
+    for (int side = large; side >= large / 2; side /= 2) {
+        const int64_t across = planes == 1 ? side : side == kVocabTile ? 128 : 64, tiles = up(m, side) / side * (up(n, across) / across), at_once = side == large ? units : 512;
+        for (int64_t s = 1; s == 1 || (s <= most && s * 512 <= terms); ++s) {
+            // (a tile's start and end take about as long as 256 terms; every part is added once more)
+            const double time = (double)((tiles * s + at_once - 1) / at_once) * (side == large ? 1.0 : part) * ((double)((terms + s - 1) / s) + 256) * (1 + 0.01 * (double)s);
+            if (!best.side || time < least) { least = time; best = {side, (int)s}; }
+        }
     }
-    return splits;
+    return best;
 }
 
 template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
@@ -158,28 +167,32 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     Layout l{ws};
     VocabParams &p = f.p;
     p.T = a->T; p.K = a->K; p.Kp = Kp; p.planes = planes; p.io = io; p.words = a->V; p.target = a->target;
-    auto copy = [&](VocabPack &k, VocabFactor &to, const void *src, int64_t ld, int64_t rows, bool must) {
-        if (!must && rows_in_place(src, ld, a->K, a->io_dtype)) { to = {reinterpret_cast<const uint16_t *>(src), 0, ld}; return; }
+    p.wide = !io && a->T <= kVocabFew;
+    auto copy = [&](VocabPack &k, VocabFactor &to, const void *src, int64_t ld, int64_t rows, int planes, bool must) {
+        if (!must) { to = {reinterpret_cast<const uint16_t *>(src), 0, ld}; return; }
         k.src = src; k.ld = ld; k.rows = rows; k.ldd = ldd; k.plane = rows * ldd; k.K = a->K; k.Kp = (int)Kp; k.io = io; k.planes = planes;
-        k.dst = l.take<uint16_t>(planes * k.plane);
+        k.dst = l.take<uint16_t>((planes ? planes : 2) * k.plane);
         to = {k.dst, k.plane, ldd};
     };
-    const bool copied = !rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype);
-    int64_t each = piece_of(a->V, copied ? planes * ldd * 2 : 0);
+    const bool copied = !(p.wide ? wide_in_place(a->weight, a->weight_stride, a->K) : rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype));
+    int64_t each = piece_of(a->V, copied ? (p.wide ? 2 : planes) * ldd * 2 : 0);
     if (backward) {
         const int64_t of_dz = piece_of(a->V, planes * a->T * 2);
         each = of_dz < each ? of_dz : each;
     }
     f.each = each;
-    copy(f.h, p.h, a->h, a->h_stride, a->T, backward);
-    copy(f.w, p.w, a->weight, a->weight_stride, each, copied);
+    copy(f.h, p.h, a->h, a->h_stride, a->T, planes, backward || !rows_in_place(a->h, a->h_stride, a->K, a->io_dtype));
+    copy(f.w, p.w, a->weight, a->weight_stride, each, p.wide ? 0 : planes, copied);
     if (!backward) {
-        p.side_z = tile_side(planes, each, a->T);
-        p.parts = up(a->V, planes == 1 ? p.side_z : kVocabTile) / (planes == 1 ? p.side_z : kVocabTile);
+        p.side_z = shape_of(planes, p.wide, each, a->T, a->K, 1).side;
+        p.parts = up(a->V, p.side_z) / p.side_z;
         p.part = l.take<float>(2 * p.parts * a->T);
         p.hit = l.take<float>(a->T);
     } else {
-        p.side_z = tile_side(planes, each, a->T); p.side_h = tile_side(planes, a->K, a->T); p.side_w = tile_side(planes, a->K, each);
+        p.side_z = shape_of(planes, p.wide, each, a->T, a->K, 1).side;
+        const VocabShape dh = shape_of(planes, p.wide, a->K, a->T, each, 256), dw = shape_of(planes, false, a->K, each, a->T, 256);
+        p.side_h = dh.side; p.splits = dh.splits;
+        p.side_w = dw.side; p.splits_w = dw.splits;
         // whole tiles, and rows that do not all start in the same channel of memory
         p.dz.ld = up(each, kVocabTile) + 128; p.dz.plane = a->T * p.dz.ld;
         p.dz.p = l.take<uint16_t>(planes * p.dz.plane);
@@ -189,8 +202,6 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
-        p.splits = splits_of(planes, p.side_h, a->K, a->T, each);
-        p.splits_w = splits_of(planes, p.side_w, a->K, each, a->T);
         if (p.splits_w > 1) p.dw_part = l.take<float>(p.splits_w * each * Kp);
         p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;

@@ -15,10 +15,11 @@ namespace lrnnx {
 // Large: 256 x 256, eight wavefronts of 128 x 64 (128 KB of LDS). Small: 128 x 128, four of 64 x 64, two workgroups a compute unit.
 // Of three planes: 256 x 128, eight of 64 x 64; all planes of a stage lie in LDS together (72 KB), so that each is loaded and read once for its six products
 // (997 x 5003, 771 terms: ? us; as six sums of a product each, tiles of 128 x 128: 100; tiles of 128 x 128, four wavefronts with all planes, three stages: 85).
-template <int M_, int N_, int WM_, int PLANES_> struct VocabSize {
+template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct VocabSize {
+    static constexpr bool WIDE = WIDE_;
     static constexpr int M = M_, N = N_, WM = WM_, PLANES = PLANES_, STEP = PLANES == 1 ? 64 : 32;
     static constexpr int NI = M / WM / 16, NJ = 4, WAVES = WM * (N / 64), THREADS = WAVES * 64;
-    static constexpr int PLANE_A = M * STEP * 2, PLANE_B = N * STEP * 2, OPERAND_A = PLANES * PLANE_A, STAGE = OPERAND_A + PLANES * PLANE_B;        // bytes of LDS
+    static constexpr int PLANE_A = M * STEP * 2, PLANE_B = N * STEP * 2, OPERAND_A = WIDE ? M * STEP * 4 : PLANES * PLANE_A, STAGE = OPERAND_A + PLANES * PLANE_B;        // bytes of LDS
     static constexpr int LOADS = STAGE / (THREADS * 16);                              // of a thread and a stage
     static constexpr int PER_UNIT = M == 256 ? 1 : 2;                                 // workgroups a compute unit
 };
@@ -27,23 +28,29 @@ template <int M_, int N_, int WM_, int PLANES_> struct VocabSize {
 // LDS, ALONG: [ROWS rows][STEP terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), or of rows of four ^ (row / 4 & 3), so that the 16 rows of a fragment,
 // read at one place each, lie in all banks.  Else [STEP terms][ROWS], pairs of pieces (16 columns, what a transposing read takes of a row) exchanged by pair ^ (bits 3, 4 and 0, 1 of the
 // row): the 16 rows that such a read touches then lie in different banks, too.
-template <class S, int ROWS, bool ALONG> struct VocabOperand {
-    static constexpr int PLANE = ROWS * S::STEP * 2, LOADS = PLANE / (S::THREADS * 16);
+// WIDE: float32 elements, split as they are read; rows of 128 bytes ALONG, else groups of 16 columns exchanged by group ^ (bits 3, 4 of the row).
+template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand {
+    static constexpr int BYTES = WIDE ? 4 : 2, EACH = 16 / BYTES;             // bytes of an element, elements of a piece
+    static constexpr int PLANE = ROWS * S::STEP * BYTES, LOADS = PLANE / (S::THREADS * 16);
     const char *base;                    // of the next stage
     int64_t step, left;                  // bytes from stage to stage; terms left
     int64_t ld, outer;                   // bytes of a row; rows (ALONG) or columns of the source from the tile's first on
     int64_t plane;                       // bytes from plane to plane
     uint32_t off[LOADS];                 // this thread's pieces
-    static constexpr int PIECES = S::STEP / 8;            // of a row, ALONG
-    static __device__ __forceinline__ int turned(int row) { return S::STEP == 64 ? row & 7 : row >> 2 & 3; }
-    static __device__ __forceinline__ int mixed(int row) { return ((row >> 3 & 3) << 2 | (row & 3)) & (ROWS / 16 - 1); }
+    static constexpr int PIECES = S::STEP / EACH;         // of a row, ALONG
+    static __device__ __forceinline__ int turned(int row) { return PIECES == 8 ? row & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int mixed(int row) {
+        if (WIDE) return row >> 3 & 3;
+        if (ROWS == 64) return (row >> 3 & 1) << 1 | (row >> 1 & 1);         // (two rows side by side in the banks)
+        return ((row >> 3 & 3) << 2 | (row & 3)) & (ROWS / 16 - 1);
+    }
     __device__ __forceinline__ void start(const VocabFactor &f, int64_t first, int64_t outer_end, int64_t k, int64_t k_end) {
-        ld = f.ld * 2;
+        ld = f.ld * BYTES;
         plane = f.plane * 2;
         outer = outer_end - first;
         left = k_end - k;
-        base = reinterpret_cast<const char *>(f.p) + (ALONG ? first * ld + k * 2 : k * ld + first * 2);
-        step = ALONG ? S::STEP * 2 : S::STEP * ld;
+        base = reinterpret_cast<const char *>(f.p) + (ALONG ? first * ld + k * BYTES : k * ld + first * BYTES);
+        step = ALONG ? S::STEP * BYTES : S::STEP * ld;
         const int tid = threadIdx.x;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
@@ -51,24 +58,24 @@ template <class S, int ROWS, bool ALONG> struct VocabOperand {
                 const int row = tid / PIECES + S::THREADS / PIECES * j, piece = (tid % PIECES) ^ turned(row);
                 off[j] = (uint32_t)(row * ld) + piece * 16;
             } else {
-                constexpr int ROW = ROWS / 8;             // pieces of a row
-                const int row = tid / ROW + S::THREADS / ROW * j, at = tid % ROW, col = ((at >> 1) ^ mixed(row)) * 16 + (at & 1) * 8;
-                off[j] = col < outer ? (uint32_t)(row * ld) + col * 2 : kOutside;
+                constexpr int ROW = ROWS / EACH, GROUP = 16 / EACH;          // pieces of a row, of 16 columns
+                const int row = tid / ROW + S::THREADS / ROW * j, at = tid % ROW, col = ((at / GROUP) ^ mixed(row)) * 16 + at % GROUP * EACH;
+                off[j] = col < outer ? (uint32_t)(row * ld) + col * BYTES : kOutside;
             }
         }
     }
     // the next 64 terms into LDS; terms behind the last and rows behind the last read as zeros
     __device__ __forceinline__ void load(char *lds) {
-        int64_t bytes = ALONG ? (outer - 1) * ld + (left + 7) / 8 * 16 : (left - 1) * ld + (outer + 7) / 8 * 16;
+        int64_t bytes = ALONG ? (outer - 1) * ld + (left + EACH - 1) / EACH * 16 : (left - 1) * ld + (outer + EACH - 1) / EACH * 16;
         bytes = left <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-        for (int q = 0; q < S::PLANES; ++q) {
+        for (int q = 0; q < (WIDE ? 1 : S::PLANES); ++q) {
             const Buffer b = buffer_of(base + q * plane, bytes);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 uint32_t o = off[j];
-                if (ALONG) o = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * 8 < left ? o : kOutside;
+                if (ALONG) o = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * EACH < left ? o : kOutside;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void *)(lds + q * PLANE + (j * S::THREADS + wave * 64) * 16), 16, o, 0, 0, 0);
             }
         }
@@ -77,6 +84,7 @@ template <class S, int ROWS, bool ALONG> struct VocabOperand {
     }
     // the fragments of N times 16 rows from `row` on, of the 32 terms from 32 kk on
     template <int N> static __device__ __forceinline__ void read(const char *lds, int row, int kk, Frag (&f)[N]) {
+        static_assert(!WIDE, "");
         const int lane = threadIdx.x & 63, g = lane >> 4;
         if (ALONG) {
             constexpr int ROW = S::STEP * 2;
@@ -95,6 +103,26 @@ template <class S, int ROWS, bool ALONG> struct VocabOperand {
                     f[i].h[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) half4 *)(at + h * 4 * ROW)));
             }
         }
+    }
+    // the same of a stage of float32 elements, not yet split
+    template <int N> static __device__ __forceinline__ void read_wide(const char *lds, int row, float (&x)[N][8]) {
+        static_assert(WIDE, "");
+        const int lane = threadIdx.x & 63, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (ALONG) {
+                const char *at = lds + (row + i * 16 + (lane & 15)) * (S::STEP * 4);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(at + (((2 * g + h) ^ turned(lane & 15)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][4 * h + e] = v[e];
+                }
+            } else {
+                const char *at = lds + g * 8 * (ROWS * 4) + ((((row >> 4) + i) ^ mixed(g << 3)) << 6) + (lane & 15) * 4;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = *reinterpret_cast<const float *>(at + e * (ROWS * 4));
+            }
     }
 };
 
@@ -120,7 +148,7 @@ template <class S, bool AA, bool BA> struct VocabFeed {
     int64_t m_end, n_end, k, k_end;
     int stages, coming;                  // of a tile; the next stage
     VocabTile t;
-    VocabOperand<S, S::M, AA> a;
+    VocabOperand<S, S::M, AA, S::WIDE> a;
     VocabOperand<S, S::N, BA> b;
     __device__ __forceinline__ VocabFeed(const VocabFactor &fa, const VocabFactor &fb, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end)
         : fa(fa), fb(fb), m_end(m_end), n_end(n_end), k(k), k_end(k_end), stages((int)((k_end - k + S::STEP - 1) / S::STEP)) {}
@@ -144,7 +172,7 @@ template <class S, bool AA, bool BA> struct VocabFeed {
 // terms so: 1000 to 1100.)  With four wavefronts of 128 x 128 the reads of LDS, which take most of the time that the matrix units do, would be a third
 // fewer, but 256 sums and two sets of fragments do not fit the registers (890).
 // MIX: reads spread between matrix instructions by hand, which pays with transposing reads (1110 -> 1240) and costs without (1195 -> 1167).
-template <class S, bool AA, bool BA, bool MIX, int PLANES = S::PLANES> struct VocabPipe {
+template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANES> struct VocabPipe {
     char *lds;
     int wm, wn, now;                     // rows and columns of this wavefront; the stage whose first half is in x0, y0
     Frag x0[S::NI], y0[S::NJ];
@@ -271,6 +299,57 @@ template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 
     __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 };
 
+// Of a float32 factor as it lies and three planes of the other: a wavefront splits what it has read of a stage, while the next two are on their way.  For few rows: every
+// element of the first factor is split once, and its bytes are what a product costs.
+template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 0> {
+    char *lds;
+    int wm, wn, now;
+    using A = VocabOperand<S, S::M, AA, true>;
+    using B = VocabOperand<S, S::N, BA>;
+    __device__ __forceinline__ VocabPipe(char *lds) : lds(lds), now(0) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = wave % S::WM * (S::M / S::WM);
+        wn = wave / S::WM * 64;
+    }
+    template <class Fetch> __device__ __forceinline__ void prime(Fetch fetch) {
+        fetch(lds);
+        __builtin_amdgcn_sched_barrier(0);        // (the waits count the second stage's loads)
+        fetch(lds + S::STAGE);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <class Fetch> __device__ __forceinline__ void run(int stages, f32x4 (&acc)[S::NI][S::NJ], Fetch fetch) {
+        for (int s = 0; s < stages; ++s) {
+            float raw[S::NI][8];
+            Frag x[3][S::NI], y[3][S::NJ];
+            const char *at = lds + now * S::STAGE;
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::LOADS) : "memory");
+            A::read_wide(at, wm, raw);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) B::read(at + S::OPERAND_A + q * S::PLANE_B, wn, 0, y[q]);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // (in everyone's registers)
+            fetch(lds + now * S::STAGE);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < S::NI; ++i) {
+                uint32_t w[4][3];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) split2<3>(raw[i][2 * e], raw[i][2 * e + 1], w[e]);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) x[q][i].v = make_uint4(w[0][q], w[1][q], w[2][q], w[3][q]);
+            }
+            constexpr int order[6][2] = {{0, 2}, {1, 1}, {2, 0}, {0, 1}, {1, 0}, {0, 0}};         // smallest first
+#pragma unroll
+            for (int o = 0; o < 6; ++o)
+#pragma unroll
+                for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[order[o][0]][i], y[order[o][1]][j], acc[i][j]);
+            now ^= 1;
+        }
+    }
+    __device__ __forceinline__ void end() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+};
+
 // One tile's product.
 template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void vocab_product(const VocabFactor &fa, const VocabFactor &fb, VocabTile t, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
     VocabFeed<S, AA, BA> feed(fa, fb, m_end, n_end, k, k_end);
@@ -286,6 +365,8 @@ template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void v
 
 // What exponents are taken relative to: the largest number, 0 where there is none but -infinity (words behind the last are -infinity too).
 __device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
+// e^x: of float32 inputs to 1 ulp; else by the hardware's power of two, off by |x| 2^-23.5 where x's product with log2(e) is rounded: nothing beside the results' bfloat16
+template <class S> __device__ __forceinline__ float vocab_exp(float x) { return S::PLANES == 3 ? expf(x) : __expf(x); }
 
 // four elements, or as many of them as are left
 template <class IO> __device__ __forceinline__ void store_part(IO *to, const float (&x)[4], int64_t left) {
@@ -329,7 +410,7 @@ template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams 
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e += __expf(acc[i][j][r] - base);
+            for (int r = 0; r < 4; ++r) e += vocab_exp<S>(acc[i][j][r] - base);
         e += __shfl_xor(e, 16, 64);
         e += __shfl_xor(e, 32, 64);
         if ((threadIdx.x & 48) == 0) sums[at.wave % S::WM * S::N + at.n + j * 16] = make_float2(m, e);
@@ -342,7 +423,7 @@ template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams 
         for (int w = 1; w < S::WM; ++w) m = fmaxf(m, sums[w * S::N + n].x);
         const float base = vocab_base(m);
 #pragma unroll
-        for (int w = 0; w < S::WM; ++w) e += sums[w * S::N + n].y * __expf(sums[w * S::N + n].x - base);
+        for (int w = 0; w < S::WM; ++w) e += sums[w * S::N + n].y * vocab_exp<S>(sums[w * S::N + n].x - base);
         reinterpret_cast<float2 *>(p.part)[(t.n + n) * p.parts + (p.v0 + t.m) / S::M] = make_float2(m, e);
     }
 }
@@ -362,7 +443,7 @@ template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p
             float d[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                d[r] = __expf(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
+                d[r] = vocab_exp<S>(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
                 d[r] = 16 * i + r < left ? d[r] * scale : 0.0f;
             }
             if (S::PLANES == 1) *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(pack_rne(d[0], d[1]), pack_rne(d[2], d[3]));
@@ -486,36 +567,56 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dw(cons
 using VocabLarge = VocabSize<256, 256, 2, 1>;
 using VocabSmall = VocabSize<128, 128, 2, 1>;
 using VocabPlanes = VocabSize<256, 128, 4, 3>;
+using VocabPlanesSmall = VocabSize<128, 64, 4, 3>;
+using VocabWide = VocabSize<128, 64, 4, 3, true>;
+using VocabWideSmall = VocabSize<64, 64, 4, 3, true>;
 template <class S> int64_t vocab_tiles(int64_t m, int64_t n) { return ((m + S::M - 1) / S::M) * ((n + S::N - 1) / S::N); }
 inline unsigned whole_dies(int64_t n) { return (unsigned)((n + 7) / 8 * 8); }
 
-template <class S> hipError_t run_logits(const VocabParams &p, bool backward, hipStream_t s) {
-    const int64_t tiles = vocab_tiles<S>(p.V, p.T), most = 256 * S::PER_UNIT;
-    const dim3 grid(whole_dies(tiles < most ? tiles : most)), block(S::THREADS);
-    if (backward) hipLaunchKernelGGL((k_vocab_logits<S, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_vocab_logits<S, false>), grid, block, 0, s, p);
-    return hipGetLastError();
-}
-template <class S> hipError_t run_dh(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dh<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.T) * p.splits)), dim3(S::THREADS), 0, s, p);
-    return hipGetLastError();
-}
-template <class S> hipError_t run_dw(const VocabParams &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V) * p.splits_w)), dim3(S::THREADS), 0, s, p);
+struct RunLogits {
+    static constexpr bool WIDE = true;
+    const VocabParams &p;
+    bool backward;
+    hipStream_t s;
+    template <class S> void run() const {
+        const int64_t tiles = vocab_tiles<S>(p.V, p.T), most = 256 * S::PER_UNIT;
+        const dim3 grid(whole_dies(tiles < most ? tiles : most)), block(S::THREADS);
+        if (backward) hipLaunchKernelGGL((k_vocab_logits<S, true>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((k_vocab_logits<S, false>), grid, block, 0, s, p);
+    }
+};
+struct RunDh {
+    static constexpr bool WIDE = true;
+    const VocabParams &p;
+    hipStream_t s;
+    template <class S> void run() const { hipLaunchKernelGGL(k_vocab_dh<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.T) * p.splits)), dim3(S::THREADS), 0, s, p); }
+};
+struct RunDw {
+    static constexpr bool WIDE = false;
+    const VocabParams &p;
+    hipStream_t s;
+    template <class S> void run() const { hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V) * p.splits_w)), dim3(S::THREADS), 0, s, p); }
+};
+template <class F> hipError_t sized(const F &f, int planes, int side, bool wide = false) {
+    if constexpr (F::WIDE) {
+        if (wide) {
+            if (side == VocabWide::M) f.template run<VocabWide>(); else f.template run<VocabWideSmall>();
+            return hipGetLastError();
+        }
+    }
+    if (planes == 3) { if (side == VocabPlanes::M) f.template run<VocabPlanes>(); else f.template run<VocabPlanesSmall>(); }
+    else { if (side == VocabLarge::M) f.template run<VocabLarge>(); else f.template run<VocabSmall>(); }
     return hipGetLastError();
 }
 hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s) {
-    if (p.planes == 3) return run_logits<VocabPlanes>(p, backward, s);
-    return p.side_z == VocabLarge::M ? run_logits<VocabLarge>(p, backward, s) : run_logits<VocabSmall>(p, backward, s);
+    const RunLogits f{p, backward, s};
+    return sized(f, p.planes, p.side_z, p.wide);
 }
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s) {
-    if (p.planes == 3) return run_dh<VocabPlanes>(p, s);
-    return p.side_h == VocabLarge::M ? run_dh<VocabLarge>(p, s) : run_dh<VocabSmall>(p, s);
+    const RunDh f{p, s};
+    return sized(f, p.planes, p.side_h, p.wide);
 }
-hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s) {
-    if (p.planes == 3) return run_dw<VocabPlanes>(p, s);
-    return p.side_w == VocabLarge::M ? run_dw<VocabLarge>(p, s) : run_dw<VocabSmall>(p, s);
-}
+hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s) { return sized(RunDw{p, s}, p.planes, p.side_w); }
 
 // ---------------------------------------------------------------- copies, rows, ends
 template <class IO, int NP> __global__ __launch_bounds__(256) void k_vocab_pack(const VocabPack p) {
@@ -533,9 +634,13 @@ template <class IO, int NP> __global__ __launch_bounds__(256) void k_vocab_pack(
         } else
 #pragma unroll
             for (int e = 0; e < 8; ++e) if (c + e < p.K) x[e] = load_io(from + e);
-        uint32_t w[4][NP];
+        if constexpr (NP == 0) {
+            Few<float, 8>::store(reinterpret_cast<float *>(p.dst) + row * p.ldd + c, x);
+            continue;
+        }
+        uint32_t w[4][NP > 0 ? NP : 1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) split2<NP>(x[2 * e], x[2 * e + 1], w[e]);
+        for (int e = 0; e < 4; ++e) split2<(NP > 0 ? NP : 1)>(x[2 * e], x[2 * e + 1], w[e]);
 #pragma unroll
         for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4 *>(p.dst + q * p.plane + row * p.ldd + c) = make_uint4(w[0][q], w[1][q], w[2][q], w[3][q]);
     }
@@ -544,7 +649,8 @@ hipError_t launch_vocab_pack(const VocabPack &p, hipStream_t s) {
     const int64_t blocks = (p.rows * (p.Kp / 8) + 255) / 256;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
     if (p.io) hipLaunchKernelGGL((k_vocab_pack<uint16_t, 1>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_vocab_pack<float, 3>), grid, block, 0, s, p);
+    else if (p.planes) hipLaunchKernelGGL((k_vocab_pack<float, 3>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_vocab_pack<float, 0>), grid, block, 0, s, p);
     return hipGetLastError();
 }
 

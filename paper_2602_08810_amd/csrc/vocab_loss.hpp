@@ -16,7 +16,8 @@ struct VocabFactor {
 
 struct VocabParams {
     int64_t T, V, K, Kp;                 // V: words of this piece; Kp: K up to whole 16-byte pieces
-    int side_z, side_h, side_w;          // rows and columns of a tile of z, dh, dw
+    int side_z, side_h, side_w;          // first side of a tile of z, dh, dw
+    bool wide;                           // w is float32, split where it is read
     int planes, io;                      // io 1: bfloat16
     const int *count;                    // device: rows that have a target (null: all T)
     VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]
@@ -39,7 +40,7 @@ hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t 
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s);
 hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s);
 
-// [rows,K] strided elements as a factor with Kp columns in rows of ldd, zeros behind the K-th; `index`: the source's row of each (and `count` rows)
+// [rows,K] strided elements as a factor with Kp columns in rows of ldd, zeros behind the K-th (no planes: in float32); `index`: the source's row of each (and `count` rows)
 struct VocabPack {
     const void *src; int64_t ld;
     uint16_t *dst; int64_t plane, ldd, rows;
