@@ -127,8 +127,9 @@ struct VocabPlan {
     size_t bytes;
 };
 
-// Float32 inputs of so few rows: the weight is split where it is read instead of copied.
-constexpr int kVocabFew = 64;
+// Float32 inputs of so few rows: the weight is split where it is read, instead of once, into a copy.  (z, dz and dh of 100 rows, 56617 words, 1472 terms 156, 163 and 141 us, from
+// a copy 193, 196 and 171 and twice 140 to make it; of 320 rows, 15179, 768 the same but for the copies; of more it is split too often.)
+constexpr int kVocabFew = 512;
 // The vocabulary is taken in as few pieces as lie in 1 GiB of workspace (a piece's dz; of a copied vocabulary its copy): of whole tiles.
 constexpr int64_t kVocabRoom = (int64_t)1 << 30;
 int64_t piece_of(int64_t words, int64_t bytes_each) {
