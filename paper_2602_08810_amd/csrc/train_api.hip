@@ -139,21 +139,21 @@ int64_t piece_of(int64_t words, int64_t bytes_each) {
     return n < words ? n : words;
 }
 
-// First side of a product's tiles and the stretches of its terms that are taken side by side (`most` at most, of 512 terms at least): what takes the least time.  Tiles are
+// First side of a product's tiles and the stretches of its terms that are taken side by side (of 512 terms at least; of z, whose parts are larger than what comes of them, of 256, and only where all fit one turn): what takes the least time.  Tiles are
 // 256 x 256 or 128 x 128, two a compute unit; of three planes 256 x 128 or 128 x 64, two a compute unit; of a wide factor 128 x 64 or 64 x 64, two.  A whole turn of the smaller
 // tiles takes 0.67 of the larger ones' time; 0.6 of three planes; 0.8 of a wide factor.  (z of 997 rows, 5003 words, 771 terms in float32: 73 us with the larger ones, 87 with the smaller;
 // of 200 rows, 15179 words, 768 terms 67 and 51; in bfloat16 of 300 rows, 32000 words, 1024 terms 34 and 38, of 100, 32768, 2048 61 and 42.)
 struct VocabShape { int side, splits; };
-VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, int most) {
+VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, bool z) {
     const int large = wide ? kVocabTile / 2 : kVocabTile, units = wide ? 512 : 256;
     const double part = wide ? 0.8 : planes == 1 ? 0.67 : 0.6;
     VocabShape best{};
     double least = 0;
     for (int side = large; side >= large / 2; side /= 2) {
         const int64_t across = planes == 1 ? side : side == kVocabTile ? 128 : 64, tiles = up(m, side) / side * (up(n, across) / across), at_once = side == large ? units : 512;
-        for (int64_t s = 1; s == 1 || (s <= most && s * 512 <= terms); ++s) {
-            // (a tile's start and end take about as long as 256 terms; every part is added once more)
-            const double time = (double)((tiles * s + at_once - 1) / at_once) * (side == large ? 1.0 : part) * ((double)((terms + s - 1) / s) + 256) * (1 + 0.01 * (double)s);
+        for (int64_t s = 1; s == 1 || (z ? tiles * s <= at_once && s * 256 <= terms : s <= 256 && s * 512 <= terms); ++s) {
+            // (a tile's start and end take about as long as 256 terms, so do two more launches; every part is added once more, those of z from memory)
+            const double time = (z && s > 1 ? 256 + 1e-4 * (double)(s * m * n) : 0) + (double)((tiles * s + at_once - 1) / at_once) * (side == large ? 1.0 : part) * ((double)((terms + s - 1) / s) + 256) * (1 + 0.01 * (double)s);
             if (!best.side || time < least) { least = time; best = {side, (int)s}; }
         }
     }
@@ -181,17 +181,19 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         const int64_t of_dz = piece_of(a->V, planes * a->T * 2);
         each = of_dz < each ? of_dz : each;
     }
-    f.each = each;
+    f.each = p.each = each;
+    p.ldz = up(each, 8);
     copy(f.h, p.h, a->h, a->h_stride, a->T, planes, backward || !rows_in_place(a->h, a->h_stride, a->K, a->io_dtype));
     copy(f.w, p.w, a->weight, a->weight_stride, each, p.wide ? 0 : planes, copied);
+    const VocabShape z = shape_of(planes, p.wide, each, a->T, a->K, true);
+    p.side_z = z.side; p.splits_z = z.splits;
+    if (z.splits > 1) p.z_part = l.take<float>(z.splits * a->T * p.ldz);
     if (!backward) {
-        p.side_z = shape_of(planes, p.wide, each, a->T, a->K, 1).side;
-        p.parts = up(a->V, p.side_z) / p.side_z;
+        p.parts = p.splits_z > 1 ? (a->V + each - 1) / each : up(a->V, p.side_z) / p.side_z;
         p.part = l.take<float>(2 * p.parts * a->T);
         p.hit = l.take<float>(a->T);
     } else {
-        p.side_z = shape_of(planes, p.wide, each, a->T, a->K, 1).side;
-        const VocabShape dh = shape_of(planes, p.wide, a->K, a->T, each, 256), dw = shape_of(planes, false, a->K, each, a->T, 256);
+        const VocabShape dh = shape_of(planes, p.wide, a->K, a->T, each, false), dw = shape_of(planes, false, a->K, each, a->T, false);
         p.side_h = dh.side; p.splits = dh.splits;
         p.side_w = dw.side; p.splits_w = dw.splits;
         // whole tiles, and rows that do not all start in the same channel of memory

@@ -366,7 +366,7 @@ template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void v
 // What exponents are taken relative to: the largest number, 0 where there is none but -infinity (words behind the last are -infinity too).
 __device__ __forceinline__ float vocab_base(float m) { return m == -INFINITY ? 0.0f : m; }
 // e^x: of float32 inputs to 1 ulp; else by the hardware's power of two, off by |x| 2^-23.5 where x's product with log2(e) is rounded: nothing beside the results' bfloat16
-template <class S> __device__ __forceinline__ float vocab_exp(float x) { return S::PLANES == 3 ? expf(x) : __expf(x); }
+template <int PLANES> __device__ __forceinline__ float vocab_exp(float x) { return PLANES == 3 ? expf(x) : __expf(x); }
 
 // four elements, or as many of them as are left
 template <class IO> __device__ __forceinline__ void store_part(IO *to, const float (&x)[4], int64_t left) {
@@ -410,7 +410,7 @@ template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams 
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e += vocab_exp<S>(acc[i][j][r] - base);
+            for (int r = 0; r < 4; ++r) e += vocab_exp<S::PLANES>(acc[i][j][r] - base);
         e += __shfl_xor(e, 16, 64);
         e += __shfl_xor(e, 32, 64);
         if ((threadIdx.x & 48) == 0) sums[at.wave % S::WM * S::N + at.n + j * 16] = make_float2(m, e);
@@ -423,11 +423,18 @@ template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams 
         for (int w = 1; w < S::WM; ++w) m = fmaxf(m, sums[w * S::N + n].x);
         const float base = vocab_base(m);
 #pragma unroll
-        for (int w = 0; w < S::WM; ++w) e += sums[w * S::N + n].y * vocab_exp<S>(sums[w * S::N + n].x - base);
+        for (int w = 0; w < S::WM; ++w) e += sums[w * S::N + n].y * vocab_exp<S::PLANES>(sums[w * S::N + n].x - base);
         reinterpret_cast<float2 *>(p.part)[(t.n + n) * p.parts + (p.v0 + t.m) / S::M] = make_float2(m, e);
     }
 }
 // and backward, dz
+template <int PLANES> __device__ __forceinline__ void store_dz(uint16_t *to, int64_t plane, const float (&d)[4]) {
+    uint32_t a[PLANES], b[PLANES];
+    split2<PLANES>(d[0], d[1], a);
+    split2<PLANES>(d[2], d[3], b);
+#pragma unroll
+    for (int q = 0; q < PLANES; ++q) *reinterpret_cast<uint2 *>(to + q * plane) = make_uint2(a[q], b[q]);
+}
 template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p, VocabTile t, int64_t T, f32x4 (&acc)[S::NI][S::NJ]) {
     const VocabPlace<S> at;
     const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
@@ -443,17 +450,10 @@ template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p
             float d[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                d[r] = vocab_exp<S>(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
+                d[r] = vocab_exp<S::PLANES>(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
                 d[r] = 16 * i + r < left ? d[r] * scale : 0.0f;
             }
-            if (S::PLANES == 1) *reinterpret_cast<uint2 *>(to + 16 * i) = make_uint2(pack_rne(d[0], d[1]), pack_rne(d[2], d[3]));
-            else {
-                uint32_t a[3], b[3];
-                split2<3>(d[0], d[1], a);
-                split2<3>(d[2], d[3], b);
-#pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2 *>(to + q * p.dz.plane + 16 * i) = make_uint2(a[q], b[q]);
-            }
+            store_dz<S::PLANES>(to + 16 * i, p.dz.plane, d);
         }
     }
 }
@@ -508,6 +508,95 @@ template <class S> struct VocabUnit {
         end = k + each < terms ? k + each : terms;
     }
 };
+
+// z in stretches of its terms side by side, where there are few tiles: words along m, rows along n
+template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_part(const VocabParams p) {
+    __shared__ __align__(16) char lds[2 * S::STAGE];
+    const int64_t T = p.count ? *p.count : p.T;
+    const VocabUnit<S> u(p.V, T, p.splits_z, p.K);
+    if (!u.there) return;
+    f32x4 acc[S::NI][S::NJ] = {};
+    vocab_product<S, true, true, false>(p.w, p.h, u.t, p.V, T, u.k, u.end, lds, acc);
+    const VocabPlace<S> place;
+    const int64_t v0 = u.t.m + place.m, n0 = u.t.n + place.n;
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) {
+        const int64_t row = n0 + j * 16;
+        if (row >= T) continue;
+        float *to = p.z_part + (u.split * p.T + row) * p.ldz + v0;
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i)
+            if (v0 + 16 * i < p.ldz) *reinterpret_cast<f32x4 *>(to + 16 * i) = acc[i][j];
+    }
+}
+// What comes of it, as of a tile of z: forward a workgroup or (few words) a wavefront a row, backward eight words a thread
+__device__ __forceinline__ f32x4 vocab_z(const VocabParams &p, int64_t row, int64_t word) {
+    const float *from = p.z_part + row * p.ldz + word;
+    f32x4 z = {};
+#pragma unroll 8
+    for (int q = 0; q < p.splits_z; ++q) z += *reinterpret_cast<const f32x4 *>(from + q * p.T * p.ldz);
+    return z;
+}
+template <int PLANES, int WAVES> __global__ __launch_bounds__(512) void k_vocab_part_sums(const VocabParams p) {
+    __shared__ float2 lds[8];
+    const int wave = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * (8 / WAVES) + wave / WAVES;
+    if (row >= p.T) return;
+    const int64_t hit = p.target[row] - p.v0;
+    float m = -INFINITY, e = 0.0f;
+    for (int64_t v = (threadIdx.x & (WAVES * 64 - 1)) * 4; v < p.V; v += WAVES * 64 * 4) {
+        f32x4 z = vocab_z(p, row, v);
+        float most = m;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (v + r >= p.V) z[r] = -INFINITY;
+            else if (v + r == hit) p.hit[row] = z[r];
+            most = fmaxf(most, z[r]);
+        }
+        const float base = vocab_base(most);
+        e *= vocab_exp<PLANES>(m - base);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e += vocab_exp<PLANES>(z[r] - base);
+        m = most;
+    }
+    float most = m;
+#pragma unroll
+    for (int x = 32; x; x >>= 1) most = fmaxf(most, __shfl_xor(most, x, 64));
+    e *= vocab_exp<PLANES>(m - vocab_base(most));
+#pragma unroll
+    for (int x = 32; x; x >>= 1) e += __shfl_xor(e, x, 64);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) lds[wave] = make_float2(most, e);
+        __syncthreads();
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, lds[w].x);
+        e = 0.0f;
+        for (int w = 0; w < WAVES; ++w) e += lds[w].y * vocab_exp<PLANES>(lds[w].x - vocab_base(most));
+    }
+    if ((threadIdx.x & (WAVES * 64 - 1)) == 0) reinterpret_cast<float2 *>(p.part)[row * p.parts + p.v0 / p.each] = make_float2(most, e);
+}
+template <int PLANES> hipError_t run_part_sums(const VocabParams &p, hipStream_t s) {
+    if (p.V <= 1024) hipLaunchKernelGGL((k_vocab_part_sums<PLANES, 1>), dim3((unsigned)((p.T + 7) / 8)), dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((k_vocab_part_sums<PLANES, 8>), dim3((unsigned)p.T), dim3(512), 0, s, p);
+    return hipGetLastError();
+}
+template <int PLANES> __global__ __launch_bounds__(256) void k_vocab_part_dz(const VocabParams p) {
+    const int64_t T = *p.count, pieces = (p.V + 7) / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / pieces, v0 = (i - row * pieces) * 8, hit = (int64_t)p.row_target[row] - p.v0 - v0;
+        const float lse = p.row_lse[row], scale = p.row_scale[row];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 z = vocab_z(p, row, v0 + 4 * h);
+            float d[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                d[r] = vocab_exp<PLANES>(z[r] - lse) - (hit == 4 * h + r ? 1.0f : 0.0f);
+                d[r] = v0 + 4 * h + r < p.V ? d[r] * scale : 0.0f;
+            }
+            store_dz<PLANES>(const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0 + 4 * h, p.dz.plane, d);
+        }
+    }
+}
 
 // dh: columns of h along m, rows along n, words summed
 template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(const VocabParams p) {
@@ -585,6 +674,12 @@ struct RunLogits {
         else hipLaunchKernelGGL((k_vocab_logits<S, false>), grid, block, 0, s, p);
     }
 };
+struct RunPart {
+    static constexpr bool WIDE = true;
+    const VocabParams &p;
+    hipStream_t s;
+    template <class S> void run() const { hipLaunchKernelGGL(k_vocab_part<S>, dim3(whole_dies(vocab_tiles<S>(p.V, p.T) * p.splits_z)), dim3(S::THREADS), 0, s, p); }
+};
 struct RunDh {
     static constexpr bool WIDE = true;
     const VocabParams &p;
@@ -609,8 +704,16 @@ template <class F> hipError_t sized(const F &f, int planes, int side, bool wide 
     return hipGetLastError();
 }
 hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s) {
-    const RunLogits f{p, backward, s};
-    return sized(f, p.planes, p.side_z, p.wide);
+    if (p.splits_z == 1) return sized(RunLogits{p, backward, s}, p.planes, p.side_z, p.wide);
+    if (const hipError_t e = sized(RunPart{p, s}, p.planes, p.side_z, p.wide); e != hipSuccess) return e;
+    if (backward) {
+        const int64_t blocks = (p.T * ((p.V + 7) / 8) + 255) / 256;
+        const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096)), block(256);
+        if (p.planes == 1) hipLaunchKernelGGL(k_vocab_part_dz<1>, grid, block, 0, s, p);
+        else hipLaunchKernelGGL(k_vocab_part_dz<3>, grid, block, 0, s, p);
+        return hipGetLastError();
+    }
+    return p.planes == 1 ? run_part_sums<1>(p, s) : run_part_sums<3>(p, s);
 }
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s) {
     const RunDh f{p, s};

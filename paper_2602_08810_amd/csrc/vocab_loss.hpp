@@ -21,9 +21,12 @@ struct VocabParams {
     int planes, io;                      // io 1: bfloat16
     const int *count;                    // device: rows that have a target (null: all T)
     VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]
-    int64_t v0, words;                   // first word of this piece, words in all
+    int64_t v0, words, each;             // first word of this piece, words in all, of a piece
+    float *z_part;                       // [splits_z,T,ldz], if there are several
+    int splits_z;
+    int64_t ldz;
     // forward
-    float *part;                         // [T, tiles of all words, 2]: largest, sum
+    float *part;                         // [T, tiles (or pieces) of all words, 2]: largest, sum
     int64_t parts;
     float *hit;                          // [T] z of the target
     const int64_t *target;
