@@ -210,3 +210,64 @@ def test_a_copied_vocabulary_in_pieces(api):
     _check(lse, want.cpu(), "lse", 5e-6)          # sums of 5001 products: 6e-8 * sqrt(5001 / 32) * 4 of a logit
     _check(r["dh"], (dz @ w.double()).cpu(), "dh")
     _check(r["dweight"], (dz.t().contiguous() @ h.double()).cpu(), "dweight")
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,K", [(90, 67, 1333), (1, 60, 4100), (3, 2500, 2050), (300, 40, 1030), (60, 1025, 600), (1100, 9, 520), (512, 260, 132), (513, 260, 132),
+                                   (520, 300, 70), (130, 2100, 772)])
+def test_long_sums_of_few_tiles(api, io, T, V, K):
+    """Logits of up to 4100 terms, in stretches of them: 6e-8 * sqrt(4100 / 32) = 7e-7 of the largest logit, up to 7, in one chain: beside lse, which is as large, under 2e-6, and
+    a factor of up to 1 + 5e-6 of an exponential."""
+    _both(api, *_make(T + V + K, T, V, K, io))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_long_sums_masks_and_strides(api, io):
+    """What is not finite, targets beyond the vocabulary and views, where the logits are summed in stretches."""
+    import torch
+    h, w, target, dloss = _make(4, 24, 300, 520, io)
+    clean = _both(api, h, w, target, dloss)
+    bad = h.clone()
+    bad[5], bad[6] = float("inf"), float("nan")
+    target[5] = target[6] = -1
+    target[8] = 300
+    for at, room in ((8, 540), (3, 541)):
+        hs, ws = (torch.full((t.shape[0], room), float("nan"), dtype=t.dtype, device="cuda")[:, at:at + 520] for t in (bad, w))
+        hs.copy_(bad)
+        ws.copy_(w)
+        loss, lse = api.lrnnx_vocab_loss_fwd(hs, ws, target.cuda())
+        others = [t for t in range(24) if t not in (5, 6, 8)]
+        assert torch.equal(loss[others], clean[0][others]) and torch.equal(lse[others], clean[1][others])
+        assert not bool(loss[5:7].any()) and bool(loss[8].isnan())
+        r = api.lrnnx_vocab_loss_bwd(hs, ws, target.cuda(), lse, dloss.cuda())
+        assert not bool(r["dh"][5:7].any()) and bool(r["dh"][8].isnan().all()) and bool(r["dweight"].isnan().all())
+        assert torch.equal(r["dh"][others], clean[2]["dh"][others])
+    target[8] = 299
+    want = vocab(h[[t for t in range(24) if t not in (5, 6)]].double(), w.double(), target[[t for t in range(24) if t not in (5, 6)]],
+                 dloss[[t for t in range(24) if t not in (5, 6)]].double())
+    loss, lse = api.lrnnx_vocab_loss_fwd(bad.cuda(), w.cuda(), target.cuda())
+    _check(api.lrnnx_vocab_loss_bwd(bad.cuda(), w.cuda(), target.cuda(), lse, dloss.cuda())["dweight"], want[3], "dweight")
+
+
+def test_long_sums_of_a_vocabulary_in_pieces(api):
+    """Rows of over a million terms that cannot be read in place, two pieces of words: the reference on the GPU, in 64 bits.  A logit in one chain of additions of 32 terms: 6e-8 *
+    sqrt(2^20 / 32) = 1.1e-5 of it (up to 7)."""
+    import torch
+    T, V, K = 3, 300, (1 << 20) - 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.randn(V, K, generator=g, device="cuda") * K ** -0.5
+    h = torch.randn(T, K, generator=g, device="cuda") * 2
+    target, dloss = torch.tensor([299, -1, 5], device="cuda"), torch.tensor([1.0, 2.0, 0.5], device="cuda")
+    loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+    r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
+    hd, wd = h.double(), w.double()
+    z = hd @ wd.t().contiguous()
+    want = torch.logsumexp(z, 1)
+    _check(lse, want.cpu(), "lse", 1.1e-5)
+    _check(loss, torch.stack([want[0] - z[0, 299], want[1] * 0, want[2] - z[2, 5]]).cpu(), "loss", 3e-5)
+    dz = torch.exp(z - want[:, None])
+    dz[0, 299] -= 1
+    dz[2, 5] -= 1
+    dz *= torch.tensor([1.0, 0.0, 0.5], device="cuda", dtype=torch.float64)[:, None]
+    _check(r["dh"], (dz @ wd).cpu(), "dh", 8e-5)
+    _check(r["dweight"], (dz.t().contiguous() @ hd).cpu(), "dweight", 8e-5)
