@@ -205,6 +205,7 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
+        if (io) p.row_rest = l.take<float>(a->T);
         if (p.splits_w > 1) p.dw_part = l.take<float>(p.splits_w * each * Kp);
         p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
@@ -275,11 +276,11 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
         if (!a->dweight) continue;
         if (launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (f.p.splits_w == 1) continue;
-        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
+        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, nullptr, nullptr, nullptr, 0, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
         if (launch_vocab_add(parts, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
     if (!a->dh) return LRNNX_OK;
-    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, a->dh};
+    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, f.p.row_rest, f.p.row_target, a->weight, a->weight_stride, a->dh};
     return status(launch_vocab_add(end, s));
 }
 

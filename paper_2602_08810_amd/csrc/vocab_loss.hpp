@@ -33,6 +33,7 @@ struct VocabParams {
     // backward, by row among those that have a target
     const float *row_lse, *row_scale;
     const int *row_target;               // -1: beyond the vocabulary
+    float *row_rest;                     // what dz of the target lost by its rounding to bfloat16
     float *dh_part;                      // [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
     float *dw_part;                      // [splits_w,V,Kp], if there are several
@@ -75,6 +76,9 @@ struct VocabAdd {
     int K, Kp, io, splits;
     const float *part;
     const int *place;                    // or null
+    const float *rest;                   // by row of the parts, or null; with the row of w that it belongs to (-1: none)
+    const int *target;
+    const void *w; int64_t w_ld;
     void *out;                           // [rows,K]
 };
 hipError_t launch_vocab_add(const VocabAdd &p, hipStream_t s);
