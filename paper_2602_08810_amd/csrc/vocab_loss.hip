@@ -641,39 +641,21 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
     static_assert(((64 + R * S::THREADS) * 2 + WAVES) * 4 <= S::STAGE, "");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % S::WM * (S::M / S::WM), wn = wave / S::WM * 64;
     const int first = (int)(p.v0 + u.t.n), some = p.V - u.t.n < S::N ? (int)(p.V - u.t.n) : S::N;
-    int held = 0;                                          // rows in the queue
-    auto stage = [&](int from, int n) {                    // n of them
-#pragma unroll 1
+    for (int j = 0; j < B::LOADS; ++j) *reinterpret_cast<uint4 *>(lb + (j * S::THREADS + tid) * 16) = make_uint4(0, 0, 0, 0);
+    uint4 h[A::LOADS];                                     // of the next 64 rows
+    float rest = 0.0f;
+    auto fetch = [&](int from, int n) {
+        if (tid < n && tid < 64) rest = p.row_rest[rows[from + tid]];
+#pragma unroll
         for (int j = 0; j < A::LOADS; ++j) {
             constexpr int ROW = S::M / 8;
             const int row = tid / ROW + S::THREADS / ROW * j, at = tid % ROW;
             const int64_t col = u.t.m + ((at >> 1) ^ A::mixed(row)) * 16 + (at & 1) * 8;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (row < n && col < p.Kp) v = *reinterpret_cast<const uint4 *>(p.h.p + rows[from + row] * p.h.ld + col);
-            *reinterpret_cast<uint4 *>(la + (j * S::THREADS + tid) * 16) = v;
+            h[j] = make_uint4(0, 0, 0, 0);
+            if (row < n && col < p.Kp) h[j] = *reinterpret_cast<const uint4 *>(p.h.p + rows[from + row] * p.h.ld + col);
         }
-#pragma unroll 1
-        for (int j = 0; j < B::LOADS; ++j) *reinterpret_cast<uint4 *>(lb + (j * S::THREADS + tid) * 16) = make_uint4(0, 0, 0, 0);
-        __syncthreads();
-        if (tid < n) {
-            const int word = words[from + tid];
-            *reinterpret_cast<uint16_t *>(lb + tid * (S::N * 2) + (((word >> 4) ^ B::mixed(tid)) << 5) + (word & 15) * 2) = (uint16_t)pack_rne(p.row_rest[rows[from + tid]], 0.0f);
-        }
-        __syncthreads();
-#pragma unroll 1
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag y[S::NJ];
-            B::read(lb, wn, kk, y);
-#pragma unroll
-            for (int i = 0; i < S::NI; ++i) {
-                Frag x[1];
-                A::read(la, wm + 16 * i, kk, x);
-#pragma unroll
-                for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[0], y[j], acc[i][j]);
-            }
-        }
-        __syncthreads();
     };
+    int held = 0;                                          // rows in the queue
     for (int64_t t0 = u.k; t0 < u.end; t0 += R * S::THREADS) {
         int word[R];
         uint64_t have[R];
@@ -688,7 +670,7 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
         if (lane == 0) found[wave] = mine;
         __syncthreads();
         int at = held;
-        for (int w = 0; w < WAVES; ++w) { if (w < wave) at += found[w]; held += found[w]; }
+        for (int w = 0; w < WAVES; ++w) { const int f = __builtin_amdgcn_readfirstlane(found[w]); if (w < wave) at += f; held += f; }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (have[r] >> lane & 1) {
@@ -701,8 +683,33 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
         __syncthreads();
         int from = 0;
         const int least = t0 + R * S::THREADS < u.end ? 64 : 1;
+        if (held >= least) fetch(0, held);
 #pragma unroll 1
-        for (; held - from >= least; from += 64) stage(from, held - from < 64 ? held - from : 64);
+        for (; held - from >= least; from += 64) {
+            const int n = held - from < 64 ? held - from : 64;
+            uint16_t *at = nullptr;                        // of the rest in its word's column
+            if (tid < n) {
+                const int word = words[from + tid];
+                at = reinterpret_cast<uint16_t *>(lb + tid * (S::N * 2) + (((word >> 4) ^ B::mixed(tid)) << 5) + (word & 15) * 2);
+                *at = (uint16_t)pack_rne(rest, 0.0f);
+            }
+#pragma unroll
+            for (int j = 0; j < A::LOADS; ++j) *reinterpret_cast<uint4 *>(la + (j * S::THREADS + tid) * 16) = h[j];
+            __syncthreads();
+            if (held - from - 64 >= least) fetch(from + 64, held - from - 64);
+#pragma unroll 1
+            for (int kk = 0; kk < 2; ++kk) {
+                Frag x[S::NI], y[S::NJ];
+                B::read(lb, wn, kk, y);
+                A::read(la, wm, kk, x);
+#pragma unroll
+                for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[i], y[j], acc[i][j]);
+            }
+            __syncthreads();
+            if (at) *at = 0;
+        }
         if (least == 1) break;
         if (from) {                                        // what is left moves to the front
             const bool moves = tid < held - from;
