@@ -1495,12 +1495,19 @@ def _grad_list(grads, name, device=None):
     return grads, ((_vp * n)(*(t.data_ptr() for t in grads)), (_i64 * n)(*(t.numel() for t in grads)), (_i32 * n)(*(_io_dtype(t) for t in grads)))
 
 
-def _apart(grads, name):
-    """Tensors that are written must not overlap."""
-    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in grads if t.numel())
-    for (_, end), (start, _) in zip(spans, spans[1:]):
-        if start < end:
+def _apart(out, name, grads=()):
+    """Tensors that are written must not overlap each other, nor what is read for another one (its own tensor is read before)."""
+    def span(t, written):
+        return t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), written
+    spans = [span(t, True) for t in out if t.numel()]
+    spans += [span(g, False) for g, t in zip(grads, out) if g.numel() and span(g, True) != span(t, True)]
+    any_end = written_end = 0
+    for start, end, written in sorted(spans):
+        if start < (any_end if written else written_end):
             raise ValueError(f"{name}: tensors overlap")
+        any_end = max(any_end, end)
+        if written:
+            written_end = max(written_end, end)
 
 
 @_native_first
@@ -1535,7 +1542,7 @@ def lrnnx_grad_clip(grads, norm, max_norm, eps=1e-6, out=None):
             if o.dtype not in (torch.float32, g.dtype):
                 raise TypeError(f"out: dtype {o.dtype}, expected torch.float32 or {g.dtype}")
         to = (ctypes.addressof(more[0]), ctypes.addressof(more[2]))
-    _apart(outs, "grads" if out is None else "out")
+    _apart(outs, "grads" if out is None else "out", () if out is None else grads)
     _check(_call("lrnnx_grad_clip", _pack_grad_clip(
         _GRAD_CLIP_SIZE, len(grads), *(ctypes.addressof(a) for a in arrays), *to, norm.data_ptr(), float(max_norm), float(eps), _stream())))
     return outs

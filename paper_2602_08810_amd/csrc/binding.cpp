@@ -4,7 +4,7 @@
 // What bounds it: small calls are bound by the host, since their kernels take 3 to 6 us.  Marshalled in Python, the
 // forward call of 16 rows of 256 steps took 15.7 us and a generated token of 64 x 1536 channels 11.2, here 6.6 and 5.0 (its
 // kernel's time); training steps, forward and backward: 16 rows of 256 steps 58.6 and 27.4, packed 76 and 35, complex 54 and 35; the
-// chained scans and their adjoints 28 and 18; a token of the short convolution 9.9 and ?; norm and clipping of 26 tensors 72 and ?.  What is left is the allocation of the outputs and the launches.
+// chained scans and their adjoints 28 and 18; a token of the short convolution 9.9 and 4.9; norm and clipping of 26 tensors 72 and 15.4.  What is left is the allocation of the outputs and the launches.
 //
 // A call is taken only where every argument has the usual form: plain strided GPU tensors on the current device with the
 // expected types and shapes, contiguous where the general path looks no further, no caller-supplied scratch,
@@ -967,14 +967,26 @@ struct Tensors {
         a.struct_size = sizeof(a);
         a.count = (int64_t)p.size(); a.grads = p.data(); a.numel = n.data(); a.dtype = type.data();
     }
-    bool apart() const {
-        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-        spans.reserve(p.size());
-        for (size_t i = 0; i < p.size(); ++i)
-            if (n[i]) spans.emplace_back((uintptr_t)p[i], (uintptr_t)p[i] + n[i] * (type[i] == LRNNX_BF16 ? 2 : 4));
-        std::sort(spans.begin(), spans.end());
-        for (size_t i = 1; i < spans.size(); ++i)
-            if (spans[i].first < spans[i - 1].second) return false;
+    struct Span { uintptr_t start, end; bool written; };
+    Span span(size_t i, bool written) const { return {(uintptr_t)p[i], (uintptr_t)p[i] + n[i] * (type[i] == LRNNX_BF16 ? 2 : 4), written}; }
+    // Tensors that are written overlap neither each other nor what is read for another one.
+    bool apart(const Tensors *grads = nullptr) const {
+        std::vector<Span> spans;
+        spans.reserve(2 * p.size());
+        for (size_t i = 0; i < p.size(); ++i) {
+            const Span s = span(i, true);
+            if (n[i]) spans.push_back(s);
+            if (!grads || !grads->n[i]) continue;
+            const Span g = grads->span(i, false);
+            if (g.start != s.start || g.end != s.end) spans.push_back(g);
+        }
+        std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.start < b.start; });
+        uintptr_t any = 0, written = 0;
+        for (const Span &s : spans) {
+            if (s.start < (s.written ? any : written)) return false;
+            any = std::max(any, s.end);
+            if (s.written) written = std::max(written, s.end);
+        }
         return true;
     }
 };
@@ -1004,11 +1016,10 @@ PyObject *grad_clip(PyObject *args, PyObject *kwargs) {
     const at::Tensor *norm = c.needed(o[1]);
     const bool out = !absent(o[4]);
     if (out) to.read(c, o[4]);
-    if (!c.good || norm->scalar_type() != at::kFloat || norm->numel() != 1 || !(out ? to : g).apart()) Py_RETURN_NONE;
+    if (!c.good || norm->scalar_type() != at::kFloat || norm->numel() != 1 || (out ? to.p.size() != g.p.size() || !to.apart(&g) : !g.apart())) Py_RETURN_NONE;
     g.give(a);
     a.norm = static_cast<const float *>(norm->data_ptr());
     if (out) {
-        if (to.p.size() != g.p.size()) Py_RETURN_NONE;
         for (size_t i = 0; i < g.p.size(); ++i)
             if ((to.type[i] != LRNNX_F32 && to.type[i] != g.type[i]) ||
                 THPVariable_Unpack(PySequence_Fast_GET_ITEM(o[4], i)).sizes() != THPVariable_Unpack(PySequence_Fast_GET_ITEM(o[0], i)).sizes()) Py_RETURN_NONE;

@@ -124,3 +124,24 @@ def test_reproducible_on_another_stream_and_in_a_graph(api):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, want)), i
+
+
+def test_results_in_the_place_of_other_gradients_are_refused(api):
+    """A result may lie where its own gradient does, and nowhere else among what the call reads or writes."""
+    import torch
+    room = torch.ones(64, device="cuda")
+    g, norm = [room[:8], room[8:16], torch.ones(8, device="cuda").bfloat16()], torch.full((), 2.0, device="cuda")
+    fresh = [torch.empty(8, device="cuda") for _ in range(3)]
+    wide = torch.ones(16, device="cuda").bfloat16()
+    for grads, out in [(g, [g[1], g[0], fresh[0]]), (g, [room[4:12], fresh[1], fresh[2]]), (g, [fresh[0], room[:8], fresh[1]]), (g, [fresh[0], fresh[0], fresh[1]]),
+                       (g[:2], [fresh[0], room[12:20]]), ([wide[:8]], [wide.view(torch.float32)])]:
+        with pytest.raises(ValueError):
+            api.lrnnx_grad_clip(grads, norm, 1.0, out=out)
+        with pytest.raises(ValueError):
+            api.lrnnx_grad_clip.__wrapped__(grads, norm, 1.0, out=out)
+    assert bool((room == 1).all())
+    api.lrnnx_grad_clip(g, norm, 1.0, 0.0, out=[g[0], fresh[1], fresh[2]])
+    assert bool((g[0] == 0.5).all()) and bool((g[1] == 1).all()) and bool((fresh[1] == 0.5).all()) and bool((fresh[2] == 0.5).all())
+    again = [room[8:16], room[8:16]]                       # read twice, written apart
+    api.lrnnx_grad_clip(again, norm, 1.0, 0.0, out=fresh[:2])
+    assert bool((fresh[0] == 0.5).all()) and bool((fresh[1] == 0.5).all()) and bool((g[1] == 1).all())
