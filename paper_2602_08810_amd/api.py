@@ -1315,6 +1315,12 @@ def _conv_rows(t, name, shape, io, out=False):
     return ptr, sb, ss
 
 
+def _not_in_place(t, name, *inputs):
+    """Steps of an input are read again where a neighbour's result may be written by then."""
+    if t is not None and any(t.data_ptr() == x.data_ptr() for x in inputs):
+        raise ValueError(f"{name}: must not be an input")
+
+
 def _state(t, name, shape, io):
     """Pointer of optional carried inputs, contiguous in the I/O type."""
     if t is None:
@@ -1357,6 +1363,7 @@ def lrnnx_short_conv_fwd(x, weight, bias=None, act="silu", x0=None, cu_seqlens=N
     packed = cu_seqlens is not None
     io, device = x.dtype, x.device
     x, shape, B, state, head = _conv_head(_CONV_FWD_SIZE, x, weight, bias, act, x0, cu_seqlens, layout)
+    _not_in_place(out, "out", x)
     y = torch.empty(shape, dtype=io, device=device) if out is None else out.unsqueeze(0) if packed else out
     last = torch.empty(state, dtype=io, device=device) if return_last_state else None
     _check(_call("lrnnx_short_conv_fwd", _pack_conv_fwd(*head, *_conv_rows(y, "out", shape, io, out=True), 0 if last is None else last.data_ptr(), _stream())))
@@ -1373,6 +1380,7 @@ def lrnnx_short_conv_bwd(x, weight, dy, bias=None, act="silu", x0=None, dx_last=
     packed = cu_seqlens is not None
     io, device = x.dtype, x.device
     x, shape, B, state, head = _conv_head(_CONV_BWD_SIZE, x, weight, bias, act, x0, cu_seqlens, layout)
+    _not_in_place(out, "out", x, dy)
     pdy = _conv_rows(dy.unsqueeze(0) if packed else dy, "dy", shape, io)
     dx = torch.empty(shape, dtype=io, device=device) if out is None else out.unsqueeze(0) if packed else out
     pdx = _conv_rows(dx, "out", shape, io, out=True)

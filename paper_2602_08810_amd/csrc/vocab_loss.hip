@@ -912,27 +912,27 @@ hipError_t launch_vocab_rows(const VocabRows &p, hipStream_t s) {
 // lse and loss of a row from its tiles' largest numbers and sums, a wavefront a row
 __global__ __launch_bounds__(256) void k_vocab_loss(const VocabLoss p) {
     const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= p.T) return;
-    const float2 *part = reinterpret_cast<const float2 *>(p.part) + row * p.parts;
-    float m = -INFINITY;
-    for (int64_t i = lane; i < p.parts; i += 64) m = fmaxf(m, part[i].x);
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < p.T; row += (int64_t)gridDim.x * 4) {
+        const float2 *part = reinterpret_cast<const float2 *>(p.part) + row * p.parts;
+        float m = -INFINITY;
+        for (int64_t i = lane; i < p.parts; i += 64) m = fmaxf(m, part[i].x);
 #pragma unroll
-    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
-    float e = 0.0f;
-    const float base = vocab_base(m);
-    for (int64_t i = lane; i < p.parts; i += 64) e += part[i].y * expf(part[i].x - base);
+        for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+        float e = 0.0f;
+        const float base = vocab_base(m);
+        for (int64_t i = lane; i < p.parts; i += 64) e += part[i].y * expf(part[i].x - base);
 #pragma unroll
-    for (int x = 32; x; x >>= 1) e += __shfl_xor(e, x, 64);
-    if (lane == 0) {
-        const float lse = base + logf(e);
-        const int64_t t = p.target[row];
-        p.lse[row] = lse;
-        p.loss[row] = t < 0 ? 0.0f : t < p.V ? lse - p.hit[row] : __builtin_nanf("");
+        for (int x = 32; x; x >>= 1) e += __shfl_xor(e, x, 64);
+        if (lane == 0) {
+            const float lse = base + logf(e);
+            const int64_t t = p.target[row];
+            p.lse[row] = lse;
+            p.loss[row] = t < 0 ? 0.0f : t < p.V ? lse - p.hit[row] : __builtin_nanf("");
+        }
     }
 }
 hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s) {
-    hipLaunchKernelGGL(k_vocab_loss, dim3((unsigned)((p.T + 3) / 4)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(k_vocab_loss, dim3((unsigned)(p.T < 1 << 22 ? (p.T + 3) / 4 : 1 << 20)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -230,3 +230,16 @@ def test_reproducible_on_another_stream_and_in_a_graph(api, layout, io):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, want)), i
+
+
+def test_in_place_is_refused(api):
+    import torch
+    x, dy, w = torch.zeros(2, 9, 8, device="cuda"), torch.zeros(2, 9, 8, device="cuda"), torch.zeros(8, 3, device="cuda")
+    with pytest.raises(ValueError):
+        api.lrnnx_short_conv_fwd(x, w, out=x)
+    for out in (x, dy):
+        with pytest.raises(ValueError):
+            api.lrnnx_short_conv_bwd(x, w, dy, out=out)
+    cu = torch.tensor([0, 9], device="cuda")
+    with pytest.raises(ValueError):
+        api.lrnnx_short_conv_fwd(x[0], w, cu_seqlens=cu, out=x[0])

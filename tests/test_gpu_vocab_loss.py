@@ -294,3 +294,19 @@ def test_gradients_in_bfloat16_are_as_exact_as_their_own_rounding(api, T, V, K, 
     dz *= torch.where(there, dloss.double(), 0.0)[:, None]
     _check(r["dh"], (dz @ wd).cpu(), "dh", 2e-3)
     _check(r["dweight"], (dz.t().contiguous() @ hd).cpu(), "dweight", 2e-3)
+
+
+def test_more_rows_than_workgroups(api):
+    """2^26 rows: a wavefront a row would be 2^32 threads.  Logits of 8 products of numbers up to 5: under 5e-6; lse of 5 of them."""
+    import torch
+    T, V, K = (1 << 26) + 3, 5, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.randn(T, K, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(V, K, generator=g, device="cuda").bfloat16()
+    target = torch.randint(-1, V, (T,), generator=g, device="cuda")
+    loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+    for rows in (slice(0, 1000), slice(1 << 25, (1 << 25) + 1000), slice(T - 1000, T)):
+        z = h[rows].double() @ w.double().t().contiguous()
+        want, t = torch.logsumexp(z, 1), target[rows]
+        pick = torch.where(t >= 0, want - z.gather(1, t.clamp(min=0)[:, None])[:, 0], 0.0)
+        assert float((lse[rows].double() - want).abs().max()) < 5e-6 and float((loss[rows].double() - pick).abs().max()) < 1e-5
