@@ -143,6 +143,7 @@ int64_t piece_of(int64_t words, int64_t bytes_each) {
 // 256 x 256 or 128 x 128, two a compute unit; of three planes 256 x 128 or 128 x 64, two a compute unit; of a wide factor 128 x 64 or 64 x 64, two.  A whole turn of the smaller
 // tiles takes 0.67 of the larger ones' time; 0.6 of three planes; 0.8 of a wide factor.  (z of 997 rows, 5003 words, 771 terms in float32: 73 us with the larger ones, 87 with the smaller;
 // of 200 rows, 15179 words, 768 terms 67 and 51; in bfloat16 of 300 rows, 32000 words, 1024 terms 34 and 38, of 100, 32768, 2048 61 and 42.)
+int64_t side_n(int planes, int side) { return planes == 1 ? side : side == kVocabTile ? 128 : 64; }
 struct VocabShape { int side, splits; };
 VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, bool z) {
     const int large = wide ? kVocabTile / 2 : kVocabTile, units = wide ? 512 : 256;
@@ -150,10 +151,10 @@ VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, 
     VocabShape best{};
     double least = 0;
     for (int side = large; side >= large / 2; side /= 2) {
-        const int64_t across = planes == 1 ? side : side == kVocabTile ? 128 : 64, tiles = up(m, side) / side * (up(n, across) / across), at_once = side == large ? units : 512;
+        const int64_t across = side_n(planes, side), tiles = up(m, side) / side * (up(n, across) / across), at_once = side == large ? units : 512;
         for (int64_t s = 1; s == 1 || (z ? tiles * s <= at_once && s * 256 <= terms : s <= 256 && s * 512 <= terms); ++s) {
-            // (a tile's start and end take about as long as 256 terms, so do two more launches; every part is added once more, those of z from memory)
-            const double time = (z && s > 1 ? 256 + 1e-4 * (double)(s * m * n) : 0) + (double)((tiles * s + at_once - 1) / at_once) * (side == large ? 1.0 : part) * ((double)((terms + s - 1) / s) + 256) * (1 + 0.01 * (double)s);
+            // (of z two more launches, as long as 256 terms, and its parts from memory)
+            const double time = (z && s > 1 ? 256 + 1e-4 * (double)(s * m * n) : 0) + (side == large ? 1.0 : part) * vocab_time(tiles, s, at_once, terms);
             if (!best.side || time < least) { least = time; best = {side, (int)s}; }
         }
     }
@@ -201,7 +202,7 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         p.dz.p = l.take<uint16_t>(planes * p.dz.plane);
         f.rows.index = l.take<int>(a->T);
         f.rows.place = l.take<int>(a->T);
-        f.rows.count = l.take<int>(1);
+        f.rows.count = l.take<int>(2);
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
@@ -210,6 +211,9 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
         f.h.index = f.rows.index; f.h.count = f.rows.count;
+        f.rows.side = (int)side_n(planes, p.side_h); f.rows.across = (int)(up(a->K, p.side_h) / p.side_h);
+        f.rows.at_once = p.side_h == kVocabTile ? 256 : 512;
+        f.rows.units = f.rows.across * (up(a->T, f.rows.side) / f.rows.side) * p.splits; f.rows.each = each; f.rows.splits = p.splits;
         f.rows.T = a->T; f.rows.V = a->V; f.rows.target = a->target;
     }
     f.bytes = l.at;
@@ -276,11 +280,11 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
         if (!a->dweight) continue;
         if (launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (f.p.splits_w == 1) continue;
-        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, nullptr, nullptr, nullptr, 0, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
+        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, nullptr, nullptr, nullptr, nullptr, 0, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
         if (launch_vocab_add(parts, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
     if (!a->dh) return LRNNX_OK;
-    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, f.p.row_rest, f.p.row_target, a->weight, a->weight_stride, a->dh};
+    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, f.rows.count, f.p.row_rest, f.p.row_target, a->weight, a->weight_stride, a->dh};
     return status(launch_vocab_add(end, s));
 }
 

@@ -614,8 +614,8 @@ template <int PLANES> __global__ __launch_bounds__(256) void k_vocab_part_dz(con
 // dh: columns of h along m, rows along n, words summed
 template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(const VocabParams p) {
     __shared__ __align__(16) char lds[2 * S::STAGE];
-    const int64_t T = p.count ? *p.count : p.T;
-    const VocabUnit<S> u(p.K, T, p.splits, p.V);
+    const int64_t T = p.count[0];
+    const VocabUnit<S> u(p.K, T, p.count[1], p.V);
     if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
     vocab_product<S, false, true, true>(p.w, p.dz, u.t, p.K, T, u.k, u.end, lds, acc);
@@ -625,7 +625,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
         if (row >= T) continue;
-        float *to = p.dh_part + (u.split * p.T + row) * p.Kp + c0;       // rows of whole 32-byte pieces: four columns are there or not
+        float *to = p.dh_part + (u.split * T + row) * p.Kp + c0;       // rows of whole 32-byte pieces: four columns are there or not
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
             if (c0 + 16 * i < p.Kp) {
@@ -902,7 +902,26 @@ __global__ __launch_bounds__(1024) void k_vocab_rows(const VocabRows p) {
         }
         __syncthreads();
     }
-    if (threadIdx.x == 0) *p.count = base;
+    // the stretches of dh's words that suit so many rows, within the room and the workgroups that there are
+    __shared__ float least[1024];
+    const int s = threadIdx.x + 1;
+    const int64_t tiles = (int64_t)p.across * ((base + p.side - 1) / p.side);
+    const bool fits = s == 1 || ((int64_t)s * base <= p.splits * p.T && tiles * s <= p.units && (int64_t)s * 512 <= p.each);
+    const float mine = fits ? vocab_time(tiles, s, p.at_once, p.each) : INFINITY;
+    least[threadIdx.x] = mine;
+    __syncthreads();
+    for (int half = 512; half; half >>= 1) {
+        if ((int)threadIdx.x < half) least[threadIdx.x] = fminf(least[threadIdx.x], least[threadIdx.x + half]);
+        __syncthreads();
+    }
+    const uint64_t best = __ballot(fits && mine == least[0]);
+    if (lane == 0) part[wave] = best ? wave * 64 + __ffsll((unsigned long long)best) : 1 << 30;
+    __syncthreads();
+    if (threadIdx.x) return;
+    int splits = part[0];
+    for (int w = 1; w < 16; ++w) splits = part[w] < splits ? part[w] : splits;
+    p.count[0] = base;
+    p.count[1] = splits;
 }
 hipError_t launch_vocab_rows(const VocabRows &p, hipStream_t s) {
     hipLaunchKernelGGL(k_vocab_rows, dim3(1), dim3(1024), 0, s, p);
@@ -941,7 +960,8 @@ hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s) {
 template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_add(const VocabAdd p) {
     constexpr int ITEMS = 256 / PARTS;
     __shared__ f32x4 lds[PARTS > 1 ? 256 : 1];
-    const int64_t pieces = p.Kp / 4, n = p.rows * pieces, step = (int64_t)gridDim.x * ITEMS;
+    const int64_t pieces = p.Kp / 4, n = p.rows * pieces, step = (int64_t)gridDim.x * ITEMS, plane = p.count ? p.count[0] * (int64_t)p.Kp : p.plane;
+    const int splits = p.count ? p.count[1] : p.splits;
     const int mine = threadIdx.x % ITEMS, q0 = threadIdx.x / ITEMS;
     for (int64_t first = (int64_t)blockIdx.x * ITEMS; first < n; first += step) {
         const int64_t i = first + mine, row = i / pieces;
@@ -951,7 +971,7 @@ template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_ad
         if (at >= 0) {
             const float *from = p.part + at * p.Kp + c;
 #pragma unroll 4
-            for (int q = q0; q < p.splits; q += PARTS) s += *reinterpret_cast<const f32x4 *>(from + q * p.plane);
+            for (int q = q0; q < splits; q += PARTS) s += *reinterpret_cast<const f32x4 *>(from + q * plane);
         }
         if constexpr (PARTS > 1) {
             lds[threadIdx.x] = s;

@@ -19,7 +19,7 @@ struct VocabParams {
     int side_z, side_h, side_w;          // first side of a tile of z, dh, dw
     bool wide;                           // w is float32, split where it is read
     int planes, io;                      // io 1: bfloat16
-    const int *count;                    // device: rows that have a target (null: all T)
+    const int *count;                    // device: rows that have a target (null: all T); stretches of dh's words
     VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]
     int64_t v0, words, each;             // first word of this piece, words in all, of a piece
     float *z_part;                       // [splits_z,T,ldz], if there are several
@@ -34,7 +34,7 @@ struct VocabParams {
     const float *row_lse, *row_scale;
     const int *row_target;               // -1: beyond the vocabulary
     float *row_rest;                     // what dz of the target lost by its rounding to bfloat16
-    float *dh_part;                      // [splits,T,Kp]
+    float *dh_part;                      // [stretches, rows that have a target, Kp], within [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
     float *dw_part;                      // [splits_w,V,Kp], if there are several
     int splits_w;
@@ -53,6 +53,12 @@ struct VocabPack {
 };
 hipError_t launch_vocab_pack(const VocabPack &p, hipStream_t s);
 
+// What a product of so many tiles takes, in so many stretches of its terms: turns of the workgroups that there are at once; a tile's start and end take about as long as 256 terms,
+// and every part is added once more.
+__host__ __device__ inline float vocab_time(int64_t tiles, int64_t splits, int64_t at_once, int64_t terms) {
+    return (float)((tiles * splits + at_once - 1) / at_once) * ((float)((terms + splits - 1) / splits) + 256.0f) * (1.0f + 0.01f * (float)splits);
+}
+
 struct VocabRows {
     int64_t T, V;
     const int64_t *target;
@@ -60,6 +66,9 @@ struct VocabRows {
     int *index, *place, *count;          // row of the T that the i-th with a target is; place: the other way, -1: none
     float *row_lse, *row_scale;
     int *row_target;
+    // for dh: tiles along K, rows of a tile, workgroups at once and in the launch; words of a piece; stretches that there is room for with all rows
+    int across, side, at_once;
+    int64_t units, each, splits;
 };
 hipError_t launch_vocab_rows(const VocabRows &p, hipStream_t s);
 
@@ -76,6 +85,7 @@ struct VocabAdd {
     int K, Kp, io, splits;
     const float *part;
     const int *place;                    // or null
+    const int *count;                    // or null; device: rows of a part, parts
     const float *rest;                   // by row of the parts, or null; with the row of w that it belongs to (-1: none)
     const int *target;
     const void *w; int64_t w_ld;
