@@ -16,6 +16,9 @@
  *     forward, backward and single-token update;
  *   - time-varying with the per-step coefficients a_k, b_k supplied by the caller, real or
  *     complex (the time-varying S5-style and gated layers of Sec. 2.2.2), forward and backward.
+ * Beside it stand the operators of a language model's block around a recurrence whose state is a
+ * matrix (gated delta rule, norms around a block) and what a training step needs around those (short
+ * causal convolution, loss over a vocabulary, norm and clipping of gradients), each with its own rules below.
  * The hidden state x[B,D,L,N] is never written to memory (Sec. 3, the stated
  * advantage of the fused kernels); the backward pass recomputes it.
  *
@@ -773,8 +776,8 @@ size_t lrnnx_vocab_loss_fwd_workspace_bytes(const lrnnx_vocab_fwd_args *args);
 /* Its reverse-mode derivative for upstream gradients dloss [T] float (element stride dloss_stride; 0: one number for all rows):
  *     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz weight,   dweight = dz^T h,
  * dh [T,K] and dweight [V,K] in io_dtype, contiguous; either may be NULL.  Inputs as in the forward call, lse as it left it.  z is
- * formed again a piece of the vocabulary at a time; a piece of dz, in bfloat16 (with float32 inputs as the sum of three), lies in the
- * workspace: lrnnx_vocab_loss_bwd_workspace_bytes(args) bytes, 256-byte aligned.  Rows without a target take no part: their dh is zero, and nothing
+ * formed again a piece of the vocabulary at a time; a piece of dz, in bfloat16 (what that takes from the target's element is added to both
+ * products; with float32 inputs as the sum of three), lies in the workspace: lrnnx_vocab_loss_bwd_workspace_bytes(args) bytes, 256-byte aligned.  Rows without a target take no part: their dh is zero, and nothing
  * in them, finite or not, reaches dweight.  Sums are taken in a fixed order: results are bitwise reproducible.            */
 typedef struct lrnnx_vocab_bwd_args {
     size_t struct_size;
