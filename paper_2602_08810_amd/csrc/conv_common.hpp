@@ -60,6 +60,7 @@ template <class T, int VEC> struct Few {
         else return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     }
     static __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {
+        static_assert(sizeof(T) == 4 ? VEC <= 2 || VEC % 4 == 0 : VEC == 1 || VEC == 4 || VEC % 8 == 0, "whole accesses");
         if constexpr (VEC == 1) store_io(p, x[0]);
         else if constexpr (sizeof(T) == 4 && VEC == 2) *reinterpret_cast<two *>(p) = u32x2{__float_as_uint(x[0]), __float_as_uint(x[1])};
         else if constexpr (sizeof(T) == 4)
