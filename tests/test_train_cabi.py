@@ -133,5 +133,5 @@ def test_gradients_refuse(api):
         numel = (ctypes.c_int64 * len(v))(*v)
         return _call(api, "lrnnx_grad_norm_workspace_bytes", _fill(api.GradNormArgs, count=len(v), numel=at(numel), grads=P, dtype=P, norm=P))
     assert sizes(0, 0) == 0 and sizes(5, -1) == 0 and sizes(1) == 8 and sizes(8192, 8193, 0) == 24
-    # pieces of total / 4096 elements rounded up by less than 2048: at least 4096 / (1 + 2048 * 4096 / total) of them
-    assert 4092 * 8 <= sizes(10 ** 10) <= 4096 * 8
+    # pieces of total / 16384 elements rounded up by less than 2048: at least 16384 / (1 + 2048 * 16384 / total) of them
+    assert 16329 * 8 <= sizes(10 ** 10) <= 16384 * 8
