@@ -29,6 +29,14 @@ template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct Vocab
     static constexpr int PER_UNIT = M == 256 ? 1 : 2;                                 // workgroups a compute unit
 };
 
+// 16 bytes a lane from memory to LDS, beside the lanes before.  Not the compiler's instruction for it: of that it takes every later read of LDS for one of what it brings, and waits for it
+// (z of 8192 x 32768, 2048 terms: 960 us so, @@); what has to be waited for is waited for where a stage changes hands.  It has no result in a register.  FRESH: the descriptor
+// may have come from the vector unit just now, which takes five instructions' time.
+__device__ __forceinline__ void load_lds(uint32_t to, const u32x4 &from, uint32_t off, bool fresh) {
+    if (fresh) asm volatile("s_nop 4");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from));
+}
+
 // One factor of a tile.  ALONG: rows of the source are the tile's rows (columns: the terms of the sum); else rows of the source are the terms.
 // LDS, ALONG: [ROWS rows][STEP terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), or of rows of four ^ (row / 4 & 3), so that the 16 rows of a fragment,
 // read at one place each, lie in all banks.  Else [STEP terms][ROWS], pairs of pieces (16 columns, what a transposing read takes of a row) exchanged by pair ^ (bits 3, 4 and 0, 1 of the
@@ -76,12 +84,14 @@ template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand 
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int q = 0; q < (WIDE ? 1 : S::PLANES); ++q) {
-            const Buffer b = buffer_of(base + q * plane, bytes);
+            const char *at = base + q * plane;
+            const u32x4 b = {(uint32_t)(uintptr_t)at, (uint32_t)((uintptr_t)at >> 32) & 0xffff, (uint32_t)bytes, 0x00020000};       // as of buffer_of
+            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)(lds + q * PLANE + wave * 1024);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 uint32_t o = off[j];
                 if (ALONG) o = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * EACH < left ? o : kOutside;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void *)(lds + q * PLANE + (j * S::THREADS + wave * 64) * 16), 16, o, 0, 0, 0);
+                load_lds(to + j * S::THREADS * 16, b, o, j == 0);
             }
         }
         base += step;
@@ -197,14 +207,13 @@ template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANE
 #pragma unroll
             for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[i], y[j], acc[i][j]);
     }
-    template <int LOADS> static __device__ __forceinline__ void spread() {
+    static __device__ __forceinline__ void spread() {
         if constexpr (MIX) {
             constexpr int MATRIX = S::NI * S::NJ, READS = (AA ? S::NI : 2 * S::NI) + (BA ? S::NJ : 2 * S::NJ), PER = MATRIX / READS;
 #pragma unroll
             for (int i = 0; i < READS; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x008, MATRIX - PER * READS, 0);
         }
@@ -223,13 +232,14 @@ template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANE
             Frag x1[S::NI], y1[S::NJ];
             read(now, 1, x1, y1);
             sums(x0, y0, acc);
-            spread<0>();
+            spread();
             // the other stage has come, and this one is in everyone's registers
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            read(now ^ 1, 0, x0, y0);
             fetch(lds + now * S::STAGE);
+            __builtin_amdgcn_sched_barrier(0);
+            read(now ^ 1, 0, x0, y0);
             sums(x1, y1, acc);
-            spread<S::LOADS>();
+            spread();
             now ^= 1;
         }
     }
@@ -480,7 +490,7 @@ template <class S, bool BWD> __global__ __launch_bounds__(S::THREADS) void k_voc
     VocabFeed<S, true, true> feed(p.w, p.h, p.V, T, 0, p.K);
     feed.t = tiles.tile(first + at);
     feed.start();
-    VocabPipe<S, true, true, false> pipe(lds);
+    VocabPipe<S, true, true, true> pipe(lds);
     auto next = [&]() __attribute__((always_inline)) {
         coming += turn;
         if (coming >= count) return false;
@@ -528,7 +538,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_part(co
     const VocabUnit<S> u(p.V, T, p.splits_z, p.K);
     if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, true, true, false>(p.w, p.h, u.t, p.V, T, u.k, u.end, lds, acc);
+    vocab_product<S, true, true, true>(p.w, p.h, u.t, p.V, T, u.k, u.end, lds, acc);
     const VocabPlace<S> place;
     const int64_t v0 = u.t.m + place.m, n0 = u.t.n + place.n;
 #pragma unroll
