@@ -400,32 +400,50 @@ template <class S> struct VocabPlace {
         n = wave / S::WM * 64 + (lane & 15);
     }
 };
-// What comes of a tile of z, words along m, rows along n: forward, the largest number and the sum of exponentials of every row
+// e^(x - base)
+template <int PLANES> struct VocabExp {
+    float base;                          // (times log2(e), but for float32 inputs)
+    __device__ __forceinline__ VocabExp(float b) : base(PLANES == 3 ? b : b * -1.44269504f) {}
+    __device__ __forceinline__ float operator()(float x) const { return PLANES == 3 ? expf(x - base) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, 1.44269504f, base)); }
+};
+// What comes of a tile of z, words along m, rows along n: forward, the largest number and the sum of exponentials of every row.  (Its 128 numbers a lane are an eighth of a tile's time: what
+// only the last tile of the vocabulary and what only a target's tile needs is apart.)
 template <class S> __device__ __forceinline__ void vocab_sums(const VocabParams &p, VocabTile t, int64_t T, float2 *sums, f32x4 (&acc)[S::NI][S::NJ]) {
     const VocabPlace<S> at;
     const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
+    if (t.m + S::M > p.V)
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) if (16 * i + r >= left) acc[i][j][r] = -INFINITY;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
         const int64_t hit = (row < T ? p.target[row] : -1) - p.v0 - v0;
-        float m = -INFINITY, z = 0.0f;
+        const bool here = hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4 && hit < left;
+        if (__any(here)) {
+            float z = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z = hit == 16 * i + r ? acc[i][j][r] : z;
+            if (here) p.hit[row] = z;
+        }
+        float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (16 * i + r >= left) acc[i][j][r] = -INFINITY;
-                m = fmaxf(m, acc[i][j][r]);
-                z = hit == 16 * i + r ? acc[i][j][r] : z;
-            }
-        if (hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4 && hit < left) p.hit[row] = z;
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[i][j][r]);
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
         float e = 0.0f;
-        const float base = vocab_base(m);
+        const VocabExp<S::PLANES> exponential(vocab_base(m));
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) e += vocab_exp<S::PLANES>(acc[i][j][r] - base);
+            for (int r = 0; r < 4; ++r) e += exponential(acc[i][j][r]);
         e += __shfl_xor(e, 16, 64);
         e += __shfl_xor(e, 32, 64);
         if ((threadIdx.x & 48) == 0) sums[at.wave % S::WM * S::N + at.n + j * 16] = make_float2(m, e);
@@ -455,27 +473,37 @@ __device__ __forceinline__ float vocab_rest(float d) {
     const float there = __uint_as_float(pack_rne(d, 0.0f) << 16);
     return fabsf(there) < INFINITY ? d - there : 0.0f;
 }
+template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(const VocabParams &p, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential, float scale,
+                                                                               f32x4 (&acc)[S::NI][S::NJ], int j) {
+    uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0;
+#pragma unroll
+    for (int i = 0; i < S::NI; ++i) {
+        float d[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            d[r] = exponential(acc[i][j][r]);
+            if (APART && hit == 16 * i + r) d[r] -= 1.0f;
+            d[r] *= scale;
+            if (APART && 16 * i + r >= left) d[r] = 0.0f;
+            if (APART && S::PLANES == 1 && hit == 16 * i + r && 16 * i + r < left) p.row_rest[row] = vocab_rest(d[r]);
+        }
+        store_dz<S::PLANES>(to + 16 * i, p.dz.plane, d);
+    }
+}
 template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p, VocabTile t, int64_t T, f32x4 (&acc)[S::NI][S::NJ]) {
     const VocabPlace<S> at;
     const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
-        if (row >= T) continue;
-        const float lse = p.row_lse[row], scale = p.row_scale[row];
-        const int64_t hit = (int64_t)p.row_target[row] - p.v0 - v0;
-        uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0;
-#pragma unroll
-        for (int i = 0; i < S::NI; ++i) {
-            float d[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                d[r] = vocab_exp<S::PLANES>(acc[i][j][r] - lse) - (hit == 16 * i + r ? 1.0f : 0.0f);
-                d[r] = 16 * i + r < left ? d[r] * scale : 0.0f;
-                if (S::PLANES == 1 && hit == 16 * i + r && 16 * i + r < left) p.row_rest[row] = vocab_rest(d[r]);
-            }
-            store_dz<S::PLANES>(to + 16 * i, p.dz.plane, d);
-        }
+        const bool there = row < T;
+        const float lse = there ? p.row_lse[row] : 0.0f, scale = there ? p.row_scale[row] : 0.0f;
+        const int64_t hit = (there ? (int64_t)p.row_target[row] : -1) - p.v0 - v0;
+        const bool apart = t.m + S::M > p.V || __any(hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4);
+        const VocabExp<S::PLANES> exponential(lse);
+        if (!there) continue;
+        if (apart) vocab_dz_column<S, true>(p, row, v0, left, hit, exponential, scale, acc, j);
+        else vocab_dz_column<S, false>(p, row, v0, left, hit, exponential, scale, acc, j);
     }
 }
 // A workgroup stays and takes a tile after the other; the next one's factors are on their way while it works on what comes of the one before.
