@@ -30,7 +30,7 @@ template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct Vocab
 };
 
 // 16 bytes a lane from memory to LDS, beside the lanes before.  Not the compiler's instruction for it: of that it takes every later read of LDS for one of what it brings, and waits for it
-// (z of 8192 x 32768, 2048 terms: 960 us so, @@); what has to be waited for is waited for where a stage changes hands.  It has no result in a register.  FRESH: the descriptor
+// (dh of 8192 x 2048, 32768 terms: 944 us so, 828); what has to be waited for is waited for where a stage changes hands.  It has no result in a register.  FRESH: the descriptor
 // may have come from the vector unit just now, which takes five instructions' time.
 __device__ __forceinline__ void load_lds(uint32_t to, const u32x4 &from, uint32_t off, bool fresh) {
     if (fresh) asm volatile("s_nop 4");
@@ -173,21 +173,25 @@ template <class S, bool AA, bool BA> struct VocabFeed {
         coming = 0;
     }
     // `next`: sets t to the next tile, false if there is none
-    template <class F> __device__ __forceinline__ void fetch(char *lds, F next) {
-        if (coming == stages && next()) start();
-        ++coming;
-        a.load(lds);
-        b.load(lds + S::OPERAND_A);
+    template <class F> __device__ __forceinline__ void fetch(char *lds, int halves, F next) {
+        if (halves & 1) {
+            if (coming == stages && next()) start();
+            ++coming;
+            a.load(lds);
+        }
+        if (halves & 2) b.load(lds + S::OPERAND_A);
     }
 };
 
 // acc[i][j] += sum over the terms of a[16 i + ..] b[16 j + ..], for this wavefront's part of the tile; acc: column (n) lane % 16, rows (m) 4 (lane / 16) .. + 3.
 // Two stages of LDS; fragments are read half a stage ahead of the instructions that use them, and a stage's memory is filled again as soon as its second half
-// is in registers, two halves before it is read: one barrier a stage.  (Fragments read where they are used: 839 TFLOP/s where this does 1070 to 1190; four stages of 32
-// terms so: 1000 to 1100.)  With four wavefronts of 128 x 128 the reads of LDS, which take most of the time that the matrix units do, would be a third
-// fewer, but 256 sums and two sets of fragments do not fit the registers (890).
-// MIX: reads spread between matrix instructions by hand, which pays with transposing reads (1110 -> 1240) and costs without (1195 -> 1167).
-template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANES> struct VocabPipe {
+// is in registers, two halves before it is read: one barrier a stage.  z of 8192 x 32768, 2048 terms: 1270 to 1310 TFLOP/s, dh 1310 to 1345.  Reads at the end of a half, where the compiler puts them if
+// left to itself: z 50 us of 980 slower; four stages of 32 terms, a barrier each: z 987 for 903, dh 863 for 828 (half as long rows a load); and so that half of the wavefronts
+// read while the others multiply, two barriers each: 1070 and 900.  With four wavefronts of 128 x 128 a third fewer reads, but 256 sums and two sets of fragments do not fit the registers.
+template <class S, bool AA, bool BA, int KIND = S::WIDE ? 0 : S::PLANES> struct VocabPipe {
+    // matrix instructions that go before the loads of a stage's first and second factor, four each, so that the matrix unit has work while they are issued.  (Transposing reads are twice as
+    // many, and need the others beside them.)  z of 8192 x 32768, 2048 terms: none before 906 us, so 845; dh 828 and 818, with loads later 866.
+    static constexpr int FIRST = AA && BA ? S::NI / 4 : 1, NEXT = AA && BA ? S::NI / 2 : 1;
     char *lds;
     int wm, wn, now;                     // rows and columns of this wavefront; the stage whose first half is in x0, y0
     Frag x0[S::NI], y0[S::NJ];
@@ -201,22 +205,21 @@ template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANE
         VocabOperand<S, S::N, BA>::read(at + S::OPERAND_A, wn, kk, y);
         VocabOperand<S, S::M, AA>::read(at, wm, kk, x);
     }
-    static __device__ __forceinline__ void sums(const Frag (&x)[S::NI], const Frag (&y)[S::NJ], f32x4 (&acc)[S::NI][S::NJ]) {
+    template <int FROM = 0, int TO = S::NI> static __device__ __forceinline__ void sums(const Frag (&x)[S::NI], const Frag (&y)[S::NJ], f32x4 (&acc)[S::NI][S::NJ]) {
 #pragma unroll
-        for (int i = 0; i < S::NI; ++i)
+        for (int i = FROM; i < TO; ++i)
 #pragma unroll
             for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(x[i], y[j], acc[i][j]);
     }
-    static __device__ __forceinline__ void spread() {
-        if constexpr (MIX) {
-            constexpr int MATRIX = S::NI * S::NJ, READS = (AA ? S::NI : 2 * S::NI) + (BA ? S::NJ : 2 * S::NJ), PER = MATRIX / READS;
+    // reads spread evenly between the matrix instructions
+    template <int FROM = 0> static __device__ __forceinline__ void spread() {
+        constexpr int MATRIX = (S::NI - FROM) * S::NJ, READS = (AA ? S::NI : 2 * S::NI) + (BA ? S::NJ : 2 * S::NJ), PER = MATRIX / READS;
 #pragma unroll
-            for (int i = 0; i < READS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, MATRIX - PER * READS, 0);
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, MATRIX - PER * READS, 0);
         __builtin_amdgcn_sched_barrier(0);
     }
     template <class Fetch> __device__ __forceinline__ void prime(Fetch fetch) {
@@ -235,11 +238,17 @@ template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANE
             spread();
             // the other stage has come, and this one is in everyone's registers
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            fetch(lds + now * S::STAGE);
+            sums<0, FIRST>(x1, y1, acc);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(lds + now * S::STAGE, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            sums<FIRST, NEXT>(x1, y1, acc);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(lds + now * S::STAGE, 2);
             __builtin_amdgcn_sched_barrier(0);
             read(now ^ 1, 0, x0, y0);
-            sums(x1, y1, acc);
-            spread();
+            sums<NEXT>(x1, y1, acc);
+            spread<NEXT>();
             now ^= 1;
         }
     }
@@ -249,7 +258,7 @@ template <class S, bool AA, bool BA, bool MIX, int KIND = S::WIDE ? 0 : S::PLANE
 
 // Of three planes: a stage is one set of fragments, six products of 16 matrix instructions each, smallest first.  The next stage's fragments are read as this one's are
 // used up, so that both fit the registers but for one plane of each factor; a stage's memory is filled again when it is in everyone's registers.
-template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 3> {
+template <class S, bool AA, bool BA> struct VocabPipe<S, AA, BA, 3> {
     struct Set { Frag x[3][S::NI], y[3][S::NJ]; };
     char *lds;
     int wm, wn, now;                     // the stage that is in `f`
@@ -273,9 +282,9 @@ template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 
             A::read(lds + q * S::PLANE_A, wm, 0, f.x[q]);
         }
     }
-    static __device__ __forceinline__ void product(const Set &s, int pa, int pb, f32x4 (&acc)[S::NI][S::NJ]) {
+    template <int FROM = 0, int TO = S::NI> static __device__ __forceinline__ void product(const Set &s, int pa, int pb, f32x4 (&acc)[S::NI][S::NJ]) {
 #pragma unroll
-        for (int i = 0; i < S::NI; ++i)
+        for (int i = FROM; i < TO; ++i)
 #pragma unroll
             for (int j = 0; j < S::NJ; ++j) acc[i][j] = mfma(s.x[pa][i], s.y[pb][j], acc[i][j]);
     }
@@ -285,9 +294,11 @@ template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 
         // the other stage has come, and this one is in everyone's registers
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         const char *a = lds + (now ^ 1) * S::STAGE, *b = a + S::OPERAND_A;
+        product<0, 1>(s, 1, 1, acc);
+        __builtin_amdgcn_sched_barrier(0);
         fetch(lds + now * S::STAGE);
         B::read(b + 2 * S::PLANE_B, wn, 0, to.y[2]);
-        product(s, 1, 1, acc);
+        product<1>(s, 1, 1, acc);
         __builtin_amdgcn_sched_barrier(0);
         A::read(a, wm, 0, to.x[0]);
         product(s, 2, 0, acc);
@@ -316,7 +327,7 @@ template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 
 
 // Of a float32 factor as it lies and three planes of the other: a wavefront splits what it has read of a stage, while the next two are on their way.  For few rows: every
 // element of the first factor is split once, and its bytes are what a product costs.
-template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 0> {
+template <class S, bool AA, bool BA> struct VocabPipe<S, AA, BA, 0> {
     char *lds;
     int wm, wn, now;
     using A = VocabOperand<S, S::M, AA, true>;
@@ -366,13 +377,13 @@ template <class S, bool AA, bool BA, bool MIX> struct VocabPipe<S, AA, BA, MIX, 
 };
 
 // One tile's product.
-template <class S, bool AA, bool BA, bool MIX> __device__ __forceinline__ void vocab_product(const VocabFactor &fa, const VocabFactor &fb, VocabTile t, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
+template <class S, bool AA, bool BA> __device__ __forceinline__ void vocab_product(const VocabFactor &fa, const VocabFactor &fb, VocabTile t, int64_t m_end, int64_t n_end, int64_t k, int64_t k_end, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
     VocabFeed<S, AA, BA> feed(fa, fb, m_end, n_end, k, k_end);
     if (feed.stages <= 0) return;
     feed.t = t;
     feed.start();
-    VocabPipe<S, AA, BA, MIX> pipe(lds);
-    auto fetch = [&](char *to) __attribute__((always_inline)) { feed.fetch(to, [] { return false; }); };
+    VocabPipe<S, AA, BA> pipe(lds);
+    auto fetch = [&](char *to, int halves = 3) __attribute__((always_inline)) { feed.fetch(to, halves, [] { return false; }); };
     pipe.prime(fetch);
     pipe.run(feed.stages, acc, fetch);
     pipe.end();
@@ -518,14 +529,14 @@ template <class S, bool BWD> __global__ __launch_bounds__(S::THREADS) void k_voc
     VocabFeed<S, true, true> feed(p.w, p.h, p.V, T, 0, p.K);
     feed.t = tiles.tile(first + at);
     feed.start();
-    VocabPipe<S, true, true, true> pipe(lds);
+    VocabPipe<S, true, true> pipe(lds);
     auto next = [&]() __attribute__((always_inline)) {
         coming += turn;
         if (coming >= count) return false;
         feed.t = tiles.tile(first + coming);
         return true;
     };
-    auto fetch = [&](char *to) __attribute__((always_inline)) { feed.fetch(to, next); };
+    auto fetch = [&](char *to, int halves = 3) __attribute__((always_inline)) { feed.fetch(to, halves, next); };
     pipe.prime(fetch);
     for (; at < count; at += turn) {
         f32x4 acc[S::NI][S::NJ] = {};
@@ -566,7 +577,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_part(co
     const VocabUnit<S> u(p.V, T, p.splits_z, p.K);
     if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, true, true, true>(p.w, p.h, u.t, p.V, T, u.k, u.end, lds, acc);
+    vocab_product<S, true, true>(p.w, p.h, u.t, p.V, T, u.k, u.end, lds, acc);
     const VocabPlace<S> place;
     const int64_t v0 = u.t.m + place.m, n0 = u.t.n + place.n;
 #pragma unroll
@@ -656,7 +667,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     const VocabUnit<S> u(p.K, T, p.count[1], p.V);
     if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, false, true, true>(p.w, p.dz, u.t, p.K, T, u.k, u.end, lds, acc);
+    vocab_product<S, false, true>(p.w, p.dz, u.t, p.K, T, u.k, u.end, lds, acc);
     const VocabPlace<S> place;
     const int64_t c0 = u.t.m + place.m, n0 = u.t.n + place.n;
 #pragma unroll
@@ -772,7 +783,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dw(cons
     const VocabUnit<S> u(p.K, p.V, p.splits_w, T);
     if (!u.there) return;
     f32x4 acc[S::NI][S::NJ] = {};
-    vocab_product<S, false, false, true>(p.h, p.dz, u.t, p.K, p.V, u.k, u.end, lds, acc);
+    vocab_product<S, false, false>(p.h, p.dz, u.t, p.K, p.V, u.k, u.end, lds, acc);
     if constexpr (S::PLANES == 1) vocab_rests<S>(p, u, lds, acc);
     const VocabPlace<S> place;
     const int64_t c0 = u.t.m + place.m, n0 = u.t.n + place.n;
