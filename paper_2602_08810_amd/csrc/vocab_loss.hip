@@ -490,7 +490,9 @@ __device__ __forceinline__ float vocab_rest(float d) {
 }
 template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(const VocabParams &p, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential, float scale,
                                                                                f32x4 (&acc)[S::NI][S::NJ], int j) {
-    uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0;
+    const int g = threadIdx.x >> 4 & 3;
+    uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0 - 4 * g;
+    uint2 part[S::PLANES][S::NI];
 #pragma unroll
     for (int i = 0; i < S::NI; ++i) {
         float d[4];
@@ -502,7 +504,24 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
             if (APART && 16 * i + r >= left) d[r] = 0.0f;
             if (APART && S::PLANES == 1 && hit == 16 * i + r && 16 * i + r < left) p.row_rest[row] = vocab_rest(d[r]);
         }
-        store_dz<S::PLANES>(to + 16 * i, p.dz.plane, d);
+        uint32_t a[S::PLANES], b[S::PLANES];
+        split2<S::PLANES>(d[0], d[1], a);
+        split2<S::PLANES>(d[2], d[3], b);
+#pragma unroll
+        for (int q = 0; q < S::PLANES; ++q) part[q][i] = make_uint2(a[q], b[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < S::PLANES; ++q) {
+        if constexpr (S::NI % 2 == 0) {
+            // of two times 16 words a lane has four each; eight of one of them, for one access, by an exchange with the lane 16 further on or back
+#pragma unroll
+            for (int i = 0; i < S::NI; i += 2) {
+                const auto x = __builtin_amdgcn_permlane16_swap(part[q][i].x, part[q][i + 1].x, false, false), y = __builtin_amdgcn_permlane16_swap(part[q][i].y, part[q][i + 1].y, false, false);
+                *reinterpret_cast<uint4 *>(to + q * p.dz.plane + 16 * (i + (g & 1)) + 8 * (g >> 1)) = make_uint4(x[0], y[0], x[1], y[1]);
+            }
+        } else
+#pragma unroll
+            for (int i = 0; i < S::NI; ++i) *reinterpret_cast<uint2 *>(to + q * p.dz.plane + 16 * i + 4 * g) = part[q][i];
     }
 }
 template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p, VocabTile t, int64_t T, f32x4 (&acc)[S::NI][S::NJ]) {
