@@ -6,8 +6,8 @@
 // rounding).  Rows without a target are left out before the products: they cost nothing and
 // nothing in them, finite or not, reaches a gradient.
 // Float32 inputs: every factor is the sum of three bfloat16 numbers, a product six of theirs (terms of 2^-24 and below are left out), summed in float32.
-// Bound by the matrix units; with few rows, by the bytes of w.  8192 rows, 32768 words, 2048 elements in bfloat16: z 931 us (1180 TFLOP/s), dz 982, dh 902, dw 1100 with half of the
-// rows' targets in one tile of words, else 930; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
+// Bound by the matrix units; with few rows, by the bytes of w.  8192 rows, 32768 words, 2048 elements in bfloat16: z 825 us (1330 TFLOP/s), dz 873, dh 815, dw 970 with half of the
+// rows' targets in one tile of words, else 830; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
 #include "vocab_loss.hpp"
 #include "conv_common.hpp"
 
@@ -16,10 +16,10 @@ namespace lrnnx {
 // The tile of a product and its wavefronts: M x N, WM wavefronts along m, each 16 NI x 64 of it; STEP terms a stage, STAGES of them in LDS.
 // Large: 256 x 256, eight wavefronts of 128 x 64 (128 KB of LDS). Small: 128 x 128, four of 64 x 64, two workgroups a compute unit.
 // Of three planes: 256 x 128, eight of 64 x 64; all planes of a stage lie in LDS together (72 KB), so that each is loaded and read once for its six products
-// (z of 997 x 5003, 771 terms: 73 us; as six sums of a product each, tiles of 128 x 128: 100; tiles of 128 x 128, four wavefronts with all planes, three stages: 85);
+// (z of 997 x 5003, 771 terms: 62 us; before loads that nothing waits for 73, as six sums of a product each, tiles of 128 x 128, then 100; tiles of 128 x 128, four wavefronts with all planes, three stages, 85);
 // the small one 128 x 64, four of 32 x 64, two a compute unit.
-// WIDE, the first factor in float32 and split as it is read: 128 x 64, four of 32 x 64, and 64 x 64, four of 16 x 64, two a compute unit (20 rows, 151790 words, 768 terms: z 160 us,
-// dh 95: 2.9 and 4.9 TB/s; all in tiles of 64 x 64: 186 and 128; four stages of LDS, one workgroup a compute unit: 190 and 145).
+// WIDE, the first factor in float32 and split as it is read: 128 x 64, four of 32 x 64, and 64 x 64, four of 16 x 64, two a compute unit (20 rows, 151790 words, 768 terms: z 150 us,
+// dh 91: 3.1 and 5.1 TB/s; all in tiles of 64 x 64, before loads that nothing waits for, 186 and 128 where this did 160 and 95; four stages of LDS, one workgroup a compute unit: 190 and 145).
 template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct VocabSize {
     static constexpr bool WIDE = WIDE_;
     static constexpr int M = M_, N = N_, WM = WM_, PLANES = PLANES_, STEP = PLANES == 1 ? 64 : 32;
@@ -707,7 +707,7 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     }
 }
 
-// dw: what is left of the targets' elements (20 us of 930 to look through the rows, 2.3 a stage).  The rows of a stretch whose target is a word of the tile, 64 at a time, are terms of one more stage: their rows of h and, in their word's
+// dw: what is left of the targets' elements (20 us of 830 to look through the rows, 2.1 a stage).  The rows of a stretch whose target is a word of the tile, 64 at a time, are terms of one more stage: their rows of h and, in their word's
 // column, the rest.
 template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams &p, const VocabUnit<S> &u, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
     using A = VocabOperand<S, S::M, false>;
