@@ -161,6 +161,9 @@ VocabShape shape_of(int planes, bool wide, int64_t m, int64_t n, int64_t terms, 
     return best;
 }
 
+// Blocks of words over which the elements of dz are added where they are made: a wavefront's part of a tile, or a thread's eight of z's parts.
+int64_t sum_blocks(const VocabParams &p, int64_t words) { return p.splits_z > 1 ? (words + 7) / 8 : up(words, p.side_z) / p.side_z * 2; }
+
 template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     VocabPlan f{};
     const int io = a->io_dtype == LRNNX_BF16, planes = io ? 1 : 3;
@@ -206,7 +209,14 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_lse = l.take<float>(a->T);
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
-        if (io) p.row_rest = l.take<float>(a->T);
+        if (io) {
+            p.rests = l.take<VocabRest>(a->T * kVocabRests);
+            f.rows.row_others = p.row_others = l.take<int>(a->T);
+            p.row_key = l.take<int>(a->T);
+            p.row_sum = l.take<float>(a->T);
+            p.row_left = l.take<float>(a->T);
+            p.sum_part = l.take<float>(a->T * sum_blocks(p, each));
+        }
         if (p.splits_w > 1) p.dw_part = l.take<float>(p.splits_w * each * Kp);
         p.dh_part = l.take<float>(p.splits * a->T * Kp);
         p.count = f.rows.count; p.row_lse = f.rows.row_lse; p.row_scale = f.rows.row_scale; p.row_target = f.rows.row_target;
@@ -225,6 +235,9 @@ int vocab_piece(VocabPlan &f, const void *weight, int64_t stride, int64_t v0, hi
     p.v0 = v0;
     p.V = p.words - v0 < f.each ? p.words - v0 : f.each;
     p.first = v0 == 0;
+    p.sum_blocks = (int)sum_blocks(p, p.V);
+    p.sum_row = p.splits_z > 1 ? p.sum_blocks : 1;
+    p.sum_block = p.splits_z > 1 ? 1 : p.T;
     const char *from = reinterpret_cast<const char *>(weight) + v0 * stride * (p.io ? 2 : 4);
     if (!f.w.src) { p.w.p = reinterpret_cast<const uint16_t *>(from); return LRNNX_OK; }
     f.w.src = from; f.w.rows = p.V;
@@ -276,15 +289,16 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
     for (int64_t v0 = 0; v0 < a->V; v0 += f.each) {
         if (const int e = vocab_piece(f, a->weight, a->weight_stride, v0, s)) return e;
         if (launch_vocab_logits(f.p, true, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
+        if (f.p.io && launch_vocab_rests(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (a->dh && launch_vocab_dh(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (!a->dweight) continue;
         if (launch_vocab_dw(f.p, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
         if (f.p.splits_w == 1) continue;
-        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, nullptr, nullptr, nullptr, nullptr, 0, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
+        const VocabAdd parts{f.p.V, f.p.V * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits_w, f.p.dw_part, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, reinterpret_cast<char *>(a->dweight) + v0 * a->K * (int64_t)es};
         if (launch_vocab_add(parts, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     }
     if (!a->dh) return LRNNX_OK;
-    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, f.rows.count, f.p.row_rest, f.p.row_target, a->weight, a->weight_stride, a->dh};
+    const VocabAdd end{a->T, a->T * f.p.Kp, a->K, (int)f.p.Kp, f.p.io, f.p.splits, f.p.dh_part, f.rows.place, f.rows.count, f.p.row_key, f.p.row_left, f.p.rests, a->weight, a->weight_stride, a->dh};
     return status(launch_vocab_add(end, s));
 }
 

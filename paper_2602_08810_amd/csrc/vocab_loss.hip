@@ -1,10 +1,11 @@
 // Softmax cross entropy over a vocabulary without its logits: z = h w^T, lse = log sum exp z, loss = lse - z[target], and
 //     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz w,   dw = dz^T h.
 // Forward: a tile of z stays in registers from its product to its largest number and sum, which is all that leaves it (8 bytes for 256 words and a row); a second
-// launch joins them.  Backward: z is formed again, a piece of the vocabulary at a time, dz of the piece goes to the workspace in bfloat16 and from there into both products; what
-// that rounding leaves of the target's element, which is most of a row's dz as a rule, is added to both (without it the gradients' error in bfloat16 was 1.5 times that of their own
-// rounding).  Rows without a target are left out before the products: they cost nothing and
-// nothing in them, finite or not, reaches a gradient.
+// launch joins them.  Backward: z is formed again, a piece of the vocabulary at a time, dz of the piece goes to the workspace in bfloat16 and from there into both products.  What
+// that rounding takes from the target's element, and from another word's whose p is over 1/8 (eight of a row at most), is kept in float32 and added to both, and to dh as much of the target's
+// word as is missing to the row's sum, which is 0: the gradients are then as exact as their own rounding to bfloat16, 1.66e-3 (all elements rounded: 2.4e-3; all but the target's, of rows that
+// give another word 0.95, 2.0e-3, and 3.8e-3 or 1.1e-2 where all words have a component in common of 3 or 10 times their own norm, which has to cancel in dh).  Rows without a target are left
+// out before the gradients' products: they cost nothing there and nothing in them, finite or not, reaches a gradient.
 // Float32 inputs: every factor is the sum of three bfloat16 numbers, a product six of theirs (terms of 2^-24 and below are left out), summed in float32.
 // Bound by the matrix units; with few rows, by the bytes of w.  8192 rows, 32768 words, 2048 elements in bfloat16: z 825 us (1330 TFLOP/s), dz 873, dh 815, dw 970 with half of the
 // rows' targets in one tile of words, else 830; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
@@ -495,8 +496,36 @@ __device__ __forceinline__ float vocab_rest(float d) {
     const float there = __uint_as_float(pack_rne(d, 0.0f) << 16);
     return fabsf(there) < INFINITY ? d - there : 0.0f;
 }
-template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(const VocabParams &p, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential, float scale,
-                                                                               f32x4 (&acc)[S::NI][S::NJ], int j) {
+// The rest of a word that is likely without being the target.  Several wavefronts add to a row's, in any order: they are sorted before they are used.
+__device__ __forceinline__ void vocab_other(const VocabParams &p, int64_t row, int64_t word, float d) {
+    const int at = atomicAdd(p.row_others + row, 1) + 1;
+    if (at < kVocabRests) p.rests[row * kVocabRests + at] = {(int)word, vocab_rest(d)};
+}
+// The rests that a column of a tile has: its lanes' target's and those of likely words.
+template <class S> __device__ __forceinline__ void vocab_column_rests(const VocabParams &p, int64_t row, int64_t v0, int64_t left, int64_t hit, VocabExp<S::PLANES> exponential, float scale,
+                                                                      const f32x4 (&acc)[S::NI][S::NJ], int j) {
+    asm volatile("" : "+v"(exponential.base));             // (formed again: the fast path's results are not to be kept for it)
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (16 * i + r < left && (hit == 16 * i + r || exponential(acc[i][j][r]) > kVocabLikely)) found |= 1u << (4 * i + r);
+    for (; found; found &= found - 1) {
+        const int at = __builtin_ctz(found), word = (at >> 2) * 16 + (at & 3);
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::NI; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z = at == 4 * i + r ? acc[i][j][r] : z;
+        const float x = exponential(z);
+        if (word == hit) p.rests[row * kVocabRests].rest = vocab_rest((x - 1.0f) * scale);
+        else vocab_other(p, row, p.v0 + v0 + word, x * scale);
+    }
+}
+template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(const VocabParams &p, bool there, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential,
+                                                                               float scale, f32x4 (&acc)[S::NI][S::NJ], int j) {
+#pragma clang fp contract(off)           // (a product fused into its own split would differ between the two forms, and so with the targets of other rows)
     const int g = threadIdx.x >> 4 & 3;
     uint16_t *to = const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0 - 4 * g;
     uint2 part[S::PLANES][S::NI];
@@ -509,7 +538,6 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
             if (APART && hit == 16 * i + r) d[r] -= 1.0f;
             d[r] *= scale;
             if (APART && 16 * i + r >= left) d[r] = 0.0f;
-            if (APART && S::PLANES == 1 && hit == 16 * i + r && 16 * i + r < left) p.row_rest[row] = vocab_rest(d[r]);
         }
         uint32_t a[S::PLANES], b[S::PLANES];
         split2<S::PLANES>(d[0], d[1], a);
@@ -517,6 +545,23 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
 #pragma unroll
         for (int q = 0; q < S::PLANES; ++q) part[q][i] = make_uint2(a[q], b[q]);
     }
+    if constexpr (S::PLANES == 1) {
+        // the sum over this wavefront's words of what is stored, as a product with ones: (which terms a lane holds is the same to a sum)
+        Frag ones;
+        ones.v = make_uint4(0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80);
+        f32x4 sum = {};
+#pragma unroll
+        for (int i = 0; i < S::NI; i += 2) {
+            Frag f;
+            f.h[0] = part[0][i];
+            f.h[1] = part[0][i + 1];
+            sum = mfma(ones, f, sum);
+        }
+        if (there && g == 0) p.sum_part[row * p.sum_row + (v0 >> (S::M / S::WM == 128 ? 7 : 6)) * p.sum_block] = sum[0];
+        // (without a likely word they add up to less, rounded as they are)
+        if (there && (APART || fabsf(sum[0]) > 0.96f * kVocabLikely * fabsf(scale))) vocab_column_rests<S>(p, row, v0, left, APART ? hit : -1, exponential, scale, acc, j);
+    }
+    if (!there) return;
 #pragma unroll
     for (int q = 0; q < S::PLANES; ++q) {
         if constexpr (S::NI % 2 == 0) {
@@ -542,9 +587,8 @@ template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p
         const int64_t hit = (there ? (int64_t)p.row_target[row] : -1) - p.v0 - v0;
         const bool apart = t.m + S::M > p.V || __any(hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4);
         const VocabExp<S::PLANES> exponential(lse);
-        if (!there) continue;
-        if (apart) vocab_dz_column<S, true>(p, row, v0, left, hit, exponential, scale, acc, j);
-        else vocab_dz_column<S, false>(p, row, v0, left, hit, exponential, scale, acc, j);
+        if (apart) vocab_dz_column<S, true>(p, there, row, v0, left, hit, exponential, scale, acc, j);
+        else vocab_dz_column<S, false>(p, there, row, v0, left, hit, exponential, scale, acc, j);
     }
 }
 // A workgroup stays and takes a tile after the other; the next one's factors are on their way while it works on what comes of the one before.
@@ -675,18 +719,25 @@ template <int PLANES> __global__ __launch_bounds__(256) void k_vocab_part_dz(con
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < T * pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / pieces, v0 = (i - row * pieces) * 8, hit = (int64_t)p.row_target[row] - p.v0 - v0;
         const float lse = p.row_lse[row], scale = p.row_scale[row];
+        float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const f32x4 z = vocab_z(p, row, v0 + 4 * h);
             float d[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                d[r] = vocab_exp<PLANES>(z[r] - lse) - (hit == 4 * h + r ? 1.0f : 0.0f);
-                d[r] = v0 + 4 * h + r < p.V ? d[r] * scale : 0.0f;
-                if (PLANES == 1 && hit == 4 * h + r && v0 + 4 * h + r < p.V) p.row_rest[row] = vocab_rest(d[r]);
+                const bool target = hit == 4 * h + r, word = v0 + 4 * h + r < p.V;
+                const float x = vocab_exp<PLANES>(z[r] - lse);
+                d[r] = word ? (x - (target ? 1.0f : 0.0f)) * scale : 0.0f;
+                if constexpr (PLANES == 1) {
+                    sum += __uint_as_float(pack_rne(d[r], 0.0f) << 16);
+                    if (word && target) p.rests[row * kVocabRests].rest = vocab_rest(d[r]);
+                    else if (word && x > kVocabLikely) vocab_other(p, row, p.v0 + v0 + 4 * h + r, d[r]);
+                }
             }
             store_dz<PLANES>(const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0 + 4 * h, p.dz.plane, d);
         }
+        if (PLANES == 1) p.sum_part[row * p.sum_row + (v0 >> 3) * p.sum_block] = sum;
     }
 }
 
@@ -714,8 +765,43 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     }
 }
 
-// dw: what is left of the targets' elements (20 us of 830 to look through the rows, 2.1 a stage).  The rows of a stretch whose target is a word of the tile, 64 at a time, are terms of one more stage: their rows of h and, in their word's
-// column, the rest.
+// A row's other rests by word, its target and their number in one, and what is missing to its sum: 64 rows a workgroup, their blocks' sums in 16 stretches.
+__global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, stretch = threadIdx.x >> 6;
+    const int64_t row = (int64_t)blockIdx.x * 64 + lane;
+    const bool there = row < *p.count;
+    float s = 0.0f;
+    if (there)
+#pragma unroll 8
+        for (int i = stretch; i < p.sum_blocks; i += 16) s += p.sum_part[row * p.sum_row + i * p.sum_block];
+    lds[stretch][lane] = s;
+    __syncthreads();
+    if (stretch || !there) return;
+    s = p.first ? 0.0f : p.row_sum[row];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += lds[i][lane];
+    p.row_sum[row] = s;
+    int n = p.row_others[row];
+    if (n >= kVocabRests) n = 0;                           // (no probabilities: lse is not the row's)
+    VocabRest *const rest = p.rests + row * kVocabRests;
+    for (int i = 2; i <= n; ++i) {
+        const VocabRest x = rest[i];
+        int at = i;
+        for (; at > 1 && rest[at - 1].word > x.word; --at) rest[at] = rest[at - 1];
+        rest[at] = x;
+    }
+    for (int i = 1; i <= n; ++i) s += rest[i].rest;
+    p.row_left[row] = fabsf(s) < INFINITY ? -s : 0.0f;
+    p.row_key[row] = p.row_target[row] < 0 ? -1 : p.row_target[row] | n << kVocabWordBits;
+}
+hipError_t launch_vocab_rests(const VocabParams &p, hipStream_t s) {
+    hipLaunchKernelGGL(k_vocab_rests, dim3((unsigned)((p.T + 63) / 64)), dim3(1024), 0, s, p);
+    return hipGetLastError();
+}
+
+// dw: what rounding took from dz.  The rows of a stretch that have a rest of a word of the tile, 64 at a time, are terms of one more stage: their rows of h and, in their word's
+// column, the rest.  First those of the rows' targets, then those of other words that are likely, one of each row at a time.
 template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams &p, const VocabUnit<S> &u, char *lds, f32x4 (&acc)[S::NI][S::NJ]) {
     using A = VocabOperand<S, S::M, false>;
     using B = VocabOperand<S, S::N, false>;
@@ -729,7 +815,7 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
     uint4 h[A::LOADS];                                     // of the next 64 rows
     float rest = 0.0f;
     auto fetch = [&](int from, int n) {
-        if (tid < n && tid < 64) rest = p.row_rest[rows[from + tid]];
+        if (tid < n && tid < 64) rest = p.rests[(int64_t)rows[from + tid] * kVocabRests + (words[from + tid] >> 8)].rest;
 #pragma unroll
         for (int j = 0; j < A::LOADS; ++j) {
             constexpr int ROW = S::M / 8;
@@ -739,41 +825,58 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
             if (row < n && col < p.Kp) h[j] = *reinterpret_cast<const uint4 *>(p.h.p + rows[from + row] * p.h.ld + col);
         }
     };
-    int held = 0;                                          // rows in the queue
-    for (int64_t t0 = u.k; t0 < u.end; t0 += R * S::THREADS) {
+    int held = 0;                                          // rests in the queue
+    int which = 0, most = 0;                               // which of the rows' rests, and the last that one of these rows has
+    int key[R];
+    for (int64_t t0 = u.k; t0 < u.end;) {
         int word[R];
         uint64_t have[R];
-        int mine = 0;
+        int mine = 0, others = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int64_t t = t0 + r * S::THREADS + tid;
-            word[r] = (t < u.end ? p.row_target[t] : -1) - first;
+            if (which == 0) key[r] = t < u.end ? p.row_key[t] : -1;
+            word[r] = -1;
+            if (which == 0 && key[r] >= 0) word[r] = (key[r] & ((1 << kVocabWordBits) - 1)) - first;
+            if (which > 0 && key[r] >> kVocabWordBits >= which) word[r] = p.rests[t * kVocabRests + which].word - first;
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) { have[r] = __ballot((unsigned)word[r] < (unsigned)some); mine += __popcll(have[r]); }
-        if (lane == 0) found[wave] = mine;
+        for (int r = 0; r < R; ++r) {
+            have[r] = __ballot((unsigned)word[r] < (unsigned)some);
+            mine += __popcll(have[r]);
+            const int n = key[r] >> kVocabWordBits;
+            for (int i = which; i < kVocabRests - 1 && __any(n > i); ++i) others = others > i + 1 ? others : i + 1;
+        }
+        if (lane == 0) found[wave] = mine | others << 16;
         __syncthreads();
         int at = held;
-        for (int w = 0; w < WAVES; ++w) { const int f = __builtin_amdgcn_readfirstlane(found[w]); if (w < wave) at += f; held += f; }
+        most = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            const int f = __builtin_amdgcn_readfirstlane(found[w]), here = f & 0xffff;
+            if (w < wave) at += here;
+            held += here;
+            most = most > f >> 16 ? most : f >> 16;
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (have[r] >> lane & 1) {
                 const int to = at + __popcll(have[r] & ((1ull << lane) - 1));
                 rows[to] = (int)(t0 + r * S::THREADS + tid);
-                words[to] = word[r];
+                words[to] = word[r] | which << 8;
             }
             at += __popcll(have[r]);
         }
         __syncthreads();
         int from = 0;
-        const int least = t0 + R * S::THREADS < u.end ? 64 : 1;
+        const bool last = which >= most && t0 + R * S::THREADS >= u.end;
+        const int least = last ? 1 : 64;
         if (held >= least) fetch(0, held);
 #pragma unroll 1
         for (; held - from >= least; from += 64) {
             const int n = held - from < 64 ? held - from : 64;
             uint16_t *at = nullptr;                        // of the rest in its word's column
             if (tid < n) {
-                const int word = words[from + tid];
+                const int word = words[from + tid] & 0xff;
                 at = reinterpret_cast<uint16_t *>(lb + tid * (S::N * 2) + (((word >> 4) ^ B::mixed(tid)) << 5) + (word & 15) * 2);
                 *at = (uint16_t)pack_rne(rest, 0.0f);
             }
@@ -794,7 +897,7 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
             __syncthreads();
             if (at) *at = 0;
         }
-        if (least == 1) break;
+        if (last) break;
         if (from) {                                        // what is left moves to the front
             const bool moves = tid < held - from;
             const int row = moves ? rows[from + tid] : 0, w = moves ? words[from + tid] : 0;
@@ -803,6 +906,8 @@ template <class S> __device__ __forceinline__ void vocab_rests(const VocabParams
             __syncthreads();
             held -= from;
         }
+        if (which < most) ++which;
+        else { which = 0; t0 += R * S::THREADS; }
     }
 }
 
@@ -976,6 +1081,7 @@ __global__ __launch_bounds__(1024) void k_vocab_rows(const VocabRows p) {
                 p.row_lse[to] = lse[r];
                 p.row_scale[to] = target[r] < p.V ? scale[r] : __builtin_nanf("");
                 p.row_target[to] = target[r] < p.V ? (int)target[r] : -1;
+                if (p.row_others) p.row_others[to] = 0;
             }
             at += __popcll(have[r]);
         }
@@ -1035,7 +1141,7 @@ hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s) {
 }
 
 // Rows of a result from the parts of its sum, four columns a thread; PARTS threads take a stretch of the parts each where there are many.  `place`: where a row's lie, -1:
-// nowhere, and the row is zero.  `rest`: so much of a row of w is added.
+// nowhere, and the row is zero.  `key`: to a row of dh what is missing to its sum is added as so much of the target's row of w, and the rests of other words as so much of theirs.
 template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_add(const VocabAdd p) {
     constexpr int ITEMS = 256 / PARTS;
     __shared__ f32x4 lds[PARTS > 1 ? 256 : 1];
@@ -1061,11 +1167,15 @@ template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_ad
             __syncthreads();
         }
         if (q0 == 0 && i < n) {
-            if (p.rest && at >= 0 && p.target[at] >= 0) {
-                const IO *w = reinterpret_cast<const IO *>(p.w) + p.target[at] * p.w_ld + c;
-                const float rest = p.rest[at];
+            const int key = p.key && at >= 0 ? p.key[at] : -1;
+            if (key >= 0) {
+                auto more = [&](int64_t word, float rest) {
+                    const IO *w = reinterpret_cast<const IO *>(p.w) + word * p.w_ld + c;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) if (c + e < p.K) s[e] = __builtin_fmaf(rest, load_io(w + e), s[e]);
+                    for (int e = 0; e < 4; ++e) if (c + e < p.K) s[e] = __builtin_fmaf(rest, load_io(w + e), s[e]);
+                };
+                more(key & ((1 << kVocabWordBits) - 1), p.left[at]);
+                for (int q = 1; q <= key >> kVocabWordBits; ++q) more(p.rests[at * kVocabRests + q].word, p.rests[at * kVocabRests + q].rest);
             }
             const float x[4] = {s[0], s[1], s[2], s[3]};
             store_part(reinterpret_cast<IO *>(p.out) + row * p.K + c, x, p.K - c);

@@ -6,6 +6,12 @@
 namespace lrnnx {
 
 constexpr int kVocabTile = 256;          // rows and columns of a product's largest tile
+// With bfloat16 inputs, what rounding takes from a row's elements of dz: the target's, and those of other words whose p is over kVocabLikely (fewer than kVocabRests).
+constexpr int kVocabRests = 9;
+constexpr float kVocabLikely = 0.125f;
+struct VocabRest { int word; float rest; };
+// A row's target and the number of its other rests in one number; -1: a target beyond the vocabulary
+constexpr int kVocabWordBits = 27;
 
 // A factor of a matrix product in bfloat16, `planes` numbers to an element (a float32 element is the sum of three): element (plane, row, column) at
 // plane * plane_stride + row * ld + column.  16-byte aligned rows of whole 16-byte pieces.
@@ -33,7 +39,13 @@ struct VocabParams {
     // backward, by row among those that have a target
     const float *row_lse, *row_scale;
     const int *row_target;               // -1: beyond the vocabulary
-    float *row_rest;                     // what dz of the target lost by its rounding to bfloat16
+    VocabRest *rests;                    // [T,kVocabRests], the target's first, the others' by word; bfloat16 only, as the next four
+    int *row_others;                     // how many others have been found
+    int *row_key;
+    float *sum_part;                     // sums of the stored dz over blocks of words: (row, block) at row * sum_row + block * sum_block
+    int64_t sum_row, sum_block;
+    int sum_blocks;
+    float *row_sum, *row_left;           // of the row's stored dz, all pieces so far; what is missing to the row's sum, which is 0, rests of other words apart
     float *dh_part;                      // [stretches, rows that have a target, Kp], within [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
     float *dw_part;                      // [splits_w,V,Kp], if there are several
@@ -41,6 +53,7 @@ struct VocabParams {
     void *dw;                            // [words,K]
 };
 hipError_t launch_vocab_logits(const VocabParams &p, bool backward, hipStream_t s);
+hipError_t launch_vocab_rests(const VocabParams &p, hipStream_t s);
 hipError_t launch_vocab_dh(const VocabParams &p, hipStream_t s);
 hipError_t launch_vocab_dw(const VocabParams &p, hipStream_t s);
 
@@ -66,6 +79,7 @@ struct VocabRows {
     int *index, *place, *count;          // row of the T that the i-th with a target is; place: the other way, -1: none
     float *row_lse, *row_scale;
     int *row_target;
+    int *row_others;                     // set to 0, or null
     // for dh: tiles along K, rows of a tile, workgroups at once and in the launch; words of a piece; stretches that there is room for with all rows
     int across, side, at_once;
     int64_t units, each, splits;
@@ -86,8 +100,9 @@ struct VocabAdd {
     const float *part;
     const int *place;                    // or null
     const int *count;                    // or null; device: rows of a part, parts
-    const float *rest;                   // by row of the parts, or null; with the row of w that it belongs to (-1: none)
-    const int *target;
+    const int *key;                      // by row of the parts, or null: as in VocabParams, with what is to be added
+    const float *left;
+    const VocabRest *rests;
     const void *w; int64_t w_ld;
     void *out;                           // [rows,K]
 };
