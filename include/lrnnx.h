@@ -683,7 +683,8 @@ size_t lrnnx_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
  * Two layouts: time_last = 0, x and y [B,L,D] with the channels contiguous (as the gated delta rule takes them; strides of batch entry and
  * step), or 1, [B,D,L] with the time axis contiguous (as the selective scan does; strides of batch entry and channel).  x, x0, x_last and y in
  * io_dtype, weight [D,W] and bias [D] (optional) float; x0, x_last contiguous, optional.  2 <= W <= 4; 1 <= D <= 65536; B <= 65535; any L >= 1.
- * Accesses are made at element alignment.  y must not overlap an input.
+ * Accesses are made at element alignment.  y and x_last must overlap neither an input nor each other (LRNNX_ERR_INVALID_ARG; views of one wider
+ * tensor whose rows lie side by side do not).
  * Packed variable-length batches: with cu_seqlens != NULL (device memory [B+1], ascending) x and y are one axis of L steps (batch strides
  * ignored) and sequence b is its steps cu_seqlens[b] .. cu_seqlens[b+1]-1; x0 and x_last stay [B,W-1,D].  Boundaries are clamped to [0,L];
  * steps outside every sequence are neither read as part of one nor written.  A sequence without steps has x0 (or zeros) for its x_last.
@@ -707,7 +708,7 @@ int lrnnx_short_conv_fwd(const lrnnx_conv_fwd_args *args);
 
 /* Its reverse-mode derivative for upstream gradients dy (of y, strided as x is) and, optionally, dx_last (of x_last, contiguous): dx strided as y was,
  * dweight [D,W] and dbias [D] (optional) float, dx0 [B,W-1,D] in io_dtype (optional; also of a call without x0).  Inputs as in the
- * forward call, from which pre is formed again.  dx of steps outside every sequence of a packed batch is zero.  The weights' gradients
+ * forward call, from which pre is formed again.  Results must overlap neither inputs nor each other.  dx of steps outside every sequence of a packed batch is zero.  The weights' gradients
  * are summed in a fixed order through the workspace: lrnnx_short_conv_bwd_workspace_bytes(args) bytes, 16-byte aligned.   */
 typedef struct lrnnx_conv_bwd_args {
     size_t struct_size;
@@ -733,7 +734,7 @@ int lrnnx_short_conv_bwd(const lrnnx_conv_bwd_args *args);
 size_t lrnnx_short_conv_bwd_workspace_bytes(const lrnnx_conv_bwd_args *args);
 
 /* One step of it (generation): state [B,W-1,D] in io_dtype, contiguous, the last W - 1 inputs, moved on by x IN PLACE; x, y [B,D] with any strides
- * (y may be x).  L calls give what the forward call gives on L steps.                                                   */
+ * (y may be x; else results overlap neither inputs nor each other).  L calls give what the forward call gives on L steps.                                                   */
 typedef struct lrnnx_conv_step_args {
     size_t struct_size;
     int32_t B, D, W;

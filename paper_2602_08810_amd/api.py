@@ -1316,7 +1316,7 @@ def _conv_rows(t, name, shape, io, out=False):
 
 
 def _not_in_place(t, name, *inputs):
-    """Steps of an input are read again where a neighbour's result may be written by then."""
+    """Steps of an input are read again where a neighbour's result may be written by then.  (The library refuses whatever else shares an element.)"""
     if t is not None and any(t.data_ptr() == x.data_ptr() for x in inputs):
         raise ValueError(f"{name}: must not be an input")
 
@@ -1359,7 +1359,8 @@ def lrnnx_short_conv_fwd(x, weight, bias=None, act="silu", x0=None, cu_seqlens=N
     x [B,L,D] (layout "bld", channels contiguous) or [B,D,L] ("bdl", time axis contiguous) float32 or bfloat16, views of wider tensors
     among them; weight [D,W] (W = 2 .. 4) and bias [D] float32; act "silu" or "none"; x0 [B,W-1,D] in x's type, the inputs before
     the first.  With `cu_seqlens` (int64 [S+1] on the device) the batch is packed: x and y without the batch axis, x0 and the last inputs
-    [S,W-1,D]; steps of y outside every sequence are not written (a new y holds anything there).  y must not overlap an input."""
+    [S,W-1,D]; steps of y outside every sequence are not written (a new y holds anything there).  An `out` that shares an element with an input is
+    refused; other channels of the same wider tensor do not."""
     packed = cu_seqlens is not None
     io, device = x.dtype, x.device
     x, shape, B, state, head = _conv_head(_CONV_FWD_SIZE, x, weight, bias, act, x0, cu_seqlens, layout)

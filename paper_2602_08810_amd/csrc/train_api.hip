@@ -5,6 +5,9 @@
 #include "grad_clip.hpp"
 #include "vocab_loss.hpp"
 
+#include <cstdlib>
+#include <initializer_list>
+
 using namespace lrnnx;
 
 namespace {
@@ -14,6 +17,50 @@ inline bool on(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t
 inline size_t elem(int dtype) { return dtype == LRNNX_BF16 ? 2 : 4; }
 inline bool io_type(int dtype) { return dtype == LRNNX_F32 || dtype == LRNNX_BF16; }
 inline int status(hipError_t e) { return e == hipSuccess ? LRNNX_OK : LRNNX_ERR_LAUNCH; }
+
+// Memory of a tensor: up to two axes of rows, steps and row in bytes.
+struct Area {
+    const char *p = nullptr;
+    int64_t row = 0, n[2] = {1, 1}, step[2] = {0, 0};
+    Area(const void *p, int64_t row, int64_t n0 = 1, int64_t step0 = 0, int64_t n1 = 1, int64_t step1 = 0) : p(static_cast<const char *>(p)), row(row) {
+        const bool turned = n1 > 1 && (n0 <= 1 || std::abs(step1) < std::abs(step0));          // the axis of smaller steps first
+        n[0] = turned ? n1 : n0; step[0] = turned ? step1 : step0;
+        n[1] = turned ? n0 : n1; step[1] = turned ? step0 : step1;
+        for (int k = 0; k < 2; ++k) if (n[k] <= 1) { n[k] = 1; step[k] = 0; }
+    }
+    int64_t low() const { return (step[0] < 0 ? step[0] * (n[0] - 1) : 0) + (step[1] < 0 ? step[1] * (n[1] - 1) : 0); }
+    int64_t high() const { return (step[0] > 0 ? step[0] * (n[0] - 1) : 0) + (step[1] > 0 ? step[1] * (n[1] - 1) : 0) + row; }
+};
+// Whether two tensors share an element.  Exact for views of the same shape and steps whose rows do not overlap themselves (parts of the channels of a wider tensor); of others it is
+// enough that their extents do.
+bool meet(const Area &a, const Area &b) {
+    if (!a.p || !b.p) return false;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+    if (a.high() <= apart + b.low() || apart + b.high() <= a.low()) return false;
+    int64_t span = a.row;
+    bool same = a.row == b.row;
+    for (int k = 0; k < 2; ++k) {
+        same = same && a.n[k] == b.n[k] && a.step[k] == b.step[k] && (a.n[k] == 1 || a.step[k] >= span);
+        span += a.step[k] * (a.n[k] - 1);
+    }
+    if (!same) return true;
+    // rows i of a and j of b lie `apart` + step (j - i) apart: below a row's length for one of the two differences next to it of either axis, or for none
+    const auto near = [](int64_t d, int64_t step, int k) { return step ? (d >= 0 ? d / step : -((-d + step - 1) / step)) + k : 0; };
+    for (int i = 0; i < 2; ++i) {
+        const int64_t c1 = near(apart, a.step[1], i);
+        if (std::abs(c1) >= a.n[1]) continue;
+        const int64_t left = apart - c1 * a.step[1];
+        for (int j = 0; j < 2; ++j) {
+            const int64_t c0 = near(left, a.step[0], j);
+            if (std::abs(c0) < a.n[0] && std::abs(left - c0 * a.step[0]) < a.row) return true;
+        }
+    }
+    return false;
+}
+bool meet(const Area &a, std::initializer_list<Area> others) {
+    for (const Area &b : others) if (meet(a, b)) return true;
+    return false;
+}
 
 // ---------------------------------------------------------------- short causal convolution
 template <class A> int conv_checks(const A *a) {
@@ -37,6 +84,15 @@ template <class A> ConvParams conv_params(const A *a, bool backward) {
     plan_conv(p, backward);
     return p;
 }
+// [B,L,D] or [B,D,L] with these strides; [B,W-1,D]; the inputs that both passes have
+template <class A> Area conv_rows(const A *a, const void *p, int64_t sb, int64_t ss) {
+    const int64_t es = elem(a->io_dtype);
+    return Area(p, (a->time_last ? a->L : a->D) * es, a->time_last ? a->D : a->L, ss * es, a->cu_seqlens ? 1 : a->B, sb * es);
+}
+template <class A> Area conv_state(const A *a, const void *p) { return Area(p, (int64_t)a->B * (a->W - 1) * a->D * (int64_t)elem(a->io_dtype)); }
+template <class A> bool over_inputs(const A *a, const Area &out) {
+    return meet(out, {conv_rows(a, a->x, a->x_stride_b, a->x_stride_s), Area(a->weight, (int64_t)a->D * a->W * 4), Area(a->bias, (int64_t)a->D * 4), conv_state(a, a->x0), Area(a->cu_seqlens, ((int64_t)a->B + 1) * 8)});
+}
 size_t conv_sums_bytes(const ConvParams &p) { return (size_t)p.blocks * (p.W + 1) * p.D * sizeof(float); }
 
 }  // namespace
@@ -48,6 +104,8 @@ int lrnnx_short_conv_fwd(const lrnnx_conv_fwd_args *a) {
     if (const int e = conv_checks(a)) return e;
     const size_t es = elem(a->io_dtype);
     if (!conv_inputs(a) || !a->y || !on(a->y, es) || !on(a->x_last, es)) return LRNNX_ERR_INVALID_ARG;
+    const Area y = conv_rows(a, a->y, a->y_stride_b, a->y_stride_s), last = conv_state(a, a->x_last);
+    if (over_inputs(a, y) || over_inputs(a, last) || meet(y, last)) return LRNNX_ERR_INVALID_ARG;
     ConvParams p = conv_params(a, false);
     p.y = a->y; p.y_b = a->y_stride_b; p.y_l = a->time_last ? 1 : a->y_stride_s; p.y_d = a->time_last ? a->y_stride_s : 1;
     p.x_last = a->x_last;
@@ -68,6 +126,10 @@ int lrnnx_short_conv_bwd(const lrnnx_conv_bwd_args *a) {
     if (!on(a->dy, es) || !on(a->dx, es) || !on(a->dx_last, es) || !on(a->dx0, es) || !on(a->dweight, 4) || !on(a->dbias, 4) || !on(a->workspace, 16)) return LRNNX_ERR_INVALID_ARG;
     ConvParams p = conv_params(a, true);
     if (!a->workspace || a->workspace_bytes < conv_sums_bytes(p)) return LRNNX_ERR_WORKSPACE;
+    const Area dx = conv_rows(a, a->dx, a->dx_stride_b, a->dx_stride_s), dx0 = conv_state(a, a->dx0), dw(a->dweight, (int64_t)a->D * a->W * 4), db(a->dbias, (int64_t)a->D * 4);
+    const Area dy = conv_rows(a, a->dy, a->dy_stride_b, a->dy_stride_s), dx_last = conv_state(a, a->dx_last);
+    for (const Area &out : {dx, dx0, dw, db}) if (over_inputs(a, out) || meet(out, {dy, dx_last})) return LRNNX_ERR_INVALID_ARG;
+    if (meet(dx, {dx0, dw, db}) || meet(dx0, {dw, db}) || meet(dw, db)) return LRNNX_ERR_INVALID_ARG;
     p.dy = a->dy; p.dy_b = a->dy_stride_b; p.dy_l = a->time_last ? 1 : a->dy_stride_s; p.dy_d = a->time_last ? a->dy_stride_s : 1;
     p.dx = a->dx; p.y_b = a->dx_stride_b; p.y_l = a->time_last ? 1 : a->dx_stride_s; p.y_d = a->time_last ? a->dx_stride_s : 1;
     p.dx_last = a->dx_last; p.dx0 = a->dx0; p.dw = a->dweight; p.db = a->dbias;
@@ -83,6 +145,12 @@ int lrnnx_short_conv_step(const lrnnx_conv_step_args *a) {
     if (a->W < 2 || a->W > 4 || a->D > 65536 || a->B > 65535) return LRNNX_ERR_UNSUPPORTED;
     const size_t es = elem(a->io_dtype);
     if (!a->x || !a->weight || !a->state || !a->y || !on(a->x, es) || !on(a->state, es) || !on(a->y, es) || !on(a->weight, 4) || !on(a->bias, 4)) return LRNNX_ERR_INVALID_ARG;
+    // (y may be x: a thread has read what it writes)
+    const int64_t bytes = (int64_t)es;
+    const Area x(a->x, bytes, a->D, a->x_stride_d * bytes, a->B, a->x_stride_b * bytes), y(a->y, bytes, a->D, a->y_stride_d * bytes, a->B, a->y_stride_b * bytes);
+    const Area state(a->state, bytes * a->B * (a->W - 1) * a->D), w(a->weight, (int64_t)a->D * a->W * 4), bias(a->bias, (int64_t)a->D * 4);
+    const bool in_place = a->x == a->y && (a->B == 1 || a->x_stride_b == a->y_stride_b) && (a->D == 1 || a->x_stride_d == a->y_stride_d);
+    if (meet(state, {x, y, w, bias}) || meet(y, {w, bias}) || (!in_place && meet(y, x))) return LRNNX_ERR_INVALID_ARG;
     ConvStepParams p{};
     p.B = a->B; p.D = a->D; p.W = a->W; p.io = a->io_dtype == LRNNX_BF16; p.act = a->act;
     p.x = a->x; p.x_b = a->x_stride_b; p.x_d = a->x_stride_d; p.w = a->weight; p.bias = a->bias; p.state = a->state;
