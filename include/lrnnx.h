@@ -806,7 +806,7 @@ size_t lrnnx_vocab_loss_bwd_workspace_bytes(const lrnnx_vocab_bwd_args *args);
  * grads, numel, dtype, out, out_dtype are HOST arrays of `count` entries, read before the call returns: device pointers (each on its element size; NULL
  * where numel is 0), numbers of elements, lrnnx_dtype of each (LRNNX_F32 or LRNNX_BF16).  out NULL: in place (nothing is read or
  * written where scale is 1); else the types of out may be LRNNX_F32 for any tensor, or the tensor's.  The tensors of out must not overlap each other (a tensor
- * given twice would be scaled twice) nor another tensor's grad.
+ * given twice would be scaled twice) nor another tensor's grad, nor norm (that is LRNNX_ERR_INVALID_ARG).
  * lrnnx_grad_norm_workspace_bytes(args) bytes of workspace, 16-byte aligned.  eps >= 0, max_norm >= 0.                */
 typedef struct lrnnx_grad_norm_args {
     size_t struct_size;

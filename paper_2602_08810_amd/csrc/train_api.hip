@@ -455,6 +455,11 @@ int lrnnx_grad_clip(const lrnnx_grad_clip_args *a) {
             if (a->out_dtype[i] != LRNNX_F32 && a->out_dtype[i] != a->dtype[i]) return LRNNX_ERR_INVALID_ARG;
             if (a->numel[i] && (!a->out[i] || !on(a->out[i], elem(a->out_dtype[i])))) return LRNNX_ERR_INVALID_ARG;
         }
+    // every workgroup reads the norm: no result may lie there
+    for (int64_t i = 0; i < a->count; ++i) {
+        const int32_t type = a->out ? a->out_dtype[i] : a->dtype[i];
+        if (a->numel[i] && meet(Area(a->norm, 4), Area(a->out ? a->out[i] : a->grads[i], a->numel[i] * (int64_t)elem(type)))) return LRNNX_ERR_INVALID_ARG;
+    }
     int64_t pieces;
     const int64_t piece = grad_piece(a->numel, a->count, kScalePieces, pieces);
     const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);

@@ -108,3 +108,13 @@ def test_exact_for_views_of_the_same_steps(api, time_last):  # noqa: F811
                   y=BUF + 2 * at, y_stride_b=sb, y_stride_s=ss)
         assert _refused(api, "lrnnx_short_conv_fwd", a) == shared, (B, L, D, sb, ss, at)
     assert 100 < met < 500
+
+
+def test_norm_among_the_results(api):  # noqa: F811
+    n, kind, wide = (ctypes.c_int64 * 3)(5, 0, 100), (ctypes.c_int32 * 3)(0, 1, 1), (ctypes.c_int32 * 3)(0, 0, 0)
+    grads, out = (ctypes.c_void_p * 3)(BUF, None, FAR), (ctypes.c_void_p * 3)(FAR * 2, None, FAR * 3)
+    at = ctypes.addressof
+    run = lambda **over: _refused(api, "lrnnx_grad_clip", _fill(api.GradClipArgs, **{**dict(count=3, grads=at(grads), numel=at(n), dtype=at(kind), norm=FAR * 4, max_norm=1.0, eps=0.0), **over}))
+    other = dict(out=at(out), out_dtype=at(wide))
+    assert not run() and not run(norm=BUF + 20) and not run(norm=FAR + 200) and not run(norm=BUF, **other) and not run(norm=FAR * 3 + 400, **other)
+    assert run(norm=BUF) and run(norm=BUF + 16) and run(norm=FAR + 196) and run(norm=FAR * 2 + 16, **other) and run(norm=FAR * 3 + 396, **other)
