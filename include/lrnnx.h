@@ -802,7 +802,8 @@ size_t lrnnx_vocab_loss_bwd_workspace_bytes(const lrnnx_vocab_bwd_args *args);
 /* ------------------------------------------------------------------ norm and clipping of a model's gradients
  * lrnnx_grad_norm: norm[0] = sqrt(sum of the squares of all elements of all tensors), summed in double precision in a fixed order.
  * lrnnx_grad_clip: out_i = scale grad_i, scale = min(1, max_norm / (norm[0] + eps)), where norm[0] is what lrnnx_grad_norm left or any other
- * device float (a norm over several processes).  A norm that is NaN makes everything NaN; an infinite one makes scale 0.
+ * device float (a norm over several processes).  A norm that is NaN makes everything NaN; an infinite one makes scale 0 of a finite max_norm.  Where norm[0] + eps
+ * is max_norm or less, 0 and infinity among them, scale is 1.
  * grads, numel, dtype, out, out_dtype are HOST arrays of `count` entries, read before the call returns: device pointers (each on its element size; NULL
  * where numel is 0), numbers of elements, lrnnx_dtype of each (LRNNX_F32 or LRNNX_BF16).  out NULL: in place (nothing is read or
  * written where scale is 1); else the types of out may be LRNNX_F32 for any tensor, or the tensor's.  The tensors of out must not overlap each other (a tensor

@@ -90,7 +90,7 @@ template <class T, class O> __device__ __forceinline__ void piece_scale(const T 
     if (threadIdx.x < n - whole) store_io(out + whole + threadIdx.x, load_io(g + whole + threadIdx.x) * scale);
 }
 __global__ __launch_bounds__(256) void k_grad_scale(const GradList l, const float *norm, float max_norm, float eps, int in_place) {
-    const float c = max_norm / (*norm + eps), scale = c >= 1.0f ? 1.0f : c;        // (a norm that is NaN stays)
+    const float all = *norm + eps, scale = all <= max_norm ? 1.0f : max_norm / all;      // (a norm that is NaN stays; 0 / 0 is 1)
     if (in_place && scale == 1.0f) return;
     const int t = grad_tensor(l, blockIdx.x);
     const int64_t at = (int64_t)(blockIdx.x - l.first[t]) * l.piece, left = l.n[t] - at;
