@@ -11,6 +11,7 @@
 // rows' targets in one tile of words, else 830; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
 #include "vocab_loss.hpp"
 #include "conv_common.hpp"
+#include "lds_load.hpp"
 
 namespace lrnnx {
 
@@ -29,20 +30,6 @@ template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct Vocab
     static constexpr int LOADS = STAGE / (THREADS * 16);                              // of a thread and a stage
     static constexpr int PER_UNIT = M == 256 ? 1 : 2;                                 // workgroups a compute unit
 };
-
-// N times 16 bytes a lane from memory to LDS, a workgroup's from STEP to STEP, beside the lanes before.  Not the compiler's instruction for it: of that it takes every later read of LDS for
-// one of what it brings, and waits for it (dh of 8192 x 2048, 32768 terms: 944 us so, 828); what has to be waited for is waited for where a stage changes hands.  There is no result in
-// a register.  The descriptor may have come from the vector unit just now, which takes five instructions' time, m0 one.
-template <int N, int STEP> __device__ __forceinline__ void load_lds(uint32_t to, const u32x4 &from, const uint32_t (&off)[N]) {
-    static_assert(N == 1 || N == 2 || N == 4, "");
-#define LOAD_FIRST "s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %1, 0 offen lds"
-#define LOAD_NEXT(o, at) "\n\ts_add_u32 m0, m0, %" at "\n\ts_nop 0\n\tbuffer_load_dwordx4 %" o ", %1, 0 offen lds"
-    if constexpr (N == 1) asm volatile(LOAD_FIRST ::"s"(to), "s"(from), "v"(off[0]));
-    else if constexpr (N == 2) asm volatile(LOAD_FIRST LOAD_NEXT("3", "4") ::"s"(to), "s"(from), "v"(off[0]), "v"(off[1]), "n"(STEP) : "scc");
-    else asm volatile(LOAD_FIRST LOAD_NEXT("3", "6") LOAD_NEXT("4", "6") LOAD_NEXT("5", "6") ::"s"(to), "s"(from), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "n"(STEP) : "scc");
-#undef LOAD_FIRST
-#undef LOAD_NEXT
-}
 
 // One factor of a tile.  ALONG: rows of the source are the tile's rows (columns: the terms of the sum); else rows of the source are the terms.
 // LDS, ALONG: [ROWS rows][STEP terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), or of rows of four ^ (row / 4 & 3), so that the 16 rows of a fragment,
