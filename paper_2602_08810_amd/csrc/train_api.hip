@@ -175,7 +175,9 @@ template <class A> bool vocab_inputs(const A *a) {
 }
 // Rows that the matrix kernels can read as they lie: whole 16-byte pieces at 16-byte steps, 256 of them within 31 bits.
 bool rows_in_place(const void *p, int64_t ld, int K, int io) { return io == LRNNX_BF16 && on(p, 16) && K % 8 == 0 && ld % 8 == 0 && ld >= K && ld <= 1 << 21; }
-bool wide_in_place(const void *p, int64_t ld, int K) { return on(p, 16) && K % 4 == 0 && ld % 4 == 0 && ld >= K && ld <= 1 << 21; }
+// What is split where it is read, an element a load if need be.
+bool wide_in_place(int64_t ld, int K) { return ld >= K && ld <= 1 << 21; }
+bool wide_pieces(const void *p, int64_t ld, int K) { return on(p, 16) && K % 4 == 0 && ld % 4 == 0; }
 
 struct Layout {
     char *base;
@@ -247,7 +249,8 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         k.dst = l.take<uint16_t>((planes ? planes : 2) * k.plane);
         to = {k.dst, k.plane, ldd};
     };
-    const bool copied = !(p.wide ? wide_in_place(a->weight, a->weight_stride, a->K) : rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype));
+    const bool copied = !(p.wide ? wide_in_place(a->weight_stride, a->K) : rows_in_place(a->weight, a->weight_stride, a->K, a->io_dtype));
+    p.any = p.wide && !copied && !wide_pieces(a->weight, a->weight_stride, a->K);
     int64_t each = piece_of(a->V, copied ? (p.wide ? 2 : planes) * ldd * 2 : 0);
     if (backward) {
         const int64_t of_dz = piece_of(a->V, planes * a->T * 2);

@@ -22,12 +22,12 @@ namespace lrnnx {
 // the small one 128 x 64, four of 32 x 64, two a compute unit.
 // WIDE, the first factor in float32 and split as it is read: 128 x 64, four of 32 x 64, and 64 x 64, four of 16 x 64, two a compute unit (20 rows, 151790 words, 768 terms: z 150 us,
 // dh 91: 3.1 and 5.1 TB/s; all in tiles of 64 x 64, before loads that nothing waits for, 186 and 128 where this did 160 and 95; four stages of LDS, one workgroup a compute unit: 190 and 145).
-template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct VocabSize {
-    static constexpr bool WIDE = WIDE_;
+template <int M_, int N_, int WM_, int PLANES_, int WIDE_ = 0> struct VocabSize {
+    static constexpr bool WIDE = WIDE_ > 0, ANY = WIDE_ > 1;
     static constexpr int M = M_, N = N_, WM = WM_, PLANES = PLANES_, STEP = PLANES == 1 ? 64 : 32;
     static constexpr int NI = M / WM / 16, NJ = 4, WAVES = WM * (N / 64), THREADS = WAVES * 64;
     static constexpr int PLANE_A = M * STEP * 2, PLANE_B = N * STEP * 2, OPERAND_A = WIDE ? M * STEP * 4 : PLANES * PLANE_A, STAGE = OPERAND_A + PLANES * PLANE_B;        // bytes of LDS
-    static constexpr int LOADS = STAGE / (THREADS * 16);                              // of a thread and a stage
+    static constexpr int LOADS = STAGE / (THREADS * 16) + (ANY ? 3 * OPERAND_A / (THREADS * 16) : 0);        // of a thread and a stage
     static constexpr int PER_UNIT = M == 256 ? 1 : 2;                                 // workgroups a compute unit
 };
 
@@ -35,15 +35,17 @@ template <int M_, int N_, int WM_, int PLANES_, bool WIDE_ = false> struct Vocab
 // LDS, ALONG: [ROWS rows][STEP terms], 16-byte pieces of a row exchanged by piece ^ (row & 7), or of rows of four ^ (row / 4 & 3), so that the 16 rows of a fragment,
 // read at one place each, lie in all banks.  Else [STEP terms][ROWS], pairs of pieces (16 columns, what a transposing read takes of a row) exchanged by pair ^ (bits 3, 4 and 0, 1 of the
 // row): the 16 rows that such a read touches then lie in different banks, too.
-// WIDE: float32 elements, split as they are read; rows of 128 bytes ALONG, else groups of 16 columns exchanged by group ^ (bits 3, 4 of the row).
+// WIDE: float32 elements, split as they are read; rows of 128 bytes ALONG, else groups of 16 columns exchanged by group ^ (bits 3, 4 of the row).  ANY: the same in LDS by loads of
+// an element, from rows that are no 16-byte pieces at 16-byte steps (forward calls of 11 rows, 50706 words, 2801 terms 160 us; from a copy 357; of 512, 20000, 2049 282 and 320).
 template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand {
     static constexpr int BYTES = WIDE ? 4 : 2, EACH = 16 / BYTES;             // bytes of an element, elements of a piece
-    static constexpr int PLANE = ROWS * S::STEP * BYTES, LOADS = PLANE / (S::THREADS * 16);
+    static constexpr bool ANY = WIDE && S::ANY;
+    static constexpr int PLANE = ROWS * S::STEP * BYTES, LOADS = PLANE / (S::THREADS * (ANY ? 4 : 16));
     const char *base;                    // of the next stage
     int64_t step, left;                  // bytes from stage to stage; terms left
     int64_t ld, outer;                   // bytes of a row; rows (ALONG) or columns of the source from the tile's first on
     int64_t plane;                       // bytes from plane to plane
-    uint32_t off[LOADS];                 // this thread's pieces
+    uint32_t off[ANY ? 4 : LOADS];       // this thread's pieces; ANY: of load j the one at ALONG 0, else (j's row >> 3) & 3, and so many rows on
     static constexpr int PIECES = S::STEP / EACH;         // of a row, ALONG
     static __device__ __forceinline__ int turned(int row) { return PIECES == 8 ? row & 7 : row >> 2 & 3; }
     static __device__ __forceinline__ int mixed(int row) {
@@ -59,6 +61,16 @@ template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand 
         base = reinterpret_cast<const char *>(f.p) + (ALONG ? first * ld + k * BYTES : k * ld + first * BYTES);
         step = ALONG ? S::STEP * BYTES : S::STEP * ld;
         const int tid = threadIdx.x;
+        if constexpr (ANY) {
+            constexpr int ROW = ALONG ? S::STEP : ROWS, EVERY = S::THREADS / ROW;             // elements of a row, rows of a load
+            static_assert(ALONG ? EVERY == 8 && PIECES == 8 : EVERY <= 8, "");              // (of which the exchange is the same for all loads, or for all rows)
+            const int row = tid / ROW, at = tid % ROW;
+#pragma unroll
+            for (int m = 0; m < (ALONG ? 1 : 4); ++m) {
+                const int e = ALONG ? ((at >> 2) ^ turned(row)) * 4 + (at & 3) : ((at >> 4) ^ m) * 16 + (at & 15);
+                off[m] = ALONG || e < outer ? (uint32_t)(row * ld) + e * 4 : kOutside;
+            }
+        } else
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             if (ALONG) {
@@ -73,21 +85,34 @@ template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand 
     }
     // the next 64 terms into LDS; terms behind the last and rows behind the last read as zeros
     __device__ __forceinline__ void load(char *lds) {
-        int64_t bytes = ALONG ? (outer - 1) * ld + (left + EACH - 1) / EACH * 16 : (left - 1) * ld + (outer + EACH - 1) / EACH * 16;
+        constexpr int WHOLE = ANY ? 1 : EACH;
+        int64_t bytes = ALONG ? (outer - 1) * ld + (left + WHOLE - 1) / WHOLE * WHOLE * BYTES : (left - 1) * ld + (outer + WHOLE - 1) / WHOLE * WHOLE * BYTES;
         bytes = left <= 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : bytes;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int q = 0; q < (WIDE ? 1 : S::PLANES); ++q) {
             const char *at = base + q * plane;
             const u32x4 b = {(uint32_t)(uintptr_t)at, (uint32_t)((uintptr_t)at >> 32) & 0xffff, (uint32_t)bytes, 0x00020000};       // as of buffer_of
-            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)(lds + q * PLANE + wave * 1024);
-            uint32_t o[LOADS];
+            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)(lds + q * PLANE + wave * (ANY ? 256 : 1024));
+            if constexpr (ANY) {
+                constexpr int EVERY = S::THREADS / (ALONG ? S::STEP : ROWS);
+                const bool there = !ALONG || ((threadIdx.x % S::STEP >> 2) ^ turned(threadIdx.x / S::STEP)) * 4 + (threadIdx.x & 3) < left;
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) {
-                o[j] = off[j];
-                if (ALONG) o[j] = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * EACH < left ? o[j] : kOutside;
+                for (int j = 0; j < LOADS; j += 4) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = there ? off[ALONG ? 0 : EVERY * (j + i) >> 3 & 3] + (uint32_t)(EVERY * (j + i) * ld) : kOutside;
+                    load_lds<4, S::THREADS * 4, 4>(to + j * S::THREADS * 4, b, o);
+                }
+            } else {
+                uint32_t o[LOADS];
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    o[j] = off[j];
+                    if (ALONG) o[j] = ((threadIdx.x % PIECES) ^ turned(threadIdx.x / PIECES)) * EACH < left ? o[j] : kOutside;
+                }
+                load_lds<LOADS, S::THREADS * 16>(to, b, o);
             }
-            load_lds<LOADS, S::THREADS * 16>(to, b, o);
         }
         base += step;
         left -= S::STEP;
@@ -934,8 +959,8 @@ using VocabLarge = VocabSize<256, 256, 2, 1>;
 using VocabSmall = VocabSize<128, 128, 2, 1>;
 using VocabPlanes = VocabSize<256, 128, 4, 3>;
 using VocabPlanesSmall = VocabSize<128, 64, 4, 3>;
-using VocabWide = VocabSize<128, 64, 4, 3, true>;
-using VocabWideSmall = VocabSize<64, 64, 4, 3, true>;
+template <bool ANY> using VocabWide = VocabSize<128, 64, 4, 3, ANY ? 2 : 1>;
+template <bool ANY> using VocabWideSmall = VocabSize<64, 64, 4, 3, ANY ? 2 : 1>;
 template <class S> int64_t vocab_tiles(int64_t m, int64_t n) { return ((m + S::M - 1) / S::M) * ((n + S::N - 1) / S::N); }
 inline unsigned whole_dies(int64_t n) { return (unsigned)((n + 7) / 8 * 8); }
 
@@ -969,13 +994,12 @@ struct RunDw {
     hipStream_t s;
     template <class S> void run() const { hipLaunchKernelGGL(k_vocab_dw<S>, dim3(whole_dies(vocab_tiles<S>(p.K, p.V) * p.splits_w)), dim3(S::THREADS), 0, s, p); }
 };
+template <bool ANY, class F> hipError_t sized_wide(const F &f, int side) {
+    if (side == VocabWide<ANY>::M) f.template run<VocabWide<ANY>>(); else f.template run<VocabWideSmall<ANY>>();
+    return hipGetLastError();
+}
 template <class F> hipError_t sized(const F &f, int planes, int side, bool wide = false) {
-    if constexpr (F::WIDE) {
-        if (wide) {
-            if (side == VocabWide::M) f.template run<VocabWide>(); else f.template run<VocabWideSmall>();
-            return hipGetLastError();
-        }
-    }
+    if constexpr (F::WIDE) if (wide) return f.p.any ? sized_wide<true>(f, side) : sized_wide<false>(f, side);
     if (planes == 3) { if (side == VocabPlanes::M) f.template run<VocabPlanes>(); else f.template run<VocabPlanesSmall>(); }
     else { if (side == VocabLarge::M) f.template run<VocabLarge>(); else f.template run<VocabSmall>(); }
     return hipGetLastError();

@@ -23,7 +23,7 @@ struct VocabFactor {
 struct VocabParams {
     int64_t T, V, K, Kp;                 // V: words of this piece; Kp: K up to whole 16-byte pieces
     int side_z, side_h, side_w;          // first side of a tile of z, dh, dw
-    bool wide;                           // w is float32, split where it is read
+    bool wide, any;                      // w is float32, split where it is read; in rows that are no 16-byte pieces at 16-byte steps
     int planes, io;                      // io 1: bfloat16
     const int *count;                    // device: rows that have a target (null: all T); stretches of dh's words
     VocabFactor h, w, dz;                // [T,K], [V,K], [T,V]

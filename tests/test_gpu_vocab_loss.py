@@ -310,3 +310,32 @@ def test_more_rows_than_workgroups(api):
         want, t = torch.logsumexp(z, 1), target[rows]
         pick = torch.where(t >= 0, want - z.gather(1, t.clamp(min=0)[:, None])[:, 0], 0.0)
         assert float((lse[rows].double() - want).abs().max()) < 5e-6 and float((loss[rows].double() - pick).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("T,V,K", [(1, 300, 65), (9, 9000, 981), (70, 700, 1333), (300, 771, 203), (512, 2100, 133)])
+def test_float32_rows_anywhere(api, T, V, K):
+    """Few rows in float32 read the words as they lie, an element at a time where those are no 16-byte pieces: any start and step gives the same numbers, and nothing beside a row is read."""
+    import torch
+    h, w, target, dloss = _make(T + K, T, V, K, "f32")
+    loss, lse, r = _both(api, h, w, target, dloss)
+    for at, room in ((1, K + 1), (2, K + 7), (0, K + 3)):
+        wide = torch.full((V, room), float("nan"), device="cuda")
+        ws = wide[:, at:at + K]
+        ws.copy_(w)
+        l2, e2 = api.lrnnx_vocab_loss_fwd(h.cuda(), ws, target.cuda())
+        r2 = api.lrnnx_vocab_loss_bwd(h.cuda(), ws, target.cuda(), e2, dloss.cuda())
+        assert torch.equal(l2, loss) and torch.equal(e2, lse) and all(torch.equal(r[n], r2[n]) for n in r)
+
+
+def test_words_that_are_one_row(api):
+    """Rows a step of 0 apart (copied first)."""
+    import torch
+    for io in ("f32", "bf16"):
+        h, w, target, dloss = (t.cuda() for t in _make(1, 20, 300, 72, io, none=0.0))
+        w = w[:1].expand(300, 72)
+        loss, lse = api.lrnnx_vocab_loss_fwd(h, w, target)
+        want = vocab(h.cpu().double(), w.cpu().double(), target.cpu(), dloss.cpu().double())
+        _check(loss, want[0], "loss")
+        r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
+        _check(r["dweight"], want[3], "dweight")
+        assert float(r["dh"].abs().max()) < 1e-5           # the formula's is 0

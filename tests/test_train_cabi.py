@@ -135,3 +135,12 @@ def test_gradients_refuse(api):
     assert sizes(0, 0) == 0 and sizes(5, -1) == 0 and sizes(1) == 8 and sizes(8192, 8193, 0) == 24
     # pieces of total / 16384 elements rounded up by less than 2048: at least 16384 / (1 + 2048 * 16384 / total) of them
     assert 16329 * 8 <= sizes(10 ** 10) <= 16384 * 8
+
+
+def test_few_float32_rows_copy_no_vocabulary(api):
+    """Whatever the start and step of its rows."""
+    for name, cls, more in (("lrnnx_vocab_loss_fwd", api.VocabFwdArgs, {}), ("lrnnx_vocab_loss_bwd", api.VocabBwdArgs, dict(dloss=P, dh=P, dweight=P))):
+        size = lambda **over: _call(api, name + "_workspace_bytes", _fill(cls, **{**VOCAB, "V": 50000, "K": 1001, "h_stride": 1001, "weight_stride": 1001, "io_dtype": 0, **more, **over}))
+        assert 0 < size(T=20) < 50000 * 1001 * 2
+        assert size(T=20, weight_stride=1003) == size(T=20, weight=P + 4) == size(T=20)
+        assert size(T=20, weight_stride=0) >= size(T=20) + 50000 * 1001 * 4              # rows in one place are copied
