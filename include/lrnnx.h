@@ -754,7 +754,7 @@ int lrnnx_short_conv_step(const lrnnx_conv_step_args *args);
  *     z[t,v] = sum_k h[t,k] weight[v,k],   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t,target[t]].
  * h [T,K] and weight [V,K] in io_dtype with row strides, target [T] int64, loss and lse [T] float.  A row whose target is negative has
  * no loss (0; its lse is there all the same); one whose target is V or more has NaN.  T, V <= 2^27, K <= 2^20.  Rows of 16-byte pieces at
- * 16-byte steps (bfloat16), and the words of any rows for up to 512 rows in float32, are read in place, others are first copied into the workspace, a piece of the vocabulary at a time.
+ * 16-byte steps (bfloat16), and the words of any rows for a few hundred rows in float32, are read in place, others are first copied into the workspace, a piece of the vocabulary at a time.
  * lrnnx_vocab_loss_fwd_workspace_bytes(args) bytes of workspace, 256-byte aligned.  Products run on matrix units and are summed in float32; a float32
  * number is taken as the sum of three bfloat16 ones, and a product as six of theirs (relative error about 2^-23 of the factors' sizes; their
  * magnitudes must stay below 3.3e38, what is smaller than 1e-30 loses accuracy).  Results are bitwise reproducible.      */

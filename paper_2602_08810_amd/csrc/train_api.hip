@@ -197,9 +197,11 @@ struct VocabPlan {
     size_t bytes;
 };
 
-// Float32 inputs of so few rows: the weight is split where it is read, instead of once, into a copy.  (z, dz and dh of 100 rows, 56617 words, 1472 terms 156, 163 and 141 us, from
-// a copy 193, 196 and 171 and twice 140 to make it; of 320 rows, 15179, 768 the same but for the copies; of more it is split too often.)
-constexpr int kVocabFew = 512;
+// Float32 inputs of so few rows: the weight is split where it is read, instead of once, into a copy.  The products then take a fifth longer (168 for 210 TFLOP/s), the copy is 10 bytes an
+// element; forward it is for one product, backward for two.  (100 rows, 56617 words, 1472 terms: z, dz and dh 156, 163 and 141 us, from a copy 193, 196 and 171 and twice 140 to make it.  Split, over
+// a copy, of 5000 to 150000 words and 332 to 4096 terms: forward, 576 rows 0.70 to 0.96, 768 0.71 to 1.05, 896 0.90 to 1.17; backward, 576 rows 0.87 to 1.03, 704 0.90 to 1.06, 896 0.98 to 1.15.
+// Where terms are few the copy is small beside what comes of z: 150000 words of 64 1.06 of 450 rows, 1.11 of 576, 1.24 of 768.)
+int64_t vocab_few(int64_t K, bool backward) { return K < 256 ? 512 : backward ? 576 : 768; }
 // The vocabulary is taken in as few pieces as lie in 1 GiB of workspace (a piece's dz; of a copied vocabulary its copy): of whole tiles.
 constexpr int64_t kVocabRoom = (int64_t)1 << 30;
 int64_t piece_of(int64_t words, int64_t bytes_each) {
@@ -242,7 +244,7 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
     Layout l{ws};
     VocabParams &p = f.p;
     p.T = a->T; p.K = a->K; p.Kp = Kp; p.planes = planes; p.io = io; p.words = a->V; p.target = a->target;
-    p.wide = !io && a->T <= kVocabFew;
+    p.wide = !io && a->T <= vocab_few(a->K, backward);
     auto copy = [&](VocabPack &k, VocabFactor &to, const void *src, int64_t ld, int64_t rows, int planes, bool must) {
         if (!must) { to = {reinterpret_cast<const uint16_t *>(src), 0, ld}; return; }
         k.src = src; k.ld = ld; k.rows = rows; k.ldd = ldd; k.plane = rows * ldd; k.K = a->K; k.Kp = (int)Kp; k.io = io; k.planes = planes;

@@ -339,3 +339,9 @@ def test_words_that_are_one_row(api):
         r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
         _check(r["dweight"], want[3], "dweight")
         assert float(r["dh"].abs().max()) < 1e-5           # the formula's is 0
+
+
+@pytest.mark.parametrize("T,V,K", [(512, 300, 255), (513, 300, 255), (576, 700, 256), (577, 700, 260), (768, 300, 259), (769, 2100, 256), (640, 7000, 333)])
+def test_float32_words_split_where_read_or_copied(api, T, V, K):
+    """Either side of where either pass goes over from one to the other, and one each."""
+    _both(api, *_make(T + K, T, V, K, "f32"))
