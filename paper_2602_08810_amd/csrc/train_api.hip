@@ -287,7 +287,7 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
             f.rows.row_others = p.row_others = l.take<int>(a->T);
             p.row_key = l.take<int>(a->T);
             p.row_sum = l.take<float>(a->T);
-            p.row_left = l.take<float>(a->T);
+            p.row_left = l.take<float2>(a->T);
             p.sum_part = l.take<float>(a->T * sum_blocks(p, each));
         }
         if (p.splits_w > 1) p.dw_part = l.take<float>(p.splits_w * each * Kp);

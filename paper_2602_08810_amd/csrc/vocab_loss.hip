@@ -2,8 +2,8 @@
 //     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz w,   dw = dz^T h.
 // Forward: a tile of z stays in registers from its product to its largest number and sum, which is all that leaves it (8 bytes for 256 words and a row); a second
 // launch joins them.  Backward: z is formed again, a piece of the vocabulary at a time, dz of the piece goes to the workspace in bfloat16 and from there into both products.  What
-// that rounding takes from the target's element, and from another word's whose p is over 1/8 (eight of a row at most), is kept in float32 and added to both, and to dh as much of the target's
-// word as is missing to the row's sum, which is 0: the gradients are then as exact as their own rounding to bfloat16, 1.66e-3 (all elements rounded: 2.4e-3; all but the target's, of rows that
+// that rounding takes from the target's element, and from another word's whose p is over 1/8 (eight of a row at most), is kept in float32 and added to both, and in dh a row's p are
+// taken relative to what they add up to as stored: the gradients are then as exact as their own rounding to bfloat16, 1.66e-3 (all elements rounded: 2.4e-3; all but the target's, of rows that
 // give another word 0.95, 2.0e-3, and 3.8e-3 or 1.1e-2 where all words have a component in common of 3 or 10 times their own norm, which has to cancel in dh).  Rows without a target are left
 // out before the gradients' products: they cost nothing there and nothing in them, finite or not, reaches a gradient.
 // Float32 inputs: every factor is the sum of three bfloat16 numbers, a product six of theirs (terms of 2^-24 and below are left out), summed in float32.
@@ -777,7 +777,10 @@ template <class S> __global__ __launch_bounds__(S::THREADS) void k_vocab_dh(cons
     }
 }
 
-// A row's other rests by word, its target and their number in one, and what is missing to its sum: 64 rows a workgroup, their blocks' sums in 16 stretches.
+// A row's other rests by word, its target and their number in one, and what is missing to its sum: 64 rows a workgroup, their blocks' sums in 16 stretches.  With the sum off by x, what
+// all words have in common does not cancel in dh, which it does of the exact dz.  The p as they are stored add up to 1 - x / dloss: they are taken relative to that, the sum (dh + dloss w[target]) / dloss
+// of their words and all.  (x given to the target instead adds its own row's error where words have nothing in common: dh of 512 rows, 4000 words in double precision 5.0e-5 so, 3.6e-5, with none 3.7e-5; with a
+// component in common of 10 times a word's own 5.2e-5, 3.6e-5, 3.6e-4.)
 __global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
     __shared__ float lds[16][64];
     const int lane = threadIdx.x & 63, stretch = threadIdx.x >> 6;
@@ -803,8 +806,9 @@ __global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
         for (; at > 1 && rest[at - 1].word > x.word; --at) rest[at] = rest[at - 1];
         rest[at] = x;
     }
-    for (int i = 1; i <= n; ++i) s += rest[i].rest;
-    p.row_left[row] = fabsf(s) < INFINITY ? -s : 0.0f;
+    for (int i = 0; i <= n; ++i) s += rest[i].rest;
+    const float scale = p.row_scale[row], grow = -s / scale;
+    p.row_left[row] = fabsf(grow) < 0.1f ? make_float2(-s, grow) : make_float2(0.0f, 0.0f);        // (else, dloss 0 or next to it among others, there is no such thing)
     p.row_key[row] = p.row_target[row] < 0 ? -1 : p.row_target[row] | n << kVocabWordBits;
 }
 hipError_t launch_vocab_rests(const VocabParams &p, hipStream_t s) {
@@ -1152,7 +1156,7 @@ hipError_t launch_vocab_loss(const VocabLoss &p, hipStream_t s) {
 }
 
 // Rows of a result from the parts of its sum, four columns a thread; PARTS threads take a stretch of the parts each where there are many.  `place`: where a row's lie, -1:
-// nowhere, and the row is zero.  `key`: to a row of dh what is missing to its sum is added as so much of the target's row of w, and the rests of other words as so much of theirs.
+// nowhere, and the row is zero.  `key`: to a row of dh the rests are added as so much of their words' rows of w, and its p brought to the sum that they have.
 template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_add(const VocabAdd p) {
     constexpr int ITEMS = 256 / PARTS;
     __shared__ f32x4 lds[PARTS > 1 ? 256 : 1];
@@ -1185,8 +1189,12 @@ template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_ad
 #pragma unroll
                     for (int e = 0; e < 4; ++e) if (c + e < p.K) s[e] = __builtin_fmaf(rest, load_io(w + e), s[e]);
                 };
-                more(key & ((1 << kVocabWordBits) - 1), p.left[at]);
+                const int64_t target = key & ((1 << kVocabWordBits) - 1);
+                const float2 left = p.left[at];
+                more(target, p.rests[at * kVocabRests].rest);
                 for (int q = 1; q <= key >> kVocabWordBits; ++q) more(p.rests[at * kVocabRests + q].word, p.rests[at * kVocabRests + q].rest);
+                s += s * left.y;
+                more(target, left.x);
             }
             const float x[4] = {s[0], s[1], s[2], s[3]};
             store_part(reinterpret_cast<IO *>(p.out) + row * p.K + c, x, p.K - c);

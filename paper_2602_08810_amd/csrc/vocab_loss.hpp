@@ -45,7 +45,8 @@ struct VocabParams {
     float *sum_part;                     // sums of the stored dz over blocks of words: (row, block) at row * sum_row + block * sum_block
     int64_t sum_row, sum_block;
     int sum_blocks;
-    float *row_sum, *row_left;           // of the row's stored dz, all pieces so far; what is missing to the row's sum, which is 0, rests of other words apart
+    float *row_sum;                      // of the row's stored dz, all pieces so far
+    float2 *row_left;                    // what is missing to the sum of its dz with all rests, which is 0; by how much its p are too small for that, relative to them
     float *dh_part;                      // [stretches, rows that have a target, Kp], within [splits,T,Kp]
     int splits, first;                   // first piece: the parts are set, not added to
     float *dw_part;                      // [splits_w,V,Kp], if there are several
@@ -101,7 +102,7 @@ struct VocabAdd {
     const int *place;                    // or null
     const int *count;                    // or null; device: rows of a part, parts
     const int *key;                      // by row of the parts, or null: as in VocabParams, with what is to be added
-    const float *left;
+    const float2 *left;
     const VocabRest *rests;
     const void *w; int64_t w_ld;
     void *out;                           // [rows,K]

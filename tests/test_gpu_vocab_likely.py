@@ -3,7 +3,7 @@ exact as their own rounding to bfloat16.
 
 Tolerance of the 2-norm, from the exact dz of each case: the result's own rounding (taken: the exact result rounded), and, independent of it, what rounding dz leaves.  Elements of a p over
 1/8 and the target's are kept whole; another's rounding is at most 2^-8 / sqrt(3) of it in the root mean square (a number at the lower end of its power of two).  To dw it counts times its row of
-h, to dh times the difference between its word and the target, since the target's element takes up what is missing to the row's sum.  A tenth on top for the finite number of elements and float32 sums."""
+h, to dh times the difference between its word and the mean of the words by their p, since these are brought to the sum that they have.  A tenth on top for the finite number of elements and float32 sums."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -59,7 +59,7 @@ def _check(api, h, w, target, dloss):
         dh[lo:lo + 2048] = dz @ wd
         dw += dz.t().contiguous() @ rows
         left = torch.where(listed, 0.0, dz).square()
-        mine = wd[at[:, 0]]
+        mine = p @ wd
         left_h += (left * (norms[None] - 2 * (mine @ wd.t().contiguous()) + (mine * mine).sum(1)[:, None])).sum().item()
         left_w += (left.sum(1) * (rows * rows).sum(1)).sum().item()
     for n, want, left in (("dh", dh, left_h), ("dweight", dw, left_w)):
