@@ -283,8 +283,7 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
         if (io) {
-            p.rests = l.take<VocabRest>(a->T * kVocabRests);
-            f.rows.row_others = p.row_others = l.take<int>(a->T);
+            f.rows.rests = p.rests = l.take<VocabRest>(a->T * kVocabRests);
             p.row_key = l.take<int>(a->T);
             p.row_sum = l.take<float>(a->T);
             p.row_left = l.take<float2>(a->T);
@@ -309,8 +308,6 @@ int vocab_piece(VocabPlan &f, const void *weight, int64_t stride, int64_t v0, hi
     p.V = p.words - v0 < f.each ? p.words - v0 : f.each;
     p.first = v0 == 0;
     p.sum_blocks = (int)sum_blocks(p, p.V);
-    p.sum_row = p.splits_z > 1 ? p.sum_blocks : 1;
-    p.sum_block = p.splits_z > 1 ? 1 : p.T;
     const char *from = reinterpret_cast<const char *>(weight) + v0 * stride * (p.io ? 2 : 4);
     if (!f.w.src) { p.w.p = reinterpret_cast<const uint16_t *>(from); return LRNNX_OK; }
     f.w.src = from; f.w.rows = p.V;

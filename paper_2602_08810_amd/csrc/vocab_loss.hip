@@ -510,32 +510,40 @@ __device__ __forceinline__ float vocab_rest(float d) {
 }
 // The rest of a word that is likely without being the target.  Several wavefronts add to a row's, in any order: they are sorted before they are used.
 __device__ __forceinline__ void vocab_other(const VocabParams &p, int64_t row, int64_t word, float d) {
-    const int at = atomicAdd(p.row_others + row, 1) + 1;
+    const int at = atomicAdd(&p.rests[row * kVocabRests].word, 1) + 1;
     if (at < kVocabRests) p.rests[row * kVocabRests + at] = {(int)word, vocab_rest(d)};
 }
-// The rests that a column of a tile has: its lanes' target's and those of likely words.
-template <class S> __device__ __forceinline__ void vocab_column_rests(const VocabParams &p, int64_t row, int64_t v0, int64_t left, int64_t hit, VocabExp<S::PLANES> exponential, float scale,
-                                                                      const f32x4 (&acc)[S::NI][S::NJ], int j) {
-    asm volatile("" : "+v"(exponential.base));             // (formed again: the fast path's results are not to be kept for it)
-    uint32_t found = 0;
+// The rests that a column of a tile has: its lanes' targets' and those of likely words.  (Few tiles have any: small code counts for more here than few instructions.)
+template <class S> __device__ __forceinline__ void vocab_column_rests(const VocabParams &p, int64_t row, int64_t v0, const f32x4 (&acc)[S::NI][S::NJ], int j) {
+    const float lse = p.row_lse[row], scale = p.row_scale[row], likely = lse + __logf(kVocabLikely);
+    const int hit = p.row_target[row] - (int)(p.v0 + v0), left = (int)(p.V - v0);
+    const VocabExp<S::PLANES> exponential(lse);
+    uint32_t found = hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4 ? 1u << ((hit >> 4) * 4 + (hit & 3)) : 0;
 #pragma unroll
     for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (16 * i + r < left && (hit == 16 * i + r || exponential(acc[i][j][r]) > kVocabLikely)) found |= 1u << (4 * i + r);
+        for (int r = 0; r < 4; ++r) {
+            found |= acc[i][j][r] > likely ? 1u << (4 * i + r) : 0;
+            asm volatile("" : "+v"(found));                // (one after the other: 32 masks at once are 64 registers)
+        }
     for (; found; found &= found - 1) {
         const int at = __builtin_ctz(found), word = (at >> 2) * 16 + (at & 3);
         float z = 0.0f;
 #pragma unroll
         for (int i = 0; i < S::NI; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) z = at == 4 * i + r ? acc[i][j][r] : z;
+            for (int r = 0; r < 4; ++r) {
+                z = at == 4 * i + r ? acc[i][j][r] : z;
+                asm volatile("" : "+v"(z));
+            }
         const float x = exponential(z);
+        if (word >= left) break;                           // (words beyond the last)
         if (word == hit) p.rests[row * kVocabRests].rest = vocab_rest((x - 1.0f) * scale);
         else vocab_other(p, row, p.v0 + v0 + word, x * scale);
     }
 }
-template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(const VocabParams &p, bool there, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential,
+// Whether there may be rests in the column.
+template <class S, bool APART> __device__ __forceinline__ bool vocab_dz_column(const VocabParams &p, bool there, int64_t row, int64_t v0, int64_t left, int64_t hit, const VocabExp<S::PLANES> &exponential,
                                                                                float scale, f32x4 (&acc)[S::NI][S::NJ], int j) {
 #pragma clang fp contract(off)           // (a product fused into its own split would differ between the two forms, and so with the targets of other rows)
     const int g = threadIdx.x >> 4 & 3;
@@ -557,6 +565,7 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
 #pragma unroll
         for (int q = 0; q < S::PLANES; ++q) part[q][i] = make_uint2(a[q], b[q]);
     }
+    bool rests = false;
     if constexpr (S::PLANES == 1) {
         // the sum over this wavefront's words of what is stored, as a product with ones: (which terms a lane holds is the same to a sum)
         Frag ones;
@@ -569,11 +578,10 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
             f.h[1] = part[0][i + 1];
             sum = mfma(ones, f, sum);
         }
-        if (there && g == 0) p.sum_part[row * p.sum_row + (v0 >> (S::M / S::WM == 128 ? 7 : 6)) * p.sum_block] = sum[0];
-        // (without a likely word they add up to less, rounded as they are)
-        if (there && (APART || fabsf(sum[0]) > 0.96f * kVocabLikely * fabsf(scale))) vocab_column_rests<S>(p, row, v0, left, APART ? hit : -1, exponential, scale, acc, j);
+        if (there && g == 0) p.sum_part[(v0 >> (S::M / S::WM == 128 ? 7 : 6)) * p.T + row] = sum[0];
+        rests = there && (APART || fabsf(sum[0]) > 0.96f * kVocabLikely * fabsf(scale));     // (without a likely word they add up to less, rounded as they are)
     }
-    if (!there) return;
+    if (!there) return false;
 #pragma unroll
     for (int q = 0; q < S::PLANES; ++q) {
         if constexpr (S::NI % 2 == 0) {
@@ -587,10 +595,12 @@ template <class S, bool APART> __device__ __forceinline__ void vocab_dz_column(c
 #pragma unroll
             for (int i = 0; i < S::NI; ++i) *reinterpret_cast<uint2 *>(to + q * p.dz.plane + 16 * i + 4 * g) = part[q][i];
     }
+    return rests;
 }
 template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p, VocabTile t, int64_t T, f32x4 (&acc)[S::NI][S::NJ]) {
     const VocabPlace<S> at;
     const int64_t v0 = t.m + at.m, n0 = t.n + at.n, left = p.V - v0;
+    uint32_t rests = 0;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
         const int64_t row = n0 + j * 16;
@@ -599,9 +609,16 @@ template <class S> __device__ __forceinline__ void vocab_dz(const VocabParams &p
         const int64_t hit = (there ? (int64_t)p.row_target[row] : -1) - p.v0 - v0;
         const bool apart = t.m + S::M > p.V || __any(hit >= 0 && hit < S::M / S::WM && (hit & 15) < 4);
         const VocabExp<S::PLANES> exponential(lse);
-        if (apart) vocab_dz_column<S, true>(p, there, row, v0, left, hit, exponential, scale, acc, j);
-        else vocab_dz_column<S, false>(p, there, row, v0, left, hit, exponential, scale, acc, j);
+        bool some;
+        if (apart) some = vocab_dz_column<S, true>(p, there, row, v0, left, hit, exponential, scale, acc, j);
+        else some = vocab_dz_column<S, false>(p, there, row, v0, left, hit, exponential, scale, acc, j);
+        rests |= some ? 1u << j : 0;
     }
+    if constexpr (S::PLANES == 1)
+        if (__any(rests != 0))
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+                if (rests >> j & 1) vocab_column_rests<S>(p, n0 + j * 16, v0, acc, j);
 }
 // A workgroup stays and takes a tile after the other; the next one's factors are on their way while it works on what comes of the one before.
 template <class S, bool BWD> __global__ __launch_bounds__(S::THREADS) void k_vocab_logits(const VocabParams p) {
@@ -749,7 +766,7 @@ template <int PLANES> __global__ __launch_bounds__(256) void k_vocab_part_dz(con
             }
             store_dz<PLANES>(const_cast<uint16_t *>(p.dz.p) + row * p.dz.ld + v0 + 4 * h, p.dz.plane, d);
         }
-        if (PLANES == 1) p.sum_part[row * p.sum_row + (v0 >> 3) * p.sum_block] = sum;
+        if (PLANES == 1) p.sum_part[row * p.sum_blocks + (v0 >> 3)] = sum;
     }
 }
 
@@ -787,9 +804,10 @@ __global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
     const int64_t row = (int64_t)blockIdx.x * 64 + lane;
     const bool there = row < *p.count;
     float s = 0.0f;
+    const int64_t first = p.splits_z > 1 ? row * p.sum_blocks : row, step = p.splits_z > 1 ? 1 : p.T;
     if (there)
 #pragma unroll 8
-        for (int i = stretch; i < p.sum_blocks; i += 16) s += p.sum_part[row * p.sum_row + i * p.sum_block];
+        for (int i = stretch; i < p.sum_blocks; i += 16) s += p.sum_part[first + i * step];
     lds[stretch][lane] = s;
     __syncthreads();
     if (stretch || !there) return;
@@ -797,9 +815,9 @@ __global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s += lds[i][lane];
     p.row_sum[row] = s;
-    int n = p.row_others[row];
-    if (n >= kVocabRests) n = 0;                           // (no probabilities: lse is not the row's)
     VocabRest *const rest = p.rests + row * kVocabRests;
+    int n = rest[0].word;
+    if (n >= kVocabRests) n = 0;                           // (no probabilities: lse is not the row's)
     for (int i = 2; i <= n; ++i) {
         const VocabRest x = rest[i];
         int at = i;
@@ -1096,7 +1114,7 @@ __global__ __launch_bounds__(1024) void k_vocab_rows(const VocabRows p) {
                 p.row_lse[to] = lse[r];
                 p.row_scale[to] = target[r] < p.V ? scale[r] : __builtin_nanf("");
                 p.row_target[to] = target[r] < p.V ? (int)target[r] : -1;
-                if (p.row_others) p.row_others[to] = 0;
+                if (p.rests) p.rests[(int64_t)to * kVocabRests].word = 0;
             }
             at += __popcll(have[r]);
         }
