@@ -776,7 +776,7 @@ size_t lrnnx_vocab_loss_fwd_workspace_bytes(const lrnnx_vocab_fwd_args *args);
 
 /* Its reverse-mode derivative for upstream gradients dloss [T] float (element stride dloss_stride; 0: one number for all rows):
  *     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz weight,   dweight = dz^T h,
- * dh [T,K] and dweight [V,K] in io_dtype, contiguous; either may be NULL.  Inputs as in the forward call, lse as it left it.  z is
+ * dh [T,K] and dweight [V,K] in io_dtype, contiguous; either may be NULL; neither may overlap weight or the other.  Inputs as in the forward call, lse as it left it.  z is
  * formed again a piece of the vocabulary at a time; a piece of dz, in bfloat16 (what that takes from the target's element, and from another word's of a
  * probability over 1/8, is added to both products, and in dh a row's probabilities are taken relative to what they add up to as they are stored; with float32 inputs as the sum of
  * three), lies in the workspace: lrnnx_vocab_loss_bwd_workspace_bytes(args) bytes, 256-byte aligned.  Rows without a target take no part: their dh is zero, and nothing

@@ -353,6 +353,10 @@ int lrnnx_vocab_loss_bwd(const lrnnx_vocab_bwd_args *a) {
     VocabPlan f = plan_vocab(a, reinterpret_cast<char *>(a->workspace), true);
     if (!a->workspace || a->workspace_bytes < f.bytes) return LRNNX_ERR_WORKSPACE;
     const hipStream_t s = reinterpret_cast<hipStream_t>(a->stream);
+    // the words are read again for dh when dweight is there
+    const int64_t bytes = (int64_t)es;
+    const Area words(a->weight, a->K * bytes, a->V, a->weight_stride * bytes), dh(a->dh, a->T * a->K * bytes), dweight(a->dweight, a->V * a->K * bytes);
+    if (meet(words, {dh, dweight}) || meet(dh, dweight)) return LRNNX_ERR_INVALID_ARG;
     f.rows.lse = a->lse; f.rows.dloss = a->dloss; f.rows.dloss_stride = a->dloss_stride;
     if (launch_vocab_rows(f.rows, s) != hipSuccess || launch_vocab_pack(f.h, s) != hipSuccess) return LRNNX_ERR_LAUNCH;
     f.p.dw = a->dweight;

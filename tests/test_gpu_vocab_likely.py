@@ -117,3 +117,24 @@ def test_signs_and_extremes_of_the_upstream_gradient(api):
     r = api.lrnnx_vocab_loss_bwd(h, w, target, lse, dloss)
     keep = [i for i in range(700) if i != 13]
     assert torch.equal(r["dh"][keep], want["dh"][keep]) and bool(r["dh"][13].isnan().all()) and bool(r["dweight"].isnan().all())
+
+
+def test_in_a_graph(api):
+    """Replays with other rows, sure of other words and of as many as before or fewer, in the same workspace."""
+    import torch
+    h, w, target, dloss = _make(3, 300, 2000, 264, 3, 0.97, 7)
+    run = lambda: list(api.lrnnx_vocab_loss_bwd(h, w, target, api.lrnnx_vocab_loss_fwd(h, w, target)[1], dloss).values())
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for i, (p, words) in enumerate([(0.97, 7), (0.9, 3), (0.5, 8), (0.95, 1), (0.97, 7)]):
+        other = _make(3, 300, 2000, 264, 3, p, words)      # (the same words, of other rows)
+        for a, b in zip((h, target, dloss), (other[0], other[2], other[3])):
+            a.copy_(b.roll(i, 0))
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), i

@@ -118,3 +118,12 @@ def test_norm_among_the_results(api):  # noqa: F811
     other = dict(out=at(out), out_dtype=at(wide))
     assert not run() and not run(norm=BUF + 20) and not run(norm=FAR + 200) and not run(norm=BUF, **other) and not run(norm=FAR * 3 + 400, **other)
     assert run(norm=BUF) and run(norm=BUF + 16) and run(norm=FAR + 196) and run(norm=FAR * 2 + 16, **other) and run(norm=FAR * 3 + 396, **other)
+
+
+def test_gradients_over_the_words(api):  # noqa: F811
+    base = dict(T=100, V=1000, K=64, io_dtype=1, h=FAR, h_stride=64, weight=BUF, weight_stride=70, target=FAR * 2, lse=FAR * 3, dloss=FAR * 4, dloss_stride=1, dh=FAR * 5, dweight=FAR * 6,
+                workspace=FAR * 7, workspace_bytes=1 << 40)
+    run = lambda **over: _refused(api, "lrnnx_vocab_loss_bwd", _fill(api.VocabBwdArgs, **{**base, **over}))
+    end = (999 * 70 + 64) * 2
+    assert not run() and not run(dweight=BUF + end) and not run(dh=BUF - 100 * 64 * 2) and not run(dh=None, dweight=FAR * 5)
+    assert run(dweight=BUF) and run(dweight=BUF + end - 2) and run(dh=BUF + 4) and run(dh=FAR * 6 + 1000) and run(dh=None, dweight=BUF)
