@@ -283,7 +283,8 @@ template <class A> VocabPlan plan_vocab(const A *a, char *ws, bool backward) {
         f.rows.row_scale = l.take<float>(a->T);
         f.rows.row_target = l.take<int>(a->T);
         if (io) {
-            f.rows.rests = p.rests = l.take<VocabRest>(a->T * kVocabRests);
+            p.rests = l.take<VocabRest>(a->T * kVocabRests);
+            f.rows.row_others = p.row_others = l.take<int>(a->T);
             p.row_key = l.take<int>(a->T);
             p.row_sum = l.take<float>(a->T);
             p.row_left = l.take<float2>(a->T);

@@ -510,7 +510,7 @@ __device__ __forceinline__ float vocab_rest(float d) {
 }
 // The rest of a word that is likely without being the target.  Several wavefronts add to a row's, in any order: they are sorted before they are used.
 __device__ __forceinline__ void vocab_other(const VocabParams &p, int64_t row, int64_t word, float d) {
-    const int at = atomicAdd(&p.rests[row * kVocabRests].word, 1) + 1;
+    const int at = atomicAdd(p.row_others + row, 1) + 1;
     if (at < kVocabRests) p.rests[row * kVocabRests + at] = {(int)word, vocab_rest(d)};
 }
 // The rests that a column of a tile has: its lanes' targets' and those of likely words.  (Few tiles have any: small code counts for more here than few instructions.)
@@ -816,7 +816,7 @@ __global__ __launch_bounds__(1024) void k_vocab_rests(const VocabParams p) {
     for (int i = 0; i < 16; ++i) s += lds[i][lane];
     p.row_sum[row] = s;
     VocabRest *const rest = p.rests + row * kVocabRests;
-    int n = rest[0].word;
+    int n = p.row_others[row];
     if (n >= kVocabRests) n = 0;                           // (no probabilities: lse is not the row's)
     for (int i = 2; i <= n; ++i) {
         const VocabRest x = rest[i];
@@ -1114,7 +1114,7 @@ __global__ __launch_bounds__(1024) void k_vocab_rows(const VocabRows p) {
                 p.row_lse[to] = lse[r];
                 p.row_scale[to] = target[r] < p.V ? scale[r] : __builtin_nanf("");
                 p.row_target[to] = target[r] < p.V ? (int)target[r] : -1;
-                if (p.rests) p.rests[(int64_t)to * kVocabRests].word = 0;
+                if (p.row_others) p.row_others[to] = 0;
             }
             at += __popcll(have[r]);
         }
@@ -1202,17 +1202,24 @@ template <class IO, int PARTS> __global__ __launch_bounds__(256) void k_vocab_ad
         if (q0 == 0 && i < n) {
             const int key = p.key && at >= 0 ? p.key[at] : -1;
             if (key >= 0) {
-                auto more = [&](int64_t word, float rest) {
+                auto words = [&](int64_t word) {
                     const IO *w = reinterpret_cast<const IO *>(p.w) + word * p.w_ld + c;
+                    f32x4 x = {};
+                    if (c + 4 <= p.K) {
+                        Few<IO, 4> v;
+                        v.load(w);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) if (c + e < p.K) s[e] = __builtin_fmaf(rest, load_io(w + e), s[e]);
+                        for (int e = 0; e < 4; ++e) x[e] = v.get(e);
+                    } else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) if (c + e < p.K) x[e] = load_io(w + e);
+                    return x;
                 };
-                const int64_t target = key & ((1 << kVocabWordBits) - 1);
+                const f32x4 target = words(key & ((1 << kVocabWordBits) - 1));
                 const float2 left = p.left[at];
-                more(target, p.rests[at * kVocabRests].rest);
-                for (int q = 1; q <= key >> kVocabWordBits; ++q) more(p.rests[at * kVocabRests + q].word, p.rests[at * kVocabRests + q].rest);
-                s += s * left.y;
-                more(target, left.x);
+                s += target * p.rests[at * kVocabRests].rest;
+                for (int q = 1; q <= key >> kVocabWordBits; ++q) s += words(p.rests[at * kVocabRests + q].word) * p.rests[at * kVocabRests + q].rest;
+                s += s * left.y + target * left.x;
             }
             const float x[4] = {s[0], s[1], s[2], s[3]};
             store_part(reinterpret_cast<IO *>(p.out) + row * p.K + c, x, p.K - c);

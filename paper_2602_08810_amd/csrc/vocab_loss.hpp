@@ -9,7 +9,7 @@ constexpr int kVocabTile = 256;          // rows and columns of a product's larg
 // With bfloat16 inputs, what rounding takes from a row's elements of dz: the target's, and those of other words whose p is over kVocabLikely (fewer than kVocabRests).
 constexpr int kVocabRests = 9;
 constexpr float kVocabLikely = 0.125f;
-struct VocabRest { int word; float rest; };        // (of the target's: how many others there are)
+struct VocabRest { int word; float rest; };
 // A row's target and the number of its other rests in one number; -1: a target beyond the vocabulary
 constexpr int kVocabWordBits = 27;
 
@@ -39,7 +39,8 @@ struct VocabParams {
     // backward, by row among those that have a target
     const float *row_lse, *row_scale;
     const int *row_target;               // -1: beyond the vocabulary
-    VocabRest *rests;                    // [T,kVocabRests], the target's first, the others' by word; bfloat16 only, as the next five
+    VocabRest *rests;                    // [T,kVocabRests], the target's first, the others' by word; bfloat16 only, as the next six
+    int *row_others;                     // how many others have been found
     int *row_key;
     float *sum_part;                     // sums of the stored dz over blocks of words: [blocks,T], of z in stretches [T,blocks]
     int sum_blocks;
@@ -78,7 +79,7 @@ struct VocabRows {
     int *index, *place, *count;          // row of the T that the i-th with a target is; place: the other way, -1: none
     float *row_lse, *row_scale;
     int *row_target;
-    VocabRest *rests;                    // number of others set to 0, or null
+    int *row_others;                     // set to 0, or null
     // for dh: tiles along K, rows of a tile, workgroups at once and in the launch; words of a piece; stretches that there is room for with all rows
     int across, side, at_once;
     int64_t units, each, splits;
