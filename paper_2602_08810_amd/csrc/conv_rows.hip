@@ -3,7 +3,8 @@
 // Backward, with pre formed again: g = dy act'(pre), dx[l] = sum_j w[j] g[l+(W-1)-j], dw[j] = sum g[l] x[l-(W-1)+j], dbias = sum g.
 // A thread walks the time axis for the channels of one 16-byte access, the last inputs (and, backward, the last g) in registers: every input is read from
 // memory once but for the W - 1 steps around a tile, which the caches have.  Bound by memory.
-// 4 x 4096 x 6144 in bfloat16: forward 92 us (4.4 TB/s), backward 144 (4.2), in float32 174 and 257 (4.6, 4.7); a copy of as much runs at 4.9 to 5.4.  Backward a piece is 8 bytes: in
+// 4 x 4096 x 6144 in bfloat16: forward 92 us (4.4 TB/s), backward 141 (4.3), in float32 175 and 257 (4.6, 4.7), each in a loop of its own; in turns, as in training, 81 and 154, 162 and 268 (what
+// one wrote last is still on its way to memory in the other); a copy of as much 76 and 150.  Backward a piece is 8 bytes: in
 // pieces of 16 inputs, g and sums do not fit 256 registers (22 to 26 spilled in bfloat16 with four weights), and a compute unit has two workgroups, not three.
 // The weights' gradients are summed in registers over all tiles of a thread, over a workgroup through LDS, and over workgroups by a second launch, in a fixed order.
 #include "conv_common.hpp"

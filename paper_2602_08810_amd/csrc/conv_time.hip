@@ -1,6 +1,7 @@
 // Short causal convolution with an activation, time axis contiguous ([B,D,L]): the formulas of the other layout's kernels.
 // The lanes of a row take a 16-byte piece of the time axis each, side by side; forward, the W - 1 inputs before a piece come from a second, narrower access that the
-// first level of cache has.  Bound by memory: 4 x 6144 x 4096 in bfloat16 92 us forward (4.4 TB/s), 131 backward (4.6), in float32 158 and 246 (5.1, 4.9).
+// first level of cache has.  Bound by memory: 4 x 6144 x 4096 in bfloat16 94 us forward (4.3 TB/s), 129 backward (4.7), in float32 158 and 240 (5.1, 5.0), each in a loop of its own; in turns
+// 83 and 138, 151 and 259.
 // A sequence of a packed batch is a row of its own, with as many lanes as one of average length needs (16384 steps of 2048 channels in bfloat16: 24 sequences 40 us
 // forward and 94 backward, 400 sequences 68 and 139; with pieces that may cross a boundary, and look for theirs, 137 and 739, 250 and 1206).
 #include "conv_common.hpp"
@@ -291,7 +292,7 @@ void plan_conv(ConvParams &p, bool backward) {
     p.tiles_each = (p.L + p.tile - 1) / p.tile;
     p.tiles = p.time_last && p.cu ? p.L / p.tile + p.seqs : p.B * p.tiles_each;
     const int64_t blocks = p.time_last ? p.tiles : (p.tiles + side - 1) / side;
-    // backward: parts of the weights' gradients.  768 workgroups are all that fit at once ([B,L,D], 4 x 4096 x 6144 in bfloat16 144 us; 1536 153, 3840 174); the sequences of a packed time
+    // backward: parts of the weights' gradients.  768 workgroups are all that fit at once ([B,L,D], 4 x 4096 x 6144 in bfloat16, in a loop of its own, 144 us; 1536 153, 3840 174); the sequences of a packed time
     // axis are of all lengths, and more even each other out (24 sequences of 16384 steps, 2048 channels: 768 159 us, 1536 110, 2304 94, 3840 119; 400: 166, 141, 139, 157)
     int64_t most = (p.time_last && p.cu ? 2304 : 768) / groups;
     if (most < 1) most = 1;

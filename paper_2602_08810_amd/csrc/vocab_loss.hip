@@ -1,4 +1,4 @@
-// Softmax cross entropy over a vocabulary without its logits: z = h w^T, lse = log sum exp z, loss = lse - z[target], and
+// Softmax cross entropy over a vocabulary, logits formed a tile at a time: z = h w^T, lse = log sum exp z, loss = lse - z[target], and
 //     dz = dloss (exp(z - lse) - onehot(target)),   dh = dz w,   dw = dz^T h.
 // Forward: a tile of z stays in registers from its product to its largest number and sum, which is all that leaves it (8 bytes for 256 words and a row); a second
 // launch joins them.  Backward: z is formed again, a piece of the vocabulary at a time, dz of the piece goes to the workspace in bfloat16 and from there into both products.  What
@@ -7,8 +7,8 @@
 // give another word 0.95, 2.0e-3, and 3.8e-3 or 1.1e-2 where all words have a component in common of 3 or 10 times their own norm, which has to cancel in dh).  Rows without a target are left
 // out before the gradients' products: they cost nothing there and nothing in them, finite or not, reaches a gradient.
 // Float32 inputs: every factor is the sum of three bfloat16 numbers, a product six of theirs (terms of 2^-24 and below are left out), summed in float32.
-// Bound by the matrix units; with few rows, by the bytes of w.  8192 rows, 32768 words, 2048 elements in bfloat16: z 825 us (1330 TFLOP/s), dz 873, dh 815, dw 970 with half of the
-// rows' targets in one tile of words, else 830; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
+// Bound by the matrix units; with few rows, by the bytes of w.  8192 rows, 32768 words, 2048 elements in bfloat16: z 805 to 850 us (1290 to 1365 TFLOP/s), dz 875 to 930, dh 795 to 820, dw 970 to 1000 with half
+// of the rows' targets in one tile of words, else 860 to 890; a library's products of these sizes 1295 to 1540 TFLOP/s, nothing but the product.
 #include "vocab_loss.hpp"
 #include "conv_common.hpp"
 #include "lds_load.hpp"
@@ -163,7 +163,8 @@ template <class S, int ROWS, bool ALONG, bool WIDE = false> struct VocabOperand 
 
 struct VocabTile { int64_t m, n; };
 // The tiles of a product in the order in which they are taken.  Workgroups go to the eight dies in turn: a die takes a stretch of the tiles, four rows of tiles at
-// a time, so that what its 32 compute units read together (4 x 8 tiles) is in its cache: 32768 x 8192 with 2048 terms 1172 TFLOP/s, eight rows 1007.
+// a time, so that what its 32 compute units read together (4 x 8 tiles) is in its cache: 32768 x 8192 with 2048 terms 1172 TFLOP/s, eight rows 1007 (of an earlier kernel,
+// now 1330).
 template <class S> struct VocabTiles {
     unsigned mt, nt, total;
     __device__ __forceinline__ VocabTiles(int64_t m, int64_t n) : mt((unsigned)((m + S::M - 1) / S::M)), nt((unsigned)((n + S::N - 1) / S::N)), total(mt * nt) {}
@@ -205,7 +206,7 @@ template <class S, bool AA, bool BA> struct VocabFeed {
 
 // acc[i][j] += sum over the terms of a[16 i + ..] b[16 j + ..], for this wavefront's part of the tile; acc: column (n) lane % 16, rows (m) 4 (lane / 16) .. + 3.
 // Two stages of LDS; fragments are read half a stage ahead of the instructions that use them, and a stage's memory is filled again as soon as its second half
-// is in registers, two halves before it is read: one barrier a stage.  z of 8192 x 32768, 2048 terms: 1270 to 1310 TFLOP/s, dh 1310 to 1345.  Reads at the end of a half, where the compiler puts them if
+// is in registers, two halves before it is read: one barrier a stage.  z of 8192 x 32768, 2048 terms: 1290 to 1365 TFLOP/s, dh 1340 to 1385.  Before other changes here: reads at the end of a half, where the compiler puts them if
 // left to itself: z 50 us of 980 slower; four stages of 32 terms, a barrier each: z 987 for 903, dh 863 for 828 (half as long rows a load); and so that half of the wavefronts
 // read while the others multiply, two barriers each: 1070 and 900.  With four wavefronts of 128 x 128 a third fewer reads, but 256 sums and two sets of fragments do not fit the registers.
 template <class S, bool AA, bool BA, int KIND = S::WIDE ? 0 : S::PLANES> struct VocabPipe {
